@@ -317,10 +317,10 @@ def _softmax(s):
     """exp of the shifted rows, their sums, and the tokens' log-probabilities."""
     x = s.logits.float()
     if s.case["temperature"] != 1.0:
-        x /= s.case["temperature"]
+        x = x / s.case["temperature"]
     at = s.chosen.long().unsqueeze(1)
     top = x.amax(dim=1, keepdim=True)
-    x -= top
+    x = x - top  # (logits in single precision stay as they are)
     chosen = x.gather(1, at)
     e = x.exp_()
     total = e.sum(dim=1, keepdim=True)
