@@ -464,6 +464,121 @@ typedef struct {
 pr_status pr_selective_metrics(pr_ctx* ctx, const float* scores, const uint8_t* labels, int64_t n,
                                double q, pr_selective* out, void* stream);
 
+/* ---- training losses over logit rows -------------------------------------------------- */
+
+/*
+ * The verifier's outcome is a training signal for the small model: a graded
+ * response gives its tokens an advantage, an escalated request a pair of
+ * answers, the large model's above the small model's.  (The paper trains the
+ * scorer only; these calls train the model whose logits it reads.)
+ *
+ * Common to both losses
+ *   - row t's log-probability is l_t = z_{y_t} - log sum_v exp(z_v) with z = x_t / T
+ *     (y_t = chosen[t], T = temperature > 0).  Logits as in pr_token_features.
+ *   - mask: device uint8 [n_rows] or NULL (every row counts).  A row with mask 0,
+ *     or one that no request owns, does not count: its logits are not used,
+ *     whatever they hold, its logp is 0 and its gradient row zero.
+ *   - offsets: device int64 [n_req + 1], non-decreasing, rows [offsets[r],
+ *     offsets[r + 1]) are request r's.  A request that reaches outside [0, n_rows]
+ *     or has a negative length counts no rows and raises PR_FLAG_BAD_OFFSETS, an
+ *     empty one PR_FLAG_EMPTY_REQ (context flag word).
+ *   - a counted row with NaN or +inf, or with nothing finite, has logp NaN
+ *     (PR_FLAG_NONFINITE), one with an id outside the vocabulary too
+ *     (PR_FLAG_BAD_CHOSEN); as the formulas say, its gradient row and the
+ *     statistics that it enters are then NaN.  -inf is a masked token (p = 0,
+ *     gradient 0); the type's lowest finite value is a logit like any other.
+ *   - grad: device [n_rows][grad_stride] elements of the logits' type, or NULL
+ *     (loss only).  d (grad_scale * loss) / d x, rounded once; columns from vocab
+ *     on are left as they are.  grad may be the logits' own buffer with the same
+ *     stride; otherwise the two must not overlap.  Written fastest where a
+ *     row of grad and its logits have the same address modulo 16.
+ *   - stats: device float [PR_NPOL / PR_NPREF]; logp: device float [n_rows].
+ *     Statistics are summed in fp64 in an order that depends on the sizes alone:
+ *     results are bit-reproducible.
+ *   - the context holds a workspace (16 bytes per row, 28 per request), allocated
+ *     or grown by the first call that needs more -- that call synchronises the
+ *     device; calls on different streams must not overlap (they share it).
+ */
+#define PR_NORM_TOKENS 0   /* mean over all counted rows */
+#define PR_NORM_REQUESTS 1 /* mean over the requests with counted rows of the mean over those */
+
+#define PR_NPOL 6
+#define PR_POL_LOSS 0      /* the loss */
+#define PR_POL_SURROGATE 1 /* mean of min(r A, clip(r) A) */
+#define PR_POL_KL 2        /* mean of the KL term (0 without ref_logp) */
+#define PR_POL_RATIO 3     /* mean of r */
+#define PR_POL_CLIPPED 4   /* share of the rows whose clipped term is the smaller one */
+#define PR_POL_OLD_KL 5    /* mean of r - 1 - log r */
+
+typedef struct {
+  float clip_low, clip_high; /* r is clipped to [1 - clip_low, 1 + clip_high]; clip_low <= 1 */
+  float kl_coef;             /* beta >= 0 */
+  float temperature;         /* T, 1e-30 .. 1e30 */
+  float grad_scale;          /* finite */
+  int32_t norm;              /* PR_NORM_* */
+  int32_t adv_per_request;   /* 0: one advantage per row, else one per request */
+} pr_policy;
+
+/*
+ * Clipped policy loss with a KL term, and its gradient:
+ *   r = exp(l - old), loss_t = -min(r A, clip(r) A) + beta (exp(ref - l) - (ref - l) - 1),
+ *   loss = the mean of loss_t as norm says (0 when no row counts);
+ *   d loss_t / d l = -r A (0 where the clipped term is strictly the smaller one)
+ *                    + beta (1 - exp(ref - l)).
+ *   old_logp   device float [n_rows], log-probabilities under the policy that
+ *              sampled, or NULL: this one (r = 1)
+ *   ref_logp   device float [n_rows] under the reference model, or NULL (no KL term)
+ *   advantage  device float [n_rows], or [n_req] with adv_per_request
+ *   offsets    may be NULL (n_req 0) with PR_NORM_TOKENS or for one request of
+ *              all rows, with an advantage per row
+ * n_rows < 2^31.
+ */
+pr_status pr_policy_loss(pr_ctx* ctx, const void* logits, pr_dtype dt, int64_t n_rows,
+                         int64_t vocab, int64_t row_stride, const int32_t* chosen,
+                         const uint8_t* mask, const int64_t* offsets, int32_t n_req,
+                         const float* old_logp, const float* ref_logp, const float* advantage,
+                         const pr_policy* params, float* stats, float* logp, void* grad,
+                         int64_t grad_stride, void* stream);
+
+#define PR_PREF_SIGMOID 0 /* -(1 - e) log sigmoid(h) - e log sigmoid(-h) */
+#define PR_PREF_SQUARED 1 /* (d - 1 / (2 beta))^2 */
+#define PR_PREF_HINGE 2   /* max(0, 1 - h) */
+
+#define PR_NPREF 5
+#define PR_PREF_LOSS 0     /* the loss */
+#define PR_PREF_ACCURACY 1 /* share of pairs with d > 0 */
+#define PR_PREF_H 2        /* mean of h */
+#define PR_PREF_REWARD_W 3 /* mean of beta s over the preferred answers */
+#define PR_PREF_REWARD_L 4 /* mean of beta s over the others */
+
+typedef struct {
+  float beta;            /* > 0 */
+  float label_smoothing; /* e in [0, 1], PR_PREF_SIGMOID only */
+  float margin;          /* finite; 0 for PR_PREF_SQUARED */
+  float temperature;     /* T, 1e-30 .. 1e30 */
+  float grad_scale;      /* finite */
+  int32_t loss;          /* PR_PREF_* */
+  int32_t length_norm;   /* 0: an answer's log ratio is a sum, else a mean over its counted rows */
+} pr_preference;
+
+/*
+ * Loss of paired log ratios, and its gradient.  Requests 2i and 2i + 1 are one
+ * pair: the preferred answer and the other one.
+ *   s_r = sum over request r's counted rows of (l_t - ref_t), or their mean;
+ *   d = s_2i - s_2i+1, h = beta d - margin; loss: mean over the pairs of which
+ *   both answers have counted rows (0 when there is none; the other pairs have
+ *   no gradient).
+ *   ref_logp   device float [n_rows] under the reference model, or NULL (0)
+ *   ratio      device float [n_req]: the s_r                    (output)
+ * n_rows < 2^31, n_req even and >= 2.
+ */
+pr_status pr_preference_loss(pr_ctx* ctx, const void* logits, pr_dtype dt, int64_t n_rows,
+                             int64_t vocab, int64_t row_stride, const int32_t* chosen,
+                             const uint8_t* mask, const int64_t* offsets, int32_t n_req,
+                             const float* ref_logp, const pr_preference* params, float* stats,
+                             float* ratio, float* logp, void* grad, int64_t grad_stride,
+                             void* stream);
+
 /* ---- verification without allocation ------------------------------------------------- */
 
 #define PR_NOALLOC_MAX_ROWS 16384    /* largest n_rows pr_route_noalloc accepts */

@@ -1,0 +1,126 @@
+"""Float64 oracle of the training losses and of the optimiser step (numpy, host
+only; shares nothing with the library's kernels).
+
+A token's log-probability is l = z_y - log sum exp(z), z = x / T.  A loss that
+depends on the logits through l alone has d loss / d x_v = (d loss / d l)
+(onehot_y(v) - p_v) / T.
+"""
+from __future__ import annotations
+
+import numpy as np
+
+SIGMOID, SQUARED, HINGE = 0, 1, 2
+
+
+def rows(x, chosen, temperature=1.0):
+    """(l [n], p [n][V]) of logit rows; a row with NaN or +inf, or without a
+    finite logit, and one whose token is outside the vocabulary has l = NaN."""
+    x = np.asarray(x, np.float64)
+    chosen = np.asarray(chosen, np.int64)
+    n, V = x.shape
+    l, p = np.full(n, np.nan), np.full((n, V), np.nan)
+    for t in range(n):
+        if np.isnan(x[t]).any() or not np.isfinite(x[t].max()):
+            continue
+        z = (x[t] - x[t].max()) / temperature
+        e = np.exp(z)
+        p[t] = e / e.sum()
+        if 0 <= chosen[t] < V:
+            l[t] = z[chosen[t]] - np.log(e.sum())
+    return l, p
+
+
+def counted(n, mask, offsets):
+    """(request of each row, -1 where the row does not count; counted rows of
+    each request).  Without offsets all rows are request 0."""
+    req = np.full(n, -1, np.int64)
+    off = [0, n] if offsets is None else [int(v) for v in offsets]
+    for r, (a, b) in enumerate(zip(off[:-1], off[1:])):
+        if a < 0 or b < a or b > n:
+            continue
+        for t in range(a, b):
+            if mask is None or mask[t]:
+                req[t] = r
+    count = np.array([(req == r).sum() for r in range(len(off) - 1)], np.int64)
+    return req, count
+
+
+def _grad(p, chosen, slope, req, temperature, grad_scale):
+    n, V = p.shape
+    g = np.zeros((n, V))
+    for t in range(n):
+        if req[t] < 0:
+            continue
+        one = np.zeros(V)
+        if 0 <= chosen[t] < V:
+            one[chosen[t]] = 1.0
+        g[t] = slope[t] * (one - p[t]) * (grad_scale / temperature)
+    return g
+
+
+def policy(x, chosen, advantage, old_logp=None, ref_logp=None, mask=None, offsets=None,
+           clip_low=0.2, clip_high=0.2, kl_coef=0.0, temperature=1.0, requests=False,
+           per_request=False, grad_scale=1.0):
+    """(statistics [6], logp [n], gradient [n][V]) of the clipped policy loss."""
+    n = len(chosen)
+    l, p = rows(x, chosen, temperature)
+    req, count = counted(n, mask, offsets)
+    stats, slope = np.zeros(6), np.zeros(n)
+    for t in range(n):
+        if req[t] < 0:
+            continue
+        w = (1.0 / ((count > 0).sum() * count[req[t]])) if requests else 1.0 / count.sum()
+        A = float(advantage[req[t]] if per_request else advantage[t])
+        d = 0.0 * l[t] if old_logp is None else l[t] - float(old_logp[t])
+        r = np.exp(d)
+        free, cut = r * A, min(max(r, 1.0 - clip_low), 1.0 + clip_high) * A
+        if np.isnan(r):
+            cut = r
+        clipped = cut < free
+        surrogate = cut if clipped else free
+        kl = 0.0
+        slope[t] = w * (0.0 if clipped else -free)
+        if ref_logp is not None:
+            q = float(ref_logp[t]) - l[t]
+            kl = np.expm1(q) - q
+            if kl_coef != 0.0:
+                slope[t] += w * kl_coef * -np.expm1(q)
+        stats += w * np.array([-surrogate + kl_coef * kl, surrogate, kl, r, float(clipped),
+                               np.expm1(d) - d])
+    logp = np.where(req >= 0, l, 0.0)
+    return stats, logp, _grad(p, chosen, slope, req, temperature, grad_scale)
+
+
+def preference(x, chosen, offsets, ref_logp=None, mask=None, beta=0.1, loss=SIGMOID,
+               label_smoothing=0.0, margin=0.0, length_norm=False, temperature=1.0,
+               grad_scale=1.0):
+    """(statistics [5], log ratios [n_req], logp [n], gradient [n][V]) of the
+    loss of paired log ratios, requests 2i preferred over 2i + 1."""
+    n = len(chosen)
+    l, p = rows(x, chosen, temperature)
+    req, count = counted(n, mask, offsets)
+    s = np.zeros(len(count))
+    for t in range(n):
+        if req[t] >= 0:
+            s[req[t]] += l[t] - (0.0 if ref_logp is None else float(ref_logp[t]))
+    if length_norm:
+        s = s / np.maximum(count, 1)
+    pairs = [i for i in range(0, len(count), 2) if count[i] > 0 and count[i + 1] > 0]
+    stats, side = np.zeros(5), np.zeros(len(count))
+    for i in pairs:
+        d = s[i] - s[i + 1]
+        h = beta * d - margin
+        if loss == SIGMOID:
+            f = (1 - label_smoothing) * np.logaddexp(0, -h) + label_smoothing * np.logaddexp(0, h)
+            slope = beta * (label_smoothing * np.exp(-np.logaddexp(0, -h))
+                            - (1 - label_smoothing) * np.exp(-np.logaddexp(0, h)))
+        elif loss == SQUARED:
+            f, slope = (d - 0.5 / beta) ** 2, 2 * (d - 0.5 / beta)
+        else:
+            f, slope = (h if np.isnan(h) else max(0.0, 1 - h)), (-beta if h < 1 else 0.0 * h)
+        stats += np.array([f, float(d > 0), h, beta * s[i], beta * s[i + 1]]) / len(pairs)
+        for r, sign in ((i, 1.0), (i + 1, -1.0)):
+            side[r] = sign * slope / len(pairs) / (count[r] if length_norm else 1)
+    slope = np.where(req >= 0, side[np.maximum(req, 0)], 0.0)
+    logp = np.where(req >= 0, l, 0.0)
+    return stats, s, logp, _grad(p, chosen, slope, req, temperature, grad_scale)

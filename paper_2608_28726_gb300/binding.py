@@ -25,6 +25,9 @@ PR_NOALLOC_MAX_ROWS, PR_NOALLOC_MAX_REQUESTS = 16384, 1024
 PR_HEAD_D, PR_HEAD_HEADS, PR_HEAD_FF, PR_HEAD_MAX_LAYERS = 64, 4, 128, 8
 PR_QMLP_SUMMARY, PR_QMLP_PARAMS = 28, 6081
 PR_LMHEAD_MAX_VOCAB = (1 << 31) - 256
+PR_NORM_TOKENS, PR_NORM_REQUESTS = 0, 1
+PR_PREF_SIGMOID, PR_PREF_SQUARED, PR_PREF_HINGE = 0, 1, 2
+PR_NPOL, PR_NPREF = 6, 5
 
 # every symbol include/pro_router.h declares
 EXPORTS = (
@@ -35,7 +38,7 @@ EXPORTS = (
     "pr_ctx_kernel_times", "pr_selective_metrics", "pr_quantile_score", "pr_lmhead_features",
     "pr_selftest_wait", "pr_lmhead_decode_step", "pr_last_error", "pr_prescorer_fit",
     "pr_prescorer_destroy", "pr_prescorer_vocab_size", "pr_prescorer_term",
-    "pr_prescorer_features", "pr_prescorer_score",
+    "pr_prescorer_features", "pr_prescorer_score", "pr_policy_loss", "pr_preference_loss",
 )
 
 if not os.path.exists(LIB):
@@ -76,6 +79,10 @@ _SIGS = {
     "pr_prescorer_features": [_P, ctypes.c_char_p, _I32, _P, _P, ctypes.POINTER(_I32),
                               ctypes.POINTER(_I64)],
     "pr_prescorer_score": [_P, _P, _P, _I32, _P, _F32, _I32, _P, _P],
+    "pr_policy_loss": [_P, _P, ctypes.c_int, _I64, _I64, _I64, _P, _P, _P, _I32, _P, _P, _P, _P, _P,
+                       _P, _P, _I64, _P],
+    "pr_preference_loss": [_P, _P, ctypes.c_int, _I64, _I64, _I64, _P, _P, _P, _I32, _P, _P, _P, _P,
+                           _P, _P, _I64, _P],
 }
 for _name, _args in _SIGS.items():
     _fn = getattr(_lib, _name)
@@ -597,6 +604,109 @@ def pr_selftest_wait(ctx, limit_ns: int) -> bool:
     done = _I32(-1)
     _check(_lib.pr_selftest_wait(ctx, int(limit_ns), ctypes.byref(done)), "pr_selftest_wait")
     return done.value == 1
+
+
+# ---- training losses over logit rows ----------------------------------------------------------
+
+class PrPolicy(ctypes.Structure):
+    _fields_ = [("clip_low", _F32), ("clip_high", _F32), ("kl_coef", _F32),
+                ("temperature", _F32), ("grad_scale", _F32), ("norm", _I32),
+                ("adv_per_request", _I32)]
+
+
+class PrPreference(ctypes.Structure):
+    _fields_ = [("beta", _F32), ("label_smoothing", _F32), ("margin", _F32),
+                ("temperature", _F32), ("grad_scale", _F32), ("loss", _I32),
+                ("length_norm", _I32)]
+
+
+def _loss_outputs(call, dev, logits, n, V, stride, n_stats, stats, logp, grad, want_grad):
+    """The loss calls' outputs, made where the caller has none, and the stride
+    of the gradient's rows."""
+    if stats is None or logp is None or (grad is None and want_grad):
+        d = logits.device
+        stats = torch.empty(n_stats, dtype=torch.float32, device=d) if stats is None else stats
+        logp = torch.empty(n, dtype=torch.float32, device=d) if logp is None else logp
+        if grad is None and want_grad:
+            # rows at the same addresses modulo 16 as the logits'
+            pad = (stride - V) % (16 // logits.element_size())
+            grad = torch.empty(n, V + pad, dtype=logits.dtype, device=d)[:, :V]
+    _dev(call, dev, "stats", stats, _F32_T, n_stats)
+    _dev(call, dev, "logp", logp, _F32_T, n)
+    if grad is None:
+        return stats, logp, None, 0
+    _dev(call, dev, "grad", grad, (logits.dtype,), contiguous=False)
+    if grad.dim() != 2 or grad.size(0) < n or grad.size(1) < V or (grad.size(1) > 1
+                                                                    and grad.stride(1) != 1):
+        raise PRError(PR_ERR_INVALID_ARG, call,
+                      "grad must be 2-D with unit stride along the vocabulary, [%d][%d]" % (n, V))
+    return stats, logp, grad, max(grad.stride(0) if grad.size(0) > 1 else V, V)
+
+
+def pr_policy_loss(ctx, logits, chosen, advantage, old_logp=None, ref_logp=None, mask=None,
+                   offsets=None, clip_low: float = 0.2, clip_high: float = 0.2,
+                   kl_coef: float = 0.0, temperature: float = 1.0, norm: int = PR_NORM_TOKENS,
+                   per_request: bool = False, grad_scale: float = 1.0, stats=None, logp=None,
+                   grad=None, want_grad: bool = True, vocab=None, stream=None):
+    """Clipped policy loss with a KL term over logit rows: (stats float32
+    [PR_NPOL], logp float32 [n], gradient of the logits or None).  `advantage`
+    has one value per row, or with `per_request` one per request; `grad` may be
+    `logits` itself."""
+    call = "pr_policy_loss"
+    dev = _ctx_device(ctx)
+    _logits(call, dev, logits)
+    n = logits.size(0)
+    V, stride = _rows(logits, vocab)
+    dt = _dtype(logits)
+    n_req = 0 if offsets is None else offsets.numel() - 1
+    _dev(call, dev, "chosen", chosen, _I32_T, n)
+    _dev(call, dev, "advantage", advantage, _F32_T, n_req if per_request else n)
+    _dev(call, dev, "old_logp", old_logp, _F32_T, n, optional=True)
+    _dev(call, dev, "ref_logp", ref_logp, _F32_T, n, optional=True)
+    _dev(call, dev, "mask", mask, _U8_T, n, optional=True)
+    _dev(call, dev, "offsets", offsets, _I64_T, optional=True)
+    stats, logp, grad, gs = _loss_outputs(call, dev, logits, n, V, stride, PR_NPOL, stats, logp,
+                                          grad, want_grad)
+    p = PrPolicy(clip_low, clip_high, kl_coef, temperature, grad_scale, int(norm),
+                 int(bool(per_request)))
+    _check(_lib.pr_policy_loss(ctx, logits.data_ptr(), dt, n, V, stride, _ptr(chosen), _ptr(mask),
+                               _ptr(offsets), n_req, _ptr(old_logp), _ptr(ref_logp),
+                               _ptr(advantage), ctypes.byref(p), _ptr(stats), _ptr(logp),
+                               _ptr(grad), gs, _stream(stream)), call)
+    return stats, logp, grad
+
+
+def pr_preference_loss(ctx, logits, chosen, offsets, ref_logp=None, mask=None, beta: float = 0.1,
+                       loss: int = PR_PREF_SIGMOID, label_smoothing: float = 0.0,
+                       margin: float = 0.0, length_norm: bool = False, temperature: float = 1.0,
+                       grad_scale: float = 1.0, stats=None, ratio=None, logp=None, grad=None,
+                       want_grad: bool = True, vocab=None, stream=None):
+    """Loss of paired log ratios over logit rows, requests 2i preferred over
+    2i + 1: (stats float32 [PR_NPREF], log ratios float32 [n_req], logp float32
+    [n], gradient of the logits or None).  `grad` may be `logits` itself."""
+    call = "pr_preference_loss"
+    dev = _ctx_device(ctx)
+    _logits(call, dev, logits)
+    n = logits.size(0)
+    V, stride = _rows(logits, vocab)
+    dt = _dtype(logits)
+    _dev(call, dev, "offsets", offsets, _I64_T, 3)
+    n_req = offsets.numel() - 1
+    _dev(call, dev, "chosen", chosen, _I32_T, n)
+    _dev(call, dev, "ref_logp", ref_logp, _F32_T, n, optional=True)
+    _dev(call, dev, "mask", mask, _U8_T, n, optional=True)
+    if ratio is None:
+        ratio = torch.empty(n_req, dtype=torch.float32, device=logits.device)
+    _dev(call, dev, "ratio", ratio, _F32_T, n_req)
+    stats, logp, grad, gs = _loss_outputs(call, dev, logits, n, V, stride, PR_NPREF, stats, logp,
+                                          grad, want_grad)
+    p = PrPreference(beta, label_smoothing, margin, temperature, grad_scale, int(loss),
+                     int(bool(length_norm)))
+    _check(_lib.pr_preference_loss(ctx, logits.data_ptr(), dt, n, V, stride, _ptr(chosen),
+                                   _ptr(mask), _ptr(offsets), n_req, _ptr(ref_logp),
+                                   ctypes.byref(p), _ptr(stats), _ptr(ratio), _ptr(logp),
+                                   _ptr(grad), gs, _stream(stream)), call)
+    return stats, ratio, logp, grad
 
 
 # ---- the prompt pre-scorer (host CPU; Section 3.1, Eq. 2) ---------------------------------

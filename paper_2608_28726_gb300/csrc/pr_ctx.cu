@@ -152,6 +152,7 @@ pr_status pr_ctx_destroy(pr_ctx* c) {
   cudaFree(c->head_scr);
   cudaFree(c->sel_ws);
   cudaFree(c->lm_parts);
+  cudaFree(c->loss_ws);
   for (cudaEvent_t e : c->tev)
     if (e) cudaEventDestroy(e);
   if (c->copy_stream) cudaStreamDestroy(c->copy_stream);

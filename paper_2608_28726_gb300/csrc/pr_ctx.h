@@ -61,6 +61,9 @@ struct pr_ctx {
   size_t lm_parts_bytes = 0;
   bool lm_ready = false;
   bool qmlp_ready = false;  // pr_quantile_score: shared memory opt-in made
+  // the training losses: workspace, grown on demand
+  void* loss_ws = nullptr;
+  size_t loss_ws_bytes = 0;
   // PR_OPT_TIMING: events after each kernel of the last multi-kernel call
   int32_t timing = 0;
   cudaEvent_t tev[PR_MAX_TIMED + 1] = {};

@@ -1,0 +1,458 @@
+"""GPU parity of the training losses (pr_policy_loss, pr_preference_loss) with
+the float64 oracle, at the sizes, masks and values where they can go wrong.
+
+Tolerances, from the kernels' arithmetic (2^-24 = 6e-8 per fp32 rounding):
+  logp   a row's sum of exponentials is a sum of positive fp32 terms, each off by
+         2^-22 and by |z - max| 2^-23 (weighted by the term itself: below 1e-6), in
+         chains of up to 500 terms (3e-5 at worst, the roundings' mean far less):
+         2e-5; the two roundings of z_y - max and of the difference: 4e-7 |l|
+  grad   dL/dl carries logp's error through an exponential and a few products: 1e-4
+         relative; p the exponent's error of |z - max| 2^-23 and logp's: 6e-5 relative.
+         Together 2e-4 |g|, and 1e-6 of the row's largest entry for those that cancel;
+         bf16 (eight significant bits) adds half a unit in the last place, 2^-8
+  stats  weighted means of the terms, whose size `scale` gives: 1e-4 of it
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import loss as L
+
+pytestmark = pytest.mark.gpu
+CLIP = dict(clip_low=0.2, clip_high=0.3)
+
+
+@pytest.fixture(scope="module")
+def B():
+    from paper_2608_28726_gb300 import build as prbuild
+    prbuild.build()
+    from paper_2608_28726_gb300 import binding
+    return binding
+
+
+@pytest.fixture(scope="module")
+def ctx(B):
+    c = B.pr_ctx_create(0, 1, 1)
+    yield c
+    B.pr_ctx_destroy(c)
+
+
+def to(a, dtype=None):
+    return None if a is None else torch.from_numpy(np.ascontiguousarray(a, dtype)).cuda()
+
+
+def draw(seed, n, V, dtype, scale=3.0, temperature=1.0):
+    """(logits as the GPU holds them, their float64 values, chosen, old, ref):
+    ratios kept off the clip bounds, where the slope jumps."""
+    g = np.random.Generator(np.random.PCG64(seed))
+    x = torch.from_numpy((scale * g.normal(size=(n, V))).astype(np.float32))
+    x[torch.arange(n), torch.from_numpy(g.integers(0, V, n))] += 6.0
+    x = x.to(torch.bfloat16 if dtype == "bf16" else torch.float32)
+    x64 = x.double().numpy()
+    ch = np.where(g.random(n) < 0.5, x64.argmax(1), g.integers(0, V, n)).astype(np.int32)
+    l, _ = L.rows(x64, ch, temperature)
+    d = 0.3 * g.normal(size=n)
+    for edge in (np.log(0.8), np.log(1.3)):
+        d = np.where(np.abs(d - edge) < 2e-3, edge + 4e-3, d)
+    old = (l - d).astype(np.float32)
+    ref = (l + 0.3 * g.normal(size=n)).astype(np.float32)
+    return g, x.cuda(), x64, ch, old, ref
+
+
+def check_rows(got, logp, want, grad, dtype, what=""):
+    l = got.double().cpu().numpy()
+    bad = ~((np.abs(l - logp) <= 2e-5 + 4e-7 * np.abs(logp)) | (np.isnan(l) & np.isnan(logp))
+            | (l == logp))
+    assert not bad.any(), "%s logp %s: %s for %s" % (what, np.flatnonzero(bad)[:5], l[bad][:5],
+                                                    logp[bad][:5])
+    if want is None:
+        return
+    w = want.double().cpu().numpy()
+    rel = 2e-4 + (2.0 ** -8 if dtype == "bf16" else 0.0)
+    with np.errstate(invalid="ignore"):
+        big = np.abs(grad).max(axis=1, keepdims=True)
+        ok = (np.abs(w - grad) <= rel * np.abs(grad) + 1e-6 * big) | (np.isnan(w) & np.isnan(grad))
+    assert ok.all(), "%s grad: %d of %d, at %s: %s for %s" % (
+        what, (~ok).sum(), ok.size, np.argwhere(~ok)[:4].tolist(), w[~ok][:4], grad[~ok][:4])
+
+
+def check_stats(got, want, scale):
+    s = got.double().cpu().numpy()
+    ok = (np.abs(s - want) <= 1e-4 * np.maximum(scale, np.abs(want))) | (np.isnan(s) & np.isnan(want))
+    assert ok.all(), (s, want)
+
+
+def offsets_of(g, n, n_req):
+    cut = np.sort(g.integers(0, n + 1, n_req - 1)) if n_req > 1 else np.zeros(0, np.int64)
+    return np.r_[0, cut, n].astype(np.int64)
+
+
+SIZES = [(1, 1), (3, 2), (5, 7), (5, 8), (4, 9), (7, 31), (9, 33), (6, 255), (3, 1000), (37, 1001),
+         (200, 515), (2, 4096), (3, 8191), (3, 16384), (5, 32000), (2, 32003), (170, 2050),
+         (2, 70001), (3, 151936), (2, 262144), (1, 300007)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,V", SIZES)
+def test_policy_sizes(B, ctx, n, V, dtype):
+    T = 1.0 if V % 2 else 0.8
+    g, x, x64, ch, old, ref = draw(V * 7 + n, n, V, dtype, temperature=T)
+    n_req = min(n, 5)
+    off = offsets_of(g, n, n_req)
+    mask = (g.random(n) < 0.8).astype(np.uint8)
+    per = bool(V % 3)
+    adv = g.normal(size=n_req if per else n).astype(np.float32)
+    norm = n % 2
+    kw = dict(kl_coef=0.05, temperature=T, per_request=per, grad_scale=1.5, **CLIP)
+    stats, logp, grad = B.pr_policy_loss(ctx, x, to(ch), to(adv), old_logp=to(old), ref_logp=to(ref),
+                                         mask=to(mask), offsets=to(off), norm=norm, **kw)
+    s, l, gr = L.policy(x64, ch, adv, old, ref, mask, off, requests=bool(norm), **kw)
+    check_rows(logp, l, grad, gr, dtype)
+    check_stats(stats, s, 2.0 * (mask.any() or 0))
+    # the loss alone gives the same bits
+    st2, lp2, none = B.pr_policy_loss(ctx, x, to(ch), to(adv), old_logp=to(old), ref_logp=to(ref),
+                                      mask=to(mask), offsets=to(off), norm=norm, want_grad=False, **kw)
+    assert none is None and torch.equal(lp2, logp) and torch.equal(st2, stats)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,V", SIZES)
+def test_preference_sizes(B, ctx, n, V, dtype):
+    T = 0.9 if V % 2 else 1.0
+    g, x, x64, ch, _, ref = draw(V * 5 + n, n, V, dtype, temperature=T)
+    n_req = 2 * min(max(n // 2, 1), 6)
+    off = offsets_of(g, n, n_req)
+    mask = (g.random(n) < 0.85).astype(np.uint8)
+    kind = n % 3
+    kw = dict(loss=kind, beta=0.2, label_smoothing=0.1 if kind == 0 else 0.0,
+              margin=0.25 if kind != 1 else 0.0, length_norm=bool(V % 2), temperature=T)
+    stats, ratio, logp, grad = B.pr_preference_loss(ctx, x, to(ch), to(off), ref_logp=to(ref),
+                                                    mask=to(mask), **kw)
+    s, r, l, gr = L.preference(x64, ch, off, ref, mask, **kw)
+    check_rows(logp, l, grad, gr, dtype)
+    # a sum of a request's rows, each off by logp's error
+    lim = 2e-5 * np.maximum(np.diff(off), 1) + 1e-6 * np.abs(r) * (1 if kw["length_norm"] else 1)
+    assert (np.abs(ratio.double().cpu().numpy() - r) <= lim + 1e-6).all()
+    check_stats(stats, s, 0.2 * np.abs(r).max() + 1.0 + (3.0 * np.abs(r).max() + 25.0) * (kind == 1))
+    st2, r2, lp2, _ = B.pr_preference_loss(ctx, x, to(ch), to(off), ref_logp=to(ref),
+                                           mask=to(mask), want_grad=False, **kw)
+    assert torch.equal(lp2, logp) and torch.equal(st2, stats) and torch.equal(r2, ratio)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V", [40, 1003, 40000])
+def test_values_that_a_softmax_can_trip_over(B, ctx, V, dtype):
+    """Masked tokens, the type's lowest value, large logits, NaN and infinities, in
+    counted and in masked rows."""
+    n = 16
+    g, x, x64, ch, old, ref = draw(V, n, V, dtype)
+    low = torch.finfo(x.dtype).min
+    mask = np.ones(n, np.uint8)
+    x[0, : V // 2] = -torch.inf
+    x[1] = -torch.inf                 # nothing left
+    x[2] = low                        # a uniform row of the lowest value
+    x[3, 1:] = low                    # one token left
+    x[4, 3] = torch.nan
+    x[5, V - 1] = torch.inf
+    x[6] = 3e4 + x[6]                 # large logits
+    x[7] = torch.where(torch.arange(V, device="cuda") % 3 == 0, 3e38, -3e38).to(x.dtype)
+    x[8], x[9], x[10] = torch.nan, torch.inf, -torch.inf  # masked rows
+    mask[8:11] = 0
+    x[11, : V - 1] = -torch.inf       # the last element alone
+    x[12, 1:] = -torch.inf            # the first alone
+    x[13, ::2] = -torch.inf
+    ch[0], ch[3], ch[7], ch[11], ch[12], ch[13] = V - 1, 0, 3, V - 1, 0, 1
+    ch[8] = -7                        # masked: not looked at
+    ch[14], ch[15] = V, -1            # outside the vocabulary
+    x64 = x.double().cpu().numpy()
+    l, _ = L.rows(x64, ch)
+    old = np.where(np.isfinite(l), l - 0.1, 0.0).astype(np.float32)
+    ref = np.where(np.isfinite(l), l + 0.2, 0.0).astype(np.float32)
+    adv = g.normal(size=n).astype(np.float32)
+    B.pr_ctx_flags(ctx, clear=True)
+    stats, logp, grad = B.pr_policy_loss(ctx, x, to(ch), to(adv), old_logp=to(old), ref_logp=to(ref),
+                                         mask=to(mask), kl_coef=0.1, **CLIP)
+    assert B.pr_ctx_flags(ctx, clear=True) == B.PR_FLAG_NONFINITE | B.PR_FLAG_BAD_CHOSEN
+    s, lo, gr = L.policy(x64, ch, adv, old, ref, mask, kl_coef=0.1, **CLIP)
+    assert np.isnan(lo[[1, 4, 5, 14, 15]]).all() and np.isfinite(lo[[0, 2, 3, 6, 7, 11, 12, 13]]).all()
+    check_rows(logp, lo, grad, gr, dtype)
+    check_stats(stats, s, 1.0)
+    assert not grad[8:11].any()
+    # without the rows that are NaN by right, everything is finite
+    mask[[1, 4, 5, 14, 15]] = 0
+    for off in ([0, 16], [0, 4, 9, 16]):
+        stats, logp, grad = B.pr_policy_loss(ctx, x, to(ch), to(adv), old_logp=to(old),
+                                             ref_logp=to(ref), mask=to(mask), kl_coef=0.1,
+                                             offsets=to(off, np.int64), **CLIP)
+        s, lo, gr = L.policy(x64, ch, adv, old, ref, mask, off, kl_coef=0.1, **CLIP)
+        assert np.isfinite(s).all() and torch.isfinite(grad).all()
+        check_rows(logp, lo, grad, gr, dtype)
+        check_stats(stats, s, 1.0)
+    off = [0, 4, 9, 12, 16]
+    st, r, logp, grad = B.pr_preference_loss(ctx, x, to(ch), to(off, np.int64), ref_logp=to(ref),
+                                             mask=to(mask))
+    s, ro, lo, gr = L.preference(x64, ch, off, ref, mask)
+    check_rows(logp, lo, grad, gr, dtype)
+    check_stats(st, s, 1.0)
+    assert B.pr_ctx_flags(ctx, clear=True) == 0
+
+
+def test_a_nan_pair_leaves_the_others_gradients(B, ctx):
+    g, x, _, ch, _, ref = draw(5, 12, 700, "f32")
+    x[1, 17] = torch.nan
+    off = np.array([0, 3, 6, 9, 12], np.int64)
+    st, r, logp, grad = B.pr_preference_loss(ctx, x, to(ch), to(off), ref_logp=to(ref))
+    s, ro, lo, gr = L.preference(x.double().cpu().numpy(), ch, off, ref)
+    assert torch.isnan(st[[0, 2, 3]]).all() and torch.isnan(grad[:6]).all()
+    check_rows(logp, lo, grad, gr, "f32")
+    B.pr_ctx_flags(ctx, clear=True)
+
+
+def test_batches_without_a_counted_row(B, ctx):
+    g, x, x64, ch, old, ref = draw(1, 6, 300, "bf16")
+    mask = to(np.zeros(6, np.uint8))
+    for norm in (0, 1):
+        st, lp, gr = B.pr_policy_loss(ctx, x, to(ch), to(old), mask=mask, norm=norm,
+                                      offsets=to([0, 2, 2, 6], np.int64))
+        assert not st.any() and not lp.any() and not gr.any()
+    st, r, lp, gr = B.pr_preference_loss(ctx, x, to(ch), to([0, 3, 6], np.int64), mask=mask)
+    assert not st.any() and not r.any() and not lp.any() and not gr.any()
+    # an answer without rows: its pair says nothing, the other one all
+    off = np.array([0, 0, 2, 4, 6], np.int64)
+    st, r, lp, gr = B.pr_preference_loss(ctx, x, to(ch), to(off), ref_logp=to(ref))
+    s, ro, lo, go = L.preference(x64, ch, off, ref)
+    check_rows(lp, lo, gr, go, "bf16")
+    check_stats(st, s, 1.0)
+    assert not gr[:2].any() and gr[2:].any()
+    assert B.pr_ctx_flags(ctx, clear=True) == B.PR_FLAG_EMPTY_REQ
+    # no rows at all
+    empty = x[:0]
+    st, lp, gr = B.pr_policy_loss(ctx, empty, to(ch), to(old))
+    assert not st.any() and gr.shape == (0, 300)
+    st, r, lp, gr = B.pr_preference_loss(ctx, empty, to(ch), to([0, 0, 0], np.int64))
+    assert not st.any() and not r.any()
+    B.pr_ctx_flags(ctx, clear=True)
+
+
+def test_offsets_that_leave_the_batch(B, ctx):
+    """Bad requests count nothing and are reported; rows outside all requests are
+    left out."""
+    g, x, x64, ch, old, ref = draw(2, 10, 500, "f32")
+    adv = g.normal(size=10).astype(np.float32)
+    for off, flag in (([2, 4, 9], 0), ([0, 4, 12], B.PR_FLAG_BAD_OFFSETS),
+                      ([-3, 4, 10], B.PR_FLAG_BAD_OFFSETS)):
+        st, lp, gr = B.pr_policy_loss(ctx, x, to(ch), to(adv), old_logp=to(old),
+                                      offsets=to(off, np.int64), norm=1)
+        s, lo, go = L.policy(x64, ch, adv, old, None, None, off, requests=True)
+        check_rows(lp, lo, gr, go, "f32")
+        check_stats(st, s, 1.0)
+        assert B.pr_ctx_flags(ctx, clear=True) == flag
+
+
+def test_on_policy_and_no_reference(B, ctx):
+    """old_logp NULL: the ratio is 1 and the slope the advantage; without a reference
+    kl_coef has nothing to weigh."""
+    g, x, x64, ch, _, _ = draw(3, 8, 4000, "bf16")
+    adv = g.normal(size=8).astype(np.float32)
+    st, lp, gr = B.pr_policy_loss(ctx, x, to(ch), to(adv), kl_coef=0.3)
+    s, lo, go = L.policy(x64, ch, adv, kl_coef=0.3)
+    check_rows(lp, lo, gr, go, "bf16")
+    check_stats(st, s, 1.0)
+    assert st[3].item() == 1.0 and st[2].item() == 0.0 and st[5].item() == 0.0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V,stride,start,gstride,gstart", [
+    (999, 999, 0, 999, 0), (1000, 1008, 3, 1003, 0), (1000, 1000, 0, 1001, 1), (2051, 2053, 5, 2053, 5),
+    (33, 40, 1, 35, 2), (20011, 20011, 7, 20016, 0), (160001, 160001, 1, 160001, 1)])
+def test_strides_and_alignments(B, ctx, V, stride, start, gstride, gstart, dtype):
+    """Rows off the 16-byte grid, gradients on another grid than their logits; bytes
+    between and around the gradient's rows stay as they are."""
+    n = 5
+    g, x, x64, ch, old, ref = draw(V + stride, n, V, dtype)
+    buf = torch.full((start + n * stride + 9,), torch.nan, dtype=x.dtype, device="cuda")
+    xs = buf[start:start + n * stride].view(n, stride)[:, :V]
+    xs.copy_(x)
+    gbuf = torch.full((gstart + n * gstride + 9,), 7.0, dtype=x.dtype, device="cuda")
+    gv = gbuf[gstart:gstart + n * gstride].view(n, gstride)
+    adv = g.normal(size=n).astype(np.float32)
+    st, lp, gr = B.pr_policy_loss(ctx, xs, to(ch), to(adv), old_logp=to(old), ref_logp=to(ref),
+                                  kl_coef=0.1, grad=gv[:, :V])
+    s, lo, go = L.policy(x64, ch, adv, old, ref, kl_coef=0.1)
+    check_rows(lp, lo, gr, go, dtype)
+    check_stats(st, s, 1.0)
+    out = gbuf.clone()
+    out[gstart:gstart + n * gstride].view(n, gstride)[:, :V] = 7.0
+    assert (out == 7.0).all()
+    off = np.array([0, 2, 5], np.int64)
+    gbuf.fill_(7.0)
+    st, r, lp, gr = B.pr_preference_loss(ctx, xs, to(ch), to(off), ref_logp=to(ref), grad=gv[:, :V])
+    s, ro, lo, go = L.preference(x64, ch, off, ref)
+    check_rows(lp, lo, gr, go, dtype)
+    out = gbuf.clone()
+    out[gstart:gstart + n * gstride].view(n, gstride)[:, :V] = 7.0
+    assert (out == 7.0).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,V", [(40, 1001), (330, 5000), (6, 151936), (3, 600003)])
+def test_gradient_in_place_of_the_logits(B, ctx, n, V, dtype):
+    g, x, _, ch, old, ref = draw(n, n, V, dtype)
+    off = offsets_of(g, n, 2)
+    adv = g.normal(size=n).astype(np.float32)
+    args = dict(ref_logp=to(ref), offsets=to(off))
+    a = B.pr_policy_loss(ctx, x, to(ch), to(adv), old_logp=to(old), kl_coef=0.1, **args)
+    y = x.clone()
+    b = B.pr_policy_loss(ctx, y, to(ch), to(adv), old_logp=to(old), kl_coef=0.1, grad=y, **args)
+    assert all(torch.equal(u, v) for u, v in zip(a, b)) and b[2].data_ptr() == y.data_ptr()
+    a = B.pr_preference_loss(ctx, x, to(ch), **args)
+    y = x.clone()
+    b = B.pr_preference_loss(ctx, y, to(ch), grad=y, **args)
+    assert all(torch.equal(u, v) for u, v in zip(a, b))
+
+
+def test_gradient_is_the_difference_of_the_loss(B, ctx):
+    """Central differences of the library's own loss in fp32: step 1/16 on the logits of
+    the emitted token and of others.  The truncation is h^2 / 6 times a third
+    derivative of at most the slope, rounding 2e-6 / h of the loss: 1.5e-3 of the row's
+    slope, and 1e-4."""
+    n, V = 6, 50
+    g, x, x64, ch, old, ref = draw(9, n, V, "f32", scale=1.0)
+    off = to([0, 1, 3, 6], np.int64)
+    adv = to(np.array([0.8, -1.2, 0.5], np.float32))
+    kw = dict(old_logp=to(old), ref_logp=to(ref), offsets=off, per_request=True, kl_coef=0.2,
+              norm=B.PR_NORM_REQUESTS, clip_low=1.0, clip_high=9.0)
+    pair = dict(ref_logp=to(ref), beta=0.5)
+
+    def policy(y):
+        return B.pr_policy_loss(ctx, y, to(ch), adv, want_grad=False, **kw)[0][0].item()
+
+    def preference(y):
+        return B.pr_preference_loss(ctx, y, to(ch), to([0, 3, 6], np.int64), want_grad=False,
+                                    **pair)[0][0].item()
+
+    for f, grad in ((policy, B.pr_policy_loss(ctx, x, to(ch), adv, **kw)[2]),
+                    (preference, B.pr_preference_loss(ctx, x, to(ch), to([0, 3, 6], np.int64),
+                                                      **pair)[3])):
+        h = 1.0 / 16
+        for t in range(n):
+            for v in {int(ch[t]), 0, V - 1}:
+                up, dn = x.clone(), x.clone()
+                up[t, v] += h
+                dn[t, v] -= h
+                d = (f(up) - f(dn)) / (2 * h)
+                assert abs(d - grad[t, v].item()) <= 1.5e-3 * grad[t].abs().max().item() + 1e-4
+
+
+def test_many_short_rows_and_one_long_request(B, ctx):
+    for n, V, n_req in ((5000, 130, 1), (3000, 64, 1500), (20011, 9, 40)):
+        g, x, x64, ch, old, ref = draw(n, n, V, "f32")
+        off = offsets_of(g, n, n_req)
+        mask = (g.random(n) < 0.7).astype(np.uint8)
+        adv = g.normal(size=n_req).astype(np.float32)
+        st, lp, gr = B.pr_policy_loss(ctx, x, to(ch), to(adv), old_logp=to(old), mask=to(mask),
+                                      offsets=to(off), per_request=True, norm=1)
+        # the oracle's loops are slow: its formulas on whole arrays
+        req, count = np.full(n, -1), np.zeros(n_req, np.int64)
+        own = np.searchsorted(off, np.arange(n), side="right") - 1
+        req[mask == 1] = own[mask == 1]
+        np.add.at(count, own, mask)
+        z = x64 - x64.max(1, keepdims=True)
+        p = np.exp(z)
+        p /= p.sum(1, keepdims=True)
+        l = np.log(p[np.arange(n), ch])
+        r = np.exp(l - old)
+        A = adv[own]
+        free, cut = r * A, np.clip(r, 0.8, 1.2) * A
+        keep = (np.abs(r - 0.8) > 1e-3) & (np.abs(r - 1.2) > 1e-3)  # away from the jumps
+        w = mask / ((count > 0).sum() * np.maximum(count[own], 1))
+        k = w * np.where(cut < free, 0.0, -free)
+        go = -k[:, None] * p
+        go[np.arange(n), ch] += k
+        check_rows(lp, l * mask, None, None, "f32")
+        check_rows(lp[torch.from_numpy(keep)], (l * mask)[keep], gr[torch.from_numpy(keep)],
+                   go[keep], "f32")
+        assert abs(st[0].item() + (w * np.minimum(free, cut)).sum()) < 1e-4
+
+
+def test_results_repeat_and_survive_other_streams_and_graphs(B, ctx):
+    n, V = 400, 9001
+    g, x, _, ch, old, ref = draw(21, n, V, "bf16")
+    off = to(offsets_of(g, n, 10))
+    adv = to(g.normal(size=n).astype(np.float32))
+    chd, oldd, refd = to(ch), to(old), to(ref)
+    grad = torch.empty_like(x)
+    stats, logp = torch.empty(6, device="cuda"), torch.empty(n, device="cuda")
+    pstats, ratio, plogp = (torch.empty(5, device="cuda"), torch.empty(10, device="cuda"),
+                            torch.empty(n, device="cuda"))
+    pgrad = torch.empty_like(x)
+    y = x.clone()
+
+    def run():
+        B.pr_policy_loss(ctx, y, chd, adv, old_logp=oldd, ref_logp=refd, offsets=off, kl_coef=0.1,
+                         stats=stats, logp=logp, grad=grad)
+        B.pr_preference_loss(ctx, y, chd, off, ref_logp=refd, stats=pstats, ratio=ratio, logp=plogp,
+                             grad=pgrad)
+
+    out = (stats, logp, grad, pstats, ratio, plogp, pgrad)
+    run()
+    torch.cuda.synchronize()
+    want = [t.clone() for t in out]
+    side = torch.cuda.Stream()
+    for _ in range(4):
+        for t in out:
+            t.zero_()
+        y.zero_()
+        y.copy_(x)  # written by the kernel just before the call
+        run()
+        for t, w in zip(out, want):
+            assert torch.equal(t, w)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        run()
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y.copy_(x)
+        run()
+    for t in out:
+        t.zero_()
+    y.zero_()
+    for _ in range(3):
+        graph.replay()
+    torch.cuda.synchronize()
+    for t, w in zip(out, want):
+        assert torch.equal(t, w)
+
+
+def test_refusals(B, ctx):
+    g, x, _, ch, old, ref = draw(2, 4, 64, "f32")
+    c, a, off = to(ch), to(old), to([0, 2, 4], np.int64)
+    bad = [dict(temperature=0.0), dict(temperature=float("nan")), dict(clip_low=-0.1),
+           dict(clip_low=1.5), dict(clip_high=-1.0), dict(kl_coef=-1.0), dict(norm=7),
+           dict(grad_scale=float("inf")), dict(per_request=True), dict(grad=x[:, :32]),
+           dict(grad=x[:2]), dict(grad=x.bfloat16()), dict(grad=torch.empty(64, 4, device="cuda").t()),
+           dict(mask=torch.ones(3, dtype=torch.uint8, device="cuda")), dict(mask=a),
+           dict(old_logp=a.double()), dict(ref_logp=a[:3]), dict(stats=a[:2]),
+           dict(logp=torch.empty(4)), dict(offsets=off.int())]
+    n0 = B.launch_count()
+    for k in bad:
+        with pytest.raises(B.PRError) as e:
+            B.pr_policy_loss(ctx, x, c, a, **k)
+        assert e.value.status == B.PR_ERR_INVALID_ARG, k
+    with pytest.raises(B.PRError):
+        B.pr_policy_loss(ctx, x, c[:3], a)
+    # the logits' buffer as the gradient, with another stride
+    wide = torch.zeros(8, 64, device="cuda")
+    with pytest.raises(B.PRError):
+        B.pr_policy_loss(ctx, wide[::2], to(ch), a, grad=wide[:4])
+    bad = [dict(beta=0.0), dict(beta=float("inf")), dict(loss=3), dict(label_smoothing=1.5),
+           dict(loss=2, label_smoothing=0.1), dict(loss=1, margin=0.5), dict(margin=float("nan")),
+           dict(ratio=a[:1]), dict(temperature=-1.0), dict(ref_logp=a[:2])]
+    for k in bad:
+        with pytest.raises(B.PRError) as e:
+            B.pr_preference_loss(ctx, x, c, off, **k)
+        assert e.value.status == B.PR_ERR_INVALID_ARG, k
+    with pytest.raises(B.PRError):  # three answers are no pairs
+        B.pr_preference_loss(ctx, x, c, to([0, 1, 2, 4], np.int64))
+    assert B.launch_count() == n0
