@@ -579,6 +579,60 @@ pr_status pr_preference_loss(pr_ctx* ctx, const void* logits, pr_dtype dt, int64
                              float* ratio, float* logp, void* grad, int64_t grad_stride,
                              void* stream);
 
+/* ---- optimiser step over many tensors ------------------------------------------------- */
+
+#define PR_ADAMW_BLOCK 256 /* elements that share the scale of an 8-bit state */
+
+/* One tensor of a step: n elements side by side, device memory. */
+typedef struct {
+  void* param;          /* of param_dtype; written */
+  const void* grad;     /* of grad_dtype */
+  float* master;        /* single-precision copy of a bf16 parameter, or NULL; written */
+  void* m;              /* first moment: float [n], or int8 codes [n] (state_bits 8); written */
+  void* v;              /* second moment: float [n], or uint8 codes [n]; written */
+  float* m_scale;       /* state_bits 8: [ceil(n / 256)], else NULL; written */
+  float* v_scale;       /* the same for v */
+  int64_t n;            /* >= 0 */
+  float weight_decay;
+  int32_t param_dtype, grad_dtype; /* pr_dtype */
+  int32_t state_bits;   /* 8 or 32 */
+} pr_adamw_tensor;
+
+/*
+ * One AdamW step, in fp32, over n_tensors tensors (host array, read during the
+ * call; tensors of different types may be mixed):
+ *   g = grad * *grad_scale;  m = beta1 m + (1 - beta1) g;  v = beta2 v + (1 - beta2) g^2;
+ *   p = p - lr ((m / (1 - beta1^step)) / (sqrt(v / (1 - beta2^step)) + eps) + weight_decay p)
+ * p is the master copy where there is one, param its rounding to bf16; without
+ * one, param itself, rounded to its type.
+ *   grad_scale  device float or NULL (1): e.g. the clip coefficient of the
+ *               gradients' norm
+ *   step        >= 1, this step's number;  beta1, beta2 in [0, 1), eps >= 0
+ * 8-bit states, per block of 256 elements (a tensor's last one may be shorter)
+ * with the block's largest magnitude as its scale:
+ *   m: code q = round(127 sqrt(|m| / scale)) with m's sign, value q |q| scale / 127^2
+ *   v: code q = round(255 (v / scale)^(1/4)), value q^4 scale / 255^4
+ * rounded to nearest, ties to even.  All-zero codes and scales are the states
+ * before the first step.  A block without a normal number is held as zeros, one with
+ * NaN or an infinity with scale NaN: its values are NaN from then on and the
+ * call raises PR_FLAG_NONFINITE (context flag word).  The parameters step with the new
+ * states before their rounding.
+ * One launch per 384 tensors of the same types, no workspace.  Tensors whose pointers
+ * are multiples of 32 bytes (16 for bf16, 8 for codes) are read and written fastest.
+ */
+pr_status pr_adamw_step(pr_ctx* ctx, const pr_adamw_tensor* tensors, int32_t n_tensors, double lr,
+                        double beta1, double beta2, double eps, int64_t step,
+                        const float* grad_scale, void* stream);
+
+/*
+ * The values that 8-bit states stand for (checkpoints, a change of the states'
+ * type): m, v device float [blocks][256], the tensors' blocks one after another,
+ * blocks = sum of ceil(n / 256); past a tensor's end its last block is zero.
+ * Every tensor must have state_bits 8.
+ */
+pr_status pr_adamw_unpack(pr_ctx* ctx, const pr_adamw_tensor* tensors, int32_t n_tensors, float* m,
+                          float* v, void* stream);
+
 /* ---- verification without allocation ------------------------------------------------- */
 
 #define PR_NOALLOC_MAX_ROWS 16384    /* largest n_rows pr_route_noalloc accepts */

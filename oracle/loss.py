@@ -124,3 +124,33 @@ def preference(x, chosen, offsets, ref_logp=None, mask=None, beta=0.1, loss=SIGM
     slope = np.where(req >= 0, side[np.maximum(req, 0)], 0.0)
     logp = np.where(req >= 0, l, 0.0)
     return stats, s, logp, _grad(p, chosen, slope, req, temperature, grad_scale)
+
+
+# ---- the optimiser step --------------------------------------------------------------------
+
+
+def adamw(p, g, m, v, lr, beta1, beta2, eps, step, weight_decay=0.0, grad_scale=1.0):
+    """(p, m, v) after one AdamW step of one tensor."""
+    p, g, m, v = (np.asarray(t, np.float64) for t in (p, g, m, v))
+    g = g * grad_scale
+    m = beta1 * m + (1 - beta1) * g
+    v = beta2 * v + (1 - beta2) * g * g
+    mhat, vhat = m / (1 - beta1 ** step), v / (1 - beta2 ** step)
+    return p - lr * (mhat / (np.sqrt(vhat) + eps) + weight_decay * p), m, v
+
+
+def held8(codes, scale, signed, block=256):
+    """The values of 8-bit codes under their blocks' scales."""
+    q = np.asarray(codes, np.float64)
+    s = np.repeat(np.asarray(scale, np.float64), block)[:q.size]
+    return q * np.abs(q) / 127.0 ** 2 * s if signed else q ** 4 / 255.0 ** 4 * s
+
+
+def codes8(x, signed, block=256):
+    """(unrounded codes, scales) of values in blocks: the root of the ratio to
+    the block's largest magnitude, times 127 with a sign, or 255."""
+    x = np.asarray(x, np.float64)
+    scale = np.array([np.abs(x[i:i + block]).max() for i in range(0, x.size, block)])
+    s = np.repeat(np.where(scale > 0, scale, 1.0), block)[:x.size]
+    r = np.sqrt(np.abs(x) / s)
+    return (np.sign(x) * r * 127.0 if signed else np.sqrt(r) * 255.0), scale

@@ -28,6 +28,7 @@ PR_LMHEAD_MAX_VOCAB = (1 << 31) - 256
 PR_NORM_TOKENS, PR_NORM_REQUESTS = 0, 1
 PR_PREF_SIGMOID, PR_PREF_SQUARED, PR_PREF_HINGE = 0, 1, 2
 PR_NPOL, PR_NPREF = 6, 5
+PR_ADAMW_BLOCK = 256
 
 # every symbol include/pro_router.h declares
 EXPORTS = (
@@ -39,6 +40,7 @@ EXPORTS = (
     "pr_selftest_wait", "pr_lmhead_decode_step", "pr_last_error", "pr_prescorer_fit",
     "pr_prescorer_destroy", "pr_prescorer_vocab_size", "pr_prescorer_term",
     "pr_prescorer_features", "pr_prescorer_score", "pr_policy_loss", "pr_preference_loss",
+    "pr_adamw_step", "pr_adamw_unpack",
 )
 
 if not os.path.exists(LIB):
@@ -83,6 +85,9 @@ _SIGS = {
                        _P, _P, _I64, _P],
     "pr_preference_loss": [_P, _P, ctypes.c_int, _I64, _I64, _I64, _P, _P, _P, _I32, _P, _P, _P, _P,
                            _P, _P, _I64, _P],
+    "pr_adamw_step": [_P, _P, _I32, ctypes.c_double, ctypes.c_double, ctypes.c_double,
+                      ctypes.c_double, _I64, _P, _P],
+    "pr_adamw_unpack": [_P, _P, _I32, _P, _P, _P],
 }
 for _name, _args in _SIGS.items():
     _fn = getattr(_lib, _name)
@@ -707,6 +712,115 @@ def pr_preference_loss(ctx, logits, chosen, offsets, ref_logp=None, mask=None, b
                                    ctypes.byref(p), _ptr(stats), _ptr(ratio), _ptr(logp),
                                    _ptr(grad), gs, _stream(stream)), call)
     return stats, ratio, logp, grad
+
+
+# ---- optimiser step over many tensors --------------------------------------------------------
+
+class PrAdamwTensor(ctypes.Structure):
+    _fields_ = [("param", _P), ("grad", _P), ("master", _P), ("m", _P), ("v", _P),
+                ("m_scale", _P), ("v_scale", _P), ("n", _I64), ("weight_decay", _F32),
+                ("param_dtype", _I32), ("grad_dtype", _I32), ("state_bits", _I32)]
+
+
+class AdamwTensors:
+    """The tensors of a step, as the library takes them.  Keeps them alive; a
+    program whose tensors stay where they are makes this once."""
+
+    def __init__(self, table, keep, device):
+        self.table, self.keep, self.device = table, keep, device
+        self.blocks = sum(-(-t.n // PR_ADAMW_BLOCK) for t in table)
+
+    def __len__(self):
+        return len(self.table)
+
+
+def pr_adamw_tensors(params, grads, m, v, master=None, m_scale=None, v_scale=None,
+                     weight_decay=0.0) -> AdamwTensors:
+    """Lists of the parameters (float32 or bfloat16), gradients (the same), and
+    moments: float32, or 8-bit codes (m int8, v uint8) with `m_scale` and
+    `v_scale`, float32 with one value per PR_ADAMW_BLOCK elements.  `master`:
+    float32 copies of bfloat16 parameters (a list, None where there is none).
+    `weight_decay`: one value, or one per tensor."""
+    call = "pr_adamw_tensors"
+    n = len(params)
+    none = [None] * n
+    lists = {"params": params, "grads": grads, "m": m, "v": v, "master": master or none,
+             "m_scale": m_scale or none, "v_scale": v_scale or none}
+    wd = [float(weight_decay)] * n if isinstance(weight_decay, (int, float)) else list(weight_decay)
+    for name, one in [*lists.items(), ("weight_decay", wd)]:
+        if len(one) != n:
+            raise PRError(PR_ERR_INVALID_ARG, call, "%s has %d entries for %d parameters" % (
+                name, len(one), n))
+    table = (PrAdamwTensor * n)()
+    dev = params[0].get_device() if n and isinstance(params[0], torch.Tensor) else 0
+    float_t = (torch.float32, torch.bfloat16)
+    for i, e in enumerate(table):
+        one = {name: t[i] for name, t in lists.items()}
+        _dev(call, dev, "params[%d]" % i, one["params"], float_t)
+        k = one["params"].numel()
+        eight = isinstance(one["m"], torch.Tensor) and one["m"].dtype == torch.int8
+        blocks = -(-k // PR_ADAMW_BLOCK)
+        want = {"grads": (float_t, k), "m": ((torch.int8,) if eight else _F32_T, k),
+                "v": ((torch.uint8,) if eight else _F32_T, k)}
+        if one["master"] is not None:
+            want["master"] = (_F32_T, k)
+        if eight:
+            want["m_scale"] = want["v_scale"] = (_F32_T, blocks)
+        for name, (dtypes, numel) in want.items():
+            _dev(call, dev, "%s[%d]" % (name, i), one[name], dtypes)
+            if one[name].numel() != numel:
+                raise PRError(PR_ERR_INVALID_ARG, call, "%s[%d] holds %d elements, expected %d" % (
+                    name, i, one[name].numel(), numel))
+        if (not eight and (one["m_scale"] is not None or one["v_scale"] is not None)) or (
+                one["master"] is not None and one["params"].dtype != torch.bfloat16):
+            raise PRError(PR_ERR_INVALID_ARG, call, "tensor %d has %s" % (
+                i, "scales without codes" if one["master"] is None else "a master copy of float32"))
+        e.param, e.grad, e.m, e.v = (one[name].data_ptr() for name in ("params", "grads", "m", "v"))
+        e.master, e.m_scale, e.v_scale = (
+            None if one[name] is None else one[name].data_ptr()
+            for name in ("master", "m_scale", "v_scale"))
+        e.n, e.weight_decay = k, wd[i]
+        e.param_dtype, e.grad_dtype = _dtype(one["params"]), _dtype(one["grads"])
+        e.state_bits = 8 if eight else 32
+    return AdamwTensors(table, lists, dev)
+
+
+def _adamw_table(call, dev, tensors):
+    if not isinstance(tensors, AdamwTensors):
+        raise PRError(PR_ERR_INVALID_ARG, call, "tensors must come from pr_adamw_tensors")
+    if len(tensors) and tensors.device != dev:
+        raise PRError(PR_ERR_INVALID_ARG, call, "tensors are on cuda:%d, the context on cuda:%d" % (
+            tensors.device, dev))
+    return ctypes.addressof(tensors.table) if len(tensors) else None
+
+
+def pr_adamw_step(ctx, tensors: AdamwTensors, lr: float, beta1: float = 0.9, beta2: float = 0.999,
+                  eps: float = 1e-8, step: int = 1, grad_scale=None, stream=None):
+    """One AdamW step in place over the tensors of `pr_adamw_tensors`;
+    `grad_scale`: a CUDA float32 value that multiplies the gradients."""
+    call = "pr_adamw_step"
+    dev = _ctx_device(ctx)
+    table = _adamw_table(call, dev, tensors)
+    _dev(call, dev, "grad_scale", grad_scale, _F32_T, 1, optional=True)
+    _check(_lib.pr_adamw_step(ctx, table, len(tensors), float(lr), float(beta1), float(beta2),
+                              float(eps), int(step), _ptr(grad_scale), _stream(stream)), call)
+
+
+def pr_adamw_unpack(ctx, tensors: AdamwTensors, m=None, v=None, stream=None):
+    """The values that 8-bit states stand for: (m, v) float32
+    [blocks][PR_ADAMW_BLOCK], the tensors' blocks one after another."""
+    call = "pr_adamw_unpack"
+    dev = _ctx_device(ctx)
+    table = _adamw_table(call, dev, tensors)
+    shape = (tensors.blocks, PR_ADAMW_BLOCK)
+    d = torch.device("cuda", dev)
+    m = torch.empty(shape, dtype=torch.float32, device=d) if m is None else m
+    v = torch.empty(shape, dtype=torch.float32, device=d) if v is None else v
+    _dev(call, dev, "m", m, _F32_T, shape[0] * shape[1])
+    _dev(call, dev, "v", v, _F32_T, shape[0] * shape[1])
+    _check(_lib.pr_adamw_unpack(ctx, table, len(tensors), m.data_ptr(), v.data_ptr(),
+                                _stream(stream)), call)
+    return m, v
 
 
 # ---- the prompt pre-scorer (host CPU; Section 3.1, Eq. 2) ---------------------------------
