@@ -64,6 +64,8 @@ struct pr_ctx {
   // the training losses: workspace, grown on demand
   void* loss_ws = nullptr;
   size_t loss_ws_bytes = 0;
+  bool loss_ready = false;             // shared memory opt-ins made
+  int loss_places[6] = {};             // rows in work at a time, per width of a row's group
   // PR_OPT_TIMING: events after each kernel of the last multi-kernel call
   int32_t timing = 0;
   cudaEvent_t tev[PR_MAX_TIMED + 1] = {};

@@ -21,12 +21,8 @@
 
 namespace prk {
 
-constexpr int LS_NT = 512;
-constexpr int LS_NW = LS_NT / 32;
 constexpr int LS_NSTAT = 6;   // statistics of a loss (the preference loss has 5)
 constexpr float LS_MIN = -3.402823466e38f;  // "no maximum yet": the lowest finite value
-
-enum LossKind { LOSS_POLICY = 0, LOSS_PREF_FWD = 1, LOSS_PREF_BWD = 2 };
 
 struct LossArgs {
   const void* logits;
@@ -53,31 +49,44 @@ struct LossArgs {
   int32_t* ticket;     // [2] arrivals, zero between calls
   int64_t* totals;     // counted tokens; requests with some (policy) or pairs of such
   int32_t* count;      // [n_req] counted tokens
+  int32_t* row_req;    // [n_rows] request of a row that counts, else -1
   float* coef;         // [n_req] dL / d log ratio (preference)
   float* term;         // [n_req / 2][LS_NSTAT] the pairs' statistics
-  float4* state;       // [n_rows] M, log2 S, l - ref, 1 - p_y (preference)
+  float4* state;       // [n_rows] M, log2 S, l - ref (preference) or dL/dx's factor, 1 - p_y
   double* part;        // [groups][LS_NSTAT] statistics of each group's rows
   uint32_t* ctx_flags;
 };
 
-// the request that owns row t and its counted tokens; -1 when there is none or its
-// bounds are not inside the batch.  Whole warp.
-__device__ __forceinline__ int32_t loss_request(const LossArgs& a, int64_t t, int lane) {
-  if (!a.offsets) return 0;
-  const int32_t r = find_request(a.offsets, a.n_req, t, lane);
-  if (r < 0) return -1;
-  return a.offsets[r] >= 0 && a.offsets[r + 1] <= a.n_rows ? r : -1;
-}
-
 // ---- counted tokens -------------------------------------------------------------------
 
-// One CTA per request; the last one to finish sums up.
+// The first n_req CTAs count a request's tokens each, the last of them to finish sums
+// up; the others find the requests of 256 rows each.
 static __global__ void __launch_bounds__(256) loss_plan(const LossArgs a, int pairs) {
   __shared__ int64_t part[8];
   __shared__ int last;
   pdl_wait();
   pdl_trigger();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  if ((int64_t)blockIdx.x >= a.n_req) {
+    const int64_t t = ((int64_t)blockIdx.x - a.n_req) * 256 + tid;
+    if (t >= a.n_rows) return;
+    int32_t r = -1;
+    if (!a.mask || a.mask[t] != 0) {
+      r = 0;
+      if (a.offsets) {
+        int32_t hi = a.n_req - 1;  // the largest r with offsets[r] <= t
+        while (r < hi) {
+          const int32_t mid = (int32_t)(((int64_t)r + hi + 1) >> 1);
+          if (a.offsets[mid] <= t) r = mid;
+          else hi = mid - 1;
+        }
+        const int64_t lo = a.offsets[r], up = a.offsets[r + 1];
+        if (lo < 0 || up > a.n_rows || t < lo || t >= up) r = -1;
+      }
+    }
+    a.row_req[t] = r;
+    return;
+  }
   const int64_t r = blockIdx.x;
   const int64_t lo = a.offsets ? a.offsets[r] : 0, hi = a.offsets ? a.offsets[r + 1] : a.n_rows;
   const bool bad = lo < 0 || hi < lo || hi > a.n_rows;
@@ -102,7 +111,7 @@ static __global__ void __launch_bounds__(256) loss_plan(const LossArgs a, int pa
     a.count[r] = (int32_t)n;
     if (bad) atomicOr(a.ctx_flags, FLAG_BAD_OFFSETS);
     else if (lo == hi) atomicOr(a.ctx_flags, FLAG_EMPTY_REQ);
-    last = atom_add_acq_rel(a.ticket, 1) == (int)gridDim.x - 1;
+    last = atom_add_acq_rel(a.ticket, 1) == a.n_req - 1;
   }
   __syncthreads();
   if (!last) return;
@@ -289,6 +298,16 @@ __device__ __forceinline__ uint4 grad_word(const RowGrad& g, const uint4& w) {
 __device__ __forceinline__ void put(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
 __device__ __forceinline__ void put(float* p, float v) { *p = v; }
 
+template <typename T>
+__device__ __forceinline__ void put_word(T* p, const uint4& w, bool vec) {
+  if (vec) {
+    *reinterpret_cast<uint4*>(p) = w;
+  } else {
+#pragma unroll
+    for (int j = 0; j < Traits<T>::VEC; ++j) put(p + j, Traits<T>::at(w, j));
+  }
+}
+
 // A row as the 16-byte words of the address grid that lie in it, and the elements
 // before and after them.
 struct RowWords {
@@ -305,139 +324,406 @@ struct RowWords {
   }
 };
 
-// ---- rows, one CTA each, two sweeps over global memory --------------------------------------
+// ---- forward: rows through rings of shared memory ---------------------------------------
+//
+// A group of warps takes a row: 1, 4 or the 16 warps of a CTA, or 16 of each CTA of a
+// cluster.  Warp w of the group takes every w-th chunk of 2 KB of (its CTA's share of)
+// the row, brings it into a ring of its own with one bulk copy, and runs ahead over its
+// next rows as far as the ring has room: nothing but the row's two sums is ever
+// waited for together.  With HOLD a row's chunks stay in the ring for the backward
+// sweep, so that its logits are read from memory once; a stage is free, and the next
+// row's chunk on its way into it, as soon as its part of the gradient is written.
+// What does not fit (or has to wait for other rows: answer pairs) leaves the row's
+// state to loss_backward.
+constexpr int RG_NW = 16;
+constexpr int RG_W = 4;                        // words per lane and chunk
+constexpr int RG_CHUNK = 32 * RG_W;            // words of a chunk
+constexpr int RG_BYTES = 16 * RG_CHUNK;
+constexpr int RG_NS = 7;                       // stages per warp
+struct RingSmem {
+  unsigned char stage[RG_NW][RG_NS][RG_BYTES];
+  uint64_t bar[RG_NW][RG_NS];
+  float2 part[2][RG_NW * MAXC];                // the warps' (m, R), two rows deep
+};
+static_assert(sizeof(RingSmem) <= 232448, "227 KB");
 
-template <typename T, int KIND>
-__global__ void __launch_bounds__(LS_NT) loss_rows(const LossArgs a) {
+// a group's share of a row: its words, those of this CTA, and this warp's chunks of those
+struct Share {
+  const char* x;       // the row
+  RowWords rw;
+  int32_t w0, w1;      // this CTA's words [w0, w1)
+  int32_t chunks;      // this warp's chunks
+};
+template <typename T, int GW>
+__device__ __forceinline__ Share share_of(const LossArgs& a, int64_t row, uint32_t C, uint32_t rank,
+                                          int wg) {
+  Share s;
+  const T* x = reinterpret_cast<const T*>(a.logits) + row * a.row_stride;
+  s.x = reinterpret_cast<const char*>(x);
+  s.rw = RowWords::of(x, a.vocab);
+  const int32_t words = (int32_t)s.rw.words;
+  const int32_t all = (words + RG_CHUNK - 1) / RG_CHUNK;
+  const int32_t per = GW < RG_NW ? all : (all + (int32_t)C - 1) / (int32_t)C;  // chunks of a CTA
+  s.w0 = min(words, (int32_t)rank * per * RG_CHUNK);
+  s.w1 = min(words, s.w0 + per * RG_CHUNK);
+  const int32_t mine = (s.w1 - s.w0 + RG_CHUNK - 1) / RG_CHUNK;
+  s.chunks = mine > wg ? (mine - wg + GW - 1) / GW : 0;
+  return s;
+}
+
+// what a row's epilogue needs, fetched while the rows before it are in work
+struct RowIn {
+  int32_t r, y, count;
+  float xy, old, ref, adv;
+};
+
+template <typename T, int GW, bool HOLD, bool PREF>
+__global__ void __launch_bounds__(RG_NW * 32, 1) loss_ring(const LossArgs a) {
+  extern __shared__ __align__(16) unsigned char smem_raw[];
+  RingSmem& sm = *reinterpret_cast<RingSmem*>(smem_raw);
   using Tr = Traits<T>;
-  __shared__ float pm[LS_NW], pS[LS_NW];
-  __shared__ float sh[4];
-  __shared__ int32_t sreq;
-  __shared__ int last;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  double stat[LS_NSTAT] = {0., 0., 0., 0., 0., 0.};
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int wg = warp % GW;
+  uint32_t C = 1, rank = 0;
+  if (GW == RG_NW) {
+    asm("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(C));
+    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+  }
+  const int64_t G = GW == RG_NW ? gridDim.x / C : (int64_t)gridDim.x * (RG_NW / GW);
+  const int64_t first = GW == RG_NW ? blockIdx.x / C : (int64_t)blockIdx.x * (RG_NW / GW) + warp / GW;
+  const bool leader = wg == 0 && rank == 0;
+  auto bar_of = [&](int s) { return (uint32_t)__cvta_generic_to_shared(&sm.bar[warp][s]); };
+  if (lane == 0) {
+    for (int s = 0; s < RG_NS; ++s)
+      asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bar_of(s)) : "memory");
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  __syncwarp();
+  if (GW == RG_NW && C > 1) cluster_sync_all();  // every CTA's memory is there
   pdl_wait();
   pdl_trigger();
-  for (int64_t row = blockIdx.x; row < a.n_rows; row += gridDim.x) {
-    const T* x = reinterpret_cast<const T*>(a.logits) + row * a.row_stride;
+
+  // ---- bringing chunks in
+  int64_t lrow = first;            // the next chunk's row, its request and the next row's
+  int32_t lreq = lrow < a.n_rows ? __ldcg(a.row_req + lrow) : -1;
+  int32_t lreq2 = lrow + G < a.n_rows ? __ldcg(a.row_req + lrow + G) : -1;
+  int32_t lchunk = 0;
+  int lstage = 0, room = RG_NS, flying = 0;
+  bool landed = true;
+  uint32_t parity = 0u;            // bit s: stage s' next phase
+  Share ls;
+  ls.chunks = 0;
+  if (lrow < a.n_rows) ls = share_of<T, GW>(a, lrow, C, rank, wg);
+  auto bring = [&]() {
+    // rows that do not count, or of which this warp has nothing
+    while (lrow < a.n_rows && (lreq < 0 || lchunk >= ls.chunks)) {
+      lrow += G;
+      lreq = lreq2;
+      lreq2 = lrow + G < a.n_rows ? __ldcg(a.row_req + lrow + G) : -1;
+      lchunk = 0;
+      if (lrow < a.n_rows) ls = share_of<T, GW>(a, lrow, C, rank, wg);
+    }
+    if (lrow >= a.n_rows || room == 0 || !landed) return;
+    if (lane == 0) {
+      const int32_t w = ls.w0 + (wg + lchunk * GW) * RG_CHUNK;
+      const uint32_t bytes = 16u * (uint32_t)min(RG_CHUNK, ls.w1 - w);
+      const uint32_t bar = bar_of(lstage);
+      asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes)
+                   : "memory");
+      asm volatile(
+          "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::
+              "r"((uint32_t)__cvta_generic_to_shared(sm.stage[warp][lstage])),
+          "l"(ls.x + (int64_t)sizeof(T) * ls.rw.head + 16 * (int64_t)w), "r"(bytes), "r"(bar)
+          : "memory");
+    }
+    lstage = lstage + 1 == RG_NS ? 0 : lstage + 1;
+    --room;
+    ++flying;
+    ++lchunk;
+  };
+  for (int s = 0; s < RG_NS; ++s) bring();
+
+  // ---- the rows' scalars, two rows ahead and one
+  auto fetch_id = [&](int64_t row, int32_t& r, int32_t& y) {
+    r = -1;
+    y = 0;
+    if (row < a.n_rows) {
+      r = __ldcg(a.row_req + row);
+      y = __ldcg(a.chosen + row);
+    }
+  };
+  auto fetch = [&](int64_t row, int32_t r, int32_t y) {
+    RowIn in;
+    in.r = r;
+    in.y = y;
+    in.count = 1;
+    in.xy = NAN;
+    in.old = in.ref = in.adv = 0.f;
+    if (r >= 0) {
+      const T* x = reinterpret_cast<const T*>(a.logits) + row * a.row_stride;
+      if (y >= 0 && (int64_t)y < a.vocab) in.xy = Tr::elem(x, y);
+      if (a.ref_logp) in.ref = __ldcg(a.ref_logp + row);
+      if (!PREF) {
+        if (a.old_logp) in.old = __ldcg(a.old_logp + row);
+        in.adv = __ldcg(a.adv + (a.per_request ? (int64_t)r : row));
+        if (a.norm) in.count = __ldcg(a.count + r);
+      }
+    }
+    return in;
+  };
+  int32_t r1, y1;
+  fetch_id(first, r1, y1);
+  RowIn in = fetch(first, r1, y1);
+  fetch_id(first + G, r1, y1);
+  const double share = PREF ? 0.0 : 1.0 / (double)__ldcg(a.totals + (a.norm ? 1 : 0));
+  double stat[LS_NSTAT] = {0., 0., 0., 0., 0., 0.};
+
+  int stage = 0, buf = 0;
+  for (int64_t row = first; row < a.n_rows; row += G) {
+    const RowIn next = row + G < a.n_rows ? fetch(row + G, r1, y1) : in;
+    fetch_id(row + 2 * G, r1, y1);
+    const Share sh = share_of<T, GW>(a, row, C, rank, wg);
+    const T* x = reinterpret_cast<const T*>(sh.x);
     T* g = reinterpret_cast<T*>(a.grad) + row * a.grad_stride;
-    const RowWords rw = RowWords::of(x, a.vocab);
-    const uint4* xw = reinterpret_cast<const uint4*>(x + rw.head);
-    const int32_t y = a.chosen[row];
-    __syncthreads();
-    if (warp == 0) {
-      const bool on = !a.mask || a.mask[row] != 0;
-      const int32_t r = on ? loss_request(a, row, lane) : -1;
-      if (lane == 0) {
-        sreq = r;
-        sh[3] = y >= 0 && (int64_t)y < a.vocab ? Tr::elem(x, y) : NAN;
+    const int64_t tail0 = sh.rw.head + sh.rw.words * Tr::VEC;
+    // element of this lane before or after the words
+    const int64_t ve = lane < 8 ? (lane < sh.rw.head ? lane : -1)
+                                : (lane - 8 < sh.rw.tail ? tail0 + lane - 8 : -1);
+    const bool edge = leader && ve >= 0;
+    if (in.r < 0) {
+      if (leader && lane == 0) a.logp[row] = 0.f;
+      if (HOLD) {
+        const bool vec = ((reinterpret_cast<uintptr_t>(x) ^ reinterpret_cast<uintptr_t>(g)) & 15u) == 0;
+        for (int32_t c = 0; c < sh.chunks; ++c) {
+          const int32_t w = sh.w0 + (wg + c * GW) * RG_CHUNK;
+#pragma unroll
+          for (int k = 0; k < RG_W; ++k) {
+            const int32_t i = w + 32 * k + lane;
+            if (i < sh.w1) put_word(g + sh.rw.head + (int64_t)i * Tr::VEC, make_uint4(0u, 0u, 0u, 0u), vec);
+          }
+        }
+        if (edge) put(g + ve, 0.f);
       }
+      in = next;
+      continue;
     }
-    __syncthreads();
-    const int32_t r = sreq;
+    const int32_t y = in.y;
     const bool yok = y >= 0 && (int64_t)y < a.vocab;
-    const int64_t ye = (int64_t)y - rw.head, yw = yok && ye >= 0 ? ye / Tr::VEC : -1;
-    const int yj = (int)(ye - yw * Tr::VEC);
-    float M, lS, k = 0.f, rest = 0.f;
-    if (KIND != LOSS_PREF_BWD) {
-      if (r < 0) {
-        if (tid == 0) a.logp[row] = 0.f;
-      } else {
-        RowSum s;
-        s.reset();
-        for (int64_t i = tid; i < rw.words; i += LS_NT) {
-          uint4 w = xw[i];
-          if (i == yw) w = without<T>(w, yj);
-          s.raise(Tr::gmax(w), a.c2, a.inv_t);
-          add_word<T>(s, w, a.c2);
-        }
-        if (tid < rw.head && tid != y) s.add1(Tr::elem(x, tid), a.c2, a.inv_t);
-        const int64_t vt = rw.head + rw.words * Tr::VEC + tid;
-        if (tid < rw.tail && vt != y) s.add1(Tr::elem(x, vt), a.c2, a.inv_t);
-        float S = s.S.x + s.S.y;
-        const float m = unord(__reduce_max_sync(FULL, ord(s.m)));
-        S *= rescale(s.m, m, a.inv_t);
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) S += __shfl_xor_sync(FULL, S, o);
-        if (lane == 0) {
-          pm[warp] = m;
-          pS[warp] = S;
-        }
-        __syncthreads();
-        M = LS_MIN;
-        for (int w = 0; w < LS_NW; ++w) M = fmaxf(M, pm[w]);
-        S = 0.f;
-        for (int w = 0; w < LS_NW; ++w) S = fmaf(pS[w], rescale(pm[w], M, a.inv_t), S);
-        const RowEnd e(a, M, S, sh[3], yok);
-        const float l = e.l;
-        M = e.M;
-        lS = e.lS;
-        rest = e.rest;
-        if (tid == 0) {
-          a.logp[row] = l;
-          if (!yok) atomicOr(a.ctx_flags, FLAG_BAD_CHOSEN);
-          else if (isnan(l)) atomicOr(a.ctx_flags, FLAG_NONFINITE);
-        }
-        if (KIND == LOSS_POLICY) {
-          const float old = a.old_logp ? a.old_logp[row] : 0.f;
-          const float ref = a.ref_logp ? a.ref_logp[row] : 0.f;
-          const PolicyTerms p = policy_terms(a, l, e.l_lo, old, ref, a.adv[a.per_request ? r : row]);
-          const double wt = a.norm ? 1.0 / ((double)a.totals[1] * (double)a.count[r])
-                                   : 1.0 / (double)a.totals[0];
-          k = (float)wt * p.slope * (a.grad_scale * a.inv_t);
-          stat[0] += wt * (double)p.loss;
-          stat[1] += wt * (double)p.surrogate;
-          stat[2] += wt * (double)p.kl;
-          stat[3] += wt * (double)p.ratio;
-          stat[4] += wt * (double)p.clipped;
-          stat[5] += wt * (double)p.old_kl;
-        } else if (tid == 0) {
-          a.state[row] = make_float4(M, lS, (l - (a.ref_logp ? a.ref_logp[row] : 0.f)) + e.l_lo, rest);
+    const int64_t yo = (int64_t)y - sh.rw.head;
+    const int32_t yw = yok && yo >= 0 ? (int32_t)(yo / Tr::VEC) : -1;
+    const int yj = (int)(yo - (int64_t)yw * Tr::VEC);
+
+    // ---- forward
+    RowSum s;
+    s.reset();
+    const int held = stage;
+    for (int32_t c = 0; c < sh.chunks; ++c) {
+      if (landed) {
+        if (!ring_test(bar_of(stage), (parity >> stage) & 1u))
+          landed = ring_wait_slow(bar_of(stage), (parity >> stage) & 1u, a.ctx_flags);
+        if (landed) {
+          parity ^= 1u << stage;
+          --flying;
         }
       }
-    } else if (r >= 0) {
-      const float4 st = a.state[row];
-      M = st.x;
-      lS = st.y;
-      rest = st.w;
-      k = a.coef[r] * (a.grad_scale * a.inv_t);
-    }
-    if (KIND == LOSS_PREF_FWD || !a.grad) continue;
-    const bool zero = r < 0 || k == 0.f;
-    const RowGrad rg{M, lS, -k, a.c2};
-    // the emitted token's entry k (1 - p_y) is written by the thread whose word holds it
-    const bool vec = ((reinterpret_cast<uintptr_t>(x) ^ reinterpret_cast<uintptr_t>(g)) & 15u) == 0;
-    const float gy = zero ? 0.f : k * rest;
-    __syncthreads();  // every thread has read what the row's gradient may overwrite
-    for (int64_t i = tid; i < rw.words; i += LS_NT) {
-      uint4 o = make_uint4(0u, 0u, 0u, 0u);
-      if (!zero) o = grad_word<T>(rg, xw[i]);
-      const int64_t v0 = rw.head + i * Tr::VEC;
-      if (vec) *reinterpret_cast<uint4*>(g + v0) = o;
-      else
-        for (int j = 0; j < Tr::VEC; ++j) put(g + v0 + j, Tr::at(o, j));
-      if (!zero && i == yw) put(g + y, gy);
-    }
-    auto edge = [&](int64_t v) {
-      put(g + v, zero ? 0.f : (v == y ? gy : rg.one(Tr::elem(x, v))));
-    };
-    if (tid < rw.head) edge(tid);
-    if (tid < rw.tail) edge(rw.head + rw.words * Tr::VEC + tid);
-  }
-  if (KIND != LOSS_POLICY) return;
-  // the statistics: each CTA's sum over its rows, then the CTAs' in order
-  if (tid == 0) {
-    for (int j = 0; j < LS_NSTAT; ++j) a.part[(int64_t)blockIdx.x * LS_NSTAT + j] = stat[j];
-    last = atom_add_acq_rel(a.ticket + 1, 1) == (int)gridDim.x - 1;
-  }
-  __syncthreads();
-  if (!last || warp >= LS_NSTAT) return;
-  double v = 0.;
-  for (int64_t i = lane; i < gridDim.x; i += 32) v += __ldcg(a.part + i * LS_NSTAT + warp);
+      __syncwarp();
+      const uint4* st = reinterpret_cast<const uint4*>(sm.stage[warp][stage]) + lane;
+      const int32_t w = sh.w0 + (wg + c * GW) * RG_CHUNK;
+      uint4 v[RG_W];
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(FULL, v, o);
-  if (lane == 0) a.stats[warp] = (float)v;
-  if (tid == 0) a.ticket[1] = 0;
+      for (int k = 0; k < RG_W; ++k) v[k] = st[32 * k];
+      if (w + RG_CHUNK > sh.w1) {
+#pragma unroll
+        for (int k = 0; k < RG_W; ++k)
+          if (w + 32 * k + lane >= sh.w1)
+            v[k] = make_uint4(Tr::NEG_WORD, Tr::NEG_WORD, Tr::NEG_WORD, Tr::NEG_WORD);
+      }
+      if (yw >= w && yw < w + RG_CHUNK) {
+#pragma unroll
+        for (int k = 0; k < RG_W; ++k)
+          if (w + 32 * k + lane == yw) v[k] = without<T>(v[k], yj);
+      }
+      const float top = Tr::tile_max(v);
+      if (__any_sync(FULL, (top - s.m) * a.c2 > 8.f)) s.raise(top, a.c2, a.inv_t);
+#pragma unroll
+      for (int k = 0; k < RG_W; ++k) add_word<T>(s, v[k], a.c2);
+      stage = stage + 1 == RG_NS ? 0 : stage + 1;
+      if (!HOLD) {
+        __syncwarp();
+        ++room;
+        bring();
+      }
+    }
+    const float xe = edge ? Tr::elem(x, ve) : 0.f;
+    if (edge && ve != y) s.add1(xe, a.c2, a.inv_t);
+    // the warp's, then the group's sums
+    float R = s.S.x + s.S.y;
+    float m = unord(__reduce_max_sync(FULL, ord(s.m)));
+    R *= rescale(s.m, m, a.inv_t);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) R += __shfl_xor_sync(FULL, R, o);
+    if (GW > 1) {
+      const float2 mine = make_float2(m, R);
+      int n = GW;
+      if (GW == RG_NW && C > 1) {
+        n = RG_NW * (int)C;
+        if (lane < (int)C)
+          dsmem_st_u64(dsmem_addr(&sm.part[buf][rank * RG_NW + warp], (uint32_t)lane),
+                       (uint64_t)__float_as_uint(m) | (uint64_t)__float_as_uint(R) << 32);
+        __syncwarp();
+        cluster_sync_all();
+      } else {
+        if (lane == 0) sm.part[buf][warp] = mine;
+        if (GW == RG_NW) __syncthreads();
+        else named_bar_sync(1 + warp / GW, 32 * GW);
+      }
+      const float2* pt = sm.part[buf] + (GW == RG_NW ? 0 : warp - wg);
+      float2 q[MAXC * RG_NW / 32];
+      m = LS_MIN;
+#pragma unroll
+      for (int k = 0; k < MAXC * RG_NW / 32; ++k) {
+        q[k] = lane + 32 * k < n ? pt[lane + 32 * k] : make_float2(LS_MIN, 0.f);
+        m = fmaxf(m, q[k].x);
+      }
+      m = unord(__reduce_max_sync(FULL, ord(m)));
+      R = 0.f;
+#pragma unroll
+      for (int k = 0; k < MAXC * RG_NW / 32; ++k)
+        if (32 * k < n) R = fmaf(q[k].y, rescale(q[k].x, m, a.inv_t), R);
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) R += __shfl_xor_sync(FULL, R, o);
+      buf ^= 1;
+    }
+    const RowEnd e(a, m, R, in.xy, yok);
+    float k = 0.f;
+    if (!PREF) {
+      const double wt = a.norm ? share / (double)in.count : share;
+      const PolicyTerms p = policy_terms(a, e.l, e.l_lo, in.old, in.ref, in.adv);
+      k = (float)wt * p.slope * (a.grad_scale * a.inv_t);
+      if (leader && lane == 0) {
+        stat[0] += wt * (double)p.loss;
+        stat[1] += wt * (double)p.surrogate;
+        stat[2] += wt * (double)p.kl;
+        stat[3] += wt * (double)p.ratio;
+        stat[4] += wt * (double)p.clipped;
+        stat[5] += wt * (double)p.old_kl;
+      }
+    }
+    if (leader && lane == 0) {
+      a.logp[row] = e.l;
+      if (!yok) atomicOr(a.ctx_flags, FLAG_BAD_CHOSEN);
+      else if (isnan(e.l)) atomicOr(a.ctx_flags, FLAG_NONFINITE);
+      if (!HOLD && a.state) {
+        a.state[row] = make_float4(e.M, e.lS, PREF ? (e.l - in.ref) + e.l_lo : k, e.rest);
+      }
+    }
+
+    // ---- backward
+    if (HOLD) {
+      const bool vec = ((reinterpret_cast<uintptr_t>(x) ^ reinterpret_cast<uintptr_t>(g)) & 15u) == 0;
+      const RowGrad rg{e.M, e.lS, -k, a.c2};
+      const float gy = k * e.rest;
+      int bs = held;
+      for (int32_t c = 0; c < sh.chunks; ++c) {
+        const uint4* st = reinterpret_cast<const uint4*>(sm.stage[warp][bs]) + lane;
+        const int32_t w = sh.w0 + (wg + c * GW) * RG_CHUNK;
+#pragma unroll
+        for (int q = 0; q < RG_W; ++q) {
+          const int32_t i = w + 32 * q + lane;
+          if (i < sh.w1) {
+            T* to = g + sh.rw.head + (int64_t)i * Tr::VEC;
+            put_word(to, grad_word<T>(rg, st[32 * q]), vec);
+            if (i == yw) put(to + yj, gy);
+          }
+        }
+        __syncwarp();
+        bs = bs + 1 == RG_NS ? 0 : bs + 1;
+        ++room;
+        bring();
+      }
+      if (edge) put(g + ve, ve == y ? gy : rg.one(xe));
+    }
+    in = next;
+  }
+  if (!landed) {  // a wait ran out: no copy may be in flight when the CTA ends
+    for (int i = 0; i < flying; ++i) {
+      lstage = lstage == 0 ? RG_NS - 1 : lstage - 1;
+      ring_wait_slow(bar_of(lstage), (parity >> lstage) & 1u, a.ctx_flags);
+    }
+  }
+  if (PREF || !leader || first >= a.n_rows) return;
+  // the statistics: each group's sum over its rows, then the groups' in order
+  int last = 0;
+  if (lane == 0) {
+    for (int j = 0; j < LS_NSTAT; ++j) a.part[first * LS_NSTAT + j] = stat[j];
+    last = atom_add_acq_rel(a.ticket + 1, 1) == (int)min(G, a.n_rows) - 1;
+  }
+  if (!__shfl_sync(FULL, last, 0)) return;
+  const int64_t groups = min(G, a.n_rows);
+  for (int j = 0; j < LS_NSTAT; ++j) {
+    double v = 0.;
+    for (int64_t i = lane; i < groups; i += 32) v += __ldcg(a.part + i * LS_NSTAT + j);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(FULL, v, o);
+    if (lane == 0) a.stats[j] = (float)v;
+  }
+  if (lane == 0) a.ticket[1] = 0;
+}
+
+// ---- backward from the rows' states ---------------------------------------------------------
+//
+// One CTA per segment of a row, the last rows first: those are still in L2 after the
+// forward sweep.
+constexpr int BW_NT = 256;
+constexpr int BW_W = 4;                      // words per thread
+constexpr int BW_SEG = BW_NT * BW_W;         // words of a segment
+
+template <typename T, bool PREF>
+__global__ void __launch_bounds__(BW_NT) loss_backward(const LossArgs a, int32_t segs) {
+  using Tr = Traits<T>;
+  const int tid = threadIdx.x;
+  pdl_wait();
+  pdl_trigger();
+  const int64_t row = a.n_rows - 1 - blockIdx.x / segs;
+  const int32_t seg = (int32_t)(blockIdx.x % segs);
+  const T* x = reinterpret_cast<const T*>(a.logits) + row * a.row_stride;
+  T* g = reinterpret_cast<T*>(a.grad) + row * a.grad_stride;
+  const RowWords rw = RowWords::of(x, a.vocab);
+  const uint4* xw = reinterpret_cast<const uint4*>(x + rw.head);
+  const int32_t w0 = seg * BW_SEG + tid, words = (int32_t)rw.words;
+  const bool vec = ((reinterpret_cast<uintptr_t>(x) ^ reinterpret_cast<uintptr_t>(g)) & 15u) == 0;
+  const int32_t r = __ldcg(a.row_req + row);
+  uint4 v[BW_W];
+#pragma unroll
+  for (int k = 0; k < BW_W; ++k)
+    if (r >= 0 && w0 + k * BW_NT < words) v[k] = ld_stream(xw + w0 + k * BW_NT);
+  float k = 0.f;
+  float4 st = make_float4(0.f, 0.f, 0.f, 0.f);
+  int32_t y = -1;
+  if (r >= 0) {
+    st = __ldcg(a.state + row);
+    k = PREF ? __ldcg(a.coef + r) * (a.grad_scale * a.inv_t) : st.z;
+    y = __ldcg(a.chosen + row);
+  }
+  const bool zero = r < 0 || k == 0.f;
+  const RowGrad rg{st.x, st.y, -k, a.c2};
+  const float gy = k * st.w;
+  const int64_t yo = (int64_t)y - rw.head;
+  const int32_t yw = y >= 0 && (int64_t)y < a.vocab && yo >= 0 ? (int32_t)(yo / Tr::VEC) : -1;
+#pragma unroll
+  for (int q = 0; q < BW_W; ++q) {
+    const int32_t i = w0 + q * BW_NT;
+    if (i < words) {
+      T* to = g + rw.head + (int64_t)i * Tr::VEC;
+      put_word(to, zero ? make_uint4(0u, 0u, 0u, 0u) : grad_word<T>(rg, v[q]), vec);
+      if (!zero && i == yw) put(to + (yo - (int64_t)yw * Tr::VEC), gy);
+    }
+  }
+  if (seg > 0) return;
+  const int64_t ve = tid < 8 ? (tid < rw.head ? tid : -1)
+                             : (tid - 8 < rw.tail ? rw.head + rw.words * Tr::VEC + tid - 8 : -1);
+  if (ve >= 0) put(g + ve, zero ? 0.f : (ve == y ? gy : rg.one(Tr::elem(x, ve))));
 }
 
 // ---- answer pairs -------------------------------------------------------------------------

@@ -40,11 +40,13 @@ pr_status check_loss(pr_dtype dt, const void* logits, int64_t n_rows, int64_t vo
 }
 
 // the workspace: [tickets, totals][per request][per pair][per row][per group]
-pr_status workspace(pr_ctx* c, prk::LossArgs& a, int64_t n_req, int64_t groups, bool pref) {
-  const size_t at_count = 64, at_coef = at_count + up16((size_t)n_req * 4),
-               at_term = at_coef + up16(pref ? (size_t)n_req * 4 : 0),
-               at_state = at_term + up16(pref ? (size_t)(n_req / 2) * prk::LS_NSTAT * 4 : 0),
-               at_part = at_state + (pref ? (size_t)a.n_rows * 16 : 0),
+pr_status workspace(pr_ctx* c, prk::LossArgs& a, int64_t groups, bool pref, bool state) {
+  const size_t n_req = (size_t)a.n_req, n_rows = (size_t)a.n_rows;
+  const size_t at_count = 64, at_coef = at_count + up16(n_req * 4),
+               at_term = at_coef + up16(pref ? n_req * 4 : 0),
+               at_req = at_term + up16(pref ? n_req / 2 * prk::LS_NSTAT * 4 : 0),
+               at_state = at_req + up16(n_rows * 4),
+               at_part = at_state + (state ? n_rows * 16 : 0),
                bytes = at_part + (pref ? 0 : (size_t)groups * prk::LS_NSTAT * 8);
   if (bytes > c->loss_ws_bytes) {
     PR_CUDA(cudaDeviceSynchronize());  // kernels may still use the old one
@@ -67,31 +69,145 @@ pr_status workspace(pr_ctx* c, prk::LossArgs& a, int64_t n_req, int64_t groups, 
   a.count = reinterpret_cast<int32_t*>(w + at_count);
   a.coef = reinterpret_cast<float*>(w + at_coef);
   a.term = reinterpret_cast<float*>(w + at_term);
-  a.state = reinterpret_cast<float4*>(w + at_state);
+  a.row_req = reinterpret_cast<int32_t*>(w + at_req);
+  a.state = state ? reinterpret_cast<float4*>(w + at_state) : nullptr;
   a.part = reinterpret_cast<double*>(w + at_part);
   return PR_OK;
 }
 
-pr_status launch(const void* kern, dim3 grid, unsigned threads, void** args, cudaStream_t s) {
+pr_status launch(const void* kern, unsigned grid, unsigned threads, size_t smem, unsigned cluster,
+                 void** args, cudaStream_t s) {
   cudaLaunchConfig_t cfg;
   memset(&cfg, 0, sizeof cfg);
-  cfg.gridDim = grid;
+  cfg.gridDim = dim3(grid);
   cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
   cfg.stream = s;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchAttribute attr[2];
+  int n = 0;
+  attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[n++].val.programmaticStreamSerializationAllowed = 1;
+  if (cluster > 1) {
+    attr[n].id = cudaLaunchAttributeClusterDimension;
+    attr[n].val.clusterDim.x = cluster;
+    attr[n].val.clusterDim.y = 1;
+    attr[n++].val.clusterDim.z = 1;
+  }
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = n;
   PR_CUDA(cudaLaunchKernelExC(&cfg, kern, args));
   g_launches.fetch_add(1, std::memory_order_relaxed);
   return PR_OK;
 }
 
-template <int KIND>
-const void* row_kernel(pr_dtype dt) {
-  return dt == PR_DTYPE_BF16 ? reinterpret_cast<const void*>(&prk::loss_rows<__nv_bfloat16, KIND>)
-                             : reinterpret_cast<const void*>(&prk::loss_rows<float, KIND>);
+template <typename T, int GW>
+const void* ring_kernel(bool hold, bool pref) {
+  return pref ? reinterpret_cast<const void*>(&prk::loss_ring<T, GW, false, true>)
+              : hold ? reinterpret_cast<const void*>(&prk::loss_ring<T, GW, true, false>)
+                     : reinterpret_cast<const void*>(&prk::loss_ring<T, GW, false, false>);
+}
+template <typename T>
+const void* ring_kernel(int gw, bool hold, bool pref) {
+  return gw == 1 ? ring_kernel<T, 1>(hold, pref)
+                 : gw == 4 ? ring_kernel<T, 4>(hold, pref) : ring_kernel<T, 16>(hold, pref);
+}
+
+// Warps of a row: `gw` of a CTA, in `cluster` CTAs.
+struct RowShape {
+  int gw, cluster;
+  bool hold;        // a row's chunks fit the group's rings
+  int64_t groups;   // rows in work at a time
+  unsigned grid;
+};
+
+constexpr int WARPS[] = {1, 4, 16, 32, 64, 128};  // of a row: of a CTA, then of 2, 4, 8 CTAs
+
+// shared memory opt-ins, and the rows that the GPU has room for at each width; once per
+// context
+pr_status ring_setup(pr_ctx* c) {
+  if (c->loss_ready) return PR_OK;
+  for (int gw : {1, 4, 16})
+    for (int m = 0; m < 3; ++m)
+      for (const void* f : {ring_kernel<__nv_bfloat16>(gw, m == 1, m == 2),
+                            ring_kernel<float>(gw, m == 1, m == 2)})
+        PR_CUDA(cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                     (int)sizeof(prk::RingSmem)));
+  for (int i = 0; i < 6; ++i) {
+    if (WARPS[i] <= 16) {
+      c->loss_places[i] = c->num_sms * (16 / WARPS[i]);
+      continue;
+    }
+    cudaLaunchConfig_t cfg;
+    memset(&cfg, 0, sizeof cfg);
+    cfg.gridDim = dim3((unsigned)(WARPS[i] / 16));
+    cfg.blockDim = dim3(prk::RG_NW * 32);
+    cfg.dynamicSmemBytes = sizeof(prk::RingSmem);
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)(WARPS[i] / 16);
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    int n = 0;
+    PR_CUDA(cudaOccupancyMaxActiveClusters(&n, ring_kernel<__nv_bfloat16>(16, true, false), &cfg));
+    c->loss_places[i] = std::max(n, 1);
+  }
+  c->loss_ready = true;
+  return PR_OK;
+}
+
+// The narrowest group whose rings hold a row and leave room for the next one's first
+// chunks (RG_NS - 2 chunks per warp); wider ones while all rows have a place at once.
+RowShape choose_shape(const pr_ctx* c, pr_dtype dt, int64_t n_rows, int64_t vocab) {
+  const int64_t words = (vocab * (int64_t)esize(dt)) / 16;
+  const int64_t chunks = (words + prk::RG_CHUNK - 1) / prk::RG_CHUNK;
+  auto per_warp = [&](int w) { return (chunks + w - 1) / w; };
+  int i = 0;
+  while (i < 5 && per_warp(WARPS[i]) > prk::RG_NS - 2) ++i;
+  while (i < 5 && n_rows <= c->loss_places[i + 1] && chunks >= 2 * WARPS[i]) ++i;
+  RowShape s;
+  s.gw = std::min(WARPS[i], 16);
+  s.cluster = std::max(1, WARPS[i] / 16);
+  s.hold = per_warp(WARPS[i]) <= prk::RG_NS;
+  s.groups = std::min<int64_t>(n_rows, c->loss_places[i]);
+  const int64_t per_cta = 16 / s.gw;
+  s.grid = (unsigned)(s.cluster > 1 ? s.groups * s.cluster : (s.groups + per_cta - 1) / per_cta);
+  return s;
+}
+
+pr_status launch_plan(pr_ctx* c, prk::LossArgs& a, int pairs, cudaStream_t s) {
+  const int64_t grid = a.n_req + (a.n_rows + 255) / 256;
+  if (grid > 0x7fffffffLL) return PR_ERR_INVALID_ARG;
+  void* args[] = {&a, &pairs};
+  const pr_status st = launch(reinterpret_cast<const void*>(&prk::loss_plan), (unsigned)grid, 256,
+                              0, 1, args, s);
+  return st == PR_OK ? timing_mark(c, s) : st;
+}
+
+pr_status launch_ring(pr_ctx* c, prk::LossArgs& a, pr_dtype dt, const RowShape& shape, bool hold,
+                      bool pref, cudaStream_t s) {
+  const void* kern = dt == PR_DTYPE_BF16 ? ring_kernel<__nv_bfloat16>(shape.gw, hold, pref)
+                                         : ring_kernel<float>(shape.gw, hold, pref);
+  void* args[] = {&a};
+  const pr_status st = launch(kern, shape.grid, prk::RG_NW * 32, sizeof(prk::RingSmem),
+                              (unsigned)shape.cluster, args, s);
+  return st == PR_OK ? timing_mark(c, s) : st;
+}
+
+pr_status launch_backward(pr_ctx* c, prk::LossArgs& a, pr_dtype dt, bool pref, cudaStream_t s) {
+  const int64_t words = (a.vocab * (int64_t)esize(dt)) / 16;
+  int32_t segs = (int32_t)std::max<int64_t>(1, (words + prk::BW_SEG - 1) / prk::BW_SEG);
+  if (a.n_rows * segs > 0x7fffffffLL) return PR_ERR_INVALID_ARG;
+  void* args[] = {&a, &segs};
+  const void* kern =
+      dt == PR_DTYPE_BF16
+          ? (pref ? reinterpret_cast<const void*>(&prk::loss_backward<__nv_bfloat16, true>)
+                  : reinterpret_cast<const void*>(&prk::loss_backward<__nv_bfloat16, false>))
+          : (pref ? reinterpret_cast<const void*>(&prk::loss_backward<float, true>)
+                  : reinterpret_cast<const void*>(&prk::loss_backward<float, false>));
+  const pr_status st = launch(kern, (unsigned)(a.n_rows * segs), prk::BW_NT, 0, 1, args, s);
+  return st == PR_OK ? timing_mark(c, s) : st;
 }
 
 void fill(prk::LossArgs& a, pr_ctx* c, const void* logits, int64_t n_rows, int64_t vocab,
@@ -155,20 +271,14 @@ pr_status pr_policy_loss(pr_ctx* c, const void* logits, pr_dtype dt, int64_t n_r
   a.clip_lo = 1.f - p->clip_low;
   a.clip_hi = 1.f + p->clip_high;
   a.kl_coef = p->kl_coef;
-  const int64_t grid = std::min<int64_t>(n_rows, (int64_t)c->num_sms * 4);
-  if ((st = workspace(c, a, a.n_req, grid, false)) != PR_OK) return st;
+  if ((st = ring_setup(c)) != PR_OK) return st;
+  const RowShape shape = choose_shape(c, dt, n_rows, vocab);
+  const bool hold = grad && shape.hold, later = grad && !shape.hold;
+  if ((st = workspace(c, a, shape.groups, false, later)) != PR_OK) return st;
   if ((st = timing_begin(c, s)) != PR_OK) return st;
-  int pairs = 0;
-  void* pargs[] = {&a, &pairs};
-  if ((st = launch(reinterpret_cast<const void*>(&prk::loss_plan), dim3((unsigned)a.n_req), 256,
-                   pargs, s)) != PR_OK)
-    return st;
-  if ((st = timing_mark(c, s)) != PR_OK) return st;
-  void* args[] = {&a};
-  if ((st = launch(row_kernel<prk::LOSS_POLICY>(dt), dim3((unsigned)grid), prk::LS_NT, args, s)) !=
-      PR_OK)
-    return st;
-  return timing_mark(c, s);
+  if ((st = launch_plan(c, a, 0, s)) != PR_OK) return st;
+  if ((st = launch_ring(c, a, dt, shape, hold, false, s)) != PR_OK) return st;
+  return later ? launch_backward(c, a, dt, false, s) : PR_OK;
 }
 
 pr_status pr_preference_loss(pr_ctx* c, const void* logits, pr_dtype dt, int64_t n_rows,
@@ -200,31 +310,18 @@ pr_status pr_preference_loss(pr_ctx* c, const void* logits, pr_dtype dt, int64_t
   a.margin = p->margin;
   a.loss = p->loss;
   a.length_norm = p->length_norm ? 1 : 0;
-  const int64_t grid = std::min<int64_t>(std::max<int64_t>(n_rows, 1), (int64_t)c->num_sms * 4);
-  if ((st = workspace(c, a, n_req, 0, true)) != PR_OK) return st;
+  if ((st = ring_setup(c)) != PR_OK) return st;
+  const RowShape shape = choose_shape(c, dt, n_rows, vocab);
+  if ((st = workspace(c, a, 0, true, true)) != PR_OK) return st;
   if ((st = timing_begin(c, s)) != PR_OK) return st;
-  int pairs = 1;
-  void* pargs[] = {&a, &pairs};
-  if ((st = launch(reinterpret_cast<const void*>(&prk::loss_plan), dim3((unsigned)n_req), 256,
-                   pargs, s)) != PR_OK)
-    return st;
-  if ((st = timing_mark(c, s)) != PR_OK) return st;
+  if ((st = launch_plan(c, a, 1, s)) != PR_OK) return st;
+  if (n_rows > 0 && (st = launch_ring(c, a, dt, shape, false, true, s)) != PR_OK) return st;
   void* args[] = {&a};
-  if ((st = launch(row_kernel<prk::LOSS_PREF_FWD>(dt), dim3((unsigned)grid), prk::LS_NT, args,
-                   s)) != PR_OK)
+  if ((st = launch(reinterpret_cast<const void*>(&prk::loss_pairs), (unsigned)((n_req / 2 + 7) / 8),
+                   256, 0, 1, args, s)) != PR_OK ||
+      (st = timing_mark(c, s)) != PR_OK)
     return st;
-  if ((st = timing_mark(c, s)) != PR_OK) return st;
-  if ((st = launch(reinterpret_cast<const void*>(&prk::loss_pairs),
-                   dim3((unsigned)((n_req / 2 + 7) / 8)), 256, args, s)) != PR_OK)
-    return st;
-  if ((st = timing_mark(c, s)) != PR_OK) return st;
-  if (grad && n_rows > 0) {
-    if ((st = launch(row_kernel<prk::LOSS_PREF_BWD>(dt), dim3((unsigned)grid), prk::LS_NT, args,
-                     s)) != PR_OK)
-      return st;
-    return timing_mark(c, s);
-  }
-  return PR_OK;
+  return grad && n_rows > 0 ? launch_backward(c, a, dt, true, s) : PR_OK;
 }
 
 }  // extern "C"
