@@ -65,7 +65,7 @@ struct pr_ctx {
   void* loss_ws = nullptr;
   size_t loss_ws_bytes = 0;
   bool loss_ready = false;             // shared memory opt-ins made
-  int loss_places[6] = {};             // rows in work at a time, per width of a row's group
+  int loss_places[2][4] = {};          // clusters of 1, 2, 4, 8 CTAs resident; half, all of the SMs
   // PR_OPT_TIMING: events after each kernel of the last multi-kernel call
   int32_t timing = 0;
   cudaEvent_t tev[PR_MAX_TIMED + 1] = {};

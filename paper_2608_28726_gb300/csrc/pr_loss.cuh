@@ -4,15 +4,16 @@
 // Row t with logits x, emitted token y and temperature T has z = x / T,
 // l = z_y - log sum_v exp(z_v), and for any loss L that depends on the row through
 // l alone dL/dx_v = (dL/dl) (onehot_y(v) - p_v) / T, p = softmax(z).  So a row needs
-// two sweeps over its logits, with the scalar dL/dl between them:
-//   forward   M = max x and S = sum 2^(c (x - M)), c = log2(e) / T; both are kept
-//             against a reference m of each thread's own: x - m is exact where it
-//             matters (equal logits of any magnitude give 2^0), -inf gives 2^-inf = 0,
-//             and the lowest finite value is a maximum like any other
-//   backward  g_v = dL/dl / T (onehot - 2^(c (x_v - M) - log2 S))
-// The emitted token's own term e_y stays out of the forward sum: with R the sum of the
-// others, 1 - p_y = R / (R + e_y) and l = -log(1 + R / e_y) keep their relative
-// accuracy where p_y is close to 1 and 1 - p_y or log(R + e_y) would cancel.
+// two sweeps over its logits, with the scalar dL/dl between them.  With c = log2(e) / T:
+//   forward   R = sum over v != y of 2^(c x_v - k), k a reference that each thread takes
+//             from its first logits and raises only where the sum would overflow
+//   backward  g_v = dL/dl / T (onehot - 2^(c x_v - K)), K = k + log2(R + e_y)
+// one FMA and one ex2 per logit and sweep.  The emitted token's own term e_y stays out
+// of the forward sum: 1 - p_y = R / (R + e_y) and l = -log(1 + R / e_y) keep their
+// relative accuracy where p_y is close to 1 and 1 - p_y or log(R + e_y) would cancel.
+// Rows whose sum is 0 or not finite that way (NaN, infinities, logits beyond 1e38) are
+// summed again with c (x_v - M) in place of c x_v - k, M the row's maximum: exact for
+// equal logits of any magnitude, and what is NaN then is NaN by the formula.
 // The policy loss' dL/dl needs the row alone; the preference loss' needs the log
 // ratios of the row's whole answer pair.
 #pragma once
@@ -38,7 +39,7 @@ struct LossArgs {
   float clip_lo, clip_hi, kl_coef;
   float beta, smooth, margin;
   int32_t loss, length_norm;
-  float inv_t, c2, skew;  // 1 / T, log2(e) / T, c2 ln 2 - inv_t
+  float inv_t, c2;  // 1 / T, log2(e) / T
   float grad_scale;
   float* stats;
   float* ratio;
@@ -52,7 +53,7 @@ struct LossArgs {
   int32_t* row_req;    // [n_rows] request of a row that counts, else -1
   float* coef;         // [n_req] dL / d log ratio (preference)
   float* term;         // [n_req / 2][LS_NSTAT] the pairs' statistics
-  float4* state;       // [n_rows] M, log2 S, l - ref (preference) or dL/dx's factor, 1 - p_y
+  float4* state;       // [n_rows][2] K, adj, rest, M; l - ref (preference) or dL/dl / T
   double* part;        // [groups][LS_NSTAT] statistics of each group's rows
   uint32_t* ctx_flags;
 };
@@ -162,46 +163,9 @@ __device__ __forceinline__ PolicyTerms policy_terms(const LossArgs& a, float l, 
 
 // ---- a row's words ------------------------------------------------------------------------
 
-// the factor from the reference m to M: expf, whose mean error is a tenth of ex2's
-// (below): a row's sum would take that on at each step of its merges
-__device__ __forceinline__ float rescale(float m, float M, float inv_t) {
-  return expf((m - M) * inv_t);
-}
-
-// running (m, S): S = sum 2^(c (x - m)).  m is raised when a word goes past it by
-// enough that S could grow out of proportion, not at every new maximum.
-struct RowSum {
-  float m;
-  float2 S;
-  __device__ __forceinline__ void reset() {
-    m = LS_MIN;
-    S = make_float2(0.f, 0.f);
-  }
-  __device__ __forceinline__ void raise(float top, float c2, float inv_t) {
-    if ((top - m) * c2 > 8.f) {
-      const float f = rescale(m, top, inv_t);
-      S = __fmul2_rn(S, make_float2(f, f));
-      m = top;
-    }
-  }
-  __device__ __forceinline__ void add2(float x, float y, float c2) {
-    float2 d = __fadd2_rn(make_float2(x, y), make_float2(-m, -m));
-    d = __fmul2_rn(d, make_float2(c2, c2));
-    S = __fadd2_rn(S, make_float2(ex2(d.x), ex2(d.y)));
-  }
-  __device__ __forceinline__ void add1(float x, float c2, float inv_t) {
-    if (x != x) S.x = x;
-    raise(x, c2, inv_t);
-    S.x += ex2((x - m) * c2);
-  }
-};
-
-template <typename T>
-__device__ __forceinline__ void add_word(RowSum& s, const uint4& w, float c2) {
-  using Tr = Traits<T>;
-#pragma unroll
-  for (int j = 0; j < Tr::VEC; j += 2) s.add2(Tr::at(w, j), Tr::at(w, j + 1), c2);
-}
+// 2^d for the factors between references: expf, whose mean error is a tenth of ex2's
+// (-5e-8): a row's sum would take that on at each step of its merges
+__device__ __forceinline__ float rescale2(float d) { return expf(d * LN2); }
 
 // the word without its element j
 template <typename T>
@@ -219,42 +183,50 @@ __device__ __forceinline__ uint4 without(uint4 w, int j) {
   return w;
 }
 
-// A row's state from R = sum over the other tokens of 2^(c (x_v - m)) and the emitted
-// token's logit: M, log2 S, 1 - p_y, and l = l_hi + l_lo: a log ratio sums hundreds of
-// differences l - ref, whose errors must neither be l's rounding (2^-24 |l|) nor
-// lean to one side.  So ln S = e ln 2 + ln f is taken with e ln 2 in two parts (Cody
-// and Waite's reduction; the first product is exact), c (x_y - M) keeps its rounding, the
-// scale is the one that the sums were taken with (c2, not 1 / T: an error common to both
-// cancels in the mean), and ex2's mean error, -5.1e-8 relative over 2^24 arguments in
-// [-30, 0], is added back.  Mean error of l over sampled rows: 1e-7 without all this.
-constexpr float LN2_A = 0.693145751953125f;       // ln 2 to 16 bits
-constexpr float LN2_B = 1.42860682e-06f;  // ln 2 - LN2_A
-constexpr float EX2_LOW = 5.1e-8f;
+// S += sum of 2^(c x - k) over the word
+template <typename T>
+__device__ __forceinline__ void add_word(float2& S, const uint4& w, float c2, float nk) {
+  using Tr = Traits<T>;
+#pragma unroll
+  for (int j = 0; j < Tr::VEC; j += 2) {
+    const float2 d = __ffma2_rn(make_float2(Tr::at(w, j), Tr::at(w, j + 1)),
+                                make_float2(c2, c2), make_float2(nk, nk));
+    S = __fadd2_rn(S, make_float2(ex2(d.x), ex2(d.y)));
+  }
+}
+
+// A row's l = l_hi + l_lo, 1 - p_y and log2 S = e + f, from R and u + u_lo, the emitted
+// token's exponent against the same reference; shift: what the reference was raised by.
+// A log ratio sums hundreds of differences l - ref, whose errors must neither be
+// l's rounding (2^-24 |l|) nor lean to one side.  So sums and products keep their
+// roundings, the scale is the one that the row's sum was taken with (an error of c common
+// to both has no mean over sampled tokens), and factors between references come from
+// rescale2.  Mean error of l over sampled rows: below 2e-8 (1e-7 without all this).
+constexpr float LN2_LOW = -1.90465421e-9f;  // ln 2 - LN2
 struct RowEnd {
-  float M, lS, l, l_lo, rest;
-  __device__ __forceinline__ RowEnd(const LossArgs& a, float m, float R, float xy, bool ok) {
-    M = ok ? fmaxf(m, xy) : m;  // (an xy of NaN leaves m, and its term is NaN)
-    R *= rescale(m, M, a.inv_t);
-    const float ey = ok ? ex2((xy - M) * a.c2) : NAN;
+  float l, l_lo, rest, shift, e, f;
+  __device__ __forceinline__ RowEnd(float R, float u, float u_lo) {
+    shift = fmaxf(u, 0.f);
+    if (u > 0.f) R *= rescale2(-u);
+    const float ey = u > 0.f ? 1.f : ex2(u);
     const float S = R + ey;
-    lS = log2f(S);
+    int ei = (int)(__float_as_uint(S) >> 23) - 127;
+    float m = __uint_as_float((__float_as_uint(S) & 0x7fffffu) | 0x3f800000u);
+    if (m > 1.41f) {
+      m *= 0.5f;
+      ++ei;
+    }
+    e = (float)ei;
+    f = log2f(m);
     rest = R / S;
     if (ey > 0.25f * S) {
-      const float q = R / ey;
-      l = -log1pf(fmaf(q, EX2_LOW, q));
+      l = -log1pf(R / ey);
       l_lo = 0.f;
     } else {
-      const float d = xy - M, u = d * a.inv_t;
-      int e = (int)(__float_as_uint(S) >> 23) - 127;
-      float f = __uint_as_float((__float_as_uint(S) & 0x7fffffu) | 0x3f800000u);
-      if (f > 1.41f) {
-        f *= 0.5f;
-        ++e;
-      }
-      const float big = (float)e * LN2_A, hi = u - big, t = hi - u;
-      float lo = (u - (hi - t)) + (-big - t);  // hi's rounding
-      lo += fmaf(d, a.inv_t, -u) + d * a.skew;
-      lo -= log1pf(f - 1.f) + fmaf((float)e, LN2_B, EX2_LOW);
+      const float v = u - shift, w = v - e, t = w - v;  // w's rounding: (v - (w - t)) + (-e - t)
+      const float w_lo = ((v - (w - t)) + (-e - t)) + u_lo - f;
+      const float hi = w * LN2;
+      const float lo = fmaf(w, LN2, -hi) + w * LN2_LOW + w_lo * LN2;
       l = hi + lo;
       l_lo = (hi - l) + lo;
       if (u == -INFINITY) {  // a masked token
@@ -266,38 +238,58 @@ struct RowEnd {
   }
 };
 
-// backward of two logits: nk (p_x, p_y), nk = -dL/dl / T
-struct RowGrad {
-  float M, lS, nk, c2;
-  __device__ __forceinline__ float2 two(float x, float y) const {
-    float2 d = __fadd2_rn(make_float2(x, y), make_float2(-M, -M));
-    d = __ffma2_rn(d, make_float2(c2, c2), make_float2(-lS, -lS));
-    return __fmul2_rn(make_float2(ex2(d.x), ex2(d.y)), make_float2(nk, nk));
-  }
-  __device__ __forceinline__ float one(float x) const { return nk * ex2(fmaf(x - M, c2, -lS)); }
+// What a row's backward sweep needs: entries nk 2^(c x - K) (FAST), nk 2^(c (x - M) - K)
+// (ROBUST) or 0; gy at the emitted token.
+enum RowMode { ROW_ZERO = 0, ROW_FAST = 1, ROW_ROBUST = 2 };
+struct RowOut {
+  float K, nk, gy, M;
+  int mode;
 };
+struct RowState {   // the same before dL/dl is known
+  float K, adj, rest, M;  // adj: 2^-(what K lost to rounding)
+};
+__device__ __forceinline__ RowOut row_out(const RowState& s, float k) {
+  RowOut o;
+  o.K = s.K;
+  o.nk = -k * s.adj;
+  o.gy = k * s.rest;
+  o.M = s.M;
+  o.mode = k == 0.f ? ROW_ZERO : s.M == INFINITY ? ROW_FAST : ROW_ROBUST;
+  return o;
+}
 
+template <bool ROBUST>
+__device__ __forceinline__ float2 grad2(const RowOut& o, float c2, float x, float y) {
+  float2 d = make_float2(x, y);
+  if (ROBUST) d = __fadd2_rn(d, make_float2(-o.M, -o.M));
+  d = __ffma2_rn(d, make_float2(c2, c2), make_float2(-o.K, -o.K));
+  return __fmul2_rn(make_float2(ex2(d.x), ex2(d.y)), make_float2(o.nk, o.nk));
+}
+__device__ __forceinline__ float grad1(const RowOut& o, float c2, float x) {
+  if (o.mode == ROW_ZERO) return 0.f;
+  return o.mode == ROW_FAST ? grad2<false>(o, c2, x, x).x : grad2<true>(o, c2, x, x).x;
+}
 __device__ __forceinline__ uint32_t bf16_pair(float2 v) {
   const __nv_bfloat162 h = __float22bfloat162_rn(v);
   return *reinterpret_cast<const uint32_t*>(&h);
 }
-template <typename T>
-__device__ __forceinline__ uint4 grad_word(const RowGrad& g, const uint4& w) {
+template <typename T, bool ROBUST>
+__device__ __forceinline__ uint4 grad_word(const RowOut& o, float c2, const uint4& w) {
   using Tr = Traits<T>;
   if constexpr (sizeof(T) == 2) {
-    return make_uint4(bf16_pair(g.two(Tr::at(w, 0), Tr::at(w, 1))),
-                      bf16_pair(g.two(Tr::at(w, 2), Tr::at(w, 3))),
-                      bf16_pair(g.two(Tr::at(w, 4), Tr::at(w, 5))),
-                      bf16_pair(g.two(Tr::at(w, 6), Tr::at(w, 7))));
+    return make_uint4(bf16_pair(grad2<ROBUST>(o, c2, Tr::at(w, 0), Tr::at(w, 1))),
+                      bf16_pair(grad2<ROBUST>(o, c2, Tr::at(w, 2), Tr::at(w, 3))),
+                      bf16_pair(grad2<ROBUST>(o, c2, Tr::at(w, 4), Tr::at(w, 5))),
+                      bf16_pair(grad2<ROBUST>(o, c2, Tr::at(w, 6), Tr::at(w, 7))));
   } else {
-    const float2 u = g.two(Tr::at(w, 0), Tr::at(w, 1)), v = g.two(Tr::at(w, 2), Tr::at(w, 3));
+    const float2 u = grad2<ROBUST>(o, c2, Tr::at(w, 0), Tr::at(w, 1));
+    const float2 v = grad2<ROBUST>(o, c2, Tr::at(w, 2), Tr::at(w, 3));
     return make_uint4(__float_as_uint(u.x), __float_as_uint(u.y), __float_as_uint(v.x),
                       __float_as_uint(v.y));
   }
 }
 __device__ __forceinline__ void put(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
 __device__ __forceinline__ void put(float* p, float v) { *p = v; }
-
 template <typename T>
 __device__ __forceinline__ void put_word(T* p, const uint4& w, bool vec) {
   if (vec) {
@@ -324,351 +316,700 @@ struct RowWords {
   }
 };
 
-// ---- forward: rows through rings of shared memory ---------------------------------------
-//
-// A group of warps takes a row: 1, 4 or the 16 warps of a CTA, or 16 of each CTA of a
-// cluster.  Warp w of the group takes every w-th chunk of 2 KB of (its CTA's share of)
-// the row, brings it into a ring of its own with one bulk copy, and runs ahead over its
-// next rows as far as the ring has room: nothing but the row's two sums is ever
-// waited for together.  With HOLD a row's chunks stay in the ring for the backward
-// sweep, so that its logits are read from memory once; a stage is free, and the next
-// row's chunk on its way into it, as soon as its part of the gradient is written.
-// What does not fit (or has to wait for other rows: answer pairs) leaves the row's
-// state to loss_backward.
-constexpr int RG_NW = 16;
-constexpr int RG_W = 4;                        // words per lane and chunk
-constexpr int RG_CHUNK = 32 * RG_W;            // words of a chunk
-constexpr int RG_BYTES = 16 * RG_CHUNK;
-constexpr int RG_NS = 7;                       // stages per warp
-struct RingSmem {
-  unsigned char stage[RG_NW][RG_NS][RG_BYTES];
-  uint64_t bar[RG_NW][RG_NS];
-  float2 part[2][RG_NW * MAXC];                // the warps' (m, R), two rows deep
-};
-static_assert(sizeof(RingSmem) <= 232448, "227 KB");
+// ---- a row among CTAs -------------------------------------------------------------------
 
-// a group's share of a row: its words, those of this CTA, and this warp's chunks of those
+// a CTA's part of a row
 struct Share {
-  const char* x;       // the row
-  RowWords rw;
-  int32_t w0, w1;      // this CTA's words [w0, w1)
-  int32_t chunks;      // this warp's chunks
+  const char* x;              // the row
+  int32_t head, tail, words;  // elements before its 16-byte words and after them
+  int32_t w0, w1;             // this CTA's words [w0, w1)
 };
-template <typename T, int GW>
-__device__ __forceinline__ Share share_of(const LossArgs& a, int64_t row, uint32_t C, uint32_t rank,
-                                          int wg) {
+constexpr int SH_CHUNK = 1024;  // a CTA's part is a multiple of so many words
+template <typename T>
+__device__ __forceinline__ Share share_of(const LossArgs& a, int64_t row, uint32_t C,
+                                          uint32_t rank) {
+  constexpr uint32_t VEC = Traits<T>::VEC;
   Share s;
   const T* x = reinterpret_cast<const T*>(a.logits) + row * a.row_stride;
   s.x = reinterpret_cast<const char*>(x);
-  s.rw = RowWords::of(x, a.vocab);
-  const int32_t words = (int32_t)s.rw.words;
-  const int32_t all = (words + RG_CHUNK - 1) / RG_CHUNK;
-  const int32_t per = GW < RG_NW ? all : (all + (int32_t)C - 1) / (int32_t)C;  // chunks of a CTA
-  s.w0 = min(words, (int32_t)rank * per * RG_CHUNK);
-  s.w1 = min(words, s.w0 + per * RG_CHUNK);
-  const int32_t mine = (s.w1 - s.w0 + RG_CHUNK - 1) / RG_CHUNK;
-  s.chunks = mine > wg ? (mine - wg + GW - 1) / GW : 0;
+  const uint32_t off = ((uint32_t)reinterpret_cast<uintptr_t>(x) & 15u) / (uint32_t)sizeof(T);
+  const uint32_t V = (uint32_t)a.vocab, head = min(off ? VEC - off : 0u, V);
+  const uint32_t words = (V - head) / VEC;
+  s.head = (int32_t)head;
+  s.words = (int32_t)words;
+  s.tail = (int32_t)(V - head - words * VEC);
+  s.w0 = 0;
+  s.w1 = s.words;
+  if (C > 1) {
+    const uint32_t all = (words + SH_CHUNK - 1) / SH_CHUNK, per = (all + C - 1) / C * SH_CHUNK;
+    s.w0 = (int32_t)min(words, rank * per);
+    s.w1 = (int32_t)min(words, (uint32_t)s.w0 + per);
+  }
   return s;
 }
+// the emitted token's word, or -1
+template <typename T>
+__device__ __forceinline__ int32_t word_of(const LossArgs& a, const Share& s, int32_t y) {
+  return y >= s.head && y < (int32_t)a.vocab - s.tail ? (y - s.head) / Traits<T>::VEC : -1;
+}
+// the element of this lane before or after the row's words, or -1
+__device__ __forceinline__ int32_t end_of(const LossArgs& a, const Share& s, int lane) {
+  return lane < 8 ? (lane < s.head ? lane : -1)
+                  : (lane - 8 < s.tail ? (int32_t)a.vocab - s.tail + lane - 8 : -1);
+}
 
-// what a row's epilogue needs, fetched while the rows before it are in work
+// what a row's end needs, fetched while the rows before it are in work
 struct RowIn {
   int32_t r, y, count;
-  float xy, old, ref, adv;
+  float xy, old, ref, adv, edge;
 };
 
-template <typename T, int GW, bool HOLD, bool PREF>
-__global__ void __launch_bounds__(RG_NW * 32, 1) loss_ring(const LossArgs a) {
+// The sum of a row (in a cluster: of this CTA's part of it) once more in M's terms, by one
+// warp from global memory.  Rows with NaN or infinities, or of nothing but masked or
+// lowest values.
+template <typename T>
+__device__ __noinline__ void robust_sum(const LossArgs& a, const Share s, bool ends, int32_t y,
+                                        float& M, float& R, int lane) {
+  using Tr = Traits<T>;
+  const T* x = reinterpret_cast<const T*>(s.x);
+  M = LS_MIN;
+  float sum = 0.f;
+  const int64_t lo = ends && s.w0 == 0 ? 0 : s.head + (int64_t)s.w0 * Tr::VEC;
+  const int64_t hi = ends && s.w0 == 0 && s.w1 == s.words ? a.vocab
+                                                         : s.head + (int64_t)s.w1 * Tr::VEC;
+  auto add = [&](int64_t v) {
+    const float e = Tr::elem(x, v);
+    if (v == y) return;
+    if (e != e) sum = e;
+    if (e > M) {
+      sum *= rescale2((M - e) * a.c2);
+      M = e;
+    }
+    sum += ex2((e - M) * a.c2);
+  };
+  for (int64_t v = lo + lane; v < hi; v += 32) add(v);
+  if (ends && hi < a.vocab && lane < s.tail) add(a.vocab - s.tail + lane);
+  const float m = unord(__reduce_max_sync(FULL, ord(M)));
+  R = sum * rescale2((M - m) * a.c2);
+  M = m;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) R += __shfl_xor_sync(FULL, R, o);
+}
+
+constexpr int RG_TERMS = 5;  // statistics that are summed row by row
+
+// A row's end from its sums: R against 2^k, or against its maximum M where that is not
+// infinite.  Writes logp, the statistics' terms (weight wt), and the result: to `out`
+// with HOLD, else the row's state.  Whole warp; apart from the kernel's registers.
+template <bool HOLD, bool PREF>
+__device__ __noinline__ void end_math(const LossArgs& a, int64_t row, const RowIn in, float k,
+                                      float R, float M, float wt, bool writes, RowOut* out,
+                                      float2* stat, int lane) {
+  float u, u_lo = 0.f;
+  bool far = false;
+  if (M == INFINITY) {
+    const float h = in.xy * a.c2, hl = fmaf(in.xy, a.c2, -h);
+    u = h - k;
+    if (isfinite(h)) {  // h's and the difference's roundings: 2^-9 where logits are about 3e4
+      const float t = u - h, left = ((h - (u - t)) + (-k - t)) + hl, all = u + left;
+      u_lo = (u - all) + left;
+      u = all;
+    }
+  } else {
+    const float d = in.xy - M;
+    u = d * a.c2;
+    if (isfinite(u)) u_lo = fmaf(d, a.c2, -u);
+    else far = d > -INFINITY;  // a finite logit that many below the maximum
+    k = 0.f;
+  }
+  const RowEnd e(R, u, u_lo);
+  const float l = far && e.l == -INFINITY ? (in.xy - M) * a.inv_t : e.l;
+  // K = k + shift + e + f, and what its rounding left
+  RowState st;
+  const float b = k + e.shift, bt = b - k, b_lo = (k - (b - bt)) + (e.shift - bt);
+  const float c = b + e.e, ct = c - b, c_lo = (b - (c - ct)) + (e.e - ct);
+  st.K = c + e.f;
+  st.adj = exp2f(-(((c - st.K) + e.f) + (b_lo + c_lo)));
+  st.rest = e.rest;
+  st.M = M;
+  RowOut o;
+  o.mode = ROW_ZERO;
+  o.K = o.nk = o.gy = 0.f;
+  o.M = M;
+  float kk = 0.f;
+  if (!PREF) {
+    const PolicyTerms p = policy_terms(a, l, e.l_lo, in.old, in.ref, in.adv);
+    kk = wt * p.slope * (a.grad_scale * a.inv_t);
+    if (lane < RG_TERMS) {
+      const float x = wt * (lane == 0 ? p.surrogate : lane == 1 ? p.kl : lane == 2 ? p.ratio
+                                                  : lane == 3 ? p.clipped : p.old_kl);
+      const float2 q = stat[lane];
+      const float y = q.x + x, z = y - q.x;
+      stat[lane] = make_float2(y, q.y + ((q.x - (y - z)) + (x - z)));
+    }
+    if (HOLD) o = row_out(st, kk);
+  }
+  if (lane == 0) {
+    *out = o;
+    if (writes) {
+      a.logp[row] = l;
+      if (in.y < 0 || (int64_t)in.y >= a.vocab) atomicOr(a.ctx_flags, FLAG_BAD_CHOSEN);
+      else if (isnan(l)) atomicOr(a.ctx_flags, FLAG_NONFINITE);
+      if (!HOLD && a.state) {
+        a.state[2 * row] = make_float4(st.K, st.adj, st.rest, st.M);
+        a.state[2 * row + 1].x = PREF ? (l - in.ref) + e.l_lo : kk;
+      }
+    }
+  }
+}
+
+// The scalars of row `row` of request r with token y.  Whole warp.
+template <typename T, bool PREF>
+__device__ __forceinline__ RowIn fetch_row(const LossArgs& a, const Share& s, int64_t row,
+                                           int32_t r, int32_t y, int lane) {
+  RowIn in;
+  in.r = r;
+  in.y = y;
+  in.count = 1;
+  in.xy = NAN;
+  in.old = in.ref = in.adv = in.edge = 0.f;
+  if (r < 0) return in;
+  const T* x = reinterpret_cast<const T*>(s.x);
+  if (y >= 0 && (int64_t)y < a.vocab) in.xy = Traits<T>::elem(x, y);
+  if (a.ref_logp) in.ref = __ldcg(a.ref_logp + row);
+  if (!PREF) {
+    if (a.old_logp) in.old = __ldcg(a.old_logp + row);
+    in.adv = __ldcg(a.adv + (a.per_request ? (int64_t)r : row));
+    if (a.norm) in.count = __ldcg(a.count + r);
+  }
+  const int32_t v = end_of(a, s, lane);
+  if (v >= 0) in.edge = Traits<T>::elem(x, v);
+  return in;
+}
+// the elements at the row's ends into its sums
+__device__ __forceinline__ void add_ends(const LossArgs& a, const Share& s, const RowIn& in,
+                                         float& k, float& R, int lane) {
+  if (s.head + s.tail == 0) return;
+  const int32_t v = end_of(a, s, lane);
+  const bool add = v >= 0 && v != in.y;
+  const float top =
+      unord(__reduce_max_sync(FULL, ord(add ? fmaxf(in.edge * a.c2, -3e38f) : -3e38f)));
+  if (top > k) {
+    R *= rescale2(k - top);
+    k = top;
+  }
+  float e = add ? ex2(fmaf(in.edge, a.c2, -k)) : 0.f;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) e += __shfl_xor_sync(FULL, e, o);
+  R += e;
+}
+// (k, R) of the lanes together, against the largest k.  `unit`: what a k counts in 2's exponent
+__device__ __forceinline__ void join(float2 q, float unit, float& k, float& R) {
+  k = unord(__reduce_max_sync(FULL, ord(q.x)));
+  R = q.y * rescale2((q.x - k) * unit);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) R += __shfl_xor_sync(FULL, R, o);
+}
+// whether a row has to be summed once more: sums that are 0 or not finite (0 is right where
+// all others are masked and the emitted token is not)
+__device__ __forceinline__ bool sum_again(float k, float R, float xy, float c2) {
+  const float h = xy * c2;
+  return !isfinite(R) || !isfinite(k) || !(h < INFINITY) || (h == -INFINITY && xy > -INFINITY) ||
+         (R == 0.f && (k > -3e38f || h == -INFINITY));
+}
+// the robust sum's M raised to the emitted token's logit
+__device__ __forceinline__ void raise_to(const LossArgs& a, float xy, float& M, float& R) {
+  const float top = isnan(xy) ? M : fmaxf(M, xy);
+  R *= rescale2((M - top) * a.c2);
+  // (an infinite row is NaN by its factor; infinity here means an ordinary sum)
+  if (top == INFINITY) R = NAN;
+  M = fminf(top, -LS_MIN);
+}
+
+// a thread's words into its sum (k, S); the first ones give k
+template <typename T, int N>
+__device__ __forceinline__ void add_words(float& k, float2& S, const uint4 (&v)[N], float c2) {
+  using Tr = Traits<T>;
+  auto top = [&]() {
+    float m = Tr::gmax(v[0]);
+#pragma unroll
+    for (int q = 1; q < N; ++q) m = fmaxf(m, Tr::gmax(v[q]));
+    return fmaxf(m * c2, -3e38f);
+  };
+  if (k == -3.4e38f) k = top();
+  const float2 before = S;
+#pragma unroll
+  for (int q = 0; q < N; ++q) add_word<T>(S, v[q], c2, -k);
+  if (__any_sync(FULL, !(S.x + S.y < 1e30f))) {
+    const float up = fmaxf(top(), k), f = rescale2(k - up);
+    k = up;
+    S = make_float2(before.x * f, before.y * f);
+#pragma unroll
+    for (int q = 0; q < N; ++q) add_word<T>(S, v[q], c2, -k);
+  }
+}
+constexpr float K_NONE = -3.4e38f;  // add_words: no word yet
+
+// The statistics: a warp's sums over its rows to a.part[at], the last of `count` warps
+// joins all in order.  Whole warp.
+__device__ __forceinline__ void write_stats(const LossArgs& a, const float2* stat, int64_t at,
+                                            int64_t count, int lane) {
+  int last = 0;
+  if (lane < RG_TERMS) a.part[at * RG_TERMS + lane] = (double)stat[lane].x + (double)stat[lane].y;
+  __syncwarp();
+  if (lane == 0) {
+    __threadfence();
+    last = atom_add_acq_rel(a.ticket + 1, 1) == (int)count - 1;
+  }
+  if (!__shfl_sync(FULL, last, 0)) return;
+  double total[RG_TERMS];
+#pragma unroll
+  for (int j = 0; j < RG_TERMS; ++j) {
+    double v = 0.;
+    for (int64_t i = lane; i < count; i += 32) v += __ldcg(a.part + i * RG_TERMS + j);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(FULL, v, o);
+    total[j] = v;
+  }
+  if (lane == 0) {
+    a.stats[0] = (float)((double)a.kl_coef * total[1] - total[0]);
+    for (int j = 0; j < RG_TERMS; ++j) a.stats[1 + j] = (float)total[j];
+    a.ticket[1] = 0;
+  }
+}
+
+// ---- forward alone ----------------------------------------------------------------------
+//
+// A CTA, or a cluster of them where there are few rows, reads a row with wide loads into
+// registers, four per thread in flight, and goes on with its next one while one of its
+// warps, another one for each row, takes the row's end.  Three CTAs of 512 threads
+// on an SM read 7.2 TB/s (2.4 GB of V = 151,936 bf16 in 335 us, rows' ends apart).
+template <int NT>
+struct ForwardSmem {
+  float2 part[2][NT / 32];
+  float2 cta[2][MAXC];
+  float2 again[MAXC];
+  float2 stat[NT / 32][RG_TERMS];
+  RowOut out[NT / 32];
+};
+
+template <typename T, int NT, bool PREF>
+__global__ void __launch_bounds__(NT, 1024 / NT) loss_forward(const __grid_constant__ LossArgs a) {
+  using Tr = Traits<T>;
+  constexpr int NW = NT / 32, U = 4;
+  __shared__ ForwardSmem<NT> sm;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  uint32_t C, rank;
+  asm("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(C));
+  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+  const int64_t G = gridDim.x / C, first = blockIdx.x / C;
+  if (lane < RG_TERMS) sm.stat[warp][lane] = make_float2(0.f, 0.f);
+  __syncthreads();
+  if (C > 1) cluster_sync_all();
+  pdl_wait();
+  pdl_trigger();
+  auto request = [&](int64_t row) { return row < a.n_rows ? __ldcg(a.row_req + row) : -1; };
+  auto token = [&](int64_t row) { return row < a.n_rows ? __ldcg(a.chosen + row) : 0; };
+  const double share = PREF ? 0.0 : 1.0 / (double)__ldcg(a.totals + (a.norm ? 1 : 0));
+  const uint4 NEG = make_uint4(Tr::NEG_WORD, Tr::NEG_WORD, Tr::NEG_WORD, Tr::NEG_WORD);
+  int turn = 0, buf = 0;
+  int32_t r = request(first), y = token(first);
+  for (int64_t row = first; row < a.n_rows; row += G) {
+    const int32_t rn = request(row + G), yn = token(row + G);
+    const bool mine = turn == warp;
+    turn = turn + 1 == NW ? 0 : turn + 1;
+    if (r < 0) {
+      if (mine && lane == 0 && rank == 0) a.logp[row] = 0.f;
+      r = rn;
+      y = yn;
+      continue;
+    }
+    const Share sh = share_of<T>(a, row, C, rank);
+    RowIn in;
+    if (mine) in = fetch_row<T, PREF>(a, sh, row, r, y, lane);
+    const int32_t yw = word_of<T>(a, sh, y);
+    const int yj = y - sh.head - yw * Tr::VEC;
+    const uint4* xw = reinterpret_cast<const uint4*>(sh.x + sizeof(T) * sh.head);
+    float k = K_NONE;
+    float2 S = make_float2(0.f, 0.f);
+    uint4 v[U];
+    int32_t i = sh.w0 + tid;
+    for (; i - tid + U * NT <= sh.w1; i += U * NT) {
+#pragma unroll
+      for (int q = 0; q < U; ++q) v[q] = ld_stream(xw + i + q * NT);
+      if ((uint32_t)(yw - (i - tid)) < (uint32_t)(U * NT)) {
+#pragma unroll
+        for (int q = 0; q < U; ++q)
+          if (i + q * NT == yw) v[q] = without<T>(v[q], yj);
+      }
+      add_words<T>(k, S, v, a.c2);
+    }
+    if (i - tid < sh.w1) {
+#pragma unroll
+      for (int q = 0; q < U; ++q) {
+        v[q] = i + q * NT < sh.w1 ? ld_stream(xw + i + q * NT) : NEG;
+        if (i + q * NT == yw) v[q] = without<T>(v[q], yj);
+      }
+      add_words<T>(k, S, v, a.c2);
+    }
+    float R;
+    join(make_float2(fmaxf(k, -3e38f), S.x + S.y), 1.f, k, R);
+    if (lane == 0) sm.part[buf][warp] = make_float2(k, R);
+    if (C == 1) __syncthreads();
+    else {
+      __syncthreads();
+      if (warp == 0) {
+        join(lane < NW ? sm.part[buf][lane] : make_float2(-3e38f, 0.f), 1.f, k, R);
+        if (lane < (int)C)
+          dsmem_st_u64(dsmem_addr(&sm.cta[buf][rank], (uint32_t)lane),
+                       (uint64_t)__float_as_uint(k) | (uint64_t)__float_as_uint(R) << 32);
+        __syncwarp();
+      }
+      cluster_sync_all();
+    }
+    // the row's end; the sums' places are written again two rows on, behind a barrier that
+    // this warp joins after it
+    if (mine) {
+      if (C == 1) join(lane < NW ? sm.part[buf][lane] : make_float2(-3e38f, 0.f), 1.f, k, R);
+      else join(lane < (int)C ? sm.cta[buf][lane] : make_float2(-3e38f, 0.f), 1.f, k, R);
+      add_ends(a, sh, in, k, R, lane);
+      float M = INFINITY;
+      if (sum_again(k, R, in.xy, a.c2)) {
+        Share all = sh;  // (nothing of the row is written: every CTA may read all of it)
+        all.w0 = 0;
+        all.w1 = all.words;
+        robust_sum<T>(a, all, true, in.y, M, R, lane);
+        raise_to(a, in.xy, M, R);
+      }
+      const float wt = PREF ? 0.f : (float)(a.norm ? share / (double)in.count : share);
+      end_math<false, PREF>(a, row, in, k, R, M, wt, rank == 0, &sm.out[warp], sm.stat[warp], lane);
+    }
+    buf ^= 1;
+    r = rn;
+    y = yn;
+  }
+  if (PREF) return;
+  __syncthreads();
+  if (warp != 0 || rank != 0) return;
+  if (lane < RG_TERMS)
+    for (int w = 1; w < NW; ++w) {  // (of few terms each: exact enough as they are)
+      const float2 q = sm.stat[w][lane];
+      float2& t = sm.stat[0][lane];
+      const float s = t.x + q.x, z = s - t.x;
+      t = make_float2(s, t.y + q.y + ((t.x - (s - z)) + (q.x - z)));
+    }
+  __syncwarp();
+  write_stats(a, sm.stat[0], first, min(G, a.n_rows), lane);
+}
+
+// ---- forward and backward in one pass -----------------------------------------------------
+//
+// A row belongs to a CTA, or its parts to the CTAs of a cluster.  Eight warps sum it and
+// write its gradient, one brings it in, one takes its end.  Chunks of 16 KB come
+// into a ring of shared memory by bulk copies; with HOLD a row's chunks stay there
+// between the two sweeps, so that the logits are read from memory once, and the ring's
+// other places take the next row's chunks meanwhile.  The row's end (the warps' sums
+// joined, those of a cluster's CTAs through distributed shared memory, the elements
+// before and after the row's 16-byte words, l and dL/dl) is a chain of some 2,000 cycles:
+// two CTAs share an SM where half its shared memory holds a part, and one streams
+// while the other waits.
+constexpr int RG_NW = 8;                       // warps that sum and write
+constexpr int RG_NT = 32 * (RG_NW + 2);
+constexpr int RG_W = 4;                        // words per lane and chunk
+constexpr int RG_CHUNK = 32 * RG_NW * RG_W;    // words of a chunk
+constexpr int RG_BYTES = 16 * RG_CHUNK;
+constexpr int RG_MOST = 14, RG_FEW = 7;        // places of the ring: one or two CTAs on an SM
+// A warp writes row n's sum after it has waited for row n - LAG's result, and with it all
+// earlier ones.  That result took row n - LAG's sums of all CTAs, whose writers had waited
+// for row n - 2 LAG's in their own CTA: with 2 LAG slots nobody still reads what is written.
+constexpr int RG_SLOTS = 4, RG_LAG = 2;
+struct RingCtl {
+  uint64_t full[RG_MOST], empty[RG_MOST];      // a chunk has landed; has been read
+  float2 part[RG_SLOTS][RG_NW];                // the warps' (k, R)
+  float2 cta[RG_SLOTS][MAXC];                  // the CTAs' (k, R), written by their peers
+  uint64_t part_bar[RG_SLOTS];                 // the warps' sums are there
+  uint64_t cta_bar[RG_SLOTS];                  // the cluster's sums are there
+  uint64_t out_bar[RG_SLOTS];                  // a row's result is there
+  float2 again[MAXC];                          // the sums of a row summed once more
+  uint64_t again_bar;
+  float2 stat[RG_TERMS];                       // sums over the rows
+  RowOut out[RG_SLOTS];                        // a row's result
+};
+static_assert(sizeof(RingCtl) <= 1024 && SH_CHUNK == RG_CHUNK, "two CTAs on an SM");
+constexpr size_t ring_bytes(int places) { return 1024 + (size_t)places * RG_BYTES; }
+
+// Bounded wait: the clock of ring_wait_slow is read only after some thousand tests.
+__device__ __forceinline__ bool ring_wait(uint32_t bar, uint32_t parity, uint32_t* flags) {
+  for (int i = 0; i < 4096; ++i)
+    if (ring_test(bar, parity)) return true;
+  return ring_wait_slow(bar, parity, flags);
+}
+
+template <typename T, bool HOLD>
+__global__ void __launch_bounds__(RG_NT, 2)
+    loss_ring(const __grid_constant__ LossArgs a, const int places) {
   extern __shared__ __align__(16) unsigned char smem_raw[];
-  RingSmem& sm = *reinterpret_cast<RingSmem*>(smem_raw);
+  RingCtl& sm = *reinterpret_cast<RingCtl*>(smem_raw);
+  unsigned char* const ring = smem_raw + 1024;
   using Tr = Traits<T>;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int wg = warp % GW;
-  uint32_t C = 1, rank = 0;
-  if (GW == RG_NW) {
-    asm("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(C));
-    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
-  }
-  const int64_t G = GW == RG_NW ? gridDim.x / C : (int64_t)gridDim.x * (RG_NW / GW);
-  const int64_t first = GW == RG_NW ? blockIdx.x / C : (int64_t)blockIdx.x * (RG_NW / GW) + warp / GW;
-  const bool leader = wg == 0 && rank == 0;
-  auto bar_of = [&](int s) { return (uint32_t)__cvta_generic_to_shared(&sm.bar[warp][s]); };
-  if (lane == 0) {
-    for (int s = 0; s < RG_NS; ++s)
-      asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bar_of(s)) : "memory");
+  uint32_t C, rank;
+  asm("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(C));
+  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+  const int64_t G = gridDim.x / C, first = blockIdx.x / C;
+  auto addr = [](const void* p) { return (uint32_t)__cvta_generic_to_shared(p); };
+  auto init = [&](uint64_t* b, int n) {
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(addr(b)), "r"(n) : "memory");
+  };
+  auto arrive = [&](uint64_t* b) {
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(addr(b)) : "memory");
+  };
+  auto expect = [&](uint64_t* b, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(addr(b)), "r"(bytes)
+                 : "memory");
+  };
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < places; ++i) {
+      init(&sm.full[i], 1);
+      init(&sm.empty[i], RG_NW);
+    }
+    for (int s = 0; s < RG_SLOTS; ++s) {
+      init(&sm.part_bar[s], RG_NW);
+      init(&sm.out_bar[s], 1);
+      init(&sm.cta_bar[s], 1);
+      if (C > 1) expect(&sm.cta_bar[s], 8 * C);
+    }
+    init(&sm.again_bar, 1);
+    if (C > 1) expect(&sm.again_bar, 8 * C);
+    for (int j = 0; j < RG_TERMS; ++j) sm.stat[j] = make_float2(0.f, 0.f);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
-  __syncwarp();
-  if (GW == RG_NW && C > 1) cluster_sync_all();  // every CTA's memory is there
+  __syncthreads();
+  if (C > 1) cluster_sync_all();  // every CTA's barriers are there
   pdl_wait();
   pdl_trigger();
 
-  // ---- bringing chunks in
-  int64_t lrow = first;            // the next chunk's row, its request and the next row's
-  int32_t lreq = lrow < a.n_rows ? __ldcg(a.row_req + lrow) : -1;
-  int32_t lreq2 = lrow + G < a.n_rows ? __ldcg(a.row_req + lrow + G) : -1;
-  int32_t lchunk = 0;
-  int lstage = 0, room = RG_NS, flying = 0;
-  bool landed = true;
-  uint32_t parity = 0u;            // bit s: stage s' next phase
-  Share ls;
-  ls.chunks = 0;
-  if (lrow < a.n_rows) ls = share_of<T, GW>(a, lrow, C, rank, wg);
-  auto bring = [&]() {
-    // rows that do not count, or of which this warp has nothing
-    while (lrow < a.n_rows && (lreq < 0 || lchunk >= ls.chunks)) {
-      lrow += G;
-      lreq = lreq2;
-      lreq2 = lrow + G < a.n_rows ? __ldcg(a.row_req + lrow + G) : -1;
-      lchunk = 0;
-      if (lrow < a.n_rows) ls = share_of<T, GW>(a, lrow, C, rank, wg);
-    }
-    if (lrow >= a.n_rows || room == 0 || !landed) return;
-    if (lane == 0) {
-      const int32_t w = ls.w0 + (wg + lchunk * GW) * RG_CHUNK;
-      const uint32_t bytes = 16u * (uint32_t)min(RG_CHUNK, ls.w1 - w);
-      const uint32_t bar = bar_of(lstage);
-      asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes)
-                   : "memory");
-      asm volatile(
-          "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::
-              "r"((uint32_t)__cvta_generic_to_shared(sm.stage[warp][lstage])),
-          "l"(ls.x + (int64_t)sizeof(T) * ls.rw.head + 16 * (int64_t)w), "r"(bytes), "r"(bar)
-          : "memory");
-    }
-    lstage = lstage + 1 == RG_NS ? 0 : lstage + 1;
-    --room;
-    ++flying;
-    ++lchunk;
+  bool ok = true;  // no wait has run out
+  auto wait = [&](uint64_t* b, uint32_t phase) {
+    if (ok) ok = ring_wait(addr(b), phase, a.ctx_flags);
+    __syncwarp();
   };
-  for (int s = 0; s < RG_NS; ++s) bring();
+  auto request = [&](int64_t row) { return row < a.n_rows ? __ldcg(a.row_req + row) : -1; };
+  auto token = [&](int64_t row) { return row < a.n_rows ? __ldcg(a.chosen + row) : 0; };
+  int place = 0;         // of the ring
+  uint32_t turn = 0u;    // how often it has been gone around, its last bit
+  auto step = [&]() {
+    if (++place == places) {
+      place = 0;
+      turn ^= 1u;
+    }
+  };
 
-  // ---- the rows' scalars, two rows ahead and one
-  auto fetch_id = [&](int64_t row, int32_t& r, int32_t& y) {
-    r = -1;
-    y = 0;
-    if (row < a.n_rows) {
-      r = __ldcg(a.row_req + row);
-      y = __ldcg(a.chosen + row);
-    }
-  };
-  auto fetch = [&](int64_t row, int32_t r, int32_t y) {
-    RowIn in;
-    in.r = r;
-    in.y = y;
-    in.count = 1;
-    in.xy = NAN;
-    in.old = in.ref = in.adv = 0.f;
-    if (r >= 0) {
-      const T* x = reinterpret_cast<const T*>(a.logits) + row * a.row_stride;
-      if (y >= 0 && (int64_t)y < a.vocab) in.xy = Tr::elem(x, y);
-      if (a.ref_logp) in.ref = __ldcg(a.ref_logp + row);
-      if (!PREF) {
-        if (a.old_logp) in.old = __ldcg(a.old_logp + row);
-        in.adv = __ldcg(a.adv + (a.per_request ? (int64_t)r : row));
-        if (a.norm) in.count = __ldcg(a.count + r);
-      }
-    }
-    return in;
-  };
-  int32_t r1, y1;
-  fetch_id(first, r1, y1);
-  RowIn in = fetch(first, r1, y1);
-  fetch_id(first + G, r1, y1);
-  const double share = PREF ? 0.0 : 1.0 / (double)__ldcg(a.totals + (a.norm ? 1 : 0));
-  double stat[LS_NSTAT] = {0., 0., 0., 0., 0., 0.};
-
-  int stage = 0, buf = 0;
-  for (int64_t row = first; row < a.n_rows; row += G) {
-    const RowIn next = row + G < a.n_rows ? fetch(row + G, r1, y1) : in;
-    fetch_id(row + 2 * G, r1, y1);
-    const Share sh = share_of<T, GW>(a, row, C, rank, wg);
-    const T* x = reinterpret_cast<const T*>(sh.x);
-    T* g = reinterpret_cast<T*>(a.grad) + row * a.grad_stride;
-    const int64_t tail0 = sh.rw.head + sh.rw.words * Tr::VEC;
-    // element of this lane before or after the words
-    const int64_t ve = lane < 8 ? (lane < sh.rw.head ? lane : -1)
-                                : (lane - 8 < sh.rw.tail ? tail0 + lane - 8 : -1);
-    const bool edge = leader && ve >= 0;
-    if (in.r < 0) {
-      if (leader && lane == 0) a.logp[row] = 0.f;
-      if (HOLD) {
-        const bool vec = ((reinterpret_cast<uintptr_t>(x) ^ reinterpret_cast<uintptr_t>(g)) & 15u) == 0;
-        for (int32_t c = 0; c < sh.chunks; ++c) {
-          const int32_t w = sh.w0 + (wg + c * GW) * RG_CHUNK;
-#pragma unroll
-          for (int k = 0; k < RG_W; ++k) {
-            const int32_t i = w + 32 * k + lane;
-            if (i < sh.w1) put_word(g + sh.rw.head + (int64_t)i * Tr::VEC, make_uint4(0u, 0u, 0u, 0u), vec);
+  if (warp == RG_NW) {
+    // ---- bringing chunks in
+    int64_t n = 0;
+    int32_t r = request(first);
+    for (int64_t row = first; row < a.n_rows; row += G) {
+      const int32_t rn = request(row + G);
+      if (r >= 0) {
+        const Share sh = share_of<T>(a, row, C, rank);
+        const char* src = sh.x + sizeof(T) * sh.head + 16 * (int64_t)sh.w0;
+        for (int32_t left = sh.w1 - sh.w0; left > 0; left -= RG_CHUNK) {
+          if (n >= places) wait(&sm.empty[place], turn ^ 1u);
+          if (ok && lane == 0) {
+            const uint32_t bytes = 16u * (uint32_t)min(RG_CHUNK, left);
+            expect(&sm.full[place], bytes);
+            asm volatile(
+                "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::
+                    "r"(addr(ring + (size_t)place * RG_BYTES)),
+                "l"(src), "r"(bytes), "r"(addr(&sm.full[place]))
+                : "memory");
           }
+          src += RG_BYTES;
+          if (ok) ++n;
+          step();
         }
-        if (edge) put(g + ve, 0.f);
       }
-      in = next;
-      continue;
+      r = rn;
     }
-    const int32_t y = in.y;
-    const bool yok = y >= 0 && (int64_t)y < a.vocab;
-    const int64_t yo = (int64_t)y - sh.rw.head;
-    const int32_t yw = yok && yo >= 0 ? (int32_t)(yo / Tr::VEC) : -1;
-    const int yj = (int)(yo - (int64_t)yw * Tr::VEC);
-
-    // ---- forward
-    RowSum s;
-    s.reset();
-    const int held = stage;
-    for (int32_t c = 0; c < sh.chunks; ++c) {
-      if (landed) {
-        if (!ring_test(bar_of(stage), (parity >> stage) & 1u))
-          landed = ring_wait_slow(bar_of(stage), (parity >> stage) & 1u, a.ctx_flags);
-        if (landed) {
-          parity ^= 1u << stage;
-          --flying;
-        }
-      }
+    // no copy may be in flight when the CTA ends (as none is unless a wait ran out)
+    ok = true;
+    for (int64_t i = n < places ? 0 : n - places; i < n; ++i)
+      wait(&sm.full[(int)(i % places)], (uint32_t)(i / places) & 1u);
+  } else if (warp == RG_NW + 1) {
+    // ---- the rows' ends
+    const double share = 1.0 / (double)__ldcg(a.totals + (a.norm ? 1 : 0));
+    // every CTA's (k, R), by lane
+    auto exchange = [&](float2* to, uint64_t* bar, uint32_t phase, float k, float R) {
+      if (lane < (int)C)
+        asm volatile(
+            "st.async.shared::cluster.mbarrier::complete_tx::bytes.b64 [%0], %1, [%2];" ::"r"(
+                dsmem_addr(to + rank, (uint32_t)lane)),
+            "l"((uint64_t)__float_as_uint(k) | (uint64_t)__float_as_uint(R) << 32),
+            "r"(dsmem_addr(bar, (uint32_t)lane))
+            : "memory");
       __syncwarp();
-      const uint4* st = reinterpret_cast<const uint4*>(sm.stage[warp][stage]) + lane;
-      const int32_t w = sh.w0 + (wg + c * GW) * RG_CHUNK;
-      uint4 v[RG_W];
-#pragma unroll
-      for (int k = 0; k < RG_W; ++k) v[k] = st[32 * k];
-      if (w + RG_CHUNK > sh.w1) {
-#pragma unroll
-        for (int k = 0; k < RG_W; ++k)
-          if (w + 32 * k + lane >= sh.w1)
-            v[k] = make_uint4(Tr::NEG_WORD, Tr::NEG_WORD, Tr::NEG_WORD, Tr::NEG_WORD);
-      }
-      if (yw >= w && yw < w + RG_CHUNK) {
-#pragma unroll
-        for (int k = 0; k < RG_W; ++k)
-          if (w + 32 * k + lane == yw) v[k] = without<T>(v[k], yj);
-      }
-      const float top = Tr::tile_max(v);
-      if (__any_sync(FULL, (top - s.m) * a.c2 > 8.f)) s.raise(top, a.c2, a.inv_t);
-#pragma unroll
-      for (int k = 0; k < RG_W; ++k) add_word<T>(s, v[k], a.c2);
-      stage = stage + 1 == RG_NS ? 0 : stage + 1;
-      if (!HOLD) {
-        __syncwarp();
-        ++room;
-        bring();
-      }
-    }
-    const float xe = edge ? Tr::elem(x, ve) : 0.f;
-    if (edge && ve != y) s.add1(xe, a.c2, a.inv_t);
-    // the warp's, then the group's sums
-    float R = s.S.x + s.S.y;
-    float m = unord(__reduce_max_sync(FULL, ord(s.m)));
-    R *= rescale(s.m, m, a.inv_t);
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) R += __shfl_xor_sync(FULL, R, o);
-    if (GW > 1) {
-      const float2 mine = make_float2(m, R);
-      int n = GW;
-      if (GW == RG_NW && C > 1) {
-        n = RG_NW * (int)C;
-        if (lane < (int)C)
-          dsmem_st_u64(dsmem_addr(&sm.part[buf][rank * RG_NW + warp], (uint32_t)lane),
-                       (uint64_t)__float_as_uint(m) | (uint64_t)__float_as_uint(R) << 32);
-        __syncwarp();
-        cluster_sync_all();
-      } else {
-        if (lane == 0) sm.part[buf][warp] = mine;
-        if (GW == RG_NW) __syncthreads();
-        else named_bar_sync(1 + warp / GW, 32 * GW);
-      }
-      const float2* pt = sm.part[buf] + (GW == RG_NW ? 0 : warp - wg);
-      float2 q[MAXC * RG_NW / 32];
-      m = LS_MIN;
-#pragma unroll
-      for (int k = 0; k < MAXC * RG_NW / 32; ++k) {
-        q[k] = lane + 32 * k < n ? pt[lane + 32 * k] : make_float2(LS_MIN, 0.f);
-        m = fmaxf(m, q[k].x);
-      }
-      m = unord(__reduce_max_sync(FULL, ord(m)));
-      R = 0.f;
-#pragma unroll
-      for (int k = 0; k < MAXC * RG_NW / 32; ++k)
-        if (32 * k < n) R = fmaf(q[k].y, rescale(q[k].x, m, a.inv_t), R);
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) R += __shfl_xor_sync(FULL, R, o);
-      buf ^= 1;
-    }
-    const RowEnd e(a, m, R, in.xy, yok);
-    float k = 0.f;
-    if (!PREF) {
-      const double wt = a.norm ? share / (double)in.count : share;
-      const PolicyTerms p = policy_terms(a, e.l, e.l_lo, in.old, in.ref, in.adv);
-      k = (float)wt * p.slope * (a.grad_scale * a.inv_t);
-      if (leader && lane == 0) {
-        stat[0] += wt * (double)p.loss;
-        stat[1] += wt * (double)p.surrogate;
-        stat[2] += wt * (double)p.kl;
-        stat[3] += wt * (double)p.ratio;
-        stat[4] += wt * (double)p.clipped;
-        stat[5] += wt * (double)p.old_kl;
-      }
-    }
-    if (leader && lane == 0) {
-      a.logp[row] = e.l;
-      if (!yok) atomicOr(a.ctx_flags, FLAG_BAD_CHOSEN);
-      else if (isnan(e.l)) atomicOr(a.ctx_flags, FLAG_NONFINITE);
-      if (!HOLD && a.state) {
-        a.state[row] = make_float4(e.M, e.lS, PREF ? (e.l - in.ref) + e.l_lo : k, e.rest);
-      }
-    }
-
-    // ---- backward
-    if (HOLD) {
-      const bool vec = ((reinterpret_cast<uintptr_t>(x) ^ reinterpret_cast<uintptr_t>(g)) & 15u) == 0;
-      const RowGrad rg{e.M, e.lS, -k, a.c2};
-      const float gy = k * e.rest;
-      int bs = held;
-      for (int32_t c = 0; c < sh.chunks; ++c) {
-        const uint4* st = reinterpret_cast<const uint4*>(sm.stage[warp][bs]) + lane;
-        const int32_t w = sh.w0 + (wg + c * GW) * RG_CHUNK;
-#pragma unroll
-        for (int q = 0; q < RG_W; ++q) {
-          const int32_t i = w + 32 * q + lane;
-          if (i < sh.w1) {
-            T* to = g + sh.rw.head + (int64_t)i * Tr::VEC;
-            put_word(to, grad_word<T>(rg, st[32 * q]), vec);
-            if (i == yw) put(to + yj, gy);
-          }
+      wait(bar, phase);
+      const float2 p = lane < (int)C ? to[lane] : make_float2(LS_MIN, 0.f);
+      __syncwarp();
+      if (lane == 0) expect(bar, 8 * C);
+      return p;
+    };
+    uint32_t n = 0, agains = 0;
+    int32_t r1 = request(first), y1 = token(first);
+    RowIn in = fetch_row<T, false>(a, share_of<T>(a, first, C, rank), first, r1, y1, lane);
+    r1 = request(first + G);
+    y1 = token(first + G);
+    for (int64_t row = first; row < a.n_rows; row += G) {
+      const Share sh = share_of<T>(a, row, C, rank);
+      const RowIn next =
+          fetch_row<T, false>(a, share_of<T>(a, row + G, C, rank), row + G, r1, y1, lane);
+      r1 = request(row + 2 * G);
+      y1 = token(row + 2 * G);
+      const int32_t v = end_of(a, sh, lane);
+      T* const g = reinterpret_cast<T*>(a.grad) + row * a.grad_stride;
+      if (in.r < 0) {
+        if (rank == 0) {
+          if (lane == 0) a.logp[row] = 0.f;
+          if (HOLD && v >= 0) put(g + v, 0.f);
         }
-        __syncwarp();
-        bs = bs + 1 == RG_NS ? 0 : bs + 1;
-        ++room;
-        bring();
+        in = next;
+        continue;
       }
-      if (edge) put(g + ve, ve == y ? gy : rg.one(xe));
+      const int s = n % RG_SLOTS;
+      const uint32_t phase = (n / RG_SLOTS) & 1u;
+      ++n;
+      wait(&sm.part_bar[s], phase);
+      float k, R, M = INFINITY;
+      join(lane < RG_NW ? sm.part[s][lane] : make_float2(-3e38f, 0.f), 1.f, k, R);
+      if (rank == 0) add_ends(a, sh, in, k, R, lane);
+      // (a peer that has this CTA's sum may write its part of the gradient, over the
+      // logits: what is read of that part has to be here)
+      in.xy = __shfl_sync(FULL, in.xy, 0);
+      if (C > 1) join(exchange(sm.cta[s], &sm.cta_bar[s], phase, k, R), 1.f, k, R);
+      if (sum_again(k, R, in.xy, a.c2)) {
+        robust_sum<T>(a, sh, rank == 0, in.y, M, R, lane);
+        if (C > 1) {
+          join(exchange(sm.again, &sm.again_bar, agains & 1u, M, R), a.c2, M, R);
+          ++agains;
+        }
+        raise_to(a, in.xy, M, R);
+      }
+      const float wt = (float)(a.norm ? share / (double)in.count : share);
+      end_math<HOLD, false>(a, row, in, k, R, M, wt, rank == 0, &sm.out[s], sm.stat, lane);
+      __syncwarp();
+      if (lane == 0) arrive(&sm.out_bar[s]);
+      if (HOLD && rank == 0 && v >= 0) put(g + v, v == in.y ? sm.out[s].gy : grad1(sm.out[s], a.c2, in.edge));
+      in = next;
     }
-    in = next;
-  }
-  if (!landed) {  // a wait ran out: no copy may be in flight when the CTA ends
-    for (int i = 0; i < flying; ++i) {
-      lstage = lstage == 0 ? RG_NS - 1 : lstage - 1;
-      ring_wait_slow(bar_of(lstage), (parity >> lstage) & 1u, a.ctx_flags);
-    }
-  }
-  if (PREF || !leader || first >= a.n_rows) return;
-  // the statistics: each group's sum over its rows, then the groups' in order
-  int last = 0;
-  if (lane == 0) {
-    for (int j = 0; j < LS_NSTAT; ++j) a.part[first * LS_NSTAT + j] = stat[j];
-    last = atom_add_acq_rel(a.ticket + 1, 1) == (int)min(G, a.n_rows) - 1;
-  }
-  if (!__shfl_sync(FULL, last, 0)) return;
-  const int64_t groups = min(G, a.n_rows);
-  for (int j = 0; j < LS_NSTAT; ++j) {
-    double v = 0.;
-    for (int64_t i = lane; i < groups; i += 32) v += __ldcg(a.part + i * LS_NSTAT + j);
+  } else {
+    // ---- the rows' words
+    uint32_t n = 0, taken = 0;  // rows summed; rows whose result was waited for
+    int32_t r = request(first), y = token(first);
+    const int at = warp * 32 + lane;  // this lane's first word of a chunk
+    for (int64_t row = first; row < a.n_rows; row += G) {
+      const int32_t rn = request(row + G), yn = token(row + G);
+      const Share sh = share_of<T>(a, row, C, rank);
+      T* const g = reinterpret_cast<T*>(a.grad) + row * a.grad_stride + sh.head;
+      const bool vec = ((reinterpret_cast<uintptr_t>(sh.x + sizeof(T) * sh.head) ^
+                         reinterpret_cast<uintptr_t>(g)) & 15u) == 0;
+      if (r < 0) {  // a row that does not count
+        if (HOLD)
+          for (int32_t i = sh.w0 + at; i < sh.w1; i += 32 * RG_NW)
+            put_word(g + (int64_t)i * Tr::VEC, make_uint4(0u, 0u, 0u, 0u), vec);
+        r = rn;
+        y = yn;
+        continue;
+      }
+      const int32_t yw = word_of<T>(a, sh, y);
+      const int yj = y - sh.head - yw * Tr::VEC;
+      // forward
+      const int place0 = place;
+      const uint32_t turn0 = turn;
+      float k = K_NONE;
+      float2 S = make_float2(0.f, 0.f);
+      for (int32_t w = sh.w0; w < sh.w1; w += RG_CHUNK) {
+        wait(&sm.full[place], turn);
+        const uint4* st = reinterpret_cast<const uint4*>(ring + (size_t)place * RG_BYTES) + at;
+        uint4 v[RG_W];
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(FULL, v, o);
-    if (lane == 0) a.stats[j] = (float)v;
+        for (int q = 0; q < RG_W; ++q) v[q] = st[32 * RG_NW * q];
+        if (w + RG_CHUNK > sh.w1) {
+#pragma unroll
+          for (int q = 0; q < RG_W; ++q)
+            if (w + 32 * RG_NW * q + at >= sh.w1)
+              v[q] = make_uint4(Tr::NEG_WORD, Tr::NEG_WORD, Tr::NEG_WORD, Tr::NEG_WORD);
+        }
+        if ((uint32_t)(yw - w) < (uint32_t)RG_CHUNK) {
+#pragma unroll
+          for (int q = 0; q < RG_W; ++q)
+            if (w + 32 * RG_NW * q + at == yw) v[q] = without<T>(v[q], yj);
+        }
+        if (!HOLD) {
+          __syncwarp();  // every lane has its words
+          if (lane == 0) arrive(&sm.empty[place]);
+        }
+        step();
+        add_words<T>(k, S, v, a.c2);
+      }
+      float R;
+      join(make_float2(fmaxf(k, -3e38f), S.x + S.y), 1.f, k, R);
+      const int s = n % RG_SLOTS;
+      if (!HOLD && n >= RG_LAG) {
+        wait(&sm.out_bar[taken % RG_SLOTS], (taken / RG_SLOTS) & 1u);
+        ++taken;
+      }
+      if (lane == 0) {
+        sm.part[s][warp] = make_float2(k, R);
+        arrive(&sm.part_bar[s]);
+      }
+      if (HOLD) {
+        // backward
+        wait(&sm.out_bar[s], (n / RG_SLOTS) & 1u);
+        const RowOut o = sm.out[s];
+        place = place0;
+        turn = turn0;
+        for (int32_t w = sh.w0; w < sh.w1; w += RG_CHUNK) {
+          const uint4* st = reinterpret_cast<const uint4*>(ring + (size_t)place * RG_BYTES) + at;
+          T* const to = g + (int64_t)(w + at) * Tr::VEC;
+          uint4 v[RG_W];
+#pragma unroll
+          for (int q = 0; q < RG_W; ++q) v[q] = st[32 * RG_NW * q];
+          if (o.mode == ROW_FAST) {
+#pragma unroll
+            for (int q = 0; q < RG_W; ++q) v[q] = grad_word<T, false>(o, a.c2, v[q]);
+          } else if (o.mode == ROW_ROBUST) {
+#pragma unroll
+            for (int q = 0; q < RG_W; ++q) v[q] = grad_word<T, true>(o, a.c2, v[q]);
+          } else {
+#pragma unroll
+            for (int q = 0; q < RG_W; ++q) v[q] = make_uint4(0u, 0u, 0u, 0u);
+          }
+          __syncwarp();
+          if (lane == 0) arrive(&sm.empty[place]);
+          step();
+          if (vec && w + RG_CHUNK <= sh.w1) {
+#pragma unroll
+            for (int q = 0; q < RG_W; ++q)
+              *reinterpret_cast<uint4*>(to + 32 * RG_NW * q * Tr::VEC) = v[q];
+          } else {
+#pragma unroll
+            for (int q = 0; q < RG_W; ++q)
+              if (w + 32 * RG_NW * q + at < sh.w1) put_word(to + 32 * RG_NW * q * Tr::VEC, v[q], vec);
+          }
+          if ((uint32_t)(yw - w) < (uint32_t)RG_CHUNK && ((yw - w) % (32 * RG_NW)) == at)
+            put(g + (int64_t)yw * Tr::VEC + yj, o.gy);
+        }
+      }
+      ++n;
+      r = rn;
+      y = yn;
+    }
   }
-  if (lane == 0) a.ticket[1] = 0;
+  __syncthreads();
+  if (C > 1) cluster_sync_all();  // no peer writes here any more
+  if (warp == 0 && rank == 0) write_stats(a, sm.stat, first, min(G, a.n_rows), lane);
 }
 
 // ---- backward from the rows' states ---------------------------------------------------------
@@ -698,17 +1039,22 @@ __global__ void __launch_bounds__(BW_NT) loss_backward(const LossArgs a, int32_t
 #pragma unroll
   for (int k = 0; k < BW_W; ++k)
     if (r >= 0 && w0 + k * BW_NT < words) v[k] = ld_stream(xw + w0 + k * BW_NT);
-  float k = 0.f;
-  float4 st = make_float4(0.f, 0.f, 0.f, 0.f);
+  RowOut o;
+  o.mode = ROW_ZERO;
+  o.K = o.nk = o.gy = o.M = 0.f;
   int32_t y = -1;
   if (r >= 0) {
-    st = __ldcg(a.state + row);
-    k = PREF ? __ldcg(a.coef + r) * (a.grad_scale * a.inv_t) : st.z;
+    const float4 q = __ldcg(a.state + 2 * row);
+    const float k = PREF ? __ldcg(a.coef + r) * (a.grad_scale * a.inv_t)
+                         : __ldcg(&a.state[2 * row + 1].x);
+    RowState st;
+    st.K = q.x;
+    st.adj = q.y;
+    st.rest = q.z;
+    st.M = q.w;
+    o = row_out(st, k);
     y = __ldcg(a.chosen + row);
   }
-  const bool zero = r < 0 || k == 0.f;
-  const RowGrad rg{st.x, st.y, -k, a.c2};
-  const float gy = k * st.w;
   const int64_t yo = (int64_t)y - rw.head;
   const int32_t yw = y >= 0 && (int64_t)y < a.vocab && yo >= 0 ? (int32_t)(yo / Tr::VEC) : -1;
 #pragma unroll
@@ -716,14 +1062,17 @@ __global__ void __launch_bounds__(BW_NT) loss_backward(const LossArgs a, int32_t
     const int32_t i = w0 + q * BW_NT;
     if (i < words) {
       T* to = g + rw.head + (int64_t)i * Tr::VEC;
-      put_word(to, zero ? make_uint4(0u, 0u, 0u, 0u) : grad_word<T>(rg, v[q]), vec);
-      if (!zero && i == yw) put(to + (yo - (int64_t)yw * Tr::VEC), gy);
+      uint4 w = make_uint4(0u, 0u, 0u, 0u);
+      if (o.mode == ROW_FAST) w = grad_word<T, false>(o, a.c2, v[q]);
+      else if (o.mode == ROW_ROBUST) w = grad_word<T, true>(o, a.c2, v[q]);
+      put_word(to, w, vec);
+      if (i == yw) put(to + (yo - (int64_t)yw * Tr::VEC), o.gy);
     }
   }
   if (seg > 0) return;
   const int64_t ve = tid < 8 ? (tid < rw.head ? tid : -1)
                              : (tid - 8 < rw.tail ? rw.head + rw.words * Tr::VEC + tid - 8 : -1);
-  if (ve >= 0) put(g + ve, zero ? 0.f : (ve == y ? gy : rg.one(Tr::elem(x, ve))));
+  if (ve >= 0) put(g + ve, ve == y ? o.gy : grad1(o, a.c2, Tr::elem(x, ve)));
 }
 
 // ---- answer pairs -------------------------------------------------------------------------
@@ -734,7 +1083,7 @@ __device__ __forceinline__ double pair_ratio(const LossArgs& a, int64_t r, int l
   double s = 0.;
   if (__ldcg(a.count + r) > 0)
     for (int64_t t = lo + lane; t < hi; t += 32)
-      if (!a.mask || a.mask[t] != 0) s += (double)__ldcg(&a.state[t].z);
+      if (!a.mask || a.mask[t] != 0) s += (double)__ldcg(&a.state[2 * t + 1].x);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(FULL, s, o);
   return s;

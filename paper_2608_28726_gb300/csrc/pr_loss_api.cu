@@ -46,7 +46,7 @@ pr_status workspace(pr_ctx* c, prk::LossArgs& a, int64_t groups, bool pref, bool
                at_term = at_coef + up16(pref ? n_req * 4 : 0),
                at_req = at_term + up16(pref ? n_req / 2 * prk::LS_NSTAT * 4 : 0),
                at_state = at_req + up16(n_rows * 4),
-               at_part = at_state + (state ? n_rows * 16 : 0),
+               at_part = at_state + (state ? n_rows * 32 : 0),
                bytes = at_part + (pref ? 0 : (size_t)groups * prk::LS_NSTAT * 8);
   if (bytes > c->loss_ws_bytes) {
     PR_CUDA(cudaDeviceSynchronize());  // kernels may still use the old one
@@ -100,79 +100,105 @@ pr_status launch(const void* kern, unsigned grid, unsigned threads, size_t smem,
   return PR_OK;
 }
 
-template <typename T, int GW>
-const void* ring_kernel(bool hold, bool pref) {
-  return pref ? reinterpret_cast<const void*>(&prk::loss_ring<T, GW, false, true>)
-              : hold ? reinterpret_cast<const void*>(&prk::loss_ring<T, GW, true, false>)
-                     : reinterpret_cast<const void*>(&prk::loss_ring<T, GW, false, false>);
+const void* ring_kernel(pr_dtype dt, bool hold) {
+  if (dt == PR_DTYPE_BF16)
+    return hold ? reinterpret_cast<const void*>(&prk::loss_ring<__nv_bfloat16, true>)
+                : reinterpret_cast<const void*>(&prk::loss_ring<__nv_bfloat16, false>);
+  return hold ? reinterpret_cast<const void*>(&prk::loss_ring<float, true>)
+              : reinterpret_cast<const void*>(&prk::loss_ring<float, false>);
 }
+
+constexpr int FW_NT = 512, FW_SMALL = 128;  // threads of a row's CTA
+
 template <typename T>
-const void* ring_kernel(int gw, bool hold, bool pref) {
-  return gw == 1 ? ring_kernel<T, 1>(hold, pref)
-                 : gw == 4 ? ring_kernel<T, 4>(hold, pref) : ring_kernel<T, 16>(hold, pref);
+const void* forward_kernel(bool small, bool pref) {
+  if (small)
+    return pref ? reinterpret_cast<const void*>(&prk::loss_forward<T, FW_SMALL, true>)
+                : reinterpret_cast<const void*>(&prk::loss_forward<T, FW_SMALL, false>);
+  return pref ? reinterpret_cast<const void*>(&prk::loss_forward<T, FW_NT, true>)
+              : reinterpret_cast<const void*>(&prk::loss_forward<T, FW_NT, false>);
 }
 
-// Warps of a row: `gw` of a CTA, in `cluster` CTAs.
-struct RowShape {
-  int gw, cluster;
-  bool hold;        // a row's chunks fit the group's rings
-  int64_t groups;   // rows in work at a time
-  unsigned grid;
-};
-
-constexpr int WARPS[] = {1, 4, 16, 32, 64, 128};  // of a row: of a CTA, then of 2, 4, 8 CTAs
-
-// shared memory opt-ins, and the rows that the GPU has room for at each width; once per
-// context
+// shared memory opt-ins, and the clusters of 2, 4 and 8 CTAs that the GPU has room for
+// with half and with all of an SM's shared memory each; once per context
 pr_status ring_setup(pr_ctx* c) {
   if (c->loss_ready) return PR_OK;
-  for (int gw : {1, 4, 16})
-    for (int m = 0; m < 3; ++m)
-      for (const void* f : {ring_kernel<__nv_bfloat16>(gw, m == 1, m == 2),
-                            ring_kernel<float>(gw, m == 1, m == 2)})
-        PR_CUDA(cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                     (int)sizeof(prk::RingSmem)));
-  for (int i = 0; i < 6; ++i) {
-    if (WARPS[i] <= 16) {
-      c->loss_places[i] = c->num_sms * (16 / WARPS[i]);
-      continue;
+  for (pr_dtype dt : {PR_DTYPE_F32, PR_DTYPE_BF16})
+    for (bool hold : {false, true})
+      PR_CUDA(cudaFuncSetAttribute(ring_kernel(dt, hold), cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                   (int)prk::ring_bytes(prk::RG_MOST)));
+  for (int i = 0; i < 4; ++i)
+    for (int whole = 0; whole < 2; ++whole) {
+      if (i == 0) {
+        c->loss_places[whole][0] = c->num_sms * (whole ? 1 : 2);
+        continue;
+      }
+      cudaLaunchConfig_t cfg;
+      memset(&cfg, 0, sizeof cfg);
+      cfg.gridDim = dim3(1u << i);
+      cfg.blockDim = dim3(prk::RG_NT);
+      cfg.dynamicSmemBytes = prk::ring_bytes(whole ? prk::RG_MOST : prk::RG_FEW);
+      cudaLaunchAttribute attr[1];
+      attr[0].id = cudaLaunchAttributeClusterDimension;
+      attr[0].val.clusterDim.x = 1u << i;
+      attr[0].val.clusterDim.y = 1;
+      attr[0].val.clusterDim.z = 1;
+      cfg.attrs = attr;
+      cfg.numAttrs = 1;
+      int n = 0;
+      PR_CUDA(cudaOccupancyMaxActiveClusters(&n, ring_kernel(PR_DTYPE_BF16, true), &cfg));
+      c->loss_places[whole][i] = std::max(n, 1);
     }
-    cudaLaunchConfig_t cfg;
-    memset(&cfg, 0, sizeof cfg);
-    cfg.gridDim = dim3((unsigned)(WARPS[i] / 16));
-    cfg.blockDim = dim3(prk::RG_NW * 32);
-    cfg.dynamicSmemBytes = sizeof(prk::RingSmem);
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = (unsigned)(WARPS[i] / 16);
-    attr[0].val.clusterDim.y = 1;
-    attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    int n = 0;
-    PR_CUDA(cudaOccupancyMaxActiveClusters(&n, ring_kernel<__nv_bfloat16>(16, true, false), &cfg));
-    c->loss_places[i] = std::max(n, 1);
-  }
   c->loss_ready = true;
   return PR_OK;
 }
 
-// The narrowest group whose rings hold a row and leave room for the next one's first
-// chunks (RG_NS - 2 chunks per warp); wider ones while all rows have a place at once.
-RowShape choose_shape(const pr_ctx* c, pr_dtype dt, int64_t n_rows, int64_t vocab) {
-  const int64_t words = (vocab * (int64_t)esize(dt)) / 16;
+// The one-pass kernel's launch: 2^split CTAs per row, `places` chunks in a CTA's ring.
+struct RingShape {
+  int split, places;
+  bool hold;        // a row's chunks fit the cluster's rings
+  int64_t groups;   // rows in work at a time
+};
+
+// The narrowest split whose CTAs hold a row in half an SM's shared memory, with two
+// places left for the next row's chunks; with all of an SM's where eight CTAs' halves do
+// not; wider ones while all rows have a place at once.  The same with and without a
+// gradient, so that the losses' bits are.
+RingShape choose_ring(const pr_ctx* c, pr_dtype dt, int64_t n_rows, int64_t vocab) {
+  const int64_t words = vocab * (int64_t)esize(dt) / 16;
   const int64_t chunks = (words + prk::RG_CHUNK - 1) / prk::RG_CHUNK;
-  auto per_warp = [&](int w) { return (chunks + w - 1) / w; };
-  int i = 0;
-  while (i < 5 && per_warp(WARPS[i]) > prk::RG_NS - 2) ++i;
-  while (i < 5 && n_rows <= c->loss_places[i + 1] && chunks >= 2 * WARPS[i]) ++i;
-  RowShape s;
-  s.gw = std::min(WARPS[i], 16);
-  s.cluster = std::max(1, WARPS[i] / 16);
-  s.hold = per_warp(WARPS[i]) <= prk::RG_NS;
-  s.groups = std::min<int64_t>(n_rows, c->loss_places[i]);
-  const int64_t per_cta = 16 / s.gw;
-  s.grid = (unsigned)(s.cluster > 1 ? s.groups * s.cluster : (s.groups + per_cta - 1) / per_cta);
+  auto per_cta = [&](int split) { return (chunks + (1 << split) - 1) >> split; };
+  int split = 0;
+  while (split < 3 && per_cta(split) > prk::RG_FEW - 2) ++split;
+  const bool whole = per_cta(split) > prk::RG_FEW - 2;
+  while (split < 3 && n_rows <= c->loss_places[whole][split + 1] && per_cta(split) > 1) ++split;
+  RingShape s;
+  s.split = split;
+  s.places = whole ? prk::RG_MOST : prk::RG_FEW;
+  s.hold = per_cta(split) <= s.places;
+  s.groups = std::min<int64_t>(n_rows, c->loss_places[whole][split]);
+  return s;
+}
+
+// The forward kernel's launch: 512 threads per row, 128 where those have less than a
+// load each; clusters where all rows have a place at once all the same.
+struct ForwardShape {
+  bool small;
+  int split;
+  int64_t groups;
+};
+
+ForwardShape choose_forward(const pr_ctx* c, pr_dtype dt, int64_t n_rows, int64_t vocab) {
+  const int64_t words = vocab * (int64_t)esize(dt) / 16;
+  ForwardShape s;
+  s.small = words <= 4 * FW_SMALL;
+  s.split = 0;
+  const int64_t places = (int64_t)c->num_sms * (1024 / (s.small ? FW_SMALL : FW_NT));
+  // (a cluster's CTAs lie in one GPC: eight of them do not fill every SM)
+  while (!s.small && s.split < 3 && n_rows << (s.split + 1) <= places * 3 / 4 &&
+         words >> s.split > 4 * FW_NT)
+    ++s.split;
+  s.groups = std::min(n_rows, places >> s.split);
   return s;
 }
 
@@ -185,13 +211,23 @@ pr_status launch_plan(pr_ctx* c, prk::LossArgs& a, int pairs, cudaStream_t s) {
   return st == PR_OK ? timing_mark(c, s) : st;
 }
 
-pr_status launch_ring(pr_ctx* c, prk::LossArgs& a, pr_dtype dt, const RowShape& shape, bool hold,
-                      bool pref, cudaStream_t s) {
-  const void* kern = dt == PR_DTYPE_BF16 ? ring_kernel<__nv_bfloat16>(shape.gw, hold, pref)
-                                         : ring_kernel<float>(shape.gw, hold, pref);
+pr_status launch_ring(pr_ctx* c, prk::LossArgs& a, pr_dtype dt, const RingShape& shape, bool hold,
+                      cudaStream_t s) {
+  int places = shape.places;
+  void* args[] = {&a, &places};
+  const pr_status st = launch(ring_kernel(dt, hold), (unsigned)(shape.groups << shape.split),
+                              prk::RG_NT, prk::ring_bytes(places), 1u << shape.split, args, s);
+  return st == PR_OK ? timing_mark(c, s) : st;
+}
+
+pr_status launch_forward(pr_ctx* c, prk::LossArgs& a, pr_dtype dt, const ForwardShape& shape,
+                         bool pref, cudaStream_t s) {
   void* args[] = {&a};
-  const pr_status st = launch(kern, shape.grid, prk::RG_NW * 32, sizeof(prk::RingSmem),
-                              (unsigned)shape.cluster, args, s);
+  const pr_status st =
+      launch(dt == PR_DTYPE_BF16 ? forward_kernel<__nv_bfloat16>(shape.small, pref)
+                                 : forward_kernel<float>(shape.small, pref),
+             (unsigned)(shape.groups << shape.split), shape.small ? FW_SMALL : FW_NT, 0,
+             1u << shape.split, args, s);
   return st == PR_OK ? timing_mark(c, s) : st;
 }
 
@@ -226,7 +262,6 @@ void fill(prk::LossArgs& a, pr_ctx* c, const void* logits, int64_t n_rows, int64
   a.ref_logp = ref_logp;
   a.inv_t = (float)(1.0 / (double)temperature);
   a.c2 = (float)(1.4426950408889634 / (double)temperature);
-  a.skew = (float)((double)a.c2 * 0.6931471805599453 - (double)a.inv_t);
   a.grad_scale = grad_scale;
   a.stats = stats;
   a.logp = logp;
@@ -272,13 +307,16 @@ pr_status pr_policy_loss(pr_ctx* c, const void* logits, pr_dtype dt, int64_t n_r
   a.clip_hi = 1.f + p->clip_high;
   a.kl_coef = p->kl_coef;
   if ((st = ring_setup(c)) != PR_OK) return st;
-  const RowShape shape = choose_shape(c, dt, n_rows, vocab);
-  const bool hold = grad && shape.hold, later = grad && !shape.hold;
-  if ((st = workspace(c, a, shape.groups, false, later)) != PR_OK) return st;
+  const RingShape ring = choose_ring(c, dt, n_rows, vocab);
+  const ForwardShape forward = choose_forward(c, dt, n_rows, vocab);
+  if ((st = workspace(c, a, std::max(ring.groups, forward.groups), false, !ring.hold)) != PR_OK)
+    return st;
   if ((st = timing_begin(c, s)) != PR_OK) return st;
   if ((st = launch_plan(c, a, 0, s)) != PR_OK) return st;
-  if ((st = launch_ring(c, a, dt, shape, hold, false, s)) != PR_OK) return st;
-  return later ? launch_backward(c, a, dt, false, s) : PR_OK;
+  if (ring.hold) return launch_ring(c, a, dt, ring, grad != nullptr, s);
+  // rows of more than eight SMs' shared memory
+  if ((st = launch_forward(c, a, dt, forward, false, s)) != PR_OK) return st;
+  return grad ? launch_backward(c, a, dt, false, s) : PR_OK;
 }
 
 pr_status pr_preference_loss(pr_ctx* c, const void* logits, pr_dtype dt, int64_t n_rows,
@@ -310,12 +348,12 @@ pr_status pr_preference_loss(pr_ctx* c, const void* logits, pr_dtype dt, int64_t
   a.margin = p->margin;
   a.loss = p->loss;
   a.length_norm = p->length_norm ? 1 : 0;
-  if ((st = ring_setup(c)) != PR_OK) return st;
-  const RowShape shape = choose_shape(c, dt, n_rows, vocab);
   if ((st = workspace(c, a, 0, true, true)) != PR_OK) return st;
   if ((st = timing_begin(c, s)) != PR_OK) return st;
   if ((st = launch_plan(c, a, 1, s)) != PR_OK) return st;
-  if (n_rows > 0 && (st = launch_ring(c, a, dt, shape, false, true, s)) != PR_OK) return st;
+  if (n_rows > 0 && (st = launch_forward(c, a, dt, choose_forward(c, dt, n_rows, vocab), true, s)) !=
+                        PR_OK)
+    return st;
   void* args[] = {&a};
   if ((st = launch(reinterpret_cast<const void*>(&prk::loss_pairs), (unsigned)((n_req / 2 + 7) / 8),
                    256, 0, 1, args, s)) != PR_OK ||
