@@ -64,6 +64,7 @@ struct pr_ctx {
   // the training losses: workspace, grown on demand
   void* loss_ws = nullptr;
   size_t loss_ws_bytes = 0;
+  size_t loss_rows = 0;                // rows that its arrivals have room for
   bool loss_ready = false;             // shared memory opt-ins made
   int loss_places[2][4] = {};          // clusters of 1, 2, 4, 8 CTAs resident; half, all of the SMs
   // PR_OPT_TIMING: events after each kernel of the last multi-kernel call

@@ -47,89 +47,202 @@ struct LossArgs {
   void* grad;
   int64_t grad_stride;
   // workspace
-  int32_t* ticket;     // [2] arrivals, zero between calls
+  int32_t* ticket;     // [2] arrivals, zero between calls (the plan's, the statistics')
   int64_t* totals;     // counted tokens; requests with some (policy) or pairs of such
   int32_t* count;      // [n_req] counted tokens
   int32_t* row_req;    // [n_rows] request of a row that counts, else -1
+  int32_t* block;      // [blocks of PL_BLOCK rows] counted rows, then those before the block
+  int4* list;          // [n_rows] {row, request, token} of the rows that count
+  int32_t* skipped;    // [n_rows] the others
+  int32_t* arrived;    // [n_rows] pieces of a row that are summed; zero between calls
+  float2* piece;       // [CTAs][2] their sums
   float* coef;         // [n_req] dL / d log ratio (preference)
   float* term;         // [n_req / 2][LS_NSTAT] the pairs' statistics
-  float4* state;       // [n_rows][2] K, adj, rest, M; l - ref (preference) or dL/dl / T
+  float4* state;       // [n_rows] K, adj, rest, M: RowState
+  float* z;            // [n_rows] l - ref (preference) or dL/dl / T
   double* part;        // [groups][LS_NSTAT] statistics of each group's rows
   uint32_t* ctx_flags;
 };
 
-// ---- counted tokens -------------------------------------------------------------------
+// ---- which rows count -----------------------------------------------------------------
+//
+// The rows that count are listed in order, so that every CTA gets its even share of
+// them whatever the mask (8,847 rows, a tenth of them masked at random, dealt out as they lie:
+// 15 for some CTAs and 13.1 on average, @@ us for @@).
+constexpr int PL_BLOCK = 1024;  // rows of a block
+constexpr int PL_FEW = 1024;    // requests that one CTA counts in shared memory
 
-// The first n_req CTAs count a request's tokens each, the last of them to finish sums
-// up; the others find the requests of 256 rows each.
-static __global__ void __launch_bounds__(256) loss_plan(const LossArgs a, int pairs) {
-  __shared__ int64_t part[8];
+// the request that counts row t, else -1
+__device__ __forceinline__ int32_t counted_by(const LossArgs& a, int64_t t) {
+  if (a.mask && a.mask[t] == 0) return -1;
+  if (!a.offsets) return 0;
+  int32_t r = 0, hi = a.n_req - 1;  // the largest r with offsets[r] <= t
+  while (r < hi) {
+    const int32_t mid = (int32_t)(((int64_t)r + hi + 1) >> 1);
+    if (a.offsets[mid] <= t) r = mid;
+    else hi = mid - 1;
+  }
+  const int64_t lo = a.offsets[r], up = a.offsets[r + 1];
+  return lo < 0 || up > a.n_rows || t < lo || t >= up ? -1 : r;
+}
+// whether request r's bounds are wrong; its flags
+__device__ __forceinline__ bool bad_bounds(const LossArgs& a, int64_t r, int64_t& lo, int64_t& hi) {
+  lo = a.offsets ? a.offsets[r] : 0;
+  hi = a.offsets ? a.offsets[r + 1] : a.n_rows;
+  const bool bad = lo < 0 || hi < lo || hi > a.n_rows;
+  if (bad) atomicOr(a.ctx_flags, FLAG_BAD_OFFSETS);
+  else if (lo == hi) atomicOr(a.ctx_flags, FLAG_EMPTY_REQ);
+  return bad;
+}
+// row t, counted by r, among the others: `before` counted ones precede it
+__device__ __forceinline__ void put_row(const LossArgs& a, int64_t t, int32_t r, int32_t before) {
+  a.row_req[t] = r;
+  if (r >= 0) {
+    a.list[before] = make_int4((int32_t)t, r, a.chosen[t], 0);
+  } else {
+    a.skipped[t - before] = (int32_t)t;
+    a.logp[t] = 0.f;
+  }
+}
+// exclusive sum over a CTA of 1,024 threads of a flag; the total in `all`
+__device__ __forceinline__ int32_t block_rank(bool on, int32_t* warps, int32_t& all) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const unsigned b = __ballot_sync(FULL, on);
+  __syncthreads();
+  if (lane == 0) warps[warp] = __popc(b);
+  __syncthreads();
+  const int32_t c = warps[lane];
+  const int32_t below = __reduce_add_sync(FULL, lane < warp ? c : 0);
+  all = __reduce_add_sync(FULL, c);
+  return below + __popc(b & ((1u << lane) - 1u));
+}
+__device__ __forceinline__ int64_t block_total(int64_t v, int64_t* part) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(FULL, v, o);
+  __syncthreads();
+  if (lane == 0) part[warp] = v;
+  __syncthreads();
+  v = part[lane];
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(FULL, v, o);
+  return v;
+}
+
+// Small batches: everything by one CTA.
+static __global__ void __launch_bounds__(PL_BLOCK) loss_plan(const LossArgs a, int pairs) {
+  __shared__ int32_t count[PL_FEW], warps[32];
+  __shared__ int64_t part[32];
+  pdl_wait();
+  pdl_trigger();
+  const int tid = threadIdx.x;
+  if (tid < a.n_req) count[tid] = 0;
+  int32_t before = 0;
+  for (int64_t t0 = 0; t0 < a.n_rows; t0 += PL_BLOCK) {
+    const int64_t t = t0 + tid;
+    const int32_t r = t < a.n_rows ? counted_by(a, t) : -1;
+    int32_t all;
+    const int32_t rank = block_rank(r >= 0, warps, all);
+    if (t < a.n_rows) put_row(a, t, r, before + rank);
+    if (r >= 0) atomicAdd(&count[r], 1);  // (whole numbers: in any order)
+    before += all;
+  }
+  __syncthreads();
+  int64_t used = 0;
+  if (tid < a.n_req) {
+    int64_t lo, hi;
+    bad_bounds(a, tid, lo, hi);
+    a.count[tid] = count[tid];
+    if (!pairs) used = count[tid] > 0;
+    else if ((tid & 1) == 0) used = count[tid] > 0 && count[tid + 1] > 0;
+  }
+  used = block_total(used, part);
+  if (tid == 0) {
+    a.totals[0] = before;
+    a.totals[1] = used;
+  }
+}
+
+// Large ones: the first n_req CTAs count a request's rows each, the others those of a
+// block of rows; the last to finish sums up.  Then loss_list.
+static __global__ void __launch_bounds__(PL_BLOCK) loss_count(const LossArgs a, int pairs) {
+  __shared__ int32_t warps[32];
+  __shared__ int64_t part[32];
   __shared__ int last;
   pdl_wait();
   pdl_trigger();
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int tid = threadIdx.x;
+  const int32_t blocks = (int32_t)((a.n_rows + PL_BLOCK - 1) / PL_BLOCK);
   if ((int64_t)blockIdx.x >= a.n_req) {
-    const int64_t t = ((int64_t)blockIdx.x - a.n_req) * 256 + tid;
-    if (t >= a.n_rows) return;
-    int32_t r = -1;
-    if (!a.mask || a.mask[t] != 0) {
-      r = 0;
-      if (a.offsets) {
-        int32_t hi = a.n_req - 1;  // the largest r with offsets[r] <= t
-        while (r < hi) {
-          const int32_t mid = (int32_t)(((int64_t)r + hi + 1) >> 1);
-          if (a.offsets[mid] <= t) r = mid;
-          else hi = mid - 1;
-        }
-        const int64_t lo = a.offsets[r], up = a.offsets[r + 1];
-        if (lo < 0 || up > a.n_rows || t < lo || t >= up) r = -1;
-      }
+    const int64_t b = (int64_t)blockIdx.x - a.n_req, t = b * PL_BLOCK + tid;
+    const int32_t r = t < a.n_rows ? counted_by(a, t) : -1;
+    if (t < a.n_rows) a.row_req[t] = r;
+    int32_t all;
+    block_rank(r >= 0, warps, all);
+    if (tid == 0) a.block[b] = all;
+  } else {
+    int64_t lo = 0, hi = 0, n = 0;
+    const int64_t r = blockIdx.x;
+    __shared__ int bad;
+    if (tid == 0) bad = bad_bounds(a, r, lo, hi);
+    __syncthreads();
+    lo = a.offsets ? a.offsets[r] : 0;
+    hi = a.offsets ? a.offsets[r + 1] : a.n_rows;
+    if (!bad) {
+      if (!a.mask) n = tid == 0 ? hi - lo : 0;
+      else
+        for (int64_t t = lo + tid; t < hi; t += PL_BLOCK) n += a.mask[t] != 0;
     }
-    a.row_req[t] = r;
-    return;
+    n = block_total(n, part);
+    if (tid == 0) a.count[r] = (int32_t)n;
   }
-  const int64_t r = blockIdx.x;
-  const int64_t lo = a.offsets ? a.offsets[r] : 0, hi = a.offsets ? a.offsets[r + 1] : a.n_rows;
-  const bool bad = lo < 0 || hi < lo || hi > a.n_rows;
-  int64_t n = 0;
-  if (!bad) {
-    if (!a.mask) n = tid == 0 ? hi - lo : 0;
-    else
-      for (int64_t t = lo + tid; t < hi; t += 256) n += a.mask[t] != 0;
-  }
-  auto block_sum = [&](int64_t v) {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(FULL, v, o);
-    __syncthreads();
-    if (lane == 0) part[warp] = v;
-    __syncthreads();
-    v = 0;
-    for (int w = 0; w < 8; ++w) v += part[w];
-    return v;
-  };
-  n = block_sum(n);
+  __syncthreads();
   if (tid == 0) {
-    a.count[r] = (int32_t)n;
-    if (bad) atomicOr(a.ctx_flags, FLAG_BAD_OFFSETS);
-    else if (lo == hi) atomicOr(a.ctx_flags, FLAG_EMPTY_REQ);
-    last = atom_add_acq_rel(a.ticket, 1) == a.n_req - 1;
+    __threadfence();
+    last = atom_add_acq_rel(a.ticket, 1) == (int)gridDim.x - 1;
   }
   __syncthreads();
   if (!last) return;
-  int64_t total = 0, used = 0;
-  for (int64_t q = tid; q < a.n_req; q += 256) {
+  int64_t used = 0;
+  for (int64_t q = tid; q < a.n_req; q += PL_BLOCK) {
     const int32_t k = __ldcg(a.count + q);
-    total += k;
     if (!pairs) used += k > 0;
     else if ((q & 1) == 0) used += k > 0 && __ldcg(a.count + q + 1) > 0;
   }
-  total = block_sum(total);
-  used = block_sum(used);
+  used = block_total(used, part);
+  int32_t before = 0;  // (blocks: a thousand at a time)
+  for (int32_t b0 = 0; b0 < blocks; b0 += PL_BLOCK) {
+    const int32_t c = b0 + tid < blocks ? __ldcg(a.block + b0 + tid) : 0;
+    int32_t x = c;
+    const int lane = tid & 31, warp = tid >> 5;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int32_t y = __shfl_up_sync(FULL, x, o);
+      if (lane >= o) x += y;
+    }
+    __syncthreads();
+    if (lane == 31) warps[warp] = x;
+    __syncthreads();
+    const int32_t w = warps[lane];
+    x += __reduce_add_sync(FULL, lane < warp ? w : 0);
+    if (b0 + tid < blocks) a.block[b0 + tid] = before + x - c;
+    before += __reduce_add_sync(FULL, w);
+  }
   if (tid == 0) {
-    a.totals[0] = total;
+    a.totals[0] = before;
     a.totals[1] = used;
     *a.ticket = 0;
   }
+}
+static __global__ void __launch_bounds__(PL_BLOCK) loss_list(const LossArgs a) {
+  __shared__ int32_t warps[32];
+  pdl_wait();
+  pdl_trigger();
+  const int64_t t = (int64_t)blockIdx.x * PL_BLOCK + threadIdx.x;
+  const int32_t r = t < a.n_rows ? __ldcg(a.row_req + t) : -1;
+  int32_t all;
+  const int32_t rank = block_rank(r >= 0, warps, all);
+  if (t < a.n_rows) put_row(a, t, r, __ldcg(a.block + blockIdx.x) + rank);
 }
 
 // ---- the losses of one row / pair -------------------------------------------------------
@@ -360,7 +473,7 @@ __device__ __forceinline__ int32_t end_of(const LossArgs& a, const Share& s, int
 
 // what a row's end needs, fetched while the rows before it are in work
 struct RowIn {
-  int32_t r, y, count;
+  int32_t y, count;
   float xy, old, ref, adv, edge;
 };
 
@@ -456,19 +569,20 @@ __device__ __noinline__ void end_math(const LossArgs& a, int64_t row, const RowI
       if (in.y < 0 || (int64_t)in.y >= a.vocab) atomicOr(a.ctx_flags, FLAG_BAD_CHOSEN);
       else if (isnan(l)) atomicOr(a.ctx_flags, FLAG_NONFINITE);
       if (!HOLD && a.state) {
-        a.state[2 * row] = make_float4(st.K, st.adj, st.rest, st.M);
-        a.state[2 * row + 1].x = PREF ? (l - in.ref) + e.l_lo : kk;
+        a.state[row] = make_float4(st.K, st.adj, st.rest, st.M);
+        a.z[row] = PREF ? (l - in.ref) + e.l_lo : kk;
       }
     }
   }
 }
 
-// The scalars of row `row` of request r with token y.  Whole warp.
+// The scalars of a listed row {row, request, token}.  Whole warp.
 template <typename T, bool PREF>
-__device__ __forceinline__ RowIn fetch_row(const LossArgs& a, const Share& s, int64_t row,
-                                           int32_t r, int32_t y, int lane) {
+__device__ __forceinline__ RowIn fetch_row(const LossArgs& a, const Share& s, const int4& ref,
+                                           int lane) {
+  const int64_t row = ref.x;
+  const int32_t r = ref.y, y = ref.z;
   RowIn in;
-  in.r = r;
   in.y = y;
   in.count = 1;
   in.xy = NAN;
@@ -526,9 +640,10 @@ __device__ __forceinline__ void raise_to(const LossArgs& a, float xy, float& M, 
   M = fminf(top, -LS_MIN);
 }
 
-// a thread's words into its sum (k, S); the first ones give k
+// a thread's words into its sum (k, S); the row's first ones give k
 template <typename T, int N>
-__device__ __forceinline__ void add_words(float& k, float2& S, const uint4 (&v)[N], float c2) {
+__device__ __forceinline__ void add_words(float& k, float2& S, const uint4 (&v)[N], float c2,
+                                          bool begin) {
   using Tr = Traits<T>;
   auto top = [&]() {
     float m = Tr::gmax(v[0]);
@@ -536,7 +651,7 @@ __device__ __forceinline__ void add_words(float& k, float2& S, const uint4 (&v)[
     for (int q = 1; q < N; ++q) m = fmaxf(m, Tr::gmax(v[q]));
     return fmaxf(m * c2, -3e38f);
   };
-  if (k == -3.4e38f) k = top();
+  if (begin) k = top();
   const float2 before = S;
 #pragma unroll
   for (int q = 0; q < N; ++q) add_word<T>(S, v[q], c2, -k);
@@ -548,8 +663,6 @@ __device__ __forceinline__ void add_words(float& k, float2& S, const uint4 (&v)[
     for (int q = 0; q < N; ++q) add_word<T>(S, v[q], c2, -k);
   }
 }
-constexpr float K_NONE = -3.4e38f;  // add_words: no word yet
-
 // The statistics: a warp's sums over its rows to a.part[at], the last of `count` warps
 // joins all in order.  Whole warp.
 __device__ __forceinline__ void write_stats(const LossArgs& a, const float2* stat, int64_t at,
@@ -578,128 +691,201 @@ __device__ __forceinline__ void write_stats(const LossArgs& a, const float2* sta
   }
 }
 
+// every CTA's (k, R) of a cluster, by lane: written into the peers' `to`, whose barrier
+// counts the bytes.  Whole warp; false when the wait has run out.
+__device__ __forceinline__ bool ring_wait(uint32_t bar, uint32_t parity, uint32_t* flags) {
+  // (the clock of ring_wait_slow is read only after some thousand tests)
+  for (int i = 0; i < 4096; ++i)
+    if (ring_test(bar, parity)) return true;
+  return ring_wait_slow(bar, parity, flags);
+}
+__device__ __forceinline__ uint32_t sm_addr(const void* p) {
+  return (uint32_t)__cvta_generic_to_shared(p);
+}
+__device__ __forceinline__ void bar_init(uint64_t* b, int n) {
+  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(sm_addr(b)), "r"(n) : "memory");
+}
+__device__ __forceinline__ void bar_arrive(uint64_t* b) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(sm_addr(b)) : "memory");
+}
+__device__ __forceinline__ void bar_expect(uint64_t* b, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(sm_addr(b)), "r"(bytes)
+               : "memory");
+}
+__device__ __forceinline__ float2 exchange(float2* to, uint64_t* bar, uint32_t phase, float k,
+                                           float R, uint32_t C, uint32_t rank, bool& ok,
+                                           uint32_t* flags, int lane) {
+  if (lane < (int)C)
+    asm volatile(
+        "st.async.shared::cluster.mbarrier::complete_tx::bytes.b64 [%0], %1, [%2];" ::"r"(
+            dsmem_addr(to + rank, (uint32_t)lane)),
+        "l"((uint64_t)__float_as_uint(k) | (uint64_t)__float_as_uint(R) << 32),
+        "r"(dsmem_addr(bar, (uint32_t)lane))
+        : "memory");
+  __syncwarp();
+  if (ok) ok = ring_wait(sm_addr(bar), phase, flags);
+  __syncwarp();
+  const float2 p = lane < (int)C ? to[lane] : make_float2(LS_MIN, 0.f);
+  __syncwarp();
+  if (lane == 0) bar_expect(bar, 8 * C);
+  return p;
+}
+
 // ---- forward alone ----------------------------------------------------------------------
 //
-// A CTA, or a cluster of them where there are few rows, reads a row with wide loads into
-// registers, four per thread in flight, and goes on with its next one while one of its
-// warps, another one for each row, takes the row's end.  Three CTAs of 512 threads
-// on an SM read 7.2 TB/s (2.4 GB of V = 151,936 bf16 in 335 us, rows' ends apart).
-template <int NT>
+// The rows' tiles of 16 KB, one row after the other, are dealt out in equal runs: a CTA
+// has the end of a row, some whole ones and the beginning of another, or, where there are few
+// rows, a piece of one.  (A row each instead: 2,073 rows of V = 262,144 fp32 are 3.4
+// for each CTA, and four for some: @@ us for @@.)  Eight warps sum, with wide loads
+// into registers, four per thread in flight; a ninth joins their sums and takes the end
+// of the rows that lie in this CTA whole.  The sums of the other rows' pieces go through
+// global memory, and the warp that brings a row's last piece joins them in the row's
+// order and takes its end.
+constexpr int FW_NW = 8;
+constexpr int FW_NT = 32 * (FW_NW + 1);
+constexpr int FW_U = 4;
+constexpr int FW_TILE = 32 * FW_NW * FW_U;  // words
+constexpr int FW_CTAS = 4;                  // on an SM
 struct ForwardSmem {
-  float2 part[2][NT / 32];
-  float2 cta[2][MAXC];
-  float2 again[MAXC];
-  float2 stat[NT / 32][RG_TERMS];
-  RowOut out[NT / 32];
+  float2 part[2][FW_NW];
+  float2 stat[RG_TERMS];
+  RowOut out;
 };
+// the run of CTA b: tiles [run_begin(b), run_begin(b + 1)); the CTA of tile t
+__device__ __forceinline__ int64_t run_begin(int64_t b, int64_t tiles, int64_t G) {
+  return b * tiles / G;
+}
+__device__ __forceinline__ int64_t run_of(int64_t t, int64_t tiles, int64_t G) {
+  return ((t + 1) * G - 1) / tiles;
+}
 
-template <typename T, int NT, bool PREF>
-__global__ void __launch_bounds__(NT, 1024 / NT) loss_forward(const __grid_constant__ LossArgs a) {
+template <typename T, bool PREF>
+__global__ void __launch_bounds__(FW_NT, FW_CTAS) loss_forward(const __grid_constant__ LossArgs a) {
   using Tr = Traits<T>;
-  constexpr int NW = NT / 32, U = 4;
-  __shared__ ForwardSmem<NT> sm;
+  __shared__ ForwardSmem sm;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  uint32_t C, rank;
-  asm("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(C));
-  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
-  const int64_t G = gridDim.x / C, first = blockIdx.x / C;
-  if (lane < RG_TERMS) sm.stat[warp][lane] = make_float2(0.f, 0.f);
+  if (tid < RG_TERMS) sm.stat[tid] = make_float2(0.f, 0.f);
   __syncthreads();
-  if (C > 1) cluster_sync_all();
   pdl_wait();
   pdl_trigger();
-  auto request = [&](int64_t row) { return row < a.n_rows ? __ldcg(a.row_req + row) : -1; };
-  auto token = [&](int64_t row) { return row < a.n_rows ? __ldcg(a.chosen + row) : 0; };
-  const double share = PREF ? 0.0 : 1.0 / (double)__ldcg(a.totals + (a.norm ? 1 : 0));
-  const uint4 NEG = make_uint4(Tr::NEG_WORD, Tr::NEG_WORD, Tr::NEG_WORD, Tr::NEG_WORD);
-  int turn = 0, buf = 0;
-  int32_t r = request(first), y = token(first);
-  for (int64_t row = first; row < a.n_rows; row += G) {
-    const int32_t rn = request(row + G), yn = token(row + G);
-    const bool mine = turn == warp;
-    turn = turn + 1 == NW ? 0 : turn + 1;
-    if (r < 0) {
-      if (mine && lane == 0 && rank == 0) a.logp[row] = 0.f;
-      r = rn;
-      y = yn;
-      continue;
-    }
-    const Share sh = share_of<T>(a, row, C, rank);
-    RowIn in;
-    if (mine) in = fetch_row<T, PREF>(a, sh, row, r, y, lane);
-    const int32_t yw = word_of<T>(a, sh, y);
-    const int yj = y - sh.head - yw * Tr::VEC;
-    const uint4* xw = reinterpret_cast<const uint4*>(sh.x + sizeof(T) * sh.head);
-    float k = K_NONE;
-    float2 S = make_float2(0.f, 0.f);
-    uint4 v[U];
-    int32_t i = sh.w0 + tid;
-    for (; i - tid + U * NT <= sh.w1; i += U * NT) {
-#pragma unroll
-      for (int q = 0; q < U; ++q) v[q] = ld_stream(xw + i + q * NT);
-      if ((uint32_t)(yw - (i - tid)) < (uint32_t)(U * NT)) {
-#pragma unroll
-        for (int q = 0; q < U; ++q)
-          if (i + q * NT == yw) v[q] = without<T>(v[q], yj);
+  const int64_t live = __ldcg(a.totals);
+  const int64_t most = (a.vocab + Tr::VEC - 1) / Tr::VEC;              // words of a row
+  const int64_t per_row = (most + FW_TILE - 1) / FW_TILE, tiles = live * per_row;
+  const int64_t G = min((int64_t)gridDim.x, max(tiles, (int64_t)1)), b = blockIdx.x;
+  if (b >= G) return;
+  const int64_t t0 = run_begin(b, tiles, G), t1 = run_begin(b + 1, tiles, G);
+  auto ref_of = [&](int64_t i) {  // the i-th row that counts
+    return i < live ? __ldcg(a.list + i) : make_int4(0, -1, 0, 0);
+  };
+  int64_t i = t0 / per_row;
+  int32_t j0 = (int32_t)(t0 - i * per_row);  // the first tile of row i here
+  int64_t left = t1 - t0;
+  uint32_t n = 0;  // pieces summed
+  if (warp == FW_NW) {
+    // ---- the rows' ends
+    const double share = PREF ? 0.0 : 1.0 / (double)__ldcg(a.totals + (a.norm ? 1 : 0));
+    int4 ref = ref_of(i), ref1 = ref_of(i + 1);
+    RowIn in = fetch_row<T, PREF>(a, share_of<T>(a, ref.x, 1, 0), ref, lane);
+    for (; left > 0; ++i, j0 = 0) {
+      const RowIn next = fetch_row<T, PREF>(a, share_of<T>(a, ref1.x, 1, 0), ref1, lane);
+      const int64_t row = ref.x;
+      ref = ref1;
+      ref1 = ref_of(i + 2);
+      const int64_t here = min(left, per_row - j0);
+      left -= here;
+      const int buf = n & 1;
+      ++n;
+      named_bar_sync(BAR_FULL + buf, FW_NT);
+      float k, R, M = INFINITY;
+      join(lane < FW_NW ? sm.part[buf][lane] : make_float2(-3e38f, 0.f), 1.f, k, R);
+      __syncwarp();
+      named_bar_arrive(BAR_EMPTY + buf, FW_NT);
+      if (here < per_row) {
+        const int64_t bs = run_of(i * per_row, tiles, G), be = run_of((i + 1) * per_row - 1, tiles, G);
+        int last = 0;
+        if (lane == 0) {
+          a.piece[2 * b + (j0 == 0 ? 1 : 0)] = make_float2(k, R);
+          last = atom_add_acq_rel(a.arrived + i, 1) == (int)(be - bs);
+          if (last) a.arrived[i] = 0;
+        }
+        last = __shfl_sync(FULL, last, 0);
+        if (!last) {
+          in = next;
+          continue;
+        }
+        k = -3e38f;
+        R = 0.f;
+        for (int64_t q = bs; q <= be; q += 32) {  // 32 pieces at a time
+          const float2 p = q + lane <= be ? __ldcg(a.piece + 2 * (q + lane) + (q + lane == bs ? 1 : 0))
+                                          : make_float2(-3e38f, 0.f);
+          float k1, R1;
+          join(p, 1.f, k1, R1);
+          const float top = fmaxf(k, k1);
+          R = R * rescale2(k - top) + R1 * rescale2(k1 - top);
+          k = top;
+        }
       }
-      add_words<T>(k, S, v, a.c2);
-    }
-    if (i - tid < sh.w1) {
-#pragma unroll
-      for (int q = 0; q < U; ++q) {
-        v[q] = i + q * NT < sh.w1 ? ld_stream(xw + i + q * NT) : NEG;
-        if (i + q * NT == yw) v[q] = without<T>(v[q], yj);
-      }
-      add_words<T>(k, S, v, a.c2);
-    }
-    float R;
-    join(make_float2(fmaxf(k, -3e38f), S.x + S.y), 1.f, k, R);
-    if (lane == 0) sm.part[buf][warp] = make_float2(k, R);
-    if (C == 1) __syncthreads();
-    else {
-      __syncthreads();
-      if (warp == 0) {
-        join(lane < NW ? sm.part[buf][lane] : make_float2(-3e38f, 0.f), 1.f, k, R);
-        if (lane < (int)C)
-          dsmem_st_u64(dsmem_addr(&sm.cta[buf][rank], (uint32_t)lane),
-                       (uint64_t)__float_as_uint(k) | (uint64_t)__float_as_uint(R) << 32);
-        __syncwarp();
-      }
-      cluster_sync_all();
-    }
-    // the row's end; the sums' places are written again two rows on, behind a barrier that
-    // this warp joins after it
-    if (mine) {
-      if (C == 1) join(lane < NW ? sm.part[buf][lane] : make_float2(-3e38f, 0.f), 1.f, k, R);
-      else join(lane < (int)C ? sm.cta[buf][lane] : make_float2(-3e38f, 0.f), 1.f, k, R);
+      const Share sh = share_of<T>(a, row, 1, 0);
       add_ends(a, sh, in, k, R, lane);
-      float M = INFINITY;
       if (sum_again(k, R, in.xy, a.c2)) {
-        Share all = sh;  // (nothing of the row is written: every CTA may read all of it)
-        all.w0 = 0;
-        all.w1 = all.words;
-        robust_sum<T>(a, all, true, in.y, M, R, lane);
+        robust_sum<T>(a, sh, true, in.y, M, R, lane);
         raise_to(a, in.xy, M, R);
       }
       const float wt = PREF ? 0.f : (float)(a.norm ? share / (double)in.count : share);
-      end_math<false, PREF>(a, row, in, k, R, M, wt, rank == 0, &sm.out[warp], sm.stat[warp], lane);
+      end_math<false, PREF>(a, row, in, k, R, M, wt, true, &sm.out, sm.stat, lane);
+      in = next;
     }
-    buf ^= 1;
-    r = rn;
-    y = yn;
+  } else {
+    const uint4 NEG = make_uint4(Tr::NEG_WORD, Tr::NEG_WORD, Tr::NEG_WORD, Tr::NEG_WORD);
+    int4 ref = ref_of(i);
+    for (; left > 0; ++i, j0 = 0) {
+      const int4 ref1 = ref_of(i + 1);
+      const int32_t here = (int32_t)min(left, per_row - j0);
+      left -= here;
+      const Share sh = share_of<T>(a, ref.x, 1, 0);
+      const int32_t yw = word_of<T>(a, sh, ref.z);
+      const int yj = ref.z - sh.head - yw * Tr::VEC;
+      const uint4* xw = reinterpret_cast<const uint4*>(sh.x + sizeof(T) * sh.head) + tid;
+      float k = -3e38f;
+      float2 S = make_float2(0.f, 0.f);
+      uint4 v[FW_U];
+      int32_t w = j0 * FW_TILE;
+      const int32_t w0 = w, w1 = min(sh.words, w + here * FW_TILE);
+      for (; w + FW_TILE <= w1; w += FW_TILE) {
+#pragma unroll
+        for (int q = 0; q < FW_U; ++q) v[q] = ld_stream(xw + w + q * 32 * FW_NW);
+        if ((uint32_t)(yw - w) < (uint32_t)FW_TILE) {
+#pragma unroll
+          for (int q = 0; q < FW_U; ++q)
+            if (w + q * 32 * FW_NW + tid == yw) v[q] = without<T>(v[q], yj);
+        }
+        add_words<T>(k, S, v, a.c2, w == w0);
+      }
+      if (w < w1) {
+#pragma unroll
+        for (int q = 0; q < FW_U; ++q) {
+          const int32_t at = w + q * 32 * FW_NW + tid;
+          v[q] = at < w1 ? ld_stream(xw + w + q * 32 * FW_NW) : NEG;
+          if (at == yw) v[q] = without<T>(v[q], yj);
+        }
+        add_words<T>(k, S, v, a.c2, w == w0);
+      }
+      float R;
+      join(make_float2(k, S.x + S.y), 1.f, k, R);
+      const int buf = n & 1;
+      if (n >= 2) named_bar_sync(BAR_EMPTY + buf, FW_NT);
+      ++n;
+      if (lane == 0) sm.part[buf][warp] = make_float2(k, R);
+      __syncwarp();
+      __threadfence_block();
+      named_bar_arrive(BAR_FULL + buf, FW_NT);
+      ref = ref1;
+    }
+    // the last pieces' places: the other warp has arrived for each
+    for (uint32_t q = n >= 2 ? n - 2 : 0; q < n; ++q) named_bar_sync(BAR_EMPTY + (q & 1), FW_NT);
   }
-  if (PREF) return;
   __syncthreads();
-  if (warp != 0 || rank != 0) return;
-  if (lane < RG_TERMS)
-    for (int w = 1; w < NW; ++w) {  // (of few terms each: exact enough as they are)
-      const float2 q = sm.stat[w][lane];
-      float2& t = sm.stat[0][lane];
-      const float s = t.x + q.x, z = s - t.x;
-      t = make_float2(s, t.y + q.y + ((t.x - (s - z)) + (q.x - z)));
-    }
-  __syncwarp();
-  write_stats(a, sm.stat[0], first, min(G, a.n_rows), lane);
+  if (!PREF && warp == 0) write_stats(a, sm.stat, b, G, lane);
 }
 
 // ---- forward and backward in one pass -----------------------------------------------------
@@ -738,13 +924,6 @@ struct RingCtl {
 static_assert(sizeof(RingCtl) <= 1024 && SH_CHUNK == RG_CHUNK, "two CTAs on an SM");
 constexpr size_t ring_bytes(int places) { return 1024 + (size_t)places * RG_BYTES; }
 
-// Bounded wait: the clock of ring_wait_slow is read only after some thousand tests.
-__device__ __forceinline__ bool ring_wait(uint32_t bar, uint32_t parity, uint32_t* flags) {
-  for (int i = 0; i < 4096; ++i)
-    if (ring_test(bar, parity)) return true;
-  return ring_wait_slow(bar, parity, flags);
-}
-
 template <typename T, bool HOLD>
 __global__ void __launch_bounds__(RG_NT, 2)
     loss_ring(const __grid_constant__ LossArgs a, const int places) {
@@ -757,30 +936,19 @@ __global__ void __launch_bounds__(RG_NT, 2)
   asm("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(C));
   asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
   const int64_t G = gridDim.x / C, first = blockIdx.x / C;
-  auto addr = [](const void* p) { return (uint32_t)__cvta_generic_to_shared(p); };
-  auto init = [&](uint64_t* b, int n) {
-    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(addr(b)), "r"(n) : "memory");
-  };
-  auto arrive = [&](uint64_t* b) {
-    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(addr(b)) : "memory");
-  };
-  auto expect = [&](uint64_t* b, uint32_t bytes) {
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(addr(b)), "r"(bytes)
-                 : "memory");
-  };
   if (threadIdx.x == 0) {
     for (int i = 0; i < places; ++i) {
-      init(&sm.full[i], 1);
-      init(&sm.empty[i], RG_NW);
+      bar_init(&sm.full[i], 1);
+      bar_init(&sm.empty[i], RG_NW);
     }
     for (int s = 0; s < RG_SLOTS; ++s) {
-      init(&sm.part_bar[s], RG_NW);
-      init(&sm.out_bar[s], 1);
-      init(&sm.cta_bar[s], 1);
-      if (C > 1) expect(&sm.cta_bar[s], 8 * C);
+      bar_init(&sm.part_bar[s], RG_NW);
+      bar_init(&sm.out_bar[s], 1);
+      bar_init(&sm.cta_bar[s], 1);
+      if (C > 1) bar_expect(&sm.cta_bar[s], 8 * C);
     }
-    init(&sm.again_bar, 1);
-    if (C > 1) expect(&sm.again_bar, 8 * C);
+    bar_init(&sm.again_bar, 1);
+    if (C > 1) bar_expect(&sm.again_bar, 8 * C);
     for (int j = 0; j < RG_TERMS; ++j) sm.stat[j] = make_float2(0.f, 0.f);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -792,11 +960,13 @@ __global__ void __launch_bounds__(RG_NT, 2)
 
   bool ok = true;  // no wait has run out
   auto wait = [&](uint64_t* b, uint32_t phase) {
-    if (ok) ok = ring_wait(addr(b), phase, a.ctx_flags);
+    if (ok) ok = ring_wait(sm_addr(b), phase, a.ctx_flags);
     __syncwarp();
   };
-  auto request = [&](int64_t row) { return row < a.n_rows ? __ldcg(a.row_req + row) : -1; };
-  auto token = [&](int64_t row) { return row < a.n_rows ? __ldcg(a.chosen + row) : 0; };
+  const int32_t live = (int32_t)__ldcg(a.totals);
+  auto ref_of = [&](int64_t i) {  // the i-th row that counts
+    return i < live ? __ldcg(a.list + i) : make_int4(0, -1, 0, 0);
+  };
   int place = 0;         // of the ring
   uint32_t turn = 0u;    // how often it has been gone around, its last bit
   auto step = [&]() {
@@ -809,29 +979,27 @@ __global__ void __launch_bounds__(RG_NT, 2)
   if (warp == RG_NW) {
     // ---- bringing chunks in
     int64_t n = 0;
-    int32_t r = request(first);
-    for (int64_t row = first; row < a.n_rows; row += G) {
-      const int32_t rn = request(row + G);
-      if (r >= 0) {
-        const Share sh = share_of<T>(a, row, C, rank);
-        const char* src = sh.x + sizeof(T) * sh.head + 16 * (int64_t)sh.w0;
-        for (int32_t left = sh.w1 - sh.w0; left > 0; left -= RG_CHUNK) {
-          if (n >= places) wait(&sm.empty[place], turn ^ 1u);
-          if (ok && lane == 0) {
-            const uint32_t bytes = 16u * (uint32_t)min(RG_CHUNK, left);
-            expect(&sm.full[place], bytes);
-            asm volatile(
-                "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::
-                    "r"(addr(ring + (size_t)place * RG_BYTES)),
-                "l"(src), "r"(bytes), "r"(addr(&sm.full[place]))
-                : "memory");
-          }
-          src += RG_BYTES;
-          if (ok) ++n;
-          step();
+    int4 ref = ref_of(first);
+    for (int64_t i = first; i < live; i += G) {
+      const int4 ref1 = ref_of(i + G);
+      const Share sh = share_of<T>(a, ref.x, C, rank);
+      const char* src = sh.x + sizeof(T) * sh.head + 16 * (int64_t)sh.w0;
+      for (int32_t left = sh.w1 - sh.w0; left > 0; left -= RG_CHUNK) {
+        if (n >= places) wait(&sm.empty[place], turn ^ 1u);
+        if (ok && lane == 0) {
+          const uint32_t bytes = 16u * (uint32_t)min(RG_CHUNK, left);
+          bar_expect(&sm.full[place], bytes);
+          asm volatile(
+              "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::
+                  "r"(sm_addr(ring + (size_t)place * RG_BYTES)),
+              "l"(src), "r"(bytes), "r"(sm_addr(&sm.full[place]))
+              : "memory");
         }
+        src += RG_BYTES;
+        if (ok) ++n;
+        step();
       }
-      r = rn;
+      ref = ref1;
     }
     // no copy may be in flight when the CTA ends (as none is unless a wait ran out)
     ok = true;
@@ -840,43 +1008,17 @@ __global__ void __launch_bounds__(RG_NT, 2)
   } else if (warp == RG_NW + 1) {
     // ---- the rows' ends
     const double share = 1.0 / (double)__ldcg(a.totals + (a.norm ? 1 : 0));
-    // every CTA's (k, R), by lane
-    auto exchange = [&](float2* to, uint64_t* bar, uint32_t phase, float k, float R) {
-      if (lane < (int)C)
-        asm volatile(
-            "st.async.shared::cluster.mbarrier::complete_tx::bytes.b64 [%0], %1, [%2];" ::"r"(
-                dsmem_addr(to + rank, (uint32_t)lane)),
-            "l"((uint64_t)__float_as_uint(k) | (uint64_t)__float_as_uint(R) << 32),
-            "r"(dsmem_addr(bar, (uint32_t)lane))
-            : "memory");
-      __syncwarp();
-      wait(bar, phase);
-      const float2 p = lane < (int)C ? to[lane] : make_float2(LS_MIN, 0.f);
-      __syncwarp();
-      if (lane == 0) expect(bar, 8 * C);
-      return p;
-    };
     uint32_t n = 0, agains = 0;
-    int32_t r1 = request(first), y1 = token(first);
-    RowIn in = fetch_row<T, false>(a, share_of<T>(a, first, C, rank), first, r1, y1, lane);
-    r1 = request(first + G);
-    y1 = token(first + G);
-    for (int64_t row = first; row < a.n_rows; row += G) {
+    int4 ref = ref_of(first), ref1 = ref_of(first + G);
+    RowIn in = fetch_row<T, false>(a, share_of<T>(a, ref.x, C, rank), ref, lane);
+    for (int64_t i = first; i < live; i += G) {
+      const RowIn next = fetch_row<T, false>(a, share_of<T>(a, ref1.x, C, rank), ref1, lane);
+      const int64_t row = ref.x;
       const Share sh = share_of<T>(a, row, C, rank);
-      const RowIn next =
-          fetch_row<T, false>(a, share_of<T>(a, row + G, C, rank), row + G, r1, y1, lane);
-      r1 = request(row + 2 * G);
-      y1 = token(row + 2 * G);
+      ref = ref1;
+      ref1 = ref_of(i + 2 * G);
       const int32_t v = end_of(a, sh, lane);
       T* const g = reinterpret_cast<T*>(a.grad) + row * a.grad_stride;
-      if (in.r < 0) {
-        if (rank == 0) {
-          if (lane == 0) a.logp[row] = 0.f;
-          if (HOLD && v >= 0) put(g + v, 0.f);
-        }
-        in = next;
-        continue;
-      }
       const int s = n % RG_SLOTS;
       const uint32_t phase = (n / RG_SLOTS) & 1u;
       ++n;
@@ -887,11 +1029,12 @@ __global__ void __launch_bounds__(RG_NT, 2)
       // (a peer that has this CTA's sum may write its part of the gradient, over the
       // logits: what is read of that part has to be here)
       in.xy = __shfl_sync(FULL, in.xy, 0);
-      if (C > 1) join(exchange(sm.cta[s], &sm.cta_bar[s], phase, k, R), 1.f, k, R);
+      if (C > 1) join(exchange(sm.cta[s], &sm.cta_bar[s], phase, k, R, C, rank, ok, a.ctx_flags, lane), 1.f, k, R);
       if (sum_again(k, R, in.xy, a.c2)) {
         robust_sum<T>(a, sh, rank == 0, in.y, M, R, lane);
         if (C > 1) {
-          join(exchange(sm.again, &sm.again_bar, agains & 1u, M, R), a.c2, M, R);
+          join(exchange(sm.again, &sm.again_bar, agains & 1u, M, R, C, rank, ok,
+                        a.ctx_flags, lane), a.c2, M, R);
           ++agains;
         }
         raise_to(a, in.xy, M, R);
@@ -899,35 +1042,28 @@ __global__ void __launch_bounds__(RG_NT, 2)
       const float wt = (float)(a.norm ? share / (double)in.count : share);
       end_math<HOLD, false>(a, row, in, k, R, M, wt, rank == 0, &sm.out[s], sm.stat, lane);
       __syncwarp();
-      if (lane == 0) arrive(&sm.out_bar[s]);
+      if (lane == 0) bar_arrive(&sm.out_bar[s]);
       if (HOLD && rank == 0 && v >= 0) put(g + v, v == in.y ? sm.out[s].gy : grad1(sm.out[s], a.c2, in.edge));
       in = next;
     }
   } else {
     // ---- the rows' words
     uint32_t n = 0, taken = 0;  // rows summed; rows whose result was waited for
-    int32_t r = request(first), y = token(first);
     const int at = warp * 32 + lane;  // this lane's first word of a chunk
-    for (int64_t row = first; row < a.n_rows; row += G) {
-      const int32_t rn = request(row + G), yn = token(row + G);
-      const Share sh = share_of<T>(a, row, C, rank);
-      T* const g = reinterpret_cast<T*>(a.grad) + row * a.grad_stride + sh.head;
+    int4 ref = ref_of(first);
+    for (int64_t i = first; i < live; i += G) {
+      const int4 ref1 = ref_of(i + G);
+      const int32_t y = ref.z;
+      const Share sh = share_of<T>(a, ref.x, C, rank);
+      T* const g = reinterpret_cast<T*>(a.grad) + ref.x * a.grad_stride + sh.head;
       const bool vec = ((reinterpret_cast<uintptr_t>(sh.x + sizeof(T) * sh.head) ^
                          reinterpret_cast<uintptr_t>(g)) & 15u) == 0;
-      if (r < 0) {  // a row that does not count
-        if (HOLD)
-          for (int32_t i = sh.w0 + at; i < sh.w1; i += 32 * RG_NW)
-            put_word(g + (int64_t)i * Tr::VEC, make_uint4(0u, 0u, 0u, 0u), vec);
-        r = rn;
-        y = yn;
-        continue;
-      }
       const int32_t yw = word_of<T>(a, sh, y);
       const int yj = y - sh.head - yw * Tr::VEC;
       // forward
       const int place0 = place;
       const uint32_t turn0 = turn;
-      float k = K_NONE;
+      float k = -3e38f;
       float2 S = make_float2(0.f, 0.f);
       for (int32_t w = sh.w0; w < sh.w1; w += RG_CHUNK) {
         wait(&sm.full[place], turn);
@@ -948,13 +1084,13 @@ __global__ void __launch_bounds__(RG_NT, 2)
         }
         if (!HOLD) {
           __syncwarp();  // every lane has its words
-          if (lane == 0) arrive(&sm.empty[place]);
+          if (lane == 0) bar_arrive(&sm.empty[place]);
         }
         step();
-        add_words<T>(k, S, v, a.c2);
+        add_words<T>(k, S, v, a.c2, w == sh.w0);
       }
       float R;
-      join(make_float2(fmaxf(k, -3e38f), S.x + S.y), 1.f, k, R);
+      join(make_float2(k, S.x + S.y), 1.f, k, R);
       const int s = n % RG_SLOTS;
       if (!HOLD && n >= RG_LAG) {
         wait(&sm.out_bar[taken % RG_SLOTS], (taken / RG_SLOTS) & 1u);
@@ -962,7 +1098,7 @@ __global__ void __launch_bounds__(RG_NT, 2)
       }
       if (lane == 0) {
         sm.part[s][warp] = make_float2(k, R);
-        arrive(&sm.part_bar[s]);
+        bar_arrive(&sm.part_bar[s]);
       }
       if (HOLD) {
         // backward
@@ -987,7 +1123,7 @@ __global__ void __launch_bounds__(RG_NT, 2)
             for (int q = 0; q < RG_W; ++q) v[q] = make_uint4(0u, 0u, 0u, 0u);
           }
           __syncwarp();
-          if (lane == 0) arrive(&sm.empty[place]);
+          if (lane == 0) bar_arrive(&sm.empty[place]);
           step();
           if (vec && w + RG_CHUNK <= sh.w1) {
 #pragma unroll
@@ -1003,13 +1139,24 @@ __global__ void __launch_bounds__(RG_NT, 2)
         }
       }
       ++n;
-      r = rn;
-      y = yn;
+      ref = ref1;
     }
+    if (HOLD)  // the rows that do not count
+      for (int64_t i = first; i < a.n_rows - live; i += G) {
+        const int64_t row = __ldcg(a.skipped + i);
+        const Share sh = share_of<T>(a, row, C, rank);
+        T* const g = reinterpret_cast<T*>(a.grad) + row * a.grad_stride;
+        const bool vec = ((reinterpret_cast<uintptr_t>(sh.x) ^ reinterpret_cast<uintptr_t>(g)) & 15u) == 0;
+        for (int32_t w = sh.w0 + at; w < sh.w1; w += 32 * RG_NW)
+          put_word(g + sh.head + (int64_t)w * Tr::VEC, make_uint4(0u, 0u, 0u, 0u), vec);
+        const int32_t v = end_of(a, sh, lane);
+        if (warp == 0 && rank == 0 && v >= 0) put(g + v, 0.f);
+      }
   }
   __syncthreads();
   if (C > 1) cluster_sync_all();  // no peer writes here any more
-  if (warp == 0 && rank == 0) write_stats(a, sm.stat, first, min(G, a.n_rows), lane);
+  const int64_t groups = max((int64_t)1, min(G, (int64_t)live));
+  if (warp == 0 && rank == 0 && first < groups) write_stats(a, sm.stat, first, groups, lane);
 }
 
 // ---- backward from the rows' states ---------------------------------------------------------
@@ -1044,9 +1191,8 @@ __global__ void __launch_bounds__(BW_NT) loss_backward(const LossArgs a, int32_t
   o.K = o.nk = o.gy = o.M = 0.f;
   int32_t y = -1;
   if (r >= 0) {
-    const float4 q = __ldcg(a.state + 2 * row);
-    const float k = PREF ? __ldcg(a.coef + r) * (a.grad_scale * a.inv_t)
-                         : __ldcg(&a.state[2 * row + 1].x);
+    const float4 q = __ldcg(a.state + row);
+    const float k = PREF ? __ldcg(a.coef + r) * (a.grad_scale * a.inv_t) : __ldcg(a.z + row);
     RowState st;
     st.K = q.x;
     st.adj = q.y;
@@ -1082,68 +1228,83 @@ __device__ __forceinline__ double pair_ratio(const LossArgs& a, int64_t r, int l
   const int64_t lo = a.offsets[r], hi = a.offsets[r + 1];
   double s = 0.;
   if (__ldcg(a.count + r) > 0)
-    for (int64_t t = lo + lane; t < hi; t += 32)
-      if (!a.mask || a.mask[t] != 0) s += (double)__ldcg(&a.state[2 * t + 1].x);
+    for (int64_t t = lo + lane; t < hi; t += 4 * 32) {
+      float z[4];
+      bool on[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        on[q] = t + 32 * q < hi && __ldcg(a.row_req + t + 32 * q) == (int32_t)r;
+        z[q] = t + 32 * q < hi ? __ldcg(a.z + t + 32 * q) : 0.f;
+      }
+#pragma unroll
+      for (int q = 0; q < 4; ++q) s += on[q] ? (double)z[q] : 0.;
+    }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(FULL, s, o);
   return s;
 }
 
-// One warp per pair; the last CTA sums the statistics.
-static __global__ void __launch_bounds__(256) loss_pairs(const LossArgs a) {
+// Two warps per pair, one for each answer; the last CTA sums the statistics.
+constexpr int PR_PAIRS = 4;  // pairs of a CTA
+static __global__ void __launch_bounds__(64 * PR_PAIRS) loss_pairs(const LossArgs a) {
+  __shared__ double ratio[2 * PR_PAIRS];
   __shared__ int last;
   pdl_wait();
   pdl_trigger();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int64_t i = (int64_t)blockIdx.x * 8 + warp, n_pairs = a.n_req / 2;
-  if (i < n_pairs) {
-    double sw = pair_ratio(a, 2 * i, lane), sl = pair_ratio(a, 2 * i + 1, lane);
+  const int64_t n_pairs = a.n_req / 2, i0 = (int64_t)blockIdx.x * PR_PAIRS;
+  {
+    const int64_t r = 2 * i0 + warp;
+    double s = 0.;
+    if (r < a.n_req) s = pair_ratio(a, r, lane);
+    if (lane == 0) ratio[warp] = s;
+  }
+  __syncthreads();
+  const int64_t i = i0 + tid;
+  if (tid < PR_PAIRS && i < n_pairs) {
+    double sw = ratio[2 * tid], sl = ratio[2 * tid + 1];
     const int32_t nw = __ldcg(a.count + 2 * i), nl = __ldcg(a.count + 2 * i + 1);
     if (a.length_norm) {
       sw /= (double)max(nw, 1);
       sl /= (double)max(nl, 1);
     }
-    if (lane == 0) {
-      a.ratio[2 * i] = (float)sw;
-      a.ratio[2 * i + 1] = (float)sl;
-      float t[LS_NSTAT] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-      float cw = 0.f, cl = 0.f;
-      if (nw > 0 && nl > 0) {
-        const double d = sw - sl;
-        const float h = (float)((double)a.beta * d - (double)a.margin);
-        float f, slope;  // loss and d loss / d d
-        if (a.loss == 0) {
-          const float e = log1pf(expf(-fabsf(h)));
-          f = (1.f - a.smooth) * (e + fmaxf(-h, 0.f)) + a.smooth * (e + fmaxf(h, 0.f));
-          slope = a.beta * (a.smooth / (1.f + expf(-h)) - (1.f - a.smooth) / (1.f + expf(h)));
-        } else if (a.loss == 1) {
-          const double q = d - 0.5 / (double)a.beta;
-          f = (float)(q * q);
-          slope = (float)(2. * q);
-        } else {
-          f = fmaxf(1.f - h, 0.f);
-          slope = h < 1.f ? -a.beta : 0.f;
-          if (h != h) f = slope = h;
-        }
-        t[0] = f;
-        t[1] = d > 0. ? 1.f : 0.f;
-        t[2] = h;
-        t[3] = (float)((double)a.beta * sw);
-        t[4] = (float)((double)a.beta * sl);
-        const double share = (double)slope / (double)__ldcg(a.totals + 1);
-        cw = (float)(a.length_norm ? share / (double)nw : share);
-        cl = (float)(a.length_norm ? -share / (double)nl : -share);
+    a.ratio[2 * i] = (float)sw;
+    a.ratio[2 * i + 1] = (float)sl;
+    float t[LS_NSTAT] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    float cw = 0.f, cl = 0.f;
+    if (nw > 0 && nl > 0) {
+      const double d = sw - sl;
+      const float h = (float)((double)a.beta * d - (double)a.margin);
+      float f, slope;  // loss and d loss / d d
+      if (a.loss == 0) {
+        const float e = log1pf(expf(-fabsf(h)));
+        f = (1.f - a.smooth) * (e + fmaxf(-h, 0.f)) + a.smooth * (e + fmaxf(h, 0.f));
+        slope = a.beta * (a.smooth / (1.f + expf(-h)) - (1.f - a.smooth) / (1.f + expf(h)));
+      } else if (a.loss == 1) {
+        const double q = d - 0.5 / (double)a.beta;
+        f = (float)(q * q);
+        slope = (float)(2. * q);
+      } else {
+        f = fmaxf(1.f - h, 0.f);
+        slope = h < 1.f ? -a.beta : 0.f;
+        if (h != h) f = slope = h;
       }
-      a.coef[2 * i] = cw;
-      a.coef[2 * i + 1] = cl;
-      for (int j = 0; j < LS_NSTAT; ++j) a.term[i * LS_NSTAT + j] = t[j];
+      t[0] = f;
+      t[1] = d > 0. ? 1.f : 0.f;
+      t[2] = h;
+      t[3] = (float)((double)a.beta * sw);
+      t[4] = (float)((double)a.beta * sl);
+      const float share = slope / (float)__ldcg(a.totals + 1);
+      cw = a.length_norm ? share / (float)nw : share;
+      cl = a.length_norm ? -share / (float)nl : -share;
     }
+    a.coef[2 * i] = cw;
+    a.coef[2 * i + 1] = cl;
+    for (int j = 0; j < LS_NSTAT; ++j) a.term[i * LS_NSTAT + j] = t[j];
+    __threadfence();
   }
   __syncthreads();
-  if (tid == 0) {
-    __threadfence();
-    last = atom_add_acq_rel(a.ticket + 1, 1) == (int)gridDim.x - 1;
-  }
+  if (tid == 0) last = atom_add_acq_rel(a.ticket + 1, 1) == (int)gridDim.x - 1;
   __syncthreads();
   if (!last || warp >= LS_NSTAT - 1) return;
   double v = 0.;

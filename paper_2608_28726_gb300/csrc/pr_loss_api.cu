@@ -39,16 +39,26 @@ pr_status check_loss(pr_dtype dt, const void* logits, int64_t n_rows, int64_t vo
   return PR_OK;
 }
 
+int64_t forward_grid(const pr_ctx* c) { return (int64_t)c->num_sms * prk::FW_CTAS; }
+
 // the workspace: [tickets, totals][per request][per pair][per row][per group]
 pr_status workspace(pr_ctx* c, prk::LossArgs& a, int64_t groups, bool pref, bool state) {
   const size_t n_req = (size_t)a.n_req, n_rows = (size_t)a.n_rows;
-  const size_t at_count = 64, at_coef = at_count + up16(n_req * 4),
+  // (what has to be zero between calls comes first, at places that do not move: the
+  // arrivals of rows by the largest batch so far)
+  const size_t rows = n_rows <= c->loss_rows ? c->loss_rows : n_rows + n_rows / 4;
+  const size_t at_piece = 64 + up16(rows * 4), at_count = at_piece + (size_t)forward_grid(c) * 16,
+               at_coef = at_count + up16(n_req * 4),
                at_term = at_coef + up16(pref ? n_req * 4 : 0),
                at_req = at_term + up16(pref ? n_req / 2 * prk::LS_NSTAT * 4 : 0),
-               at_state = at_req + up16(n_rows * 4),
-               at_part = at_state + (state ? n_rows * 32 : 0),
+               at_block = at_req + up16(n_rows * 4),
+               at_list = at_block + up16((n_rows / prk::PL_BLOCK + 1) * 4),
+               at_skipped = at_list + n_rows * 16,
+               at_state = at_skipped + up16(n_rows * 4),
+               at_z = at_state + (state ? n_rows * 16 : 0),
+               at_part = at_z + up16(state ? n_rows * 4 : 0),
                bytes = at_part + (pref ? 0 : (size_t)groups * prk::LS_NSTAT * 8);
-  if (bytes > c->loss_ws_bytes) {
+  if (bytes > c->loss_ws_bytes || rows > c->loss_rows) {
     PR_CUDA(cudaDeviceSynchronize());  // kernels may still use the old one
     cudaFree(c->loss_ws);
     c->loss_ws = nullptr;
@@ -62,21 +72,29 @@ pr_status workspace(pr_ctx* c, prk::LossArgs& a, int64_t groups, bool pref, bool
     PR_CUDA(cudaMemset(c->loss_ws, 0, room));
     PR_CUDA(cudaDeviceSynchronize());
     c->loss_ws_bytes = room;
+    c->loss_rows = rows;
   }
   char* w = static_cast<char*>(c->loss_ws);
   a.ticket = reinterpret_cast<int32_t*>(w);
   a.totals = reinterpret_cast<int64_t*>(w + 16);
+  a.arrived = reinterpret_cast<int32_t*>(w + 64);
+  a.piece = reinterpret_cast<float2*>(w + at_piece);
   a.count = reinterpret_cast<int32_t*>(w + at_count);
   a.coef = reinterpret_cast<float*>(w + at_coef);
   a.term = reinterpret_cast<float*>(w + at_term);
   a.row_req = reinterpret_cast<int32_t*>(w + at_req);
+  a.block = reinterpret_cast<int32_t*>(w + at_block);
+  a.list = reinterpret_cast<int4*>(w + at_list);
+  a.skipped = reinterpret_cast<int32_t*>(w + at_skipped);
   a.state = state ? reinterpret_cast<float4*>(w + at_state) : nullptr;
+  a.z = state ? reinterpret_cast<float*>(w + at_z) : nullptr;
   a.part = reinterpret_cast<double*>(w + at_part);
   return PR_OK;
 }
 
+// early: set up while the kernel before it still runs
 pr_status launch(const void* kern, unsigned grid, unsigned threads, size_t smem, unsigned cluster,
-                 void** args, cudaStream_t s) {
+                 void** args, cudaStream_t s, bool early = true) {
   cudaLaunchConfig_t cfg;
   memset(&cfg, 0, sizeof cfg);
   cfg.gridDim = dim3(grid);
@@ -85,8 +103,10 @@ pr_status launch(const void* kern, unsigned grid, unsigned threads, size_t smem,
   cfg.stream = s;
   cudaLaunchAttribute attr[2];
   int n = 0;
-  attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[n++].val.programmaticStreamSerializationAllowed = 1;
+  if (early) {
+    attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[n++].val.programmaticStreamSerializationAllowed = 1;
+  }
   if (cluster > 1) {
     attr[n].id = cudaLaunchAttributeClusterDimension;
     attr[n].val.clusterDim.x = cluster;
@@ -108,15 +128,10 @@ const void* ring_kernel(pr_dtype dt, bool hold) {
               : reinterpret_cast<const void*>(&prk::loss_ring<float, false>);
 }
 
-constexpr int FW_NT = 512, FW_SMALL = 128;  // threads of a row's CTA
-
 template <typename T>
-const void* forward_kernel(bool small, bool pref) {
-  if (small)
-    return pref ? reinterpret_cast<const void*>(&prk::loss_forward<T, FW_SMALL, true>)
-                : reinterpret_cast<const void*>(&prk::loss_forward<T, FW_SMALL, false>);
-  return pref ? reinterpret_cast<const void*>(&prk::loss_forward<T, FW_NT, true>)
-              : reinterpret_cast<const void*>(&prk::loss_forward<T, FW_NT, false>);
+const void* forward_kernel(bool pref) {
+  return pref ? reinterpret_cast<const void*>(&prk::loss_forward<T, true>)
+              : reinterpret_cast<const void*>(&prk::loss_forward<T, false>);
 }
 
 // shared memory opt-ins, and the clusters of 2, 4 and 8 CTAs that the GPU has room for
@@ -157,57 +172,51 @@ pr_status ring_setup(pr_ctx* c) {
 struct RingShape {
   int split, places;
   bool hold;        // a row's chunks fit the cluster's rings
+  bool full;        // every place is taken
   int64_t groups;   // rows in work at a time
 };
 
-// The narrowest split whose CTAs hold a row in half an SM's shared memory, with two
-// places left for the next row's chunks; with all of an SM's where eight CTAs' halves do
-// not; wider ones while all rows have a place at once.  The same with and without a
-// gradient, so that the losses' bits are.
+// Splits whose CTAs hold a row in half an SM's shared memory, with two places left for the
+// next row's chunks; all of an SM's where eight CTAs' halves do not.  Of those the one that
+// takes the fewest steps: the rows of each cluster, one after the other, each as many steps
+// as its CTAs have chunks and two for its end.  The same with and without a gradient, so
+// that the losses' bits are.
 RingShape choose_ring(const pr_ctx* c, pr_dtype dt, int64_t n_rows, int64_t vocab) {
   const int64_t words = vocab * (int64_t)esize(dt) / 16;
   const int64_t chunks = (words + prk::RG_CHUNK - 1) / prk::RG_CHUNK;
   auto per_cta = [&](int split) { return (chunks + (1 << split) - 1) >> split; };
-  int split = 0;
-  while (split < 3 && per_cta(split) > prk::RG_FEW - 2) ++split;
-  const bool whole = per_cta(split) > prk::RG_FEW - 2;
-  while (split < 3 && n_rows <= c->loss_places[whole][split + 1] && per_cta(split) > 1) ++split;
+  const bool whole = per_cta(3) > prk::RG_FEW - 2;
+  auto steps = [&](int split) {
+    const int64_t places = c->loss_places[whole][split];
+    return (n_rows + places - 1) / places * (per_cta(split) + 2);
+  };
+  int split = 3;
+  for (int i = 2; i >= 0; --i)
+    if (per_cta(i) <= (whole ? prk::RG_MOST : prk::RG_FEW) - 2 && steps(i) <= steps(split)) split = i;
   RingShape s;
   s.split = split;
   s.places = whole ? prk::RG_MOST : prk::RG_FEW;
   s.hold = per_cta(split) <= s.places;
   s.groups = std::min<int64_t>(n_rows, c->loss_places[whole][split]);
+  s.full = n_rows >= c->loss_places[whole][split];
   return s;
 }
 
-// The forward kernel's launch: 512 threads per row, 128 where those have less than a
-// load each; clusters where all rows have a place at once all the same.
-struct ForwardShape {
-  bool small;
-  int split;
-  int64_t groups;
-};
-
-ForwardShape choose_forward(const pr_ctx* c, pr_dtype dt, int64_t n_rows, int64_t vocab) {
-  const int64_t words = vocab * (int64_t)esize(dt) / 16;
-  ForwardShape s;
-  s.small = words <= 4 * FW_SMALL;
-  s.split = 0;
-  const int64_t places = (int64_t)c->num_sms * (1024 / (s.small ? FW_SMALL : FW_NT));
-  // (a cluster's CTAs lie in one GPC: eight of them do not fill every SM)
-  while (!s.small && s.split < 3 && n_rows << (s.split + 1) <= places * 3 / 4 &&
-         words >> s.split > 4 * FW_NT)
-    ++s.split;
-  s.groups = std::min(n_rows, places >> s.split);
-  return s;
-}
-
+// One CTA where it takes no longer than the second launch (about 3 us) that many need.
 pr_status launch_plan(pr_ctx* c, prk::LossArgs& a, int pairs, cudaStream_t s) {
-  const int64_t grid = a.n_req + (a.n_rows + 255) / 256;
-  if (grid > 0x7fffffffLL) return PR_ERR_INVALID_ARG;
   void* args[] = {&a, &pairs};
-  const pr_status st = launch(reinterpret_cast<const void*>(&prk::loss_plan), (unsigned)grid, 256,
-                              0, 1, args, s);
+  if (a.n_rows <= 4 * prk::PL_BLOCK && a.n_req <= prk::PL_FEW) {
+    const pr_status st = launch(reinterpret_cast<const void*>(&prk::loss_plan), 1, prk::PL_BLOCK, 0,
+                                1, args, s);
+    return st == PR_OK ? timing_mark(c, s) : st;
+  }
+  const int64_t blocks = (a.n_rows + prk::PL_BLOCK - 1) / prk::PL_BLOCK, grid = a.n_req + blocks;
+  if (grid > 0x7fffffffLL) return PR_ERR_INVALID_ARG;
+  pr_status st = launch(reinterpret_cast<const void*>(&prk::loss_count), (unsigned)grid,
+                        prk::PL_BLOCK, 0, 1, args, s);
+  if (st != PR_OK || (st = timing_mark(c, s)) != PR_OK || blocks == 0) return st;
+  st = launch(reinterpret_cast<const void*>(&prk::loss_list), (unsigned)blocks, prk::PL_BLOCK, 0, 1,
+              args, s);
   return st == PR_OK ? timing_mark(c, s) : st;
 }
 
@@ -215,19 +224,20 @@ pr_status launch_ring(pr_ctx* c, prk::LossArgs& a, pr_dtype dt, const RingShape&
                       cudaStream_t s) {
   int places = shape.places;
   void* args[] = {&a, &places};
+  // A grid that takes every place is not set up early: clusters placed around the CTAs
+  // of the launch before do not all find one, and the last run alone (8,847 rows of V =
+  // 151,936 bf16 back to back: 1,538 us, 890 set up after it).
   const pr_status st = launch(ring_kernel(dt, hold), (unsigned)(shape.groups << shape.split),
-                              prk::RG_NT, prk::ring_bytes(places), 1u << shape.split, args, s);
+                              prk::RG_NT, prk::ring_bytes(places), 1u << shape.split, args, s,
+                              !shape.full);
   return st == PR_OK ? timing_mark(c, s) : st;
 }
 
-pr_status launch_forward(pr_ctx* c, prk::LossArgs& a, pr_dtype dt, const ForwardShape& shape,
-                         bool pref, cudaStream_t s) {
+pr_status launch_forward(pr_ctx* c, prk::LossArgs& a, pr_dtype dt, bool pref, cudaStream_t s) {
   void* args[] = {&a};
-  const pr_status st =
-      launch(dt == PR_DTYPE_BF16 ? forward_kernel<__nv_bfloat16>(shape.small, pref)
-                                 : forward_kernel<float>(shape.small, pref),
-             (unsigned)(shape.groups << shape.split), shape.small ? FW_SMALL : FW_NT, 0,
-             1u << shape.split, args, s);
+  const pr_status st = launch(dt == PR_DTYPE_BF16 ? forward_kernel<__nv_bfloat16>(pref)
+                                                  : forward_kernel<float>(pref),
+                              (unsigned)forward_grid(c), prk::FW_NT, 0, 1, args, s);
   return st == PR_OK ? timing_mark(c, s) : st;
 }
 
@@ -308,14 +318,13 @@ pr_status pr_policy_loss(pr_ctx* c, const void* logits, pr_dtype dt, int64_t n_r
   a.kl_coef = p->kl_coef;
   if ((st = ring_setup(c)) != PR_OK) return st;
   const RingShape ring = choose_ring(c, dt, n_rows, vocab);
-  const ForwardShape forward = choose_forward(c, dt, n_rows, vocab);
-  if ((st = workspace(c, a, std::max(ring.groups, forward.groups), false, !ring.hold)) != PR_OK)
+  if ((st = workspace(c, a, std::max(ring.groups, forward_grid(c)), false, !ring.hold)) != PR_OK)
     return st;
   if ((st = timing_begin(c, s)) != PR_OK) return st;
   if ((st = launch_plan(c, a, 0, s)) != PR_OK) return st;
   if (ring.hold) return launch_ring(c, a, dt, ring, grad != nullptr, s);
   // rows of more than eight SMs' shared memory
-  if ((st = launch_forward(c, a, dt, forward, false, s)) != PR_OK) return st;
+  if ((st = launch_forward(c, a, dt, false, s)) != PR_OK) return st;
   return grad ? launch_backward(c, a, dt, false, s) : PR_OK;
 }
 
@@ -351,12 +360,12 @@ pr_status pr_preference_loss(pr_ctx* c, const void* logits, pr_dtype dt, int64_t
   if ((st = workspace(c, a, 0, true, true)) != PR_OK) return st;
   if ((st = timing_begin(c, s)) != PR_OK) return st;
   if ((st = launch_plan(c, a, 1, s)) != PR_OK) return st;
-  if (n_rows > 0 && (st = launch_forward(c, a, dt, choose_forward(c, dt, n_rows, vocab), true, s)) !=
-                        PR_OK)
+  if (n_rows > 0 && (st = launch_forward(c, a, dt, true, s)) != PR_OK)
     return st;
   void* args[] = {&a};
-  if ((st = launch(reinterpret_cast<const void*>(&prk::loss_pairs), (unsigned)((n_req / 2 + 7) / 8),
-                   256, 0, 1, args, s)) != PR_OK ||
+  if ((st = launch(reinterpret_cast<const void*>(&prk::loss_pairs), 
+                   (unsigned)((n_req / 2 + prk::PR_PAIRS - 1) / prk::PR_PAIRS), 64 * prk::PR_PAIRS, 0, 1,
+                   args, s)) != PR_OK ||
       (st = timing_mark(c, s)) != PR_OK)
     return st;
   return grad && n_rows > 0 ? launch_backward(c, a, dt, true, s) : PR_OK;
