@@ -429,6 +429,28 @@ struct RowWords {
   }
 };
 
+// ---- barriers in shared memory --------------------------------------------------------------
+
+__device__ __forceinline__ bool ring_wait(uint32_t bar, uint32_t parity, uint32_t* flags) {
+  // (the clock of ring_wait_slow is read only after some thousand tests)
+  for (int i = 0; i < 4096; ++i)
+    if (ring_test(bar, parity)) return true;
+  return ring_wait_slow(bar, parity, flags);
+}
+__device__ __forceinline__ uint32_t sm_addr(const void* p) {
+  return (uint32_t)__cvta_generic_to_shared(p);
+}
+__device__ __forceinline__ void bar_init(uint64_t* b, int n) {
+  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(sm_addr(b)), "r"(n) : "memory");
+}
+__device__ __forceinline__ void bar_arrive(uint64_t* b) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(sm_addr(b)) : "memory");
+}
+__device__ __forceinline__ void bar_expect(uint64_t* b, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(sm_addr(b)), "r"(bytes)
+               : "memory");
+}
+
 // ---- a row among CTAs -------------------------------------------------------------------
 
 // a CTA's part of a row
@@ -512,12 +534,13 @@ __device__ __noinline__ void robust_sum(const LossArgs& a, const Share s, bool e
 constexpr int RG_TERMS = 5;  // statistics that are summed row by row
 
 // A row's end from its sums: R against 2^k, or against its maximum M where that is not
-// infinite.  Writes logp, the statistics' terms (weight wt), and the result: to `out`
-// with HOLD, else the row's state.  Whole warp; apart from the kernel's registers.
-template <bool HOLD, bool PREF>
+// infinite.  Writes logp, the statistics' terms (weight wt), and the result: to `out`,
+// whose barrier learns of it first, else the row's state.  Whole warp; apart from the
+// kernel's registers.
+template <bool PREF>
 __device__ __noinline__ void end_math(const LossArgs& a, int64_t row, const RowIn in, float k,
                                       float R, float M, float wt, bool writes, RowOut* out,
-                                      float2* stat, int lane) {
+                                      uint64_t* out_bar, float2* stat, int lane) {
   float u, u_lo = 0.f;
   bool far = false;
   if (M == INFINITY) {
@@ -545,33 +568,30 @@ __device__ __noinline__ void end_math(const LossArgs& a, int64_t row, const RowI
   st.adj = exp2f(-(((c - st.K) + e.f) + (b_lo + c_lo)));
   st.rest = e.rest;
   st.M = M;
-  RowOut o;
-  o.mode = ROW_ZERO;
-  o.K = o.nk = o.gy = 0.f;
-  o.M = M;
   float kk = 0.f;
+  PolicyTerms p;
   if (!PREF) {
-    const PolicyTerms p = policy_terms(a, l, e.l_lo, in.old, in.ref, in.adv);
+    p = policy_terms(a, l, e.l_lo, in.old, in.ref, in.adv);
     kk = wt * p.slope * (a.grad_scale * a.inv_t);
-    if (lane < RG_TERMS) {
-      const float x = wt * (lane == 0 ? p.surrogate : lane == 1 ? p.kl : lane == 2 ? p.ratio
-                                                  : lane == 3 ? p.clipped : p.old_kl);
-      const float2 q = stat[lane];
-      const float y = q.x + x, z = y - q.x;
-      stat[lane] = make_float2(y, q.y + ((q.x - (y - z)) + (x - z)));
-    }
-    if (HOLD) o = row_out(st, kk);
   }
-  if (lane == 0) {
-    *out = o;
-    if (writes) {
-      a.logp[row] = l;
-      if (in.y < 0 || (int64_t)in.y >= a.vocab) atomicOr(a.ctx_flags, FLAG_BAD_CHOSEN);
-      else if (isnan(l)) atomicOr(a.ctx_flags, FLAG_NONFINITE);
-      if (!HOLD && a.state) {
-        a.state[row] = make_float4(st.K, st.adj, st.rest, st.M);
-        a.z[row] = PREF ? (l - in.ref) + e.l_lo : kk;
-      }
+  if (out && lane == 0) {
+    *out = row_out(st, kk);
+    bar_arrive(out_bar);
+  }
+  if (!PREF && lane < RG_TERMS) {
+    const float x = wt * (lane == 0 ? p.surrogate : lane == 1 ? p.kl : lane == 2 ? p.ratio
+                                                : lane == 3 ? p.clipped : p.old_kl);
+    const float2 q = stat[lane];
+    const float y = q.x + x, z = y - q.x;
+    stat[lane] = make_float2(y, q.y + ((q.x - (y - z)) + (x - z)));
+  }
+  if (lane == 0 && writes) {
+    a.logp[row] = l;
+    if (in.y < 0 || (int64_t)in.y >= a.vocab) atomicOr(a.ctx_flags, FLAG_BAD_CHOSEN);
+    else if (isnan(l)) atomicOr(a.ctx_flags, FLAG_NONFINITE);
+    if (a.state) {
+      a.state[row] = make_float4(st.K, st.adj, st.rest, st.M);
+      a.z[row] = PREF ? (l - in.ref) + e.l_lo : kk;
     }
   }
 }
@@ -691,46 +711,6 @@ __device__ __forceinline__ void write_stats(const LossArgs& a, const float2* sta
   }
 }
 
-// every CTA's (k, R) of a cluster, by lane: written into the peers' `to`, whose barrier
-// counts the bytes.  Whole warp; false when the wait has run out.
-__device__ __forceinline__ bool ring_wait(uint32_t bar, uint32_t parity, uint32_t* flags) {
-  // (the clock of ring_wait_slow is read only after some thousand tests)
-  for (int i = 0; i < 4096; ++i)
-    if (ring_test(bar, parity)) return true;
-  return ring_wait_slow(bar, parity, flags);
-}
-__device__ __forceinline__ uint32_t sm_addr(const void* p) {
-  return (uint32_t)__cvta_generic_to_shared(p);
-}
-__device__ __forceinline__ void bar_init(uint64_t* b, int n) {
-  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(sm_addr(b)), "r"(n) : "memory");
-}
-__device__ __forceinline__ void bar_arrive(uint64_t* b) {
-  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(sm_addr(b)) : "memory");
-}
-__device__ __forceinline__ void bar_expect(uint64_t* b, uint32_t bytes) {
-  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(sm_addr(b)), "r"(bytes)
-               : "memory");
-}
-__device__ __forceinline__ float2 exchange(float2* to, uint64_t* bar, uint32_t phase, float k,
-                                           float R, uint32_t C, uint32_t rank, bool& ok,
-                                           uint32_t* flags, int lane) {
-  if (lane < (int)C)
-    asm volatile(
-        "st.async.shared::cluster.mbarrier::complete_tx::bytes.b64 [%0], %1, [%2];" ::"r"(
-            dsmem_addr(to + rank, (uint32_t)lane)),
-        "l"((uint64_t)__float_as_uint(k) | (uint64_t)__float_as_uint(R) << 32),
-        "r"(dsmem_addr(bar, (uint32_t)lane))
-        : "memory");
-  __syncwarp();
-  if (ok) ok = ring_wait(sm_addr(bar), phase, flags);
-  __syncwarp();
-  const float2 p = lane < (int)C ? to[lane] : make_float2(LS_MIN, 0.f);
-  __syncwarp();
-  if (lane == 0) bar_expect(bar, 8 * C);
-  return p;
-}
-
 // ---- forward alone ----------------------------------------------------------------------
 //
 // The rows' tiles of 16 KB, one row after the other, are dealt out in equal runs: a CTA
@@ -749,7 +729,6 @@ constexpr int FW_CTAS = 4;                  // on an SM
 struct ForwardSmem {
   float2 part[2][FW_NW];
   float2 stat[RG_TERMS];
-  RowOut out;
 };
 // the run of CTA b: tiles [run_begin(b), run_begin(b + 1)); the CTA of tile t
 __device__ __forceinline__ int64_t run_begin(int64_t b, int64_t tiles, int64_t G) {
@@ -832,7 +811,7 @@ __global__ void __launch_bounds__(FW_NT, FW_CTAS) loss_forward(const __grid_cons
         raise_to(a, in.xy, M, R);
       }
       const float wt = PREF ? 0.f : (float)(a.norm ? share / (double)in.count : share);
-      end_math<false, PREF>(a, row, in, k, R, M, wt, true, &sm.out, sm.stat, lane);
+      end_math<PREF>(a, row, in, k, R, M, wt, true, nullptr, nullptr, sm.stat, lane);
       in = next;
     }
   } else {
@@ -905,47 +884,76 @@ constexpr int RG_W = 4;                        // words per lane and chunk
 constexpr int RG_CHUNK = 32 * RG_NW * RG_W;    // words of a chunk
 constexpr int RG_BYTES = 16 * RG_CHUNK;
 constexpr int RG_MOST = 14, RG_FEW = 7;        // places of the ring: one or two CTAs on an SM
-// A warp writes row n's sum after it has waited for row n - LAG's result, and with it all
-// earlier ones.  That result took row n - LAG's sums of all CTAs, whose writers had waited
-// for row n - 2 LAG's in their own CTA: with 2 LAG slots nobody still reads what is written.
-constexpr int RG_SLOTS = 4, RG_LAG = 2;
+// A warp sends row n + 2's sum after it has waited for row n + 1's result.  That took row
+// n + 1's sums of all CTAs, whose senders had waited for row n's result in their own CTA, and
+// that one's sums have been read by then: two slots.
+constexpr int RG_SLOTS = 2;
 struct RingCtl {
   uint64_t full[RG_MOST], empty[RG_MOST];      // a chunk has landed; has been read
-  float2 part[RG_SLOTS][RG_NW];                // the warps' (k, R)
-  float2 cta[RG_SLOTS][MAXC];                  // the CTAs' (k, R), written by their peers
-  uint64_t part_bar[RG_SLOTS];                 // the warps' sums are there
-  uint64_t cta_bar[RG_SLOTS];                  // the cluster's sums are there
+  uint64_t sum_bar[RG_SLOTS];                  // the warps' sums are there
   uint64_t out_bar[RG_SLOTS];                  // a row's result is there
-  float2 again[MAXC];                          // the sums of a row summed once more
+  float2 again[MAXC];                          // the CTAs' sums of a row summed once more
   uint64_t again_bar;
   float2 stat[RG_TERMS];                       // sums over the rows
   RowOut out[RG_SLOTS];                        // a row's result
 };
-static_assert(sizeof(RingCtl) <= 1024 && SH_CHUNK == RG_CHUNK, "two CTAs on an SM");
-constexpr size_t ring_bytes(int places) { return 1024 + (size_t)places * RG_BYTES; }
+// then the (k, R) of all warps of the cluster, [RG_SLOTS][C][RG_NW]; then the ring
+constexpr size_t RING_SUMS = (sizeof(RingCtl) + 15) / 16 * 16;
+__host__ __device__ constexpr size_t ring_start(int C) {
+  return RING_SUMS + (size_t)RG_SLOTS * C * RG_NW * sizeof(float2);
+}
+static_assert(ring_start(4) <= 1024 && SH_CHUNK == RG_CHUNK, "two CTAs of a cluster of 4 on an SM");
+constexpr int BAR_IN = 5;  // the first row's scalars are there
+
+// (k, R) to the same place of each of a cluster's CTAs; its barrier there counts the bytes
+__device__ __forceinline__ void send(float2* to, uint64_t* bar, float k, float R, uint32_t C,
+                                     int lane) {
+  if (lane < (int)C)
+    asm volatile(
+        "st.async.shared::cluster.mbarrier::complete_tx::bytes.b64 [%0], %1, [%2];" ::"r"(
+            dsmem_addr(to, (uint32_t)lane)),
+        "l"((uint64_t)__float_as_uint(k) | (uint64_t)__float_as_uint(R) << 32),
+        "r"(dsmem_addr(bar, (uint32_t)lane))
+        : "memory");
+}
+// every CTA's (k, R) of a cluster, by lane: written into the peers' `to`, whose barrier
+// counts the bytes.  Whole warp; ok turns false when the wait runs out.
+__device__ __forceinline__ float2 exchange(float2* to, uint64_t* bar, uint32_t phase, float k,
+                                           float R, uint32_t C, uint32_t rank, bool& ok,
+                                           uint32_t* flags, int lane) {
+  send(to + rank, bar, k, R, C, lane);
+  __syncwarp();
+  if (ok) ok = ring_wait(sm_addr(bar), phase, flags);
+  __syncwarp();
+  const float2 p = lane < (int)C ? to[lane] : make_float2(LS_MIN, 0.f);
+  __syncwarp();
+  if (lane == 0) bar_expect(bar, 8 * C);
+  return p;
+}
+
 
 template <typename T, bool HOLD>
 __global__ void __launch_bounds__(RG_NT, 2)
     loss_ring(const __grid_constant__ LossArgs a, const int places) {
   extern __shared__ __align__(16) unsigned char smem_raw[];
   RingCtl& sm = *reinterpret_cast<RingCtl*>(smem_raw);
-  unsigned char* const ring = smem_raw + 1024;
   using Tr = Traits<T>;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   uint32_t C, rank;
   asm("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(C));
   asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
   const int64_t G = gridDim.x / C, first = blockIdx.x / C;
+  float2* const sums = reinterpret_cast<float2*>(smem_raw + RING_SUMS);
+  unsigned char* const ring = smem_raw + ring_start((int)C);
   if (threadIdx.x == 0) {
     for (int i = 0; i < places; ++i) {
       bar_init(&sm.full[i], 1);
       bar_init(&sm.empty[i], RG_NW);
     }
     for (int s = 0; s < RG_SLOTS; ++s) {
-      bar_init(&sm.part_bar[s], RG_NW);
+      bar_init(&sm.sum_bar[s], C > 1 ? 1 : RG_NW);
       bar_init(&sm.out_bar[s], 1);
-      bar_init(&sm.cta_bar[s], 1);
-      if (C > 1) bar_expect(&sm.cta_bar[s], 8 * C);
+      if (C > 1) bar_expect(&sm.sum_bar[s], 8 * RG_NW * C);
     }
     bar_init(&sm.again_bar, 1);
     if (C > 1) bar_expect(&sm.again_bar, 8 * C);
@@ -1011,8 +1019,16 @@ __global__ void __launch_bounds__(RG_NT, 2)
     uint32_t n = 0, agains = 0;
     int4 ref = ref_of(first), ref1 = ref_of(first + G);
     RowIn in = fetch_row<T, false>(a, share_of<T>(a, ref.x, C, rank), ref, lane);
+    // What a peer's gradient may be written over (the logits' own buffer) has been read when
+    // this CTA's sums are sent: the next row's scalars are there before a result is given.
+    auto landed = [&](RowIn& q) {
+      q.xy = __shfl_sync(FULL, q.xy, lane);
+      q.edge = __shfl_sync(FULL, q.edge, lane);
+    };
+    landed(in);
+    if (C > 1) named_bar_arrive(BAR_IN, 32 * (RG_NW + 1));
     for (int64_t i = first; i < live; i += G) {
-      const RowIn next = fetch_row<T, false>(a, share_of<T>(a, ref1.x, C, rank), ref1, lane);
+      RowIn next = fetch_row<T, false>(a, share_of<T>(a, ref1.x, C, rank), ref1, lane);
       const int64_t row = ref.x;
       const Share sh = share_of<T>(a, row, C, rank);
       ref = ref1;
@@ -1022,14 +1038,22 @@ __global__ void __launch_bounds__(RG_NT, 2)
       const int s = n % RG_SLOTS;
       const uint32_t phase = (n / RG_SLOTS) & 1u;
       ++n;
-      wait(&sm.part_bar[s], phase);
+      wait(&sm.sum_bar[s], phase);
       float k, R, M = INFINITY;
-      join(lane < RG_NW ? sm.part[s][lane] : make_float2(-3e38f, 0.f), 1.f, k, R);
-      if (rank == 0) add_ends(a, sh, in, k, R, lane);
-      // (a peer that has this CTA's sum may write its part of the gradient, over the
-      // logits: what is read of that part has to be here)
-      in.xy = __shfl_sync(FULL, in.xy, 0);
-      if (C > 1) join(exchange(sm.cta[s], &sm.cta_bar[s], phase, k, R, C, rank, ok, a.ctx_flags, lane), 1.f, k, R);
+      {
+        const float2* q = sums + s * RG_NW * C;
+        const float2 none = make_float2(-3e38f, 0.f);
+        float2 p = lane < (int)(RG_NW * C) ? q[lane] : none;
+        if (C > 4) {
+          const float2 p2 = q[32 + lane];
+          const float top = fmaxf(p.x, p2.x);
+          p = make_float2(top, p.y * rescale2(p.x - top) + p2.y * rescale2(p2.x - top));
+        }
+        __syncwarp();
+        if (C > 1 && lane == 0) bar_expect(&sm.sum_bar[s], 8 * RG_NW * C);
+        join(p, 1.f, k, R);
+      }
+      add_ends(a, sh, in, k, R, lane);
       if (sum_again(k, R, in.xy, a.c2)) {
         robust_sum<T>(a, sh, rank == 0, in.y, M, R, lane);
         if (C > 1) {
@@ -1040,15 +1064,16 @@ __global__ void __launch_bounds__(RG_NT, 2)
         raise_to(a, in.xy, M, R);
       }
       const float wt = (float)(a.norm ? share / (double)in.count : share);
-      end_math<HOLD, false>(a, row, in, k, R, M, wt, rank == 0, &sm.out[s], sm.stat, lane);
+      landed(next);
+      end_math<false>(a, row, in, k, R, M, wt, rank == 0, &sm.out[s], &sm.out_bar[s], sm.stat, lane);
       __syncwarp();
-      if (lane == 0) bar_arrive(&sm.out_bar[s]);
       if (HOLD && rank == 0 && v >= 0) put(g + v, v == in.y ? sm.out[s].gy : grad1(sm.out[s], a.c2, in.edge));
       in = next;
     }
   } else {
     // ---- the rows' words
-    uint32_t n = 0, taken = 0;  // rows summed; rows whose result was waited for
+    uint32_t n = 0;  // rows
+    if (C > 1) named_bar_sync(BAR_IN, 32 * (RG_NW + 1));
     const int at = warp * 32 + lane;  // this lane's first word of a chunk
     int4 ref = ref_of(first);
     for (int64_t i = first; i < live; i += G) {
@@ -1092,13 +1117,12 @@ __global__ void __launch_bounds__(RG_NT, 2)
       float R;
       join(make_float2(k, S.x + S.y), 1.f, k, R);
       const int s = n % RG_SLOTS;
-      if (!HOLD && n >= RG_LAG) {
-        wait(&sm.out_bar[taken % RG_SLOTS], (taken / RG_SLOTS) & 1u);
-        ++taken;
-      }
-      if (lane == 0) {
-        sm.part[s][warp] = make_float2(k, R);
-        bar_arrive(&sm.part_bar[s]);
+      if (!HOLD && n >= 1) wait(&sm.out_bar[s ^ 1], ((n - 1) / RG_SLOTS) & 1u);
+      if (C > 1) {
+        send(sums + (s * C + rank) * RG_NW + warp, &sm.sum_bar[s], k, R, C, lane);
+      } else if (lane == 0) {
+        sums[s * RG_NW + warp] = make_float2(k, R);
+        bar_arrive(&sm.sum_bar[s]);
       }
       if (HOLD) {
         // backward

@@ -120,6 +120,10 @@ pr_status launch(const void* kern, unsigned grid, unsigned threads, size_t smem,
   return PR_OK;
 }
 
+size_t ring_bytes(int places, int cluster) {
+  return prk::ring_start(cluster) + (size_t)places * prk::RG_BYTES;
+}
+
 const void* ring_kernel(pr_dtype dt, bool hold) {
   if (dt == PR_DTYPE_BF16)
     return hold ? reinterpret_cast<const void*>(&prk::loss_ring<__nv_bfloat16, true>)
@@ -141,7 +145,7 @@ pr_status ring_setup(pr_ctx* c) {
   for (pr_dtype dt : {PR_DTYPE_F32, PR_DTYPE_BF16})
     for (bool hold : {false, true})
       PR_CUDA(cudaFuncSetAttribute(ring_kernel(dt, hold), cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                   (int)prk::ring_bytes(prk::RG_MOST)));
+                                   (int)ring_bytes(prk::RG_MOST, 8)));
   for (int i = 0; i < 4; ++i)
     for (int whole = 0; whole < 2; ++whole) {
       if (i == 0) {
@@ -152,7 +156,7 @@ pr_status ring_setup(pr_ctx* c) {
       memset(&cfg, 0, sizeof cfg);
       cfg.gridDim = dim3(1u << i);
       cfg.blockDim = dim3(prk::RG_NT);
-      cfg.dynamicSmemBytes = prk::ring_bytes(whole ? prk::RG_MOST : prk::RG_FEW);
+      cfg.dynamicSmemBytes = ring_bytes(whole ? prk::RG_MOST : prk::RG_FEW, 1 << i);
       cudaLaunchAttribute attr[1];
       attr[0].id = cudaLaunchAttributeClusterDimension;
       attr[0].val.clusterDim.x = 1u << i;
@@ -176,29 +180,35 @@ struct RingShape {
   int64_t groups;   // rows in work at a time
 };
 
-// Splits whose CTAs hold a row in half an SM's shared memory, with two places left for the
-// next row's chunks; all of an SM's where eight CTAs' halves do not.  Of those the one that
-// takes the fewest steps: the rows of each cluster, one after the other, each as many steps
-// as its CTAs have chunks and two for its end.  The same with and without a gradient, so
-// that the losses' bits are.
+// Of the launches whose CTAs hold a row, with two places left for the next row's chunks,
+// the one that takes the least time by this count, in the time that an SM takes for a
+// chunk: each cluster's rows come one after the other, a row takes its CTA's chunks and about
+// three for its end, which two CTAs on an SM hide from one another.  The same with and
+// without a gradient, so that the losses' bits are.
 RingShape choose_ring(const pr_ctx* c, pr_dtype dt, int64_t n_rows, int64_t vocab) {
   const int64_t words = vocab * (int64_t)esize(dt) / 16;
   const int64_t chunks = (words + prk::RG_CHUNK - 1) / prk::RG_CHUNK;
-  auto per_cta = [&](int split) { return (chunks + (1 << split) - 1) >> split; };
-  const bool whole = per_cta(3) > prk::RG_FEW - 2;
-  auto steps = [&](int split) {
-    const int64_t places = c->loss_places[whole][split];
-    return (n_rows + places - 1) / places * (per_cta(split) + 2);
-  };
-  int split = 3;
-  for (int i = 2; i >= 0; --i)
-    if (per_cta(i) <= (whole ? prk::RG_MOST : prk::RG_FEW) - 2 && steps(i) <= steps(split)) split = i;
   RingShape s;
-  s.split = split;
-  s.places = whole ? prk::RG_MOST : prk::RG_FEW;
-  s.hold = per_cta(split) <= s.places;
-  s.groups = std::min<int64_t>(n_rows, c->loss_places[whole][split]);
-  s.full = n_rows >= c->loss_places[whole][split];
+  s.split = 3;
+  s.places = prk::RG_MOST;
+  int64_t best = -1;
+  for (int whole = 0; whole < 2; ++whole)
+    for (int split = 0; split < (whole ? 4 : 3); ++split) {
+      const int64_t here = (chunks + (1 << split) - 1) >> split, at_once = c->loss_places[whole][split];
+      const int places = whole ? prk::RG_MOST : prk::RG_FEW;
+      if (here > places - 2) continue;
+      const int64_t time = (n_rows + at_once - 1) / at_once *
+                           (whole ? here + 3 : std::max(2 * here, here + 3));
+      if (best < 0 || time < best) {
+        best = time;
+        s.split = split;
+        s.places = places;
+      }
+    }
+  const int64_t at_once = c->loss_places[s.places == prk::RG_MOST][s.split];
+  s.hold = (chunks + (1 << s.split) - 1) >> s.split <= s.places;
+  s.groups = std::min<int64_t>(n_rows, at_once);
+  s.full = n_rows >= at_once;
   return s;
 }
 
@@ -228,7 +238,7 @@ pr_status launch_ring(pr_ctx* c, prk::LossArgs& a, pr_dtype dt, const RingShape&
   // of the launch before do not all find one, and the last run alone (8,847 rows of V =
   // 151,936 bf16 back to back: 1,538 us, 890 set up after it).
   const pr_status st = launch(ring_kernel(dt, hold), (unsigned)(shape.groups << shape.split),
-                              prk::RG_NT, prk::ring_bytes(places), 1u << shape.split, args, s,
+                              prk::RG_NT, ring_bytes(places, 1 << shape.split), 1u << shape.split, args, s,
                               !shape.full);
   return st == PR_OK ? timing_mark(c, s) : st;
 }
