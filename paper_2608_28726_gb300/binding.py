@@ -625,27 +625,29 @@ class PrPreference(ctypes.Structure):
                 ("length_norm", _I32)]
 
 
-def _loss_outputs(call, dev, logits, n, V, stride, n_stats, stats, logp, grad, want_grad):
-    """The loss calls' outputs, made where the caller has none, and the stride
-    of the gradient's rows."""
-    if stats is None or logp is None or (grad is None and want_grad):
-        d = logits.device
-        stats = torch.empty(n_stats, dtype=torch.float32, device=d) if stats is None else stats
-        logp = torch.empty(n, dtype=torch.float32, device=d) if logp is None else logp
-        if grad is None and want_grad:
-            # rows at the same addresses modulo 16 as the logits'
-            pad = (stride - V) % (16 // logits.element_size())
-            grad = torch.empty(n, V + pad, dtype=logits.dtype, device=d)[:, :V]
-    _dev(call, dev, "stats", stats, _F32_T, n_stats)
-    _dev(call, dev, "logp", logp, _F32_T, n)
+def _loss_grad(call, dev, logits, n, V, stride, grad, want_grad):
+    """(gradient, its address, the stride of its rows) of a loss call."""
     if grad is None:
-        return stats, logp, None, 0
+        if not want_grad:
+            return None, None, 0
+        # rows at the same addresses modulo 16 as the logits'
+        width = V + (stride - V) % (16 // logits.element_size())
+        grad = torch.empty(n, width, dtype=logits.dtype, device=logits.device)
+        return grad if width == V else grad[:, :V], grad.data_ptr(), width
     _dev(call, dev, "grad", grad, (logits.dtype,), contiguous=False)
     if grad.dim() != 2 or grad.size(0) < n or grad.size(1) < V or (grad.size(1) > 1
                                                                     and grad.stride(1) != 1):
         raise PRError(PR_ERR_INVALID_ARG, call,
                       "grad must be 2-D with unit stride along the vocabulary, [%d][%d]" % (n, V))
-    return stats, logp, grad, max(grad.stride(0) if grad.size(0) > 1 else V, V)
+    return grad, grad.data_ptr(), max(grad.stride(0) if grad.size(0) > 1 else V, V)
+
+
+def _loss_out(call, dev, name, t, numel, device):
+    """(output, its address) of a loss call, made where the caller has none."""
+    if t is None:
+        t = torch.empty(numel, dtype=torch.float32, device=device)
+        return t, t.data_ptr()
+    return t, _dptr(call, dev, name, t, _F32_T, numel)
 
 
 def pr_policy_loss(ctx, logits, chosen, advantage, old_logp=None, ref_logp=None, mask=None,
@@ -662,22 +664,20 @@ def pr_policy_loss(ctx, logits, chosen, advantage, old_logp=None, ref_logp=None,
     _logits(call, dev, logits)
     n = logits.size(0)
     V, stride = _rows(logits, vocab)
-    dt = _dtype(logits)
     n_req = 0 if offsets is None else offsets.numel() - 1
-    _dev(call, dev, "chosen", chosen, _I32_T, n)
-    _dev(call, dev, "advantage", advantage, _F32_T, n_req if per_request else n)
-    _dev(call, dev, "old_logp", old_logp, _F32_T, n, optional=True)
-    _dev(call, dev, "ref_logp", ref_logp, _F32_T, n, optional=True)
-    _dev(call, dev, "mask", mask, _U8_T, n, optional=True)
-    _dev(call, dev, "offsets", offsets, _I64_T, optional=True)
-    stats, logp, grad, gs = _loss_outputs(call, dev, logits, n, V, stride, PR_NPOL, stats, logp,
-                                          grad, want_grad)
-    p = PrPolicy(clip_low, clip_high, kl_coef, temperature, grad_scale, int(norm),
-                 int(bool(per_request)))
-    _check(_lib.pr_policy_loss(ctx, logits.data_ptr(), dt, n, V, stride, _ptr(chosen), _ptr(mask),
-                               _ptr(offsets), n_req, _ptr(old_logp), _ptr(ref_logp),
-                               _ptr(advantage), ctypes.byref(p), _ptr(stats), _ptr(logp),
-                               _ptr(grad), gs, _stream(stream)), call)
+    chosen_p = _dptr(call, dev, "chosen", chosen, _I32_T, n)
+    adv_p = _dptr(call, dev, "advantage", advantage, _F32_T, n_req if per_request else n)
+    old_p = _dptr_opt(call, dev, "old_logp", old_logp, _F32_T, n)
+    ref_p = _dptr_opt(call, dev, "ref_logp", ref_logp, _F32_T, n)
+    mask_p = _dptr_opt(call, dev, "mask", mask, _U8_T, n)
+    offsets_p = _dptr_opt(call, dev, "offsets", offsets, _I64_T, 0)
+    stats, stats_p = _loss_out(call, dev, "stats", stats, PR_NPOL, logits.device)
+    logp, logp_p = _loss_out(call, dev, "logp", logp, n, logits.device)
+    grad, grad_p, gs = _loss_grad(call, dev, logits, n, V, stride, grad, want_grad)
+    p = PrPolicy(clip_low, clip_high, kl_coef, temperature, grad_scale, norm, bool(per_request))
+    _check(_lib.pr_policy_loss(ctx, logits.data_ptr(), _dtype(logits), n, V, stride, chosen_p,
+                               mask_p, offsets_p, n_req, old_p, ref_p, adv_p, ctypes.byref(p),
+                               stats_p, logp_p, grad_p, gs, _stream(stream)), call)
     return stats, logp, grad
 
 
@@ -694,23 +694,20 @@ def pr_preference_loss(ctx, logits, chosen, offsets, ref_logp=None, mask=None, b
     _logits(call, dev, logits)
     n = logits.size(0)
     V, stride = _rows(logits, vocab)
-    dt = _dtype(logits)
-    _dev(call, dev, "offsets", offsets, _I64_T, 3)
+    offsets_p = _dptr(call, dev, "offsets", offsets, _I64_T, 3)
     n_req = offsets.numel() - 1
-    _dev(call, dev, "chosen", chosen, _I32_T, n)
-    _dev(call, dev, "ref_logp", ref_logp, _F32_T, n, optional=True)
-    _dev(call, dev, "mask", mask, _U8_T, n, optional=True)
-    if ratio is None:
-        ratio = torch.empty(n_req, dtype=torch.float32, device=logits.device)
-    _dev(call, dev, "ratio", ratio, _F32_T, n_req)
-    stats, logp, grad, gs = _loss_outputs(call, dev, logits, n, V, stride, PR_NPREF, stats, logp,
-                                          grad, want_grad)
-    p = PrPreference(beta, label_smoothing, margin, temperature, grad_scale, int(loss),
-                     int(bool(length_norm)))
-    _check(_lib.pr_preference_loss(ctx, logits.data_ptr(), dt, n, V, stride, _ptr(chosen),
-                                   _ptr(mask), _ptr(offsets), n_req, _ptr(ref_logp),
-                                   ctypes.byref(p), _ptr(stats), _ptr(ratio), _ptr(logp),
-                                   _ptr(grad), gs, _stream(stream)), call)
+    chosen_p = _dptr(call, dev, "chosen", chosen, _I32_T, n)
+    ref_p = _dptr_opt(call, dev, "ref_logp", ref_logp, _F32_T, n)
+    mask_p = _dptr_opt(call, dev, "mask", mask, _U8_T, n)
+    stats, stats_p = _loss_out(call, dev, "stats", stats, PR_NPREF, logits.device)
+    ratio, ratio_p = _loss_out(call, dev, "ratio", ratio, n_req, logits.device)
+    logp, logp_p = _loss_out(call, dev, "logp", logp, n, logits.device)
+    grad, grad_p, gs = _loss_grad(call, dev, logits, n, V, stride, grad, want_grad)
+    p = PrPreference(beta, label_smoothing, margin, temperature, grad_scale, loss,
+                     bool(length_norm))
+    _check(_lib.pr_preference_loss(ctx, logits.data_ptr(), _dtype(logits), n, V, stride, chosen_p,
+                                   mask_p, offsets_p, n_req, ref_p, ctypes.byref(p), stats_p,
+                                   ratio_p, logp_p, grad_p, gs, _stream(stream)), call)
     return stats, ratio, logp, grad
 
 

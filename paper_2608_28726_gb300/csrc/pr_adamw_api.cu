@@ -108,6 +108,7 @@ pr_status run_kind(pr_ctx* c, const pr_adamw_tensor* t, int32_t n_tensors, int k
   a.c2 = step.c2;
   a.ibc1 = step.ibc1;
   a.ibc2 = step.ibc2;
+  a.one = 1.f;
   a.grad_scale = step.grad_scale;
   a.m_out = step.m_out;
   a.v_out = step.v_out;
