@@ -48,20 +48,26 @@ int kind_of(const pr_adamw_tensor& t) {
 }
 constexpr int KINDS = 12;
 
+struct Kernel {
+  void* f;
+  size_t smem;
+};
+
 template <int N, int KIND>
-void* step_kernel() {
+Kernel step_kernel() {
   using B = __nv_bfloat16;
   constexpr int BITS = KIND >= 6 ? 8 : 32;
-  constexpr bool GB = (KIND / 3) % 2 == 1;
+  constexpr bool GB = (KIND / 3) % 2 == 1, MASTER = KIND % 3 == 2;
   using G = typename std::conditional<GB, B, float>::type;
   using P = typename std::conditional<KIND % 3 != 0, B, float>::type;
-  return reinterpret_cast<void*>(&prk::adamw_step<P, G, KIND % 3 == 2, BITS, N>);
+  return {reinterpret_cast<void*>(&prk::adamw_step<P, G, MASTER, BITS, N>),
+          BITS == 8 ? prk::Staged<P, G, MASTER>::BYTES : 0};
 }
 
 template <int N>
-void* kernel_of(int kind, bool unpack) {
-  if (unpack) return reinterpret_cast<void*>(&prk::adamw_unpack<N>);
-  void* const k[KINDS] = {step_kernel<N, 0>(), step_kernel<N, 1>(),  step_kernel<N, 2>(),
+Kernel kernel_of(int kind, bool unpack) {
+  if (unpack) return {reinterpret_cast<void*>(&prk::adamw_unpack<N>), 0};
+  const Kernel k[KINDS] = {step_kernel<N, 0>(), step_kernel<N, 1>(),  step_kernel<N, 2>(),
                           step_kernel<N, 3>(), step_kernel<N, 4>(),  step_kernel<N, 5>(),
                           step_kernel<N, 6>(), step_kernel<N, 7>(),  step_kernel<N, 8>(),
                           step_kernel<N, 9>(), step_kernel<N, 10>(), step_kernel<N, 11>()};
@@ -69,11 +75,12 @@ void* kernel_of(int kind, bool unpack) {
 }
 
 template <int N>
-pr_status launch(pr_ctx* c, prk::AdamwArgs<N>& a, void* kern, cudaStream_t s) {
+pr_status launch(pr_ctx* c, prk::AdamwArgs<N>& a, const Kernel& kern, cudaStream_t s) {
   cudaLaunchConfig_t cfg;
   memset(&cfg, 0, sizeof cfg);
   cfg.gridDim = dim3((unsigned)a.chunk0[a.count]);
   cfg.blockDim = dim3(prk::AW_NT);
+  cfg.dynamicSmemBytes = kern.smem;
   cfg.stream = s;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -81,7 +88,7 @@ pr_status launch(pr_ctx* c, prk::AdamwArgs<N>& a, void* kern, cudaStream_t s) {
   cfg.attrs = attr;
   cfg.numAttrs = 1;
   void* args[] = {&a};
-  PR_CUDA(cudaLaunchKernelExC(&cfg, kern, args));
+  PR_CUDA(cudaLaunchKernelExC(&cfg, kern.f, args));
   g_launches.fetch_add(1, std::memory_order_relaxed);
   a.count = 0;
   return timing_mark(c, s);
@@ -114,7 +121,12 @@ pr_status run_kind(pr_ctx* c, const pr_adamw_tensor* t, int32_t n_tensors, int k
   a.v_out = step.v_out;
   a.ctx_flags = c->flags;
   a.chunk0[0] = 0;
-  void* const kern = kernel_of<N>(kind, unpack);
+  const Kernel kern = kernel_of<N>(kind, unpack);
+  bool& ready = c->adamw_ready[N == prk::AW_MANY][kind];
+  if (!unpack && !ready) {
+    PR_CUDA(cudaFuncSetAttribute(kern.f, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kern.smem));
+    ready = true;
+  }
   const int64_t chunk = (int64_t)prk::AW_NW * per_warp, most = (int64_t)1 << 30;
   int64_t block0 = 0;
   for (int32_t i = 0; i < n_tensors; ++i) {
@@ -150,19 +162,29 @@ pr_status run_kind(pr_ctx* c, const pr_adamw_tensor* t, int32_t n_tensors, int k
   return a.count > 0 ? launch(c, a, kern, s) : PR_OK;
 }
 
-// Blocks per warp: four where that fills the GPU eight CTAs deep, one where the
-// step is short and a warp's four blocks would follow one another.
+// Blocks per warp: enough for the GPU's CTAs to be filled several times over; with
+// 8-bit states 16, for a warp's pipeline of blocks to begin seldom (134 M fp32 parameters:
+// 524 us with their expansion, 617 with four), else four (LM head with states in 32 bits:
+// 2.21 ms, 2.22 with 16); one where the step is short and a warp's blocks would follow one
+// another.
+int blocks_per_warp(const pr_ctx* c, int64_t blocks, bool eight) {
+  const int64_t wave = (int64_t)prk::AW_NW * 3 * c->num_sms;
+  if (eight && blocks >= 2 * 16 * wave) return 16;
+  return blocks >= 2 * 4 * wave ? 4 : 1;
+}
+
 pr_status run(pr_ctx* c, const pr_adamw_tensor* t, int32_t n_tensors, const Step& step,
               bool unpack, cudaStream_t s) {
   int32_t of[KINDS] = {};
-  int64_t blocks = 0;
+  int64_t blocks[KINDS] = {};
   for (int32_t i = 0; i < n_tensors; ++i) {
-    if (t[i].n > 0) ++of[unpack ? 0 : kind_of(t[i])];
-    blocks += (t[i].n + prk::AW_BLOCK - 1) / prk::AW_BLOCK;
+    const int k = unpack ? 0 : kind_of(t[i]);
+    if (t[i].n > 0) ++of[k];
+    blocks[k] += (t[i].n + prk::AW_BLOCK - 1) / prk::AW_BLOCK;
   }
-  const int per_warp = blocks >= (int64_t)4 * prk::AW_NW * 8 * c->num_sms ? 4 : 1;
   for (int k = 0; k < KINDS; ++k) {
     if (of[k] == 0) continue;
+    const int per_warp = blocks_per_warp(c, blocks[k], !unpack && k >= 6);
     const pr_status st =
         of[k] <= prk::AW_FEW
             ? run_kind<prk::AW_FEW>(c, t, n_tensors, k, step, unpack, per_warp, s)

@@ -67,6 +67,7 @@ struct pr_ctx {
   size_t loss_rows = 0;                // rows that its arrivals have room for
   bool loss_ready = false;             // shared memory opt-ins made
   int loss_places[2][4] = {};          // clusters of 1, 2, 4, 8 CTAs resident; half, all of the SMs
+  bool adamw_ready[2][12] = {};        // pr_adamw_step: shared memory opt-ins made
   // PR_OPT_TIMING: events after each kernel of the last multi-kernel call
   int32_t timing = 0;
   cudaEvent_t tev[PR_MAX_TIMED + 1] = {};
