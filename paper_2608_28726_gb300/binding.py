@@ -28,6 +28,9 @@ PR_LMHEAD_MAX_VOCAB = (1 << 31) - 256
 PR_NORM_TOKENS, PR_NORM_REQUESTS = 0, 1
 PR_PREF_SIGMOID, PR_PREF_SQUARED, PR_PREF_HINGE = 0, 1, 2
 PR_NPOL, PR_NPREF = 6, 5
+(PR_POL_LOSS, PR_POL_SURROGATE, PR_POL_KL, PR_POL_RATIO, PR_POL_CLIPPED,
+ PR_POL_OLD_KL) = range(PR_NPOL)
+PR_PREF_LOSS, PR_PREF_ACCURACY, PR_PREF_H, PR_PREF_REWARD_W, PR_PREF_REWARD_L = range(PR_NPREF)
 PR_ADAMW_BLOCK = 256
 
 # every symbol include/pro_router.h declares
@@ -625,6 +628,16 @@ class PrPreference(ctypes.Structure):
                 ("length_norm", _I32)]
 
 
+def _loss_rows(call, t, name, n, V):
+    """The stride of the rows of a loss call's logits or gradient, [n][V] of them."""
+    shape, strides = t.shape, t.stride()
+    if (len(shape) != 2 or shape[0] < n or not 0 < V <= shape[1]
+            or (V > 1 and strides[1] != 1) or (n > 1 and strides[0] < V)):
+        raise PRError(PR_ERR_INVALID_ARG, call, "%s must be 2-D with unit stride along the "
+                      "vocabulary and rows that do not overlap, [%s][%s]" % (name, n, V))
+    return strides[0] if n > 1 else V
+
+
 def _loss_grad(call, dev, logits, n, V, stride, grad, want_grad):
     """(gradient, its address, the stride of its rows) of a loss call."""
     if grad is None:
@@ -635,11 +648,7 @@ def _loss_grad(call, dev, logits, n, V, stride, grad, want_grad):
         grad = torch.empty(n, width, dtype=logits.dtype, device=logits.device)
         return grad if width == V else grad[:, :V], grad.data_ptr(), width
     _dev(call, dev, "grad", grad, (logits.dtype,), contiguous=False)
-    if grad.dim() != 2 or grad.size(0) < n or grad.size(1) < V or (grad.size(1) > 1
-                                                                    and grad.stride(1) != 1):
-        raise PRError(PR_ERR_INVALID_ARG, call,
-                      "grad must be 2-D with unit stride along the vocabulary, [%d][%d]" % (n, V))
-    return grad, grad.data_ptr(), max(grad.stride(0) if grad.size(0) > 1 else V, V)
+    return grad, grad.data_ptr(), _loss_rows(call, grad, "grad", n, V)
 
 
 def _loss_out(call, dev, name, t, numel, device):
@@ -662,8 +671,9 @@ def pr_policy_loss(ctx, logits, chosen, advantage, old_logp=None, ref_logp=None,
     call = "pr_policy_loss"
     dev = _ctx_device(ctx)
     _logits(call, dev, logits)
-    n = logits.size(0)
-    V, stride = _rows(logits, vocab)
+    n, width = logits.shape if logits.dim() == 2 else (0, 0)
+    V = width if vocab is None else int(vocab)
+    stride = _loss_rows(call, logits, "logits", n, V)
     n_req = 0 if offsets is None else offsets.numel() - 1
     chosen_p = _dptr(call, dev, "chosen", chosen, _I32_T, n)
     adv_p = _dptr(call, dev, "advantage", advantage, _F32_T, n_req if per_request else n)
@@ -692,8 +702,9 @@ def pr_preference_loss(ctx, logits, chosen, offsets, ref_logp=None, mask=None, b
     call = "pr_preference_loss"
     dev = _ctx_device(ctx)
     _logits(call, dev, logits)
-    n = logits.size(0)
-    V, stride = _rows(logits, vocab)
+    n, width = logits.shape if logits.dim() == 2 else (0, 0)
+    V = width if vocab is None else int(vocab)
+    stride = _loss_rows(call, logits, "logits", n, V)
     offsets_p = _dptr(call, dev, "offsets", offsets, _I64_T, 3)
     n_req = offsets.numel() - 1
     chosen_p = _dptr(call, dev, "chosen", chosen, _I32_T, n)

@@ -456,3 +456,32 @@ def test_refusals(B, ctx):
     with pytest.raises(B.PRError):  # three answers are no pairs
         B.pr_preference_loss(ctx, x, c, to([0, 1, 2, 4], np.int64))
     assert B.launch_count() == n0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rows_that_overlap_or_end_early_are_refused(B, ctx, dtype):
+    g, x, _, ch, old, ref = draw(3, 4, 64, dtype)
+    c, a, off = to(ch), to(old), to([0, 2, 4], np.int64)
+    one = x[:1].expand(4, 64)
+    steps = torch.zeros(200, dtype=x.dtype, device="cuda").as_strided((4, 64), (32, 1))
+    n0 = B.launch_count()
+    for call in (lambda **k: B.pr_policy_loss(ctx, k.pop("x", x), c, a, **k),
+                 lambda **k: B.pr_preference_loss(ctx, k.pop("x", x), c, off, **k)):
+        for k in (dict(x=one), dict(x=steps), dict(grad=one), dict(grad=steps), dict(vocab=65),
+                  dict(vocab=0), dict(vocab=-1), dict(x=x[0]), dict(x=x.view(2, 2, 64)),
+                  dict(x=x[:, :0])):
+            with pytest.raises(B.PRError) as e:
+                call(**k)
+            assert e.value.status == B.PR_ERR_INVALID_ARG, k
+    assert B.launch_count() == n0
+
+
+def test_one_row_has_any_stride(B, ctx):
+    """A single row's stride is never used, so whatever a view says of it will do."""
+    g, x, x64, ch, old, ref = draw(5, 1, 96, "f32")
+    one = torch.zeros(1, 96, device="cuda").as_strided((1, 96), (0, 1)).copy_(x)
+    want = B.pr_policy_loss(ctx, x, to(ch), to(old))
+    got = B.pr_policy_loss(ctx, one, to(ch), to(old), grad=torch.empty(96, device="cuda").as_strided(
+        (1, 96), (3, 1)))
+    for w, t in zip(want, got):
+        assert torch.equal(w, t)
