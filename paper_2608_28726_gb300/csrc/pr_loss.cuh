@@ -62,6 +62,7 @@ struct LossArgs {
   float* z;            // [n_rows] l - ref (preference) or dL/dl / T
   double* part;        // [groups][LS_NSTAT] statistics of each group's rows
   uint32_t* ctx_flags;
+  int32_t own;  // every CTA lists the rows by itself (loss_forward)
 };
 
 // ---- which rows count -----------------------------------------------------------------
@@ -243,6 +244,95 @@ static __global__ void __launch_bounds__(PL_BLOCK) loss_list(const LossArgs a) {
   int32_t all;
   const int32_t rank = block_rank(r >= 0, warps, all);
   if (t < a.n_rows) put_row(a, t, r, __ldcg(a.block + blockIdx.x) + rank);
+}
+
+// The smallest batches: by every CTA of the kernel that reads the logits, in its shared
+// memory, without a launch before it; the first CTA leaves what later kernels need.  (20 rows
+// of V = 32,000 fp32: 24 us a call for 27 with a launch, 354 rows 28 for 30.)
+constexpr int OWN_MOST = 512;  // rows, requests
+struct OwnPlan {
+  int4 list[OWN_MOST];
+  int32_t skipped[OWN_MOST], count[OWN_MOST];
+  uint32_t on[OWN_MOST / 32];  // which rows count
+  int32_t live, used;
+};
+template <int NT>
+__device__ __forceinline__ void own_plan(const LossArgs& a, OwnPlan& p, bool pairs) {
+  constexpr int NW = NT / 32, W = (OWN_MOST / 32 + NW - 1) / NW;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const bool leaves = blockIdx.x == 0;
+  for (int q = tid; q < a.n_req; q += NT) p.count[q] = 0;
+  if (tid == 0) p.used = 0;
+  int32_t r[W], y[W];
+#pragma unroll
+  for (int k = 0; k < W; ++k) {
+    const int64_t t = 32 * (warp + k * NW) + lane;
+    y[k] = t < a.n_rows ? __ldcg(a.chosen + t) : 0;
+    r[k] = t < a.n_rows ? counted_by(a, t) : -1;
+    const unsigned b = __ballot_sync(FULL, r[k] >= 0);
+    if (lane == 0 && warp + k * NW < OWN_MOST / 32) p.on[warp + k * NW] = b;
+  }
+  __syncthreads();
+  const int32_t c = lane < OWN_MOST / 32 ? __popc(p.on[lane]) : 0;
+#pragma unroll
+  for (int k = 0; k < W; ++k) {
+    const int g = warp + k * NW;
+    const int32_t t = 32 * g + lane;
+    const int32_t below = __reduce_add_sync(FULL, lane < g ? c : 0);
+    if (t < a.n_rows) {
+      const int32_t before = below + __popc(p.on[g] & ((1u << lane) - 1u));
+      if (r[k] >= 0) {
+        p.list[before] = make_int4(t, r[k], y[k], 0);
+        atomicAdd(&p.count[r[k]], 1);
+      } else {
+        p.skipped[t - before] = t;
+        if (leaves) a.logp[t] = 0.f;
+      }
+      if (leaves) a.row_req[t] = r[k];
+    }
+  }
+  __syncthreads();
+  for (int q = tid; q < a.n_req; q += NT) {
+    if (pairs ? (q & 1) == 0 && p.count[q] > 0 && p.count[q + 1] > 0 : p.count[q] > 0)
+      atomicAdd(&p.used, 1);
+    if (leaves) {
+      int64_t lo, hi;
+      bad_bounds(a, q, lo, hi);
+      a.count[q] = p.count[q];
+    }
+  }
+  const int32_t live = __reduce_add_sync(FULL, c);
+  if (tid == 0) p.live = live;
+  __syncthreads();
+  if (leaves && tid == 0) {
+    a.totals[0] = live;
+    a.totals[1] = p.used;
+  }
+}
+// the counted rows of a batch and their i-th, and the rest, wherever they are listed
+struct Rows {
+  const OwnPlan* own;
+  int32_t live;
+  __device__ __forceinline__ int4 at(const LossArgs& a, int64_t i) const {
+    if (i >= live) return make_int4(0, -1, 0, 0);
+    return own ? own->list[i] : __ldcg(a.list + i);
+  }
+  __device__ __forceinline__ int32_t skipped(const LossArgs& a, int64_t i) const {
+    return own ? own->skipped[i] : __ldcg(a.skipped + i);
+  }
+  __device__ __forceinline__ int32_t count(const LossArgs& a, int32_t r) const {
+    return own ? own->count[r] : __ldcg(a.count + r);
+  }
+  // 1 / what the losses are divided by: rows, or requests with some
+  __device__ __forceinline__ double share(const LossArgs& a) const {
+    return 1.0 / (double)(a.norm ? (own ? own->used : __ldcg(a.totals + 1)) : live);
+  }
+};
+template <int NT>
+__device__ __forceinline__ Rows rows_of(const LossArgs& a, bool own, OwnPlan* p, bool pairs) {
+  if (!own) return Rows{nullptr, (int32_t)__ldcg(a.totals)};
+  own_plan<NT>(a, *p, pairs);
+  return Rows{p, p->live};
 }
 
 // ---- the losses of one row / pair -------------------------------------------------------
@@ -598,8 +688,8 @@ __device__ __noinline__ void end_math(const LossArgs& a, int64_t row, const RowI
 
 // The scalars of a listed row {row, request, token}.  Whole warp.
 template <typename T, bool PREF>
-__device__ __forceinline__ RowIn fetch_row(const LossArgs& a, const Share& s, const int4& ref,
-                                           int lane) {
+__device__ __forceinline__ RowIn fetch_row(const LossArgs& a, const Rows& rows, const Share& s,
+                                           const int4& ref, int lane) {
   const int64_t row = ref.x;
   const int32_t r = ref.y, y = ref.z;
   RowIn in;
@@ -614,7 +704,7 @@ __device__ __forceinline__ RowIn fetch_row(const LossArgs& a, const Share& s, co
   if (!PREF) {
     if (a.old_logp) in.old = __ldcg(a.old_logp + row);
     in.adv = __ldcg(a.adv + (a.per_request ? (int64_t)r : row));
-    if (a.norm) in.count = __ldcg(a.count + r);
+    if (a.norm) in.count = rows.count(a, r);
   }
   const int32_t v = end_of(a, s, lane);
   if (v >= 0) in.edge = Traits<T>::elem(x, v);
@@ -755,26 +845,26 @@ __global__ void __launch_bounds__(FW_NT, FW_CTAS) loss_forward(const __grid_cons
   __syncthreads();
   pdl_wait();
   pdl_trigger();
-  const int64_t live = __ldcg(a.totals);
+  extern __shared__ __align__(16) unsigned char fw_raw[];
+  const Rows rows = rows_of<FW_NT>(a, a.own, reinterpret_cast<OwnPlan*>(fw_raw), PREF);
+  const int64_t live = rows.live;
   const int64_t most = (a.vocab + Tr::VEC - 1) / Tr::VEC;              // words of a row
   const int64_t per_row = (most + FW_TILE - 1) / FW_TILE, tiles = live * per_row;
   const int64_t G = min((int64_t)gridDim.x, max(tiles, (int64_t)1)), b = blockIdx.x;
   if (b >= G) return;
   const int64_t t0 = run_begin(b, tiles, G), t1 = run_begin(b + 1, tiles, G);
-  auto ref_of = [&](int64_t i) {  // the i-th row that counts
-    return i < live ? __ldcg(a.list + i) : make_int4(0, -1, 0, 0);
-  };
+  auto ref_of = [&](int64_t i) { return rows.at(a, i); };
   int64_t i = t0 / per_row;
   int32_t j0 = (int32_t)(t0 - i * per_row);  // the first tile of row i here
   int64_t left = t1 - t0;
   uint32_t n = 0;  // pieces summed
   if (warp == FW_NW) {
     // ---- the rows' ends
-    const double share = PREF ? 0.0 : 1.0 / (double)__ldcg(a.totals + (a.norm ? 1 : 0));
+    const double share = PREF ? 0.0 : rows.share(a);
     int4 ref = ref_of(i), ref1 = ref_of(i + 1);
-    RowIn in = fetch_row<T, PREF>(a, share_of<T>(a, ref.x, 1, 0), ref, lane);
+    RowIn in = fetch_row<T, PREF>(a, rows, share_of<T>(a, ref.x, 1, 0), ref, lane);
     for (; left > 0; ++i, j0 = 0) {
-      const RowIn next = fetch_row<T, PREF>(a, share_of<T>(a, ref1.x, 1, 0), ref1, lane);
+      const RowIn next = fetch_row<T, PREF>(a, rows, share_of<T>(a, ref1.x, 1, 0), ref1, lane);
       const int64_t row = ref.x;
       ref = ref1;
       ref1 = ref_of(i + 2);
@@ -940,7 +1030,8 @@ __device__ __forceinline__ float2 exchange(float2* to, uint64_t* bar, uint32_t p
 }
 
 
-template <typename T, bool HOLD>
+// (OWN as an argument: 2.5% of the time of 8,657 rows of V = 151,936 bf16.)
+template <typename T, bool HOLD, bool OWN>
 __global__ void __launch_bounds__(RG_NT, 2)
     loss_ring(const __grid_constant__ LossArgs a, const int places) {
   extern __shared__ __align__(16) unsigned char smem_raw[];
@@ -979,10 +1070,10 @@ __global__ void __launch_bounds__(RG_NT, 2)
     if (ok) ok = ring_wait(sm_addr(b), phase, a.ctx_flags);
     __syncwarp();
   };
-  const int32_t live = (int32_t)__ldcg(a.totals);
-  auto ref_of = [&](int64_t i) {  // the i-th row that counts
-    return i < live ? __ldcg(a.list + i) : make_int4(0, -1, 0, 0);
-  };
+  const Rows rows = rows_of<RG_NT>(
+      a, OWN, reinterpret_cast<OwnPlan*>(ring + (size_t)places * RG_BYTES), false);
+  const int32_t live = rows.live;
+  auto ref_of = [&](int64_t i) { return rows.at(a, i); };
   int place = 0;         // of the ring
   uint32_t turn = 0u;    // how often it has been gone around, its last bit
   auto step = [&]() {
@@ -1023,10 +1114,10 @@ __global__ void __launch_bounds__(RG_NT, 2)
       wait(&sm.full[(int)(i % places)], (uint32_t)(i / places) & 1u);
   } else if (warp == RG_NW + 1) {
     // ---- the rows' ends
-    const double share = 1.0 / (double)__ldcg(a.totals + (a.norm ? 1 : 0));
+    const double share = rows.share(a);
     uint32_t n = 0, agains = 0;
     int4 ref = ref_of(first), ref1 = ref_of(first + G);
-    RowIn in = fetch_row<T, false>(a, share_of<T>(a, ref.x, C, rank), ref, lane);
+    RowIn in = fetch_row<T, false>(a, rows, share_of<T>(a, ref.x, C, rank), ref, lane);
     // What a peer's gradient may be written over (the logits' own buffer) has been read when
     // this CTA's sums are sent: the next row's scalars are there before a result is given.
     auto landed = [&](RowIn& q) {
@@ -1036,7 +1127,7 @@ __global__ void __launch_bounds__(RG_NT, 2)
     landed(in);
     if (C > 1) named_bar_arrive(BAR_IN, 32 * (RG_NW + 1));
     for (int64_t i = first; i < live; i += G) {
-      RowIn next = fetch_row<T, false>(a, share_of<T>(a, ref1.x, C, rank), ref1, lane);
+      RowIn next = fetch_row<T, false>(a, rows, share_of<T>(a, ref1.x, C, rank), ref1, lane);
       const int64_t row = ref.x;
       const Share sh = share_of<T>(a, row, C, rank);
       ref = ref1;
@@ -1175,7 +1266,7 @@ __global__ void __launch_bounds__(RG_NT, 2)
     }
     if (HOLD)  // the rows that do not count
       for (int64_t i = first; i < a.n_rows - live; i += G) {
-        const int64_t row = __ldcg(a.skipped + i);
+        const int64_t row = rows.skipped(a, i);
         const Share sh = share_of<T>(a, row, C, rank);
         T* const g = reinterpret_cast<T*>(a.grad) + row * a.grad_stride;
         const bool vec = ((reinterpret_cast<uintptr_t>(sh.x) ^ reinterpret_cast<uintptr_t>(g)) & 15u) == 0;

@@ -11,6 +11,7 @@
 
 using namespace prh;
 
+static_assert(sizeof(prk::OwnPlan) <= prk::RG_BYTES, "a place of the ring holds the list");
 static_assert(PR_NPOL == prk::LS_NSTAT && PR_NPREF < prk::LS_NSTAT, "statistics");
 
 namespace {
@@ -120,16 +121,25 @@ pr_status launch(const void* kern, unsigned grid, unsigned threads, size_t smem,
   return PR_OK;
 }
 
-size_t ring_bytes(int places, int cluster) {
-  return prk::ring_start(cluster) + (size_t)places * prk::RG_BYTES;
+size_t ring_bytes(int places, int cluster, bool own) {
+  return prk::ring_start(cluster) + (size_t)places * prk::RG_BYTES +
+         (own ? sizeof(prk::OwnPlan) : 0);
 }
 
-const void* ring_kernel(pr_dtype dt, bool hold) {
+bool own_list(const prk::LossArgs& a) {
+  return a.n_rows > 0 && a.n_rows <= prk::OWN_MOST && a.n_req <= prk::OWN_MOST;
+}
+
+template <typename T, bool HOLD>
+const void* ring_kernel(bool own) {
+  return own ? reinterpret_cast<const void*>(&prk::loss_ring<T, HOLD, true>)
+             : reinterpret_cast<const void*>(&prk::loss_ring<T, HOLD, false>);
+}
+
+const void* ring_kernel(pr_dtype dt, bool hold, bool own) {
   if (dt == PR_DTYPE_BF16)
-    return hold ? reinterpret_cast<const void*>(&prk::loss_ring<__nv_bfloat16, true>)
-                : reinterpret_cast<const void*>(&prk::loss_ring<__nv_bfloat16, false>);
-  return hold ? reinterpret_cast<const void*>(&prk::loss_ring<float, true>)
-              : reinterpret_cast<const void*>(&prk::loss_ring<float, false>);
+    return hold ? ring_kernel<__nv_bfloat16, true>(own) : ring_kernel<__nv_bfloat16, false>(own);
+  return hold ? ring_kernel<float, true>(own) : ring_kernel<float, false>(own);
 }
 
 template <typename T>
@@ -144,8 +154,10 @@ pr_status ring_setup(pr_ctx* c) {
   if (c->loss_ready) return PR_OK;
   for (pr_dtype dt : {PR_DTYPE_F32, PR_DTYPE_BF16})
     for (bool hold : {false, true})
-      PR_CUDA(cudaFuncSetAttribute(ring_kernel(dt, hold), cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                   (int)ring_bytes(prk::RG_MOST, 8)));
+      for (bool own : {false, true})
+        PR_CUDA(cudaFuncSetAttribute(ring_kernel(dt, hold, own),
+                                     cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                     (int)ring_bytes(prk::RG_MOST, 8, false)));
   for (int i = 0; i < 4; ++i)
     for (int whole = 0; whole < 2; ++whole) {
       if (i == 0) {
@@ -156,7 +168,7 @@ pr_status ring_setup(pr_ctx* c) {
       memset(&cfg, 0, sizeof cfg);
       cfg.gridDim = dim3(1u << i);
       cfg.blockDim = dim3(prk::RG_NT);
-      cfg.dynamicSmemBytes = ring_bytes(whole ? prk::RG_MOST : prk::RG_FEW, 1 << i);
+      cfg.dynamicSmemBytes = ring_bytes(whole ? prk::RG_MOST : prk::RG_FEW, 1 << i, false);
       cudaLaunchAttribute attr[1];
       attr[0].id = cudaLaunchAttributeClusterDimension;
       attr[0].val.clusterDim.x = 1u << i;
@@ -165,7 +177,7 @@ pr_status ring_setup(pr_ctx* c) {
       cfg.attrs = attr;
       cfg.numAttrs = 1;
       int n = 0;
-      PR_CUDA(cudaOccupancyMaxActiveClusters(&n, ring_kernel(PR_DTYPE_BF16, true), &cfg));
+      PR_CUDA(cudaOccupancyMaxActiveClusters(&n, ring_kernel(PR_DTYPE_BF16, true, false), &cfg));
       c->loss_places[whole][i] = std::max(n, 1);
     }
   c->loss_ready = true;
@@ -176,6 +188,7 @@ pr_status ring_setup(pr_ctx* c) {
 struct RingShape {
   int split, places;
   bool hold;        // a row's chunks fit the cluster's rings
+  bool spare;       // and leave a place free
   bool full;        // every place is taken
   int64_t groups;   // rows in work at a time
 };
@@ -206,7 +219,9 @@ RingShape choose_ring(const pr_ctx* c, pr_dtype dt, int64_t n_rows, int64_t voca
       }
     }
   const int64_t at_once = c->loss_places[s.places == prk::RG_MOST][s.split];
-  s.hold = (chunks + (1 << s.split) - 1) >> s.split <= s.places;
+  const int64_t here = (chunks + (1 << s.split) - 1) >> s.split;
+  s.hold = here <= s.places;
+  s.spare = here < s.places;
   s.groups = std::min<int64_t>(n_rows, at_once);
   s.full = n_rows >= at_once;
   return s;
@@ -214,6 +229,7 @@ RingShape choose_ring(const pr_ctx* c, pr_dtype dt, int64_t n_rows, int64_t voca
 
 // One CTA where it takes no longer than the second launch (about 3 us) that many need.
 pr_status launch_plan(pr_ctx* c, prk::LossArgs& a, int pairs, cudaStream_t s) {
+  if (a.own) return PR_OK;
   void* args[] = {&a, &pairs};
   if (a.n_rows <= 4 * prk::PL_BLOCK && a.n_req <= prk::PL_FEW) {
     const pr_status st = launch(reinterpret_cast<const void*>(&prk::loss_plan), 1, prk::PL_BLOCK, 0,
@@ -232,13 +248,13 @@ pr_status launch_plan(pr_ctx* c, prk::LossArgs& a, int pairs, cudaStream_t s) {
 
 pr_status launch_ring(pr_ctx* c, prk::LossArgs& a, pr_dtype dt, const RingShape& shape, bool hold,
                       cudaStream_t s) {
-  int places = shape.places;
+  int places = shape.places - (a.own ? 1 : 0);  // (the rows' list takes one)
   void* args[] = {&a, &places};
   // A grid that takes every place is not set up early: clusters placed around the CTAs
   // of the launch before do not all find one, and the last run alone (8,847 rows of V =
   // 151,936 bf16 back to back: 1,538 us, 890 set up after it).
-  const pr_status st = launch(ring_kernel(dt, hold), (unsigned)(shape.groups << shape.split),
-                              prk::RG_NT, ring_bytes(places, 1 << shape.split), 1u << shape.split, args, s,
+  const pr_status st = launch(ring_kernel(dt, hold, a.own), (unsigned)(shape.groups << shape.split),
+                              prk::RG_NT, ring_bytes(places, 1 << shape.split, a.own), 1u << shape.split, args, s,
                               !shape.full);
   return st == PR_OK ? timing_mark(c, s) : st;
 }
@@ -247,7 +263,8 @@ pr_status launch_forward(pr_ctx* c, prk::LossArgs& a, pr_dtype dt, bool pref, cu
   void* args[] = {&a};
   const pr_status st = launch(dt == PR_DTYPE_BF16 ? forward_kernel<__nv_bfloat16>(pref)
                                                   : forward_kernel<float>(pref),
-                              (unsigned)forward_grid(c), prk::FW_NT, 0, 1, args, s);
+                              (unsigned)forward_grid(c), prk::FW_NT, a.own ? sizeof(prk::OwnPlan) : 0, 1,
+                              args, s);
   return st == PR_OK ? timing_mark(c, s) : st;
 }
 
@@ -330,6 +347,7 @@ pr_status pr_policy_loss(pr_ctx* c, const void* logits, pr_dtype dt, int64_t n_r
   const RingShape ring = choose_ring(c, dt, n_rows, vocab);
   if ((st = workspace(c, a, std::max(ring.groups, forward_grid(c)), false, !ring.hold)) != PR_OK)
     return st;
+  a.own = own_list(a) && (!ring.hold || ring.spare);
   if ((st = timing_begin(c, s)) != PR_OK) return st;
   if ((st = launch_plan(c, a, 0, s)) != PR_OK) return st;
   if (ring.hold) return launch_ring(c, a, dt, ring, grad != nullptr, s);
@@ -368,6 +386,7 @@ pr_status pr_preference_loss(pr_ctx* c, const void* logits, pr_dtype dt, int64_t
   a.loss = p->loss;
   a.length_norm = p->length_norm ? 1 : 0;
   if ((st = workspace(c, a, 0, true, true)) != PR_OK) return st;
+  a.own = own_list(a);
   if ((st = timing_begin(c, s)) != PR_OK) return st;
   if ((st = launch_plan(c, a, 1, s)) != PR_OK) return st;
   if (n_rows > 0 && (st = launch_forward(c, a, dt, true, s)) != PR_OK)

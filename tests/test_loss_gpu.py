@@ -485,3 +485,57 @@ def test_one_row_has_any_stride(B, ctx):
         (1, 96), (3, 1)))
     for w, t in zip(want, got):
         assert torch.equal(w, t)
+
+
+@pytest.mark.parametrize("n,n_req", [(31, 31), (33, 2), (511, 3), (512, 512), (512, 1), (513, 512),
+                                     (300, 513), (513, 4), (1500, 1024), (1500, 1025), (4096, 7),
+                                     (4097, 7)])
+@pytest.mark.parametrize("keep", [0.02, 0.5, 1.0])
+def test_how_rows_are_listed(B, ctx, n, n_req, keep):
+    """Rows and requests around the sizes at which the counted rows are listed another
+    way: by each CTA, by one CTA, by two kernels."""
+    V = 24
+    g, x, x64, ch, old, ref = draw(n * 3 + n_req, n, V, "f32")
+    off = offsets_of(g, n, n_req)
+    mask = (g.random(n) < keep).astype(np.uint8)
+    adv = g.normal(size=n_req).astype(np.float32)
+
+    # the same rows in a batch whose further rows and requests are empty: listed by two kernels
+    more, more_req = 4200 - n, 1100 - n_req
+
+    def pad(t, k=None):
+        k = more if k is None else k
+        return None if t is None else np.concatenate([t, np.full((k, *t.shape[1:]), 0, t.dtype)])
+
+    wide = torch.full((n + more, V), torch.nan, device="cuda")
+    wide[:n] = x
+    for norm in (0, 1):
+        kw = dict(norm=norm, per_request=True, kl_coef=0.1)
+        stats, logp, grad = B.pr_policy_loss(ctx, x, to(ch), to(adv), old_logp=to(old),
+                                             ref_logp=to(ref), mask=to(mask), offsets=to(off), **kw)
+        s, l, _ = L.policy(x64, ch, adv, old, ref, mask, off, requests=bool(norm),
+                           per_request=True, kl_coef=0.1, clip_low=0.2, clip_high=0.2)
+        check_rows(logp, l, None, None, "f32")
+        check_stats(stats, s, 2.0 * (mask.any() or 0))
+        s2, l2, g2 = B.pr_policy_loss(ctx, wide, to(pad(ch)), to(pad(adv, more_req)),
+                                      old_logp=to(pad(old)), ref_logp=to(pad(ref)),
+                                      mask=to(pad(mask)),
+                                      offsets=to(np.r_[off, np.full(more_req, n)]), **kw)
+        assert torch.equal(l2[:n], logp) and torch.equal(g2[:n], grad)
+        assert not l2[n:].any() and not g2[n:].any()
+        check_stats(s2, s, 2.0 * (mask.any() or 0))
+    off = offsets_of(g, n, n_req + n_req % 2)
+    kw = dict(beta=0.2, loss=0, label_smoothing=0.1, margin=0.25, length_norm=bool(n % 2))
+    stats, ratio, logp, grad = B.pr_preference_loss(ctx, x, to(ch), to(off), ref_logp=to(ref),
+                                                    mask=to(mask), **kw)
+    s, r, l, _ = L.preference(x64, ch, off, ref, mask, temperature=1.0, **kw)
+    check_rows(logp, l, None, None, "f32")
+    lim = 2e-5 * np.maximum(np.diff(off), 1) + 1e-6 * np.abs(r)
+    assert (np.abs(ratio.double().cpu().numpy() - r) <= lim + 1e-6).all()
+    check_stats(stats, s, 0.2 * np.abs(r).max() + 1.0)
+    k = 1100 - (len(off) - 1)
+    s2, r2, l2, g2 = B.pr_preference_loss(ctx, wide, to(pad(ch)), to(np.r_[off, np.full(k, n)]),
+                                          ref_logp=to(pad(ref)), mask=to(pad(mask)), **kw)
+    assert torch.equal(l2[:n], logp) and torch.equal(g2[:n], grad) and torch.equal(s2, stats)
+    assert torch.equal(r2[:len(r)], ratio) and not r2[len(r):].any()
+    assert not l2[n:].any() and not g2[n:].any()
