@@ -47,7 +47,7 @@ struct AdamwArgs {
   AdamwEntry t[N];
   int32_t chunk0[N + 1];  // first chunk of each tensor; a chunk is AW_NW * per_warp blocks
   int32_t count, per_warp;
-  float lr, eps, b1, c1, b2, c2, ibc1, ibc2;  // c = 1 - b, ibc = 1 / (1 - b^t)
+  float lr, eps, b1, c1, b2, c2, ibc1, ibc2, root_ibc2;  // c = 1 - b, ibc = 1 / (1 - b^t)
   float one;              // 1: see sum2
   const float* grad_scale;
   float *m_out, *v_out;  // expansion: [blocks][256]
@@ -193,34 +193,31 @@ __device__ __forceinline__ float sqrt_fast(float x) {
   asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-// m / (sqrt(v) + eps), within 2^-21.  Subnormal numbers may be taken for 0 where eps is
-// far above their roots.
-__device__ __forceinline__ float update_fast(float m, float v, float eps) {
-  float r;
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(sqrt_fast(v) + eps));
-  return m * r;
+__device__ __forceinline__ float rcp_fast(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
 }
-__device__ __forceinline__ float update_any(float m, float v, float eps) {
-  return m / (sqrtf(v) + eps);
-}
+// From this eps on m / (sqrt(v) + eps) takes approximate roots and reciprocals (within
+// 2^-21): subnormal numbers taken for 0 then have roots far below eps.
 constexpr float EPS_FAST = 1e-12f;
 // The codes round(STEPS r) of ratios' roots r = sqrt(x) (ROOTS = 1) or x^(1/4) (2), x
 // already divided by the scale, in the last bytes of q.  The definition takes IEEE roots;
 // approximate ones (within 2^-22) give the same code unless STEPS r lies within 255 x 2^-21
 // of the middle between two, which the whole warp then looks up exactly (one block in
 // ten).  45% fewer instructions than with IEEE roots throughout.
-// With ROOTS = 1 they take the signs of `m`.
-template <int ROOTS>
-__device__ __forceinline__ void codes_of(const float2 (&x)[4], const float2 (&m)[4],
+// With ROOTS = 1 they take the signs of `m`.  `rooted`: x, or with ROOTS = 2 its root.
+template <int ROOTS, typename Rooted>
+__device__ __forceinline__ void codes_of(const float2 (&x)[4], const float2 (&m)[4], Rooted rooted,
                                          uint32_t (&q)[8]) {
   constexpr float STEPS = ROOTS == 1 ? 127.f : 255.f;
   constexpr float MAGIC = 12582912.f;  // 1.5 x 2^23: a sum's last bits are the rounded addend
   float off = 0.f;
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    float2 r = make_float2(sqrt_fast(x[j].x), sqrt_fast(x[j].y));
-    if (ROOTS == 2) r = make_float2(sqrt_fast(r.x), sqrt_fast(r.y));
-    else r = make_float2(copysignf(r.x, m[j].x), copysignf(r.y, m[j].y));
+    float2 r = rooted(j);
+    r = make_float2(sqrt_fast(r.x), sqrt_fast(r.y));
+    if (ROOTS == 1) r = make_float2(copysignf(r.x, m[j].x), copysignf(r.y, m[j].y));
     const float2 steps = make_float2(STEPS, STEPS);
     const float2 t = __ffma2_rn(r, steps, make_float2(MAGIC, MAGIC));
     const float2 w = __fadd2_rn(make_float2(MAGIC, MAGIC), make_float2(-t.x, -t.y));
@@ -318,23 +315,33 @@ __device__ __forceinline__ void step_block(const BlockIn<P, G, MASTER, BITS>& in
       }
   }
   auto both = [](float x) { return make_float2(x, x); };
+  float2 roots[4];  // of v
   auto update = [&](auto quotient) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const float2 x = __fmul2_rn(make_float2(g[2 * j], g[2 * j + 1]), both(gs));
       m[j] = sum2(__fmul2_rn(m[j], both(a.b1)), __fmul2_rn(x, both(a.c1)), a.one);
       v[j] = sum2(__fmul2_rn(v[j], both(a.b2)), __fmul2_rn(__fmul2_rn(x, x), both(a.c2)), a.one);
-      const float2 mh = __fmul2_rn(m[j], both(a.ibc1)), vh = __fmul2_rn(v[j], both(a.ibc2));
+      const float2 mh = __fmul2_rn(m[j], both(a.ibc1));
       float2 q = make_float2(p[2 * j], p[2 * j + 1]);
-      const float2 by = __ffma2_rn(both(t.wd), q, make_float2(quotient(mh.x, vh.x, a.eps),
-                                                              quotient(mh.y, vh.y, a.eps)));
+      const float2 by = __ffma2_rn(both(t.wd), q, quotient(mh, j));
       q = __ffma2_rn(both(-a.lr), by, q);
       p[2 * j] = q.x;
       p[2 * j + 1] = q.y;
     }
   };
-  if (a.eps >= EPS_FAST) update(update_fast);
-  else update(update_any);
+  const bool fast = a.eps >= EPS_FAST;
+  if (fast)
+    update([&](const float2& mh, int j) {
+      roots[j] = make_float2(sqrt_fast(v[j].x), sqrt_fast(v[j].y));
+      const float2 d = __ffma2_rn(roots[j], both(a.root_ibc2), both(a.eps));
+      return __fmul2_rn(mh, make_float2(rcp_fast(d.x), rcp_fast(d.y)));
+    });
+  else
+    update([&](const float2& mh, int j) {
+      const float2 vh = __fmul2_rn(v[j], both(a.ibc2));
+      return make_float2(mh.x / (sqrtf(vh.x) + a.eps), mh.y / (sqrtf(vh.y) + a.eps));
+    });
   if (MASTER) set(t.master, b.at, wide, b.left, p);
   set(reinterpret_cast<P*>(t.p), b.at, wide, b.left, p);
   if constexpr (BITS == 32) {
@@ -350,13 +357,19 @@ __device__ __forceinline__ void step_block(const BlockIn<P, G, MASTER, BITS>& in
 #pragma unroll
     for (int j = 0; j < 4; ++j)
       x[j] = __fmul2_rn(make_float2(fabsf(m[j].x), fabsf(m[j].y)), both(im));
-    codes_of<1>(x, m, q);
+    codes_of<1>(x, m, [&](int j) { return x[j]; }, q);
     uint2 c = pack_codes(q);
     if (isnan(tm)) c = make_uint2(0u, 0u);
     set_codes(reinterpret_cast<uint8_t*>(t.m), b.at, wide, b.left, c);
 #pragma unroll
     for (int j = 0; j < 4; ++j) x[j] = __fmul2_rn(v[j], both(iv));
-    codes_of<2>(x, m, q);
+    // v's roots are there; those of subnormal numbers, taken for 0, have code 0 next to 1e-26
+    if (fast && tv > 1e-26f) {
+      const float by = sqrt_fast(iv);
+      codes_of<2>(x, m, [&](int j) { return __fmul2_rn(roots[j], both(by)); }, q);
+    } else {
+      codes_of<2>(x, m, [&](int j) { return make_float2(sqrt_fast(x[j].x), sqrt_fast(x[j].y)); }, q);
+    }
     c = pack_codes(q);
     if (isnan(tv)) c = make_uint2(0u, 0u);
     set_codes(reinterpret_cast<uint8_t*>(t.v), b.at, wide, b.left, c);
@@ -367,9 +380,10 @@ __device__ __forceinline__ void step_block(const BlockIn<P, G, MASTER, BITS>& in
 
 // With 8-bit states a block's arithmetic takes as long as its data: each warp has those of
 // the next AW_STAGES - 1 blocks on their way into shared memory meanwhile.  (155 M bf16
-// parameters: 295 us, 380 with the next block's data in registers, 433 with none; the
-// arithmetic, some 55 instructions per element, bounds it there, memory bounds 134 M fp32
-// ones: 312 us, 2.1 GB.)
+// parameters: 295 us, 380 with the next block's data in registers, 433 with none; 287 since
+// the update and the codes share v's roots.  The arithmetic, some 55 instructions per
+// element, bounds it there: issue slots 72% busy, DRAM 61%; four CTAs on an SM, with spills,
+// gain 1% there and lose 2% in fp32.  Memory bounds 134 M fp32 ones: 310 us, 2.1 GB.)
 constexpr int AW_STAGES = 3;
 template <typename P, typename G, bool MASTER>
 struct Staged {

@@ -95,7 +95,7 @@ pr_status launch(pr_ctx* c, prk::AdamwArgs<N>& a, const Kernel& kern, cudaStream
 }
 
 struct Step {
-  float lr = 0.f, eps = 0.f, b1 = 0.f, c1 = 0.f, b2 = 0.f, c2 = 0.f, ibc1 = 0.f, ibc2 = 0.f;
+  float lr = 0.f, eps = 0.f, b1 = 0.f, c1 = 0.f, b2 = 0.f, c2 = 0.f, ibc1 = 0.f, ibc2 = 0.f, root_ibc2 = 0.f;
   const float* grad_scale = nullptr;
   float *m_out = nullptr, *v_out = nullptr;
 };
@@ -115,6 +115,7 @@ pr_status run_kind(pr_ctx* c, const pr_adamw_tensor* t, int32_t n_tensors, int k
   a.c2 = step.c2;
   a.ibc1 = step.ibc1;
   a.ibc2 = step.ibc2;
+  a.root_ibc2 = step.root_ibc2;
   a.one = 1.f;
   a.grad_scale = step.grad_scale;
   a.m_out = step.m_out;
@@ -222,6 +223,7 @@ pr_status pr_adamw_step(pr_ctx* c, const pr_adamw_tensor* tensors, int32_t n_ten
   a.c2 = (float)(1.0 - beta2);
   a.ibc1 = (float)(1.0 / (1.0 - std::pow(beta1, (double)step)));
   a.ibc2 = (float)(1.0 / (1.0 - std::pow(beta2, (double)step)));
+  a.root_ibc2 = (float)std::sqrt(1.0 / (1.0 - std::pow(beta2, (double)step)));
   a.grad_scale = grad_scale;
   return run(c, tensors, n_tensors, a, false, s);
 }

@@ -323,3 +323,29 @@ def test_refusals(B, ctx):
         assert err.value.status == B.PR_ERR_INVALID_ARG
     B.pr_adamw_step(ctx, B.pr_adamw_tensors([], [], [], []), **HYPER)
     assert B.launch_count() == n0
+
+
+@pytest.mark.parametrize("eps", [1e-8, 1e-30])
+@pytest.mark.parametrize("scale", [1.0, 1e-10, 1e-12, 3e-13, 1e-13, 3e-14, 1e-15, 1e-17, 1e-18])
+def test_codes_of_tiny_second_moments(B, ctx, scale, eps):
+    """First steps whose squares go down to the subnormal numbers: v is (1 - beta2) g^2 in two
+    rounded products, its code the nearest one.  An IEEE reciprocal, a product and two
+    roots put 255 x 2^-22 = 6e-5 onto a code: 1e-4."""
+    n = 40 * 256 + 77
+    g = torch.Generator(device="cuda").manual_seed(11)
+    grad = torch.randn(n, generator=g, device="cuda") * scale
+    p = torch.randn(n, generator=g, device="cuda")
+    m, v = torch.zeros(n, dtype=torch.int8, device="cuda"), torch.zeros(n, dtype=torch.uint8, device="cuda")
+    blocks = -(-n // 256)
+    ms, vs = torch.zeros(blocks, device="cuda"), torch.zeros(blocks, device="cuda")
+    t = B.pr_adamw_tensors([p], [grad], [m], [v], m_scale=[ms], v_scale=[vs])
+    B.pr_adamw_step(ctx, t, 1e-2, beta1=0.9, beta2=0.95, eps=eps, step=1)
+    x = grad.cpu().numpy()
+    want = (np.float32(1.0 - 0.95) * (x * x)).astype(np.float64)
+    top = np.maximum.reduceat(want, np.arange(0, n, 256))
+    top = np.where(top < 2.0 ** -126, 0.0, top)
+    assert (f64(vs) == top).all()
+    per = np.repeat(top, 256)[:n]
+    u = np.where(per > 0, 255.0 * (want / np.where(per > 0, per, 1.0)) ** 0.25, 0.0)
+    off = np.abs(f64(v) - u)
+    assert (off <= 0.5 + 1e-4).all(), (off.max(), x[off.argmax()])
