@@ -625,7 +625,7 @@ constexpr int RG_TERMS = 5;  // statistics that are summed row by row
 
 // A row's end from its sums: R against 2^k, or against its maximum M where that is not
 // infinite.  Writes logp, the statistics' terms (weight wt), and the result: to `out`,
-// whose barrier learns of it first, else the row's state.  Whole warp; apart from the
+// whose barrier (where there is one) learns of it first, else the row's state.  Whole warp; apart from the
 // kernel's registers.
 template <bool PREF>
 __device__ __noinline__ void end_math(const LossArgs& a, int64_t row, const RowIn in, float k,
@@ -666,7 +666,7 @@ __device__ __noinline__ void end_math(const LossArgs& a, int64_t row, const RowI
   }
   if (out && lane == 0) {
     *out = row_out(st, kk);
-    bar_arrive(out_bar);
+    if (out_bar) bar_arrive(out_bar);
   }
   if (!PREF && lane < RG_TERMS) {
     const float x = wt * (lane == 0 ? p.surrogate : lane == 1 ? p.kl : lane == 2 ? p.ratio
@@ -780,12 +780,17 @@ __device__ __forceinline__ void add_words(float& k, float2& S, const uint4 (&v)[
   }
 }
 
-// The statistics: a warp's sums over its rows to a.part[at], the last of `count` warps
-// joins all in order.  Whole warp.
-__device__ __forceinline__ void write_stats(const LossArgs& a, const float2* stat, int64_t at,
-                                            int64_t count, int lane) {
+// The statistics: a CTA's sums (of `warps` warps' rows) to a.part[at], the last of `count`
+// CTAs joins all in order.  Whole warp.
+__device__ __forceinline__ void write_stats(const LossArgs& a, const float2* stat, int warps,
+                                            int64_t at, int64_t count, int lane) {
   int last = 0;
-  if (lane < RG_TERMS) a.part[at * RG_TERMS + lane] = (double)stat[lane].x + (double)stat[lane].y;
+  if (lane < RG_TERMS) {
+    double v = 0.;
+    for (int w = 0; w < warps; ++w)
+      v += (double)stat[w * RG_TERMS + lane].x + (double)stat[w * RG_TERMS + lane].y;
+    a.part[at * RG_TERMS + lane] = v;
+  }
   __syncwarp();
   if (lane == 0) {
     __threadfence();
@@ -962,7 +967,7 @@ __global__ void __launch_bounds__(FW_NT, FW_CTAS) loss_forward(const __grid_cons
     for (uint32_t q = n >= 2 ? n - 2 : 0; q < n; ++q) named_bar_sync(BAR_EMPTY + (q & 1), FW_NT);
   }
   __syncthreads();
-  if (!PREF && warp == 0) write_stats(a, sm.stat, b, G, lane);
+  if (!PREF && warp == 0) write_stats(a, sm.stat, 1, b, G, lane);
 }
 
 // ---- forward and backward in one pass -----------------------------------------------------
@@ -973,7 +978,7 @@ __global__ void __launch_bounds__(FW_NT, FW_CTAS) loss_forward(const __grid_cons
 // between the two sweeps, so that the logits are read from memory once, and the ring's
 // other places take the next row's chunks meanwhile.  The row's end (the warps' sums
 // joined, those of a cluster's CTAs through distributed shared memory, the elements
-// before and after the row's 16-byte words, l and dL/dl) is a chain of some 2,000 cycles:
+// before and after the row's 16-byte words, l and dL/dl) is a chain of 3,000 to 5,000 cycles:
 // two CTAs share an SM where half its shared memory holds a part, and one streams
 // while the other waits.
 constexpr int RG_NW = 8;                       // warps that sum and write
@@ -1031,9 +1036,13 @@ __device__ __forceinline__ float2 exchange(float2* to, uint64_t* bar, uint32_t p
 
 
 // (OWN as an argument: 2.5% of the time of 8,657 rows of V = 151,936 bf16.)
+//
+// lag 1: a row's gradient is written when the next row has been summed, so that its end is
+// worked out meanwhile; the ring has to hold both (30,400 rows of V = 24,576 bf16: 465 us for
+// 510, V = 12,480: 352 for 410).  For one CTA to a row: a cluster's would need more slots.
 template <typename T, bool HOLD, bool OWN>
 __global__ void __launch_bounds__(RG_NT, 2)
-    loss_ring(const __grid_constant__ LossArgs a, const int places) {
+    loss_ring(const __grid_constant__ LossArgs a, const int places, const int lag) {
   extern __shared__ __align__(16) unsigned char smem_raw[];
   RingCtl& sm = *reinterpret_cast<RingCtl*>(smem_raw);
   using Tr = Traits<T>;
@@ -1171,66 +1180,73 @@ __global__ void __launch_bounds__(RG_NT, 2)
     }
   } else {
     // ---- the rows' words
-    uint32_t n = 0;  // rows
+    uint32_t n = 0, m = 0;  // rows summed; written
+    const uint32_t mine = first < live ? (uint32_t)((live - 1 - first) / G) + 1u : 0u;
     if (C > 1) named_bar_sync(BAR_IN, 32 * (RG_NW + 1));
     const int at = warp * 32 + lane;  // this lane's first word of a chunk
-    int4 ref = ref_of(first);
-    for (int64_t i = first; i < live; i += G) {
-      const int4 ref1 = ref_of(i + G);
-      const int32_t y = ref.z;
-      const Share sh = share_of<T>(a, ref.x, C, rank);
-      T* const g = reinterpret_cast<T*>(a.grad) + ref.x * a.grad_stride + sh.head;
-      const bool vec = ((reinterpret_cast<uintptr_t>(sh.x + sizeof(T) * sh.head) ^
-                         reinterpret_cast<uintptr_t>(g)) & 15u) == 0;
-      const int32_t yw = word_of<T>(a, sh, y);
-      const int yj = y - sh.head - yw * Tr::VEC;
-      // forward
-      const int place0 = place;
-      const uint32_t turn0 = turn;
-      float k = -3e38f;
-      float2 S = make_float2(0.f, 0.f);
-      for (int32_t w = sh.w0; w < sh.w1; w += RG_CHUNK) {
-        wait(&sm.full[place], turn);
-        const uint4* st = reinterpret_cast<const uint4*>(ring + (size_t)place * RG_BYTES) + at;
-        uint4 v[RG_W];
-#pragma unroll
-        for (int q = 0; q < RG_W; ++q) v[q] = st[32 * RG_NW * q];
-        if (w + RG_CHUNK > sh.w1) {
-#pragma unroll
-          for (int q = 0; q < RG_W; ++q)
-            if (w + 32 * RG_NW * q + at >= sh.w1)
-              v[q] = make_uint4(Tr::NEG_WORD, Tr::NEG_WORD, Tr::NEG_WORD, Tr::NEG_WORD);
-        }
-        if ((uint32_t)(yw - w) < (uint32_t)RG_CHUNK) {
-#pragma unroll
-          for (int q = 0; q < RG_W; ++q)
-            if (w + 32 * RG_NW * q + at == yw) v[q] = without<T>(v[q], yj);
-        }
-        if (!HOLD) {
-          __syncwarp();  // every lane has its words
-          if (lane == 0) bar_arrive(&sm.empty[place]);
-        }
-        step();
-        add_words<T>(k, S, v, a.c2, w == sh.w0);
-      }
-      float R;
-      join(make_float2(k, S.x + S.y), 1.f, k, R);
-      const int s = n % RG_SLOTS;
-      if (!HOLD && n >= 1) wait(&sm.out_bar[s ^ 1], ((n - 1) / RG_SLOTS) & 1u);
-      if (C > 1) {
-        send(sums + (s * C + rank) * RG_NW + warp, &sm.sum_bar[s], k, R, C, lane);
-      } else if (lane == 0) {
-        sums[s * RG_NW + warp] = make_float2(k, R);
-        bar_arrive(&sm.sum_bar[s]);
-      }
-      if (HOLD) {
-        // backward
-        wait(&sm.out_bar[s], (n / RG_SLOTS) & 1u);
-        const RowOut o = sm.out[s];
-        place = place0;
-        turn = turn0;
+    int4 ref = ref_of(first), next = ref_of(first + G);  // the row to be summed; the one after it
+    int4 held = ref, last = ref;  // the row to be written; the one summed last
+    int place0 = 0;               // its place
+    while ((HOLD ? m : n) < mine) {
+      if (n < mine) {
+        // forward
+        const Share sh = share_of<T>(a, ref.x, C, rank);
+        const int32_t yw = word_of<T>(a, sh, ref.z);
+        const int yj = ref.z - sh.head - yw * Tr::VEC;
+        float k = -3e38f;
+        float2 S = make_float2(0.f, 0.f);
         for (int32_t w = sh.w0; w < sh.w1; w += RG_CHUNK) {
+          wait(&sm.full[place], turn);
           const uint4* st = reinterpret_cast<const uint4*>(ring + (size_t)place * RG_BYTES) + at;
+          uint4 v[RG_W];
+#pragma unroll
+          for (int q = 0; q < RG_W; ++q) v[q] = st[32 * RG_NW * q];
+          if (w + RG_CHUNK > sh.w1) {
+#pragma unroll
+            for (int q = 0; q < RG_W; ++q)
+              if (w + 32 * RG_NW * q + at >= sh.w1)
+                v[q] = make_uint4(Tr::NEG_WORD, Tr::NEG_WORD, Tr::NEG_WORD, Tr::NEG_WORD);
+          }
+          if ((uint32_t)(yw - w) < (uint32_t)RG_CHUNK) {
+#pragma unroll
+            for (int q = 0; q < RG_W; ++q)
+              if (w + 32 * RG_NW * q + at == yw) v[q] = without<T>(v[q], yj);
+          }
+          if (!HOLD) {
+            __syncwarp();  // every lane has its words
+            if (lane == 0) bar_arrive(&sm.empty[place]);
+          }
+          step();
+          add_words<T>(k, S, v, a.c2, w == sh.w0);
+        }
+        float R;
+        join(make_float2(k, S.x + S.y), 1.f, k, R);
+        const int s = n % RG_SLOTS;
+        if (!HOLD && n >= 1) wait(&sm.out_bar[s ^ 1], ((n - 1) / RG_SLOTS) & 1u);
+        if (C > 1) {
+          send(sums + (s * C + rank) * RG_NW + warp, &sm.sum_bar[s], k, R, C, lane);
+        } else if (lane == 0) {
+          sums[s * RG_NW + warp] = make_float2(k, R);
+          bar_arrive(&sm.sum_bar[s]);
+        }
+        last = ref;
+        ++n;
+        ref = next;
+        next = ref_of(first + (int64_t)(n + 1) * G);
+      }
+      if (HOLD && (n > (uint32_t)lag || n == mine)) {
+        // backward
+        const Share sh = share_of<T>(a, held.x, C, rank);
+        T* const g = reinterpret_cast<T*>(a.grad) + held.x * a.grad_stride + sh.head;
+        const bool vec = ((reinterpret_cast<uintptr_t>(sh.x + sizeof(T) * sh.head) ^
+                           reinterpret_cast<uintptr_t>(g)) & 15u) == 0;
+        const int32_t yw = word_of<T>(a, sh, held.z);
+        const int yj = held.z - sh.head - yw * Tr::VEC;
+        const int s = m % RG_SLOTS;
+        wait(&sm.out_bar[s], (m / RG_SLOTS) & 1u);
+        const RowOut o = sm.out[s];
+        for (int32_t w = sh.w0; w < sh.w1; w += RG_CHUNK) {
+          const uint4* st = reinterpret_cast<const uint4*>(ring + (size_t)place0 * RG_BYTES) + at;
           T* const to = g + (int64_t)(w + at) * Tr::VEC;
           uint4 v[RG_W];
 #pragma unroll
@@ -1246,8 +1262,8 @@ __global__ void __launch_bounds__(RG_NT, 2)
             for (int q = 0; q < RG_W; ++q) v[q] = make_uint4(0u, 0u, 0u, 0u);
           }
           __syncwarp();
-          if (lane == 0) bar_arrive(&sm.empty[place]);
-          step();
+          if (lane == 0) bar_arrive(&sm.empty[place0]);
+          if (++place0 == places) place0 = 0;
           if (vec && w + RG_CHUNK <= sh.w1) {
 #pragma unroll
             for (int q = 0; q < RG_W; ++q)
@@ -1260,9 +1276,9 @@ __global__ void __launch_bounds__(RG_NT, 2)
           if ((uint32_t)(yw - w) < (uint32_t)RG_CHUNK && ((yw - w) % (32 * RG_NW)) == at)
             put(g + (int64_t)yw * Tr::VEC + yj, o.gy);
         }
+        ++m;
+        held = m == n ? ref : last;
       }
-      ++n;
-      ref = ref1;
     }
     if (HOLD)  // the rows that do not count
       for (int64_t i = first; i < a.n_rows - live; i += G) {
@@ -1279,7 +1295,132 @@ __global__ void __launch_bounds__(RG_NT, 2)
   __syncthreads();
   if (C > 1) cluster_sync_all();  // no peer writes here any more
   const int64_t groups = max((int64_t)1, min(G, (int64_t)live));
-  if (warp == 0 && rank == 0 && first < groups) write_stats(a, sm.stat, first, groups, lane);
+  if (warp == 0 && rank == 0 && first < groups) write_stats(a, sm.stat, 1, first, groups, lane);
+}
+
+// ---- short rows: one to a warp ---------------------------------------------------------------
+//
+// A row's end is some 500 instructions one after the other, 2,600 to 4,400 cycles of a warp.
+// Where a row is short that is longer than its data take, so each warp has a row of its
+// own, brought into its part of shared memory by one bulk copy: up to 32 rows of an SM are
+// in work at a time, some of them on their way while others are summed, ended or written.
+// (30,400 rows of V = 5,504 bf16 with their gradient: 143 us for
+// 317 with a CTA to a row; V = 512: 53 for 301; of 25 KB, four to a CTA: 405 for 440 there, but
+// 65 for 57 with 2,500 rows.)
+constexpr int RW_MOST = 16;  // warps of a CTA; two CTAs on an SM
+struct RowsCtl {
+  uint64_t full[RW_MOST];    // a row has landed
+  RowOut out[RW_MOST];
+  float2 stat[RW_MOST * RG_TERMS];
+};
+constexpr size_t RW_CTL = (sizeof(RowsCtl) + 15) / 16 * 16;
+
+template <typename T, bool PREF, bool HOLD>
+__global__ void __launch_bounds__(32 * RW_MOST, 2)
+    loss_rows(const __grid_constant__ LossArgs a, const int bytes) {  // of a warp's part
+  extern __shared__ __align__(16) unsigned char smem_raw[];
+  RowsCtl& sm = *reinterpret_cast<RowsCtl*>(smem_raw);
+  using Tr = Traits<T>;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+  unsigned char* const part = smem_raw + RW_CTL + (size_t)warp * bytes;
+  uint64_t* const full = &sm.full[warp];
+  float2* const stat = sm.stat + warp * RG_TERMS;
+  if (lane == 0) {
+    bar_init(full, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (lane < RG_TERMS) stat[lane] = make_float2(0.f, 0.f);
+  __syncthreads();
+  pdl_wait();
+  pdl_trigger();
+  const Rows rows{nullptr, (int32_t)__ldcg(a.totals)};
+  const double share = PREF ? 0.0 : rows.share(a);
+  const int64_t G = (int64_t)gridDim.x * warps, first = (int64_t)warp * gridDim.x + blockIdx.x;
+  uint32_t phase = 0;
+  int4 ref = rows.at(a, first);
+  for (int64_t i = first; i < rows.live; i += G) {
+    const Share sh = share_of<T>(a, ref.x, 1, 0);
+    if (lane == 0) {
+      const uint32_t n = 16u * (uint32_t)sh.words;
+      bar_expect(full, n);
+      if (n > 0)
+        asm volatile(
+            "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::
+                "r"(sm_addr(part)),
+            "l"(sh.x + sizeof(T) * sh.head), "r"(n), "r"(sm_addr(full))
+            : "memory");
+    }
+    const RowIn in = fetch_row<T, PREF>(a, rows, sh, ref, lane);
+    const int4 ref1 = rows.at(a, i + G);
+    const int32_t yw = word_of<T>(a, sh, in.y);
+    const int yj = in.y - sh.head - yw * Tr::VEC;
+    if (!ring_wait(sm_addr(full), phase, a.ctx_flags)) {
+      ring_wait(sm_addr(full), phase, a.ctx_flags);  // no copy may be in flight at the end
+      break;
+    }
+    phase ^= 1u;
+    __syncwarp();
+    const uint4* const st = reinterpret_cast<const uint4*>(part) + lane;
+    float k = -3e38f, R, M = INFINITY;
+    float2 S = make_float2(0.f, 0.f);
+    for (int32_t w = 0; w < sh.words; w += 32 * RG_W) {
+      uint4 v[RG_W];
+#pragma unroll
+      for (int q = 0; q < RG_W; ++q)
+        v[q] = w + 32 * q + lane < sh.words
+                   ? st[w + 32 * q]
+                   : make_uint4(Tr::NEG_WORD, Tr::NEG_WORD, Tr::NEG_WORD, Tr::NEG_WORD);
+      if ((uint32_t)(yw - w) < 32u * RG_W) {
+#pragma unroll
+        for (int q = 0; q < RG_W; ++q)
+          if (w + 32 * q + lane == yw) v[q] = without<T>(v[q], yj);
+      }
+      add_words<T>(k, S, v, a.c2, w == 0);
+    }
+    join(make_float2(k, S.x + S.y), 1.f, k, R);
+    add_ends(a, sh, in, k, R, lane);
+    if (sum_again(k, R, in.xy, a.c2)) {
+      robust_sum<T>(a, sh, true, in.y, M, R, lane);
+      raise_to(a, in.xy, M, R);
+    }
+    const float wt = PREF ? 0.f : (float)(a.norm ? share / (double)in.count : share);
+    end_math<PREF>(a, ref.x, in, k, R, M, wt, true, HOLD ? &sm.out[warp] : nullptr, nullptr, stat,
+                   lane);
+    __syncwarp();
+    if (HOLD) {
+      const RowOut o = sm.out[warp];
+      T* const g = reinterpret_cast<T*>(a.grad) + (int64_t)ref.x * a.grad_stride;
+      T* const gw = g + sh.head;
+      const bool vec = ((reinterpret_cast<uintptr_t>(sh.x) ^ reinterpret_cast<uintptr_t>(g)) & 15u) == 0;
+      for (int32_t w = lane; w < sh.words; w += 32) {
+        uint4 v = make_uint4(0u, 0u, 0u, 0u);
+        if (o.mode == ROW_FAST) v = grad_word<T, false>(o, a.c2, st[w - lane]);
+        else if (o.mode == ROW_ROBUST) v = grad_word<T, true>(o, a.c2, st[w - lane]);
+        put_word(gw + (int64_t)w * Tr::VEC, v, vec);
+        if (w == yw) put(gw + (int64_t)w * Tr::VEC + yj, o.gy);
+      }
+      const int32_t v = end_of(a, sh, lane);
+      if (v >= 0) put(g + v, v == in.y ? o.gy : grad1(o, a.c2, in.edge));
+      __syncwarp();  // every lane has read what the next row is written over
+    }
+    ref = ref1;
+  }
+  if (HOLD)  // the rows that do not count
+    for (int64_t i = first; i < a.n_rows - rows.live; i += G) {
+      const int64_t row = rows.skipped(a, i);
+      const Share sh = share_of<T>(a, row, 1, 0);
+      T* const g = reinterpret_cast<T*>(a.grad) + row * a.grad_stride;
+      const bool vec = ((reinterpret_cast<uintptr_t>(sh.x) ^ reinterpret_cast<uintptr_t>(g)) & 15u) == 0;
+      for (int32_t w = lane; w < sh.words; w += 32)
+        put_word(g + sh.head + (int64_t)w * Tr::VEC, make_uint4(0u, 0u, 0u, 0u), vec);
+      const int32_t v = end_of(a, sh, lane);
+      if (v >= 0) put(g + v, 0.f);
+    }
+  if (PREF) return;
+  __syncthreads();
+  const int64_t groups = max((int64_t)1, min((int64_t)gridDim.x, (int64_t)rows.live));
+  if (warp == 0 && blockIdx.x < groups) write_stats(a, sm.stat, warps, blockIdx.x, groups, lane);
 }
 
 // ---- backward from the rows' states ---------------------------------------------------------

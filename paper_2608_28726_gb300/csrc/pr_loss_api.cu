@@ -148,6 +148,21 @@ const void* forward_kernel(bool pref) {
               : reinterpret_cast<const void*>(&prk::loss_forward<T, false>);
 }
 
+template <typename T>
+const void* rows_kernel(bool pref, bool hold) {
+  return pref   ? reinterpret_cast<const void*>(&prk::loss_rows<T, true, false>)
+         : hold ? reinterpret_cast<const void*>(&prk::loss_rows<T, false, true>)
+                : reinterpret_cast<const void*>(&prk::loss_rows<T, false, false>);
+}
+
+const void* rows_kernel(pr_dtype dt, bool pref, bool hold) {
+  return dt == PR_DTYPE_BF16 ? rows_kernel<__nv_bfloat16>(pref, hold)
+                             : rows_kernel<float>(pref, hold);
+}
+
+// half of an SM's shared memory
+constexpr size_t HALF = prk::ring_start(4) + (size_t)prk::RG_FEW * prk::RG_BYTES;
+
 // shared memory opt-ins, and the clusters of 2, 4 and 8 CTAs that the GPU has room for
 // with half and with all of an SM's shared memory each; once per context
 pr_status ring_setup(pr_ctx* c) {
@@ -158,6 +173,10 @@ pr_status ring_setup(pr_ctx* c) {
         PR_CUDA(cudaFuncSetAttribute(ring_kernel(dt, hold, own),
                                      cudaFuncAttributeMaxDynamicSharedMemorySize,
                                      (int)ring_bytes(prk::RG_MOST, 8, false)));
+  for (pr_dtype dt : {PR_DTYPE_F32, PR_DTYPE_BF16})
+    for (int kind = 0; kind < 3; ++kind)
+      PR_CUDA(cudaFuncSetAttribute(rows_kernel(dt, kind == 2, kind == 1),
+                                   cudaFuncAttributeMaxDynamicSharedMemorySize, (int)HALF));
   for (int i = 0; i < 4; ++i)
     for (int whole = 0; whole < 2; ++whole) {
       if (i == 0) {
@@ -187,6 +206,7 @@ pr_status ring_setup(pr_ctx* c) {
 // The one-pass kernel's launch: 2^split CTAs per row, `places` chunks in a CTA's ring.
 struct RingShape {
   int split, places;
+  int here;         // chunks of a row's part
   bool hold;        // a row's chunks fit the cluster's rings
   bool spare;       // and leave a place free
   bool full;        // every place is taken
@@ -219,9 +239,9 @@ RingShape choose_ring(const pr_ctx* c, pr_dtype dt, int64_t n_rows, int64_t voca
       }
     }
   const int64_t at_once = c->loss_places[s.places == prk::RG_MOST][s.split];
-  const int64_t here = (chunks + (1 << s.split) - 1) >> s.split;
-  s.hold = here <= s.places;
-  s.spare = here < s.places;
+  s.here = (int)std::min<int64_t>((chunks + (1 << s.split) - 1) >> s.split, prk::RG_MOST + 1);
+  s.hold = s.here <= s.places;
+  s.spare = s.here < s.places;
   s.groups = std::min<int64_t>(n_rows, at_once);
   s.full = n_rows >= at_once;
   return s;
@@ -249,13 +269,33 @@ pr_status launch_plan(pr_ctx* c, prk::LossArgs& a, int pairs, cudaStream_t s) {
 pr_status launch_ring(pr_ctx* c, prk::LossArgs& a, pr_dtype dt, const RingShape& shape, bool hold,
                       cudaStream_t s) {
   int places = shape.places - (a.own ? 1 : 0);  // (the rows' list takes one)
-  void* args[] = {&a, &places};
+  int lag = shape.split == 0 && 2 * shape.here + 1 <= places ? 1 : 0;
+  void* args[] = {&a, &places, &lag};
   // A grid that takes every place is not set up early: clusters placed around the CTAs
   // of the launch before do not all find one, and the last run alone (8,847 rows of V =
   // 151,936 bf16 back to back: 1,538 us, 890 set up after it).
   const pr_status st = launch(ring_kernel(dt, hold, a.own), (unsigned)(shape.groups << shape.split),
                               prk::RG_NT, ring_bytes(places, 1 << shape.split, a.own), 1u << shape.split, args, s,
                               !shape.full);
+  return st == PR_OK ? timing_mark(c, s) : st;
+}
+
+// Warps of a CTA of loss_rows, or 0 where the other kernels take less time: rows of which
+// fewer than ten fit an SM, or no more than two for a CTA.
+int rows_warps(const pr_ctx* c, const prk::LossArgs& a, pr_dtype dt) {
+  if (a.own || a.n_rows <= 4 * c->num_sms) return 0;
+  const int64_t part = std::max<int64_t>(16, a.vocab * (int64_t)esize(dt) / 16 * 16);
+  const int64_t w = std::min<int64_t>(prk::RW_MOST, ((int64_t)HALF - (int64_t)prk::RW_CTL) / part);
+  return w >= 5 ? (int)w : 0;
+}
+
+pr_status launch_rows(pr_ctx* c, prk::LossArgs& a, pr_dtype dt, int warps, bool pref, bool hold,
+                      cudaStream_t s) {
+  int part = (int)std::max<int64_t>(16, a.vocab * (int64_t)esize(dt) / 16 * 16);
+  void* args[] = {&a, &part};
+  const pr_status st = launch(rows_kernel(dt, pref, hold),
+                              (unsigned)std::min<int64_t>(2 * c->num_sms, a.n_rows), 32u * warps,
+                              prk::RW_CTL + (size_t)warps * part, 1, args, s);
   return st == PR_OK ? timing_mark(c, s) : st;
 }
 
@@ -350,6 +390,8 @@ pr_status pr_policy_loss(pr_ctx* c, const void* logits, pr_dtype dt, int64_t n_r
   a.own = own_list(a) && (!ring.hold || ring.spare);
   if ((st = timing_begin(c, s)) != PR_OK) return st;
   if ((st = launch_plan(c, a, 0, s)) != PR_OK) return st;
+  if (const int warps = rows_warps(c, a, dt))
+    return launch_rows(c, a, dt, warps, false, grad != nullptr, s);
   if (ring.hold) return launch_ring(c, a, dt, ring, grad != nullptr, s);
   // rows of more than eight SMs' shared memory
   if ((st = launch_forward(c, a, dt, false, s)) != PR_OK) return st;
@@ -385,11 +427,14 @@ pr_status pr_preference_loss(pr_ctx* c, const void* logits, pr_dtype dt, int64_t
   a.margin = p->margin;
   a.loss = p->loss;
   a.length_norm = p->length_norm ? 1 : 0;
+  if ((st = ring_setup(c)) != PR_OK) return st;
   if ((st = workspace(c, a, 0, true, true)) != PR_OK) return st;
   a.own = own_list(a);
   if ((st = timing_begin(c, s)) != PR_OK) return st;
   if ((st = launch_plan(c, a, 1, s)) != PR_OK) return st;
-  if (n_rows > 0 && (st = launch_forward(c, a, dt, true, s)) != PR_OK)
+  const int warps = rows_warps(c, a, dt);
+  if (n_rows > 0 && (st = warps ? launch_rows(c, a, dt, warps, true, false, s)
+                                : launch_forward(c, a, dt, true, s)) != PR_OK)
     return st;
   void* args[] = {&a};
   if ((st = launch(reinterpret_cast<const void*>(&prk::loss_pairs), 

@@ -539,3 +539,81 @@ def test_how_rows_are_listed(B, ctx, n, n_req, keep):
     assert torch.equal(l2[:n], logp) and torch.equal(g2[:n], grad) and torch.equal(s2, stats)
     assert torch.equal(r2[:len(r)], ratio) and not r2[len(r):].any()
     assert not l2[n:].any() and not g2[n:].any()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V,stride,start", [(1, 1, 0), (7, 9, 3), (515, 515, 0), (3001, 3003, 1),
+                                            (3536, 3536, 0), (5504, 5504, 0), (5653, 5660, 5),
+                                            (9000, 9008, 8), (11400, 11400, 0), (12474, 12474, 2)])
+def test_many_short_rows(B, ctx, V, stride, start, dtype):
+    """More rows than the CTAs have places, of lengths that give a warp, a CTA or several
+    CTAs to a row, at any alignment, some of them odd; the gradient in place too.
+
+    Gradients: check_rows' bounds, and what an error of 3e-7 (1 + |l|) in l does to the two
+    terms of the slope, which may cancel or be small by themselves."""
+    n = 1300 if V < 6000 else 700
+    g, x, x64, ch, old, ref = draw(V, n, V, dtype)
+    off = offsets_of(g, n, 8)
+    mask = (g.random(n) < 0.9).astype(np.uint8)
+    odd = {3: np.nan, 5: np.inf, 8: -np.inf, 11: float(torch.finfo(x.dtype).min)}
+    for t, v in odd.items():
+        x[t] = v
+        x64[t] = v
+        mask[t] = t == 11  # (a row of the lowest value counts, the others must not be seen)
+    if V > 7:
+        x[14, : V // 2] = -torch.inf
+        x64[14, : V // 2] = -np.inf
+        ch[14] = V - 1
+    l64, p64 = L.rows(x64, ch, 1.0)
+    for t in (11, 14):
+        old[t], ref[t] = l64[t] - 0.1, l64[t] + 0.1
+    ch[3:9:5] = -1  # (ids of masked rows are not looked at)
+    adv = g.normal(size=n).astype(np.float32)
+    kw = dict(kl_coef=0.1, grad_scale=2.0)
+
+    buf = torch.zeros(start + n * stride + 16, dtype=x.dtype, device="cuda")
+    xs = buf[start:start + n * stride].view(n, stride)[:, :V]
+    xs.copy_(x)
+    B.pr_ctx_flags(ctx, clear=True)
+    args = dict(old_logp=to(old), ref_logp=to(ref), mask=to(mask), offsets=to(off))
+    stats, logp, grad = B.pr_policy_loss(ctx, xs, to(ch), to(adv), norm=1, **args, **kw)
+    s, l, gr = L.policy(x64, ch, adv, old, ref, mask, off, requests=True, clip_low=0.2,
+                        clip_high=0.2, **kw)
+    assert B.pr_ctx_flags(ctx, clear=True) & ~B.PR_FLAG_EMPTY_REQ == 0
+    check_rows(logp, l, None, None, dtype)
+    check_stats(stats, s, 2.0)
+    req = np.searchsorted(off, np.arange(n), side="right") - 1
+    count = np.array([mask[a:b].sum() for a, b in zip(off[:-1], off[1:])])
+    on = mask != 0
+    with np.errstate(invalid="ignore", over="ignore"):
+        share = 2.0 / (count > 0).sum() / np.maximum(count[req], 1)
+        terms = share * (0.1 * np.exp(ref - l64) + np.exp(l64 - old) * np.abs(adv))
+        one = np.zeros_like(p64)
+        one[np.arange(n)[on], ch[on]] = 1.0
+        slack = (terms * 3e-7 * (1.0 + np.abs(l64)))[:, None] * np.abs(one - p64)
+        rel = 2e-4 + (2.0 ** -8 if dtype == "bf16" else 0.0)
+        big = np.abs(gr).max(axis=1, keepdims=True)
+        ok = np.abs(f64(grad) - gr) <= rel * np.abs(gr) + 1e-6 * big + np.where(on[:, None], slack, 0.0)
+    assert ok.all(), ((~ok).sum(), np.argwhere(~ok)[:4])
+    assert not grad[torch.from_numpy(~on).cuda()].any()
+    st2, lp2, _ = B.pr_policy_loss(ctx, xs, to(ch), to(adv), norm=1, want_grad=False, **args, **kw)
+    assert torch.equal(st2, stats) and torch.equal(lp2, logp)
+
+    pk = dict(beta=0.3, loss=2, length_norm=True)
+    stats, ratio, logp2, pgrad = B.pr_preference_loss(ctx, xs, to(ch), to(off), ref_logp=to(ref),
+                                                      mask=to(mask), **pk)
+    s, r, l, pr = L.preference(x64, ch, off, ref, mask, **pk)
+    check_rows(logp2, l, pgrad, pr, dtype)
+    assert (np.abs(f64(ratio) - r) <= 2e-5 * np.maximum(np.diff(off), 1) + 1e-6 * np.abs(r)).all()
+    check_stats(stats, s, np.abs(r).max() + 1.0)
+
+    after = buf.clone()
+    inplace = after[start:start + n * stride].view(n, stride)[:, :V]
+    B.pr_policy_loss(ctx, inplace, to(ch), to(adv), norm=1, grad=inplace, **args, **kw)
+    assert torch.equal(inplace, grad)
+    inplace.copy_(xs)
+    assert torch.equal(after.nan_to_num(nan=7.0), buf.nan_to_num(nan=7.0))  # nothing between the rows
+
+
+def f64(t):
+    return t.double().cpu().numpy()
