@@ -1302,12 +1302,13 @@ __global__ void __launch_bounds__(RG_NT, 2)
 //
 // A row's end is some 500 instructions one after the other, 2,600 to 4,400 cycles of a warp.
 // Where a row is short that is longer than its data take, so each warp has a row of its
-// own, brought into its part of shared memory by one bulk copy: up to 32 rows of an SM are
+// own, brought into its part of shared memory by one bulk copy: up to 20 rows of an SM are
 // in work at a time, some of them on their way while others are summed, ended or written.
-// (30,400 rows of V = 5,504 bf16 with their gradient: 143 us for
-// 317 with a CTA to a row; V = 512: 53 for 301; of 25 KB, four to a CTA: 405 for 440 there, but
-// 65 for 57 with 2,500 rows.)
-constexpr int RW_MOST = 16;  // warps of a CTA; two CTAs on an SM
+// (30,400 rows of V = 5,504 bf16 with their gradient: 133 us for 317 with a CTA to a row,
+// 1,500 of them 27 for 33; V = 512: 51 for 301.  Rows of 25 KB, eight on an SM: 356 for 352 as
+// the ring does them now, 61 for 55 with 2,500.  More warps leave a warp fewer registers:
+// sixteen 143, unrolling the gradient's loop with them 188, twelve 145.)
+constexpr int RW_MOST = 10;  // warps of a CTA; two CTAs on an SM
 struct RowsCtl {
   uint64_t full[RW_MOST];    // a row has landed
   RowOut out[RW_MOST];
