@@ -112,8 +112,9 @@ typedef enum { PR_DTYPE_F32 = 0, PR_DTYPE_BF16 = 1 } pr_dtype;
                                 the preceding kernel starts (e.g. back-to-back verifier calls
                                 on resident logits).  Default 0. */
 #define PR_OPT_TIMING 4      /* 1: the calls after the verifier's (pr_head_score,
-                                pr_quantile_score, pr_selective_metrics, pr_lmhead_features)
-                                record a CUDA event after each kernel, for
+                                pr_quantile_score, pr_selective_metrics, pr_lmhead_features,
+                                the training losses, the optimiser step) record a CUDA
+                                event after each kernel, for
                                 pr_ctx_kernel_times; the kernels then no longer overlap one
                                 another.  Default 0. */
 
@@ -165,7 +166,9 @@ pr_status pr_last_error(pr_ctx* ctx, uint32_t* flags);
  * than the device has SMs), then the pool; for pr_selective_metrics the histogram of leading bits, the plan of
  * the buckets, their counts, their offsets, the scatter into them, the counts of
  * crowded ones (above 65,535 scores), the buckets' groups and the final
- * reduction.  Waits for the call's last event.  Writes min(count, cap) values to
+ * reduction; for the training losses the listing of the rows (one kernel, two for
+ * large batches, none for up to 512 rows), the pass over the logits, the answer pairs
+ * (preference loss) and a second pass where the gradient takes one.  Waits for the call's last event.  Writes min(count, cap) values to
  * `ms` and the count to *n (0 if no timed call was made).
  */
 pr_status pr_ctx_kernel_times(pr_ctx* ctx, float* ms, int32_t cap, int32_t* n);

@@ -247,8 +247,9 @@ static __global__ void __launch_bounds__(PL_BLOCK) loss_list(const LossArgs a) {
 }
 
 // The smallest batches: by every CTA of the kernel that reads the logits, in its shared
-// memory, without a launch before it; the first CTA leaves what later kernels need.  (20 rows
-// of V = 32,000 fp32: 24 us a call for 27 with a launch, 354 rows 28 for 30.)
+// memory, without a launch before it; the first CTA leaves what later kernels need.  (24 rows
+// of V = 32,000 fp32: 24 us a call for 27 with a launch; 285 rows of V = 151,936 bf16 28 for
+// 30.)
 constexpr int OWN_MOST = 512;  // rows, requests
 struct OwnPlan {
   int4 list[OWN_MOST];

@@ -272,7 +272,7 @@ pr_status launch_ring(pr_ctx* c, prk::LossArgs& a, pr_dtype dt, const RingShape&
   int lag = shape.split == 0 && 2 * shape.here + 1 <= places ? 1 : 0;
   void* args[] = {&a, &places, &lag};
   // A grid that takes every place is not set up early: clusters placed around the CTAs
-  // of the launch before do not all find one, and the last run alone (8,847 rows of V =
+  // of the launch before do not all find one, and the last run alone (8,657 rows of V =
   // 151,936 bf16 back to back: 1,538 us, 890 set up after it).
   const pr_status st = launch(ring_kernel(dt, hold, a.own), (unsigned)(shape.groups << shape.split),
                               prk::RG_NT, ring_bytes(places, 1 << shape.split, a.own), 1u << shape.split, args, s,
