@@ -339,28 +339,26 @@ __device__ __forceinline__ Rows rows_of(const LossArgs& a, bool own, OwnPlan* p,
 // ---- the losses of one row / pair -------------------------------------------------------
 
 struct PolicyTerms {
-  float loss, surrogate, kl, ratio, clipped, old_kl;
-  float slope;  // dloss / dl
+  float d, q, e;  // l - old, ref - l, e^q - 1
+  float surrogate, ratio, clipped;
+  float slope;    // dloss / dl
 };
 
 __device__ __forceinline__ PolicyTerms policy_terms(const LossArgs& a, float l, float l_lo,
                                                     float old, float ref, float adv) {
   PolicyTerms p;
-  const float d = a.old_logp ? (l - old) + l_lo : l - l;  // (NaN for a row without l)
-  p.ratio = expf(d);
-  p.old_kl = expm1f(d) - d;
+  p.d = a.old_logp ? (l - old) + l_lo : l - l;  // (NaN for a row without l)
+  p.ratio = expf(p.d);
   const float free = p.ratio * adv;
   const float bound = fminf(fmaxf(p.ratio, a.clip_lo), a.clip_hi) * adv;
   p.clipped = bound < free ? 1.f : 0.f;
   p.surrogate = bound < free ? bound : free;
   p.slope = bound < free ? 0.f : -free;
-  p.loss = -p.surrogate;
-  p.kl = 0.f;
+  p.q = p.e = 0.f;
   if (a.ref_logp) {
-    const float q = (ref - l) - l_lo, e = expm1f(q);
-    p.kl = e - q;
-    p.loss = fmaf(a.kl_coef, p.kl, p.loss);
-    if (a.kl_coef != 0.f) p.slope = fmaf(-a.kl_coef, e, p.slope);
+    p.q = (ref - l) - l_lo;
+    p.e = expm1f(p.q);
+    if (a.kl_coef != 0.f) p.slope = fmaf(-a.kl_coef, p.e, p.slope);
   }
   return p;
 }
@@ -670,8 +668,8 @@ __device__ __noinline__ void end_math(const LossArgs& a, int64_t row, const RowI
     if (out_bar) bar_arrive(out_bar);
   }
   if (!PREF && lane < RG_TERMS) {
-    const float x = wt * (lane == 0 ? p.surrogate : lane == 1 ? p.kl : lane == 2 ? p.ratio
-                                                : lane == 3 ? p.clipped : p.old_kl);
+    const float x = wt * (lane == 0 ? p.surrogate : lane == 1 ? p.e - p.q : lane == 2 ? p.ratio
+                                                : lane == 3 ? p.clipped : expm1f(p.d) - p.d);
     const float2 q = stat[lane];
     const float y = q.x + x, z = y - q.x;
     stat[lane] = make_float2(y, q.y + ((q.x - (y - z)) + (x - z)));
