@@ -349,3 +349,39 @@ def test_codes_of_tiny_second_moments(B, ctx, scale, eps):
     u = np.where(per > 0, 255.0 * (want / np.where(per > 0, per, 1.0)) ** 0.25, 0.0)
     off = np.abs(f64(v) - u)
     assert (off <= 0.5 + 1e-4).all(), (off.max(), x[off.argmax()])
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_tensor_past_32_bits(B, ctx, bits):
+    """Elements beyond the 2^31st take the step that the same elements take by themselves."""
+    n, tail = 2 ** 31 + 4096 + 77, 8192 + 77  # the tail begins with a block
+    f = torch.float32
+
+    def states(k):
+        if bits == 32:
+            return [torch.zeros(k, dtype=f, device="cuda") for _ in range(2)], None
+        blocks = -(-k // 256)
+        return ([torch.zeros(k, dtype=t, device="cuda") for t in (torch.int8, torch.uint8)],
+                [torch.zeros(blocks, device="cuda") for _ in range(2)])
+
+    g = torch.Generator(device="cuda").manual_seed(3)
+    p = torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    grad = torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    p[-tail:] = torch.randn(tail, generator=g, device="cuda").bfloat16()
+    grad[-tail:] = torch.randn(tail, generator=g, device="cuda").bfloat16()
+    few = [p[-tail:].clone(), grad[-tail:].clone()]
+    big_s, big_scale = states(n)
+    few_s, few_scale = states(tail)
+    for params, gr, (m, v), scale in ((p, grad, big_s, big_scale), (few[0], few[1], few_s, few_scale)):
+        t = B.pr_adamw_tensors([params], [gr], [m], [v], weight_decay=0.1,
+                               m_scale=[scale[0]] if scale else None,
+                               v_scale=[scale[1]] if scale else None)
+        for step in (1, 2):
+            B.pr_adamw_step(ctx, t, 1e-2, step=step)
+    assert torch.equal(p[-tail:], few[0])
+    assert not p[:-tail].any()
+    for a, b in zip(big_s, few_s):
+        assert torch.equal(a[-tail:], b) and not a[:-tail].any()
+    if bits == 8:
+        for a, b in zip(big_scale, few_scale):
+            assert torch.equal(a[-b.numel():], b) and not a[:-b.numel()].any()

@@ -617,3 +617,58 @@ def test_many_short_rows(B, ctx, V, stride, start, dtype):
 
 def f64(t):
     return t.double().cpu().numpy()
+
+
+@pytest.mark.parametrize("n", [40, 700, 5000])
+def test_bad_offsets_and_empty_batches_of_every_size(B, ctx, n):
+    """Bounds outside the batch and batches of masked rows, however the rows are listed."""
+    V = 40
+    g, x, x64, ch, old, ref = draw(n, n, V, "f32")
+    adv = g.normal(size=n).astype(np.float32)
+    B.pr_ctx_flags(ctx, clear=True)
+    for off, flag in (([n // 4, n // 2, n - 3], 0), ([0, n // 2, n + 2], B.PR_FLAG_BAD_OFFSETS),
+                      ([-3, n // 3, n], B.PR_FLAG_BAD_OFFSETS),
+                      ([0, n // 5, n // 5, n], B.PR_FLAG_EMPTY_REQ)):
+        for mask in (None, (g.random(n) < 0.7).astype(np.uint8)):
+            st, lp, gr = B.pr_policy_loss(ctx, x, to(ch), to(adv), old_logp=to(old), mask=to(mask),
+                                          offsets=to(off, np.int64), norm=1)
+            s, lo, go = L.policy(x64, ch, adv, old, None, mask, off, requests=True)
+            check_rows(lp, lo, gr, go, "f32")
+            check_stats(st, s, 1.0)
+            assert B.pr_ctx_flags(ctx, clear=True) == flag
+    off = [0, n // 4, n // 2, n // 2, n]
+    mask = np.zeros(n, np.uint8)
+    for k in range(2):
+        st, lp, gr = B.pr_policy_loss(ctx, x, to(ch), to(adv), mask=to(mask), norm=k,
+                                      offsets=to(off, np.int64))
+        assert not st.any() and not lp.any() and not gr.any()
+    st, r, lp, gr = B.pr_preference_loss(ctx, x, to(ch), to(off, np.int64), mask=to(mask))
+    assert not st.any() and not r.any() and not lp.any() and not gr.any()
+    # the second pair has one answer: its rows have l, and no gradient
+    st, r, lp, gr = B.pr_preference_loss(ctx, x, to(ch), to(off, np.int64), ref_logp=to(ref))
+    s, ro, lo, go = L.preference(x64, ch, off, ref)
+    check_rows(lp, lo, gr, go, "f32")
+    check_stats(st, s, 1.0 + np.abs(ro).max())
+    assert not gr[n // 2:].any() and gr[:n // 2].any()
+    B.pr_ctx_flags(ctx, clear=True)
+
+
+@pytest.mark.parametrize("n,stride", [(20, 2 ** 27 + 8), (700, 2 ** 22 + 24)])
+def test_rows_past_32_bits(B, ctx, n, stride):
+    """Rows that lie more than 2^31 elements apart give the bits of rows side by side."""
+    V = 1000
+    assert (n - 1) * stride > 2 ** 31
+    g, x, _, ch, old, ref = draw(17, n, V, "bf16")
+    off = offsets_of(g, n, 6)
+    buf = torch.empty((n - 1) * stride + V, dtype=x.dtype, device="cuda")
+    out = torch.empty_like(buf)
+    far, grad = buf.as_strided((n, V), (stride, 1)), out.as_strided((n, V), (stride, 1))
+    far.copy_(x)
+    want = B.pr_policy_loss(ctx, x, to(ch), to(old), ref_logp=to(ref), kl_coef=0.1)
+    got = B.pr_policy_loss(ctx, far, to(ch), to(old), ref_logp=to(ref), kl_coef=0.1, grad=grad)
+    for w, t in zip(want, got):
+        assert torch.equal(w, t)
+    want = B.pr_preference_loss(ctx, x, to(ch), to(off), ref_logp=to(ref))
+    got = B.pr_preference_loss(ctx, far, to(ch), to(off), ref_logp=to(ref), grad=grad)
+    for w, t in zip(want, got):
+        assert torch.equal(w, t)
