@@ -622,7 +622,8 @@ typedef struct {
  * call raises PR_FLAG_NONFINITE (context flag word).  The parameters step with the new
  * states before their rounding.
  * One launch per 384 tensors of the same types, no workspace.  Tensors whose pointers
- * are multiples of 32 bytes (16 for bf16, 8 for codes) are read and written fastest.
+ * are multiples of 32 bytes (16 for bf16 and for codes) are read and written fastest; any
+ * other address of an element will do.
  */
 pr_status pr_adamw_step(pr_ctx* ctx, const pr_adamw_tensor* tensors, int32_t n_tensors, double lr,
                         double beta1, double beta2, double eps, int64_t step,

@@ -38,7 +38,7 @@ struct AdamwEntry {
   float* vs;
   int64_t n;
   float wd;
-  int32_t wide;     // every pointer fits the 8-element accesses
+  int32_t wide;     // every pointer fits the 8-element accesses (the step's codes: 16)
   int64_t block0;   // blocks of the tensors before it in the caller's list
 };
 

@@ -152,7 +152,8 @@ pr_status run_kind(pr_ctx* c, const pr_adamw_tensor* t, int32_t n_tensors, int k
     e.n = t[i].n;
     e.wd = t[i].weight_decay;
     e.block0 = mine;
-    const size_t sb = t[i].state_bits == 8 ? 8 : 32;
+    // (the step copies codes 16 bytes at a time, the expansion loads 8)
+    const size_t sb = t[i].state_bits == 32 ? 32 : unpack ? 8 : 16;
     e.wide = fits(t[i].m, sb) && fits(t[i].v, sb) && (unpack ||
              (fits(t[i].param, 8 * esize(t[i].param_dtype)) && fits(t[i].master, 32) &&
               fits(t[i].grad, 8 * esize(t[i].grad_dtype))));

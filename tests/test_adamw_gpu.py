@@ -385,3 +385,57 @@ def test_tensor_past_32_bits(B, ctx, bits):
     if bits == 8:
         for a, b in zip(big_scale, few_scale):
             assert torch.equal(a[-b.numel():], b) and not a[:-b.numel()].any()
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+@pytest.mark.parametrize("param,grad,master", TYPES)
+@pytest.mark.parametrize("start", [8, 16, 24])
+def test_starts_on_the_grid_of_the_parameters(B, ctx, param, grad, master, bits, start):
+    """Starts at which parameters and gradients fit the wide accesses, and codes, of a byte
+    each, may not."""
+    t = Tensors(SIZES, param, grad, master, bits, seed=bits + start, start=start)
+    check_step(B, ctx, t)
+    check_step(B, ctx, t, dict(HYPER, step=8), torch.tensor([0.37], device="cuda"))
+
+
+@pytest.mark.parametrize("param,grad,master", TYPES)
+@pytest.mark.parametrize("off_m,off_v", [(8, 0), (0, 8), (8, 8), (24, 16), (4, 0), (0, 2), (1, 8)])
+def test_either_moments_codes_anywhere(B, ctx, param, grad, master, off_m, off_v):
+    """Codes at any byte, one moment's or both, give the bits of codes on the grid."""
+    a = Tensors([70001, 256, 1000], param, grad, master, 8, 12)
+    b = Tensors([70001, 256, 1000], param, grad, master, 8, 12)
+
+    def moved(t, by):
+        buf = torch.full((by + t.numel() + 8,), 5, dtype=t.dtype, device="cuda")
+        buf[by:by + t.numel()] = t
+        return buf[by:by + t.numel()]
+
+    b.m, b.v = [moved(t, off_m) for t in b.m], [moved(t, off_v) for t in b.v]
+    for t in (a, b):
+        B.pr_adamw_step(ctx, t.table(B), **HYPER)
+    for name in ("p", "master", "m", "v", "m_scale", "v_scale"):
+        for x, y in zip(getattr(a, name) or [], getattr(b, name) or []):
+            assert torch.equal(x, y), name
+    for x, y in zip(B.pr_adamw_unpack(ctx, a.table(B)), B.pr_adamw_unpack(ctx, b.table(B))):
+        assert torch.equal(x, y)
+    for t, by in [(t, off_m) for t in b.m] + [(t, off_v) for t in b.v]:
+        assert (t._base[:by] == 5).all() and (t._base[by + t.numel():] == 5).all()
+
+
+@pytest.mark.parametrize("param,grad,master", TYPES)
+def test_tensors_packed_one_behind_the_other(B, ctx, param, grad, master):
+    """Tensors of 1,000 elements that share one buffer of each kind: every other one's codes
+    lie 8 past a multiple of 16."""
+    n, k = 1000, 5
+    t = Tensors([n * k], param, grad, master, 8, 13)
+    blocks = -(-n // 256)
+    g = torch.Generator("cuda").manual_seed(13)
+    scales = [0.5 * torch.rand(k * blocks, generator=g, device="cuda") for _ in range(2)]
+    t.p, t.g, t.m, t.v = ([x[0][i * n:(i + 1) * n] for i in range(k)] for x in (t.p, t.g, t.m, t.v))
+    if t.master:
+        t.master = [t.master[0][i * n:(i + 1) * n] for i in range(k)]
+    t.m_scale, t.v_scale = ([s[i * blocks:(i + 1) * blocks] for i in range(k)] for s in scales)
+    t.wd = [0.1 * (i % 3) for i in range(k)]
+    assert t.m[1].data_ptr() % 16 == 8
+    check_step(B, ctx, t)
+    check_step(B, ctx, t, dict(HYPER, step=8))
