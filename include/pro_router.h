@@ -498,10 +498,12 @@ pr_status pr_selective_metrics(pr_ctx* ctx, const float* scores, const uint8_t* 
  *   - stats: device float [PR_NPOL / PR_NPREF]; logp: device float [n_rows].
  *     Statistics are summed in fp64 in an order that depends on the sizes alone:
  *     results are bit-reproducible.
- *   - the context holds a workspace (48 bytes per row, 20 per request, a quarter more
- *     than the largest call needed), allocated or grown by the first call that needs more
- *     -- that call synchronises the device; calls on different streams must not overlap
- *     (they share it).
+ *   - the context holds a workspace (48 bytes per row, 20 per request), allocated or grown
+ *     by the first call that needs more, at least to twice what it was -- that call
+ *     waits for the allocation and may be captured.  What it has outgrown is kept until
+ *     the context is destroyed, for the graphs captured before (together no more than the
+ *     workspace itself).  Calls and replays on different streams must not overlap (they
+ *     share it).
  */
 #define PR_NORM_TOKENS 0   /* mean over all counted rows */
 #define PR_NORM_REQUESTS 1 /* mean over the requests with counted rows of the mean over those */

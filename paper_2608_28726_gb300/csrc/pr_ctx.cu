@@ -4,6 +4,7 @@
 // host helpers every translation unit of the library shares.
 #include <cuda_runtime.h>
 
+#include <algorithm>
 #include <atomic>
 #include <cmath>
 #include <cstdio>
@@ -35,6 +36,60 @@ float zthreshold(float tau) {
 pr_status set_device(pr_ctx* c) {
   PR_CUDA(cudaSetDevice(c->device));
   return PR_OK;
+}
+
+// What allocates is refused to a thread while a stream is captured, unless it says that it
+// touches no captured stream.
+struct RelaxedCapture {
+  cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
+  RelaxedCapture() { cudaThreadExchangeStreamCaptureMode(&mode); }
+  ~RelaxedCapture() { cudaThreadExchangeStreamCaptureMode(&mode); }
+};
+
+pr_status grow(pr_grown& g, size_t bytes, bool zero) {
+  if (bytes <= g.bytes) return PR_OK;
+  RelaxedCapture relaxed;
+  pr_grown* older = nullptr;
+  if (g.p) {
+    older = new (std::nothrow) pr_grown(g);
+    if (!older) return PR_ERR_NO_MEMORY;
+  }
+  const size_t room = std::max(bytes + bytes / 4, 2 * g.bytes);
+  void* p = nullptr;
+  if (cudaMalloc(&p, room) != cudaSuccess) {
+    cudaGetLastError();
+    delete older;
+    return PR_ERR_NO_MEMORY;
+  }
+  if (zero) {  // on a stream of its own: the caller's may be captured
+    cudaStream_t s = nullptr;
+    cudaError_t e = cudaStreamCreateWithFlags(&s, cudaStreamNonBlocking);
+    if (e == cudaSuccess) {
+      e = cudaMemsetAsync(p, 0, room, s);
+      if (e == cudaSuccess) e = cudaStreamSynchronize(s);
+      cudaStreamDestroy(s);
+    }
+    if (e != cudaSuccess) {
+      cudaFree(p);
+      delete older;
+      return cuda_fail(e, "zeroing a workspace");
+    }
+  }
+  g.p = p;
+  g.bytes = room;
+  g.older = older;
+  return PR_OK;
+}
+
+void free_grown(pr_grown& g) {
+  cudaFree(g.p);
+  for (pr_grown* o = g.older; o;) {
+    pr_grown* const next = o->older;
+    cudaFree(o->p);
+    delete o;
+    o = next;
+  }
+  g = pr_grown();
 }
 
 pr_status timing_begin(pr_ctx* c, cudaStream_t s) {
@@ -152,7 +207,8 @@ pr_status pr_ctx_destroy(pr_ctx* c) {
   cudaFree(c->head_scr);
   cudaFree(c->sel_ws);
   cudaFree(c->lm_parts);
-  cudaFree(c->loss_ws);
+  free_grown(c->loss_ws);
+  free_grown(c->loss_zero);
   for (cudaEvent_t e : c->tev)
     if (e) cudaEventDestroy(e);
   if (c->copy_stream) cudaStreamDestroy(c->copy_stream);

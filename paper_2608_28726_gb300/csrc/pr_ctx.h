@@ -11,6 +11,14 @@
 
 #define PR_MAX_TIMED 32  // kernels one call can time under PR_OPT_TIMING
 
+// Device memory that grows on demand.  What it has outgrown is kept as long as the context:
+// a captured graph may hold its address.
+struct pr_grown {
+  void* p = nullptr;
+  size_t bytes = 0;
+  pr_grown* older = nullptr;
+};
+
 struct pr_ctx {
   int device = 0;
   int num_sms = 0;
@@ -61,10 +69,8 @@ struct pr_ctx {
   size_t lm_parts_bytes = 0;
   bool lm_ready = false;
   bool qmlp_ready = false;  // pr_quantile_score: shared memory opt-in made
-  // the training losses: workspace, grown on demand
-  void* loss_ws = nullptr;
-  size_t loss_ws_bytes = 0;
-  size_t loss_rows = 0;                // rows that its arrivals have room for
+  // the training losses: workspace, and what of it is zero between calls
+  pr_grown loss_ws, loss_zero;
   bool loss_ready = false;             // shared memory opt-ins made
   int loss_places[2][4] = {};          // clusters of 1, 2, 4, 8 CTAs resident; half, all of the SMs
   bool adamw_ready[2][12] = {};        // pr_adamw_step: shared memory opt-ins made
@@ -85,6 +91,10 @@ bool aligned16(const void* p);
 // the ship threshold on z = logit(score): log(tau / (1 - tau)), +-inf outside (0, 1)
 float zthreshold(float tau);
 pr_status set_device(pr_ctx* c);
+// at least `bytes` of g, all zero where it grows and `zero` says so; also while a stream is
+// captured.  Each growth at least doubles it, so that all outgrown ones together take no more.
+pr_status grow(pr_grown& g, size_t bytes, bool zero);
+void free_grown(pr_grown& g);
 // PR_OPT_TIMING: start a timed call / mark the end of one of its kernels
 pr_status timing_begin(pr_ctx* c, cudaStream_t s);
 pr_status timing_mark(pr_ctx* c, cudaStream_t s);

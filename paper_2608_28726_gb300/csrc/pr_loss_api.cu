@@ -42,14 +42,12 @@ pr_status check_loss(pr_dtype dt, const void* logits, int64_t n_rows, int64_t vo
 
 int64_t forward_grid(const pr_ctx* c) { return (int64_t)c->num_sms * prk::FW_CTAS; }
 
-// the workspace: [tickets, totals][per request][per pair][per row][per group]
+// The workspace: what is zero between calls, [tickets, totals][arrivals per row], and the
+// rest, [per CTA][per request][per pair][per row][per group].  Neither is freed before the
+// context is: a captured graph may hold them.
 pr_status workspace(pr_ctx* c, prk::LossArgs& a, int64_t groups, bool pref, bool state) {
   const size_t n_req = (size_t)a.n_req, n_rows = (size_t)a.n_rows;
-  // (what has to be zero between calls comes first, at places that do not move: the
-  // arrivals of rows by the largest batch so far)
-  const size_t rows = n_rows <= c->loss_rows ? c->loss_rows : n_rows + n_rows / 4;
-  const size_t at_piece = 64 + up16(rows * 4), at_count = at_piece + (size_t)forward_grid(c) * 16,
-               at_coef = at_count + up16(n_req * 4),
+  const size_t at_count = (size_t)forward_grid(c) * 16, at_coef = at_count + up16(n_req * 4),
                at_term = at_coef + up16(pref ? n_req * 4 : 0),
                at_req = at_term + up16(pref ? n_req / 2 * prk::LS_NSTAT * 4 : 0),
                at_block = at_req + up16(n_rows * 4),
@@ -59,27 +57,14 @@ pr_status workspace(pr_ctx* c, prk::LossArgs& a, int64_t groups, bool pref, bool
                at_z = at_state + (state ? n_rows * 16 : 0),
                at_part = at_z + up16(state ? n_rows * 4 : 0),
                bytes = at_part + (pref ? 0 : (size_t)groups * prk::LS_NSTAT * 8);
-  if (bytes > c->loss_ws_bytes || rows > c->loss_rows) {
-    PR_CUDA(cudaDeviceSynchronize());  // kernels may still use the old one
-    cudaFree(c->loss_ws);
-    c->loss_ws = nullptr;
-    c->loss_ws_bytes = 0;
-    const size_t room = bytes + bytes / 4;
-    if (cudaMalloc(&c->loss_ws, room) != cudaSuccess) {
-      cudaGetLastError();
-      c->loss_ws = nullptr;
-      return PR_ERR_NO_MEMORY;
-    }
-    PR_CUDA(cudaMemset(c->loss_ws, 0, room));
-    PR_CUDA(cudaDeviceSynchronize());
-    c->loss_ws_bytes = room;
-    c->loss_rows = rows;
-  }
-  char* w = static_cast<char*>(c->loss_ws);
-  a.ticket = reinterpret_cast<int32_t*>(w);
-  a.totals = reinterpret_cast<int64_t*>(w + 16);
-  a.arrived = reinterpret_cast<int32_t*>(w + 64);
-  a.piece = reinterpret_cast<float2*>(w + at_piece);
+  pr_status st = grow(c->loss_zero, 64 + n_rows * 4, true);
+  if (st != PR_OK || (st = grow(c->loss_ws, bytes, false)) != PR_OK) return st;
+  char* const z = static_cast<char*>(c->loss_zero.p);
+  a.ticket = reinterpret_cast<int32_t*>(z);
+  a.totals = reinterpret_cast<int64_t*>(z + 16);
+  a.arrived = reinterpret_cast<int32_t*>(z + 64);
+  char* const w = static_cast<char*>(c->loss_ws.p);
+  a.piece = reinterpret_cast<float2*>(w);
   a.count = reinterpret_cast<int32_t*>(w + at_count);
   a.coef = reinterpret_cast<float*>(w + at_coef);
   a.term = reinterpret_cast<float*>(w + at_term);

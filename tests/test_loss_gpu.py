@@ -672,3 +672,76 @@ def test_rows_past_32_bits(B, ctx, n, stride):
     got = B.pr_preference_loss(ctx, far, to(ch), to(off), ref_logp=to(ref), grad=grad)
     for w, t in zip(want, got):
         assert torch.equal(w, t)
+
+
+def both_losses(B, c, n, V, seed):
+    """(a call of both losses into buffers of its own, those buffers) of n rows."""
+    g, x, _, ch, old, ref = draw(seed, n, V, "bf16")
+    n_req = 2 * (1 + n // 50)
+    args = [to(t) for t in (ch, g.normal(size=n).astype(np.float32), old, ref, offsets_of(g, n, n_req))]
+    f = dict(device="cuda")
+    out = [torch.zeros(6, **f), torch.zeros(n, **f), torch.zeros_like(x), torch.zeros(5, **f),
+           torch.zeros(n_req, **f), torch.zeros(n, **f), torch.zeros_like(x)]
+
+    def run():
+        chd, adv, oldd, refd, off = args
+        B.pr_policy_loss(c, x, chd, adv, old_logp=oldd, ref_logp=refd, offsets=off, kl_coef=0.1,
+                         norm=1, stats=out[0], logp=out[1], grad=out[2])
+        B.pr_preference_loss(c, x, chd, off, ref_logp=refd, stats=out[3], ratio=out[4],
+                             logp=out[5], grad=out[6])
+
+    return run, out
+
+
+def test_graphs_outlive_larger_calls(B):
+    """Batches of growing size, each captured, then run; every graph replayed after all
+    of them, while other memory has been taken and filled."""
+    c = B.pr_ctx_create(0, 1, 1)
+    graphs = []
+    for i, n in enumerate((30, 600, 5000, 21000)):
+        run, out = both_losses(B, c, n, 200, 30 + i)
+        run()
+        torch.cuda.synchronize()
+        want = [t.clone() for t in out]
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            run()
+        graphs.append((graph, out, want, run))  # (the call keeps its inputs)
+    other = [torch.full((1 << 22,), -1, dtype=torch.int32, device="cuda") for _ in range(8)]
+    for _ in range(2):
+        for graph, out, want, _ in graphs:
+            for t in out:
+                t.zero_()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(t, w) for t, w in zip(out, want))
+    assert all((t == -1).all() for t in other)
+    # and calls still give what they gave
+    run, out = both_losses(B, c, 600, 200, 31)
+    run()
+    assert all(torch.equal(t, w) for t, w in zip(out, graphs[1][2]))
+    B.pr_ctx_destroy(c)
+
+
+@pytest.mark.parametrize("mode", ["global", "thread_local", "relaxed"])
+@pytest.mark.parametrize("n", [30, 900, 6000])
+def test_the_first_call_of_a_context_captured(B, ctx, n, mode):
+    """A context that has no workspace yet takes it during the capture; so does one whose
+    workspace is too small."""
+    run, want = both_losses(B, ctx, n, 150, n)
+    run()
+    torch.cuda.synchronize()
+    for first in (0, 10):
+        c = B.pr_ctx_create(0, 1, 1)
+        if first:
+            both_losses(B, c, first, 150, 1)[0]()
+        run, out = both_losses(B, c, n, 150, n)
+        graph = torch.cuda.CUDAGraph()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph, capture_error_mode=mode):
+            run()
+        graph.replay()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(t, w) for t, w in zip(out, want))
+        B.pr_ctx_destroy(c)
