@@ -531,6 +531,8 @@ typedef struct {
  *   loss = the mean of loss_t as norm says (0 when no row counts);
  *   d loss_t / d l = -r A (0 where the clipped term is strictly the smaller one)
  *                    + beta (1 - exp(ref - l)).
+ *   With beta = 0 the KL term is a statistic alone: neither the loss nor the gradient
+ *   has a part of it, whatever its value.
  *   old_logp   device float [n_rows], log-probabilities under the policy that
  *              sampled, or NULL: this one (r = 1)
  *   ref_logp   device float [n_rows] under the reference model, or NULL (no KL term)

@@ -85,8 +85,8 @@ def policy(x, chosen, advantage, old_logp=None, ref_logp=None, mask=None, offset
             kl = np.expm1(q) - q
             if kl_coef != 0.0:
                 slope[t] += w * kl_coef * -np.expm1(q)
-        stats += w * np.array([-surrogate + kl_coef * kl, surrogate, kl, r, float(clipped),
-                               np.expm1(d) - d])
+        loss = -surrogate + (kl_coef * kl if kl_coef != 0.0 else 0.0)
+        stats += w * np.array([loss, surrogate, kl, r, float(clipped), np.expm1(d) - d])
     logp = np.where(req >= 0, l, 0.0)
     return stats, logp, _grad(p, chosen, slope, req, temperature, grad_scale)
 

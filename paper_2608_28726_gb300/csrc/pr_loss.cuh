@@ -806,7 +806,9 @@ __device__ __forceinline__ void write_stats(const LossArgs& a, const float2* sta
     total[j] = v;
   }
   if (lane == 0) {
-    a.stats[0] = (float)((double)a.kl_coef * total[1] - total[0]);
+    // (a KL term that is only watched, coefficient 0, may be infinite)
+    const double kl = a.kl_coef != 0.f ? (double)a.kl_coef * total[1] : 0.;
+    a.stats[0] = (float)(kl - total[0]);
     for (int j = 0; j < RG_TERMS; ++j) a.stats[1 + j] = (float)total[j];
     a.ticket[1] = 0;
   }

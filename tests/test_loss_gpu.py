@@ -745,3 +745,31 @@ def test_the_first_call_of_a_context_captured(B, ctx, n, mode):
         torch.cuda.synchronize()
         assert all(torch.equal(t, w) for t, w in zip(out, want))
         B.pr_ctx_destroy(c)
+
+
+# one CTA and several to a row, a warp to a row, rows of more than eight SMs
+KERNELS = [(6, 300), (5, 151936), (700, 40), (3, 1000003)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,V", KERNELS)
+def test_a_kl_term_of_no_weight_is_no_part_of_the_loss(B, ctx, n, V, dtype):
+    """kl_coef 0 with a reference 200 above a row's l, and a masked emitted token."""
+    g, x, x64, ch, old, ref = draw(n + V, n, V, dtype)
+    ref[1] += 200.0
+    x[2, ch[2]] = -torch.inf
+    x64 = x.double().cpu().numpy()
+    adv = g.normal(size=n).astype(np.float32)
+    B.pr_ctx_flags(ctx, clear=True)
+    for want_grad in (True, False):
+        args = dict(old_logp=to(old), want_grad=want_grad, **CLIP)
+        a = B.pr_policy_loss(ctx, x, to(ch), to(adv), **args)
+        b = B.pr_policy_loss(ctx, x, to(ch), to(adv), ref_logp=to(ref), **args)
+        s, l, gr = L.policy(x64, ch, adv, old, ref, **CLIP)
+        assert np.isfinite(s[0]) and not torch.isfinite(b[0][B.PR_POL_KL])
+        check_stats(b[0][:2], s[:2], 2.0)
+        assert torch.equal(a[0][:2], b[0][:2]) and torch.equal(a[0][3:5], b[0][3:5])
+        assert torch.equal(a[1], b[1])
+        check_rows(b[1], l, b[2], gr, dtype)
+        assert not want_grad or torch.equal(a[2], b[2])
+    assert B.pr_ctx_flags(ctx, clear=True) == 0

@@ -70,3 +70,17 @@ def test_closed_forms():
     # nothing counts
     stats, logp, grad = L.policy(x, [0, 0], [1.0, 1.0], mask=[0, 0])
     assert (stats == 0).all() and (logp == 0).all() and (grad == 0).all()
+
+
+def test_a_kl_term_of_no_weight_is_no_part_of_the_loss():
+    g, x, ch, mask, off = _batch(5)
+    l, _ = L.rows(x, ch)
+    old, ref = l + 0.1 * g.normal(size=14), l + 0.1
+    ref[1], ref[8] = np.inf, np.nan
+    mask[[1, 8]] = 1
+    adv = g.normal(size=14)
+    a = L.policy(x, ch, adv, old, None, mask, off)
+    b = L.policy(x, ch, adv, old, ref, mask, off)
+    assert np.isfinite(a[0]).all() and not np.isfinite(b[0][2])
+    assert (np.delete(a[0], 2) == np.delete(b[0], 2)).all()
+    assert (a[1] == b[1]).all() and (a[2] == b[2]).all()
