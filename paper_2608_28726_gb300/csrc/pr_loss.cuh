@@ -786,8 +786,10 @@ __device__ __forceinline__ void write_stats(const LossArgs& a, const float2* sta
   int last = 0;
   if (lane < RG_TERMS) {
     double v = 0.;
-    for (int w = 0; w < warps; ++w)
-      v += (double)stat[w * RG_TERMS + lane].x + (double)stat[w * RG_TERMS + lane].y;
+    for (int w = 0; w < warps; ++w) {  // (an infinite sum's compensation is NaN)
+      const float2 q = stat[w * RG_TERMS + lane];
+      v += isinf(q.x) ? (double)q.x : (double)q.x + (double)q.y;
+    }
     a.part[at * RG_TERMS + lane] = v;
   }
   __syncwarp();

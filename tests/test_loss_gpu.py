@@ -773,3 +773,40 @@ def test_a_kl_term_of_no_weight_is_no_part_of_the_loss(B, ctx, n, V, dtype):
         check_rows(b[1], l, b[2], gr, dtype)
         assert not want_grad or torch.equal(a[2], b[2])
     assert B.pr_ctx_flags(ctx, clear=True) == 0
+
+
+@pytest.mark.parametrize("n,V", KERNELS)
+def test_infinite_means_are_infinite(B, ctx, n, V):
+    """Terms beyond single precision (200 above: 7e86) and a token that the policy has
+    masked since: the means that they enter are infinite, the others what they are."""
+    g, x, x64, ch, old, ref = draw(n + V, n, V, "f32")
+    adv = np.abs(g.normal(size=n)).astype(np.float32)
+
+    def check(x, x64, old, ref, adv, infinite):
+        for want_grad in (True, False):
+            st, lp, _ = B.pr_policy_loss(ctx, x, to(ch), to(adv), old_logp=to(old), ref_logp=to(ref),
+                                         kl_coef=0.1, want_grad=want_grad, **CLIP)
+            s, l, _ = L.policy(x64, ch, adv, old, ref, kl_coef=0.1, **CLIP)
+            with np.errstate(over="ignore"):
+                s = s.astype(np.float32).astype(np.float64)
+            got = f64(st)
+            assert [i for i in range(6) if np.isinf(s[i])] == infinite
+            assert (got[infinite] == s[infinite]).all(), (got, s)
+            rest = [i for i in range(6) if i not in infinite]
+            check_stats(st[rest], s[rest], 2.0)
+            check_rows(lp, l, None, None, "f32")
+
+    far = ref.copy()
+    far[1] += 200.0
+    check(x, x64, old, far, adv, [B.PR_POL_LOSS, B.PR_POL_KL])
+    far = old.copy()
+    far[1] -= 200.0  # clipped: the surrogate stays finite
+    check(x, x64, far, ref, adv, [B.PR_POL_RATIO, B.PR_POL_OLD_KL])
+    minus = adv.copy()
+    minus[1] = -1.0  # not clipped
+    check(x, x64, far, ref, minus, [B.PR_POL_LOSS, B.PR_POL_SURROGATE, B.PR_POL_RATIO,
+                                    B.PR_POL_OLD_KL])
+    x = x.clone()
+    x[1, ch[1]] = -torch.inf
+    check(x, f64(x), old, None, adv, [B.PR_POL_OLD_KL])
+    B.pr_ctx_flags(ctx, clear=True)
