@@ -575,7 +575,7 @@ typedef struct {
  *   s_r = sum over request r's counted rows of (l_t - ref_t), or their mean;
  *   d = s_2i - s_2i+1, h = beta d - margin; loss: mean over the pairs of which
  *   both answers have counted rows (0 when there is none; the other pairs have
- *   no gradient).
+ *   no gradient, zeros whatever their logits hold).
  *   ref_logp   device float [n_rows] under the reference model, or NULL (0)
  *   ratio      device float [n_req]: the s_r                    (output)
  * n_rows < 2^31, n_req even and >= 2.

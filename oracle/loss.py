@@ -49,7 +49,7 @@ def _grad(p, chosen, slope, req, temperature, grad_scale):
     n, V = p.shape
     g = np.zeros((n, V))
     for t in range(n):
-        if req[t] < 0:
+        if req[t] < 0 or slope[t] == 0:  # (a row that has no part in the loss may hold NaN)
             continue
         one = np.zeros(V)
         if 0 <= chosen[t] < V:

@@ -454,7 +454,7 @@ __device__ __forceinline__ RowOut row_out(const RowState& s, float k) {
   RowOut o;
   o.K = s.K;
   o.nk = -k * s.adj;
-  o.gy = k * s.rest;
+  o.gy = k == 0.f ? 0.f : k * s.rest;  // (0, too, where rest is NaN)
   o.M = s.M;
   o.mode = k == 0.f ? ROW_ZERO : s.M == INFINITY ? ROW_FAST : ROW_ROBUST;
   return o;

@@ -810,3 +810,29 @@ def test_infinite_means_are_infinite(B, ctx, n, V):
     x[1, ch[1]] = -torch.inf
     check(x, f64(x), old, None, adv, [B.PR_POL_OLD_KL])
     B.pr_ctx_flags(ctx, clear=True)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,V", [(9, 701), (9, 704), (700, 43), (3, 1000003)])
+def test_an_answer_without_a_partner_has_no_gradient(B, ctx, n, V, dtype):
+    """NaN and infinities in an answer whose partner is empty or masked: zeros, at the emitted
+    token (in the row's words or at its ends) as elsewhere."""
+    g, x, _, ch, _, ref = draw(n + V, n, V, dtype)
+    m = n // 3
+    rows = range(m)
+    for t in rows:
+        x[t, (7 * t) % V] = (torch.nan, torch.inf)[t % 2]
+        ch[t] = (0, V // 2, V - 1)[t % 3]
+    x64 = f64(x)
+    mask = np.ones(n, np.uint8)
+    for off in ([0, 0, m, 2 * m, n], [0, m, m, 2 * m, n], [0, m, n]):
+        if len(off) == 3:
+            mask[m:] = 0  # the partner's rows are all masked
+        st, r, lp, gr = B.pr_preference_loss(ctx, x, to(ch), to(off, np.int64), ref_logp=to(ref),
+                                             mask=to(mask))
+        s, ro, lo, go = L.preference(x64, ch, off, ref, mask)
+        assert torch.isnan(lp[:m]).all() and not gr[:m].any()
+        check_rows(lp, lo, gr, go, dtype)
+        check_stats(st, s, 1.0 + np.nan_to_num(np.abs(ro)).max())
+        assert not torch.isnan(st).any()
+    B.pr_ctx_flags(ctx, clear=True)

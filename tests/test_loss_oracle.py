@@ -84,3 +84,10 @@ def test_a_kl_term_of_no_weight_is_no_part_of_the_loss():
     assert np.isfinite(a[0]).all() and not np.isfinite(b[0][2])
     assert (np.delete(a[0], 2) == np.delete(b[0], 2)).all()
     assert (a[1] == b[1]).all() and (a[2] == b[2]).all()
+
+
+def test_an_answer_without_a_partner_has_no_gradient():
+    x = np.random.Generator(np.random.PCG64(6)).normal(size=(8, 5))
+    x[1, 2], x[2] = np.nan, np.inf
+    _, _, logp, grad = L.preference(x, [0] * 8, [0, 0, 4, 6, 8])
+    assert np.isnan(logp[1:3]).all() and not grad[:4].any() and (grad[4:] != 0).all()
