@@ -484,7 +484,9 @@ pr_status pr_selective_metrics(pr_ctx* ctx, const float* scores, const uint8_t* 
  *   - offsets: device int64 [n_req + 1], non-decreasing, rows [offsets[r],
  *     offsets[r + 1]) are request r's.  A request that reaches outside [0, n_rows]
  *     or has a negative length counts no rows and raises PR_FLAG_BAD_OFFSETS, an
- *     empty one PR_FLAG_EMPTY_REQ (context flag word).
+ *     empty one PR_FLAG_EMPTY_REQ (context flag word).  Where offsets decrease
+ *     all the same, a row counts at most once, for the request in whose bounds a bisection
+ *     of the offsets finds it.
  *   - a counted row with NaN or +inf, or with nothing finite, has logp NaN
  *     (PR_FLAG_NONFINITE), one with an id outside the vocabulary too
  *     (PR_FLAG_BAD_CHOSEN); as the formulas say, its gradient row and the

@@ -32,15 +32,22 @@ def rows(x, chosen, temperature=1.0):
 
 def counted(n, mask, offsets):
     """(request of each row, -1 where the row does not count; counted rows of
-    each request).  Without offsets all rows are request 0."""
+    each request).  Without offsets all rows are request 0.  A row is looked up by
+    bisection: the last request that begins at or before it, if its bounds hold the row
+    and lie in the batch."""
     req = np.full(n, -1, np.int64)
     off = [0, n] if offsets is None else [int(v) for v in offsets]
-    for r, (a, b) in enumerate(zip(off[:-1], off[1:])):
-        if a < 0 or b < a or b > n:
-            continue
-        for t in range(a, b):
-            if mask is None or mask[t]:
-                req[t] = r
+    for t in range(n):
+        first, end = 0, len(off) - 1  # the request is in [first, end)
+        while end - first > 1:
+            mid = (first + end) // 2
+            if off[mid] <= t:
+                first = mid
+            else:
+                end = mid
+        a, b = off[first], off[first + 1]
+        if 0 <= a <= t < b <= n and (mask is None or mask[t]):
+            req[t] = first
     count = np.array([(req == r).sum() for r in range(len(off) - 1)], np.int64)
     return req, count
 

@@ -47,7 +47,7 @@ struct LossArgs {
   void* grad;
   int64_t grad_stride;
   // workspace
-  int32_t* ticket;     // [2] arrivals, zero between calls (the plan's, the statistics')
+  int32_t* ticket;     // [3] zero between calls: arrivals (the plan's, the statistics'); offsets decrease
   int64_t* totals;     // counted tokens; requests with some (policy) or pairs of such
   int32_t* count;      // [n_req] counted tokens
   int32_t* row_req;    // [n_rows] request of a row that counts, else -1
@@ -73,7 +73,8 @@ struct LossArgs {
 constexpr int PL_BLOCK = 1024;  // rows of a block
 constexpr int PL_FEW = 1024;    // requests that one CTA counts in shared memory
 
-// the request that counts row t, else -1
+// The request that counts row t, else -1.  Where offsets decrease, the request that this
+// search finds is the row's, on every way of listing.
 __device__ __forceinline__ int32_t counted_by(const LossArgs& a, int64_t t) {
   if (a.mask && a.mask[t] == 0) return -1;
   if (!a.offsets) return 0;
@@ -185,7 +186,10 @@ static __global__ void __launch_bounds__(PL_BLOCK) loss_count(const LossArgs a, 
     int64_t lo = 0, hi = 0, n = 0;
     const int64_t r = blockIdx.x;
     __shared__ int bad;
-    if (tid == 0) bad = bad_bounds(a, r, lo, hi);
+    if (tid == 0) {
+      bad = bad_bounds(a, r, lo, hi);
+      if (hi < lo) a.ticket[2] = 1;  // (seen by the last CTA with this one's arrival)
+    }
     __syncthreads();
     lo = a.offsets ? a.offsets[r] : 0;
     hi = a.offsets ? a.offsets[r + 1] : a.n_rows;
@@ -204,6 +208,17 @@ static __global__ void __launch_bounds__(PL_BLOCK) loss_count(const LossArgs a, 
   }
   __syncthreads();
   if (!last) return;
+  if (__ldcg(a.ticket + 2)) {
+    // Offsets that decrease: requests' bounds overlap, and which rows are whose is for the
+    // rows to say.
+    for (int64_t q = tid; q < a.n_req; q += PL_BLOCK) a.count[q] = 0;
+    __syncthreads();
+    for (int64_t t = tid; t < a.n_rows; t += PL_BLOCK) {
+      const int32_t r = __ldcg(a.row_req + t);
+      if (r >= 0) atomicAdd(a.count + r, 1);
+    }
+    __syncthreads();
+  }
   int64_t used = 0;
   for (int64_t q = tid; q < a.n_req; q += PL_BLOCK) {
     const int32_t k = __ldcg(a.count + q);
@@ -232,7 +247,7 @@ static __global__ void __launch_bounds__(PL_BLOCK) loss_count(const LossArgs a, 
   if (tid == 0) {
     a.totals[0] = before;
     a.totals[1] = used;
-    *a.ticket = 0;
+    a.ticket[0] = a.ticket[2] = 0;
   }
 }
 static __global__ void __launch_bounds__(PL_BLOCK) loss_list(const LossArgs a) {

@@ -836,3 +836,45 @@ def test_an_answer_without_a_partner_has_no_gradient(B, ctx, n, V, dtype):
         check_stats(st, s, 1.0 + np.nan_to_num(np.abs(ro)).max())
         assert not torch.isnan(st).any()
     B.pr_ctx_flags(ctx, clear=True)
+
+
+@pytest.mark.parametrize("n", [40, 700, 5000])
+def test_offsets_that_decrease(B, ctx, n):
+    """Bounds that overlap: each row counts once, for the same request however large the
+    batch, and a request's mean is over the rows that it counts."""
+    V = 24
+    g, x, x64, ch, old, ref = draw(n, n, V, "f32")
+    B.pr_ctx_flags(ctx, clear=True)
+    for off in ([0, 6, 3, 10], [0, 10, 3, 6, 10], [4, 10, 2, 1, 8], [0, 12, 3, 6, 10], [10, 6, 3, 0, 0],
+                [3, -2, 5, 10, 4]):
+        off = [v * n // 10 for v in off]
+        n_req = len(off) - 1
+        adv = g.normal(size=n_req).astype(np.float32)
+        for mask in (None, (g.random(n) < 0.7).astype(np.uint8)):
+            for norm in (0, 1):
+                kw = dict(per_request=True, **CLIP)
+                st, lp, gr = B.pr_policy_loss(ctx, x, to(ch), to(adv), old_logp=to(old), norm=norm,
+                                              mask=to(mask), offsets=to(off, np.int64), **kw)
+                s, lo, go = L.policy(x64, ch, adv, old, None, mask, off, requests=bool(norm), **kw)
+                check_rows(lp, lo, gr, go, "f32")
+                check_stats(st, s, 2.0)
+                assert B.pr_ctx_flags(ctx, clear=True) & B.PR_FLAG_BAD_OFFSETS
+            if n_req % 2:
+                continue
+            st, r, lp, gr = B.pr_preference_loss(ctx, x, to(ch), to(off, np.int64), ref_logp=to(ref),
+                                                 mask=to(mask), length_norm=True)
+            s, ro, lo, go = L.preference(x64, ch, off, ref, mask, length_norm=True)
+            check_rows(lp, lo, gr, go, "f32")
+            assert (np.abs(f64(r) - ro) <= 2e-5 + 1e-6 * np.abs(ro)).all()
+            check_stats(st, s, 1.0 + np.abs(ro).max())
+            assert B.pr_ctx_flags(ctx, clear=True) & B.PR_FLAG_BAD_OFFSETS
+    # nothing of it is left for the next batch
+    off = offsets_of(g, n, 6)
+    adv = g.normal(size=6).astype(np.float32)
+    kw = dict(per_request=True, **CLIP)
+    st, lp, gr = B.pr_policy_loss(ctx, x, to(ch), to(adv), old_logp=to(old), norm=1,
+                                  offsets=to(off), **kw)
+    s, lo, go = L.policy(x64, ch, adv, old, None, None, off, requests=True, **kw)
+    check_rows(lp, lo, gr, go, "f32")
+    check_stats(st, s, 2.0)
+    B.pr_ctx_flags(ctx, clear=True)

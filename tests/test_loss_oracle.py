@@ -91,3 +91,18 @@ def test_an_answer_without_a_partner_has_no_gradient():
     x[1, 2], x[2] = np.nan, np.inf
     _, _, logp, grad = L.preference(x, [0] * 8, [0, 0, 4, 6, 8])
     assert np.isnan(logp[1:3]).all() and not grad[:4].any() and (grad[4:] != 0).all()
+
+
+def test_rows_belong_to_one_request():
+    """In order: the request whose bounds hold the row.  Where offsets decrease each row is
+    counted at most once."""
+    g = np.random.Generator(np.random.PCG64(7))
+    for _ in range(50):
+        off = np.sort(g.integers(-1, 14, 6))
+        req, count = L.counted(12, None, off)
+        for t in range(12):
+            own = [r for r in range(5) if 0 <= off[r] <= t < off[r + 1] <= 12]
+            assert req[t] == (own[0] if own else -1)
+        assert (count == [(req == r).sum() for r in range(5)]).all()
+    req, count = L.counted(10, None, [0, 6, 3, 10])
+    assert req.tolist() == [0] * 6 + [2] * 4 and count.tolist() == [6, 0, 4]
