@@ -355,10 +355,6 @@ pr_status pr_policy_loss(pr_ctx* c, const void* logits, pr_dtype dt, int64_t n_r
   if (p->adv_per_request && !offsets) return PR_ERR_INVALID_ARG;
   if ((st = set_device(c)) != PR_OK) return st;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-  if (n_rows == 0) {
-    PR_CUDA(cudaMemsetAsync(stats, 0, PR_NPOL * sizeof(float), s));
-    return PR_OK;
-  }
   prk::LossArgs a;
   fill(a, c, logits, n_rows, vocab, row_stride, chosen, mask, offsets, n_req, ref_logp,
        p->temperature, p->grad_scale, stats, logp, grad, grad_stride);
@@ -369,6 +365,14 @@ pr_status pr_policy_loss(pr_ctx* c, const void* logits, pr_dtype dt, int64_t n_r
   a.clip_lo = 1.f - p->clip_low;
   a.clip_hi = 1.f + p->clip_high;
   a.kl_coef = p->kl_coef;
+  if (n_rows == 0) {  // the requests' bounds are looked at all the same
+    if ((st = timing_begin(c, s)) != PR_OK) return st;
+    if (offsets && ((st = workspace(c, a, 0, false, false)) != PR_OK ||
+                    (st = launch_plan(c, a, 0, s)) != PR_OK))
+      return st;
+    PR_CUDA(cudaMemsetAsync(stats, 0, PR_NPOL * sizeof(float), s));
+    return PR_OK;
+  }
   if ((st = ring_setup(c)) != PR_OK) return st;
   const RingShape ring = choose_ring(c, dt, n_rows, vocab);
   if ((st = workspace(c, a, std::max(ring.groups, forward_grid(c)), false, !ring.hold)) != PR_OK)

@@ -878,3 +878,37 @@ def test_offsets_that_decrease(B, ctx, n):
     check_rows(lp, lo, gr, go, "f32")
     check_stats(st, s, 2.0)
     B.pr_ctx_flags(ctx, clear=True)
+
+
+@pytest.mark.parametrize("n_req", [2, 1024, 3000])
+def test_batches_without_rows_report_their_bounds(B, ctx, n_req):
+    """Both losses raise the same flags for requests of a batch that has no rows."""
+    x = torch.zeros(0, 40, device="cuda")
+    ch, f = torch.zeros(0, dtype=torch.int32, device="cuda"), torch.zeros(0, device="cuda")
+    B.pr_ctx_flags(ctx, clear=True)
+    for last, flags in ((0, B.PR_FLAG_EMPTY_REQ), (3, B.PR_FLAG_EMPTY_REQ | B.PR_FLAG_BAD_OFFSETS)):
+        off = np.zeros(n_req + 1, np.int64)
+        off[-1] = last
+        for norm in (0, 1):
+            stats = torch.full((6,), 7.0, device="cuda")
+            st, lp, gr = B.pr_policy_loss(ctx, x, ch, f, offsets=to(off), norm=norm, stats=stats)
+            assert not st.any() and lp.numel() == 0 and gr.shape == (0, 40)
+            assert B.pr_ctx_flags(ctx, clear=True) == flags
+        st, r, lp, gr = B.pr_preference_loss(ctx, x, ch, to(off))
+        assert not st.any() and not r.any()
+        assert B.pr_ctx_flags(ctx, clear=True) == flags
+    st = B.pr_policy_loss(ctx, x, ch, f)[0]
+    assert not st.any() and B.pr_ctx_flags(ctx, clear=True) == 0
+
+
+def test_a_batch_without_rows_has_its_own_kernel_times(B):
+    c = B.pr_ctx_create(0, 1, 1)
+    B.pr_ctx_set_option(c, B.PR_OPT_TIMING, 1)
+    g, x, _, ch, old, _ = draw(4, 4, 40, "f32")
+    B.pr_policy_loss(c, x, to(ch), to(old))
+    assert len(B.pr_ctx_kernel_times(c)) == 1
+    B.pr_policy_loss(c, x[:0], to(ch), to(old))
+    assert len(B.pr_ctx_kernel_times(c)) == 0
+    B.pr_policy_loss(c, x[:0], to(ch), to(old), offsets=to([0, 0], np.int64))
+    assert len(B.pr_ctx_kernel_times(c)) == 1
+    B.pr_ctx_destroy(c)
