@@ -363,8 +363,9 @@ __device__ __forceinline__ void step_block(const BlockIn<P, G, MASTER, BITS>& in
     set_codes(reinterpret_cast<uint8_t*>(t.m), b.at, wide, b.left, c);
 #pragma unroll
     for (int j = 0; j < 4; ++j) x[j] = __fmul2_rn(v[j], both(iv));
-    // v's roots are there; those of subnormal numbers, taken for 0, have code 0 next to 1e-26
-    if (fast && tv > 1e-26f) {
+    // v's roots are there; those of subnormal numbers, taken for 0, have code 0 next to 1e-26,
+    // and above 2^126 the scale's reciprocal would be taken for 0
+    if (fast && tv > 1e-26f && tv < 8.5e37f) {
       const float by = sqrt_fast(iv);
       codes_of<2>(x, m, [&](int j) { return __fmul2_rn(roots[j], both(by)); }, q);
     } else {

@@ -439,3 +439,43 @@ def test_tensors_packed_one_behind_the_other(B, ctx, param, grad, master):
     assert t.m[1].data_ptr() % 16 == 8
     check_step(B, ctx, t)
     check_step(B, ctx, t, dict(HYPER, step=8))
+
+
+@pytest.mark.parametrize("eps", [1e-8, 1e-30])
+@pytest.mark.parametrize("top", [1.0e19, 9.2e18, 9.3e18, 1.3e19, 1.84e19])
+def test_codes_of_huge_second_moments(B, ctx, top, eps):
+    """Gradients whose squares come near the largest number (beta2 0: v is the square, one
+    rounded product), among them blocks above 2^126, where the scale's reciprocal is
+    subnormal: 21 bits of it are left, which moves a code by 255 x 2^-23 = 3e-5 beside the
+    6e-5 of its roots: 1e-4."""
+    n = 40 * 256 + 77
+    g = torch.Generator(device="cuda").manual_seed(12)
+    grad = (top * torch.rand(n, generator=g, device="cuda")).contiguous()
+    grad[::256] = top
+    p = torch.zeros(n, device="cuda")
+    m, v = torch.zeros(n, dtype=torch.int8, device="cuda"), torch.zeros(n, dtype=torch.uint8, device="cuda")
+    blocks = -(-n // 256)
+    ms, vs = torch.zeros(blocks, device="cuda"), torch.zeros(blocks, device="cuda")
+    t = B.pr_adamw_tensors([p], [grad], [m], [v], m_scale=[ms], v_scale=[vs])
+    B.pr_ctx_flags(ctx, clear=True)
+    B.pr_adamw_step(ctx, t, 1e-2, beta1=0.0, beta2=0.0, eps=eps, step=1)
+    x = grad.cpu().numpy()
+    for got, scale, want, steps, power in ((m, ms, x, 127.0, 0.5), (v, vs, x * x, 255.0, 0.25)):
+        want = want.astype(np.float64)
+        per = np.maximum.reduceat(want, np.arange(0, n, 256))
+        assert (f64(scale) == per).all()
+        u = steps * (want / np.repeat(per, 256)[:n]) ** power
+        off = np.abs(f64(got) - u)
+        assert (off <= 0.5 + 1e-4).all(), (off.max(), x[off.argmax()])
+    assert torch.isfinite(p).all() and B.pr_ctx_flags(ctx, clear=True) == 0
+
+
+def test_states_under_huge_scales_are_kept(B, ctx):
+    """States of 3e38 without a gradient: one step gives beta2 v, whatever its code."""
+    t = Tensors([2000], "f32", "f32", False, 8, 14)
+    t.g[0].zero_()
+    t.v_scale[0].fill_(3e38)
+    t.v[0][::256] = 255
+    for step in (7, 8):
+        check_step(B, ctx, t, dict(HYPER, step=step))
+    assert (t.v_scale[0] > 2e38).all() and (t.v[0][::256] == 255).all()
