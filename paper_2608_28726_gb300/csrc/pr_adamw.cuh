@@ -155,25 +155,33 @@ __device__ __forceinline__ void set_codes(uint8_t* p, int64_t at, bool wide, int
 
 // ---- 8-bit states ---------------------------------------------------------------------
 
-// Byte j of w as a float: into the last byte of 2^23's significand, and 2^23 away again.
-// `bias` more goes with it: signed codes come with their top bit turned, 128 too much.
+// Byte j of w over 2^K as a float: into the last byte of a significand whose last place counts
+// 2^-K, and the rest of that number away again.  `bias` more goes with it: signed codes come
+// with their top bit turned, 128 too much.
+template <int K>
 __device__ __forceinline__ float byte_of(uint32_t w, int j, float bias) {
-  return __uint_as_float(__byte_perm(w, 0x4b000000u, 0x7440 + j)) - (8388608.f + bias);
+  constexpr uint32_t BASE = (uint32_t)(127 + 23 - K) << 23;
+  constexpr float SIZE = (float)(1 << (23 - K)), LAST = 1.f / (float)(1 << K);
+  return __uint_as_float(__byte_perm(w, BASE, 0x7640 + j)) - (SIZE + bias * LAST);
 }
-// what the codes of a word's half (bytes j, j + 1) stand for; unit: the scale's share
+// What the codes of a word's half (bytes j, j + 1) stand for; unit: the scale's share.  The
+// codes are taken over 2^6 and 2^7, exactly, so that the unit is a quarter and a sixteenth
+// of the scale, not 1 / 127^2 and 1 / 255^4 of it, which small scales have no normal number
+// for.
+constexpr int M_K = 6, V_K = 7;
 __device__ __forceinline__ float2 held_m(uint32_t w, int j, float unit) {
   w ^= 0x80808080u;
-  const float a = byte_of(w, j, 128.f), b = byte_of(w, j + 1, 128.f);
+  const float a = byte_of<M_K>(w, j, 128.f), b = byte_of<M_K>(w, j + 1, 128.f);
   return __fmul2_rn(make_float2(__fmul_rn(a, fabsf(a)), __fmul_rn(b, fabsf(b))),
                     make_float2(unit, unit));
 }
 __device__ __forceinline__ float2 held_v(uint32_t w, int j, float unit) {
-  float2 q = make_float2(byte_of(w, j, 0.f), byte_of(w, j + 1, 0.f));
+  float2 q = make_float2(byte_of<V_K>(w, j, 0.f), byte_of<V_K>(w, j + 1, 0.f));
   q = __fmul2_rn(q, q);
   return __fmul2_rn(__fmul2_rn(q, q), make_float2(unit, unit));
 }
-constexpr float UNIT_M = (float)(1.0 / (127.0 * 127.0));
-constexpr float UNIT_V = (float)(1.0 / (255.0 * 255.0 * 255.0 * 255.0));
+constexpr float UNIT_M = (float)(4096.0 / (127.0 * 127.0));                      // 2^(2 M_K)
+constexpr float UNIT_V = (float)(268435456.0 / (255.0 * 255.0 * 255.0 * 255.0));  // 2^(4 V_K)
 
 // the block's largest magnitude as its scale (bit patterns of non-negative floats are
 // ordered, NaN above all): NaN where it is not finite, 0 below the normal numbers

@@ -479,3 +479,28 @@ def test_states_under_huge_scales_are_kept(B, ctx):
     for step in (7, 8):
         check_step(B, ctx, t, dict(HYPER, step=step))
     assert (t.v_scale[0] > 2e38).all() and (t.v[0][::256] == 255).all()
+
+
+@pytest.mark.parametrize("scale", [3e38, 1e-30, 1e-33, 1e-34, 1e-35, 1e-36, 1e-37, 2.0 ** -126])
+def test_every_scale_holds_its_values(B, ctx, scale):
+    """Every code under scales down to the smallest normal number: the documented value by 3e-7,
+    and by what the share of a scale loses where it is subnormal: half of 2^-149 times up to
+    (255 / 2^7)^4 = 16 for v, (127 / 2^6)^2 = 4 for m; and the value's own last place."""
+    q = torch.arange(256, device="cuda")
+    m, v = (q - 128).clamp(min=-127).to(torch.int8), q.to(torch.uint8)
+    s = [torch.full((1,), scale, device="cuda") for _ in range(2)]
+    z = torch.zeros(256, device="cuda")
+    t = B.pr_adamw_tensors([z], [z], [m], [v], m_scale=s[:1], v_scale=s[1:])
+    got = B.pr_adamw_unpack(ctx, t)
+    for x, codes, signed in ((got[0], m, True), (got[1], v, False)):
+        want = L.held8(f64(codes), f64(s[0]), signed)
+        assert (np.abs(f64(x[0]) - want) <= 3e-7 * np.abs(want) + 9 * 2.0 ** -149).all()
+    # and the step reads the same ones: without a gradient or decay it writes them back
+    b = 1.0 - 2.0 ** -53
+    m0, v0 = m.clone(), v.clone()
+    B.pr_adamw_step(ctx, t, 0.0, beta1=b, beta2=b)
+    if scale > 1e-30:  # (below, small codes' values are subnormal)
+        assert torch.equal(m, m0) and torch.equal(v, v0)
+    assert m[255] == 127 and v[255] == 255
+    for x in s:
+        assert abs(x.item() / np.float32(scale) - 1.0) <= 1e-6 + (9 * 2.0 ** -149) / scale
