@@ -638,7 +638,8 @@ pr_status pr_adamw_step(pr_ctx* ctx, const pr_adamw_tensor* tensors, int32_t n_t
 /*
  * The values that 8-bit states stand for (checkpoints, a change of the states'
  * type): m, v device float [blocks][256], the tensors' blocks one after another,
- * blocks = sum of ceil(n / 256); past a tensor's end its last block is zero.
+ * blocks = sum of ceil(n / 256); past a tensor's end its last block is zero.  They may be
+ * NULL where there is no block.
  * Every tensor must have state_bits 8.
  */
 pr_status pr_adamw_unpack(pr_ctx* ctx, const pr_adamw_tensor* tensors, int32_t n_tensors, float* m,

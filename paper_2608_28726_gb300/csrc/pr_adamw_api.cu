@@ -231,12 +231,12 @@ pr_status pr_adamw_step(pr_ctx* c, const pr_adamw_tensor* tensors, int32_t n_ten
 
 pr_status pr_adamw_unpack(pr_ctx* c, const pr_adamw_tensor* tensors, int32_t n_tensors, float* m,
                           float* v, void* stream) {
-  if (!c || n_tensors < 0 || (n_tensors > 0 && (!tensors || !m || !v))) return PR_ERR_INVALID_ARG;
+  if (!c || n_tensors < 0 || (n_tensors > 0 && !tensors)) return PR_ERR_INVALID_ARG;
   if (!fits(m, 4) || !fits(v, 4)) return PR_ERR_INVALID_ARG;
   for (int32_t i = 0; i < n_tensors; ++i) {
     const pr_status st = check(tensors[i]);
     if (st != PR_OK) return st;
-    if (tensors[i].state_bits != 8) return PR_ERR_INVALID_ARG;
+    if (tensors[i].state_bits != 8 || (tensors[i].n > 0 && (!m || !v))) return PR_ERR_INVALID_ARG;
   }
   pr_status st = set_device(c);
   if (st != PR_OK) return st;

@@ -504,3 +504,23 @@ def test_every_scale_holds_its_values(B, ctx, scale):
     assert m[255] == 127 and v[255] == 255
     for x in s:
         assert abs(x.item() / np.float32(scale) - 1.0) <= 1e-6 + (9 * 2.0 ** -149) / scale
+
+
+def test_tensors_without_elements(B, ctx):
+    """They step and expand to nothing, alone and among others."""
+    e = Tensors([0, 0], "f32", "f32", False, 8, 1)
+    for t in (e.table(B), B.pr_adamw_tensors([], [], [], [])):
+        n0 = B.launch_count()
+        B.pr_adamw_step(ctx, t, **HYPER)
+        m, v = B.pr_adamw_unpack(ctx, t)
+        assert m.shape == v.shape == (0, 256) and B.launch_count() == n0
+    a, b = Tensors([0, 300, 0], "f32", "f32", False, 8, 1), Tensors([300], "f32", "f32", False, 8, 1)
+    a.m[1], a.v[1], a.m_scale[1], a.v_scale[1] = b.m[0], b.v[0], b.m_scale[0], b.v_scale[0]
+    for x, y in zip(B.pr_adamw_unpack(ctx, a.table(B)), B.pr_adamw_unpack(ctx, b.table(B))):
+        assert x.shape == (2, 256) and torch.equal(x, y)
+    # the library itself: no output for tensors that have elements
+    t = b.table(B)
+    out = torch.empty(2, 256, device="cuda")
+    lib, addr = B._lib, B._adamw_table("", 0, t)
+    for m, v in ((None, out.data_ptr()), (out.data_ptr(), None)):
+        assert lib.pr_adamw_unpack(ctx, addr, 1, m, v, None) == B.PR_ERR_INVALID_ARG
