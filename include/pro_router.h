@@ -550,7 +550,7 @@ pr_status pr_policy_loss(pr_ctx* ctx, const void* logits, pr_dtype dt, int64_t n
                          const pr_policy* params, float* stats, float* logp, void* grad,
                          int64_t grad_stride, void* stream);
 
-#define PR_PREF_SIGMOID 0 /* -(1 - e) log sigmoid(h) - e log sigmoid(-h) */
+#define PR_PREF_SIGMOID 0 /* -(1 - e) log sigmoid(h) - e log sigmoid(-h); a term of weight 0 is 0 */
 #define PR_PREF_SQUARED 1 /* (d - 1 / (2 beta))^2 */
 #define PR_PREF_HINGE 2   /* max(0, 1 - h) */
 

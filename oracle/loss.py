@@ -118,13 +118,14 @@ def preference(x, chosen, offsets, ref_logp=None, mask=None, beta=0.1, loss=SIGM
         d = s[i] - s[i + 1]
         h = beta * d - margin
         if loss == SIGMOID:
-            f = (1 - label_smoothing) * np.logaddexp(0, -h) + label_smoothing * np.logaddexp(0, h)
+            f = sum(w * np.logaddexp(0, z) for w, z in ((1 - label_smoothing, -h),
+                                                        (label_smoothing, h)) if w != 0)
             slope = beta * (label_smoothing * np.exp(-np.logaddexp(0, -h))
                             - (1 - label_smoothing) * np.exp(-np.logaddexp(0, h)))
         elif loss == SQUARED:
             f, slope = (d - 0.5 / beta) ** 2, 2 * (d - 0.5 / beta)
         else:
-            f, slope = (h if np.isnan(h) else max(0.0, 1 - h)), (-beta if h < 1 else 0.0 * h)
+            f, slope = (h, h) if np.isnan(h) else (max(0.0, 1 - h), -beta if h < 1 else 0.0)
         stats += np.array([f, float(d > 0), h, beta * s[i], beta * s[i + 1]]) / len(pairs)
         for r, sign in ((i, 1.0), (i + 1, -1.0)):
             side[r] = sign * slope / len(pairs) / (count[r] if length_norm else 1)

@@ -1561,7 +1561,9 @@ static __global__ void __launch_bounds__(64 * PR_PAIRS) loss_pairs(const LossArg
       float f, slope;  // loss and d loss / d d
       if (a.loss == 0) {
         const float e = log1pf(expf(-fabsf(h)));
-        f = (1.f - a.smooth) * (e + fmaxf(-h, 0.f)) + a.smooth * (e + fmaxf(h, 0.f));
+        const float up = e + fmaxf(-h, 0.f), down = e + fmaxf(h, 0.f);
+        // (either may be infinite: a masked emitted token; without weight it is no part)
+        f = (a.smooth < 1.f ? (1.f - a.smooth) * up : 0.f) + (a.smooth > 0.f ? a.smooth * down : 0.f);
         slope = a.beta * (a.smooth / (1.f + expf(-h)) - (1.f - a.smooth) / (1.f + expf(h)));
       } else if (a.loss == 1) {
         const double q = d - 0.5 / (double)a.beta;

@@ -912,3 +912,29 @@ def test_a_batch_without_rows_has_its_own_kernel_times(B):
     B.pr_policy_loss(c, x[:0], to(ch), to(old), offsets=to([0, 0], np.int64))
     assert len(B.pr_ctx_kernel_times(c)) == 1
     B.pr_ctx_destroy(c)
+
+
+@pytest.mark.parametrize("n,V", [(12, 701), (700, 43)])
+@pytest.mark.parametrize("kind,smooth", [(0, 0.0), (0, 0.1), (0, 1.0), (1, 0.0), (2, 0.0)])
+@pytest.mark.parametrize("side", [0, 1])
+def test_masked_emitted_token_in_an_answer(B, ctx, n, V, kind, smooth, side):
+    """An answer with a token that the model has masked has the log ratio -inf: the loss of its
+    pair is 0 or infinite as the formulas say, and no part of it is 0 times infinity."""
+    g, x, _, ch, _, ref = draw(n + V, n, V, "f32")
+    off = [0, n // 4, n // 2, 3 * n // 4, n]
+    t = off[side] + 1
+    x[t, ch[t]] = -torch.inf
+    kw = dict(loss=kind, label_smoothing=smooth, beta=0.2)
+    st, r, lp, gr = B.pr_preference_loss(ctx, x, to(ch), to(off, np.int64), ref_logp=to(ref), **kw)
+    s, ro, lo, go = L.preference(f64(x), ch, off, ref, **kw)
+    got = f64(st)
+    assert not np.isnan(s[:2]).any() and (got[np.isinf(s)] == s[np.isinf(s)]).all()
+    fin = torch.from_numpy(np.isfinite(s))
+    check_stats(st.cpu()[fin], s[np.isfinite(s)], 1.0 + 0.2 * np.abs(ro[2:]).max() + (
+        (3.0 * np.abs(ro[2:]).max() + 25.0) if kind == 1 else 0.0))
+    check_rows(lp, lo, None, None, "f32")
+    rest = slice(off[2], n)
+    check_rows(lp[rest], lo[rest], gr[rest], go[rest], "f32")
+    if kind != 1:  # (the squared loss' slope is infinite)
+        check_rows(lp, lo, gr, go, "f32")
+    assert B.pr_ctx_flags(ctx, clear=True) == 0

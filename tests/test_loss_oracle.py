@@ -106,3 +106,12 @@ def test_rows_belong_to_one_request():
         assert (count == [(req == r).sum() for r in range(5)]).all()
     req, count = L.counted(10, None, [0, 6, 3, 10])
     assert req.tolist() == [0] * 6 + [2] * 4 and count.tolist() == [6, 0, 4]
+
+
+def test_a_term_of_no_weight_is_no_part_of_the_pair_loss():
+    x = np.random.Generator(np.random.PCG64(8)).normal(size=(4, 5))
+    x[3, 0] = -np.inf  # the other answer has a masked token: h is infinite
+    assert L.preference(x, [0] * 4, [0, 2, 4])[0][0] == 0.0
+    assert L.preference(x, [0] * 4, [0, 2, 4], label_smoothing=0.1)[0][0] == np.inf
+    assert L.preference(x[::-1], [0] * 4, [0, 2, 4], label_smoothing=1.0)[0][0] == 0.0
+    assert np.isinf(L.preference(x[::-1], [0] * 4, [0, 2, 4])[0][0])
