@@ -364,7 +364,8 @@ __device__ __forceinline__ PolicyTerms policy_terms(const LossArgs& a, float l, 
   PolicyTerms p;
   p.d = a.old_logp ? (l - old) + l_lo : l - l;  // (NaN for a row without l)
   p.ratio = expf(p.d);
-  const float free = p.ratio * adv;
+  // (a ratio beyond single precision under an advantage of 0: its surrogate is 0)
+  const float free = p.ratio == INFINITY && adv == 0.f ? 0.f : p.ratio * adv;
   const float bound = fminf(fmaxf(p.ratio, a.clip_lo), a.clip_hi) * adv;
   p.clipped = bound < free ? 1.f : 0.f;
   p.surrogate = bound < free ? bound : free;

@@ -938,3 +938,28 @@ def test_masked_emitted_token_in_an_answer(B, ctx, n, V, kind, smooth, side):
     if kind != 1:  # (the squared loss' slope is infinite)
         check_rows(lp, lo, gr, go, "f32")
     assert B.pr_ctx_flags(ctx, clear=True) == 0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,V", KERNELS)
+def test_no_advantage_under_a_ratio_out_of_range(B, ctx, n, V, dtype):
+    """r = e^200 is beyond single precision, and r times an advantage of 0 is 0."""
+    g, x, x64, ch, old, ref = draw(n + V, n, V, dtype)
+    adv = g.normal(size=n).astype(np.float32)
+    adv[1] = 0.0
+    old[1] -= 200.0
+    for beta, r in ((0.0, None), (0.1, ref)):
+        for want_grad in (True, False):
+            st, lp, gr = B.pr_policy_loss(ctx, x, to(ch), to(adv), old_logp=to(old), ref_logp=to(r),
+                                          kl_coef=beta, want_grad=want_grad, **CLIP)
+            s, l, go = L.policy(x64, ch, adv, old, r, kl_coef=beta, **CLIP)
+            check_rows(lp, l, gr, go, dtype)
+            check_stats(st[:3], s[:3], 2.0)
+            assert f64(st)[B.PR_POL_RATIO] == np.inf
+    assert B.pr_ctx_flags(ctx, clear=True) == 0
+    # a row of NaN stays NaN whatever its advantage
+    x = x.clone()
+    x[1, 0] = torch.nan
+    st, lp, gr = B.pr_policy_loss(ctx, x, to(ch), to(adv), old_logp=to(old))
+    assert torch.isnan(st[0]) and torch.isnan(gr[1]).all() and torch.isfinite(gr[0]).all()
+    assert B.pr_ctx_flags(ctx, clear=True) == B.PR_FLAG_NONFINITE
