@@ -326,8 +326,9 @@ int64_t pr_head_param_count(int32_t n_layers);
  * bounded wait on the tensor cores that runs out raises PR_FLAG_TIMEOUT in
  * the context's flag word (that call's outputs are invalid).  The
  * context holds a device scratch of 1 KB per row, allocated (or grown) by the
- * first call with more rows than before -- that call synchronises the device;
- * calls on different streams must not overlap (they share that scratch).
+ * first call with more rows than before -- that call synchronises the device and cannot
+ * be captured, and graphs captured before it hold the old scratch: capture them
+ * again; calls on different streams must not overlap (they share that scratch).
  */
 pr_status pr_head_score(pr_ctx* ctx, const float* feat, const uint32_t* row_flags,
                         int64_t n_rows, const int64_t* offsets, int32_t n_req, const float* w,
@@ -356,9 +357,9 @@ pr_status pr_head_score(pr_ctx* ctx, const float* feat, const uint32_t* row_flag
  * fp32 logits; uses the context's PR_OPT_TOPK_RENORM.  Two launches on
  * `stream` (the first in thread-block clusters of two CTAs sharing each
  * tcgen05 MMA); the context holds a state buffer of 288 bytes per row and
- * vocabulary split (grown on demand; that call synchronises the device).  A
- * device-side wait that runs out (2 s) raises PR_FLAG_TIMEOUT in the context
- * flag word.
+ * vocabulary split (grown on demand; that call synchronises the device and cannot be
+ * captured, and graphs captured before it have to be captured again).  A device-side
+ * wait that runs out (2 s) raises PR_FLAG_TIMEOUT in the context flag word.
  */
 pr_status pr_lmhead_features(pr_ctx* ctx, const void* hidden, const void* weight, int64_t n_rows,
                              int64_t d, int64_t vocab, const int32_t* chosen, int32_t topk,
@@ -498,8 +499,10 @@ pr_status pr_selective_metrics(pr_ctx* ctx, const float* scores, const uint8_t* 
  *     stride; otherwise the two must not overlap.  Written fastest where a
  *     row of grad and its logits have the same address modulo 16.
  *   - stats: device float [PR_NPOL / PR_NPREF]; logp: device float [n_rows].
- *     Statistics are summed in fp64 in an order that depends on the sizes alone:
- *     results are bit-reproducible.
+ *     Statistics are summed in fp32 with what the roundings lose beside it, then in fp64
+ *     over CTAs (the pairs' in fp64), exponentials are within 2^-22.  All sums run in an
+ *     order that depends on the sizes and on which rows count: results are
+ *     bit-reproducible, and the same with and without a gradient.
  *   - the context holds a workspace (48 bytes per row, 20 per request), allocated or grown
  *     by the first call that needs more, at least to twice what it was -- that call
  *     waits for the allocation and may be captured.  What it has outgrown is kept until
@@ -609,24 +612,29 @@ typedef struct {
 } pr_adamw_tensor;
 
 /*
- * One AdamW step, in fp32, over n_tensors tensors (host array, read during the
- * call; tensors of different types may be mixed):
+ * One AdamW step over n_tensors tensors (host array, read during the call; tensors of
+ * different types may be mixed):
  *   g = grad * *grad_scale;  m = beta1 m + (1 - beta1) g;  v = beta2 v + (1 - beta2) g^2;
  *   p = p - lr ((m / (1 - beta1^step)) / (sqrt(v / (1 - beta2^step)) + eps) + weight_decay p)
- * p is the master copy where there is one, param its rounding to bf16; without
- * one, param itself, rounded to its type.
+ * in fp32; from eps 1e-12 on the quotient's root and reciprocal are approximate, within
+ * 2^-21 of it together.  p is the master copy where there is one, param its rounding to
+ * bf16; without one, param itself, rounded to its type.
  *   grad_scale  device float or NULL (1): e.g. the clip coefficient of the
  *               gradients' norm
  *   step        >= 1, this step's number;  beta1, beta2 in [0, 1), eps >= 0
+ * step and the coefficients are values of the call: a captured one repeats them, so a
+ * graph of training steps has to be captured with the steps it stands for (grad_scale is
+ * read on the device).
  * 8-bit states, per block of 256 elements (a tensor's last one may be shorter)
  * with the block's largest magnitude as its scale:
  *   m: code q = round(127 sqrt(|m| / scale)) with m's sign, value q |q| scale / 127^2
  *   v: code q = round(255 (v / scale)^(1/4)), value q^4 scale / 255^4
- * rounded to nearest, ties to even.  All-zero codes and scales are the states
- * before the first step.  A block without a normal number is held as zeros, one with
- * NaN or an infinity with scale NaN: its values are NaN from then on and the
- * call raises PR_FLAG_NONFINITE (context flag word).  The parameters step with the new
- * states before their rounding.
+ * rounded to nearest, ties to even.  The roots are fp32 ones: the code is the other
+ * neighbour's at most where the exact root lies within 1e-4 of a tie.  All-zero codes
+ * and scales are the states before the first step.  A block without a normal number is
+ * held as zeros, one with NaN or an infinity with scale NaN: its values are NaN from then
+ * on and the call raises PR_FLAG_NONFINITE (context flag word).  The parameters step with
+ * the new states before their rounding.
  * One launch per 384 tensors of the same types, no workspace.  Tensors whose pointers
  * are multiples of 32 bytes (16 for bf16 and for codes) are read and written fastest; any
  * other address of an element will do.
@@ -639,8 +647,7 @@ pr_status pr_adamw_step(pr_ctx* ctx, const pr_adamw_tensor* tensors, int32_t n_t
  * The values that 8-bit states stand for (checkpoints, a change of the states'
  * type): m, v device float [blocks][256], the tensors' blocks one after another,
  * blocks = sum of ceil(n / 256); past a tensor's end its last block is zero.  They may be
- * NULL where there is no block.
- * Every tensor must have state_bits 8.
+ * NULL where there is no block.  Every tensor must have state_bits 8.
  */
 pr_status pr_adamw_unpack(pr_ctx* ctx, const pr_adamw_tensor* tensors, int32_t n_tensors, float* m,
                           float* v, void* stream);

@@ -12,9 +12,10 @@
 //   v: q = round(255 (v / max)^(1/4)),               held value q^4 max / 255^4
 // Equal steps of the root put the codes where the values are: a v of 4e-9 of the
 // block's largest still has a code of its own (its square root divides the
-// update), an m of 6e-5.  All products, roots and roundings of the states are IEEE single
-// operations in the order written, so that the codes do not depend on how a compiler
-// contracts them.
+// update), an m of 6e-5.  All products, sums and roundings of the states are IEEE single
+// operations in the order written, so that the states do not depend on how a compiler
+// contracts them, and the codes are those of IEEE roots (codes_of).  The parameters'
+// update takes approximate roots and reciprocals (EPS_FAST).
 #pragma once
 
 #include <type_traits>
