@@ -592,6 +592,135 @@ pr_status pr_preference_loss(pr_ctx* ctx, const void* logits, pr_dtype dt, int64
                              float* ratio, float* logp, void* grad, int64_t grad_stride,
                              void* stream);
 
+/* ---- the first logits of a row, and distillation from them ----------------------------- */
+
+#define PR_MAX_LISTED 64 /* largest k of the two calls below */
+
+/*
+ * What a model's answer can be sent with: the k largest logits of each row, as the tokens
+ * and their log-probabilities (the large model's, for pr_distill_loss; or a client's
+ * "first tokens").
+ *   logits       as in pr_token_features; z = x / temperature
+ *   k            1 .. PR_MAX_LISTED
+ *   temperature  1e-3 .. 1e3
+ *   ids          device int32 [n_rows][k]: tokens in the order (logit descending, id
+ *                ascending)                                                   (output)
+ *   logp         device float [n_rows][k]: z_v - log sum_u exp(z_u)           (output)
+ * z from 1e9 on counts as +inf, from -1e9 down (so the type's lowest value) as -inf: masked,
+ * never listed.  Where fewer than k are left the list ends with id -1 and log-probability -inf.
+ * A row with NaN or +inf, or with nothing finite, has ids -1 and log-probabilities NaN
+ * (PR_FLAG_NONFINITE in the context flag word).  Orders are exact; sums are fp32, in an order that depends on
+ * the sizes alone.  n_rows < 2^31; one launch, no workspace.
+ */
+pr_status pr_top_logits(pr_ctx* ctx, const void* logits, pr_dtype dt, int64_t n_rows,
+                        int64_t vocab, int64_t row_stride, int32_t k, float temperature,
+                        int32_t* ids, float* logp, void* stream);
+
+#define PR_DISTILL_FORWARD 0 /* KL(large || small) */
+#define PR_DISTILL_REVERSE 1 /* KL(small || large) */
+#define PR_REST_CLASS 0 /* all tokens that are not listed are one class more */
+#define PR_REST_NONE 1  /* the listed ones are the whole distribution, renormalised */
+
+#define PR_NDIS 5
+#define PR_DIS_LOSS 0    /* the loss */
+#define PR_DIS_KL 1      /* mean divergence */
+#define PR_DIS_CE 2      /* mean of -l_y (0 without chosen) */
+#define PR_DIS_LISTED 3  /* mean of the large model's probability of the listed tokens, as given */
+#define PR_DIS_COVERED 4 /* mean of the small model's probability of them */
+
+#define PR_DISTILL_MAX_VOCAB 393216 /* 3 x 2^17: rows that the SMs of a cluster hold */
+
+typedef struct {
+  float kl_coef;     /* >= 0 */
+  float ce_coef;     /* >= 0, of the hard labels; needs chosen */
+  float temperature; /* T, 1e-3 .. 1e3; of both terms */
+  float grad_scale;  /* finite */
+  int32_t loss;      /* PR_DISTILL_* */
+  int32_t rest;      /* PR_REST_* */
+  int32_t norm;      /* PR_NORM_* */
+} pr_distill;
+
+/*
+ * Distillation of the small model from a large one's first logits, and its gradient.
+ * Row t lists tokens S with the large model's log-probabilities t_v (at this call's
+ * temperature); p_v = exp(t_v), q = softmax(x / T), l = log q, rho = max(1 - sum_S p, 2^-24)
+ * (below that it is what the roundings of the t_v leave) and sigma = the sum of q outside S.
+ *   PR_DISTILL_FORWARD  KL = sum_S p (t - l)  + rho (log rho - log sigma)
+ *   PR_DISTILL_REVERSE  KL = sum_S q (l - t)  + sigma (log sigma - log rho)
+ * with PR_REST_NONE without the second term and with p, and in the reverse direction q,
+ * divided by their sums over S (the t_v may then be logits / T: a constant drops out).
+ *   loss = mean over the counted rows, as norm says, of kl_coef KL + ce_coef (-l_y);
+ *   a term with coefficient 0 is a statistic alone, whatever its value.
+ *   logits, mask, offsets, grad, workspace, sums: as "common to both losses" above says, but
+ *              that vocab <= PR_DISTILL_MAX_VOCAB and that x / T from 1e9 on counts as +inf,
+ *              from -1e9 down as -inf
+ *   ids        device int32 [n_rows][k], 1 <= k <= PR_MAX_LISTED, in any order.  An entry
+ *              with id -1, or with log-probability -inf, is absent; a row without entries
+ *              has KL 0 and no gradient of it.
+ *   t_logp     device float [n_rows][k]
+ *   chosen     device int32 [n_rows], the hard labels y, or NULL
+ *   kl         device float [n_rows]: each row's KL, 0 where the row does not count (output)
+ * Where every token outside S is masked there is no class of the rest.  A counted row has
+ * KL and gradient NaN, and so have the statistics that it enters, if it has NaN or +inf or nothing finite among its logits
+ * or NaN or +inf among its t_logp, or reverse with PR_REST_NONE and no listed token unmasked (PR_FLAG_NONFINITE), or
+ * an id outside the vocabulary, one listed twice or a label outside the vocabulary
+ * (PR_FLAG_BAD_CHOSEN).  n_rows < 2^31.
+ */
+pr_status pr_distill_loss(pr_ctx* ctx, const void* logits, pr_dtype dt, int64_t n_rows,
+                          int64_t vocab, int64_t row_stride, const int32_t* ids,
+                          const float* t_logp, int32_t k, const int32_t* chosen,
+                          const uint8_t* mask, const int64_t* offsets, int32_t n_req,
+                          const pr_distill* params, float* stats, float* kl, void* grad,
+                          int64_t grad_stride, void* stream);
+
+/* ---- the norm before the LM head -------------------------------------------------------- */
+
+#define PR_NORM_MAX_D (1 << 20) /* largest width */
+
+/*
+ * Layer norm, or RMS norm, of rows of width d, a residual added first (what pr_lmhead_*
+ * takes as hidden states):
+ *   h = x + residual, rounded to the rows' type;  m = mean(h), or 0 with rms;
+ *   rstd = 1 / sqrt(mean((h - m)^2) + eps);  y = (h - m) rstd weight + bias
+ * in fp32, y rounded once; the sums are of h - m itself, not of squares less a square.
+ *   x, residual, total, y   device [n_rows][stride] of type dt, strides >= d; residual may
+ *                be NULL.  total receives h, or is NULL
+ *   weight, bias device [d] of type wdt; bias may be NULL
+ *   eps          >= 0, finite
+ *   mean, rstd   device float [n_rows] for the backward pass, or NULL (mean is not written with rms)
+ * total and y may each be the buffer of x or of residual, with the same stride; else outputs overlap
+ * nothing.  Any element alignment; rows whose bases and strides are multiples of 16 bytes are
+ * read and written fastest.  n_rows < 2^31, 1 <= d <= PR_NORM_MAX_D.  One launch, no workspace;
+ * NaN and infinities stay in their rows.
+ */
+pr_status pr_layernorm(pr_ctx* ctx, const void* x, pr_dtype dt, int64_t n_rows, int64_t d,
+                       int64_t x_stride, const void* residual, int64_t residual_stride,
+                       const void* weight, const void* bias, pr_dtype wdt, float eps, int32_t rms,
+                       void* total, int64_t total_stride, void* y, int64_t y_stride, float* mean,
+                       float* rstd, void* stream);
+
+/*
+ * The backward pass, from the rows that were normalised (x or total), mean and rstd:
+ *   xhat = (x - mean) rstd, g = dy weight;
+ *   dx = rstd (g - mean(g) - xhat mean(g xhat)) + dtotal   (with rms without mean(g))
+ *   dweight = sum over the rows of dy xhat, dbias = sum of dy
+ *   dy, x, dtotal, dx   device [n_rows][stride] of type dt; dtotal (the gradient that reaches
+ *                total by other ways) may be NULL; dx may be NULL, or the buffer of
+ *                dy, x or dtotal with the same stride
+ *   mean         device float [n_rows] (not read with rms, may then be NULL); rstd [n_rows]
+ *   dweight, dbias  device float [d] or NULL; with accumulate they are added to
+ * One of dx, dweight, dbias must be asked for.  Sums are fp32 in an order that depends on the
+ * sizes alone: results are bit-reproducible.  The context holds a workspace (up to 16 bytes
+ * per column and SM), allocated or grown by the first call that needs more, as the training losses'; calls and
+ * replays on different streams must not overlap (they share it).
+ */
+pr_status pr_layernorm_backward(pr_ctx* ctx, const void* dy, int64_t dy_stride, const void* x,
+                                int64_t x_stride, pr_dtype dt, int64_t n_rows, int64_t d,
+                                const void* weight, pr_dtype wdt, const float* mean,
+                                const float* rstd, int32_t rms, const void* dtotal,
+                                int64_t dtotal_stride, void* dx, int64_t dx_stride,
+                                float* dweight, float* dbias, int32_t accumulate, void* stream);
+
 /* ---- optimiser step over many tensors ------------------------------------------------- */
 
 #define PR_ADAMW_BLOCK 256 /* elements that share the scale of an 8-bit state */

@@ -32,6 +32,11 @@ PR_NPOL, PR_NPREF = 6, 5
  PR_POL_OLD_KL) = range(PR_NPOL)
 PR_PREF_LOSS, PR_PREF_ACCURACY, PR_PREF_H, PR_PREF_REWARD_W, PR_PREF_REWARD_L = range(PR_NPREF)
 PR_ADAMW_BLOCK = 256
+PR_MAX_LISTED, PR_DISTILL_MAX_VOCAB, PR_NORM_MAX_D = 64, 3 << 17, 1 << 20
+PR_DISTILL_FORWARD, PR_DISTILL_REVERSE = 0, 1
+PR_REST_CLASS, PR_REST_NONE = 0, 1
+PR_NDIS = 5
+PR_DIS_LOSS, PR_DIS_KL, PR_DIS_CE, PR_DIS_LISTED, PR_DIS_COVERED = range(PR_NDIS)
 
 # every symbol include/pro_router.h declares
 EXPORTS = (
@@ -43,7 +48,8 @@ EXPORTS = (
     "pr_selftest_wait", "pr_lmhead_decode_step", "pr_last_error", "pr_prescorer_fit",
     "pr_prescorer_destroy", "pr_prescorer_vocab_size", "pr_prescorer_term",
     "pr_prescorer_features", "pr_prescorer_score", "pr_policy_loss", "pr_preference_loss",
-    "pr_adamw_step", "pr_adamw_unpack",
+    "pr_adamw_step", "pr_adamw_unpack", "pr_top_logits", "pr_distill_loss", "pr_layernorm",
+    "pr_layernorm_backward",
 )
 
 if not os.path.exists(LIB):
@@ -91,6 +97,13 @@ _SIGS = {
     "pr_adamw_step": [_P, _P, _I32, ctypes.c_double, ctypes.c_double, ctypes.c_double,
                       ctypes.c_double, _I64, _P, _P],
     "pr_adamw_unpack": [_P, _P, _I32, _P, _P, _P],
+    "pr_top_logits": [_P, _P, ctypes.c_int, _I64, _I64, _I64, _I32, _F32, _P, _P, _P],
+    "pr_distill_loss": [_P, _P, ctypes.c_int, _I64, _I64, _I64, _P, _P, _I32, _P, _P, _P, _I32, _P,
+                        _P, _P, _P, _I64, _P],
+    "pr_layernorm": [_P, _P, ctypes.c_int, _I64, _I64, _I64, _P, _I64, _P, _P, ctypes.c_int, _F32,
+                     _I32, _P, _I64, _P, _I64, _P, _P, _P],
+    "pr_layernorm_backward": [_P, _P, _I64, _P, _I64, ctypes.c_int, _I64, _I64, _P, ctypes.c_int,
+                              _P, _P, _I32, _P, _I64, _P, _I64, _P, _P, _I32, _P],
 }
 for _name, _args in _SIGS.items():
     _fn = getattr(_lib, _name)
@@ -720,6 +733,171 @@ def pr_preference_loss(ctx, logits, chosen, offsets, ref_logp=None, mask=None, b
                                    mask_p, offsets_p, n_req, ref_p, ctypes.byref(p), stats_p,
                                    ratio_p, logp_p, grad_p, gs, _stream(stream)), call)
     return stats, ratio, logp, grad
+
+
+# ---- the first logits of a row, and distillation from them -------------------------------------
+
+class PrDistill(ctypes.Structure):
+    _fields_ = [("kl_coef", _F32), ("ce_coef", _F32), ("temperature", _F32),
+                ("grad_scale", _F32), ("loss", _I32), ("rest", _I32), ("norm", _I32)]
+
+
+def pr_top_logits(ctx, logits, k: int, temperature: float = 1.0, ids=None, logp=None, vocab=None,
+                  stream=None):
+    """The k largest logits of each row: (ids int32 [n, k], log-probabilities
+    float32 [n, k]), largest first, of equal ones the lowest token."""
+    call = "pr_top_logits"
+    dev = _ctx_device(ctx)
+    _logits(call, dev, logits)
+    n, width = logits.shape if logits.dim() == 2 else (0, 0)
+    V = width if vocab is None else int(vocab)
+    stride = _loss_rows(call, logits, "logits", n, V)
+    k = int(k)
+    if not 1 <= k <= PR_MAX_LISTED:
+        raise PRError(PR_ERR_INVALID_ARG, call, "k must be 1 .. %d, got %d" % (PR_MAX_LISTED, k))
+    if ids is None:
+        ids = torch.empty(n, k, dtype=torch.int32, device=logits.device)
+    if logp is None:
+        logp = torch.empty(n, k, dtype=torch.float32, device=logits.device)
+    _check(_lib.pr_top_logits(ctx, logits.data_ptr(), _dtype(logits), n, V, stride, k, temperature,
+                              _dptr(call, dev, "ids", ids, _I32_T, n * k),
+                              _dptr(call, dev, "logp", logp, _F32_T, n * k), _stream(stream)), call)
+    return ids, logp
+
+
+def pr_distill_loss(ctx, logits, ids, t_logp, chosen=None, mask=None, offsets=None,
+                    kl_coef: float = 1.0, ce_coef: float = 0.0, temperature: float = 1.0,
+                    loss: int = PR_DISTILL_FORWARD, rest: int = PR_REST_CLASS,
+                    norm: int = PR_NORM_TOKENS, grad_scale: float = 1.0, stats=None, kl=None,
+                    grad=None, want_grad: bool = True, vocab=None, stream=None):
+    """Loss of logit rows against a large model's first tokens `ids` [n, k] and
+    their log-probabilities `t_logp` [n, k], as pr_top_logits gives them: (stats
+    float32 [PR_NDIS], the rows' divergences float32 [n], gradient of the logits
+    or None).  `chosen`: hard labels, weighted by `ce_coef`; `grad` may be
+    `logits` itself."""
+    call = "pr_distill_loss"
+    dev = _ctx_device(ctx)
+    _logits(call, dev, logits)
+    n, width = logits.shape if logits.dim() == 2 else (0, 0)
+    V = width if vocab is None else int(vocab)
+    stride = _loss_rows(call, logits, "logits", n, V)
+    n_req = 0 if offsets is None else offsets.numel() - 1
+    k = ids.shape[1] if isinstance(ids, torch.Tensor) and ids.dim() == 2 else 0
+    for name, t in (("ids", ids), ("t_logp", t_logp)):
+        if not isinstance(t, torch.Tensor) or t.dim() != 2 or t.shape[0] < n or t.shape[1] != k:
+            raise PRError(PR_ERR_INVALID_ARG, call, "%s must be [%d][k], of one k" % (name, n))
+    ids_p = _dptr(call, dev, "ids", ids, _I32_T, n * k)
+    t_p = _dptr(call, dev, "t_logp", t_logp, _F32_T, n * k)
+    chosen_p = _dptr_opt(call, dev, "chosen", chosen, _I32_T, n)
+    mask_p = _dptr_opt(call, dev, "mask", mask, _U8_T, n)
+    offsets_p = _dptr_opt(call, dev, "offsets", offsets, _I64_T, 0)
+    stats, stats_p = _loss_out(call, dev, "stats", stats, PR_NDIS, logits.device)
+    kl, kl_p = _loss_out(call, dev, "kl", kl, n, logits.device)
+    grad, grad_p, gs = _loss_grad(call, dev, logits, n, V, stride, grad, want_grad)
+    p = PrDistill(kl_coef, ce_coef, temperature, grad_scale, loss, rest, norm)
+    _check(_lib.pr_distill_loss(ctx, logits.data_ptr(), _dtype(logits), n, V, stride, ids_p, t_p, k,
+                                chosen_p, mask_p, offsets_p, n_req, ctypes.byref(p), stats_p, kl_p,
+                                grad_p, gs, _stream(stream)), call)
+    return stats, kl, grad
+
+
+# ---- the norm before the LM head ---------------------------------------------------------------
+
+_ROWS_T = (torch.float32, torch.bfloat16)
+
+
+def _norm_rows(call, dev, name, t, like=None):
+    """(address, stride) of rows [n][d], or (None, 0) for an absent tensor."""
+    if t is None:
+        return None, 0
+    _dev(call, dev, name, t, _ROWS_T if like is None else (like.dtype,), contiguous=False)
+    if t.dim() != 2 or t.shape[1] < 1 or (like is not None and t.shape != like.shape):
+        raise PRError(PR_ERR_INVALID_ARG, call, "%s must be 2-D%s" % (
+            name, "" if like is None else ", %s" % list(like.shape)))
+    d = t.shape[1]
+    if (d > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < d):
+        raise PRError(PR_ERR_INVALID_ARG, call, "%s must have unit stride along its rows, which "
+                      "must not overlap" % name)
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else d
+
+
+def _norm_weights(call, dev, d, weight, bias=None):
+    w = _dptr(call, dev, "weight", weight, _ROWS_T, d)
+    b = _dptr_opt(call, dev, "bias", bias, (weight.dtype,), d)
+    for name, t in (("weight", weight), ("bias", bias)):
+        if t is not None and t.numel() != d:
+            raise PRError(PR_ERR_INVALID_ARG, call, "%s holds %d elements for rows of %d" % (
+                name, t.numel(), d))
+    return w, b, _dtype(weight)
+
+
+def pr_layernorm(ctx, x, weight, bias=None, residual=None, eps: float = 1e-5, rms: bool = False,
+                 want_stats: bool = True, want_total: bool = True, y=None, total=None, mean=None,
+                 rstd=None, stream=None):
+    """Layer norm, or RMS norm, of the rows of x + residual: (y, the sum or None
+    without a residual, mean float32 [n] or None with `rms`, rstd float32 [n]);
+    the last two for the backward pass, None without `want_stats`.  `y` and
+    `total` may be `x` or `residual` themselves."""
+    call = "pr_layernorm"
+    dev = _ctx_device(ctx)
+    x_p, xs = _norm_rows(call, dev, "x", x)
+    if x_p is None:
+        raise PRError(PR_ERR_INVALID_ARG, call, "x is required")
+    n, d = x.shape
+    w_p, b_p, wdt = _norm_weights(call, dev, d, weight, bias)
+    r_p, rs = _norm_rows(call, dev, "residual", residual, x)
+    if y is None:
+        y = torch.empty(n, d, dtype=x.dtype, device=x.device)
+    if total is None and residual is not None and want_total:
+        total = torch.empty(n, d, dtype=x.dtype, device=x.device)
+    if want_stats:
+        mean = torch.empty(n, dtype=torch.float32, device=x.device) if mean is None and not rms else mean
+        rstd = torch.empty(n, dtype=torch.float32, device=x.device) if rstd is None else rstd
+    y_p, ys = _norm_rows(call, dev, "y", y, x)
+    t_p, ts = _norm_rows(call, dev, "total", total, x)
+    mean_p = _dptr_opt(call, dev, "mean", mean, _F32_T, n)
+    rstd_p = _dptr_opt(call, dev, "rstd", rstd, _F32_T, n)
+    _check(_lib.pr_layernorm(ctx, x_p, _dtype(x), n, d, xs, r_p, rs, w_p, b_p, wdt, eps, bool(rms),
+                             t_p, ts, y_p, ys, mean_p, rstd_p, _stream(stream)), call)
+    return y, total, mean, rstd
+
+
+def pr_layernorm_backward(ctx, dy, x, weight, rstd, mean=None, dtotal=None, rms: bool = False,
+                          accumulate: bool = False, want_dx: bool = True, want_dweight: bool = True,
+                          want_dbias: bool = False, dx=None, dweight=None, dbias=None, stream=None):
+    """The backward pass of pr_layernorm, from the rows it normalised (`x`, or
+    its `total`) and their `mean` (not with `rms`) and `rstd`: (dx, dweight
+    float32 [d], dbias float32 [d]; None for what is not wanted).  `dtotal` is
+    added to dx, which may be `dy`, `x` or `dtotal` itself; with `accumulate`
+    `dweight` and `dbias` are added to."""
+    call = "pr_layernorm_backward"
+    dev = _ctx_device(ctx)
+    x_p, xs = _norm_rows(call, dev, "x", x)
+    if x_p is None:
+        raise PRError(PR_ERR_INVALID_ARG, call, "x is required")
+    n, d = x.shape
+    dy_p, dys = _norm_rows(call, dev, "dy", dy, x)
+    if dy_p is None:
+        raise PRError(PR_ERR_INVALID_ARG, call, "dy is required")
+    w_p, _, wdt = _norm_weights(call, dev, d, weight)
+    t_p, ts = _norm_rows(call, dev, "dtotal", dtotal, x)
+    rstd_p = _dptr(call, dev, "rstd", rstd, _F32_T, n)
+    mean_p = None if rms else _dptr(call, dev, "mean", mean, _F32_T, n)
+    if accumulate and ((want_dweight and dweight is None) or (want_dbias and dbias is None)):
+        raise PRError(PR_ERR_INVALID_ARG, call, "accumulate needs dweight, and dbias where wanted")
+    if dx is None and want_dx:
+        dx = torch.empty(n, d, dtype=x.dtype, device=x.device)
+    if dweight is None and want_dweight:
+        dweight = torch.empty(d, dtype=torch.float32, device=x.device)
+    if dbias is None and want_dbias:
+        dbias = torch.empty(d, dtype=torch.float32, device=x.device)
+    dx_p, dxs = _norm_rows(call, dev, "dx", dx, x)
+    dw_p = _dptr_opt(call, dev, "dweight", dweight, _F32_T, d)
+    db_p = _dptr_opt(call, dev, "dbias", dbias, _F32_T, d)
+    _check(_lib.pr_layernorm_backward(ctx, dy_p, dys, x_p, xs, _dtype(x), n, d, w_p, wdt, mean_p,
+                                      rstd_p, bool(rms), t_p, ts, dx_p, dxs, dw_p, db_p,
+                                      bool(accumulate), _stream(stream)), call)
+    return dx, dweight, dbias
 
 
 # ---- optimiser step over many tensors --------------------------------------------------------

@@ -100,7 +100,7 @@ __device__ __forceinline__ bool bad_bounds(const LossArgs& a, int64_t r, int64_t
 __device__ __forceinline__ void put_row(const LossArgs& a, int64_t t, int32_t r, int32_t before) {
   a.row_req[t] = r;
   if (r >= 0) {
-    a.list[before] = make_int4((int32_t)t, r, a.chosen[t], 0);
+    a.list[before] = make_int4((int32_t)t, r, a.chosen ? a.chosen[t] : -1, 0);
   } else {
     a.skipped[t - before] = (int32_t)t;
     a.logp[t] = 0.f;
@@ -283,7 +283,7 @@ __device__ __forceinline__ void own_plan(const LossArgs& a, OwnPlan& p, bool pai
 #pragma unroll
   for (int k = 0; k < W; ++k) {
     const int64_t t = 32 * (warp + k * NW) + lane;
-    y[k] = t < a.n_rows ? __ldcg(a.chosen + t) : 0;
+    y[k] = t < a.n_rows && a.chosen ? __ldcg(a.chosen + t) : -1;
     r[k] = t < a.n_rows ? counted_by(a, t) : -1;
     const unsigned b = __ballot_sync(FULL, r[k] >= 0);
     if (lane == 0 && warp + k * NW < OWN_MOST / 32) p.on[warp + k * NW] = b;

@@ -1,0 +1,152 @@
+// Host side of pr_layernorm and pr_layernorm_backward: argument checks and the launches of
+// the kernels in pr_norm.cuh.
+#include <cuda_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+
+#include "pr_ctx.h"
+#include "pr_norm.cuh"
+
+using namespace prh;
+
+namespace {
+
+bool type_ok(pr_dtype dt) { return dt == PR_DTYPE_F32 || dt == PR_DTYPE_BF16; }
+size_t esize(pr_dtype dt) { return dt == PR_DTYPE_BF16 ? 2 : 4; }
+bool on_grid(const void* p, pr_dtype dt) { return reinterpret_cast<uintptr_t>(p) % esize(dt) == 0; }
+
+// rows [n][stride] of a call that has any
+bool rows_ok(const void* p, int64_t d, int64_t stride, pr_dtype dt) {
+  return p && stride >= d && on_grid(p, dt);
+}
+// an output that is an input's buffer has its rows where the input has them
+bool same_rows(const void* out, int64_t out_stride, const void* in, int64_t in_stride) {
+  return out != in || out_stride == in_stride;
+}
+
+pr_status finish(pr_ctx* c, cudaStream_t s) {
+  PR_CUDA(cudaGetLastError());
+  g_launches.fetch_add(1, std::memory_order_relaxed);
+  return timing_mark(c, s);
+}
+
+}  // namespace
+
+extern "C" {
+
+pr_status pr_layernorm(pr_ctx* c, const void* x, pr_dtype dt, int64_t n_rows, int64_t d,
+                       int64_t x_stride, const void* residual, int64_t residual_stride,
+                       const void* weight, const void* bias, pr_dtype wdt, float eps, int32_t rms,
+                       void* total, int64_t total_stride, void* y, int64_t y_stride, float* mean,
+                       float* rstd, void* stream) {
+  if (!c || !type_ok(dt) || !type_ok(wdt)) return PR_ERR_INVALID_ARG;
+  if (n_rows < 0 || n_rows > 0x7fffffffLL || d < 1 || d > PR_NORM_MAX_D) return PR_ERR_INVALID_ARG;
+  if (!(eps >= 0.f) || !std::isfinite(eps)) return PR_ERR_INVALID_ARG;
+  if (!weight || !on_grid(weight, wdt) || !on_grid(bias, wdt)) return PR_ERR_INVALID_ARG;
+  if (n_rows > 0) {
+    if (!rows_ok(x, d, x_stride, dt) || !rows_ok(y, d, y_stride, dt) ||
+        (residual && !rows_ok(residual, d, residual_stride, dt)) ||
+        (total && !rows_ok(total, d, total_stride, dt)) || y == total)
+      return PR_ERR_INVALID_ARG;
+    if (!same_rows(y, y_stride, x, x_stride) || !same_rows(y, y_stride, residual, residual_stride) ||
+        (total && (!same_rows(total, total_stride, x, x_stride) ||
+                   !same_rows(total, total_stride, residual, residual_stride))))
+      return PR_ERR_INVALID_ARG;
+  }
+  pr_status st = set_device(c);
+  if (st != PR_OK) return st;
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  if ((st = timing_begin(c, s)) != PR_OK || n_rows == 0) return st;
+  prk::NormArgs a;
+  memset(&a, 0, sizeof a);
+  a.x = x;
+  a.res = residual;
+  a.w = weight;
+  a.b = bias;
+  a.total = total;
+  a.y = y;
+  a.mean = mean;
+  a.rstd = rstd;
+  a.n_rows = n_rows;
+  a.d = d;
+  a.x_stride = x_stride;
+  a.res_stride = residual_stride;
+  a.total_stride = total_stride;
+  a.y_stride = y_stride;
+  a.eps = eps;
+  a.inv_d = (float)(1.0 / (double)d);
+  a.rms = rms ? 1 : 0;
+  a.wide_w = wdt == PR_DTYPE_F32;
+  if (dt == PR_DTYPE_BF16)
+    prk::norm_wide<__nv_bfloat16><<<(unsigned)n_rows, prk::NW_NT, 0, s>>>(a);
+  else
+    prk::norm_wide<float><<<(unsigned)n_rows, prk::NW_NT, 0, s>>>(a);
+  return finish(c, s);
+}
+
+pr_status pr_layernorm_backward(pr_ctx* c, const void* dy, int64_t dy_stride, const void* x,
+                                int64_t x_stride, pr_dtype dt, int64_t n_rows, int64_t d,
+                                const void* weight, pr_dtype wdt, const float* mean,
+                                const float* rstd, int32_t rms, const void* dtotal,
+                                int64_t dtotal_stride, void* dx, int64_t dx_stride, float* dweight,
+                                float* dbias, int32_t accumulate, void* stream) {
+  if (!c || !type_ok(dt) || !type_ok(wdt)) return PR_ERR_INVALID_ARG;
+  if (n_rows < 0 || n_rows > 0x7fffffffLL || d < 1 || d > PR_NORM_MAX_D) return PR_ERR_INVALID_ARG;
+  if (!weight || !on_grid(weight, wdt) || (!dx && !dweight && !dbias)) return PR_ERR_INVALID_ARG;
+  if (n_rows > 0) {
+    if (!rows_ok(dy, d, dy_stride, dt) || !rows_ok(x, d, x_stride, dt) || !rstd || (!mean && !rms) ||
+        (dtotal && !rows_ok(dtotal, d, dtotal_stride, dt)) || (dx && !rows_ok(dx, d, dx_stride, dt)))
+      return PR_ERR_INVALID_ARG;
+    if (dx && (!same_rows(dx, dx_stride, dy, dy_stride) || !same_rows(dx, dx_stride, x, x_stride) ||
+               !same_rows(dx, dx_stride, dtotal, dtotal_stride)))
+      return PR_ERR_INVALID_ARG;
+  }
+  pr_status st = set_device(c);
+  if (st != PR_OK) return st;
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  if ((st = timing_begin(c, s)) != PR_OK) return st;
+  if (n_rows == 0) {
+    for (float* p : {dweight, dbias})
+      if (p && !accumulate) PR_CUDA(cudaMemsetAsync(p, 0, (size_t)d * sizeof(float), s));
+    return PR_OK;
+  }
+  prk::NormArgs a;
+  memset(&a, 0, sizeof a);
+  a.x = x;
+  a.dy = dy;
+  a.res = dtotal;
+  a.w = weight;
+  a.y = dx;
+  a.mean = const_cast<float*>(mean);
+  a.rstd = const_cast<float*>(rstd);
+  a.dw = dweight;
+  a.db = dbias;
+  a.n_rows = n_rows;
+  a.d = d;
+  a.x_stride = x_stride;
+  a.dy_stride = dy_stride;
+  a.res_stride = dtotal_stride;
+  a.y_stride = dx_stride;
+  a.inv_d = (float)(1.0 / (double)d);
+  a.rms = rms ? 1 : 0;
+  a.wide_w = wdt == PR_DTYPE_F32;
+  a.accumulate = accumulate ? 1 : 0;
+  if (dweight || dbias) {  // first: dx may be written over dy and x
+    const unsigned grid = (unsigned)((d + 31) / 32);
+    if (dt == PR_DTYPE_BF16)
+      prk::dnorm_columns<__nv_bfloat16><<<grid, prk::NC_NT, 0, s>>>(a);
+    else
+      prk::dnorm_columns<float><<<grid, prk::NC_NT, 0, s>>>(a);
+    if ((st = finish(c, s)) != PR_OK) return st;
+  }
+  if (!dx) return PR_OK;
+  if (dt == PR_DTYPE_BF16)
+    prk::dnorm_wide<__nv_bfloat16><<<(unsigned)n_rows, prk::NW_NT, 0, s>>>(a);
+  else
+    prk::dnorm_wide<float><<<(unsigned)n_rows, prk::NW_NT, 0, s>>>(a);
+  return finish(c, s);
+}
+
+}  // extern "C"

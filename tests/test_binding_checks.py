@@ -83,3 +83,43 @@ def test_host_call_refuses_device_tensors(monkeypatch):
     x, ch, off, w = _host_batch()
     monkeypatch.setattr(torch.Tensor, "is_cuda", property(lambda self: True))
     _raises_invalid(B.pr_route_host, None, x, ch, off, w, 0.0, 0.5)
+
+
+def test_distillation_and_norm_calls_refuse_host_tensors():
+    x, ch, off, _ = _host_batch()
+    ids, logp = torch.zeros(4, 8, dtype=torch.int32), torch.zeros(4, 8)
+    assert "CUDA tensor" in _raises_invalid(B.pr_top_logits, None, x, 8)
+    _raises_invalid(B.pr_distill_loss, None, x, ids, logp)
+    w = torch.ones(64)
+    assert "CUDA tensor" in _raises_invalid(B.pr_layernorm, None, x, w)
+    _raises_invalid(B.pr_layernorm_backward, None, x, x, w, torch.ones(4), mean=torch.ones(4))
+
+
+def test_sizes_and_types_of_the_distillation_and_norm_calls(monkeypatch):
+    """With the device check passed (faked here), everything else still stops the call."""
+    x, ch, off, _ = _host_batch()
+    monkeypatch.setattr(torch.Tensor, "is_cuda", property(lambda self: True))
+    monkeypatch.setattr(torch.Tensor, "device", property(lambda self: torch.device("cuda", 0)))
+    monkeypatch.setattr(torch.Tensor, "get_device", lambda self: 0)
+    ids, logp = torch.zeros(4, 8, dtype=torch.int32), torch.zeros(4, 8)
+    out = dict(ids=torch.zeros(4, 8, dtype=torch.int32), logp=torch.zeros(4, 8))
+    for k in (0, 65, -3):
+        assert "k must be" in _raises_invalid(B.pr_top_logits, None, x, k)
+    _raises_invalid(B.pr_top_logits, None, x, 9, **out)
+    _raises_invalid(B.pr_top_logits, None, x, 8, vocab=65, **out)
+    _raises_invalid(B.pr_top_logits, None, x.t(), 8, **out)
+    assert "one k" in _raises_invalid(B.pr_distill_loss, None, x, ids, logp[:, :7])
+    _raises_invalid(B.pr_distill_loss, None, x, ids[:3], logp[:3])
+    _raises_invalid(B.pr_distill_loss, None, x, ids.long(), logp)
+    _raises_invalid(B.pr_distill_loss, None, x, ids, logp.double())
+    w, y = torch.ones(64), torch.zeros(4, 64, dtype=torch.bfloat16)
+    m = torch.ones(4)
+    off = dict(y=y, want_stats=False)
+    _raises_invalid(B.pr_layernorm, None, x, w[:63], **off)
+    _raises_invalid(B.pr_layernorm, None, x, w, bias=w.bfloat16(), **off)
+    _raises_invalid(B.pr_layernorm, None, x, w, y=y[:, :63], want_stats=False)
+    _raises_invalid(B.pr_layernorm, None, x, w, residual=y.float(), **off)
+    _raises_invalid(B.pr_layernorm, None, x, w, y=y, mean=m[:3], rstd=m)
+    _raises_invalid(B.pr_layernorm_backward, None, y, x, w, m, dx=y)
+    _raises_invalid(B.pr_layernorm_backward, None, y[:3], x, w, m, mean=m, dx=y)
+    _raises_invalid(B.pr_layernorm_backward, None, y, x, w, m, mean=m, accumulate=True, dx=y)

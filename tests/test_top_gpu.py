@@ -1,0 +1,176 @@
+"""GPU parity of pr_top_logits with the float64 oracle, at the sizes, ties and values where a
+selection can go wrong.  Tokens have to be the oracle's, one by one.  Log-probabilities: a
+row's sum of positive fp32 terms, each off by 2^-22 and by |z - max| 2^-23 (weighted by
+the term itself: below 1e-6), in chains of up to 1,000 terms (6e-5 at worst, the roundings'
+mean far less): 2e-5; the roundings of the difference and of its product: 4e-7 |l|."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import distill as D
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def B():
+    from paper_2608_28726_gb300 import build as prbuild
+    prbuild.build()
+    from paper_2608_28726_gb300 import binding
+    return binding
+
+
+@pytest.fixture(scope="module")
+def ctx(B):
+    c = B.pr_ctx_create(0, 1, 1)
+    yield c
+    B.pr_ctx_destroy(c)
+
+
+TYPES = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+def rows(seed, n, V, dtype, scale=3.0):
+    g = np.random.Generator(np.random.PCG64(seed))
+    x = torch.from_numpy((scale * g.normal(size=(n, V))).astype(np.float32))
+    x[torch.arange(n), torch.from_numpy(g.integers(0, V, n))] += 6.0
+    return x.to(TYPES[dtype]).cuda()
+
+
+def check(ids, logp, x, k, temperature=1.0):
+    want, lw = D.top_logits(x.double().cpu().numpy(), k, temperature)
+    got, l = ids.cpu().numpy(), logp.double().cpu().numpy()
+    assert (got == want).all(), (np.argwhere(got != want)[:5], got[got != want][:5], want[got != want][:5])
+    with np.errstate(invalid="ignore"):
+        ok = (np.abs(l - lw) <= 2e-5 + 4e-7 * np.abs(lw)) | (l == lw) | (np.isnan(l) & np.isnan(lw))
+    assert ok.all(), (np.argwhere(~ok)[:5], l[~ok][:5], lw[~ok][:5])
+
+
+SIZES = [(1, 1), (3, 2), (5, 7), (5, 8), (4, 9), (7, 31), (9, 33), (3, 64), (3, 65), (6, 255),
+         (3, 1000), (37, 1001), (200, 515), (2, 4096), (3, 8191), (5, 32000), (2, 32003), (170, 2050),
+         (700, 4000), (2, 70001), (3, 151936), (40, 151936), (1, 262144), (1, 300007), (1, 1000003)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,V", SIZES)
+def test_sizes(B, ctx, n, V, dtype):
+    x = rows(3 * n + V, n, V, dtype)
+    for k in (1, 20, 32, 33, 64):
+        T = 0.7 if k == 20 else 1.0
+        check(*B.pr_top_logits(ctx, x, k, temperature=T), x, k, T)
+    assert B.pr_ctx_flags(ctx) == 0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,V", [(6, 777), (6, 40000), (300, 5000), (6, 151936)])
+def test_rows_in_order_and_rows_of_ties(B, ctx, n, V, dtype):
+    """What a threshold that rises along the row meets at worst."""
+    x = rows(V, n, V, "f32")
+    x[0] = torch.sort(x[0])[0]
+    x[1] = torch.sort(x[1], descending=True)[0]
+    x[2] = 1.5                                             # all alike
+    x[3] = (torch.arange(V, device="cuda") % 7).float()    # few values
+    x[4] = -torch.arange(V, device="cuda").float() / 64    # the first k
+    x = x.to(TYPES[dtype])
+    x[-1, V // 2:] = x[-1].max()                           # a tail of ties
+    for k in (1, 31, 64):
+        check(*B.pr_top_logits(ctx, x, k), x, k)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,V", [(12, 40), (12, 1003), (12, 40000), (400, 1003)])
+def test_values_that_a_row_can_hold(B, ctx, n, V, dtype):
+    x = rows(V + 1, n, V, dtype)
+    low = torch.finfo(x.dtype).min
+    x[0, : V // 2] = -torch.inf
+    x[1] = -torch.inf                      # nothing left
+    x[2] = low                             # nothing left either
+    x[3, 1:] = low                         # one token left
+    x[4, 3] = torch.nan
+    x[5, V - 1] = torch.inf
+    x[6] = 3e4 + x[6]                      # large logits
+    x[7] = torch.where(torch.arange(V, device="cuda") % 3 == 0, 0.0, -0.0).to(x.dtype)
+    x[8, 10:] = -torch.inf                 # fewer than k left
+    x[9, :-3] = low
+    x[10] = -9e8
+    x[11, V // 2] = 1.1e9                  # counts as infinite
+    for k in (20, 64):
+        B.pr_ctx_flags(ctx, clear=True)
+        ids, logp = B.pr_top_logits(ctx, x, k)
+        check(ids, logp, x, k)
+        assert B.pr_ctx_flags(ctx, clear=True) == B.PR_FLAG_NONFINITE
+        assert (ids[[1, 2, 4, 5, 11]] == -1).all() and logp[[1, 2, 4, 5, 11]].isnan().all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V,stride,start", [(1000, 1003, 1), (5001, 5001, 3), (777, 1024, 0),
+                                            (32000, 32001, 5), (32000, 32008, 8), (9, 11, 2)])
+def test_strides_and_alignments(B, ctx, V, stride, start, dtype):
+    for n in (3, 400):
+        if n * stride > 3e6:
+            continue
+        buf = rows(V, 1, n * stride + start + 8, dtype)[0]
+        x = buf[start:start + n * stride].view(n, stride)
+        check(*B.pr_top_logits(ctx, x, 24, vocab=V), x[:, :V], 24)
+        check(*B.pr_top_logits(ctx, x[:, :V], 24), x[:, :V], 24)
+
+
+def test_outputs_stay_in_their_place_and_streams_and_graphs(B, ctx):
+    n, V, k = 50, 8000, 17
+    x = rows(1, n, V, "bf16")
+    ids = torch.full((n + 2, k), 77, dtype=torch.int32, device="cuda")
+    logp = torch.full((n + 2, k), 7.5, device="cuda")
+    B.pr_top_logits(ctx, x, k, ids=ids[1:n + 1], logp=logp[1:n + 1])
+    check(ids[1:n + 1], logp[1:n + 1], x, k)
+    assert (ids[[0, -1]] == 77).all() and (logp[[0, -1]] == 7.5).all()
+    first = ids.clone(), logp.clone()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        B.pr_top_logits(ctx, x, k, ids=ids[1:n + 1], logp=logp[1:n + 1])
+    torch.cuda.synchronize()
+    assert torch.equal(ids, first[0]) and torch.equal(logp, first[1])
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        B.pr_top_logits(ctx, x, k, ids=ids[1:n + 1], logp=logp[1:n + 1])
+    x.copy_(rows(2, n, V, "bf16"))
+    for _ in range(2):
+        g.replay()
+        check(ids[1:n + 1], logp[1:n + 1], x, k)
+
+
+def test_rows_past_32_bits(B, ctx):
+    V, n, stride = 1000, 3, (1 << 31) + 24
+    buf = torch.zeros(2 * stride + V, dtype=torch.bfloat16, device="cuda")
+    x = torch.as_strided(buf, (n, V), (stride, 1))
+    x.copy_(rows(9, n, V, "bf16"))
+    check(*B.pr_top_logits(ctx, x, 20), x, 20)
+
+
+def test_refusals(B, ctx):
+    x = rows(0, 4, 100, "f32")
+    n0 = B.launch_count()
+
+    def refused(*a, **kw):
+        with pytest.raises(B.PRError) as e:
+            B.pr_top_logits(ctx, *a, **kw)
+        assert e.value.status == B.PR_ERR_INVALID_ARG
+
+    for k in (0, -1, 65):
+        refused(x, k)
+    for T in (0.0, -1.0, 1e-4, 2e3, float("nan"), float("inf")):
+        refused(x, 5, temperature=T)
+    refused(x.cpu(), 5)
+    refused(x, 5, vocab=101)
+    refused(x, 5, vocab=0)
+    refused(x[0], 5)
+    refused(x.t(), 5)
+    refused(x, 5, ids=torch.empty(3, 5, dtype=torch.int32, device="cuda"))
+    refused(x, 5, ids=torch.empty(4, 5, dtype=torch.int64, device="cuda"))
+    refused(x, 5, logp=torch.empty(4, 5, dtype=torch.float64, device="cuda"))
+    refused(x, 5, logp=torch.empty(4, 5))
+    with pytest.raises(TypeError):
+        B.pr_top_logits(ctx, x.half(), 5)
+    ids, logp = B.pr_top_logits(ctx, x[:0], 5)
+    assert ids.shape == (0, 5) and logp.shape == (0, 5)
+    assert B.launch_count() == n0
