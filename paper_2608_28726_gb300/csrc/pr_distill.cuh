@@ -39,12 +39,6 @@ struct ListIn {
   int32_t y, count;
   float xy, edge;
 };
-// What a row's gradient needs.
-struct ListOut {
-  RowOut o;                         // o.gy: the label's entry, where it is not listed
-  float g[DS_MAX];
-};
-
 template <typename T>
 __device__ __forceinline__ ListIn fetch_list(const DistillArgs& d, const Rows& rows, const Share& s,
                                              const int4& ref, int lane) {
@@ -105,30 +99,77 @@ __device__ __forceinline__ bool listed_twice(const ListIn& in, int lane) {
   return __any_sync(FULL, twice);
 }
 
-// A row's end: its sum R against 2^k, the list's and label's logits left out.  Writes the row's
-// KL, the statistics' terms (weight wt) and the result.  Whole warp.
-__device__ __noinline__ void list_math(const DistillArgs& d, int64_t row, const ListIn in, float k,
-                                       float R, float wt, bool writes, ListOut* out, float2* stat,
-                                       int lane) {
+// The large model's side of a row, which does not wait for the row's sum.
+struct ListPre {
+  float p[2], lt[2];     // probabilities and their logarithms
+  float rho, l_rho, mass;
+  bool bad, bad_id, labelled;
+};
+// Whole warp.
+static __device__ __noinline__ void list_pre(const DistillArgs& d, const ListIn& in, ListPre& o,
+                                             int lane) {
+  const LossArgs& a = d.a;
+  bool bad_id = a.chosen && !(in.y >= 0 && (int64_t)in.y < a.vocab), bad = false, labelled = false;
+  bool on[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    on[h] = in.id[h] != -1;
+    bad_id |= on[h] && (in.id[h] < 0 || (int64_t)in.id[h] >= a.vocab);
+    bad |= on[h] && !(in.t[h] < INFINITY);
+    labelled |= on[h] && in.id[h] == in.y;
+  }
+  const bool twice = listed_twice(in, lane);
+  o.bad_id = __any_sync(FULL, bad_id) || twice;
+  o.bad = __any_sync(FULL, bad);
+  o.labelled = __any_sync(FULL, labelled);
+  o.rho = o.l_rho = o.mass = 0.f;
+  if (d.none) {
+    const float tm = warp_max(fmaxf(on[0] ? in.t[0] : -INFINITY, on[1] ? in.t[1] : -INFINITY));
+#pragma unroll
+    for (int h = 0; h < 2; ++h) o.p[h] = on[h] ? expf(in.t[h] - tm) : 0.f;
+    const float P = warp_sum(o.p[0] + o.p[1]), lP = logf(P);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      o.lt[h] = (in.t[h] - tm) - lP;
+      o.p[h] /= P;
+    }
+    if (tm > -INFINITY) o.mass = expf(tm) * P;
+  } else {
+    double s = 0.;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const double v = on[h] ? exp((double)in.t[h]) : 0.;
+      o.p[h] = (float)v;
+      o.lt[h] = in.t[h];
+      s += v;
+    }
+    s = warp_sum(s);
+    o.mass = (float)s;
+    o.rho = fmaxf((float)(1. - s), DS_RHO);
+    o.l_rho = logf(o.rho);
+  }
+}
+
+// A row's end: its sum R against 2^k, the list's and label's logits left out.  Writes the
+// result (out, and the list's entries of the gradient to g), whose barrier learns of it first, then
+// the row's KL and the statistics' terms (weight wt).  Whole warp; apart from the kernel's registers.
+static __device__ __noinline__ void list_math(const DistillArgs& d, int64_t row, const ListIn& in,
+                                              const ListPre& pre, float k, float R, float wt,
+                                              bool writes, RowOut* out, float* g, uint64_t* out_bar,
+                                              float2* stat, int lane) {
   const LossArgs& a = d.a;
   const float big = d.big * a.c2;
-  bool on[2];
+  bool on[2], bad = false;
   float x[2];
-  bool bad_id = a.chosen && !(in.y >= 0 && (int64_t)in.y < a.vocab), bad = false;
-  bool labelled = false;  // the label is listed
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     on[h] = in.id[h] != -1;
     x[h] = in.x[h] <= -d.big ? -INFINITY : in.x[h];
-    bad_id |= on[h] && (in.id[h] < 0 || (int64_t)in.id[h] >= a.vocab);
-    bad |= on[h] && (!(in.t[h] < INFINITY) || !(x[h] < d.big));
-    labelled |= on[h] && in.id[h] == in.y;
+    bad |= on[h] && !(x[h] < d.big);
   }
-  bad_id = __any_sync(FULL, bad_id) || listed_twice(in, lane);
-  labelled = __any_sync(FULL, labelled);
-  const bool apart = a.chosen && !labelled;
+  const bool apart = a.chosen && !pre.labelled;
   const float xy = in.xy <= -d.big ? -INFINITY : in.xy;
-  bad |= !(k < big) || !(R >= 0.f) || !(R < INFINITY) || (a.chosen && !(xy < d.big));
+  bad |= pre.bad || !(k < big) || !(R >= 0.f) || !(R < INFINITY) || (a.chosen && !(xy < d.big));
   bad = __any_sync(FULL, bad);
   if (!(k > -big)) R = 0.f;
   // the rest with the label's term, against 2^k: R; without it R0
@@ -146,7 +187,7 @@ __device__ __noinline__ void list_math(const DistillArgs& d, int64_t row, const 
                                        on[1] ? x[1] * a.c2 : -INFINITY)),
                         rest ? k : -INFINITY);
   if (!(K > -INFINITY)) bad = true;
-  float u[2], e[2], l[2], q[2], p[2], lt[2];
+  float u[2], e[2], l[2], q[2];
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     u[h] = on[h] ? fmaf(x[h], a.c2, -K) : -INFINITY;
@@ -157,158 +198,116 @@ __device__ __noinline__ void list_math(const DistillArgs& d, int64_t row, const 
   const float m = warp_max(fmaxf(e[0], e[1]));
   const unsigned w0 = __ballot_sync(FULL, on[0] && e[0] == m), w1 = __ballot_sync(FULL, on[1] && e[1] == m);
   const int first = w0 ? __ffs(w0) - 1 : w1 ? 32 + __ffs(w1) - 1 : -1;  // its place
+  const bool any = first >= 0;
   const bool is[2] = {first == lane, first == 32 + lane};
-  const float listed = warp_sum((is[0] ? 0.f : e[0]) + (is[1] ? 0.f : e[1]));  // but the largest
-  const float others = Rk + listed, S = first >= 0 ? others + m : Rk;
+  const float listed = warp_sum((is[0] ? 0.f : e[0]) + (is[1] ? 0.f : e[1]));
+  const float others = Rk + listed, S = any ? others + m : Rk;
   const float L = log2f(S), inv = 1.f / S;
-  const bool most = first >= 0 && m > 0.5f * S;
-  const float compl1 = most ? others * inv : 0.f;  // 1 - q of the largest
+  const bool most = any && m > 0.5f * S;
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
-    l[h] = (u[h] - L) * LN2;
-    if (most && is[h]) l[h] = -log1pf(others / m);
+    l[h] = most && is[h] ? -log1pf(others / m) : (u[h] - L) * LN2;
     q[h] = on[h] ? e[h] * inv : 0.f;
   }
-  const float E = listed + (first >= 0 ? m : 0.f), sigma = Rk * inv;
+  const float E = listed + (any ? m : 0.f), sigma = Rk * inv;
   const float l_sigma = Rk > 0.5f * S ? -log1pf(E / Rk) : (k - K + log2f(R) - L) * LN2;
-  // the large model's side
-  const bool any = first >= 0 || __any_sync(FULL, on[0] || on[1]);
-  const bool klass = !d.none && rest;
-  float l_rho = 0.f, rho = 0.f, mass;
-  if (d.none) {
-    const float tm = warp_max(fmaxf(in.id[0] != -1 ? in.t[0] : -INFINITY, in.id[1] != -1 ? in.t[1] : -INFINITY));
-#pragma unroll
-    for (int h = 0; h < 2; ++h) p[h] = on[h] ? expf(in.t[h] - tm) : 0.f;
-    const float P = warp_sum(p[0] + p[1]), lP = logf(P);
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      lt[h] = (in.t[h] - tm) - lP;
-      p[h] /= P;
-    }
-    mass = any ? expf(tm) * P : 0.f;
-  } else {
-    double s = 0.;
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const double v = on[h] ? exp((double)in.t[h]) : 0.;
-      p[h] = (float)v;
-      lt[h] = in.t[h];
-      s += v;
-    }
-    s = warp_sum(s);
-    mass = (float)s;
-    rho = fmaxf((float)(1. - s), DS_RHO);
-    l_rho = logf(rho);
+  // the label
+  float ce = 0.f;
+  const float not_y = R0 * f + E;
+  if (apart) {
+    ce = eyk > 0.25f * S ? log1pf(not_y / eyk) : -(fmaf(xy, a.c2, -K) - L) * LN2;
+  } else if (a.chosen) {
+    const bool y0 = on[0] && in.id[0] == in.y, y1 = on[1] && in.id[1] == in.y;
+    const unsigned who = __ballot_sync(FULL, y0 || y1);
+    ce = -__shfl_sync(FULL, y0 ? l[0] : l[1], who ? __ffs(who) - 1 : 0);
   }
   // KL, a and b
-  float kl = 0.f, av[2] = {0.f, 0.f}, b = 0.f;
+  const bool klass = !d.none && rest;
+  float kl = 0.f, av[2] = {0.f, 0.f}, b = 0.f, kA = 0.f;
   if (any) {
     if (!d.reverse) {
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        if (on[h] && p[h] > 0.f) kl += p[h] * (lt[h] - l[h]);
-        av[h] = -p[h];
+        if (pre.p[h] > 0.f) kl += pre.p[h] * (pre.lt[h] - l[h]);
+        av[h] = -pre.p[h];
       }
       kl = warp_sum(kl);
+      kA = warp_sum(av[0] + av[1]);
       if (klass) {
-        kl += rho * (l_rho - l_sigma);
-        b = -rho;
+        kl += pre.rho * (pre.l_rho - l_sigma);
+        b = -pre.rho;
+        kA += b;
       }
-    } else {
+    } else {  // (a and b add up to 0)
+      av[0] = q[0];
+      av[1] = q[1];
       if (d.none) {  // q over the list
         const float um = warp_max(fmaxf(u[0], u[1]));
         if (um == -INFINITY) bad = true;
-        float qe[2];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) qe[h] = on[h] ? exp2f(u[h] - um) : 0.f;
-        const float Q = warp_sum(qe[0] + qe[1]), lQ = logf(Q);
+        for (int h = 0; h < 2; ++h) av[h] = on[h] ? exp2f(u[h] - um) : 0.f;
+        const float Q = warp_sum(av[0] + av[1]), lQ = logf(Q);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           l[h] = (u[h] - um) * LN2 - lQ;
-          qe[h] /= Q;
-          av[h] = qe[h];
+          av[h] /= Q;
         }
-      } else {
-        av[0] = q[0];
-        av[1] = q[1];
       }
 #pragma unroll
       for (int h = 0; h < 2; ++h)
-        if (av[h] > 0.f) kl += av[h] * (l[h] - lt[h]);
+        if (av[h] > 0.f) kl += av[h] * (l[h] - pre.lt[h]);
       kl = warp_sum(kl);
-      const float far = l_sigma - l_rho;
+      const float far = l_sigma - pre.l_rho;
       if (klass && sigma > 0.f) kl += sigma * far;
 #pragma unroll
-      for (int h = 0; h < 2; ++h) av[h] = av[h] > 0.f ? av[h] * (l[h] - lt[h] - kl) : 0.f;
+      for (int h = 0; h < 2; ++h) av[h] = av[h] > 0.f ? av[h] * (l[h] - pre.lt[h] - kl) : 0.f;
       if (klass && sigma > 0.f) b = sigma * (far - kl);
     }
   }
-  // the label
-  float ce = 0.f;
-  if (a.chosen) {
-    if (apart) {
-      const float not_y = R0 * f + E;
-      ce = eyk > 0.25f * S ? log1pf(not_y / eyk) : -(fmaf(xy, a.c2, -K) - L) * LN2;
-    } else {
-      const float v = on[0] && in.id[0] == in.y ? l[0] : on[1] && in.id[1] == in.y ? l[1] : 0.f;
-      // (reverse over the list alone has put other logarithms in l)
-      const float w = d.reverse && d.none
-                          ? (on[0] && in.id[0] == in.y ? (most && is[0] ? -log1pf(others / m) : (u[0] - L) * LN2)
-                             : on[1] && in.id[1] == in.y ? (most && is[1] ? -log1pf(others / m) : (u[1] - L) * LN2)
-                                                         : 0.f)
-                          : v;
-      const unsigned who = __ballot_sync(FULL, (on[0] && in.id[0] == in.y) || (on[1] && in.id[1] == in.y));
-      ce = -__shfl_sync(FULL, w, (who ? __ffs(who) - 1 : 0));
-    }
-  }
-  bad |= bad_id;
+  bad |= pre.bad_id;
   // the gradient
-  const float kc = d.kl_coef, cc = a.chosen ? d.ce_coef : 0.f;
-  const float w = wt * (a.grad_scale * a.inv_t);
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    av[h] = kc != 0.f ? kc * av[h] : 0.f;
-    if (on[h] && !apart && in.id[h] == in.y) av[h] -= cc;
-  }
-  b = kc != 0.f ? kc * b : 0.f;
-  const float lesser = warp_sum((is[0] ? 0.f : av[0]) + (is[1] ? 0.f : av[1]));
-  const float a1 = warp_sum((is[0] ? av[0] : 0.f) + (is[1] ? av[1] : 0.f));
-  // A without the rounding of sums that are 0 by their form: reverse has sum a + b = 0
-  const float kA = d.reverse || !any ? 0.f : kc * (klass ? -(warp_sum(p[0] + p[1]) + rho) : -warp_sum(p[0] + p[1]));
-  const float A = kA - cc;
-  (void)a1;
   if (out) {
+    const float kc = d.kl_coef, cc = a.chosen ? d.ce_coef : 0.f;
+    const float w = wt * (a.grad_scale * a.inv_t);
+    b = kc != 0.f ? kc * b : 0.f;
+    kA = kc != 0.f ? kc * kA : 0.f;
+    const float A = kA - cc;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      float g = av[h] - A * q[h];
+      av[h] = kc != 0.f ? kc * av[h] : 0.f;
+      if (on[h] && in.id[h] == in.y && a.chosen) av[h] -= cc;
+    }
+    const float lesser = warp_sum((is[0] ? 0.f : av[0]) + (is[1] ? 0.f : av[1]));
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
       // a - A q = (a - A) + A (1 - q), with a - A = -(the other a and b)
-      if (most && is[h]) g = fmaf(A, compl1, -(lesser + b - (apart ? cc : 0.f)));
-      out->g[32 * h + lane] = bad ? NAN : w * g;
+      const float v = most && is[h] ? fmaf(A, others * inv, -(lesser + b - (apart ? cc : 0.f)))
+                                    : av[h] - A * q[h];
+      g[32 * h + lane] = bad ? NAN : w * v;
     }
     if (lane == 0) {
       RowOut o;
-      const float D = b - A * sigma;
       o.K = k;
       o.M = 0.f;
-      o.nk = bad ? NAN : rest ? w * D / R : 0.f;
+      o.nk = bad ? NAN : rest ? w * (b - A * sigma) / R : 0.f;
       o.mode = o.nk == 0.f ? ROW_ZERO : ROW_FAST;
       // q_y (b / sigma - kA) - ce (1 - q_y)
-      const float share = rest ? ey / R : 0.f;
-      o.gy = bad ? NAN : w * (share * (b - kA * sigma) - cc * ((R0 * f + E) * inv));
-      out->o = o;
+      o.gy = bad ? NAN : w * ((rest ? ey / R : 0.f) * (b - kA * sigma) - cc * (not_y * inv));
+      *out = o;
     }
+    __syncwarp();
   }
-  if (bad) kl = ce = mass = NAN;
+  if (out_bar && lane == 0) bar_arrive(out_bar);
+  if (bad) kl = ce = NAN;
   if (lane < DS_TERMS) {
-    const float covered = bad ? NAN : E * inv;
-    const float t = wt * (lane == 0 ? kl : lane == 1 ? ce : lane == 2 ? mass : covered);
+    const float t = wt * (lane == 0 ? kl : lane == 1 ? ce : bad ? NAN : lane == 2 ? pre.mass : E * inv);
     const float2 s = stat[lane];
     const float y = s.x + t, z = y - s.x;
     stat[lane] = make_float2(y, s.y + ((s.x - (y - z)) + (t - z)));
   }
   if (lane == 0 && writes) {
     a.logp[row] = kl;
-    if (bad) atomicOr(a.ctx_flags, bad_id ? FLAG_BAD_CHOSEN : FLAG_NONFINITE);
+    if (bad) atomicOr(a.ctx_flags, pre.bad_id ? FLAG_BAD_CHOSEN : FLAG_NONFINITE);
   }
 }
 
@@ -348,92 +347,508 @@ __device__ __forceinline__ void list_stats(const DistillArgs& d, const float2* s
   }
 }
 
-// ---- a CTA per row, which it reads twice -------------------------------------------------
-
-constexpr int DL_NT = 256;
-struct PlainSmem {
-  float2 part[DL_NT / 32];
-  float2 stat[DS_TERMS];
-  ListOut out;
-  int4 unused;
-};
-
+// The elements at a row's ends (this lane's at v, its value in.edge) into the sum, but the
+// listed ones and the label.  `at`: what v is, an entry's place, DS_LABEL, or DS_REST.
+constexpr int DS_REST = -1, DS_LABEL = -2;
+__device__ __forceinline__ int end_kind(const DistillArgs& d, const Share& s, const ListIn& in,
+                                        int32_t v, int lane) {
+  int kind = d.a.chosen && v == in.y ? DS_LABEL : DS_REST;
+  const int32_t lo = s.head, hi = (int32_t)d.a.vocab - s.tail;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    unsigned b = __ballot_sync(FULL, in.id[h] >= 0 && (in.id[h] < lo || in.id[h] >= hi));
+    while (b) {
+      const int q = __ffs(b) - 1;
+      b &= b - 1;
+      const int32_t id = __shfl_sync(FULL, in.id[h], q);
+      if (id == v) kind = 32 * h + q;
+    }
+  }
+  return kind;
+}
+__device__ __forceinline__ void add_rest_ends(const DistillArgs& d, const Share& s, const ListIn& in,
+                                              int32_t v, int kind, float& k, float& R) {
+  if (s.head + s.tail == 0) return;
+  const float c2 = d.a.c2;
+  const bool add = v >= 0 && kind == DS_REST;
+  const float top = warp_max(add ? fmaxf(in.edge * c2, -3e38f) : -3e38f);
+  if (top > k) {
+    R *= rescale2(k - top);
+    k = top;
+  }
+  R += warp_sum(add ? ex2(fmaf(in.edge, c2, -k)) : 0.f);
+}
 template <typename T>
-__global__ void __launch_bounds__(DL_NT) distill_plain(const DistillArgs d) {
-  extern __shared__ __align__(16) unsigned char ds_raw[];
-  uint32_t* const listed = reinterpret_cast<uint32_t*>(ds_raw);  // a bit per token
-  __shared__ PlainSmem sm;
+__device__ __forceinline__ void put_end(T* g, int32_t v, int kind, const RowOut& o, const float* list,
+                                        float c2, float edge) {
+  if (v >= 0) put(g + v, kind >= 0 ? list[kind] : kind == DS_LABEL ? o.gy : grad1(o, c2, edge));
+}
+
+// Element `e` of a row in shared memory is no part of its sum.  (Written by this thread's proxy, and
+// the next copy into the place by the other one: fenced by the writer.)
+template <typename T>
+__device__ __forceinline__ void leave_out(unsigned char* row, int32_t e) {
+  if constexpr (sizeof(T) == 2) reinterpret_cast<uint16_t*>(row)[e] = 0xff80u;
+  else reinterpret_cast<uint32_t*>(row)[e] = 0xff800000u;
+}
+__device__ __forceinline__ void fence_async() {
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+}
+
+// ---- rows in a ring of shared memory ---------------------------------------------------------
+//
+// As the policy loss': a row to a CTA, or its parts to the CTAs of a cluster; one warp
+// brings chunks of 16 KB in by bulk copies, eight sum them and write the gradient from
+// them, one takes the row's end.  Before a warp sums its words of a chunk, the lanes that
+// hold one of the row's listed tokens there write -inf over it; when it has written the words'
+// gradient, the same lanes write the list's entries over that.
+
+// a lane's tokens among its warp's words of this CTA's part of a row: their elements from the
+// row's first word on, or -1
+struct Mine {
+  int32_t e[3];  // entries lane and 32 + lane; the label (lane 0)
+};
+struct Ids {
+  int32_t id[2];
+};
+__device__ __forceinline__ Ids fetch_ids(const DistillArgs& d, const int4& ref, int lane) {
+  Ids r;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int j = 32 * h + lane;
+    const int64_t at = (int64_t)ref.x * d.k + j;
+    r.id[h] = ref.y >= 0 && j < d.k && __ldcg(d.t_logp + at) != -INFINITY ? __ldcg(d.ids + at) : -1;
+  }
+  return r;
+}
+template <int VEC>
+__device__ __forceinline__ Mine mine_of(const DistillArgs& d, const Share& s, const Ids& ids, int32_t y,
+                                        int warp, int lane) {
+  Mine m;
+  const bool listed = ids.id[0] == y || ids.id[1] == y;
+  const bool apart = d.a.chosen && !__any_sync(FULL, listed);
+#pragma unroll
+  for (int h = 0; h < 3; ++h) {
+    const int32_t id = h < 2 ? ids.id[h] : apart && lane == 0 ? y : -1;
+    const int32_t e = id - s.head, w = e / VEC - s.w0;  // (a negative e divides to a word of its own check)
+    const bool in = id >= s.head && w >= 0 && e / VEC < s.w1;
+    m.e[h] = in && ((w % (32 * RG_NW)) >> 5) == warp ? e : -1;
+  }
+  return m;
+}
+
+struct DistillCtl {
+  uint64_t sum_bar[RG_SLOTS];  // the warps' sums are there
+  uint64_t out_bar[RG_SLOTS];  // a row's result is there
+  float2 stat[DS_TERMS];       // sums over the rows
+  RowOut out[RG_SLOTS];        // a row's result
+};
+// then the bars of the ring's places (landed, read), the warps' (k, R) [RG_SLOTS][C][RG_NW], the
+// lists' entries of the gradient [1 + lag][DS_MAX], and the ring
+constexpr size_t DS_BARS = (sizeof(DistillCtl) + 15) / 16 * 16;
+__host__ __device__ constexpr size_t distill_sums(int places) { return DS_BARS + 16 * (size_t)places; }
+__host__ __device__ constexpr size_t distill_list(int C, int places) {
+  return distill_sums(places) + (size_t)RG_SLOTS * C * RG_NW * sizeof(float2);
+}
+__host__ __device__ constexpr size_t distill_start(int C, int places, int lag) {
+  return distill_list(C, places) + (size_t)(1 + lag) * DS_MAX * sizeof(float);
+}
+static_assert(distill_start(4, RG_FEW, 0) <= 1024 && distill_start(1, RG_FEW, 1) <= 1024,
+              "two CTAs on an SM");
+
+template <typename T, bool HOLD, bool OWN>
+__global__ void __launch_bounds__(RG_NT, 2)
+    distill_ring(const __grid_constant__ DistillArgs d, const int places, const int lag) {
+  extern __shared__ __align__(16) unsigned char smem_raw[];
+  DistillCtl& sm = *reinterpret_cast<DistillCtl*>(smem_raw);
   const LossArgs& a = d.a;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  if (tid < DS_TERMS) sm.stat[tid] = make_float2(0.f, 0.f);
+  using Tr = Traits<T>;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  uint32_t C, rank;
+  asm("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(C));
+  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+  const int64_t G = gridDim.x / C, first = blockIdx.x / C;
+  uint64_t* const full = reinterpret_cast<uint64_t*>(smem_raw + DS_BARS);
+  uint64_t* const empty = full + places;
+  float2* const sums = reinterpret_cast<float2*>(smem_raw + distill_sums(places));
+  float* const list = reinterpret_cast<float*>(smem_raw + distill_list((int)C, places));
+  unsigned char* const ring = smem_raw + distill_start((int)C, places, lag);
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < places; ++i) {
+      bar_init(&full[i], 1);
+      bar_init(&empty[i], RG_NW);
+    }
+    for (int s = 0; s < RG_SLOTS; ++s) {
+      bar_init(&sm.sum_bar[s], C > 1 ? 1 : RG_NW);
+      bar_init(&sm.out_bar[s], 1);
+      if (C > 1) bar_expect(&sm.sum_bar[s], 8 * RG_NW * C);
+    }
+    for (int j = 0; j < DS_TERMS; ++j) sm.stat[j] = make_float2(0.f, 0.f);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    fence_async();
+  }
+  __syncthreads();
+  if (C > 1) cluster_sync_all();  // every CTA's barriers are there
+  pdl_wait();
+  pdl_trigger();
+
+  bool ok = true;  // no wait has run out
+  auto wait = [&](uint64_t* b, uint32_t phase) {
+    if (ok) ok = ring_wait(sm_addr(b), phase, a.ctx_flags);
+    __syncwarp();
+  };
+  const Rows rows = rows_of<RG_NT>(
+      a, OWN, reinterpret_cast<OwnPlan*>(ring + (size_t)places * RG_BYTES), false);
+  const int32_t live = rows.live;
+  auto ref_of = [&](int64_t i) { return rows.at(a, i); };
+  int place = 0;         // of the ring
+  uint32_t turn = 0u;    // how often it has been gone around, its last bit
+  auto step = [&]() {
+    if (++place == places) {
+      place = 0;
+      turn ^= 1u;
+    }
+  };
+
+  if (warp == RG_NW) {
+    // ---- bringing chunks in
+    int64_t n = 0;
+    int4 ref = ref_of(first);
+    for (int64_t i = first; i < live; i += G) {
+      const int4 ref1 = ref_of(i + G);
+      const Share sh = share_of<T>(a, ref.x, C, rank);
+      const char* src = sh.x + sizeof(T) * sh.head + 16 * (int64_t)sh.w0;
+      for (int32_t left = sh.w1 - sh.w0; left > 0; left -= RG_CHUNK) {
+        if (n >= places) wait(&empty[place], turn ^ 1u);
+        if (ok && lane == 0) {
+          const uint32_t bytes = 16u * (uint32_t)min(RG_CHUNK, left);
+          bar_expect(&full[place], bytes);
+          asm volatile(
+              "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::
+                  "r"(sm_addr(ring + (size_t)place * RG_BYTES)),
+              "l"(src), "r"(bytes), "r"(sm_addr(&full[place]))
+              : "memory");
+        }
+        src += RG_BYTES;
+        if (ok) ++n;
+        step();
+      }
+      ref = ref1;
+    }
+    // no copy may be in flight when the CTA ends (as none is unless a wait ran out)
+    ok = true;
+    for (int64_t i = n < places ? 0 : n - places; i < n; ++i)
+      wait(&full[(int)(i % places)], (uint32_t)(i / places) & 1u);
+  } else if (warp == RG_NW + 1) {
+    // ---- the rows' ends
+    const double share = rows.share(a);
+    uint32_t n = 0;
+    int4 ref = ref_of(first), ref1 = ref_of(first + G);
+    ListIn in = fetch_list<T>(d, rows, share_of<T>(a, ref.x, C, rank), ref, lane);
+    // What a peer's gradient may be written over (the logits' own buffer) has been read when
+    // this CTA's sums are sent: the next row's logits are there before a result is given.
+    auto landed = [&](ListIn& q) {
+      q.x[0] = __shfl_sync(FULL, q.x[0], lane);
+      q.x[1] = __shfl_sync(FULL, q.x[1], lane);
+      q.xy = __shfl_sync(FULL, q.xy, lane);
+      q.edge = __shfl_sync(FULL, q.edge, lane);
+    };
+    landed(in);
+    if (C > 1) named_bar_arrive(BAR_IN, 32 * (RG_NW + 1));
+    for (int64_t i = first; i < live; i += G) {
+      const int64_t row = ref.x;
+      const Share sh = share_of<T>(a, row, C, rank);
+      ListIn next = fetch_list<T>(d, rows, share_of<T>(a, ref1.x, C, rank), ref1, lane);
+      ref = ref1;
+      ref1 = ref_of(i + 2 * G);
+      const int32_t v = end_of(a, sh, lane);
+      const int kind = sh.head + sh.tail ? end_kind(d, sh, in, v, lane) : DS_REST;
+      ListPre pre;
+      list_pre(d, in, pre, lane);
+      T* const g = reinterpret_cast<T*>(a.grad) + row * a.grad_stride;
+      const int s = n % RG_SLOTS;
+      const uint32_t phase = (n / RG_SLOTS) & 1u;
+      float* const entries = list + (lag ? s : 0) * DS_MAX;
+      ++n;
+      wait(&sm.sum_bar[s], phase);
+      float k, R;
+      {
+        const float2* q = sums + s * RG_NW * C;
+        const float2 none = make_float2(-3e38f, 0.f);
+        float2 p = lane < (int)(RG_NW * C) ? q[lane] : none;
+        if (C > 4) {
+          const float2 p2 = q[32 + lane];
+          const float top = fmaxf(p.x, p2.x);
+          p = make_float2(top, p.y * rescale2(p.x - top) + p2.y * rescale2(p2.x - top));
+        }
+        __syncwarp();
+        if (C > 1 && lane == 0) bar_expect(&sm.sum_bar[s], 8 * RG_NW * C);
+        join(p, 1.f, k, R);
+      }
+      add_rest_ends(d, sh, in, v, kind, k, R);
+      const float wt = (float)(a.norm ? share / (double)in.count : share);
+      landed(next);
+      list_math(d, row, in, pre, k, R, wt, rank == 0, HOLD ? &sm.out[s] : nullptr, entries,
+                &sm.out_bar[s], sm.stat, lane);
+      __syncwarp();
+      if (HOLD && rank == 0) put_end(g, v, kind, sm.out[s], entries, a.c2, in.edge);
+      in = next;
+    }
+  } else {
+    // ---- the rows' words
+    uint32_t n = 0, m = 0;  // rows summed; written
+    const uint32_t mine = first < live ? (uint32_t)((live - 1 - first) / G) + 1u : 0u;
+    if (C > 1) named_bar_sync(BAR_IN, 32 * (RG_NW + 1));
+    const int at = warp * 32 + lane;  // this lane's first word of a chunk
+    int4 ref = ref_of(first), next = ref_of(first + G);  // the row to be summed; the one after it
+    int4 held = ref;              // the row to be written
+    Ids ids = fetch_ids(d, ref, lane);
+    int4 last = ref;              // the one summed last
+    Mine own, kept;               // the tokens of that one; of the one to be written
+    int place0 = 0;               // its place
+    auto within = [&](int32_t e, int32_t w) {  // whether element e is in the chunk at word w
+      return e >= 0 && (uint32_t)(e / Tr::VEC - w) < (uint32_t)RG_CHUNK;
+    };
+    while ((HOLD ? m : n) < mine) {
+      if (n < mine) {
+        // forward
+        const Share sh = share_of<T>(a, ref.x, C, rank);
+        own = mine_of<Tr::VEC>(d, sh, ids, ref.z, warp, lane);
+        if (m == n) kept = own;
+        ids = fetch_ids(d, next, lane);
+        float k = -3e38f;
+        float2 S = make_float2(0.f, 0.f);
+        for (int32_t w = sh.w0; w < sh.w1; w += RG_CHUNK) {
+          wait(&full[place], turn);
+          unsigned char* const here = ring + (size_t)place * RG_BYTES;
+          bool wrote = false;
+#pragma unroll
+          for (int h = 0; h < 3; ++h)
+            if (within(own.e[h], w)) {
+              leave_out<T>(here, own.e[h] - w * Tr::VEC);
+              wrote = true;
+            }
+          if (wrote) fence_async();
+          __syncwarp();
+          const uint4* st = reinterpret_cast<const uint4*>(here) + at;
+          uint4 v[RG_W];
+#pragma unroll
+          for (int q = 0; q < RG_W; ++q) v[q] = st[32 * RG_NW * q];
+          if (w + RG_CHUNK > sh.w1) {
+#pragma unroll
+            for (int q = 0; q < RG_W; ++q)
+              if (w + 32 * RG_NW * q + at >= sh.w1)
+                v[q] = make_uint4(Tr::NEG_WORD, Tr::NEG_WORD, Tr::NEG_WORD, Tr::NEG_WORD);
+          }
+          if (!HOLD) {
+            __syncwarp();  // every lane has its words
+            if (lane == 0) bar_arrive(&empty[place]);
+          }
+          step();
+          add_words<T>(k, S, v, a.c2, w == sh.w0);
+        }
+        float R;
+        join(make_float2(k, S.x + S.y), 1.f, k, R);
+        const int s = n % RG_SLOTS;
+        if (!HOLD && n >= 1) wait(&sm.out_bar[s ^ 1], ((n - 1) / RG_SLOTS) & 1u);
+        if (C > 1) {
+          send(sums + (s * C + rank) * RG_NW + warp, &sm.sum_bar[s], k, R, C, lane);
+        } else if (lane == 0) {
+          sums[s * RG_NW + warp] = make_float2(k, R);
+          bar_arrive(&sm.sum_bar[s]);
+        }
+        last = ref;
+        ++n;
+        ref = next;
+        next = ref_of(first + (int64_t)(n + 1) * G);
+      }
+      if (HOLD && (n > (uint32_t)lag || n == mine)) {
+        // backward
+        const Share sh = share_of<T>(a, held.x, C, rank);
+        T* const g = reinterpret_cast<T*>(a.grad) + held.x * a.grad_stride + sh.head;
+        const bool vec = ((reinterpret_cast<uintptr_t>(sh.x + sizeof(T) * sh.head) ^
+                           reinterpret_cast<uintptr_t>(g)) & 15u) == 0;
+        const int s = m % RG_SLOTS;
+        wait(&sm.out_bar[s], (m / RG_SLOTS) & 1u);
+        const RowOut o = sm.out[s];
+        const float* const entries = list + (lag ? s : 0) * DS_MAX;
+        const float mine0 = entries[lane], mine1 = entries[32 + lane];
+        for (int32_t w = sh.w0; w < sh.w1; w += RG_CHUNK) {
+          const uint4* st = reinterpret_cast<const uint4*>(ring + (size_t)place0 * RG_BYTES) + at;
+          T* const to = g + (int64_t)(w + at) * Tr::VEC;
+          uint4 v[RG_W];
+#pragma unroll
+          for (int q = 0; q < RG_W; ++q) v[q] = st[32 * RG_NW * q];
+          if (o.mode == ROW_FAST) {
+#pragma unroll
+            for (int q = 0; q < RG_W; ++q) v[q] = grad_word<T, false>(o, a.c2, v[q]);
+          } else {
+#pragma unroll
+            for (int q = 0; q < RG_W; ++q) v[q] = make_uint4(0u, 0u, 0u, 0u);
+          }
+          __syncwarp();
+          if (lane == 0) bar_arrive(&empty[place0]);
+          if (++place0 == places) place0 = 0;
+          if (vec && w + RG_CHUNK <= sh.w1) {
+#pragma unroll
+            for (int q = 0; q < RG_W; ++q)
+              *reinterpret_cast<uint4*>(to + 32 * RG_NW * q * Tr::VEC) = v[q];
+          } else {
+#pragma unroll
+            for (int q = 0; q < RG_W; ++q)
+              if (w + 32 * RG_NW * q + at < sh.w1) put_word(to + 32 * RG_NW * q * Tr::VEC, v[q], vec);
+          }
+          __syncwarp();  // the warp's words are written: the list's entries over them
+#pragma unroll
+          for (int h = 0; h < 3; ++h)
+            if (within(kept.e[h], w)) put(g + kept.e[h], h == 0 ? mine0 : h == 1 ? mine1 : o.gy);
+        }
+        ++m;
+        held = m == n ? ref : last;
+        kept = own;
+      }
+    }
+    if (HOLD)  // the rows that do not count
+      for (int64_t i = first; i < a.n_rows - live; i += G) {
+        const int64_t row = rows.skipped(a, i);
+        const Share sh = share_of<T>(a, row, C, rank);
+        T* const g = reinterpret_cast<T*>(a.grad) + row * a.grad_stride;
+        const bool vec = ((reinterpret_cast<uintptr_t>(sh.x) ^ reinterpret_cast<uintptr_t>(g)) & 15u) == 0;
+        for (int32_t w = sh.w0 + at; w < sh.w1; w += 32 * RG_NW)
+          put_word(g + sh.head + (int64_t)w * Tr::VEC, make_uint4(0u, 0u, 0u, 0u), vec);
+        const int32_t v = end_of(a, sh, lane);
+        if (warp == 0 && rank == 0 && v >= 0) put(g + v, 0.f);
+      }
+  }
+  __syncthreads();
+  if (C > 1) cluster_sync_all();  // no peer writes here any more
+  const int64_t groups = max((int64_t)1, min(G, (int64_t)live));
+  if (warp == 0 && rank == 0 && first < groups) list_stats(d, sm.stat, 1, first, groups, lane);
+}
+
+// ---- short rows: one to a warp ----------------------------------------------------------------
+//
+// As the other losses': a row's end is longer than a short row's data take, so that up to
+// 20 rows of an SM are in work at a time.
+
+struct DistillRowsCtl {
+  uint64_t full[RW_MOST];    // a row has landed
+  RowOut out[RW_MOST];
+  float2 stat[RW_MOST * DS_TERMS];
+  float list[RW_MOST * DS_MAX];
+};
+constexpr size_t DR_CTL = (sizeof(DistillRowsCtl) + 15) / 16 * 16;
+
+template <typename T, bool HOLD>
+__global__ void __launch_bounds__(32 * RW_MOST, 2)
+    distill_rows(const __grid_constant__ DistillArgs d, const int bytes) {  // of a warp's part
+  extern __shared__ __align__(16) unsigned char smem_raw[];
+  DistillRowsCtl& sm = *reinterpret_cast<DistillRowsCtl*>(smem_raw);
+  const LossArgs& a = d.a;
+  using Tr = Traits<T>;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+  unsigned char* const part = smem_raw + DR_CTL + (size_t)warp * bytes;
+  uint64_t* const full = &sm.full[warp];
+  float2* const stat = sm.stat + warp * DS_TERMS;
+  float* const list = sm.list + warp * DS_MAX;
+  if (lane == 0) {
+    bar_init(full, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    fence_async();
+  }
+  if (lane < DS_TERMS) stat[lane] = make_float2(0.f, 0.f);
+  __syncthreads();
   pdl_wait();
   pdl_trigger();
   const Rows rows{nullptr, (int32_t)__ldcg(a.totals)};
   const double share = rows.share(a);
-  for (int64_t i = blockIdx.x; i < rows.live; i += gridDim.x) {
-    const int4 ref = rows.at(a, i);
-    const Share s = share_of<T>(a, ref.x, 1, 0);
-    const T* x = reinterpret_cast<const T*>(s.x);
-    __syncthreads();
-    for (int q = tid; q < (int)((a.vocab + 31) / 32); q += DL_NT) listed[q] = 0u;
-    __syncthreads();
-    if (tid <= d.k) {
-      const int32_t v = tid < d.k ? d.ids[(int64_t)ref.x * d.k + tid] : ref.z;
-      const bool on = tid < d.k ? d.t_logp[(int64_t)ref.x * d.k + tid] != -INFINITY : true;
-      if (on && v >= 0 && (int64_t)v < a.vocab) atomicOr(&listed[v >> 5], 1u << (v & 31));
+  const int64_t G = (int64_t)gridDim.x * warps, first = (int64_t)warp * gridDim.x + blockIdx.x;
+  uint32_t phase = 0;
+  int4 ref = rows.at(a, first);
+  for (int64_t i = first; i < rows.live; i += G) {
+    const Share sh = share_of<T>(a, ref.x, 1, 0);
+    if (lane == 0) {
+      const uint32_t n = 16u * (uint32_t)sh.words;
+      bar_expect(full, n);
+      if (n > 0)
+        asm volatile(
+            "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::
+                "r"(sm_addr(part)),
+            "l"(sh.x + sizeof(T) * sh.head), "r"(n), "r"(sm_addr(full))
+            : "memory");
     }
-    __syncthreads();
-    float k = -3e38f, S = 0.f;
-    for (int64_t v = tid; v < a.vocab; v += DL_NT) {
-      if (listed[v >> 5] >> (v & 31) & 1u) continue;
-      const float f = Traits<T>::elem(x, v), t = f * a.c2;
-      if (t > k) {
-        S *= exp2f(k - t);
-        k = t;
+    const ListIn in = fetch_list<T>(d, rows, sh, ref, lane);
+    const int4 ref1 = rows.at(a, i + G);
+    const int32_t v = end_of(a, sh, lane);
+    const int kind = sh.head + sh.tail ? end_kind(d, sh, in, v, lane) : DS_REST;
+    ListPre pre;
+    list_pre(d, in, pre, lane);
+    if (!ring_wait(sm_addr(full), phase, a.ctx_flags)) {
+      ring_wait(sm_addr(full), phase, a.ctx_flags);  // no copy may be in flight at the end
+      break;
+    }
+    phase ^= 1u;
+    __syncwarp();
+    const int32_t end = sh.words * Tr::VEC;
+    auto inside = [&](int32_t id) { return id >= sh.head && id - sh.head < end; };
+    const bool label = a.chosen && inside(in.y);
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      if (inside(in.id[h])) leave_out<T>(part, in.id[h] - sh.head);
+    if (lane == 0 && label) leave_out<T>(part, in.y - sh.head);
+    fence_async();
+    __syncwarp();
+    const uint4* const st = reinterpret_cast<const uint4*>(part) + lane;
+    float k = -3e38f, R;
+    float2 S = make_float2(0.f, 0.f);
+    for (int32_t w = 0; w < sh.words; w += 32 * RG_W) {
+      uint4 x[RG_W];
+#pragma unroll
+      for (int q = 0; q < RG_W; ++q)
+        x[q] = w + 32 * q + lane < sh.words
+                   ? st[w + 32 * q]
+                   : make_uint4(Tr::NEG_WORD, Tr::NEG_WORD, Tr::NEG_WORD, Tr::NEG_WORD);
+      add_words<T>(k, S, x, a.c2, w == 0);
+    }
+    join(make_float2(k, S.x + S.y), 1.f, k, R);
+    add_rest_ends(d, sh, in, v, kind, k, R);
+    const float wt = (float)(a.norm ? share / (double)in.count : share);
+    list_math(d, ref.x, in, pre, k, R, wt, true, HOLD ? &sm.out[warp] : nullptr, list, nullptr, stat, lane);
+    __syncwarp();
+    if (HOLD) {
+      const RowOut o = sm.out[warp];
+      T* const g = reinterpret_cast<T*>(a.grad) + (int64_t)ref.x * a.grad_stride;
+      T* const gw = g + sh.head;
+      const bool vec = ((reinterpret_cast<uintptr_t>(sh.x) ^ reinterpret_cast<uintptr_t>(g)) & 15u) == 0;
+      for (int32_t w = lane; w < sh.words; w += 32) {
+        uint4 x = make_uint4(0u, 0u, 0u, 0u);
+        if (o.mode == ROW_FAST) x = grad_word<T, false>(o, a.c2, st[w - lane]);
+        put_word(gw + (int64_t)w * Tr::VEC, x, vec);
       }
-      S += exp2f(fmaf(f, a.c2, -k));
+      put_end(g, v, kind, o, list, a.c2, in.edge);
+      __syncwarp();  // the row is written: the list's entries over it
+      if (lane == 0 && label && !pre.labelled) put(g + in.y, o.gy);
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        if (inside(in.id[h])) put(g + in.id[h], list[32 * h + lane]);
+      __syncwarp();  // every lane has read what the next row is written over
     }
-    float R;
-    join(make_float2(k, S), 1.f, k, R);
-    if (lane == 0) sm.part[warp] = make_float2(k, R);
-    __syncthreads();
-    if (warp == 0) {
-      join(lane < DL_NT / 32 ? sm.part[lane] : make_float2(-3e38f, 0.f), 1.f, k, R);
-      const ListIn in = fetch_list<T>(d, rows, s, ref, lane);
-      const float wt = (float)(a.norm ? share / (double)in.count : share);
-      list_math(d, ref.x, in, k, R, wt, true, &sm.out, sm.stat, lane);
-    }
-    __syncthreads();
-    if (!a.grad) continue;
-    const RowOut o = sm.out.o;
-    T* const g = reinterpret_cast<T*>(a.grad) + (int64_t)ref.x * a.grad_stride;
-    for (int64_t v = tid; v < a.vocab; v += DL_NT) {
-      const bool l = listed[v >> 5] >> (v & 31) & 1u;
-      const float f = Traits<T>::elem(x, v);
-      if (!l) put(g + v, f <= -d.big && o.nk == o.nk ? 0.f : grad1(o, a.c2, f));
-    }
-    __syncthreads();
-    if (tid < d.k) {
-      const int32_t v = d.ids[(int64_t)ref.x * d.k + tid];
-      const bool on = d.t_logp[(int64_t)ref.x * d.k + tid] != -INFINITY;
-      if (on && v >= 0 && (int64_t)v < a.vocab) put(g + v, sm.out.g[tid]);
-      else if (false) put(g, 0.f);
-    }
-    if (tid == 0 && ref.z >= 0 && (int64_t)ref.z < a.vocab) {
-      bool in = false;
-      for (int j = 0; j < d.k; ++j)
-        in |= d.ids[(int64_t)ref.x * d.k + j] == ref.z && d.t_logp[(int64_t)ref.x * d.k + j] != -INFINITY;
-      if (!in) put(g + ref.z, o.gy);
-    }
+    ref = ref1;
   }
-  if (a.grad)
-    for (int64_t i = blockIdx.x; i < a.n_rows - rows.live; i += gridDim.x) {
-      T* const g = reinterpret_cast<T*>(a.grad) + (int64_t)rows.skipped(a, i) * a.grad_stride;
-      for (int64_t v = tid; v < a.vocab; v += DL_NT) put(g + v, 0.f);
+  if (HOLD)  // the rows that do not count
+    for (int64_t i = first; i < a.n_rows - rows.live; i += G) {
+      const int64_t row = rows.skipped(a, i);
+      const Share sh = share_of<T>(a, row, 1, 0);
+      T* const g = reinterpret_cast<T*>(a.grad) + row * a.grad_stride;
+      const bool vec = ((reinterpret_cast<uintptr_t>(sh.x) ^ reinterpret_cast<uintptr_t>(g)) & 15u) == 0;
+      for (int32_t w = lane; w < sh.words; w += 32)
+        put_word(g + sh.head + (int64_t)w * Tr::VEC, make_uint4(0u, 0u, 0u, 0u), vec);
+      const int32_t v = end_of(a, sh, lane);
+      if (v >= 0) put(g + v, 0.f);
     }
   __syncthreads();
   const int64_t groups = max((int64_t)1, min((int64_t)gridDim.x, (int64_t)rows.live));
-  if (warp == 0 && blockIdx.x < groups) list_stats(d, sm.stat, 1, blockIdx.x, groups, lane);
+  if (warp == 0 && blockIdx.x < groups) list_stats(d, sm.stat, warps, blockIdx.x, groups, lane);
 }
 
 }  // namespace prk

@@ -8,6 +8,105 @@ using namespace prh;
 static_assert(PR_MAX_LISTED == prk::DS_MAX && PR_NDIS == prk::DS_TERMS + 1, "lists, statistics");
 static_assert(prk::DS_TERMS <= prk::LS_NSTAT, "the workspace's places for sums");
 
+namespace {
+
+size_t ring_bytes(int places, int cluster, int lag, bool own) {
+  return prk::distill_start(cluster, places, lag) + (size_t)places * prk::RG_BYTES +
+         (own ? sizeof(prk::OwnPlan) : 0);
+}
+
+template <typename T>
+const void* ring_kernel(bool hold, bool own) {
+  return hold ? (own ? reinterpret_cast<const void*>(&prk::distill_ring<T, true, true>)
+                     : reinterpret_cast<const void*>(&prk::distill_ring<T, true, false>))
+              : (own ? reinterpret_cast<const void*>(&prk::distill_ring<T, false, true>)
+                     : reinterpret_cast<const void*>(&prk::distill_ring<T, false, false>));
+}
+const void* ring_kernel(pr_dtype dt, bool hold, bool own) {
+  return dt == PR_DTYPE_BF16 ? ring_kernel<__nv_bfloat16>(hold, own) : ring_kernel<float>(hold, own);
+}
+
+const void* rows_kernel(pr_dtype dt, bool hold) {
+  if (dt == PR_DTYPE_BF16)
+    return hold ? reinterpret_cast<const void*>(&prk::distill_rows<__nv_bfloat16, true>)
+                : reinterpret_cast<const void*>(&prk::distill_rows<__nv_bfloat16, false>);
+  return hold ? reinterpret_cast<const void*>(&prk::distill_rows<float, true>)
+              : reinterpret_cast<const void*>(&prk::distill_rows<float, false>);
+}
+
+// half of an SM's shared memory
+constexpr size_t HALF = prk::distill_start(4, prk::RG_FEW, 0) + (size_t)prk::RG_FEW * prk::RG_BYTES;
+
+// shared memory opt-ins, and the clusters that the GPU has room for, as ring_setup of the other losses
+pr_status setup(pr_ctx* c) {
+  if (c->distill_ready) return PR_OK;
+  for (pr_dtype dt : {PR_DTYPE_F32, PR_DTYPE_BF16})
+    for (bool hold : {false, true}) {
+      for (bool own : {false, true})
+        PR_CUDA(cudaFuncSetAttribute(ring_kernel(dt, hold, own),
+                                     cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                     (int)ring_bytes(prk::RG_MOST, 8, 0, false)));
+      PR_CUDA(cudaFuncSetAttribute(rows_kernel(dt, hold), cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                   (int)HALF));
+    }
+  for (int i = 0; i < 4; ++i)
+    for (int whole = 0; whole < 2; ++whole) {
+      if (i == 0) {
+        c->distill_places[whole][0] = c->num_sms * (whole ? 1 : 2);
+        continue;
+      }
+      cudaLaunchConfig_t cfg;
+      memset(&cfg, 0, sizeof cfg);
+      cfg.gridDim = dim3(1u << i);
+      cfg.blockDim = dim3(prk::RG_NT);
+      cfg.dynamicSmemBytes = ring_bytes(whole ? prk::RG_MOST : prk::RG_FEW, 1 << i, 0, false);
+      cudaLaunchAttribute attr[1];
+      attr[0].id = cudaLaunchAttributeClusterDimension;
+      attr[0].val.clusterDim.x = 1u << i;
+      attr[0].val.clusterDim.y = 1;
+      attr[0].val.clusterDim.z = 1;
+      cfg.attrs = attr;
+      cfg.numAttrs = 1;
+      int n = 0;
+      PR_CUDA(cudaOccupancyMaxActiveClusters(&n, ring_kernel(PR_DTYPE_BF16, true, false), &cfg));
+      c->distill_places[whole][i] = std::max(n, 1);
+    }
+  c->distill_ready = true;
+  return PR_OK;
+}
+
+pr_status launch_ring(pr_ctx* c, prk::DistillArgs& d, pr_dtype dt, const RingShape& shape, bool hold,
+                      cudaStream_t s) {
+  int places = shape.places - (d.a.own ? 1 : 0);  // (the rows' list takes one)
+  int lag = hold && shape.split == 0 && 2 * shape.here + 1 <= places ? 1 : 0;
+  void* args[] = {&d, &places, &lag};
+  // (a grid that takes every place is not set up early: see launch_ring of the other losses)
+  const pr_status st = launch(ring_kernel(dt, hold, d.a.own), (unsigned)(shape.groups << shape.split),
+                              prk::RG_NT, ring_bytes(places, 1 << shape.split, lag, d.a.own),
+                              1u << shape.split, args, s, !shape.full);
+  return st == PR_OK ? timing_mark(c, s) : st;
+}
+
+// Warps of a CTA of distill_rows, or 0 where the ring takes less time: the other losses' rule.
+int rows_warps(const pr_ctx* c, const prk::LossArgs& a, pr_dtype dt) {
+  if (a.own || a.n_rows <= 4 * c->num_sms) return 0;
+  const int64_t part = std::max<int64_t>(16, a.vocab * (int64_t)esize(dt) / 16 * 16);
+  const int64_t w = std::min<int64_t>(prk::RW_MOST, ((int64_t)HALF - (int64_t)prk::DR_CTL) / part);
+  return w >= 5 ? (int)w : 0;
+}
+
+pr_status launch_rows(pr_ctx* c, prk::DistillArgs& d, pr_dtype dt, int warps, bool hold,
+                      cudaStream_t s) {
+  int part = (int)std::max<int64_t>(16, d.a.vocab * (int64_t)esize(dt) / 16 * 16);
+  void* args[] = {&d, &part};
+  const pr_status st = launch(rows_kernel(dt, hold),
+                              (unsigned)std::min<int64_t>(2 * c->num_sms, d.a.n_rows), 32u * warps,
+                              prk::DR_CTL + (size_t)warps * part, 1, args, s);
+  return st == PR_OK ? timing_mark(c, s) : st;
+}
+
+}  // namespace
+
 extern "C" {
 
 pr_status pr_distill_loss(pr_ctx* c, const void* logits, pr_dtype dt, int64_t n_rows,
@@ -53,22 +152,16 @@ pr_status pr_distill_loss(pr_ctx* c, const void* logits, pr_dtype dt, int64_t n_
     PR_CUDA(cudaMemsetAsync(stats, 0, PR_NDIS * sizeof(float), s));
     return PR_OK;
   }
-  const unsigned grid = (unsigned)std::min<int64_t>(n_rows, 4 * c->num_sms);
-  if ((st = workspace(c, d.a, std::max<int64_t>(grid, forward_grid(c)), false, false)) != PR_OK) return st;
+  if ((st = setup(c)) != PR_OK) return st;
+  const RingShape ring = choose_ring(c->distill_places, dt, n_rows, vocab);  // (PR_DISTILL_MAX_VOCAB: it holds)
+  if ((st = workspace(c, d.a, std::max(ring.groups, forward_grid(c)), false, false)) != PR_OK)
+    return st;
+  d.a.own = own_list(d.a);
   if ((st = timing_begin(c, s)) != PR_OK) return st;
   if ((st = launch_plan(c, d.a, 0, s)) != PR_OK) return st;
-  void* args[] = {&d};
-  const size_t smem = (size_t)(vocab + 31) / 32 * 4;
-  const void* kern = dt == PR_DTYPE_BF16 ? reinterpret_cast<const void*>(&prk::distill_plain<__nv_bfloat16>)
-                                         : reinterpret_cast<const void*>(&prk::distill_plain<float>);
-  if (!c->distill_ready) {
-    for (const void* q : {reinterpret_cast<const void*>(&prk::distill_plain<__nv_bfloat16>),
-                          reinterpret_cast<const void*>(&prk::distill_plain<float>)})
-      PR_CUDA(cudaFuncSetAttribute(q, cudaFuncAttributeMaxDynamicSharedMemorySize, PR_DISTILL_MAX_VOCAB / 8));
-    c->distill_ready = true;
-  }
-  st = launch(kern, grid, prk::DL_NT, smem, 1, args, s);
-  return st == PR_OK ? timing_mark(c, s) : st;
+  if (const int warps = rows_warps(c, d.a, dt))
+    return launch_rows(c, d, dt, warps, grad != nullptr, s);
+  return launch_ring(c, d, dt, ring, grad != nullptr, s);
 }
 
 }  // extern "C"

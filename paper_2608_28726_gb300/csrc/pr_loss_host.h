@@ -126,6 +126,50 @@ inline pr_status launch_plan(pr_ctx* c, prk::LossArgs& a, int pairs, cudaStream_
   return st == PR_OK ? timing_mark(c, s) : st;
 }
 
+// The one-pass kernel's launch: 2^split CTAs per row, `places` chunks in a CTA's ring.
+struct RingShape {
+  int split, places;
+  int here;         // chunks of a row's part
+  bool hold;        // a row's chunks fit the cluster's rings
+  bool spare;       // and leave a place free
+  bool full;        // every place is taken
+  int64_t groups;   // rows in work at a time
+};
+
+// Of the launches whose CTAs hold a row, with two places left for the next row's chunks,
+// the one that takes the least time by this count (room: clusters resident, as ring_setup finds), in the time that an SM takes for a
+// chunk: each cluster's rows come one after the other, a row takes its CTA's chunks and about
+// three for its end, which two CTAs on an SM hide from one another.  The same with and
+// without a gradient, so that the losses' bits are.
+inline RingShape choose_ring(const int (&room)[2][4], pr_dtype dt, int64_t n_rows, int64_t vocab) {
+  const int64_t words = vocab * (int64_t)esize(dt) / 16;
+  const int64_t chunks = (words + prk::RG_CHUNK - 1) / prk::RG_CHUNK;
+  RingShape s;
+  s.split = 3;
+  s.places = prk::RG_MOST;
+  int64_t best = -1;
+  for (int whole = 0; whole < 2; ++whole)
+    for (int split = 0; split < (whole ? 4 : 3); ++split) {
+      const int64_t here = (chunks + (1 << split) - 1) >> split, at_once = room[whole][split];
+      const int places = whole ? prk::RG_MOST : prk::RG_FEW;
+      if (here > places - 2) continue;
+      const int64_t time = (n_rows + at_once - 1) / at_once *
+                           (whole ? here + 3 : std::max(2 * here, here + 3));
+      if (best < 0 || time < best) {
+        best = time;
+        s.split = split;
+        s.places = places;
+      }
+    }
+  const int64_t at_once = room[s.places == prk::RG_MOST][s.split];
+  s.here = (int)std::min<int64_t>((chunks + (1 << s.split) - 1) >> s.split, prk::RG_MOST + 1);
+  s.hold = s.here <= s.places;
+  s.spare = s.here < s.places;
+  s.groups = std::min<int64_t>(n_rows, at_once);
+  s.full = n_rows >= at_once;
+  return s;
+}
+
 inline void fill(prk::LossArgs& a, pr_ctx* c, const void* logits, int64_t n_rows, int64_t vocab,
           int64_t row_stride, const int32_t* chosen, const uint8_t* mask, const int64_t* offsets,
           int32_t n_req, const float* ref_logp, float temperature, float grad_scale, float* stats,
