@@ -11,7 +11,7 @@
 // g_v = n 2^(c x_v - k) with n = (b - A sigma) / (T R), which neither a small sigma
 // nor a small q makes lose anything.  The list's own entries and the label's are then written over
 // that.  S stays out of the sum, as a rest of 1e-6 has no digits in 1 - sum_S q; for
-// the same reason rho = 1 - sum_S p is summed in fp64 (a list is short).
+// the same reason rho = 1 - sum_S p is summed in two fp32 parts.
 #pragma once
 
 #include "pr_loss.cuh"
@@ -39,38 +39,41 @@ struct ListIn {
   int32_t y, count;
   float xy, edge;
 };
-template <typename T>
-__device__ __forceinline__ ListIn fetch_list(const DistillArgs& d, const Rows& rows, const Share& s,
-                                             const int4& ref, int lane) {
-  const LossArgs& a = d.a;
-  const int64_t row = ref.x;
-  const T* x = reinterpret_cast<const T*>(s.x);
+// A listed row's entries and scalars; then, once those are there, its logits at them.  Two steps, as
+// each waits for memory: a row's entries are fetched two rows ahead, its logits one.
+__device__ __forceinline__ ListIn fetch_list(const DistillArgs& d, const Rows& rows, const int4& ref,
+                                             int lane) {
   ListIn in;
   in.y = ref.z;
   in.count = 1;
-  in.xy = -INFINITY;
-  in.edge = 0.f;
-  in.id[0] = in.id[1] = -1;
-  in.t[0] = in.t[1] = in.x[0] = in.x[1] = -INFINITY;
-  if (ref.y < 0) return in;
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     const int j = 32 * h + lane;
-    if (j < d.k) {
-      in.id[h] = __ldcg(d.ids + row * d.k + j);
-      in.t[h] = __ldcg(d.t_logp + row * d.k + j);
-    }
+    const int64_t at = (int64_t)ref.x * d.k + j;
+    const bool on = ref.y >= 0 && j < d.k;
+    in.id[h] = on ? __ldcg(d.ids + at) : -1;
+    in.t[h] = on ? __ldcg(d.t_logp + at) : -INFINITY;
   }
+  if (d.a.norm && ref.y >= 0) in.count = rows.count(d.a, ref.y);
+  return in;
+}
+template <typename T>
+__device__ __forceinline__ void fetch_logits(const DistillArgs& d, const Share& s, const int4& ref,
+                                             ListIn& in, int lane) {
+  const LossArgs& a = d.a;
+  const T* x = reinterpret_cast<const T*>(s.x);
+  in.xy = -INFINITY;
+  in.edge = 0.f;
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     if (in.t[h] == -INFINITY) in.id[h] = -1;
+    in.x[h] = -INFINITY;
     if (in.id[h] >= 0 && (int64_t)in.id[h] < a.vocab) in.x[h] = Traits<T>::elem(x, in.id[h]);
   }
+  if (ref.y < 0) return;
   if (a.chosen && in.y >= 0 && (int64_t)in.y < a.vocab) in.xy = Traits<T>::elem(x, in.y);
-  if (a.norm) in.count = rows.count(a, ref.y);
   const int32_t v = end_of(a, s, lane);
   if (v >= 0) in.edge = Traits<T>::elem(x, v);
-  return in;
 }
 
 __device__ __forceinline__ float warp_sum(float v) {
@@ -82,6 +85,53 @@ __device__ __forceinline__ double warp_sum(double v) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(FULL, v, o);
   return v;
+}
+// A value as the sum of two fp32 numbers, for 1 - sum p.  (In fp64 the exponentials of a list and their
+// sum are 3,400 cycles of the warp that takes the rows' ends: 1,500 rows of V = 262,144 fp32 without
+// a gradient and lists of 64 784 us for 588.)
+struct Pair {
+  float hi, lo;
+};
+__device__ __forceinline__ Pair operator+(const Pair& a, const Pair& b) {
+  Pair r;
+  r.hi = a.hi + b.hi;
+  const float v = r.hi - a.hi;
+  r.lo = (a.lo + b.lo) + ((a.hi - (r.hi - v)) + (b.hi - v));
+  return r;
+}
+__device__ __forceinline__ Pair warp_sum(Pair v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    Pair w;
+    w.hi = __shfl_xor_sync(FULL, v.hi, o);
+    w.lo = __shfl_xor_sync(FULL, v.lo, o);
+    v = v + w;
+  }
+  return v;
+}
+// exp(t) within 2e-9 of itself: 2^n exp(z), t log2(e) = n + z log2(e) with z in two parts, and the
+// exponential's series, its first three terms in two parts
+__device__ __forceinline__ Pair exp_pair(float t) {
+  constexpr float L2E_LOW = 1.92596303e-8f;  // log2(e) - L2E
+  const float y = t * L2E, n = rintf(y), r = y - n;
+  const float y_lo = fmaf(t, L2E, -y) + t * L2E_LOW;
+  const float z = r * LN2, z_lo = fmaf(r, LN2, -z) + (r * LN2_LOW + y_lo * LN2);
+  float c = fmaf(z, 1.f / 362880.f, 1.f / 40320.f);
+  c = fmaf(z, c, 1.f / 5040.f);
+  c = fmaf(z, c, 1.f / 720.f);
+  c = fmaf(z, c, 1.f / 120.f);
+  c = fmaf(z, c, 1.f / 24.f);
+  c = fmaf(z, c, 1.f / 6.f);
+  c = c * z * z * z;
+  const float h = 0.5f * z, q = h * z, q_lo = fmaf(h, z, -q) + z * z_lo;
+  const float s1 = 1.f + z, e1 = z - (s1 - 1.f);
+  const float s2 = s1 + q, e2 = q - (s2 - s1);
+  const float s3 = s2 + c, e3 = c - (s3 - s2);
+  const float scale = n < -126.f ? 0.f : exp2f(n);  // (a power of two: exact)
+  Pair p;
+  p.hi = scale * s3;
+  p.lo = n < -100.f ? 0.f : scale * ((e1 + e2) + (e3 + (z_lo + q_lo)));
+  return p;
 }
 __device__ __forceinline__ float warp_max(float v) { return unord(__reduce_max_sync(FULL, ord(v))); }
 
@@ -102,11 +152,12 @@ __device__ __forceinline__ bool listed_twice(const ListIn& in, int lane) {
 // The large model's side of a row, which does not wait for the row's sum.
 struct ListPre {
   float p[2], lt[2];     // probabilities and their logarithms
+  float sum;             // of p
   float rho, l_rho, mass;
   bool bad, bad_id, labelled;
 };
 // Whole warp.
-static __device__ __noinline__ void list_pre(const DistillArgs& d, const ListIn& in, ListPre& o,
+__device__ __forceinline__ void list_pre(const DistillArgs& d, const ListIn& in, ListPre& o,
                                              int lane) {
   const LossArgs& a = d.a;
   bool bad_id = a.chosen && !(in.y >= 0 && (int64_t)in.y < a.vocab), bad = false, labelled = false;
@@ -122,7 +173,7 @@ static __device__ __noinline__ void list_pre(const DistillArgs& d, const ListIn&
   o.bad_id = __any_sync(FULL, bad_id) || twice;
   o.bad = __any_sync(FULL, bad);
   o.labelled = __any_sync(FULL, labelled);
-  o.rho = o.l_rho = o.mass = 0.f;
+  o.sum = o.rho = o.l_rho = o.mass = 0.f;
   if (d.none) {
     const float tm = warp_max(fmaxf(on[0] ? in.t[0] : -INFINITY, on[1] ? in.t[1] : -INFINITY));
 #pragma unroll
@@ -133,19 +184,21 @@ static __device__ __noinline__ void list_pre(const DistillArgs& d, const ListIn&
       o.lt[h] = (in.t[h] - tm) - lP;
       o.p[h] /= P;
     }
-    if (tm > -INFINITY) o.mass = expf(tm) * P;
+    if (tm > -INFINITY) {
+      o.sum = 1.f;
+      o.mass = expf(tm) * P;
+    }
   } else {
-    double s = 0.;
+    Pair v[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const double v = on[h] ? exp((double)in.t[h]) : 0.;
-      o.p[h] = (float)v;
+      v[h] = on[h] ? exp_pair(in.t[h]) : Pair{0.f, 0.f};
+      o.p[h] = v[h].hi;
       o.lt[h] = in.t[h];
-      s += v;
     }
-    s = warp_sum(s);
-    o.mass = (float)s;
-    o.rho = fmaxf((float)(1. - s), DS_RHO);
+    const Pair s = warp_sum(v[0] + v[1]);
+    o.sum = o.mass = s.hi;
+    o.rho = fmaxf((1.f - s.hi) - s.lo, DS_RHO);
     o.l_rho = logf(o.rho);
   }
 }
@@ -153,7 +206,7 @@ static __device__ __noinline__ void list_pre(const DistillArgs& d, const ListIn&
 // A row's end: its sum R against 2^k, the list's and label's logits left out.  Writes the
 // result (out, and the list's entries of the gradient to g), whose barrier learns of it first, then
 // the row's KL and the statistics' terms (weight wt).  Whole warp; apart from the kernel's registers.
-static __device__ __noinline__ void list_math(const DistillArgs& d, int64_t row, const ListIn& in,
+__device__ __forceinline__ void list_math(const DistillArgs& d, int64_t row, const ListIn& in,
                                               const ListPre& pre, float k, float R, float wt,
                                               bool writes, RowOut* out, float* g, uint64_t* out_bar,
                                               float2* stat, int lane) {
@@ -202,18 +255,61 @@ static __device__ __noinline__ void list_math(const DistillArgs& d, int64_t row,
   const bool is[2] = {first == lane, first == 32 + lane};
   const float listed = warp_sum((is[0] ? 0.f : e[0]) + (is[1] ? 0.f : e[1]));
   const float others = Rk + listed, S = any ? others + m : Rk;
-  const float L = log2f(S), inv = 1.f / S;
+  const float inv = 1.f / S;
   const bool most = any && m > 0.5f * S;
+  q[0] = on[0] ? e[0] * inv : 0.f;
+  q[1] = on[1] ? e[1] * inv : 0.f;
+  const float E = listed + (any ? m : 0.f), sigma = Rk * inv, not_y = R0 * f + E;
+  const bool klass = !d.none && rest;
+  float av[2] = {0.f, 0.f}, b = 0.f, kA = 0.f;
+  // the gradient, from a (av) and b, whose sum is kA
+  auto result = [&]() {
+    const float kc = d.kl_coef, cc = a.chosen ? d.ce_coef : 0.f;
+    const float w = wt * (a.grad_scale * a.inv_t), A = (kc != 0.f ? kc * kA : 0.f) - cc;
+    const float bc = kc != 0.f ? kc * b : 0.f;
+    float ac[2];
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    l[h] = most && is[h] ? -log1pf(others / m) : (u[h] - L) * LN2;
-    q[h] = on[h] ? e[h] * inv : 0.f;
+    for (int h = 0; h < 2; ++h) {
+      ac[h] = kc != 0.f ? kc * av[h] : 0.f;
+      if (on[h] && in.id[h] == in.y && a.chosen) ac[h] -= cc;
+    }
+    const float lesser = warp_sum((is[0] ? 0.f : ac[0]) + (is[1] ? 0.f : ac[1]));
+    const bool nan = bad || pre.bad_id;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      // a - A q = (a - A) + A (1 - q), with a - A = -(the other a and b)
+      const float v = most && is[h] ? fmaf(A, others * inv, -(lesser + bc - (apart ? cc : 0.f)))
+                                    : ac[h] - A * q[h];
+      g[32 * h + lane] = nan ? NAN : w * v;
+    }
+    if (lane == 0) {
+      RowOut o;
+      o.K = k;
+      o.M = 0.f;
+      o.nk = nan ? NAN : rest ? w * (bc - A * sigma) / R : 0.f;
+      o.mode = o.nk == 0.f ? ROW_ZERO : ROW_FAST;
+      // q_y (b / sigma - kA) - ce (1 - q_y)
+      o.gy = nan ? NAN : w * ((rest ? ey / R : 0.f) * (bc - (A + cc) * sigma) - cc * (not_y * inv));
+      *out = o;
+    }
+    __syncwarp();
+  };
+  if (!d.reverse) {  // its gradient needs no logarithm: given first
+    if (any) {
+      av[0] = -pre.p[0];
+      av[1] = -pre.p[1];
+      b = klass ? -pre.rho : 0.f;
+      kA = b - pre.sum;
+    }
+    if (out) result();
+    if (out_bar && lane == 0) bar_arrive(out_bar);
   }
-  const float E = listed + (any ? m : 0.f), sigma = Rk * inv;
+  const float L = log2f(S);
+#pragma unroll
+  for (int h = 0; h < 2; ++h) l[h] = most && is[h] ? -log1pf(others / m) : (u[h] - L) * LN2;
   const float l_sigma = Rk > 0.5f * S ? -log1pf(E / Rk) : (k - K + log2f(R) - L) * LN2;
   // the label
   float ce = 0.f;
-  const float not_y = R0 * f + E;
   if (apart) {
     ce = eyk > 0.25f * S ? log1pf(not_y / eyk) : -(fmaf(xy, a.c2, -K) - L) * LN2;
   } else if (a.chosen) {
@@ -221,24 +317,16 @@ static __device__ __noinline__ void list_math(const DistillArgs& d, int64_t row,
     const unsigned who = __ballot_sync(FULL, y0 || y1);
     ce = -__shfl_sync(FULL, y0 ? l[0] : l[1], who ? __ffs(who) - 1 : 0);
   }
-  // KL, a and b
-  const bool klass = !d.none && rest;
-  float kl = 0.f, av[2] = {0.f, 0.f}, b = 0.f, kA = 0.f;
-  if (any) {
-    if (!d.reverse) {
+  // the divergence
+  float kl = 0.f;
+  if (!d.reverse) {
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        if (pre.p[h] > 0.f) kl += pre.p[h] * (pre.lt[h] - l[h]);
-        av[h] = -pre.p[h];
-      }
-      kl = warp_sum(kl);
-      kA = warp_sum(av[0] + av[1]);
-      if (klass) {
-        kl += pre.rho * (pre.l_rho - l_sigma);
-        b = -pre.rho;
-        kA += b;
-      }
-    } else {  // (a and b add up to 0)
+    for (int h = 0; h < 2; ++h)
+      if (pre.p[h] > 0.f) kl += pre.p[h] * (pre.lt[h] - l[h]);
+    kl = warp_sum(kl);
+    if (klass && any) kl += pre.rho * (pre.l_rho - l_sigma);
+  } else {
+    if (any) {  // (a and b add up to 0)
       av[0] = q[0];
       av[1] = q[1];
       if (d.none) {  // q over the list
@@ -258,46 +346,16 @@ static __device__ __noinline__ void list_math(const DistillArgs& d, int64_t row,
         if (av[h] > 0.f) kl += av[h] * (l[h] - pre.lt[h]);
       kl = warp_sum(kl);
       const float far = l_sigma - pre.l_rho;
-      if (klass && sigma > 0.f) kl += sigma * far;
+      const bool out_there = klass && sigma > 0.f;
+      if (out_there) kl += sigma * far;
 #pragma unroll
       for (int h = 0; h < 2; ++h) av[h] = av[h] > 0.f ? av[h] * (l[h] - pre.lt[h] - kl) : 0.f;
-      if (klass && sigma > 0.f) b = sigma * (far - kl);
+      if (out_there) b = sigma * (far - kl);
     }
+    if (out) result();
+    if (out_bar && lane == 0) bar_arrive(out_bar);
   }
   bad |= pre.bad_id;
-  // the gradient
-  if (out) {
-    const float kc = d.kl_coef, cc = a.chosen ? d.ce_coef : 0.f;
-    const float w = wt * (a.grad_scale * a.inv_t);
-    b = kc != 0.f ? kc * b : 0.f;
-    kA = kc != 0.f ? kc * kA : 0.f;
-    const float A = kA - cc;
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      av[h] = kc != 0.f ? kc * av[h] : 0.f;
-      if (on[h] && in.id[h] == in.y && a.chosen) av[h] -= cc;
-    }
-    const float lesser = warp_sum((is[0] ? 0.f : av[0]) + (is[1] ? 0.f : av[1]));
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      // a - A q = (a - A) + A (1 - q), with a - A = -(the other a and b)
-      const float v = most && is[h] ? fmaf(A, others * inv, -(lesser + b - (apart ? cc : 0.f)))
-                                    : av[h] - A * q[h];
-      g[32 * h + lane] = bad ? NAN : w * v;
-    }
-    if (lane == 0) {
-      RowOut o;
-      o.K = k;
-      o.M = 0.f;
-      o.nk = bad ? NAN : rest ? w * (b - A * sigma) / R : 0.f;
-      o.mode = o.nk == 0.f ? ROW_ZERO : ROW_FAST;
-      // q_y (b / sigma - kA) - ce (1 - q_y)
-      o.gy = bad ? NAN : w * ((rest ? ey / R : 0.f) * (b - kA * sigma) - cc * (not_y * inv));
-      *out = o;
-    }
-    __syncwarp();
-  }
-  if (out_bar && lane == 0) bar_arrive(out_bar);
   if (bad) kl = ce = NAN;
   if (lane < DS_TERMS) {
     const float t = wt * (lane == 0 ? kl : lane == 1 ? ce : bad ? NAN : lane == 2 ? pre.mass : E * inv);
@@ -410,6 +468,7 @@ struct Mine {
 };
 struct Ids {
   int32_t id[2];
+  float t[2];
 };
 __device__ __forceinline__ Ids fetch_ids(const DistillArgs& d, const int4& ref, int lane) {
   Ids r;
@@ -417,7 +476,9 @@ __device__ __forceinline__ Ids fetch_ids(const DistillArgs& d, const int4& ref, 
   for (int h = 0; h < 2; ++h) {
     const int j = 32 * h + lane;
     const int64_t at = (int64_t)ref.x * d.k + j;
-    r.id[h] = ref.y >= 0 && j < d.k && __ldcg(d.t_logp + at) != -INFINITY ? __ldcg(d.ids + at) : -1;
+    const bool on = ref.y >= 0 && j < d.k;
+    r.id[h] = on ? __ldcg(d.ids + at) : -1;  // (both loads at once: the row is the next one)
+    r.t[h] = on ? __ldcg(d.t_logp + at) : -INFINITY;
   }
   return r;
 }
@@ -425,11 +486,12 @@ template <int VEC>
 __device__ __forceinline__ Mine mine_of(const DistillArgs& d, const Share& s, const Ids& ids, int32_t y,
                                         int warp, int lane) {
   Mine m;
-  const bool listed = ids.id[0] == y || ids.id[1] == y;
+  const int32_t l[2] = {ids.t[0] == -INFINITY ? -1 : ids.id[0], ids.t[1] == -INFINITY ? -1 : ids.id[1]};
+  const bool listed = l[0] == y || l[1] == y;
   const bool apart = d.a.chosen && !__any_sync(FULL, listed);
 #pragma unroll
   for (int h = 0; h < 3; ++h) {
-    const int32_t id = h < 2 ? ids.id[h] : apart && lane == 0 ? y : -1;
+    const int32_t id = h < 2 ? l[h] : apart && lane == 0 ? y : -1;
     const int32_t e = id - s.head, w = e / VEC - s.w0;  // (a negative e divides to a word of its own check)
     const bool in = id >= s.head && w >= 0 && e / VEC < s.w1;
     m.e[h] = in && ((w % (32 * RG_NW)) >> 5) == warp ? e : -1;
@@ -543,8 +605,9 @@ __global__ void __launch_bounds__(RG_NT, 2)
     // ---- the rows' ends
     const double share = rows.share(a);
     uint32_t n = 0;
-    int4 ref = ref_of(first), ref1 = ref_of(first + G);
-    ListIn in = fetch_list<T>(d, rows, share_of<T>(a, ref.x, C, rank), ref, lane);
+    int4 ref = ref_of(first), ref1 = ref_of(first + G), ref2 = ref_of(first + 2 * G);
+    ListIn in = fetch_list(d, rows, ref, lane), next = fetch_list(d, rows, ref1, lane);
+    fetch_logits<T>(d, share_of<T>(a, ref.x, C, rank), ref, in, lane);
     // What a peer's gradient may be written over (the logits' own buffer) has been read when
     // this CTA's sums are sent: the next row's logits are there before a result is given.
     auto landed = [&](ListIn& q) {
@@ -558,13 +621,16 @@ __global__ void __launch_bounds__(RG_NT, 2)
     for (int64_t i = first; i < live; i += G) {
       const int64_t row = ref.x;
       const Share sh = share_of<T>(a, row, C, rank);
-      ListIn next = fetch_list<T>(d, rows, share_of<T>(a, ref1.x, C, rank), ref1, lane);
+      fetch_logits<T>(d, share_of<T>(a, ref1.x, C, rank), ref1, next, lane);
+      const ListIn after = fetch_list(d, rows, ref2, lane);
       ref = ref1;
-      ref1 = ref_of(i + 2 * G);
+      ref1 = ref2;
+      ref2 = ref_of(i + 3 * G);
       const int32_t v = end_of(a, sh, lane);
       const int kind = sh.head + sh.tail ? end_kind(d, sh, in, v, lane) : DS_REST;
       ListPre pre;
       list_pre(d, in, pre, lane);
+      const float wt = (float)(a.norm ? share / (double)in.count : share);
       T* const g = reinterpret_cast<T*>(a.grad) + row * a.grad_stride;
       const int s = n % RG_SLOTS;
       const uint32_t phase = (n / RG_SLOTS) & 1u;
@@ -586,13 +652,13 @@ __global__ void __launch_bounds__(RG_NT, 2)
         join(p, 1.f, k, R);
       }
       add_rest_ends(d, sh, in, v, kind, k, R);
-      const float wt = (float)(a.norm ? share / (double)in.count : share);
-      landed(next);
+      if (C > 1) landed(next);
       list_math(d, row, in, pre, k, R, wt, rank == 0, HOLD ? &sm.out[s] : nullptr, entries,
                 &sm.out_bar[s], sm.stat, lane);
       __syncwarp();
       if (HOLD && rank == 0) put_end(g, v, kind, sm.out[s], entries, a.c2, in.edge);
       in = next;
+      next = after;
     }
   } else {
     // ---- the rows' words
@@ -777,8 +843,9 @@ __global__ void __launch_bounds__(32 * RW_MOST, 2)
             "l"(sh.x + sizeof(T) * sh.head), "r"(n), "r"(sm_addr(full))
             : "memory");
     }
-    const ListIn in = fetch_list<T>(d, rows, sh, ref, lane);
+    ListIn in = fetch_list(d, rows, ref, lane);
     const int4 ref1 = rows.at(a, i + G);
+    fetch_logits<T>(d, sh, ref, in, lane);
     const int32_t v = end_of(a, sh, lane);
     const int kind = sh.head + sh.tail ? end_kind(d, sh, in, v, lane) : DS_REST;
     ListPre pre;
