@@ -35,10 +35,21 @@ struct DistillArgs {
 // a row's list and scalars: entries lane and 32 + lane, absent ones with id -1
 struct ListIn {
   int32_t id[2];
-  float t[2], x[2];
+  float t[2];
   int32_t y, count;
-  float xy, edge;
+  uint32_t x[2], xy, edge;  // logits as they came from memory: what widens them would wait for them
 };
+template <typename T>
+__device__ __forceinline__ uint32_t raw_at(const void* row, int64_t v) {
+  if constexpr (sizeof(T) == 2) return reinterpret_cast<const uint16_t*>(row)[v];
+  else return reinterpret_cast<const uint32_t*>(row)[v];
+}
+template <typename T>
+__device__ __forceinline__ float wide(uint32_t raw) {
+  return __uint_as_float(sizeof(T) == 2 ? raw << 16 : raw);
+}
+template <typename T>
+constexpr uint32_t DS_MASKED = sizeof(T) == 2 ? 0xff80u : 0xff800000u;  // -inf
 // A listed row's entries and scalars; then, once those are there, its logits at them.  Two steps, as
 // each waits for memory: a row's entries are fetched two rows ahead, its logits one.
 __device__ __forceinline__ ListIn fetch_list(const DistillArgs& d, const Rows& rows, const int4& ref,
@@ -61,19 +72,18 @@ template <typename T>
 __device__ __forceinline__ void fetch_logits(const DistillArgs& d, const Share& s, const int4& ref,
                                              ListIn& in, int lane) {
   const LossArgs& a = d.a;
-  const T* x = reinterpret_cast<const T*>(s.x);
-  in.xy = -INFINITY;
-  in.edge = 0.f;
+  in.xy = DS_MASKED<T>;
+  in.edge = 0u;
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     if (in.t[h] == -INFINITY) in.id[h] = -1;
-    in.x[h] = -INFINITY;
-    if (in.id[h] >= 0 && (int64_t)in.id[h] < a.vocab) in.x[h] = Traits<T>::elem(x, in.id[h]);
+    in.x[h] = DS_MASKED<T>;
+    if (in.id[h] >= 0 && (int64_t)in.id[h] < a.vocab) in.x[h] = raw_at<T>(s.x, in.id[h]);
   }
   if (ref.y < 0) return;
-  if (a.chosen && in.y >= 0 && (int64_t)in.y < a.vocab) in.xy = Traits<T>::elem(x, in.y);
+  if (a.chosen && in.y >= 0 && (int64_t)in.y < a.vocab) in.xy = raw_at<T>(s.x, in.y);
   const int32_t v = end_of(a, s, lane);
-  if (v >= 0) in.edge = Traits<T>::elem(x, v);
+  if (v >= 0) in.edge = raw_at<T>(s.x, v);
 }
 
 __device__ __forceinline__ float warp_sum(float v) {
@@ -142,6 +152,7 @@ __device__ __forceinline__ bool listed_twice(const ListIn& in, int lane) {
   const unsigned m0 = __match_any_sync(FULL, in.id[0]), m1 = __match_any_sync(FULL, in.id[1]);
   twice = (in.id[0] >= 0 && m0 != at) || (in.id[1] >= 0 && m1 != at);
   if (__any_sync(FULL, in.id[1] >= 0))
+#pragma unroll 8
     for (int o = 0; o < 32; ++o) {
       const int32_t other = __shfl_xor_sync(FULL, in.id[1], o);  // (by every lane)
       twice |= in.id[0] >= 0 && in.id[0] == other;
@@ -178,11 +189,11 @@ __device__ __forceinline__ void list_pre(const DistillArgs& d, const ListIn& in,
     const float tm = warp_max(fmaxf(on[0] ? in.t[0] : -INFINITY, on[1] ? in.t[1] : -INFINITY));
 #pragma unroll
     for (int h = 0; h < 2; ++h) o.p[h] = on[h] ? expf(in.t[h] - tm) : 0.f;
-    const float P = warp_sum(o.p[0] + o.p[1]), lP = logf(P);
+    const float P = warp_sum(o.p[0] + o.p[1]), lP = logf(P), inv = __fdividef(1.f, P);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       o.lt[h] = (in.t[h] - tm) - lP;
-      o.p[h] /= P;
+      o.p[h] *= inv;
     }
     if (tm > -INFINITY) {
       o.sum = 1.f;
@@ -206,6 +217,7 @@ __device__ __forceinline__ void list_pre(const DistillArgs& d, const ListIn& in,
 // A row's end: its sum R against 2^k, the list's and label's logits left out.  Writes the
 // result (out, and the list's entries of the gradient to g), whose barrier learns of it first, then
 // the row's KL and the statistics' terms (weight wt).  Whole warp; apart from the kernel's registers.
+template <typename T>
 __device__ __forceinline__ void list_math(const DistillArgs& d, int64_t row, const ListIn& in,
                                               const ListPre& pre, float k, float R, float wt,
                                               bool writes, RowOut* out, float* g, uint64_t* out_bar,
@@ -217,11 +229,12 @@ __device__ __forceinline__ void list_math(const DistillArgs& d, int64_t row, con
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     on[h] = in.id[h] != -1;
-    x[h] = in.x[h] <= -d.big ? -INFINITY : in.x[h];
+    x[h] = wide<T>(in.x[h]);
+    if (x[h] <= -d.big) x[h] = -INFINITY;
     bad |= on[h] && !(x[h] < d.big);
   }
   const bool apart = a.chosen && !pre.labelled;
-  const float xy = in.xy <= -d.big ? -INFINITY : in.xy;
+  const float yx = wide<T>(in.xy), xy = yx <= -d.big ? -INFINITY : yx;
   bad |= pre.bad || !(k < big) || !(R >= 0.f) || !(R < INFINITY) || (a.chosen && !(xy < d.big));
   bad = __any_sync(FULL, bad);
   if (!(k > -big)) R = 0.f;
@@ -229,8 +242,8 @@ __device__ __forceinline__ void list_math(const DistillArgs& d, int64_t row, con
   float R0 = R, ey = 0.f;
   if (apart && xy > -INFINITY) {
     const float top = R > 0.f ? fmaxf(k, xy * a.c2) : xy * a.c2;
-    R0 = R > 0.f ? R * exp2f(k - top) : 0.f;
-    ey = exp2f(fmaf(xy, a.c2, -top));
+    R0 = R > 0.f ? R * ex2(k - top) : 0.f;
+    ey = ex2(fmaf(xy, a.c2, -top));
     R = R0 + ey;
     k = top;
   }
@@ -244,9 +257,9 @@ __device__ __forceinline__ void list_math(const DistillArgs& d, int64_t row, con
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     u[h] = on[h] ? fmaf(x[h], a.c2, -K) : -INFINITY;
-    e[h] = exp2f(u[h]);
+    e[h] = ex2(u[h]);
   }
-  const float f = rest ? exp2f(k - K) : 0.f, Rk = R * f, eyk = ey * f;
+  const float f = rest ? ex2(k - K) : 0.f, Rk = R * f, eyk = ey * f;
   // the largest listed term stays out of the sum of the others: 1 - q of it is others / S
   const float m = warp_max(fmaxf(e[0], e[1]));
   const unsigned w0 = __ballot_sync(FULL, on[0] && e[0] == m), w1 = __ballot_sync(FULL, on[1] && e[1] == m);
@@ -255,7 +268,7 @@ __device__ __forceinline__ void list_math(const DistillArgs& d, int64_t row, con
   const bool is[2] = {first == lane, first == 32 + lane};
   const float listed = warp_sum((is[0] ? 0.f : e[0]) + (is[1] ? 0.f : e[1]));
   const float others = Rk + listed, S = any ? others + m : Rk;
-  const float inv = 1.f / S;
+  const float inv = __fdividef(1.f, S);  // (S is at least about 1)
   const bool most = any && m > 0.5f * S;
   q[0] = on[0] ? e[0] * inv : 0.f;
   q[1] = on[1] ? e[1] * inv : 0.f;
@@ -286,10 +299,11 @@ __device__ __forceinline__ void list_math(const DistillArgs& d, int64_t row, con
       RowOut o;
       o.K = k;
       o.M = 0.f;
-      o.nk = nan ? NAN : rest ? w * (bc - A * sigma) / R : 0.f;
+      const float per_R = rest ? __fdividef(1.f, R) : 0.f;
+      o.nk = nan ? NAN : w * (bc - A * sigma) * per_R;
       o.mode = o.nk == 0.f ? ROW_ZERO : ROW_FAST;
       // q_y (b / sigma - kA) - ce (1 - q_y)
-      o.gy = nan ? NAN : w * ((rest ? ey / R : 0.f) * (bc - (A + cc) * sigma) - cc * (not_y * inv));
+      o.gy = nan ? NAN : w * (ey * per_R * (bc - (A + cc) * sigma) - cc * (not_y * inv));
       *out = o;
     }
     __syncwarp();
@@ -304,18 +318,31 @@ __device__ __forceinline__ void list_math(const DistillArgs& d, int64_t row, con
     if (out) result();
     if (out_bar && lane == 0) bar_arrive(out_bar);
   }
-  const float L = log2f(S);
-#pragma unroll
-  for (int h = 0; h < 2; ++h) l[h] = most && is[h] ? -log1pf(others / m) : (u[h] - L) * LN2;
-  const float l_sigma = Rk > 0.5f * S ? -log1pf(E / Rk) : (k - K + log2f(R) - L) * LN2;
-  // the label
+  // log q, of what single precision holds from q itself (1.5 x 2^-24 off, whatever the exponents)
+  auto log_q = [&](float v, float exponent) {
+    return v > 1e-30f ? logf(v) : (exponent - log2f(S)) * LN2;
+  };
+  l[0] = log_q(q[0], u[0]);
+  l[1] = log_q(q[1], u[1]);
+  const float l_sigma = log_q(sigma, k - K + log2f(R));
+  // the label, from 1 - q where that is small
   float ce = 0.f;
-  if (apart) {
-    ce = eyk > 0.25f * S ? log1pf(not_y / eyk) : -(fmaf(xy, a.c2, -K) - L) * LN2;
-  } else if (a.chosen) {
-    const bool y0 = on[0] && in.id[0] == in.y, y1 = on[1] && in.id[1] == in.y;
-    const unsigned who = __ballot_sync(FULL, y0 || y1);
-    ce = -__shfl_sync(FULL, y0 ? l[0] : l[1], who ? __ffs(who) - 1 : 0);
+  if (a.chosen) {
+    float v, less, exponent;
+    if (apart) {
+      v = eyk * inv;
+      less = not_y * inv;
+      exponent = fmaf(xy, a.c2, -K);
+    } else {
+      const bool y0 = on[0] && in.id[0] == in.y, y1 = on[1] && in.id[1] == in.y;
+      const unsigned who = __ballot_sync(FULL, y0 || y1);
+      const int from = who ? __ffs(who) - 1 : 0;
+      const bool sure = most && (y0 ? is[0] : is[1]);
+      v = __shfl_sync(FULL, y0 ? q[0] : q[1], from);
+      less = __shfl_sync(FULL, sure ? others * inv : 1.f - (y0 ? q[0] : q[1]), from);
+      exponent = __shfl_sync(FULL, y0 ? u[0] : u[1], from);
+    }
+    ce = v > 0.5f ? -log1pf(-less) : -log_q(v, exponent);
   }
   // the divergence
   float kl = 0.f;
@@ -333,12 +360,12 @@ __device__ __forceinline__ void list_math(const DistillArgs& d, int64_t row, con
         const float um = warp_max(fmaxf(u[0], u[1]));
         if (um == -INFINITY) bad = true;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) av[h] = on[h] ? exp2f(u[h] - um) : 0.f;
-        const float Q = warp_sum(av[0] + av[1]), lQ = logf(Q);
+        for (int h = 0; h < 2; ++h) av[h] = on[h] ? ex2(u[h] - um) : 0.f;
+        const float Q = warp_sum(av[0] + av[1]), lQ = logf(Q), per_Q = __fdividef(1.f, Q);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           l[h] = (u[h] - um) * LN2 - lQ;
-          av[h] /= Q;
+          av[h] *= per_Q;
         }
       }
 #pragma unroll
@@ -424,17 +451,17 @@ __device__ __forceinline__ int end_kind(const DistillArgs& d, const Share& s, co
   }
   return kind;
 }
-__device__ __forceinline__ void add_rest_ends(const DistillArgs& d, const Share& s, const ListIn& in,
+__device__ __forceinline__ void add_rest_ends(const DistillArgs& d, const Share& s, float edge,
                                               int32_t v, int kind, float& k, float& R) {
   if (s.head + s.tail == 0) return;
   const float c2 = d.a.c2;
   const bool add = v >= 0 && kind == DS_REST;
-  const float top = warp_max(add ? fmaxf(in.edge * c2, -3e38f) : -3e38f);
+  const float top = warp_max(add ? fmaxf(edge * c2, -3e38f) : -3e38f);
   if (top > k) {
     R *= rescale2(k - top);
     k = top;
   }
-  R += warp_sum(add ? ex2(fmaf(in.edge, c2, -k)) : 0.f);
+  R += warp_sum(add ? ex2(fmaf(edge, c2, -k)) : 0.f);
 }
 template <typename T>
 __device__ __forceinline__ void put_end(T* g, int32_t v, int kind, const RowOut& o, const float* list,
@@ -442,8 +469,8 @@ __device__ __forceinline__ void put_end(T* g, int32_t v, int kind, const RowOut&
   if (v >= 0) put(g + v, kind >= 0 ? list[kind] : kind == DS_LABEL ? o.gy : grad1(o, c2, edge));
 }
 
-// Element `e` of a row in shared memory is no part of its sum.  (Written by this thread's proxy, and
-// the next copy into the place by the other one: fenced by the writer.)
+// Element `e` of a row in shared memory is no part of its sum.  (The next copy into the place is the
+// async proxy's: a fence before the place is given back.)
 template <typename T>
 __device__ __forceinline__ void leave_out(unsigned char* row, int32_t e) {
   if constexpr (sizeof(T) == 2) reinterpret_cast<uint16_t*>(row)[e] = 0xff80u;
@@ -460,11 +487,16 @@ __device__ __forceinline__ void fence_async() {
 // them, one takes the row's end.  Before a warp sums its words of a chunk, the lanes that
 // hold one of the row's listed tokens there write -inf over it; when it has written the words'
 // gradient, the same lanes write the list's entries over that.
+//
+// Without a gradient nothing has to be held, and `parts` of a row may go through one CTA, one after the
+// other: a row of a cluster's eight parts fills 120 of 152 SMs, as clusters of eight find no more room.
+// Sums are kept apart as a cluster's CTAs keep them, so that the loss has the same bits.
 
 // a lane's tokens among its warp's words of this CTA's part of a row: their elements from the
 // row's first word on, or -1
 struct Mine {
-  int32_t e[3];  // entries lane and 32 + lane; the label (lane 0)
+  int32_t e[3];     // entries lane and 32 + lane; the label (lane 0)
+  uint32_t chunks;  // of the CTA's part in which the warp has any, a bit each
 };
 struct Ids {
   int32_t id[2];
@@ -486,6 +518,7 @@ template <int VEC>
 __device__ __forceinline__ Mine mine_of(const DistillArgs& d, const Share& s, const Ids& ids, int32_t y,
                                         int warp, int lane) {
   Mine m;
+  m.chunks = 0u;
   const int32_t l[2] = {ids.t[0] == -INFINITY ? -1 : ids.id[0], ids.t[1] == -INFINITY ? -1 : ids.id[1]};
   const bool listed = l[0] == y || l[1] == y;
   const bool apart = d.a.chosen && !__any_sync(FULL, listed);
@@ -494,8 +527,11 @@ __device__ __forceinline__ Mine mine_of(const DistillArgs& d, const Share& s, co
     const int32_t id = h < 2 ? l[h] : apart && lane == 0 ? y : -1;
     const int32_t e = id - s.head, w = e / VEC - s.w0;  // (a negative e divides to a word of its own check)
     const bool in = id >= s.head && w >= 0 && e / VEC < s.w1;
-    m.e[h] = in && ((w % (32 * RG_NW)) >> 5) == warp ? e : -1;
+    const bool here = in && ((w % (32 * RG_NW)) >> 5) == warp;
+    m.e[h] = here ? e : -1;
+    m.chunks |= here ? 1u << (w / RG_CHUNK) : 0u;
   }
+  m.chunks = __reduce_or_sync(FULL, m.chunks);
   return m;
 }
 
@@ -520,7 +556,8 @@ static_assert(distill_start(4, RG_FEW, 0) <= 1024 && distill_start(1, RG_FEW, 1)
 
 template <typename T, bool HOLD, bool OWN>
 __global__ void __launch_bounds__(RG_NT, 2)
-    distill_ring(const __grid_constant__ DistillArgs d, const int places, const int lag) {
+    distill_ring(const __grid_constant__ DistillArgs d, const int places, const int lag,
+                 const int parts) {
   extern __shared__ __align__(16) unsigned char smem_raw[];
   DistillCtl& sm = *reinterpret_cast<DistillCtl*>(smem_raw);
   const LossArgs& a = d.a;
@@ -530,11 +567,13 @@ __global__ void __launch_bounds__(RG_NT, 2)
   asm("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(C));
   asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
   const int64_t G = gridDim.x / C, first = blockIdx.x / C;
+  const uint32_t P = HOLD ? C : C * parts;  // parts of a row; this CTA has rank, or all of them
+  const uint32_t p_first = HOLD || parts == 1 ? rank : 0, p_last = HOLD || parts == 1 ? rank + 1 : P;
   uint64_t* const full = reinterpret_cast<uint64_t*>(smem_raw + DS_BARS);
   uint64_t* const empty = full + places;
   float2* const sums = reinterpret_cast<float2*>(smem_raw + distill_sums(places));
-  float* const list = reinterpret_cast<float*>(smem_raw + distill_list((int)C, places));
-  unsigned char* const ring = smem_raw + distill_start((int)C, places, lag);
+  float* const list = reinterpret_cast<float*>(smem_raw + distill_list((int)P, places));
+  unsigned char* const ring = smem_raw + distill_start((int)P, places, lag);
   if (threadIdx.x == 0) {
     for (int i = 0; i < places; ++i) {
       bar_init(&full[i], 1);
@@ -578,22 +617,24 @@ __global__ void __launch_bounds__(RG_NT, 2)
     int4 ref = ref_of(first);
     for (int64_t i = first; i < live; i += G) {
       const int4 ref1 = ref_of(i + G);
-      const Share sh = share_of<T>(a, ref.x, C, rank);
-      const char* src = sh.x + sizeof(T) * sh.head + 16 * (int64_t)sh.w0;
-      for (int32_t left = sh.w1 - sh.w0; left > 0; left -= RG_CHUNK) {
-        if (n >= places) wait(&empty[place], turn ^ 1u);
-        if (ok && lane == 0) {
-          const uint32_t bytes = 16u * (uint32_t)min(RG_CHUNK, left);
-          bar_expect(&full[place], bytes);
-          asm volatile(
-              "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::
-                  "r"(sm_addr(ring + (size_t)place * RG_BYTES)),
-              "l"(src), "r"(bytes), "r"(sm_addr(&full[place]))
-              : "memory");
+      for (uint32_t p = p_first; p < p_last; ++p) {
+        const Share sh = share_of<T>(a, ref.x, P, p);
+        const char* src = sh.x + sizeof(T) * sh.head + 16 * (int64_t)sh.w0;
+        for (int32_t left = sh.w1 - sh.w0; left > 0; left -= RG_CHUNK) {
+          if (n >= places) wait(&empty[place], turn ^ 1u);
+          if (ok && lane == 0) {
+            const uint32_t bytes = 16u * (uint32_t)min(RG_CHUNK, left);
+            bar_expect(&full[place], bytes);
+            asm volatile(
+                "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::
+                    "r"(sm_addr(ring + (size_t)place * RG_BYTES)),
+                "l"(src), "r"(bytes), "r"(sm_addr(&full[place]))
+                : "memory");
+          }
+          src += RG_BYTES;
+          if (ok) ++n;
+          step();
         }
-        src += RG_BYTES;
-        if (ok) ++n;
-        step();
       }
       ref = ref1;
     }
@@ -639,10 +680,10 @@ __global__ void __launch_bounds__(RG_NT, 2)
       wait(&sm.sum_bar[s], phase);
       float k, R;
       {
-        const float2* q = sums + s * RG_NW * C;
+        const float2* q = sums + s * RG_NW * P;
         const float2 none = make_float2(-3e38f, 0.f);
-        float2 p = lane < (int)(RG_NW * C) ? q[lane] : none;
-        if (C > 4) {
+        float2 p = lane < (int)(RG_NW * P) ? q[lane] : none;
+        if (P > 4) {
           const float2 p2 = q[32 + lane];
           const float top = fmaxf(p.x, p2.x);
           p = make_float2(top, p.y * rescale2(p.x - top) + p2.y * rescale2(p2.x - top));
@@ -651,12 +692,12 @@ __global__ void __launch_bounds__(RG_NT, 2)
         if (C > 1 && lane == 0) bar_expect(&sm.sum_bar[s], 8 * RG_NW * C);
         join(p, 1.f, k, R);
       }
-      add_rest_ends(d, sh, in, v, kind, k, R);
+      add_rest_ends(d, sh, wide<T>(in.edge), v, kind, k, R);
       if (C > 1) landed(next);
-      list_math(d, row, in, pre, k, R, wt, rank == 0, HOLD ? &sm.out[s] : nullptr, entries,
+      list_math<T>(d, row, in, pre, k, R, wt, rank == 0, HOLD ? &sm.out[s] : nullptr, entries,
                 &sm.out_bar[s], sm.stat, lane);
       __syncwarp();
-      if (HOLD && rank == 0) put_end(g, v, kind, sm.out[s], entries, a.c2, in.edge);
+      if (HOLD && rank == 0) put_end(g, v, kind, sm.out[s], entries, a.c2, wide<T>(in.edge));
       in = next;
       next = after;
     }
@@ -678,51 +719,52 @@ __global__ void __launch_bounds__(RG_NT, 2)
     while ((HOLD ? m : n) < mine) {
       if (n < mine) {
         // forward
-        const Share sh = share_of<T>(a, ref.x, C, rank);
-        own = mine_of<Tr::VEC>(d, sh, ids, ref.z, warp, lane);
-        if (m == n) kept = own;
-        ids = fetch_ids(d, next, lane);
-        float k = -3e38f;
-        float2 S = make_float2(0.f, 0.f);
-        for (int32_t w = sh.w0; w < sh.w1; w += RG_CHUNK) {
-          wait(&full[place], turn);
-          unsigned char* const here = ring + (size_t)place * RG_BYTES;
-          bool wrote = false;
-#pragma unroll
-          for (int h = 0; h < 3; ++h)
-            if (within(own.e[h], w)) {
-              leave_out<T>(here, own.e[h] - w * Tr::VEC);
-              wrote = true;
-            }
-          if (wrote) fence_async();
-          __syncwarp();
-          const uint4* st = reinterpret_cast<const uint4*>(here) + at;
-          uint4 v[RG_W];
-#pragma unroll
-          for (int q = 0; q < RG_W; ++q) v[q] = st[32 * RG_NW * q];
-          if (w + RG_CHUNK > sh.w1) {
-#pragma unroll
-            for (int q = 0; q < RG_W; ++q)
-              if (w + 32 * RG_NW * q + at >= sh.w1)
-                v[q] = make_uint4(Tr::NEG_WORD, Tr::NEG_WORD, Tr::NEG_WORD, Tr::NEG_WORD);
-          }
-          if (!HOLD) {
-            __syncwarp();  // every lane has its words
-            if (lane == 0) bar_arrive(&empty[place]);
-          }
-          step();
-          add_words<T>(k, S, v, a.c2, w == sh.w0);
-        }
-        float R;
-        join(make_float2(k, S.x + S.y), 1.f, k, R);
         const int s = n % RG_SLOTS;
-        if (!HOLD && n >= 1) wait(&sm.out_bar[s ^ 1], ((n - 1) / RG_SLOTS) & 1u);
-        if (C > 1) {
-          send(sums + (s * C + rank) * RG_NW + warp, &sm.sum_bar[s], k, R, C, lane);
-        } else if (lane == 0) {
-          sums[s * RG_NW + warp] = make_float2(k, R);
-          bar_arrive(&sm.sum_bar[s]);
+        const Ids here_ids = ids;
+        ids = fetch_ids(d, next, lane);
+        for (uint32_t p = p_first; p < p_last; ++p) {
+          const Share sh = share_of<T>(a, ref.x, P, p);
+          own = mine_of<Tr::VEC>(d, sh, here_ids, ref.z, warp, lane);
+          if (m == n) kept = own;
+          float k = -3e38f;
+          float2 S = make_float2(0.f, 0.f);
+          uint32_t chunks = own.chunks;
+          for (int32_t w = sh.w0; w < sh.w1; w += RG_CHUNK, chunks >>= 1) {
+            wait(&full[place], turn);
+            unsigned char* const here = ring + (size_t)place * RG_BYTES;
+            if (chunks & 1u) {
+#pragma unroll
+              for (int h = 0; h < 3; ++h)
+                if (within(own.e[h], w)) leave_out<T>(here, own.e[h] - w * Tr::VEC);
+              __syncwarp();
+            }
+            const uint4* st = reinterpret_cast<const uint4*>(here) + at;
+            uint4 v[RG_W];
+#pragma unroll
+            for (int q = 0; q < RG_W; ++q) v[q] = st[32 * RG_NW * q];
+            if (w + RG_CHUNK > sh.w1) {
+#pragma unroll
+              for (int q = 0; q < RG_W; ++q)
+                if (w + 32 * RG_NW * q + at >= sh.w1)
+                  v[q] = make_uint4(Tr::NEG_WORD, Tr::NEG_WORD, Tr::NEG_WORD, Tr::NEG_WORD);
+            }
+            if (!HOLD) {
+              __syncwarp();  // every lane has its words
+              if (lane == 0) {
+                if (chunks & 1u) fence_async();
+                bar_arrive(&empty[place]);
+              }
+            }
+            step();
+            add_words<T>(k, S, v, a.c2, w == sh.w0);
+          }
+          float R;
+          join(make_float2(k, S.x + S.y), 1.f, k, R);
+          if (!HOLD && p == p_first && n >= 1) wait(&sm.out_bar[s ^ 1], ((n - 1) / RG_SLOTS) & 1u);
+          if (C > 1) send(sums + (s * C + rank) * RG_NW + warp, &sm.sum_bar[s], k, R, C, lane);
+          else if (lane == 0) sums[(s * P + p) * RG_NW + warp] = make_float2(k, R);
         }
+        if (C == 1 && lane == 0) bar_arrive(&sm.sum_bar[s]);
         last = ref;
         ++n;
         ref = next;
@@ -739,7 +781,8 @@ __global__ void __launch_bounds__(RG_NT, 2)
         const RowOut o = sm.out[s];
         const float* const entries = list + (lag ? s : 0) * DS_MAX;
         const float mine0 = entries[lane], mine1 = entries[32 + lane];
-        for (int32_t w = sh.w0; w < sh.w1; w += RG_CHUNK) {
+        uint32_t chunks = kept.chunks;
+        for (int32_t w = sh.w0; w < sh.w1; w += RG_CHUNK, chunks >>= 1) {
           const uint4* st = reinterpret_cast<const uint4*>(ring + (size_t)place0 * RG_BYTES) + at;
           T* const to = g + (int64_t)(w + at) * Tr::VEC;
           uint4 v[RG_W];
@@ -753,7 +796,10 @@ __global__ void __launch_bounds__(RG_NT, 2)
             for (int q = 0; q < RG_W; ++q) v[q] = make_uint4(0u, 0u, 0u, 0u);
           }
           __syncwarp();
-          if (lane == 0) bar_arrive(&empty[place0]);
+          if (lane == 0) {
+            if (chunks & 1u) fence_async();
+            bar_arrive(&empty[place0]);
+          }
           if (++place0 == places) place0 = 0;
           if (vec && w + RG_CHUNK <= sh.w1) {
 #pragma unroll
@@ -764,10 +810,12 @@ __global__ void __launch_bounds__(RG_NT, 2)
             for (int q = 0; q < RG_W; ++q)
               if (w + 32 * RG_NW * q + at < sh.w1) put_word(to + 32 * RG_NW * q * Tr::VEC, v[q], vec);
           }
-          __syncwarp();  // the warp's words are written: the list's entries over them
+          if (chunks & 1u) {
+            __syncwarp();  // the warp's words are written: the list's entries over them
 #pragma unroll
-          for (int h = 0; h < 3; ++h)
-            if (within(kept.e[h], w)) put(g + kept.e[h], h == 0 ? mine0 : h == 1 ? mine1 : o.gy);
+            for (int h = 0; h < 3; ++h)
+              if (within(kept.e[h], w)) put(g + kept.e[h], h == 0 ? mine0 : h == 1 ? mine1 : o.gy);
+          }
         }
         ++m;
         held = m == n ? ref : last;
@@ -878,9 +926,9 @@ __global__ void __launch_bounds__(32 * RW_MOST, 2)
       add_words<T>(k, S, x, a.c2, w == 0);
     }
     join(make_float2(k, S.x + S.y), 1.f, k, R);
-    add_rest_ends(d, sh, in, v, kind, k, R);
+    add_rest_ends(d, sh, wide<T>(in.edge), v, kind, k, R);
     const float wt = (float)(a.norm ? share / (double)in.count : share);
-    list_math(d, ref.x, in, pre, k, R, wt, true, HOLD ? &sm.out[warp] : nullptr, list, nullptr, stat, lane);
+    list_math<T>(d, ref.x, in, pre, k, R, wt, true, HOLD ? &sm.out[warp] : nullptr, list, nullptr, stat, lane);
     __syncwarp();
     if (HOLD) {
       const RowOut o = sm.out[warp];
@@ -892,7 +940,7 @@ __global__ void __launch_bounds__(32 * RW_MOST, 2)
         if (o.mode == ROW_FAST) x = grad_word<T, false>(o, a.c2, st[w - lane]);
         put_word(gw + (int64_t)w * Tr::VEC, x, vec);
       }
-      put_end(g, v, kind, o, list, a.c2, in.edge);
+      put_end(g, v, kind, o, list, a.c2, wide<T>(in.edge));
       __syncwarp();  // the row is written: the list's entries over it
       if (lane == 0 && label && !pre.labelled) put(g + in.y, o.gy);
 #pragma unroll

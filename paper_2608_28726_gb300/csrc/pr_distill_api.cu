@@ -77,13 +77,24 @@ pr_status setup(pr_ctx* c) {
 
 pr_status launch_ring(pr_ctx* c, prk::DistillArgs& d, pr_dtype dt, const RingShape& shape, bool hold,
                       cudaStream_t s) {
-  int places = shape.places - (d.a.own ? 1 : 0);  // (the rows' list takes one)
+  int places = shape.places, parts = 1, cluster = 1 << shape.split;
+  int64_t groups = shape.groups;
+  bool full = shape.full;
+  // rows one to a CTA, all their parts, once there are some for each: see distill_ring
+  if (!hold && cluster > 1 && d.a.n_rows >= 4 * c->num_sms) {
+    parts = cluster;
+    cluster = 1;
+    places = prk::RG_FEW - 1;
+    groups = std::min<int64_t>(d.a.n_rows, 2 * c->num_sms);
+    full = true;
+  }
+  if (d.a.own) --places;  // (the rows' list takes one)
   int lag = hold && shape.split == 0 && 2 * shape.here + 1 <= places ? 1 : 0;
-  void* args[] = {&d, &places, &lag};
+  void* args[] = {&d, &places, &lag, &parts};
   // (a grid that takes every place is not set up early: see launch_ring of the other losses)
-  const pr_status st = launch(ring_kernel(dt, hold, d.a.own), (unsigned)(shape.groups << shape.split),
-                              prk::RG_NT, ring_bytes(places, 1 << shape.split, lag, d.a.own),
-                              1u << shape.split, args, s, !shape.full);
+  const pr_status st = launch(ring_kernel(dt, hold, d.a.own), (unsigned)(groups * cluster),
+                              prk::RG_NT, ring_bytes(places, cluster * parts, lag, d.a.own),
+                              (unsigned)cluster, args, s, !full);
   return st == PR_OK ? timing_mark(c, s) : st;
 }
 
