@@ -210,6 +210,7 @@ pr_status pr_ctx_destroy(pr_ctx* c) {
   free_grown(c->loss_ws);
   free_grown(c->loss_zero);
   free_grown(c->norm_ws);
+  free_grown(c->distill_ws);
   for (cudaEvent_t e : c->tev)
     if (e) cudaEventDestroy(e);
   if (c->copy_stream) cudaStreamDestroy(c->copy_stream);

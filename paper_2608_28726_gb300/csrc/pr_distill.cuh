@@ -30,6 +30,9 @@ struct DistillArgs {
   int32_t reverse, none;            // direction; no class of the rest
   float kl_coef, ce_coef;
   float big;                        // logits from here on are infinite: 1e9 T
+  // workspace: the listed rows' entries and what their ends need beside them (distill_lists)
+  int4* entries;                    // [n_rows][k] {id, logit, p, log p}
+  float4* scalars;                  // [n_rows][2]
 };
 
 // a row's list and scalars: entries lane and 32 + lane, absent ones with id -1
@@ -86,16 +89,6 @@ __device__ __forceinline__ void fetch_logits(const DistillArgs& d, const Share& 
   if (v >= 0) in.edge = raw_at<T>(s.x, v);
 }
 
-__device__ __forceinline__ float warp_sum(float v) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(FULL, v, o);
-  return v;
-}
-__device__ __forceinline__ double warp_sum(double v) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(FULL, v, o);
-  return v;
-}
 // A value as the sum of two fp32 numbers, for 1 - sum p.  (In fp64 the exponentials of a list and their
 // sum are 3,400 cycles of the warp that takes the rows' ends: 1,500 rows of V = 262,144 fp32 without
 // a gradient and lists of 64 784 us for 588.)
@@ -143,7 +136,6 @@ __device__ __forceinline__ Pair exp_pair(float t) {
   p.lo = n < -100.f ? 0.f : scale * ((e1 + e2) + (e3 + (z_lo + q_lo)));
   return p;
 }
-__device__ __forceinline__ float warp_max(float v) { return unord(__reduce_max_sync(FULL, ord(v))); }
 
 // whether an id is listed twice.  Whole warp.
 __device__ __forceinline__ bool listed_twice(const ListIn& in, int lane) {
@@ -212,6 +204,39 @@ __device__ __forceinline__ void list_pre(const DistillArgs& d, const ListIn& in,
     o.rho = fmaxf((1.f - s.hi) - s.lo, DS_RHO);
     o.l_rho = logf(o.rho);
   }
+}
+
+// The same for the i-th listed row, and its weight wt, as distill_lists left them.
+__device__ __forceinline__ void fetch_prepared(const DistillArgs& d, int64_t i, const int4& ref,
+                                               ListIn& in, ListPre& o, float& wt, int lane) {
+  in.y = ref.z;
+  in.edge = 0u;
+  wt = 0.f;
+  in.xy = 0u;
+  o.sum = o.rho = o.l_rho = o.mass = 0.f;
+  o.bad = o.bad_id = o.labelled = false;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int j = 32 * h + lane;
+    int4 e = make_int4(-1, 0, 0, 0);
+    if (ref.y >= 0 && j < d.k) e = __ldcg(d.entries + i * d.k + j);
+    in.id[h] = e.x;
+    in.x[h] = (uint32_t)e.y;
+    o.p[h] = __int_as_float(e.z);
+    o.lt[h] = __int_as_float(e.w);
+  }
+  if (ref.y < 0) return;
+  const float4 q = __ldcg(d.scalars + 2 * i), r = __ldcg(d.scalars + 2 * i + 1);
+  o.sum = q.x;
+  o.rho = q.y;
+  o.l_rho = q.z;
+  o.mass = q.w;
+  wt = r.x;
+  in.xy = __float_as_uint(r.y);
+  const uint32_t f = __float_as_uint(r.z);
+  o.bad = f & 1u;
+  o.bad_id = f & 2u;
+  o.labelled = f & 4u;
 }
 
 // A row's end: its sum R against 2^k, the list's and label's logits left out.  Writes the
@@ -432,6 +457,43 @@ __device__ __forceinline__ void list_stats(const DistillArgs& d, const float2* s
   }
 }
 
+// ---- the lists of larger batches, ahead of the rows ---------------------------------------------
+//
+// What of a row's end does not wait for its sum, a row to a warp: the warp that takes the ends would
+// wait for the entries, then for the logits at them, and work out their probabilities, longer than
+// its row takes (64 answers of V = 151,936 bf16 with their gradient: DS_LISTS_FIGURE).
+constexpr int DP_NT = 256;
+template <typename T>
+__global__ void __launch_bounds__(DP_NT) distill_lists(const __grid_constant__ DistillArgs d) {
+  const LossArgs& a = d.a;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  pdl_wait();
+  pdl_trigger();
+  const Rows rows{nullptr, (int32_t)__ldcg(a.totals)};
+  const int64_t i = (int64_t)blockIdx.x * (DP_NT / 32) + warp;
+  if (i >= rows.live) return;
+  const int4 ref = rows.at(a, i);
+  ListIn in = fetch_list(d, rows, ref, lane);
+  fetch_logits<T>(d, share_of<T>(a, ref.x, 1, 0), ref, in, lane);
+  ListPre o;
+  list_pre(d, in, o, lane);
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int j = 32 * h + lane;
+    if (j < d.k)
+      d.entries[i * d.k + j] = make_int4(in.id[h], (int32_t)in.x[h], __float_as_int(o.p[h]),
+                                         __float_as_int(o.lt[h]));
+  }
+  if (lane == 0) {
+    const double share = rows.share(a);
+    const float wt = (float)(a.norm ? share / (double)in.count : share);
+    d.scalars[2 * i] = make_float4(o.sum, o.rho, o.l_rho, o.mass);
+    d.scalars[2 * i + 1] = make_float4(
+        wt, __uint_as_float(in.xy),
+        __uint_as_float((o.bad ? 1u : 0u) | (o.bad_id ? 2u : 0u) | (o.labelled ? 4u : 0u)), 0.f);
+  }
+}
+
 // The elements at a row's ends (this lane's at v, its value in.edge) into the sum, but the
 // listed ones and the label.  `at`: what v is, an entry's place, DS_LABEL, or DS_REST.
 constexpr int DS_REST = -1, DS_LABEL = -2;
@@ -554,6 +616,7 @@ __host__ __device__ constexpr size_t distill_start(int C, int places, int lag) {
 static_assert(distill_start(4, RG_FEW, 0) <= 1024 && distill_start(1, RG_FEW, 1) <= 1024,
               "two CTAs on an SM");
 
+// PREPARED: distill_lists ran ahead (with a gradient, which has the ends on the way of the rows).
 template <typename T, bool HOLD, bool OWN>
 __global__ void __launch_bounds__(RG_NT, 2)
     distill_ring(const __grid_constant__ DistillArgs d, const int places, const int lag,
@@ -562,13 +625,14 @@ __global__ void __launch_bounds__(RG_NT, 2)
   DistillCtl& sm = *reinterpret_cast<DistillCtl*>(smem_raw);
   const LossArgs& a = d.a;
   using Tr = Traits<T>;
+  constexpr bool PREPARED = HOLD && !OWN;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   uint32_t C, rank;
   asm("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(C));
   asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
   const int64_t G = gridDim.x / C, first = blockIdx.x / C;
   const uint32_t P = HOLD ? C : C * parts;  // parts of a row; this CTA has rank, or all of them
-  const uint32_t p_first = HOLD || parts == 1 ? rank : 0, p_last = HOLD || parts == 1 ? rank + 1 : P;
+  const uint32_t p_first = HOLD || parts == 1 ? rank : 0, p_last = HOLD ? p_first + 1 : parts == 1 ? rank + 1 : P;
   uint64_t* const full = reinterpret_cast<uint64_t*>(smem_raw + DS_BARS);
   uint64_t* const empty = full + places;
   float2* const sums = reinterpret_cast<float2*>(smem_raw + distill_sums(places));
@@ -644,17 +708,33 @@ __global__ void __launch_bounds__(RG_NT, 2)
       wait(&full[(int)(i % places)], (uint32_t)(i / places) & 1u);
   } else if (warp == RG_NW + 1) {
     // ---- the rows' ends
-    const double share = rows.share(a);
+    const double share = !PREPARED ? rows.share(a) : 0.0;
     uint32_t n = 0;
     int4 ref = ref_of(first), ref1 = ref_of(first + G), ref2 = ref_of(first + 2 * G);
-    ListIn in = fetch_list(d, rows, ref, lane), next = fetch_list(d, rows, ref1, lane);
-    fetch_logits<T>(d, share_of<T>(a, ref.x, C, rank), ref, in, lane);
+    ListIn in, next;
+    ListPre pre, pre1;
+    float wt, wt1;
+    auto edge = [&](const int4& r, ListIn& q) {  // the element at the row's ends of this lane
+      const Share sh = share_of<T>(a, r.x, C, rank);
+      const int32_t v = r.y >= 0 ? end_of(a, sh, lane) : -1;
+      if (v >= 0) q.edge = raw_at<T>(sh.x, v);
+    };
+    if constexpr (!PREPARED) {
+      in = fetch_list(d, rows, ref, lane);
+      next = fetch_list(d, rows, ref1, lane);
+      fetch_logits<T>(d, share_of<T>(a, ref.x, C, rank), ref, in, lane);
+    } else {
+      fetch_prepared(d, first, ref, in, pre, wt, lane);
+      edge(ref, in);
+    }
     // What a peer's gradient may be written over (the logits' own buffer) has been read when
     // this CTA's sums are sent: the next row's logits are there before a result is given.
     auto landed = [&](ListIn& q) {
-      q.x[0] = __shfl_sync(FULL, q.x[0], lane);
-      q.x[1] = __shfl_sync(FULL, q.x[1], lane);
-      q.xy = __shfl_sync(FULL, q.xy, lane);
+      if (!PREPARED) {
+        q.x[0] = __shfl_sync(FULL, q.x[0], lane);
+        q.x[1] = __shfl_sync(FULL, q.x[1], lane);
+        q.xy = __shfl_sync(FULL, q.xy, lane);
+      }
       q.edge = __shfl_sync(FULL, q.edge, lane);
     };
     landed(in);
@@ -662,16 +742,23 @@ __global__ void __launch_bounds__(RG_NT, 2)
     for (int64_t i = first; i < live; i += G) {
       const int64_t row = ref.x;
       const Share sh = share_of<T>(a, row, C, rank);
-      fetch_logits<T>(d, share_of<T>(a, ref1.x, C, rank), ref1, next, lane);
-      const ListIn after = fetch_list(d, rows, ref2, lane);
+      ListIn after;
+      if constexpr (!PREPARED) {
+        fetch_logits<T>(d, share_of<T>(a, ref1.x, C, rank), ref1, next, lane);
+        after = fetch_list(d, rows, ref2, lane);
+      } else {
+        fetch_prepared(d, i + G, ref1, next, pre1, wt1, lane);
+        edge(ref1, next);
+      }
       ref = ref1;
       ref1 = ref2;
       ref2 = ref_of(i + 3 * G);
       const int32_t v = end_of(a, sh, lane);
       const int kind = sh.head + sh.tail ? end_kind(d, sh, in, v, lane) : DS_REST;
-      ListPre pre;
-      list_pre(d, in, pre, lane);
-      const float wt = (float)(a.norm ? share / (double)in.count : share);
+      if constexpr (!PREPARED) {
+        list_pre(d, in, pre, lane);
+        wt = (float)(a.norm ? share / (double)in.count : share);
+      }
       T* const g = reinterpret_cast<T*>(a.grad) + row * a.grad_stride;
       const int s = n % RG_SLOTS;
       const uint32_t phase = (n / RG_SLOTS) & 1u;
@@ -699,7 +786,12 @@ __global__ void __launch_bounds__(RG_NT, 2)
       __syncwarp();
       if (HOLD && rank == 0) put_end(g, v, kind, sm.out[s], entries, a.c2, wide<T>(in.edge));
       in = next;
-      next = after;
+      if constexpr (!PREPARED) {
+        next = after;
+      } else {
+        pre = pre1;
+        wt = wt1;
+      }
     }
   } else {
     // ---- the rows' words

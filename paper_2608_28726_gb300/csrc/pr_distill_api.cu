@@ -75,6 +75,16 @@ pr_status setup(pr_ctx* c) {
   return PR_OK;
 }
 
+pr_status launch_lists(pr_ctx* c, prk::DistillArgs& d, pr_dtype dt, cudaStream_t s) {
+  void* args[] = {&d};
+  const pr_status st = launch(dt == PR_DTYPE_BF16
+                                  ? reinterpret_cast<const void*>(&prk::distill_lists<__nv_bfloat16>)
+                                  : reinterpret_cast<const void*>(&prk::distill_lists<float>),
+                              (unsigned)((d.a.n_rows + prk::DP_NT / 32 - 1) / (prk::DP_NT / 32)),
+                              prk::DP_NT, 0, 1, args, s);
+  return st == PR_OK ? timing_mark(c, s) : st;
+}
+
 pr_status launch_ring(pr_ctx* c, prk::DistillArgs& d, pr_dtype dt, const RingShape& shape, bool hold,
                       cudaStream_t s) {
   int places = shape.places, parts = 1, cluster = 1 << shape.split;
@@ -168,10 +178,18 @@ pr_status pr_distill_loss(pr_ctx* c, const void* logits, pr_dtype dt, int64_t n_
   if ((st = workspace(c, d.a, std::max(ring.groups, forward_grid(c)), false, false)) != PR_OK)
     return st;
   d.a.own = own_list(d.a);
+  const bool prepared = grad && !d.a.own && rows_warps(c, d.a, dt) == 0;
+  if (prepared) {
+    const size_t scalars = (size_t)n_rows * 32;
+    if ((st = grow(c->distill_ws, scalars + (size_t)n_rows * k * 16, false)) != PR_OK) return st;
+    d.scalars = static_cast<float4*>(c->distill_ws.p);
+    d.entries = reinterpret_cast<int4*>(static_cast<char*>(c->distill_ws.p) + scalars);
+  }
   if ((st = timing_begin(c, s)) != PR_OK) return st;
   if ((st = launch_plan(c, d.a, 0, s)) != PR_OK) return st;
   if (const int warps = rows_warps(c, d.a, dt))
     return launch_rows(c, d, dt, warps, grad != nullptr, s);
+  if (prepared && (st = launch_lists(c, d, dt, s)) != PR_OK) return st;
   return launch_ring(c, d, dt, ring, grad != nullptr, s);
 }
 

@@ -556,6 +556,20 @@ __device__ __forceinline__ void bar_expect(uint64_t* b, uint32_t bytes) {
                : "memory");
 }
 
+// ---- sums and maxima over a warp -------------------------------------------------------------
+
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(FULL, v, o);
+  return v;
+}
+__device__ __forceinline__ double warp_sum(double v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(FULL, v, o);
+  return v;
+}
+__device__ __forceinline__ float warp_max(float v) { return unord(__reduce_max_sync(FULL, ord(v))); }
+
 // ---- a row among CTAs -------------------------------------------------------------------
 
 // a CTA's part of a row

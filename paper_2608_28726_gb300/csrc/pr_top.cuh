@@ -12,7 +12,7 @@
 // within the exponent's range: hence the bound of 1e9 T on what counts as finite.
 #pragma once
 
-#include "pr_kernels.cuh"
+#include "pr_loss.cuh"
 
 namespace prk {
 
@@ -88,13 +88,17 @@ struct TopList {
 // a value as a key has it: -0 is 0
 __device__ __forceinline__ uint64_t top_key(float v, uint32_t index) { return make_key(v + 0.f, index); }
 
+__device__ __forceinline__ float top_max(float m) { return m; }
+__device__ __forceinline__ float top_max(uint16_t m) { return __uint_as_float((uint32_t)m << 16); }
+
 // The first k of n groups by their maxima at gm (shared memory): ranks lane and 32 + lane in hi and lo.
-__device__ __forceinline__ void top_groups(TopList& l, const float* gm, int n, float big, int lane) {
+template <typename M>
+__device__ __forceinline__ void top_groups(TopList& l, const M* gm, int n, float big, int lane) {
   // a bound that k groups reach: of 64 sets of groups the k-th largest maximum
   float m0 = -INFINITY, m1 = -INFINITY;
   for (int g = lane; g < n; g += 64) {
-    m0 = fmaxf(m0, gm[g]);
-    if (g + 32 < n) m1 = fmaxf(m1, gm[g + 32]);
+    m0 = fmaxf(m0, top_max(gm[g]));
+    if (g + 32 < n) m1 = fmaxf(m1, top_max(gm[g + 32]));
   }
   TopList s(l.buf, l.k);
   s.take(top_key(m0, lane), lane);
@@ -102,13 +106,13 @@ __device__ __forceinline__ void top_groups(TopList& l, const float* gm, int n, f
   const float bound = fmaxf(key_val(s.least), -big);
   for (int g0 = 0; g0 < n; g0 += 32) {
     const int g = g0 + lane;
-    const float m = g < n ? gm[g] : -INFINITY;
+    const float m = g < n ? top_max(gm[g]) : -INFINITY;
     l.push(m >= bound && m > -big, top_key(m, (uint32_t)g), lane);
   }
   l.finish(lane);
 }
 
-// ---- one row to a CTA -----------------------------------------------------------------
+// ---- any row: one to a CTA, in up to 8,192 groups, whatever their length --------------------
 
 struct TopSmem {
   float gm[TP_GROUPS];
@@ -183,6 +187,330 @@ __global__ void __launch_bounds__(TP_NT) top_rows(const TopArgs a, const int64_t
       logp[j] = q ? fmaf(key_val(q), a.c2, -K) * LN2 - lS : -INFINITY;
     }
   }
+}
+
+// ---- rows through a ring of shared memory ------------------------------------------------------
+//
+// A row to a CTA, or its parts to the CTAs of a cluster; a warp brings 16 KB chunks in by bulk copies, eight
+// sum them and keep the groups' maxima: a group is what a thread takes of a chunk, GW
+// 16-byte words side by side.  Then the eight choose together, by counting instead of
+// sorting: of the threads' own maxima the k-th largest is a bound that k groups reach; the
+// groups that reach it (some 75 for k = 64 in a row of random values) are read again, which the chunks of the
+// next row do not wait for, and each of their elements that reaches it finds its place
+// by counting the ones before it.  Where more groups or elements reach the bound than there is
+// room for (rows of few values), a warp finds the first k groups and elements
+// in TopLists.
+constexpr int TR_NW = 8;
+constexpr int TR_NT = 32 * (TR_NW + 1);
+constexpr int TR_W = 4;                       // words of a thread and chunk
+constexpr int TR_CHUNK = 32 * TR_NW * TR_W;   // words
+constexpr int TR_BYTES = 16 * TR_CHUNK;
+constexpr int TR_MOST = 12;                   // places of the ring
+constexpr int TR_GROUPS = 256, TR_KEYS = 512; // that reach the bound
+constexpr int BAR_TOP = 1;                    // the eight warps
+static_assert(TR_CHUNK == SH_CHUNK, "parts of a row are multiples of chunks");
+
+struct TopRing {
+  uint64_t full[TR_MOST], empty[TR_MOST];
+  float2 part[TR_NW];            // the warps' sums
+  float max[32 * TR_NW];         // the threads' largest elements
+  float bound;
+  int groups[2], keys[2];        // how many reach it; of rows of either parity
+  uint32_t group[TR_GROUPS];
+  uint64_t key[TR_KEYS];
+  uint64_t top[TP_MAX];          // the first ones of this CTA's part, in order; 0: none
+  // cluster rank 0: the CTAs' sums and lists
+  float2 sums[MAXC];
+  uint64_t lists[MAXC][TP_MAX];
+};
+constexpr size_t TR_START = (sizeof(TopRing) + 127) / 128 * 128;  // then the groups' maxima, then the ring
+
+template <typename T>
+struct TopMax;
+template <>
+struct TopMax<float> {
+  using type = float;
+  static __device__ __forceinline__ float of(float m) { return m; }
+};
+template <>
+struct TopMax<__nv_bfloat16> {
+  using type = uint16_t;
+  static __device__ __forceinline__ uint16_t of(float m) { return (uint16_t)(__float_as_uint(m) >> 16); }
+};
+
+// GW 4: rows of many words; GW 1: where a bound needs more groups than those have
+template <typename T, int GW>
+__global__ void __launch_bounds__(TR_NT, 2)
+    top_ring(const __grid_constant__ LossArgs a, const int k, const float big, int32_t* const out_ids,
+             const int places, const int gm_bytes) {
+  extern __shared__ __align__(16) unsigned char smem_raw[];
+  TopRing& sm = *reinterpret_cast<TopRing*>(smem_raw);
+  using Tr = Traits<T>;
+  using M = typename TopMax<T>::type;
+  M* const gm = reinterpret_cast<M*>(smem_raw + TR_START);
+  unsigned char* const ring = smem_raw + TR_START + gm_bytes;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  uint32_t C, rank;
+  asm("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(C));
+  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+  const int64_t G = gridDim.x / C, first = blockIdx.x / C;
+  if (tid == 0) {
+    for (int i = 0; i < places; ++i) {
+      bar_init(&sm.full[i], 1);
+      bar_init(&sm.empty[i], TR_NW);
+    }
+    sm.groups[0] = sm.groups[1] = sm.keys[0] = sm.keys[1] = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  __syncthreads();
+  if (C > 1) cluster_sync_all();
+  pdl_wait();
+  pdl_trigger();
+
+  bool ok = true;  // no wait has run out
+  auto wait = [&](uint64_t* b, uint32_t phase) {
+    if (ok) ok = ring_wait(sm_addr(b), phase, a.ctx_flags);
+    __syncwarp();
+  };
+  int place = 0;
+  uint32_t turn = 0u;
+  auto step = [&]() {
+    if (++place == places) {
+      place = 0;
+      turn ^= 1u;
+    }
+  };
+  uint32_t parity = 0u;
+  int64_t n = 0;  // chunks brought in
+  for (int64_t row = first; row < a.n_rows; row += G, parity ^= 1u) {
+    const Share sh = share_of<T>(a, row, C, rank);
+    if (warp == TR_NW) {
+      const char* src = sh.x + sizeof(T) * sh.head + 16 * (int64_t)sh.w0;
+      for (int32_t left = sh.w1 - sh.w0; left > 0; left -= TR_CHUNK) {
+        if (n >= places) wait(&sm.empty[place], turn ^ 1u);
+        if (ok && lane == 0) {
+          const uint32_t bytes = 16u * (uint32_t)min(TR_CHUNK, left);
+          bar_expect(&sm.full[place], bytes);
+          asm volatile(
+              "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::
+                  "r"(sm_addr(ring + (size_t)place * TR_BYTES)),
+              "l"(src), "r"(bytes), "r"(sm_addr(&sm.full[place]))
+              : "memory");
+        }
+        src += TR_BYTES;
+        if (ok) ++n;
+        step();
+      }
+      if (C > 1) {
+        cluster_sync_all();
+        cluster_sync_all();
+      }
+      continue;
+    }
+    // ---- the row's sum and its groups' maxima
+    float ref = -3e38f, top = -INFINITY;
+    float2 S = make_float2(0.f, 0.f);
+    const int32_t groups = (sh.w1 - sh.w0 + GW - 1) / GW;
+    for (int32_t w = sh.w0; w < sh.w1; w += TR_CHUNK) {
+      wait(&sm.full[place], turn);
+      const uint4* st = reinterpret_cast<const uint4*>(ring + (size_t)place * TR_BYTES);
+      uint4 v[TR_W];
+      int32_t at[TR_W];
+#pragma unroll
+      for (int q = 0; q < TR_W; ++q) {
+        // (GW 4: neighbouring lanes begin with different words, so that no two meet in a bank)
+        at[q] = GW == 4 ? 4 * tid + ((q + (lane >> 1)) & 3) : 32 * TR_NW * q + tid;
+        v[q] = st[at[q]];
+      }
+      if (w + TR_CHUNK > sh.w1) {
+#pragma unroll
+        for (int q = 0; q < TR_W; ++q)
+          if (w + at[q] >= sh.w1) v[q] = make_uint4(Tr::NEG_WORD, Tr::NEG_WORD, Tr::NEG_WORD, Tr::NEG_WORD);
+      }
+      __syncwarp();
+      if (lane == 0) bar_arrive(&sm.empty[place]);
+      step();
+      const int32_t g = (w - sh.w0) / GW + tid;
+      if constexpr (GW == 4) {
+        const float m = Tr::tile_max(v);
+        if (g < groups) gm[g] = TopMax<T>::of(m);
+        top = fmaxf(top, m);
+      } else {
+#pragma unroll
+        for (int q = 0; q < TR_W; ++q) {
+          const float m = Tr::gmax(v[q]);
+          if (g + 32 * TR_NW * q < groups) gm[g + 32 * TR_NW * q] = TopMax<T>::of(m);
+          top = fmaxf(top, m);
+        }
+      }
+      add_words<T>(ref, S, v, a.c2, w == sh.w0);
+    }
+    float R;
+    join(make_float2(ref, S.x + S.y), 1.f, ref, R);
+    // the elements before and after the words: the first CTA's
+    int32_t v_end = -1;
+    float x_end = -INFINITY;
+    if (warp == 0) {
+      v_end = rank == 0 ? end_of(a, sh, lane) : -1;
+      if (v_end >= 0) x_end = Tr::elem(sh.x, v_end);
+      const float t = fmaxf(warp_max(x_end * a.c2), -3e38f);
+      if (t > ref) {
+        R *= rescale2(ref - t);
+        ref = t;
+      }
+      R += warp_sum(v_end >= 0 ? ex2(fmaf(x_end, a.c2, -ref)) : 0.f);
+      top = fmaxf(top, x_end);
+      if (lane == 0) sm.groups[parity ^ 1u] = sm.keys[parity ^ 1u] = 0;
+    }
+    if (lane == 0) sm.part[warp] = make_float2(ref, R);
+    sm.max[tid] = top;
+    named_bar_sync(BAR_TOP, 32 * TR_NW);
+    // ---- the bound: the k-th largest of the threads' maxima
+    join(lane < TR_NW ? sm.part[lane] : make_float2(-3e38f, 0.f), 1.f, ref, R);
+    {
+      const float4* q = reinterpret_cast<const float4*>(sm.max);
+      int before = 0;
+#pragma unroll 8
+      for (int i = 0; i < 8 * TR_NW; ++i) {
+        const float4 f = q[i];
+        before += (f.x > top || (f.x == top && 4 * i < tid)) + (f.y > top || (f.y == top && 4 * i + 1 < tid)) +
+                  (f.z > top || (f.z == top && 4 * i + 2 < tid)) +
+                  (f.w > top || (f.w == top && 4 * i + 3 < tid));
+      }
+      if (before == k - 1) sm.bound = top;
+    }
+    named_bar_sync(BAR_TOP, 32 * TR_NW);
+    const float bound = sm.bound;
+    auto reaches = [&](float x) { return x >= bound && x > -big; };
+    if (reaches(top)) {
+      for (int32_t g = tid; g < groups; g += 32 * TR_NW)
+        if (reaches(top_max(gm[g]))) {
+          const int i = atomicAdd(&sm.groups[parity], 1);
+          if (i < TR_GROUPS) sm.group[i] = (uint32_t)g;
+        }
+    }
+    named_bar_sync(BAR_TOP, 32 * TR_NW);
+    // ---- the elements that reach it
+    const int found = sm.groups[parity];
+    auto take = [&](float x, int32_t v) {
+      if (reaches(x)) {
+        const int i = atomicAdd(&sm.keys[parity], 1);
+        if (i < TR_KEYS) sm.key[i] = top_key(x, (uint32_t)v);
+      }
+    };
+    const char* const words = sh.x + sizeof(T) * sh.head;
+    if (found <= TR_GROUPS)
+      for (int i = tid; i < found * GW; i += 32 * TR_NW) {
+        const int32_t w = sh.w0 + (int32_t)sm.group[i / GW] * GW + i % GW;
+        if (w < sh.w1) {
+          const uint4 q = ld_reread(words + 16 * (int64_t)w);
+          if (reaches(Tr::gmax(q))) {
+#pragma unroll
+            for (int j = 0; j < Tr::VEC; ++j) take(Tr::at(q, j), sh.head + w * Tr::VEC + j);
+          }
+        }
+      }
+    if (v_end >= 0) take(x_end, v_end);
+    named_bar_sync(BAR_TOP, 32 * TR_NW);
+    // ---- their order
+    const int count = sm.keys[parity];
+    if (found <= TR_GROUPS && count <= TR_KEYS) {
+      for (int i = tid; i < count; i += 32 * TR_NW) {
+        const uint64_t mine = sm.key[i];
+        int before = 0;
+#pragma unroll 4
+        for (int j = 0; j < count; ++j) before += sm.key[j] > mine;
+        if (before < k) sm.top[before] = mine;
+      }
+      if (tid >= count && tid < k) sm.top[tid] = 0ull;
+    } else if (warp == 0) {
+      TopList l(sm.key, k);
+      top_groups(l, gm, groups, big, lane);
+      TopList e(sm.key, k);
+      for (int j = 0; j < k; ++j) {
+        const uint64_t q = shfl64(j < 32 ? l.hi : l.lo, j & 31);
+        if (q == 0) break;
+        const int32_t w = sh.w0 + (int32_t)key_idx(q) * GW, el = (w - sh.w0) * Tr::VEC + lane;
+        const bool in = lane < GW * Tr::VEC && el < (sh.w1 - sh.w0) * Tr::VEC;
+        const int32_t v = sh.head + sh.w0 * Tr::VEC + el;
+        const float x = in ? Tr::elem(sh.x, v) : -INFINITY;
+        e.push(x > -big, top_key(x, (uint32_t)v), lane);
+      }
+      e.push(v_end >= 0 && x_end > -big, top_key(x_end, (uint32_t)v_end), lane);
+      e.finish(lane);
+      if (lane < k) sm.top[lane] = e.hi;
+      if (32 + lane < k) sm.top[32 + lane] = e.lo;
+    }
+    named_bar_sync(BAR_TOP, 32 * TR_NW);
+    // ---- the list
+    uint64_t mine = tid < k ? sm.top[tid] : 0ull;
+    float2 all = make_float2(ref, R);
+    if (C > 1) {
+      if (tid < k) dsmem_st_u64(dsmem_addr(&sm.lists[rank][tid], 0), mine);
+      if (tid == 0)
+        dsmem_st_u64(dsmem_addr(&sm.sums[rank], 0),
+                     (uint64_t)__float_as_uint(ref) | (uint64_t)__float_as_uint(R) << 32);
+      __syncwarp();
+      cluster_sync_all();
+    }
+    if (rank == 0) {
+      if (C > 1) join(lane < (int)C ? sm.sums[lane] : make_float2(-3e38f, 0.f), 1.f, all.x, all.y);
+      // against the row's largest element
+      uint64_t best = 0ull;
+      for (uint32_t c = 0; c < C; ++c) best = max(best, C > 1 ? sm.lists[c][0] : sm.top[0]);
+      const float K = best ? key_val(best) * a.c2 : -INFINITY;
+      const float rows_sum = all.y * rescale2(all.x - K);
+      const bool bad = !(all.x < big * a.c2) || !(all.y < INFINITY) || !(all.y >= 0.f) || !best;
+      const float log_sum = logf(rows_sum);
+      auto give = [&](int j, uint64_t q) {
+        out_ids[row * k + j] = bad || q == 0 ? -1 : (int32_t)key_idx(q);
+        a.logp[row * k + j] = bad ? NAN : q ? fmaf(key_val(q), a.c2, -K) * LN2 - log_sum : -INFINITY;
+      };
+      if (C == 1) {
+        if (tid < k) give(tid, mine);
+      } else {
+        // an element's place is the number of those before it in each list, found by bisection
+        int valid = 0;
+        for (uint32_t c = 0; c < C; ++c) {
+          int lo = 0, hi = k;
+          while (lo < hi) {
+            const int mid = (lo + hi) >> 1;
+            if (sm.lists[c][mid] > 0ull) lo = mid + 1;
+            else hi = mid;
+          }
+          valid += lo;
+        }
+        for (int i = tid; i < (int)C * k; i += 32 * TR_NW) {
+          const uint64_t q = sm.lists[i / k][i % k];
+          if (q == 0ull) continue;
+          int before = 0;
+          for (uint32_t c = 0; c < C; ++c) {
+            int lo = 0, hi = k;
+            while (lo < hi) {
+              const int mid = (lo + hi) >> 1;
+              if (sm.lists[c][mid] > q) lo = mid + 1;
+              else hi = mid;
+            }
+            before += lo;
+          }
+          if (before < k) give(before, q);
+        }
+        if (tid < k && tid >= valid) give(tid, 0ull);
+      }
+      if (bad && tid == 0) atomicOr(a.ctx_flags, FLAG_NONFINITE);
+    }
+    __syncwarp();
+    if (C > 1) cluster_sync_all();
+  }
+  if (warp == TR_NW) {
+    // no copy may be in flight when the CTA ends (as none is unless a wait ran out)
+    ok = true;
+    for (int64_t i = n < places ? 0 : n - places; i < n; ++i)
+      wait(&sm.full[(int)(i % places)], (uint32_t)(i / places) & 1u);
+  }
+  __syncthreads();
+  if (C > 1) cluster_sync_all();
 }
 
 }  // namespace prk

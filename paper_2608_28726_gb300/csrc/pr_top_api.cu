@@ -4,12 +4,62 @@
 #include <algorithm>
 #include <cmath>
 
-#include "pr_ctx.h"
+#include "pr_loss_host.h"
 #include "pr_top.cuh"
 
 using namespace prh;
 
 static_assert(PR_MAX_LISTED == prk::TP_MAX, "list length");
+
+namespace {
+
+template <typename T>
+const void* ring_kernel(bool words) {
+  return words ? reinterpret_cast<const void*>(&prk::top_ring<T, 1>)
+               : reinterpret_cast<const void*>(&prk::top_ring<T, 4>);
+}
+const void* ring_kernel(pr_dtype dt, bool words) {
+  return dt == PR_DTYPE_BF16 ? ring_kernel<__nv_bfloat16>(words) : ring_kernel<float>(words);
+}
+
+constexpr size_t SM_BYTES = 227 * 1024;         // a CTA alone on an SM
+constexpr size_t HALF_BYTES = 113 * 1024;       // one of two
+
+// The ring's launch: CTAs per row, words of a group, bytes of the groups' maxima, places.
+struct TopShape {
+  int cluster, places;
+  bool words, fits;
+  size_t gm, smem;
+};
+
+TopShape choose(const pr_ctx* c, pr_dtype dt, int64_t n_rows, int64_t vocab) {
+  const int64_t words = vocab * (int64_t)esize(dt) / 16 + 1;
+  TopShape s;
+  s.cluster = 1;
+  s.fits = false;
+  // as many CTAs per row as the SMs have room for, while each has a chunk
+  while (s.cluster < 8 && n_rows * s.cluster * 2 <= 2 * c->num_sms &&
+         words > (int64_t)s.cluster * prk::TR_CHUNK)
+    s.cluster *= 2;
+  for (; s.cluster <= 8; s.cluster *= 2) {
+    const int64_t chunks = (words + prk::TR_CHUNK - 1) / prk::TR_CHUNK;
+    const int64_t part = std::min(words, (chunks + s.cluster - 1) / s.cluster * prk::TR_CHUNK);
+    s.words = part <= 4096;  // (a bound from fewer than 1,024 groups lets too much through)
+    const int64_t groups = s.words ? part : (part + 3) / 4;
+    s.gm = ((size_t)groups * (dt == PR_DTYPE_BF16 ? 2 : 4) + 127) / 128 * 128;
+    const size_t fixed = prk::TR_START + s.gm;
+    if (fixed + 2 * prk::TR_BYTES > SM_BYTES) continue;
+    s.places = fixed + 3 * prk::TR_BYTES <= HALF_BYTES ? (int)((HALF_BYTES - fixed) / prk::TR_BYTES)
+                                                       : (int)((SM_BYTES - fixed) / prk::TR_BYTES);
+    s.places = std::min(s.places, (int)prk::TR_MOST);
+    s.smem = fixed + (size_t)s.places * prk::TR_BYTES;
+    s.fits = true;
+    return s;
+  }
+  return s;
+}
+
+}  // namespace
 
 extern "C" {
 
@@ -28,6 +78,30 @@ pr_status pr_top_logits(pr_ctx* c, const void* logits, pr_dtype dt, int64_t n_ro
   if (st != PR_OK) return st;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   if ((st = timing_begin(c, s)) != PR_OK || n_rows == 0) return st;
+  const float big = (float)(1e9 * (double)temperature);
+  const TopShape shape = choose(c, dt, n_rows, vocab);
+  if (shape.fits) {
+    if (!c->top_ready) {
+      for (pr_dtype t : {PR_DTYPE_F32, PR_DTYPE_BF16})
+        for (bool words : {false, true})
+          PR_CUDA(cudaFuncSetAttribute(ring_kernel(t, words), cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                       (int)SM_BYTES));
+      c->top_ready = true;
+    }
+    prk::LossArgs l;
+    fill(l, c, logits, n_rows, vocab, row_stride, nullptr, nullptr, nullptr, 0, nullptr, temperature, 1.f,
+         nullptr, logp, nullptr, 0);
+    int kk = k, places = shape.places, gm = (int)shape.gm;
+    float limit = big;
+    int32_t* out = ids;
+    const int64_t at_once = shape.smem <= HALF_BYTES ? 2 * c->num_sms : c->num_sms;
+    const int64_t groups = std::min<int64_t>(n_rows, shape.cluster > 1 ? n_rows : at_once);
+    void* args[] = {&l, &kk, &limit, &out, &places, &gm};
+    st = launch(ring_kernel(dt, shape.words),
+                (unsigned)(std::min<int64_t>(groups, 0x7fffffffLL / shape.cluster) * shape.cluster),
+                prk::TR_NT, shape.smem, (unsigned)shape.cluster, args, s, shape.cluster > 1 || n_rows < at_once);
+    return st == PR_OK ? timing_mark(c, s) : st;
+  }
   prk::TopArgs a;
   a.logits = logits;
   a.n_rows = n_rows;
@@ -35,18 +109,16 @@ pr_status pr_top_logits(pr_ctx* c, const void* logits, pr_dtype dt, int64_t n_ro
   a.row_stride = row_stride;
   a.k = k;
   a.c2 = (float)(1.4426950408889634 / (double)temperature);
-  a.big = (float)(1e9 * (double)temperature);
+  a.big = big;
   a.ids = ids;
   a.logp = logp;
   a.ctx_flags = c->flags;
-  const int64_t group = std::max<int64_t>(32, (vocab + prk::TP_GROUPS - 1) / prk::TP_GROUPS);
-  if (dt == PR_DTYPE_BF16)
-    prk::top_rows<__nv_bfloat16><<<(unsigned)n_rows, prk::TP_NT, 0, s>>>(a, group);
-  else
-    prk::top_rows<float><<<(unsigned)n_rows, prk::TP_NT, 0, s>>>(a, group);
-  PR_CUDA(cudaGetLastError());
-  g_launches.fetch_add(1, std::memory_order_relaxed);
-  return timing_mark(c, s);
+  int64_t group = std::max<int64_t>(32, (vocab + prk::TP_GROUPS - 1) / prk::TP_GROUPS);
+  void* args[] = {&a, &group};
+  st = launch(dt == PR_DTYPE_BF16 ? reinterpret_cast<const void*>(&prk::top_rows<__nv_bfloat16>)
+                                  : reinterpret_cast<const void*>(&prk::top_rows<float>),
+              (unsigned)n_rows, prk::TP_NT, 0, 1, args, s);
+  return st == PR_OK ? timing_mark(c, s) : st;
 }
 
 }  // extern "C"

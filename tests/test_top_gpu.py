@@ -102,6 +102,14 @@ def test_values_that_a_row_can_hold(B, ctx, n, V, dtype):
         assert (ids[[1, 2, 4, 5, 11]] == -1).all() and logp[[1, 2, 4, 5, 11]].isnan().all()
 
 
+@pytest.mark.parametrize("dtype,V", [("f32", 6_500_001), ("bf16", 26_000_003)])
+def test_vocabularies_beyond_a_cluster(B, ctx, dtype, V):
+    x = torch.empty(2, V, device="cuda").normal_(generator=torch.Generator("cuda").manual_seed(3))
+    x = x.to(TYPES[dtype])
+    x[1] = 2.0
+    check(*B.pr_top_logits(ctx, x, 40), x, 40)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("V,stride,start", [(1000, 1003, 1), (5001, 5001, 3), (777, 1024, 0),
                                             (32000, 32001, 5), (32000, 32008, 8), (9, 11, 2)])
