@@ -206,23 +206,25 @@ constexpr int TR_W = 4;                       // words of a thread and chunk
 constexpr int TR_CHUNK = 32 * TR_NW * TR_W;   // words
 constexpr int TR_BYTES = 16 * TR_CHUNK;
 constexpr int TR_MOST = 12;                   // places of the ring
-constexpr int TR_GROUPS = 256, TR_KEYS = 512; // that reach the bound
+constexpr int TR_GROUPS = 64, TR_KEYS = 512;  // that reach the bound: groups of a warp, elements
 constexpr int BAR_TOP = 1;                    // the eight warps
 static_assert(TR_CHUNK == SH_CHUNK, "parts of a row are multiples of chunks");
 
 struct TopRing {
   uint64_t full[TR_MOST], empty[TR_MOST];
   float2 part[TR_NW];            // the warps' sums
-  float max[32 * TR_NW];         // the threads' largest elements
+  uint32_t max[32 * TR_NW];      // the threads' largest elements as ord() has them, each warp's in order
   float bound;
-  int groups[2], keys[2];        // how many reach it; of rows of either parity
-  uint32_t group[TR_GROUPS];
+  int keys[2];                   // how many elements reach it; of rows of either parity
+  int crowded[2];                // there is no room for what reaches it
+  uint16_t group[TR_NW][TR_GROUPS];
   uint64_t key[TR_KEYS];
   uint64_t top[TP_MAX];          // the first ones of this CTA's part, in order; 0: none
   // cluster rank 0: the CTAs' sums and lists
   float2 sums[MAXC];
   uint64_t lists[MAXC][TP_MAX];
 };
+static_assert(32 * TR_NW == 256 && TP_MAX == 64, "bisections and places below");
 constexpr size_t TR_START = (sizeof(TopRing) + 127) / 128 * 128;  // then the groups' maxima, then the ring
 
 template <typename T>
@@ -240,7 +242,7 @@ struct TopMax<__nv_bfloat16> {
 
 // GW 4: rows of many words; GW 1: where a bound needs more groups than those have
 template <typename T, int GW>
-__global__ void __launch_bounds__(TR_NT, 2)
+__global__ void __launch_bounds__(TR_NT, 3)
     top_ring(const __grid_constant__ LossArgs a, const int k, const float big, int32_t* const out_ids,
              const int places, const int gm_bytes) {
   extern __shared__ __align__(16) unsigned char smem_raw[];
@@ -259,7 +261,7 @@ __global__ void __launch_bounds__(TR_NT, 2)
       bar_init(&sm.full[i], 1);
       bar_init(&sm.empty[i], TR_NW);
     }
-    sm.groups[0] = sm.groups[1] = sm.keys[0] = sm.keys[1] = 0;
+    sm.keys[0] = sm.keys[1] = sm.crowded[0] = sm.crowded[1] = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
@@ -310,6 +312,9 @@ __global__ void __launch_bounds__(TR_NT, 2)
     }
     // ---- the row's sum and its groups' maxima
     float ref = -3e38f, top = -INFINITY;
+    // (GW 4) this thread's first groups by their maxima, top being the first's, and where they are
+    float top2 = -INFINITY, top3 = -INFINITY, top4 = -INFINITY;
+    int32_t at1 = 0, at2 = 0, at3 = 0;
     float2 S = make_float2(0.f, 0.f);
     const int32_t groups = (sh.w1 - sh.w0 + GW - 1) / GW;
     for (int32_t w = sh.w0; w < sh.w1; w += TR_CHUNK) {
@@ -335,7 +340,16 @@ __global__ void __launch_bounds__(TR_NT, 2)
       if constexpr (GW == 4) {
         const float m = Tr::tile_max(v);
         if (g < groups) gm[g] = TopMax<T>::of(m);
-        top = fmaxf(top, m);
+        if (m > top4) {
+          const bool b1 = m > top, b2 = m > top2, b3 = m > top3;
+          top4 = b3 ? top3 : m;
+          top3 = b2 ? top2 : b3 ? m : top3;
+          at3 = b2 ? at2 : b3 ? g : at3;
+          top2 = b1 ? top : b2 ? m : top2;
+          at2 = b1 ? at1 : b2 ? g : at2;
+          top = b1 ? m : top;
+          at1 = b1 ? g : at1;
+        }
       } else {
 #pragma unroll
         for (int q = 0; q < TR_W; ++q) {
@@ -349,6 +363,7 @@ __global__ void __launch_bounds__(TR_NT, 2)
     float R;
     join(make_float2(ref, S.x + S.y), 1.f, ref, R);
     // the elements before and after the words: the first CTA's
+    const float first_max = top;
     int32_t v_end = -1;
     float x_end = -INFINITY;
     if (warp == 0) {
@@ -361,67 +376,127 @@ __global__ void __launch_bounds__(TR_NT, 2)
       }
       R += warp_sum(v_end >= 0 ? ex2(fmaf(x_end, a.c2, -ref)) : 0.f);
       top = fmaxf(top, x_end);
-      if (lane == 0) sm.groups[parity ^ 1u] = sm.keys[parity ^ 1u] = 0;
+      if (lane == 0) sm.crowded[parity ^ 1u] = sm.keys[parity ^ 1u] = 0;
     }
     if (lane == 0) sm.part[warp] = make_float2(ref, R);
-    sm.max[tid] = top;
+    const uint32_t sorted = warp_sort_desc(ord(top), lane);
+    sm.max[tid] = sorted;
     named_bar_sync(BAR_TOP, 32 * TR_NW);
     // ---- the bound: the k-th largest of the threads' maxima
     join(lane < TR_NW ? sm.part[lane] : make_float2(-3e38f, 0.f), 1.f, ref, R);
     {
-      const float4* q = reinterpret_cast<const float4*>(sm.max);
+      // the values before this lane's in each warp's list, of equal ones those of earlier warps
       int before = 0;
-#pragma unroll 8
-      for (int i = 0; i < 8 * TR_NW; ++i) {
-        const float4 f = q[i];
-        before += (f.x > top || (f.x == top && 4 * i < tid)) + (f.y > top || (f.y == top && 4 * i + 1 < tid)) +
-                  (f.z > top || (f.z == top && 4 * i + 2 < tid)) +
-                  (f.w > top || (f.w == top && 4 * i + 3 < tid));
+#pragma unroll
+      for (int w = 0; w < TR_NW; ++w) {
+        const uint32_t* l = sm.max + 32 * w;
+        const uint32_t least = w < warp ? sorted : sorted + 1u;
+        int n_before = 0;
+#pragma unroll
+        for (int s = 16; s > 0; s >>= 1)
+          if (l[n_before + s - 1] >= least) n_before += s;
+        if (l[n_before] >= least) ++n_before;
+        before += w == warp ? lane : n_before;
       }
-      if (before == k - 1) sm.bound = top;
+      if (before == k - 1) sm.bound = unord(sorted);
     }
     named_bar_sync(BAR_TOP, 32 * TR_NW);
     const float bound = sm.bound;
     auto reaches = [&](float x) { return x >= bound && x > -big; };
-    if (reaches(top)) {
-      for (int32_t g = tid; g < groups; g += 32 * TR_NW)
-        if (reaches(top_max(gm[g]))) {
-          const int i = atomicAdd(&sm.groups[parity], 1);
-          if (i < TR_GROUPS) sm.group[i] = (uint32_t)g;
-        }
-    }
-    named_bar_sync(BAR_TOP, 32 * TR_NW);
-    // ---- the elements that reach it
-    const int found = sm.groups[parity];
-    auto take = [&](float x, int32_t v) {
-      if (reaches(x)) {
-        const int i = atomicAdd(&sm.keys[parity], 1);
-        if (i < TR_KEYS) sm.key[i] = top_key(x, (uint32_t)v);
-      }
+    // ---- the groups that reach it: each warp those of its threads
+    int found = 0;
+    auto list_groups = [&](bool on, int32_t g) {
+      const unsigned b = __ballot_sync(FULL, on);
+      const int i = found + __popc(b & ((1u << lane) - 1u));
+      if (on && i < TR_GROUPS) sm.group[warp][i] = (uint16_t)g;
+      found += __popc(b);
     };
-    const char* const words = sh.x + sizeof(T) * sh.head;
-    if (found <= TR_GROUPS)
-      for (int i = tid; i < found * GW; i += 32 * TR_NW) {
-        const int32_t w = sh.w0 + (int32_t)sm.group[i / GW] * GW + i % GW;
-        if (w < sh.w1) {
-          const uint4 q = ld_reread(words + 16 * (int64_t)w);
-          if (reaches(Tr::gmax(q))) {
+    if (GW == 4 && !__any_sync(FULL, reaches(top4))) {
+      list_groups(reaches(first_max), at1);
+      list_groups(reaches(top2), at2);
+      list_groups(reaches(top3), at3);
+    } else if (__any_sync(FULL, reaches(top))) {
+      for (int32_t g0 = 32 * warp; g0 < groups; g0 += 4 * 32 * TR_NW) {
+        bool on[4];
 #pragma unroll
-            for (int j = 0; j < Tr::VEC; ++j) take(Tr::at(q, j), sh.head + w * Tr::VEC + j);
+        for (int q = 0; q < 4; ++q) {
+          const int32_t g = g0 + 32 * TR_NW * q + lane;
+          on[q] = g < groups && reaches(top_max(gm[g]));
+        }
+#pragma unroll
+        for (int q = 0; q < 4; ++q) list_groups(on[q], g0 + 32 * TR_NW * q + lane);
+      }
+    }
+    __syncwarp();
+    // ---- their elements that do
+    const char* const words = sh.x + sizeof(T) * sh.head;
+    auto take = [&](int mine) {  // the place of this lane's elements, `mine` of them
+      int at = mine;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int u = __shfl_up_sync(FULL, at, o);
+        if (lane >= o) at += u;
+      }
+      const int all = __shfl_sync(FULL, at, 31);
+      int base = 0;
+      if (lane == 0 && all > 0) base = atomicAdd(&sm.keys[parity], all);
+      return __shfl_sync(FULL, base, 0) + at - mine;
+    };
+    if (found <= TR_GROUPS) {
+      constexpr int U = 2;  // words of a lane on their way
+      for (int i0 = 0; i0 < found * GW; i0 += 32 * U) {
+        uint4 q[U];
+        int32_t w[U];
+        int mine = 0;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const int i = i0 + 32 * u + lane;
+          q[u] = make_uint4(Tr::NEG_WORD, Tr::NEG_WORD, Tr::NEG_WORD, Tr::NEG_WORD);
+          w[u] = i < found * GW ? sh.w0 + (int32_t)sm.group[warp][i / GW] * GW + i % GW : sh.w1;
+          if (w[u] < sh.w1) q[u] = ld_reread(words + 16 * (int64_t)w[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+          if (reaches(Tr::gmax(q[u]))) {
+#pragma unroll
+            for (int j = 0; j < Tr::VEC; ++j) mine += reaches(Tr::at(q[u], j));
+          }
+        int to = take(mine);
+        if (mine > 0) {
+#pragma unroll
+          for (int u = 0; u < U; ++u) {
+#pragma unroll
+            for (int j = 0; j < Tr::VEC; ++j) {
+              const float x = Tr::at(q[u], j);
+              if (reaches(x)) {
+                if (to < TR_KEYS) sm.key[to] = top_key(x, (uint32_t)(sh.head + w[u] * Tr::VEC + j));
+                ++to;
+              }
+            }
           }
         }
       }
-    if (v_end >= 0) take(x_end, v_end);
+    } else if (lane == 0) {
+      sm.crowded[parity] = 1;
+    }
+    if (warp == 0 && sh.head + sh.tail > 0) {
+      const int mine = v_end >= 0 && reaches(x_end);
+      const int to = take(mine);
+      if (mine && to < TR_KEYS) sm.key[to] = top_key(x_end, (uint32_t)v_end);
+    }
     named_bar_sync(BAR_TOP, 32 * TR_NW);
     // ---- their order
     const int count = sm.keys[parity];
-    if (found <= TR_GROUPS && count <= TR_KEYS) {
-      for (int i = tid; i < count; i += 32 * TR_NW) {
-        const uint64_t mine = sm.key[i];
+    if (count <= TR_KEYS && !sm.crowded[parity]) {
+      for (int i0 = 0; i0 < count; i0 += 8 * TR_NW) {  // four lanes a key
+        const int i = i0 + (tid >> 2);
+        const uint64_t mine = i < count ? sm.key[i] : 0ull;
         int before = 0;
 #pragma unroll 4
-        for (int j = 0; j < count; ++j) before += sm.key[j] > mine;
-        if (before < k) sm.top[before] = mine;
+        for (int j = lane & 3; j < count; j += 4) before += sm.key[j] > mine;
+        before += __shfl_xor_sync(FULL, before, 1);
+        before += __shfl_xor_sync(FULL, before, 2);
+        if ((lane & 3) == 0 && i < count && before < k) sm.top[before] = mine;
       }
       if (tid >= count && tid < k) sm.top[tid] = 0ull;
     } else if (warp == 0) {
@@ -444,10 +519,10 @@ __global__ void __launch_bounds__(TR_NT, 2)
     }
     named_bar_sync(BAR_TOP, 32 * TR_NW);
     // ---- the list
-    uint64_t mine = tid < k ? sm.top[tid] : 0ull;
+    const uint64_t mine = tid < k ? sm.top[tid] : 0ull;
     float2 all = make_float2(ref, R);
     if (C > 1) {
-      if (tid < k) dsmem_st_u64(dsmem_addr(&sm.lists[rank][tid], 0), mine);
+      if (tid < TP_MAX) dsmem_st_u64(dsmem_addr(&sm.lists[rank][tid], 0), mine);
       if (tid == 0)
         dsmem_st_u64(dsmem_addr(&sm.sums[rank], 0),
                      (uint64_t)__float_as_uint(ref) | (uint64_t)__float_as_uint(R) << 32);
@@ -470,33 +545,28 @@ __global__ void __launch_bounds__(TR_NT, 2)
       if (C == 1) {
         if (tid < k) give(tid, mine);
       } else {
-        // an element's place is the number of those before it in each list, found by bisection
-        int valid = 0;
-        for (uint32_t c = 0; c < C; ++c) {
-          int lo = 0, hi = k;
-          while (lo < hi) {
-            const int mid = (lo + hi) >> 1;
-            if (sm.lists[c][mid] > 0ull) lo = mid + 1;
-            else hi = mid;
-          }
-          valid += lo;
-        }
-        for (int i = tid; i < (int)C * k; i += 32 * TR_NW) {
-          const uint64_t q = sm.lists[i / k][i % k];
-          if (q == 0ull) continue;
-          int before = 0;
-          for (uint32_t c = 0; c < C; ++c) {
-            int lo = 0, hi = k;
-            while (lo < hi) {
-              const int mid = (lo + hi) >> 1;
-              if (sm.lists[c][mid] > q) lo = mid + 1;
-              else hi = mid;
+        // an element's place is the number of those before it in each list, found by bisection (lists
+        // end with zeros, which come after everything)
+        for (int i = tid; i < (int)C * TP_MAX; i += 32 * TR_NW) {
+          const int c = i / TP_MAX, j = i % TP_MAX;
+          const uint64_t q = sm.lists[c][j];
+          int before = j;
+#pragma unroll
+          for (int o = 0; o < MAXC; ++o) {
+            const uint64_t* l = sm.lists[o];
+            if (o < (int)C && o != c) {
+              // of zeros, too, one comes after the other
+              const uint64_t least = q == 0ull ? (o < c ? 0ull : 1ull) : q;
+              int n_before = 0;
+#pragma unroll
+              for (int s = TP_MAX / 2; s > 0; s >>= 1)
+                if (l[n_before + s - 1] >= least) n_before += s;
+              if (l[n_before] >= least) ++n_before;
+              before += n_before;
             }
-            before += lo;
           }
           if (before < k) give(before, q);
         }
-        if (tid < k && tid >= valid) give(tid, 0ull);
       }
       if (bad && tid == 0) atomicOr(a.ctx_flags, FLAG_NONFINITE);
     }

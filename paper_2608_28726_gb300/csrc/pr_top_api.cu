@@ -22,12 +22,12 @@ const void* ring_kernel(pr_dtype dt, bool words) {
   return dt == PR_DTYPE_BF16 ? ring_kernel<__nv_bfloat16>(words) : ring_kernel<float>(words);
 }
 
-constexpr size_t SM_BYTES = 227 * 1024;         // a CTA alone on an SM
-constexpr size_t HALF_BYTES = 113 * 1024;       // one of two
+// shared memory of one, two or three CTAs on an SM
+constexpr size_t SM_BYTES = 227 * 1024, HALF_BYTES = 113 * 1024, THIRD_BYTES = 75 * 1024;
 
 // The ring's launch: CTAs per row, words of a group, bytes of the groups' maxima, places.
 struct TopShape {
-  int cluster, places;
+  int cluster, places, on_sm;
   bool words, fits;
   size_t gm, smem;
 };
@@ -48,9 +48,17 @@ TopShape choose(const pr_ctx* c, pr_dtype dt, int64_t n_rows, int64_t vocab) {
     const int64_t groups = s.words ? part : (part + 3) / 4;
     s.gm = ((size_t)groups * (dt == PR_DTYPE_BF16 ? 2 : 4) + 127) / 128 * 128;
     const size_t fixed = prk::TR_START + s.gm;
-    if (fixed + 2 * prk::TR_BYTES > SM_BYTES) continue;
-    s.places = fixed + 3 * prk::TR_BYTES <= HALF_BYTES ? (int)((HALF_BYTES - fixed) / prk::TR_BYTES)
-                                                       : (int)((SM_BYTES - fixed) / prk::TR_BYTES);
+    if (fixed + 2 * prk::TR_BYTES > SM_BYTES || groups > 65536) continue;
+    // Three CTAs on an SM where their rings keep three places, two with four: while one chooses, the
+    // others stream (4,096 rows of V = 151,936 bf16, k = 20: 206 us for 234 with two).  Where
+    // that leaves one CTA, two with a row's parts are better (1,000 rows of V = 262,144 fp32: 190
+    // for 202).  Fewer CTAs than would fit get the room of the others.
+    const int64_t ctas = n_rows * s.cluster;
+    s.on_sm = fixed + 3 * prk::TR_BYTES <= THIRD_BYTES ? 3 : fixed + 4 * prk::TR_BYTES <= HALF_BYTES ? 2 : 1;
+    if (s.on_sm == 1 && s.cluster < 4 && words > 2 * s.cluster * prk::TR_CHUNK) continue;
+    s.on_sm = (int)std::min<int64_t>(s.on_sm, (ctas + c->num_sms - 1) / c->num_sms);
+    const size_t room = s.on_sm == 3 ? THIRD_BYTES : s.on_sm == 2 ? HALF_BYTES : SM_BYTES;
+    s.places = (int)((room - fixed) / prk::TR_BYTES);
     s.places = std::min(s.places, (int)prk::TR_MOST);
     s.smem = fixed + (size_t)s.places * prk::TR_BYTES;
     s.fits = true;
@@ -94,12 +102,12 @@ pr_status pr_top_logits(pr_ctx* c, const void* logits, pr_dtype dt, int64_t n_ro
     int kk = k, places = shape.places, gm = (int)shape.gm;
     float limit = big;
     int32_t* out = ids;
-    const int64_t at_once = shape.smem <= HALF_BYTES ? 2 * c->num_sms : c->num_sms;
-    const int64_t groups = std::min<int64_t>(n_rows, shape.cluster > 1 ? n_rows : at_once);
+    const int64_t at_once = (int64_t)shape.on_sm * c->num_sms;
+    const int64_t groups = std::min<int64_t>(n_rows, std::max<int64_t>(1, at_once / shape.cluster));
     void* args[] = {&l, &kk, &limit, &out, &places, &gm};
     st = launch(ring_kernel(dt, shape.words),
-                (unsigned)(std::min<int64_t>(groups, 0x7fffffffLL / shape.cluster) * shape.cluster),
-                prk::TR_NT, shape.smem, (unsigned)shape.cluster, args, s, shape.cluster > 1 || n_rows < at_once);
+                (unsigned)(groups * shape.cluster), prk::TR_NT, shape.smem, (unsigned)shape.cluster, args, s,
+                n_rows < groups + 1 && groups * shape.cluster < at_once);
     return st == PR_OK ? timing_mark(c, s) : st;
   }
   prk::TopArgs a;
