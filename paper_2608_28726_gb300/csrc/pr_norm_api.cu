@@ -26,6 +26,63 @@ bool same_rows(const void* out, int64_t out_stride, const void* in, int64_t in_s
   return out != in || out_stride == in_stride;
 }
 
+bool on_words(const void* p, int64_t stride, pr_dtype dt) {
+  return !p || (aligned16(p) && stride * (int64_t)esize(dt) % 16 == 0);
+}
+// eight weights of fp32, or of bf16, are read as words of 16 or 8 bytes
+bool weights_on_words(const void* p) { return aligned16(p); }
+
+// What has a row in registers: threads and words of each.
+struct NormShape {
+  const void* kernel;
+  int threads;  // of a row
+};
+template <typename T, int L, int N>
+NormShape forward_shape() {
+  return {reinterpret_cast<const void*>(&prk::norm_rows<T, L, N>), L};
+}
+template <typename T>
+NormShape forward_of(int64_t words) {
+  if (words <= 16) return forward_shape<T, 8, 2>();
+  if (words <= 64) return forward_shape<T, 32, 2>();
+  if (words <= 128) return forward_shape<T, 32, 4>();
+  if (words <= 256) return forward_shape<T, 128, 2>();
+  if (words <= 512) return forward_shape<T, 128, 4>();
+  if (words <= 1024) return forward_shape<T, 512, 2>();
+  if (words <= 2048) return forward_shape<T, 512, 4>();
+  return {nullptr, 0};
+}
+template <typename T, int L, int N>
+NormShape backward_shape() {
+  return {reinterpret_cast<const void*>(&prk::dnorm_rows<T, L, N>), L};
+}
+template <typename T>
+NormShape backward_of(int64_t words) {
+  if (words <= 16) return backward_shape<T, 8, 2>();
+  if (words <= 64) return backward_shape<T, 32, 2>();
+  if (words <= 256) return backward_shape<T, 128, 2>();
+  if (words <= 512) return backward_shape<T, 256, 2>();
+  if (words <= 1024) return backward_shape<T, 512, 2>();
+  if (words <= 2048) return backward_shape<T, 512, 4>();
+  return {nullptr, 0};
+}
+
+pr_status launch(pr_ctx* c, const void* kernel, dim3 grid, unsigned threads, void** args, cudaStream_t s) {
+  cudaLaunchConfig_t cfg;
+  memset(&cfg, 0, sizeof cfg);
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  PR_CUDA(cudaLaunchKernelExC(&cfg, kernel, args));
+  g_launches.fetch_add(1, std::memory_order_relaxed);
+  return timing_mark(c, s);
+}
+
 pr_status finish(pr_ctx* c, cudaStream_t s) {
   PR_CUDA(cudaGetLastError());
   g_launches.fetch_add(1, std::memory_order_relaxed);
@@ -79,6 +136,17 @@ pr_status pr_layernorm(pr_ctx* c, const void* x, pr_dtype dt, int64_t n_rows, in
   a.inv_d = (float)(1.0 / (double)d);
   a.rms = rms ? 1 : 0;
   a.wide_w = wdt == PR_DTYPE_F32;
+  a.vec = on_words(x, x_stride, dt) && on_words(residual, residual_stride, dt) &&
+          on_words(total, total_stride, dt) && on_words(y, y_stride, dt);
+  a.vec_w = weights_on_words(weight) && weights_on_words(bias);
+  const int64_t words = (d * (int64_t)esize(dt) + 15) / 16;
+  const NormShape shape = dt == PR_DTYPE_BF16 ? forward_of<__nv_bfloat16>(words) : forward_of<float>(words);
+  if (shape.kernel) {
+    const int threads = std::max(shape.threads, prk::NR_NT), rows = threads / shape.threads;
+    const int64_t grid = std::min<int64_t>((n_rows + rows - 1) / rows, (int64_t)c->num_sms * 2048 / threads);
+    void* args[] = {&a};
+    return launch(c, shape.kernel, dim3((unsigned)grid), (unsigned)threads, args, s);
+  }
   if (dt == PR_DTYPE_BF16)
     prk::norm_wide<__nv_bfloat16><<<(unsigned)n_rows, prk::NW_NT, 0, s>>>(a);
   else
@@ -133,6 +201,26 @@ pr_status pr_layernorm_backward(pr_ctx* c, const void* dy, int64_t dy_stride, co
   a.rms = rms ? 1 : 0;
   a.wide_w = wdt == PR_DTYPE_F32;
   a.accumulate = accumulate ? 1 : 0;
+  a.vec = on_words(x, x_stride, dt) && on_words(dy, dy_stride, dt) && on_words(dtotal, dtotal_stride, dt) &&
+          on_words(dx, dx_stride, dt);
+  a.vec_w = weights_on_words(weight);
+  const int64_t words = (d * (int64_t)esize(dt) + 15) / 16;
+  const NormShape shape = dt == PR_DTYPE_BF16 ? backward_of<__nv_bfloat16>(words) : backward_of<float>(words);
+  if (shape.kernel) {
+    const int threads = std::max(shape.threads, prk::NR_NT), rows = threads / shape.threads;
+    const int64_t grid = std::min<int64_t>((n_rows + rows - 1) / rows, (int64_t)c->num_sms * 512 / threads);
+    if (dweight || dbias) {
+      if ((st = grow(c->norm_ws, (size_t)grid * 2 * d * sizeof(float), false)) != PR_OK) return st;
+      a.part = static_cast<float*>(c->norm_ws.p);
+    }
+    void* args[] = {&a};
+    if ((st = launch(c, shape.kernel, dim3((unsigned)grid), (unsigned)threads, args, s)) != PR_OK) return st;
+    if (!a.part) return PR_OK;
+    int ctas = (int)grid;
+    void* sum_args[] = {&a, &ctas};
+    return launch(c, reinterpret_cast<const void*>(&prk::dnorm_sum), dim3((unsigned)((d + 31) / 32), 2),
+                  prk::NS_NT, sum_args, s);
+  }
   if (dweight || dbias) {  // first: dx may be written over dy and x
     const unsigned grid = (unsigned)((d + 31) / 32);
     if (dt == PR_DTYPE_BF16)
