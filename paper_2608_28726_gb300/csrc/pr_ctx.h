@@ -74,6 +74,7 @@ struct pr_ctx {
   bool loss_ready = false;             // shared memory opt-ins made
   int loss_places[2][4] = {};          // clusters of 1, 2, 4, 8 CTAs resident; half, all of the SMs
   bool adamw_ready[2][12] = {};        // pr_adamw_step: shared memory opt-ins made
+  bool norm_ready = false;             // pr_layernorm and its backward pass: shared memory opt-ins made
   bool top_ready = false;              // pr_top_logits: shared memory opt-ins made
   bool distill_ready = false;          // pr_distill_loss: the same
   int distill_places[2][4] = {};       // and its loss_places

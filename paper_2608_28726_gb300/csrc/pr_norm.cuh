@@ -9,7 +9,7 @@
 // the variance's corrects both.
 #pragma once
 
-#include "pr_device.cuh"
+#include "pr_loss.cuh"
 
 namespace prk {
 
@@ -30,8 +30,12 @@ struct NormArgs {
   float eps, inv_d;
   int32_t rms, wide_w;  // wide_w: weights are fp32 (else bf16)
   int32_t accumulate;
-  int32_t vec, vec_w;   // rows (weights) begin at multiples of 16 bytes
+  int32_t vec_w;        // the weights begin at multiples of 16 bytes
+  int32_t stages;       // rows of a group on their way into shared memory
+  int32_t row_bytes;    // room of one there
+  int32_t stage_res;    // backward: dtotal's, too (else its threads read it)
   float* part;          // workspace: [CTAs][2][d] sums of dy xhat and of dy
+  uint32_t* ctx_flags;
 };
 
 __device__ __forceinline__ float nm_get(const float* p) { return *p; }
@@ -68,89 +72,137 @@ __device__ __forceinline__ float nm_block_sum(float v, float* part) {
   return v;
 }
 
-// ---- rows in registers -----------------------------------------------------------------
+// ---- rows in shared memory -------------------------------------------------------------
 //
-// L threads have a row, N 16-byte words each, and read it once: what the moments and the output
-// need stays in registers.  Rows of up to 32 threads are summed by shuffles, wider ones
-// through shared memory with a barrier of the row's threads alone, so that the CTA's other rows
-// go on meanwhile; enough CTAs are on an SM to keep memory busy.
+// L threads have a row, N words of 16 bytes each, and memory is read once: rows come into shared
+// memory by bulk copies, a few ahead, so that what is on its way takes no registers and memory stays
+// busy while rows are summed.  Rows of up to 16 words are read by their threads.  Rows of up to 32
+// threads are summed by shuffles, wider ones through shared memory with a barrier of the row's
+// threads alone, so that the CTA's other rows go on meanwhile.  The weights are in shared memory, too.
+//
+// Columns of thread t's word i: VEC neighbours from (t + i L) VEC on; in rows off the 16-byte grid, L
+// apart from t + i VEC L on, so that a warp's accesses stay side by side.  Of such a row the copy
+// takes every 16-byte word that it touches (a word with a byte of an allocation lies in it whole).
 
 constexpr int NR_NT = 256;  // threads of a CTA of rows of up to so many
 
-template <typename T>
+// WHOLE: rows on the grid, of whole words.  (A template: what chooses at run time issues both ways'
+// instructions, 4,150 a warp and row of 3,584 bf16 for NORM_INSTR.)
+template <typename T, int L, bool WHOLE>
 struct RowWord {
   static constexpr int VEC = 16 / (int)sizeof(T);
-  static __device__ __forceinline__ float at(const uint4& w, int j) {
+  float2 f[VEC / 2];
+  static __device__ __forceinline__ int column(int t, int i, int j) {
+    return WHOLE ? (t + i * L) * VEC + j : t + (i * VEC + j) * L;
+  }
+  // whether word i has all of its columns, or any
+  static __device__ __forceinline__ bool full(int t, int i, int d) { return column(t, i, VEC - 1) < d; }
+  static __device__ __forceinline__ bool some(int t, int i, int d) { return column(t, i, 0) < d; }
+  __device__ __forceinline__ void zero() {
+#pragma unroll
+    for (int j = 0; j < VEC / 2; ++j) f[j] = make_float2(0.f, 0.f);
+  }
+  __device__ __forceinline__ void set(int j, float v) {
+    if (j & 1) f[j / 2].y = v;
+    else f[j / 2].x = v;
+  }
+  __device__ __forceinline__ float get(int j) const { return j & 1 ? f[j / 2].y : f[j / 2].x; }
+  __device__ __forceinline__ void from(const uint4& w) {
+    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
     if constexpr (sizeof(T) == 4) {
-      return __uint_as_float(j == 0 ? w.x : j == 1 ? w.y : j == 2 ? w.z : w.w);
+      f[0] = make_float2(__uint_as_float(u[0]), __uint_as_float(u[1]));
+      f[1] = make_float2(__uint_as_float(u[2]), __uint_as_float(u[3]));
     } else {
-      const int q = j >> 1;
-      const uint32_t u = q == 0 ? w.x : q == 1 ? w.y : q == 2 ? w.z : w.w;
-      return __uint_as_float((j & 1) ? (u & 0xffff0000u) : (u << 16));
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        f[q] = make_float2(__uint_as_float(u[q] << 16), __uint_as_float(u[q] & 0xffff0000u));
     }
   }
-  static __device__ __forceinline__ uint4 of(const float (&f)[VEC]) {
-    uint4 r;
-    uint32_t* u = reinterpret_cast<uint32_t*>(&r);
+  __device__ __forceinline__ uint4 packed() const {
+    if constexpr (sizeof(T) == 4) {
+      return make_uint4(__float_as_uint(f[0].x), __float_as_uint(f[0].y), __float_as_uint(f[1].x),
+                        __float_as_uint(f[1].y));
+    } else {
+      uint32_t u[4];
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      if constexpr (sizeof(T) == 4) {
-        u[q] = __float_as_uint(f[q]);
-      } else {
-        const __nv_bfloat162 h = __floats2bfloat162_rn(f[2 * q], f[2 * q + 1]);
+      for (int q = 0; q < 4; ++q) {
+        const __nv_bfloat162 h = __float22bfloat162_rn(f[q]);
         u[q] = *reinterpret_cast<const uint32_t*>(&h);
       }
+      return make_uint4(u[0], u[1], u[2], u[3]);
     }
-    return r;
   }
-  // word i of a row of d elements, 0 past its end
-  static __device__ __forceinline__ uint4 load(const T* row, int64_t i, int64_t d, bool vec) {
-    if (vec && (i + 1) * VEC <= d) return ld_stream(row + i * VEC);
-    uint4 r = make_uint4(0u, 0u, 0u, 0u);
-    float f[VEC];
+  // word i of thread t of a row of d elements (in shared or global memory), 0 past its end
+  __device__ __forceinline__ void load(const T* row, int t, int i, int d) {
+    if constexpr (WHOLE) {
+      if (full(t, i, d)) from(*reinterpret_cast<const uint4*>(row + (t + i * L) * VEC));
+      else zero();
+    } else if (full(t, i, d)) {
 #pragma unroll
-    for (int j = 0; j < VEC; ++j) f[j] = i * VEC + j < d ? nm_get(row + i * VEC + j) : 0.f;
-    if (i * VEC < d) r = of(f);
-    return r;
+      for (int j = 0; j < VEC; ++j) set(j, nm_get(row + column(t, i, j)));
+    } else {
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) set(j, column(t, i, j) < d ? nm_get(row + column(t, i, j)) : 0.f);
+    }
   }
-  static __device__ __forceinline__ void store(T* row, int64_t i, int64_t d, bool vec, const float (&f)[VEC]) {
-    if (vec && (i + 1) * VEC <= d) {
-      *reinterpret_cast<uint4*>(row + i * VEC) = of(f);
+  __device__ __forceinline__ void store(T* row, int t, int i, int d) const {  // (of a word with some)
+    if constexpr (WHOLE) {
+      *reinterpret_cast<uint4*>(row + (t + i * L) * VEC) = packed();
     } else {
 #pragma unroll
       for (int j = 0; j < VEC; ++j)
-        if (i * VEC + j < d) nm_put(row + i * VEC + j, f[j]);
+        if (column(t, i, j) < d) nm_put(row + column(t, i, j), get(j));
     }
   }
-  // the weights of word i's elements (they stay in L1)
-  static __device__ __forceinline__ void weights(const void* w, bool wide, bool vec, int64_t i, int64_t d,
-                                                 float (&f)[VEC]) {
-    if (vec && (i + 1) * VEC <= d) {
-      if (wide) {
+  // its weights, which shared memory holds
+  __device__ __forceinline__ void weights(const unsigned char* w, bool wide, int t, int i, int d) {
+    if constexpr (WHOLE) {
+      const int c0 = (t + i * L) * VEC;
+      if (!some(t, i, d)) {
+        zero();
+      } else if (wide) {
 #pragma unroll
         for (int q = 0; q < VEC / 4; ++q) {
-          const float4 v = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(w) + i * VEC + 4 * q);
-          f[4 * q] = v.x;
-          f[4 * q + 1] = v.y;
-          f[4 * q + 2] = v.z;
-          f[4 * q + 3] = v.w;
+          const float4 v = reinterpret_cast<const float4*>(w)[c0 / 4 + q];
+          f[2 * q] = make_float2(v.x, v.y);
+          f[2 * q + 1] = make_float2(v.z, v.w);
         }
       } else {
 #pragma unroll
         for (int q = 0; q < VEC / 4; ++q) {
-          const uint2 v = *reinterpret_cast<const uint2*>(reinterpret_cast<const __nv_bfloat16*>(w) + i * VEC + 4 * q);
-          f[4 * q] = __uint_as_float(v.x << 16);
-          f[4 * q + 1] = __uint_as_float(v.x & 0xffff0000u);
-          f[4 * q + 2] = __uint_as_float(v.y << 16);
-          f[4 * q + 3] = __uint_as_float(v.y & 0xffff0000u);
+          const uint2 v = reinterpret_cast<const uint2*>(w)[c0 / 4 + q];
+          f[2 * q] = make_float2(__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xffff0000u));
+          f[2 * q + 1] = make_float2(__uint_as_float(v.y << 16), __uint_as_float(v.y & 0xffff0000u));
         }
       }
+    } else if (wide) {
+#pragma unroll
+      for (int j = 0; j < VEC; ++j)
+        set(j, column(t, i, j) < d ? reinterpret_cast<const float*>(w)[column(t, i, j)] : 0.f);
     } else {
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) f[j] = i * VEC + j < d ? nm_weight(w, wide, i * VEC + j) : 0.f;
+      for (int j = 0; j < VEC; ++j)
+        set(j, column(t, i, j) < d ? nm_get(reinterpret_cast<const __nv_bfloat16*>(w) + column(t, i, j)) : 0.f);
     }
   }
 };
+__device__ __forceinline__ float2 nm_both(float v) { return make_float2(v, v); }
+
+// the weights of d columns into shared memory, 0 up to a multiple of eight; by a CTA, then a barrier
+__device__ __forceinline__ int nm_weight_bytes(int d, bool wide) { return (d + 7) / 8 * 8 * (wide ? 4 : 2); }
+__device__ __forceinline__ void nm_keep(unsigned char* to, const void* w, bool wide, bool vec, int d) {
+  const int words = vec ? d / (wide ? 4 : 8) : 0;
+#pragma unroll 4
+  for (int i = threadIdx.x; i < words; i += blockDim.x)
+    reinterpret_cast<uint4*>(to)[i] = reinterpret_cast<const uint4*>(w)[i];
+#pragma unroll 4
+  for (int i = words * (wide ? 4 : 8) + threadIdx.x; i < (d + 7) / 8 * 8; i += blockDim.x) {
+    if (wide)
+      reinterpret_cast<float*>(to)[i] = i < d ? reinterpret_cast<const float*>(w)[i] : 0.f;
+    else
+      reinterpret_cast<uint16_t*>(to)[i] = i < d ? reinterpret_cast<const uint16_t*>(w)[i] : (uint16_t)0;
+  }
+}
 
 // (a, b) summed over a row's L threads.  `part`: two buffers of a float2 per warp of the CTA, used in turn.
 template <int L>
@@ -165,97 +217,193 @@ __device__ __forceinline__ float2 nm_row_sum(float2 v, float2 (*part)[32], int t
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, row = warp / W;
     if (lane == 0) part[turn][warp] = v;
     asm volatile("bar.sync %0, %1;" ::"r"(1 + row), "r"(L) : "memory");
-    v = lane < W ? part[turn][row * W + lane] : make_float2(0.f, 0.f);
+    v = part[turn][row * W + (lane & (W - 1))];
 #pragma unroll
-    for (int o = (W > 16 ? 32 : W > 8 ? 16 : W > 4 ? 8 : W > 2 ? 4 : 2) / 2; o > 0; o >>= 1) {
+    for (int o = W / 2; o > 0; o >>= 1) {
       v.x += __shfl_xor_sync(FULL, v.x, o);
       v.y += __shfl_xor_sync(FULL, v.y, o);
     }
-    v.x = __shfl_sync(FULL, v.x, 0);
-    v.y = __shfl_sync(FULL, v.y, 0);
   }
   return v;
 }
 
-template <typename T, int L, int N>
-__global__ void __launch_bounds__(L > NR_NT ? L : NR_NT) norm_rows(const __grid_constant__ NormArgs a) {
-  using W = RowWord<T>;
+// The rows of a group of L threads in shared memory: `stages` places for the words of K rows each (x and
+// the residual; x, dy and dtotal).  One thread fills them; a place is filled again once every
+// thread is past a later sum.
+template <typename T, int L>
+struct RowStages {
+  uint64_t* full;        // a barrier per place
+  unsigned char* at;     // this group's places
+  int stages, bytes, row_bytes, d;  // bytes of a place, and of a row in it
+  int place = 0;
+  uint32_t turn = 0u;
+  uint32_t* flags;
+  bool ok = true;
+  __device__ __forceinline__ RowStages(unsigned char* smem, const NormArgs& a, int k)
+      : stages(a.stages), row_bytes(a.row_bytes), d((int)a.d), flags(a.ctx_flags) {
+    const int groups = blockDim.x / L, group = threadIdx.x / L;
+    bytes = k * row_bytes;
+    full = reinterpret_cast<uint64_t*>(smem) + group * stages;
+    at = smem + (groups * stages * 8 + 127) / 128 * 128 + (size_t)group * stages * bytes;
+  }
+  __device__ __forceinline__ void init() {  // then a barrier of the CTA
+    if (threadIdx.x % L == 0) {
+      for (int i = 0; i < stages; ++i) bar_init(&full[i], 1);
+      asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+  }
+  // the words that a row touches
+  __device__ __forceinline__ uint32_t size(const T* row) const {
+    return ((uint32_t)(reinterpret_cast<uintptr_t>(row) & 15u) + (uint32_t)d * (uint32_t)sizeof(T) + 15u) & ~15u;
+  }
+  __device__ __forceinline__ void expect(int i, uint32_t all) { bar_expect(&full[i], all); }
+  __device__ __forceinline__ void copy(int i, int j, const T* row) {
+    asm volatile(
+        "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
+            sm_addr(at + (size_t)i * bytes + (size_t)j * row_bytes)),
+        "l"(reinterpret_cast<uintptr_t>(row) & ~(uintptr_t)15), "r"(size(row)), "r"(sm_addr(&full[i]))
+        : "memory");
+  }
+  __device__ __forceinline__ void wait() {
+    if (ok) ok = ring_wait(sm_addr(&full[place]), turn, flags);
+    __syncwarp();
+  }
+  // the j-th row of the place, whose memory is at `row`
+  __device__ __forceinline__ const T* here(int j, const T* row) const {
+    return reinterpret_cast<const T*>(at + (size_t)place * bytes + (size_t)j * row_bytes +
+                                      (reinterpret_cast<uintptr_t>(row) & 15u));
+  }
+  __device__ __forceinline__ void step() {
+    if (++place == stages) {
+      place = 0;
+      turn ^= 1u;
+    }
+  }
+};
+
+template <typename T, int L, int N, bool STAGED, bool WHOLE>
+__global__ void __launch_bounds__(L > NR_NT ? L : NR_NT, L > NR_NT ? 1 : 3)
+    norm_rows(const __grid_constant__ NormArgs a) {
+  using W = RowWord<T, L, WHOLE>;
+  constexpr int H = W::VEC / 2;
+  extern __shared__ __align__(16) unsigned char nm_raw[];
   __shared__ float2 part[2][32];
+  const int rows = blockDim.x / L, in_row = threadIdx.x % L, group = threadIdx.x / L;
+  const int d = (int)a.d;
+  const bool wide = a.wide_w, res = a.res != nullptr;
+  const int w_bytes = nm_weight_bytes(d, wide);
+  const int64_t step = (int64_t)gridDim.x * rows, first = (int64_t)blockIdx.x * rows;
+  auto x_of = [&](int64_t row) { return reinterpret_cast<const T*>(a.x) + row * a.x_stride; };
+  auto res_of = [&](int64_t row) { return reinterpret_cast<const T*>(a.res) + row * a.res_stride; };
+  RowStages<T, L> st(nm_raw + (a.b ? 2 : 1) * w_bytes, a, res ? 2 : 1);
+  auto fill = [&](int i, int64_t row) {
+    st.expect(i, st.size(x_of(row)) + (res ? st.size(res_of(row)) : 0u));
+    st.copy(i, 0, x_of(row));
+    if (res) st.copy(i, 1, res_of(row));
+  };
+  if (STAGED) {
+    st.init();
+    __syncthreads();
+  }
   pdl_wait();
   pdl_trigger();
-  const int rows = blockDim.x / L, in_row = threadIdx.x % L;
-  const int64_t d = a.d;
-  const bool vec = a.vec, vec_w = a.vec_w, wide = a.wide_w;
+  if (STAGED && in_row == 0)
+    for (int i = 0; i < a.stages; ++i)
+      if (first + group + i * step < a.n_rows) fill(i, first + group + i * step);
+  nm_keep(nm_raw, a.w, wide, a.vec_w, d);
+  if (a.b) nm_keep(nm_raw + w_bytes, a.b, wide, a.vec_w, d);
+  __syncthreads();
   int turn = 0;  // of the sums' buffers
   // (every thread of a warp goes through the sums: the last rows of a CTA may be none)
-  for (int64_t r0 = (int64_t)blockIdx.x * rows; r0 < a.n_rows; r0 += (int64_t)gridDim.x * rows) {
-    const int64_t row = r0 + threadIdx.x / L;
+  for (int64_t r0 = first; r0 < a.n_rows; r0 += step) {
+    const int64_t row = r0 + group;
     const bool on = row < a.n_rows;
-    uint4 h[N];
-    const T* x = reinterpret_cast<const T*>(a.x) + row * a.x_stride;
+    W h[N];
+    float2 sum = make_float2(0.f, 0.f);
+    if (on) {
+      const T *x = x_of(row), *r = res_of(row);
+      if (STAGED) {
+        st.wait();
+        x = st.here(0, x);
+        r = st.here(1, r);
+      }
 #pragma unroll
-    for (int i = 0; i < N; ++i)
-      h[i] = on ? W::load(x, in_row + (int64_t)i * L, d, vec) : make_uint4(0u, 0u, 0u, 0u);
-    if (a.res) {
-      const T* res = reinterpret_cast<const T*>(a.res) + row * a.res_stride;
-      uint4 r[N];
+      for (int i = 0; i < N; ++i) h[i].load(x, in_row, i, d);
+      if (res) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          W q;
+          q.load(r, in_row, i, d);
+#pragma unroll
+          for (int j = 0; j < H; ++j) h[i].f[j] = __fadd2_rn(h[i].f[j], q.f[j]);
+          h[i].from(h[i].packed());  // rounded
+        }
+      }
+    } else {
 #pragma unroll
       for (int i = 0; i < N; ++i)
-        r[i] = on ? W::load(res, in_row + (int64_t)i * L, d, vec) : make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        float f[W::VEC];
-#pragma unroll
-        for (int j = 0; j < W::VEC; ++j) f[j] = W::at(h[i], j) + W::at(r[i], j);
-        h[i] = W::of(f);
-      }
+        for (int j = 0; j < H; ++j) h[i].f[j] = make_float2(0.f, 0.f);
     }
     float m = 0.f;
     if (!a.rms) {
-      float s = 0.f;
 #pragma unroll
       for (int i = 0; i < N; ++i)
 #pragma unroll
-        for (int j = 0; j < W::VEC; ++j) s += W::at(h[i], j);
-      m = nm_row_sum<L>(make_float2(s, 0.f), part, turn).x * a.inv_d;
+        for (int j = 0; j < H; ++j) sum = __fadd2_rn(sum, h[i].f[j]);
+      m = nm_row_sum<L>(make_float2(sum.x + sum.y, 0.f), part, turn).x * a.inv_d;
       turn ^= 1;
     }
-    float2 s = make_float2(0.f, 0.f);
+    float2 sq = make_float2(0.f, 0.f);
+    sum = make_float2(0.f, 0.f);
 #pragma unroll
-    for (int i = 0; i < N; ++i)
+    for (int i = 0; i < N; ++i) {
+      if (W::full(in_row, i, d)) {
 #pragma unroll
-      for (int j = 0; j < W::VEC; ++j) {
-        const bool in = (in_row + (int64_t)i * L) * W::VEC + j < d;
-        const float v = in ? W::at(h[i], j) - m : 0.f;
-        s.x = fmaf(v, v, s.x);
-        s.y += v;
+        for (int j = 0; j < H; ++j) {
+          const float2 v = __fadd2_rn(h[i].f[j], nm_both(-m));
+          sq = __ffma2_rn(v, v, sq);
+          sum = __fadd2_rn(sum, v);
+        }
+      } else if (!WHOLE) {
+#pragma unroll
+        for (int j = 0; j < W::VEC; ++j) {
+          const float v = W::column(in_row, i, j) < d ? h[i].get(j) - m : 0.f;
+          sq.x = fmaf(v, v, sq.x);
+          sum.x += v;
+        }
       }
-    s = nm_row_sum<L>(s, part, turn);
+    }
+    const float2 s = nm_row_sum<L>(make_float2(sq.x + sq.y, sum.x + sum.y), part, turn);
     turn ^= 1;
+    if (STAGED) {  // every thread has its words
+      if (in_row == 0 && row + a.stages * step < a.n_rows) fill(st.place, row + a.stages * step);
+      st.step();
+    }
     const float off = a.rms ? 0.f : s.y * a.inv_d, rstd = nm_rstd(s.x, off, a);
     if (on) {
       T* y = reinterpret_cast<T*>(a.y) + row * a.y_stride;
       T* total = reinterpret_cast<T*>(a.total) + row * a.total_stride;
+      const float mean = m + off;
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        const int64_t at = in_row + (int64_t)i * L;
-        if (at * W::VEC >= d) continue;
-        float w[W::VEC], b[W::VEC], f[W::VEC];
-        W::weights(a.w, wide, vec_w, at, d, w);
+        if (!W::some(in_row, i, d)) continue;
+        if (a.total) h[i].store(total, in_row, i, d);
+        W w, b;
+        w.weights(nm_raw, wide, in_row, i, d);
 #pragma unroll
-        for (int j = 0; j < W::VEC; ++j) b[j] = 0.f;
-        if (a.b) W::weights(a.b, wide, vec_w, at, d, b);
-        if (a.total) {
+        for (int j = 0; j < H; ++j) b.f[j] = make_float2(0.f, 0.f);
+        if (a.b) b.weights(nm_raw + w_bytes, wide, in_row, i, d);
 #pragma unroll
-          for (int j = 0; j < W::VEC; ++j) f[j] = W::at(h[i], j);
-          W::store(total, at, d, vec, f);
+        for (int j = 0; j < H; ++j) {
+          const float2 v = __fmul2_rn(__fadd2_rn(h[i].f[j], nm_both(-mean)), nm_both(rstd));
+          h[i].f[j] = __ffma2_rn(v, w.f[j], b.f[j]);
         }
-#pragma unroll
-        for (int j = 0; j < W::VEC; ++j) f[j] = fmaf(((W::at(h[i], j) - m) - off) * rstd, w[j], b[j]);
-        W::store(y, at, d, vec, f);
+        h[i].store(y, in_row, i, d);
       }
       if (in_row == 0) {
-        if (a.mean && !a.rms) a.mean[row] = m + off;
+        if (a.mean && !a.rms) a.mean[row] = mean;
         if (a.rstd) a.rstd[row] = rstd;
       }
     }
@@ -264,108 +412,124 @@ __global__ void __launch_bounds__(L > NR_NT ? L : NR_NT) norm_rows(const __grid_
 
 // The backward pass.  A thread keeps the sums of its columns over all rows of its CTA; the CTA's
 // rows are added up in order at the end and go to the workspace, and dnorm_sum adds up the CTAs.
-// The next row's words are on their way while one is summed.
-template <typename T, int L, int N>
-__global__ void __launch_bounds__(L > NR_NT ? L : NR_NT)
+template <typename T, int L, int N, bool STAGED, bool WHOLE>
+__global__ void __launch_bounds__(L > NR_NT ? L : NR_NT, L > NR_NT ? 1 : 2)
     dnorm_rows(const __grid_constant__ NormArgs a) {
-  using W = RowWord<T>;
-  constexpr int VEC = W::VEC, NT = L > NR_NT ? L : NR_NT, ROWS = NT / L;
+  using W = RowWord<T, L, WHOLE>;
+  constexpr int VEC = W::VEC, H = VEC / 2, NT = L > NR_NT ? L : NR_NT, ROWS = NT / L;
+  extern __shared__ __align__(16) unsigned char nm_raw[];
   __shared__ float2 part[2][32];
-  __shared__ float columns[ROWS > 1 ? NT * N * VEC : 1];
+  const int in_row = threadIdx.x % L, group = threadIdx.x / L;
+  const int d = (int)a.d;
+  const bool wide = a.wide_w, res = a.res && a.y, res_staged = res && a.stage_res;
+  const int w_bytes = nm_weight_bytes(d, wide);
+  const int64_t step = (int64_t)gridDim.x * ROWS, first = (int64_t)blockIdx.x * ROWS;
+  auto x_of = [&](int64_t row) { return reinterpret_cast<const T*>(a.x) + row * a.x_stride; };
+  auto dy_of = [&](int64_t row) { return reinterpret_cast<const T*>(a.dy) + row * a.dy_stride; };
+  auto res_of = [&](int64_t row) { return reinterpret_cast<const T*>(a.res) + row * a.res_stride; };
+  RowStages<T, L> st(nm_raw + w_bytes, a, res_staged ? 3 : 2);
+  auto fill = [&](int i, int64_t row) {
+    st.expect(i, st.size(x_of(row)) + st.size(dy_of(row)) + (res_staged ? st.size(res_of(row)) : 0u));
+    st.copy(i, 0, x_of(row));
+    st.copy(i, 1, dy_of(row));
+    if (res_staged) st.copy(i, 2, res_of(row));
+  };
+  if (STAGED) {
+    st.init();
+    __syncthreads();
+  }
   pdl_wait();
   pdl_trigger();
-  const int in_row = threadIdx.x % L, group = threadIdx.x / L;
-  const int64_t d = a.d;
-  const bool vec = a.vec, vec_w = a.vec_w, wide = a.wide_w, sums = a.part != nullptr;
-  float cw[N][VEC], cb[N][VEC];
+  if (STAGED && in_row == 0)
+    for (int i = 0; i < a.stages; ++i)
+      if (first + group + i * step < a.n_rows) fill(i, first + group + i * step);
+  nm_keep(nm_raw, a.w, wide, a.vec_w, d);
+  __syncthreads();
+  W cw[N], cb[N];
 #pragma unroll
   for (int i = 0; i < N; ++i)
 #pragma unroll
-    for (int j = 0; j < VEC; ++j) cw[i][j] = cb[i][j] = 0.f;
-  struct Row {
-    uint4 x[N], dy[N];
-    float m, rstd;
+    for (int j = 0; j < H; ++j) cw[i].f[j] = cb[i].f[j] = make_float2(0.f, 0.f);
+  auto moments = [&](int64_t row) {
+    return row < a.n_rows ? make_float2(a.rms ? 0.f : __ldcg(a.mean + row), __ldcg(a.rstd + row))
+                          : make_float2(0.f, 0.f);
   };
-  auto fetch = [&](int64_t row) {
-    Row r;
-    const bool on = row < a.n_rows;
-    const T* x = reinterpret_cast<const T*>(a.x) + row * a.x_stride;
-    const T* dy = reinterpret_cast<const T*>(a.dy) + row * a.dy_stride;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int64_t at = in_row + (int64_t)i * L;
-      r.x[i] = on ? W::load(x, at, d, vec) : make_uint4(0u, 0u, 0u, 0u);
-      r.dy[i] = on ? W::load(dy, at, d, vec) : make_uint4(0u, 0u, 0u, 0u);
-    }
-    r.m = on && !a.rms ? __ldcg(a.mean + row) : 0.f;
-    r.rstd = on ? __ldcg(a.rstd + row) : 0.f;
-    return r;
-  };
-  const int64_t step = (int64_t)gridDim.x * ROWS;
-  int64_t r0 = (int64_t)blockIdx.x * ROWS;
-  int turn = 0;
-  Row r = fetch(r0 + group);
-  for (; r0 < a.n_rows; r0 += step, turn ^= 1) {
+  int turn = 0, free_place = -1;  // the place of the row before this one
+  float2 mo = moments(first + group);
+  for (int64_t r0 = first; r0 < a.n_rows; r0 += step, turn ^= 1) {
     const int64_t row = r0 + group;
     const bool on = row < a.n_rows;
-    const Row next = fetch(row + step);
-    uint4 t[N];
-    if (a.res && a.y) {
-      const T* res = reinterpret_cast<const T*>(a.res) + row * a.res_stride;
-#pragma unroll
-      for (int i = 0; i < N; ++i)
-        t[i] = on ? W::load(res, in_row + (int64_t)i * L, d, vec) : make_uint4(0u, 0u, 0u, 0u);
-    }
-    float2 s = make_float2(0.f, 0.f);
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int64_t at = in_row + (int64_t)i * L;
-      float w[VEC];
-      W::weights(a.w, wide, vec_w, at, d, w);
-#pragma unroll
-      for (int j = 0; j < VEC; ++j) {
-        const float dy = W::at(r.dy[i], j), hat = (W::at(r.x[i], j) - r.m) * r.rstd, g = dy * w[j];
-        // (past the row's end dy and w are 0)
-        s.x += g;
-        s.y = fmaf(g, hat, s.y);
-        cw[i][j] = fmaf(dy, hat, cw[i][j]);
-        cb[i][j] += dy;
+    const float2 next = moments(row + step);
+    const T *x = x_of(row), *dy = dy_of(row), *t = res_of(row);
+    float2 s1 = make_float2(0.f, 0.f), s2 = make_float2(0.f, 0.f);
+    if (on) {
+      if (STAGED) {
+        st.wait();
+        x = st.here(0, x);
+        dy = st.here(1, dy);
+        if (res_staged) t = st.here(2, t);
       }
-    }
-    if (a.y) {
-      s = nm_row_sum<L>(s, part, turn);
-      const float s1 = a.rms ? 0.f : s.x * a.inv_d, s2 = s.y * a.inv_d;
-      if (on) {
-        T* dx = reinterpret_cast<T*>(a.y) + row * a.y_stride;
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-          const int64_t at = in_row + (int64_t)i * L;
-          if (at * VEC >= d) continue;
-          float w[VEC], f[VEC];
-          W::weights(a.w, wide, vec_w, at, d, w);
+      for (int i = 0; i < N; ++i) {
+        W xv, dv, w;
+        xv.load(x, in_row, i, d);
+        dv.load(dy, in_row, i, d);
+        w.weights(nm_raw, wide, in_row, i, d);
 #pragma unroll
-          for (int j = 0; j < VEC; ++j) {
-            const float hat = (W::at(r.x[i], j) - r.m) * r.rstd;
-            f[j] = r.rstd * (W::at(r.dy[i], j) * w[j] - s1 - hat * s2);
-            if (a.res) f[j] += W::at(t[i], j);
-          }
-          W::store(dx, at, d, vec, f);
+        for (int j = 0; j < H; ++j) {  // (past the row's end dy and w are 0)
+          const float2 hat = __fmul2_rn(__fadd2_rn(xv.f[j], nm_both(-mo.x)), nm_both(mo.y));
+          const float2 g = __fmul2_rn(dv.f[j], w.f[j]);
+          s1 = __fadd2_rn(s1, g);
+          s2 = __ffma2_rn(g, hat, s2);
+          cw[i].f[j] = __ffma2_rn(dv.f[j], hat, cw[i].f[j]);
+          cb[i].f[j] = __fadd2_rn(cb[i].f[j], dv.f[j]);
         }
       }
     }
-    r = next;
+    const float2 s = nm_row_sum<L>(make_float2(s1.x + s1.y, s2.x + s2.y), part, turn);
+    if (STAGED) {  // every thread is past the row before
+      if (in_row == 0 && free_place >= 0 && row + (a.stages - 1) * step < a.n_rows)
+        fill(free_place, row + (a.stages - 1) * step);
+      free_place = st.place;
+      st.step();
+    }
+    if (a.y && on) {
+      const float m1 = a.rms ? 0.f : s.x * a.inv_d, m2 = s.y * a.inv_d;
+      T* dx = reinterpret_cast<T*>(a.y) + row * a.y_stride;
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        if (!W::some(in_row, i, d)) continue;
+        W xv, dv, w, tv;
+        xv.load(x, in_row, i, d);
+        dv.load(dy, in_row, i, d);
+        w.weights(nm_raw, wide, in_row, i, d);
+#pragma unroll
+        for (int j = 0; j < H; ++j) tv.f[j] = make_float2(0.f, 0.f);
+        if (res) tv.load(t, in_row, i, d);
+#pragma unroll
+        for (int j = 0; j < H; ++j) {
+          const float2 hat = __fmul2_rn(__fadd2_rn(xv.f[j], nm_both(-mo.x)), nm_both(mo.y));
+          const float2 g = __fadd2_rn(__fmul2_rn(dv.f[j], w.f[j]), nm_both(-m1));
+          xv.f[j] = __ffma2_rn(__ffma2_rn(hat, nm_both(-m2), g), nm_both(mo.y), tv.f[j]);
+        }
+        xv.store(dx, in_row, i, d);
+      }
+    }
+    mo = next;
   }
-  if (!sums) return;
+  if (!a.part) return;
+  float* const columns = reinterpret_cast<float*>(nm_raw);  // (ROWS > 1: [ROWS][L N VEC])
 #pragma unroll
   for (int which = 0; which < 2; ++which) {
-    float* to = a.part + ((int64_t)blockIdx.x * 2 + which) * d;
+    float* to = a.part + ((int64_t)blockIdx.x * 2 + which) * a.d;
     if constexpr (ROWS > 1) {
       __syncthreads();
 #pragma unroll
       for (int i = 0; i < N; ++i)
 #pragma unroll
         for (int j = 0; j < VEC; ++j)
-          columns[(group * N * L + i * L + in_row) * VEC + j] = which ? cb[i][j] : cw[i][j];
+          columns[group * N * L * VEC + W::column(in_row, i, j)] =
+              which ? cb[i].get(j) : cw[i].get(j);
       __syncthreads();
       for (int c = threadIdx.x; c < L * N * VEC && c < d; c += NT) {
         float v = 0.f;
@@ -377,15 +541,15 @@ __global__ void __launch_bounds__(L > NR_NT ? L : NR_NT)
       for (int i = 0; i < N; ++i)
 #pragma unroll
         for (int j = 0; j < VEC; ++j) {
-          const int64_t c = (in_row + (int64_t)i * L) * VEC + j;
-          if (c < d) to[c] = which ? cb[i][j] : cw[i][j];
+          const int c = W::column(in_row, i, j);
+          if (c < d) to[c] = which ? cb[i].get(j) : cw[i].get(j);
         }
     }
   }
 }
 
-// The gradients of the weights from the CTAs' sums: 32 columns a CTA, each warp every eighth of them
-constexpr int NS_NT = 256;
+// The gradients of the weights from the CTAs' sums: 32 columns a CTA, each warp every 32nd of them
+constexpr int NS_NT = 1024;
 static __global__ void __launch_bounds__(NS_NT) dnorm_sum(const __grid_constant__ NormArgs a, const int ctas) {
   __shared__ float part[NS_NT / 32][32];
   pdl_wait();
@@ -397,7 +561,7 @@ static __global__ void __launch_bounds__(NS_NT) dnorm_sum(const __grid_constant_
   float v = 0.f;
   if (c < a.d) {
     const float* p = a.part + which * a.d + c;
-#pragma unroll 4
+#pragma unroll 10
     for (int i = warp; i < ctas; i += NS_NT / 32) v += __ldcg(p + (int64_t)i * 2 * a.d);
   }
   part[warp][lane] = v;

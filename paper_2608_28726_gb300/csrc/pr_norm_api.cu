@@ -29,17 +29,17 @@ bool same_rows(const void* out, int64_t out_stride, const void* in, int64_t in_s
 bool on_words(const void* p, int64_t stride, pr_dtype dt) {
   return !p || (aligned16(p) && stride * (int64_t)esize(dt) % 16 == 0);
 }
-// eight weights of fp32, or of bf16, are read as words of 16 or 8 bytes
-bool weights_on_words(const void* p) { return aligned16(p); }
-
-// What has a row in registers: threads and words of each.
+// The kernel for rows of so many words, [of whole ones on the grid], and whether it stages them; threads of a
+// row, words of each.
 struct NormShape {
-  const void* kernel;
-  int threads;  // of a row
+  const void* kernel[2];
+  bool staged;
+  int threads, words;
 };
 template <typename T, int L, int N>
 NormShape forward_shape() {
-  return {reinterpret_cast<const void*>(&prk::norm_rows<T, L, N>), L};
+  return {{reinterpret_cast<const void*>(&prk::norm_rows<T, L, N, (L > 8), false>),
+           reinterpret_cast<const void*>(&prk::norm_rows<T, L, N, (L > 8), true>)}, L > 8, L, N};
 }
 template <typename T>
 NormShape forward_of(int64_t words) {
@@ -48,30 +48,64 @@ NormShape forward_of(int64_t words) {
   if (words <= 128) return forward_shape<T, 32, 4>();
   if (words <= 256) return forward_shape<T, 128, 2>();
   if (words <= 512) return forward_shape<T, 128, 4>();
-  if (words <= 1024) return forward_shape<T, 512, 2>();
+  if (words <= 1024) return forward_shape<T, 256, 4>();
   if (words <= 2048) return forward_shape<T, 512, 4>();
-  return {nullptr, 0};
+  return {{nullptr, nullptr}, false, 0, 0};
 }
 template <typename T, int L, int N>
 NormShape backward_shape() {
-  return {reinterpret_cast<const void*>(&prk::dnorm_rows<T, L, N>), L};
+  return {{reinterpret_cast<const void*>(&prk::dnorm_rows<T, L, N, (L > 8), false>),
+           reinterpret_cast<const void*>(&prk::dnorm_rows<T, L, N, (L > 8), true>)}, L > 8, L, N};
 }
 template <typename T>
 NormShape backward_of(int64_t words) {
   if (words <= 16) return backward_shape<T, 8, 2>();
   if (words <= 64) return backward_shape<T, 32, 2>();
+  if (words <= 128) return backward_shape<T, 64, 2>();
   if (words <= 256) return backward_shape<T, 128, 2>();
   if (words <= 512) return backward_shape<T, 256, 2>();
   if (words <= 1024) return backward_shape<T, 512, 2>();
   if (words <= 2048) return backward_shape<T, 512, 4>();
-  return {nullptr, 0};
+  return {{nullptr, nullptr}, 0, 0, 0};
 }
 
-pr_status launch(pr_ctx* c, const void* kernel, dim3 grid, unsigned threads, void** args, cudaStream_t s) {
+constexpr int NORM_STAGES = 4;  // at most
+constexpr size_t NORM_ROOM = 220 * 1024;
+// The shared memory of a CTA, `ctas` of which are to be on an SM: the weights (`weights` arrays), and
+// places for k rows, at least `least`.  Returns whether it fits.
+bool stage(prk::NormArgs& a, const NormShape& shape, pr_dtype dt, int ctas, int k, int weights, int least,
+           size_t& smem) {
+  a.row_bytes = (int32_t)((a.d * (int64_t)esize(dt) + 30) / 16 * 16);  // wherever a row begins
+  a.stages = 0;
+  smem = (size_t)weights * ((a.d + 7) / 8 * 8) * (a.wide_w ? 4 : 2);
+  if (!shape.staged) return true;
+  const int groups = std::max(shape.threads, prk::NR_NT) / shape.threads;
+  const size_t room = NORM_ROOM / ctas - 128, place = (size_t)groups * k * a.row_bytes;
+  if (room < smem + least * place) return false;
+  a.stages = (int)std::min<size_t>(NORM_STAGES, (room - smem) / place);
+  smem += (size_t)(groups * a.stages * 8 + 127) / 128 * 128 + a.stages * place;
+  return true;
+}
+
+// shared memory opt-ins, once per context
+pr_status setup(pr_ctx* c) {
+  if (c->norm_ready) return PR_OK;
+  for (int64_t words = 16; words <= 2048; words *= 2)
+    for (const NormShape& s : {forward_of<float>(words), forward_of<__nv_bfloat16>(words),
+                               backward_of<float>(words), backward_of<__nv_bfloat16>(words)})
+      for (const void* kernel : s.kernel)
+        PR_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)NORM_ROOM));
+  c->norm_ready = true;
+  return PR_OK;
+}
+
+pr_status launch(pr_ctx* c, const void* kernel, dim3 grid, unsigned threads, size_t smem, void** args,
+                 cudaStream_t s) {
   cudaLaunchConfig_t cfg;
   memset(&cfg, 0, sizeof cfg);
   cfg.gridDim = grid;
   cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
   cfg.stream = s;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -136,16 +170,26 @@ pr_status pr_layernorm(pr_ctx* c, const void* x, pr_dtype dt, int64_t n_rows, in
   a.inv_d = (float)(1.0 / (double)d);
   a.rms = rms ? 1 : 0;
   a.wide_w = wdt == PR_DTYPE_F32;
-  a.vec = on_words(x, x_stride, dt) && on_words(residual, residual_stride, dt) &&
-          on_words(total, total_stride, dt) && on_words(y, y_stride, dt);
-  a.vec_w = weights_on_words(weight) && weights_on_words(bias);
+  a.vec_w = aligned16(weight) && aligned16(bias);
+  a.ctx_flags = c->flags;
+  const bool whole = d * (int64_t)esize(dt) % 16 == 0 && on_words(x, x_stride, dt) &&
+                     on_words(residual, residual_stride, dt) && on_words(total, total_stride, dt) &&
+                     on_words(y, y_stride, dt);
   const int64_t words = (d * (int64_t)esize(dt) + 15) / 16;
   const NormShape shape = dt == PR_DTYPE_BF16 ? forward_of<__nv_bfloat16>(words) : forward_of<float>(words);
-  if (shape.kernel) {
+  if (shape.threads) {
+    if ((st = setup(c)) != PR_OK) return st;
     const int threads = std::max(shape.threads, prk::NR_NT), rows = threads / shape.threads;
-    const int64_t grid = std::min<int64_t>((n_rows + rows - 1) / rows, (int64_t)c->num_sms * 2048 / threads);
-    void* args[] = {&a};
-    return launch(c, shape.kernel, dim3((unsigned)grid), (unsigned)threads, args, s);
+    const int k = residual ? 2 : 1, weights = bias ? 2 : 1;
+    int ctas = threads > prk::NR_NT ? 1 : 3;
+    size_t smem = 0;
+    while (ctas > 1 && !stage(a, shape, dt, ctas, k, weights, 2, smem)) --ctas;
+    if (ctas > 1 || stage(a, shape, dt, 1, k, weights, 1, smem)) {
+      if (!shape.staged) ctas = 2048 / threads;
+      const int64_t grid = std::min<int64_t>((n_rows + rows - 1) / rows, (int64_t)c->num_sms * ctas);
+      void* args[] = {&a};
+      return launch(c, shape.kernel[whole], dim3((unsigned)grid), (unsigned)threads, smem, args, s);
+    }
   }
   if (dt == PR_DTYPE_BF16)
     prk::norm_wide<__nv_bfloat16><<<(unsigned)n_rows, prk::NW_NT, 0, s>>>(a);
@@ -201,25 +245,40 @@ pr_status pr_layernorm_backward(pr_ctx* c, const void* dy, int64_t dy_stride, co
   a.rms = rms ? 1 : 0;
   a.wide_w = wdt == PR_DTYPE_F32;
   a.accumulate = accumulate ? 1 : 0;
-  a.vec = on_words(x, x_stride, dt) && on_words(dy, dy_stride, dt) && on_words(dtotal, dtotal_stride, dt) &&
-          on_words(dx, dx_stride, dt);
-  a.vec_w = weights_on_words(weight);
+  a.vec_w = aligned16(weight);
+  a.ctx_flags = c->flags;
+  const bool whole = d * (int64_t)esize(dt) % 16 == 0 && on_words(x, x_stride, dt) && on_words(dy, dy_stride, dt) &&
+                     on_words(dtotal, dtotal_stride, dt) && on_words(dx, dx_stride, dt);
   const int64_t words = (d * (int64_t)esize(dt) + 15) / 16;
   const NormShape shape = dt == PR_DTYPE_BF16 ? backward_of<__nv_bfloat16>(words) : backward_of<float>(words);
-  if (shape.kernel) {
+  if (shape.threads) {
+    if ((st = setup(c)) != PR_OK) return st;
     const int threads = std::max(shape.threads, prk::NR_NT), rows = threads / shape.threads;
-    const int64_t grid = std::min<int64_t>((n_rows + rows - 1) / rows, (int64_t)c->num_sms * 512 / threads);
-    if (dweight || dbias) {
-      if ((st = grow(c->norm_ws, (size_t)grid * 2 * d * sizeof(float), false)) != PR_OK) return st;
-      a.part = static_cast<float*>(c->norm_ws.p);
+    int ctas = threads > prk::NR_NT ? 1 : 2;
+    size_t smem = 0;
+    // Places for three rows each decide how many CTAs an SM has, whether dtotal is there or not: the order
+    // of the columns' sums is to depend on the sizes alone.  (A place is filled again a row later: two at
+    // least.)  Where three rows do not fit dtotal is read by its threads.
+    while (ctas > 1 && !stage(a, shape, dt, ctas, 3, 1, 2, smem)) --ctas;
+    a.stage_res = dtotal && dx && stage(a, shape, dt, ctas, 3, 1, 2, smem);
+    const bool fits = stage(a, shape, dt, ctas, a.stage_res ? 3 : 2, 1, 2, smem);
+    if (fits) {
+      const int64_t grid = std::min<int64_t>((n_rows + rows - 1) / rows, (int64_t)c->num_sms * ctas);
+      if (dweight || dbias) {
+        if ((st = grow(c->norm_ws, (size_t)grid * 2 * d * sizeof(float), false)) != PR_OK) return st;
+        a.part = static_cast<float*>(c->norm_ws.p);
+        if (rows > 1)  // the rows' columns, added up at the end
+          smem = std::max(smem, (size_t)threads * shape.words * (16 / esize(dt)) * sizeof(float));
+      }
+      void* args[] = {&a};
+      if ((st = launch(c, shape.kernel[whole], dim3((unsigned)grid), (unsigned)threads, smem, args, s)) != PR_OK)
+        return st;
+      if (!a.part) return PR_OK;
+      int parts = (int)grid;
+      void* sum_args[] = {&a, &parts};
+      return launch(c, reinterpret_cast<const void*>(&prk::dnorm_sum), dim3((unsigned)((d + 31) / 32), 2),
+                    prk::NS_NT, 0, sum_args, s);
     }
-    void* args[] = {&a};
-    if ((st = launch(c, shape.kernel, dim3((unsigned)grid), (unsigned)threads, args, s)) != PR_OK) return st;
-    if (!a.part) return PR_OK;
-    int ctas = (int)grid;
-    void* sum_args[] = {&a, &ctas};
-    return launch(c, reinterpret_cast<const void*>(&prk::dnorm_sum), dim3((unsigned)((d + 31) / 32), 2),
-                  prk::NS_NT, sum_args, s);
   }
   if (dweight || dbias) {  // first: dx may be written over dy and x
     const unsigned grid = (unsigned)((d + 31) / 32);
