@@ -811,23 +811,32 @@ def _norm_rows(call, dev, name, t, like=None):
     if t is None:
         return None, 0
     _dev(call, dev, name, t, _ROWS_T if like is None else (like.dtype,), contiguous=False)
-    if t.dim() != 2 or t.shape[1] < 1 or (like is not None and t.shape != like.shape):
+    shape = t.shape
+    if len(shape) != 2 or shape[1] < 1 or (like is not None and shape != like.shape):
         raise PRError(PR_ERR_INVALID_ARG, call, "%s must be 2-D%s" % (
             name, "" if like is None else ", %s" % list(like.shape)))
-    d = t.shape[1]
-    if (d > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < d):
+    n, d = shape
+    strides = t.stride()
+    if (d > 1 and strides[1] != 1) or (n > 1 and strides[0] < d):
         raise PRError(PR_ERR_INVALID_ARG, call, "%s must have unit stride along its rows, which "
                       "must not overlap" % name)
-    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else d
+    return t.data_ptr(), strides[0] if n > 1 else d
+
+
+def _norm_out(call, dev, name, t, like):
+    """The same of an output, made where the caller has none: (tensor, address, stride)."""
+    if t is None:
+        t = torch.empty(like.shape, dtype=like.dtype, device=like.device)
+        return t, t.data_ptr(), like.shape[1]
+    return (t, *_norm_rows(call, dev, name, t, like))
 
 
 def _norm_weights(call, dev, d, weight, bias=None):
     w = _dptr(call, dev, "weight", weight, _ROWS_T, d)
     b = _dptr_opt(call, dev, "bias", bias, (weight.dtype,), d)
-    for name, t in (("weight", weight), ("bias", bias)):
-        if t is not None and t.numel() != d:
-            raise PRError(PR_ERR_INVALID_ARG, call, "%s holds %d elements for rows of %d" % (
-                name, t.numel(), d))
+    if weight.numel() != d or (bias is not None and bias.numel() != d):
+        raise PRError(PR_ERR_INVALID_ARG, call, "weight and bias must hold one element for each of the "
+                      "%d columns" % d)
     return w, b, _dtype(weight)
 
 
@@ -846,17 +855,15 @@ def pr_layernorm(ctx, x, weight, bias=None, residual=None, eps: float = 1e-5, rm
     n, d = x.shape
     w_p, b_p, wdt = _norm_weights(call, dev, d, weight, bias)
     r_p, rs = _norm_rows(call, dev, "residual", residual, x)
-    if y is None:
-        y = torch.empty(n, d, dtype=x.dtype, device=x.device)
-    if total is None and residual is not None and want_total:
-        total = torch.empty(n, d, dtype=x.dtype, device=x.device)
-    if want_stats:
-        mean = torch.empty(n, dtype=torch.float32, device=x.device) if mean is None and not rms else mean
-        rstd = torch.empty(n, dtype=torch.float32, device=x.device) if rstd is None else rstd
-    y_p, ys = _norm_rows(call, dev, "y", y, x)
-    t_p, ts = _norm_rows(call, dev, "total", total, x)
-    mean_p = _dptr_opt(call, dev, "mean", mean, _F32_T, n)
-    rstd_p = _dptr_opt(call, dev, "rstd", rstd, _F32_T, n)
+    y, y_p, ys = _norm_out(call, dev, "y", y, x)
+    t_p, ts = None, 0
+    if total is not None or (residual is not None and want_total):
+        total, t_p, ts = _norm_out(call, dev, "total", total, x)
+    mean_p = rstd_p = None
+    if mean is not None or (want_stats and not rms):
+        mean, mean_p = _loss_out(call, dev, "mean", mean, n, x.device)
+    if rstd is not None or want_stats:
+        rstd, rstd_p = _loss_out(call, dev, "rstd", rstd, n, x.device)
     _check(_lib.pr_layernorm(ctx, x_p, _dtype(x), n, d, xs, r_p, rs, w_p, b_p, wdt, eps, bool(rms),
                              t_p, ts, y_p, ys, mean_p, rstd_p, _stream(stream)), call)
     return y, total, mean, rstd
@@ -885,15 +892,13 @@ def pr_layernorm_backward(ctx, dy, x, weight, rstd, mean=None, dtotal=None, rms:
     mean_p = None if rms else _dptr(call, dev, "mean", mean, _F32_T, n)
     if accumulate and ((want_dweight and dweight is None) or (want_dbias and dbias is None)):
         raise PRError(PR_ERR_INVALID_ARG, call, "accumulate needs dweight, and dbias where wanted")
-    if dx is None and want_dx:
-        dx = torch.empty(n, d, dtype=x.dtype, device=x.device)
-    if dweight is None and want_dweight:
-        dweight = torch.empty(d, dtype=torch.float32, device=x.device)
-    if dbias is None and want_dbias:
-        dbias = torch.empty(d, dtype=torch.float32, device=x.device)
-    dx_p, dxs = _norm_rows(call, dev, "dx", dx, x)
-    dw_p = _dptr_opt(call, dev, "dweight", dweight, _F32_T, d)
-    db_p = _dptr_opt(call, dev, "dbias", dbias, _F32_T, d)
+    dx_p, dxs, dw_p, db_p = None, 0, None, None
+    if dx is not None or want_dx:
+        dx, dx_p, dxs = _norm_out(call, dev, "dx", dx, x)
+    if dweight is not None or want_dweight:
+        dweight, dw_p = _loss_out(call, dev, "dweight", dweight, d, x.device)
+    if dbias is not None or want_dbias:
+        dbias, db_p = _loss_out(call, dev, "dbias", dbias, d, x.device)
     _check(_lib.pr_layernorm_backward(ctx, dy_p, dys, x_p, xs, _dtype(x), n, d, w_p, wdt, mean_p,
                                       rstd_p, bool(rms), t_p, ts, dx_p, dxs, dw_p, db_p,
                                       bool(accumulate), _stream(stream)), call)

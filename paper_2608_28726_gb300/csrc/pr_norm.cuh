@@ -522,28 +522,32 @@ __global__ void __launch_bounds__(L > NR_NT ? L : NR_NT, L > NR_NT ? 1 : 2)
 #pragma unroll
   for (int which = 0; which < 2; ++which) {
     float* to = a.part + ((int64_t)blockIdx.x * 2 + which) * a.d;
-    if constexpr (ROWS > 1) {
-      __syncthreads();
+    float* const at = ROWS > 1 ? columns + group * N * L * VEC : to;
+    if (ROWS > 1) __syncthreads();
 #pragma unroll
-      for (int i = 0; i < N; ++i)
+    for (int i = 0; i < N; ++i) {
+      const W& v = which ? cb[i] : cw[i];
+      if constexpr (WHOLE) {
+        // (four columns at once: one by one a warp's stores would lie 32 bytes apart)
+        if (ROWS > 1 || W::some(in_row, i, d)) {
+#pragma unroll
+          for (int j = 0; j < VEC; j += 4)
+            *reinterpret_cast<float4*>(at + W::column(in_row, i, j)) =
+                make_float4(v.f[j / 2].x, v.f[j / 2].y, v.f[j / 2 + 1].x, v.f[j / 2 + 1].y);
+        }
+      } else {
 #pragma unroll
         for (int j = 0; j < VEC; ++j)
-          columns[group * N * L * VEC + W::column(in_row, i, j)] =
-              which ? cb[i].get(j) : cw[i].get(j);
+          if (ROWS > 1 || W::column(in_row, i, j) < d) at[W::column(in_row, i, j)] = v.get(j);
+      }
+    }
+    if constexpr (ROWS > 1) {
       __syncthreads();
       for (int c = threadIdx.x; c < L * N * VEC && c < d; c += NT) {
         float v = 0.f;
         for (int g = 0; g < ROWS; ++g) v += columns[g * N * L * VEC + c];
         to[c] = v;
       }
-    } else {
-#pragma unroll
-      for (int i = 0; i < N; ++i)
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) {
-          const int c = W::column(in_row, i, j);
-          if (c < d) to[c] = which ? cb[i].get(j) : cw[i].get(j);
-        }
     }
   }
 }
