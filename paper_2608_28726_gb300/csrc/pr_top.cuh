@@ -583,4 +583,151 @@ __global__ void __launch_bounds__(TR_NT, 3)
   if (C > 1) cluster_sync_all();
 }
 
+// ---- short rows: one to a warp ---------------------------------------------------------------
+//
+// A CTA's choice is a chain of some 10,000 cycles, many times what a short row's data take.  So each warp
+// has a row of its own, brought into its part of shared memory by one bulk copy: a group is a
+// word, the bound is found bit by bit among the lanes' four largest groups each, and the
+// elements that reach it go through a TopList.
+constexpr int TS_MOST = 10;  // warps of a CTA; two CTAs on an SM
+struct TopShort {
+  uint64_t full[TS_MOST];    // a row has landed
+  uint64_t buf[TS_MOST][64];
+};
+constexpr size_t TS_START = (sizeof(TopShort) + 15) / 16 * 16;
+
+template <typename T>
+__global__ void __launch_bounds__(32 * TS_MOST, 2)
+    top_short(const __grid_constant__ LossArgs a, const int k, const float big, int32_t* const out_ids,
+              const int bytes) {  // of a warp's part
+  extern __shared__ __align__(16) unsigned char smem_raw[];
+  TopShort& sm = *reinterpret_cast<TopShort*>(smem_raw);
+  using Tr = Traits<T>;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+  unsigned char* const part = smem_raw + TS_START + (size_t)warp * bytes;
+  uint64_t* const full = &sm.full[warp];
+  if (lane == 0) {
+    bar_init(full, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  __syncwarp();
+  pdl_wait();
+  pdl_trigger();
+  const int64_t G = (int64_t)gridDim.x * warps;
+  uint32_t phase = 0;
+  for (int64_t row = (int64_t)warp * gridDim.x + blockIdx.x; row < a.n_rows; row += G) {
+    const Share sh = share_of<T>(a, row, 1, 0);
+    if (lane == 0) {
+      const uint32_t n = 16u * (uint32_t)sh.words;
+      bar_expect(full, n);
+      if (n > 0)
+        asm volatile(
+            "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::
+                "r"(sm_addr(part)),
+            "l"(sh.x + sizeof(T) * sh.head), "r"(n), "r"(sm_addr(full))
+            : "memory");
+    }
+    const int32_t v_end = end_of(a, sh, lane);
+    const float x_end = v_end >= 0 ? Tr::elem(sh.x, v_end) : -INFINITY;
+    if (!ring_wait(sm_addr(full), phase, a.ctx_flags)) {
+      ring_wait(sm_addr(full), phase, a.ctx_flags);  // no copy may be in flight at the end
+      break;
+    }
+    phase ^= 1u;
+    __syncwarp();
+    const uint4* const st = reinterpret_cast<const uint4*>(part) + lane;
+    // ---- the sum, and the lane's four largest groups
+    float ref = -3e38f, R, t1 = x_end, t2 = -INFINITY, t3 = -INFINITY, t4 = -INFINITY;
+    float2 S = make_float2(0.f, 0.f);
+    for (int32_t w = 0; w < sh.words; w += 32 * TR_W) {
+      uint4 v[TR_W];
+#pragma unroll
+      for (int q = 0; q < TR_W; ++q)
+        v[q] = w + 32 * q + lane < sh.words
+                   ? st[w + 32 * q]
+                   : make_uint4(Tr::NEG_WORD, Tr::NEG_WORD, Tr::NEG_WORD, Tr::NEG_WORD);
+#pragma unroll
+      for (int q = 0; q < TR_W; ++q) {
+        float m = Tr::gmax(v[q]), u = fminf(t1, m);
+        t1 = fmaxf(t1, m);
+        m = u;
+        u = fminf(t2, m);
+        t2 = fmaxf(t2, m);
+        m = u;
+        u = fminf(t3, m);
+        t3 = fmaxf(t3, m);
+        t4 = fmaxf(t4, u);
+      }
+      add_words<T>(ref, S, v, a.c2, w == 0);
+    }
+    join(make_float2(ref, S.x + S.y), 1.f, ref, R);
+    if (sh.head + sh.tail > 0) {
+      const float t = fmaxf(warp_max(x_end * a.c2), -3e38f);
+      if (t > ref) {
+        R *= rescale2(ref - t);
+        ref = t;
+      }
+      R += warp_sum(v_end >= 0 ? ex2(fmaf(x_end, a.c2, -ref)) : 0.f);
+    }
+    int32_t* const ids = out_ids + row * k;
+    float* const logp = a.logp + row * k;
+    const float best = warp_max(t1), K = best * a.c2;
+    if (!(ref < big * a.c2) || !(best > -big) || !(R >= 0.f) || !(R < INFINITY)) {
+      for (int j = lane; j < k; j += 32) {
+        ids[j] = -1;
+        logp[j] = NAN;
+      }
+      if (lane == 0) atomicOr(a.ctx_flags, FLAG_NONFINITE);
+      __syncwarp();
+      continue;
+    }
+    // ---- the bound: the k-th largest of those, from the first bit on
+    const uint32_t o1 = ord(t1), o2 = ord(t2), o3 = ord(t3), o4 = ord(t4);
+    uint32_t reach = 0u;
+#pragma unroll
+    for (int b = 31; b >= (sizeof(T) == 2 ? 16 : 0); --b) {
+      const uint32_t c = reach | 1u << b;
+      const int n = __popc(__ballot_sync(FULL, o1 >= c)) + __popc(__ballot_sync(FULL, o2 >= c)) +
+                    __popc(__ballot_sync(FULL, o3 >= c)) + __popc(__ballot_sync(FULL, o4 >= c));
+      if (n >= k) reach = c;
+    }
+    // (fewer than k finite ones: the bound is below all)
+    const float bound = reach > ord(-big) ? unord(reach) : -big;
+    auto reaches = [&](float x) { return x >= bound && x > -big; };
+    // ---- the elements that reach it
+    TopList l(sm.buf[warp], k);
+    for (int32_t w = 0; w < sh.words; w += 32) {
+      const bool in = w + lane < sh.words;
+      const uint4 q = in ? st[w] : make_uint4(Tr::NEG_WORD, Tr::NEG_WORD, Tr::NEG_WORD, Tr::NEG_WORD);
+      if (!__any_sync(FULL, reaches(Tr::gmax(q)))) continue;
+      uint32_t on = 0u;  // a bit per element
+#pragma unroll
+      for (int j = 0; j < Tr::VEC; ++j) on |= reaches(Tr::at(q, j)) ? 1u << j : 0u;
+      while (__any_sync(FULL, on != 0u)) {
+        const int j = __ffs(on) - 1;
+        float x = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < Tr::VEC; ++i)
+          if (i == j) x = Tr::at(q, i);
+        l.push(on != 0u, top_key(x, (uint32_t)(sh.head + (w + lane) * Tr::VEC + j)), lane);
+        on &= on - 1u;
+      }
+    }
+    if (sh.head + sh.tail > 0) l.push(v_end >= 0 && reaches(x_end), top_key(x_end, (uint32_t)v_end), lane);
+    l.finish(lane);
+    const float log_sum = logf(R * rescale2(ref - K));
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int j = 32 * h + lane;
+      const uint64_t q = h == 0 ? l.hi : l.lo;
+      if (j < k) {
+        ids[j] = q ? (int32_t)key_idx(q) : -1;
+        logp[j] = q ? fmaf(key_val(q), a.c2, -K) * LN2 - log_sum : -INFINITY;
+      }
+    }
+    __syncwarp();  // every lane has read what the next row is written over
+  }
+}
+
 }  // namespace prk

@@ -22,6 +22,11 @@ const void* ring_kernel(pr_dtype dt, bool words) {
   return dt == PR_DTYPE_BF16 ? ring_kernel<__nv_bfloat16>(words) : ring_kernel<float>(words);
 }
 
+const void* short_kernel(pr_dtype dt) {
+  return dt == PR_DTYPE_BF16 ? reinterpret_cast<const void*>(&prk::top_short<__nv_bfloat16>)
+                             : reinterpret_cast<const void*>(&prk::top_short<float>);
+}
+
 // shared memory of one, two or three CTAs on an SM
 constexpr size_t SM_BYTES = 227 * 1024, HALF_BYTES = 113 * 1024, THIRD_BYTES = 75 * 1024;
 
@@ -31,6 +36,15 @@ struct TopShape {
   bool words, fits;
   size_t gm, smem;
 };
+
+// Warps of a CTA of top_short, or 0 where the ring takes less time: with fewer than five rows of
+// a CTA, or no more than two for each CTA of the ring (TOP_SHORT_FIGURE).
+int short_warps(const pr_ctx* c, int64_t n_rows, int64_t vocab, pr_dtype dt) {
+  if (n_rows <= 6 * c->num_sms) return 0;
+  const int64_t part = std::max<int64_t>(16, vocab * (int64_t)esize(dt) / 16 * 16);
+  const int64_t w = std::min<int64_t>(prk::TS_MOST, ((int64_t)HALF_BYTES - (int64_t)prk::TS_START) / part);
+  return w >= 5 ? (int)w : 0;
+}
 
 TopShape choose(const pr_ctx* c, pr_dtype dt, int64_t n_rows, int64_t vocab) {
   const int64_t words = vocab * (int64_t)esize(dt) / 16 + 1;
@@ -87,21 +101,31 @@ pr_status pr_top_logits(pr_ctx* c, const void* logits, pr_dtype dt, int64_t n_ro
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   if ((st = timing_begin(c, s)) != PR_OK || n_rows == 0) return st;
   const float big = (float)(1e9 * (double)temperature);
+  if (!c->top_ready) {
+    for (pr_dtype t : {PR_DTYPE_F32, PR_DTYPE_BF16}) {
+      for (bool words : {false, true})
+        PR_CUDA(cudaFuncSetAttribute(ring_kernel(t, words), cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                     (int)SM_BYTES));
+      PR_CUDA(cudaFuncSetAttribute(short_kernel(t), cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                   (int)HALF_BYTES));
+    }
+    c->top_ready = true;
+  }
+  prk::LossArgs l;
+  fill(l, c, logits, n_rows, vocab, row_stride, nullptr, nullptr, nullptr, 0, nullptr, temperature, 1.f,
+       nullptr, logp, nullptr, 0);
+  int kk = k;
+  float limit = big;
+  int32_t* out = ids;
+  if (const int warps = short_warps(c, n_rows, vocab, dt)) {
+    int part = (int)std::max<int64_t>(16, vocab * (int64_t)esize(dt) / 16 * 16);
+    void* args[] = {&l, &kk, &limit, &out, &part};
+    st = launch(short_kernel(dt), 2 * c->num_sms, 32u * warps, prk::TS_START + (size_t)warps * part, 1, args, s);
+    return st == PR_OK ? timing_mark(c, s) : st;
+  }
   const TopShape shape = choose(c, dt, n_rows, vocab);
   if (shape.fits) {
-    if (!c->top_ready) {
-      for (pr_dtype t : {PR_DTYPE_F32, PR_DTYPE_BF16})
-        for (bool words : {false, true})
-          PR_CUDA(cudaFuncSetAttribute(ring_kernel(t, words), cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                       (int)SM_BYTES));
-      c->top_ready = true;
-    }
-    prk::LossArgs l;
-    fill(l, c, logits, n_rows, vocab, row_stride, nullptr, nullptr, nullptr, 0, nullptr, temperature, 1.f,
-         nullptr, logp, nullptr, 0);
-    int kk = k, places = shape.places, gm = (int)shape.gm;
-    float limit = big;
-    int32_t* out = ids;
+    int places = shape.places, gm = (int)shape.gm;
     const int64_t at_once = (int64_t)shape.on_sm * c->num_sms;
     const int64_t groups = std::min<int64_t>(n_rows, std::max<int64_t>(1, at_once / shape.cluster));
     void* args[] = {&l, &kk, &limit, &out, &places, &gm};
