@@ -33,7 +33,7 @@ struct NormArgs {
   int32_t vec_w;        // the weights begin at multiples of 16 bytes
   int32_t stages;       // rows of a group on their way into shared memory
   int32_t row_bytes;    // room of one there
-  int32_t stage_res;    // backward: dtotal's, too (else its threads read it)
+  int32_t stage_res;    // the residual's (dtotal's), too; else its threads read it
   float* part;          // workspace: [CTAs][2][d] sums of dy xhat and of dy
   uint32_t* ctx_flags;
 };
@@ -296,11 +296,12 @@ __global__ void __launch_bounds__(L > NR_NT ? L : NR_NT, L > NR_NT ? 1 : 3)
   const int64_t step = (int64_t)gridDim.x * rows, first = (int64_t)blockIdx.x * rows;
   auto x_of = [&](int64_t row) { return reinterpret_cast<const T*>(a.x) + row * a.x_stride; };
   auto res_of = [&](int64_t row) { return reinterpret_cast<const T*>(a.res) + row * a.res_stride; };
-  RowStages<T, L> st(nm_raw + (a.b ? 2 : 1) * w_bytes, a, res ? 2 : 1);
+  const bool res_staged = res && a.stage_res;
+  RowStages<T, L> st(nm_raw + (a.b ? 2 : 1) * w_bytes, a, res_staged ? 2 : 1);
   auto fill = [&](int i, int64_t row) {
-    st.expect(i, st.size(x_of(row)) + (res ? st.size(res_of(row)) : 0u));
+    st.expect(i, st.size(x_of(row)) + (res_staged ? st.size(res_of(row)) : 0u));
     st.copy(i, 0, x_of(row));
-    if (res) st.copy(i, 1, res_of(row));
+    if (res_staged) st.copy(i, 1, res_of(row));
   };
   if (STAGED) {
     st.init();
@@ -326,7 +327,7 @@ __global__ void __launch_bounds__(L > NR_NT ? L : NR_NT, L > NR_NT ? 1 : 3)
       if (STAGED) {
         st.wait();
         x = st.here(0, x);
-        r = st.here(1, r);
+        if (res_staged) r = st.here(1, r);
       }
 #pragma unroll
       for (int i = 0; i < N; ++i) h[i].load(x, in_row, i, d);
@@ -487,7 +488,8 @@ __global__ void __launch_bounds__(L > NR_NT ? L : NR_NT, L > NR_NT ? 1 : 2)
       }
     }
     const float2 s = nm_row_sum<L>(make_float2(s1.x + s1.y, s2.x + s2.y), part, turn);
-    if (STAGED) {  // every thread is past the row before
+    const bool alone = N == 8 && a.stages == 1;  // (rows of up to 64 KB: one place)
+    if (STAGED && !alone) {  // every thread is past the row before
       if (in_row == 0 && free_place >= 0 && row + (a.stages - 1) * step < a.n_rows)
         fill(free_place, row + (a.stages - 1) * step);
       free_place = st.place;
@@ -514,6 +516,11 @@ __global__ void __launch_bounds__(L > NR_NT ? L : NR_NT, L > NR_NT ? 1 : 2)
         }
         xv.store(dx, in_row, i, d);
       }
+    }
+    if (STAGED && alone) {  // filled when every thread is past this row
+      nm_row_sum<L>(make_float2(0.f, 0.f), part, turn ^ 1);
+      if (in_row == 0 && row + step < a.n_rows) fill(0, row + step);
+      st.step();
     }
     mo = next;
   }

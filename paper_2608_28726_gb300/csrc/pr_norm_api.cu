@@ -50,6 +50,7 @@ NormShape forward_of(int64_t words) {
   if (words <= 512) return forward_shape<T, 128, 4>();
   if (words <= 1024) return forward_shape<T, 256, 4>();
   if (words <= 2048) return forward_shape<T, 512, 4>();
+  if (sizeof(T) == 4 && words <= 4096) return forward_shape<T, 512, 8>();
   return {{nullptr, nullptr}, false, 0, 0};
 }
 template <typename T, int L, int N>
@@ -66,7 +67,8 @@ NormShape backward_of(int64_t words) {
   if (words <= 512) return backward_shape<T, 256, 2>();
   if (words <= 1024) return backward_shape<T, 512, 2>();
   if (words <= 2048) return backward_shape<T, 512, 4>();
-  return {{nullptr, nullptr}, 0, 0, 0};
+  if (sizeof(T) == 4 && words <= 4096) return backward_shape<T, 512, 8>();
+  return {{nullptr, nullptr}, false, 0, 0};
 }
 
 constexpr int NORM_STAGES = 4;  // at most
@@ -90,11 +92,11 @@ bool stage(prk::NormArgs& a, const NormShape& shape, pr_dtype dt, int ctas, int 
 // shared memory opt-ins, once per context
 pr_status setup(pr_ctx* c) {
   if (c->norm_ready) return PR_OK;
-  for (int64_t words = 16; words <= 2048; words *= 2)
+  for (int64_t words = 16; words <= 4096; words *= 2)
     for (const NormShape& s : {forward_of<float>(words), forward_of<__nv_bfloat16>(words),
                                backward_of<float>(words), backward_of<__nv_bfloat16>(words)})
       for (const void* kernel : s.kernel)
-        PR_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)NORM_ROOM));
+        if (kernel) PR_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)NORM_ROOM));
   c->norm_ready = true;
   return PR_OK;
 }
@@ -183,8 +185,14 @@ pr_status pr_layernorm(pr_ctx* c, const void* x, pr_dtype dt, int64_t n_rows, in
     const int k = residual ? 2 : 1, weights = bias ? 2 : 1;
     int ctas = threads > prk::NR_NT ? 1 : 3;
     size_t smem = 0;
+    a.stage_res = residual != nullptr;
     while (ctas > 1 && !stage(a, shape, dt, ctas, k, weights, 2, smem)) --ctas;
-    if (ctas > 1 || stage(a, shape, dt, 1, k, weights, 1, smem)) {
+    bool fits = ctas > 1 || stage(a, shape, dt, 1, k, weights, 1, smem);
+    if (!fits && residual) {
+      a.stage_res = 0;
+      fits = stage(a, shape, dt, 1, 1, weights, 1, smem);
+    }
+    if (fits) {
       if (!shape.staged) ctas = 2048 / threads;
       const int64_t grid = std::min<int64_t>((n_rows + rows - 1) / rows, (int64_t)c->num_sms * ctas);
       void* args[] = {&a};
@@ -257,11 +265,12 @@ pr_status pr_layernorm_backward(pr_ctx* c, const void* dy, int64_t dy_stride, co
     int ctas = threads > prk::NR_NT ? 1 : 2;
     size_t smem = 0;
     // Places for three rows each decide how many CTAs an SM has, whether dtotal is there or not: the order
-    // of the columns' sums is to depend on the sizes alone.  (A place is filled again a row later: two at
-    // least.)  Where three rows do not fit dtotal is read by its threads.
+    // of the columns' sums is to depend on the sizes alone.  Two places at least, as one is filled again a
+    // row later; where those do not fit dtotal is read by its threads, and the widest rows (eight
+    // words a thread) have one place.
     while (ctas > 1 && !stage(a, shape, dt, ctas, 3, 1, 2, smem)) --ctas;
     a.stage_res = dtotal && dx && stage(a, shape, dt, ctas, 3, 1, 2, smem);
-    const bool fits = stage(a, shape, dt, ctas, a.stage_res ? 3 : 2, 1, 2, smem);
+    const bool fits = stage(a, shape, dt, ctas, a.stage_res ? 3 : 2, 1, shape.words == 8 ? 1 : 2, smem);
     if (fits) {
       const int64_t grid = std::min<int64_t>((n_rows + rows - 1) / rows, (int64_t)c->num_sms * ctas);
       if (dweight || dbias) {
