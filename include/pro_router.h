@@ -113,7 +113,8 @@ typedef enum { PR_DTYPE_F32 = 0, PR_DTYPE_BF16 = 1 } pr_dtype;
                                 on resident logits).  Default 0. */
 #define PR_OPT_TIMING 4      /* 1: the calls after the verifier's (pr_head_score,
                                 pr_quantile_score, pr_selective_metrics, pr_lmhead_features,
-                                the training losses, the optimiser step) record a CUDA
+                                the training losses, pr_top_logits, the norms, the
+                                optimiser step) record a CUDA
                                 event after each kernel, for
                                 pr_ctx_kernel_times; the kernels then no longer overlap one
                                 another.  Default 0. */
@@ -168,7 +169,10 @@ pr_status pr_last_error(pr_ctx* ctx, uint32_t* flags);
  * crowded ones (above 65,535 scores), the buckets' groups and the final
  * reduction; for the training losses the listing of the rows (one kernel, two for
  * large batches, none for up to 512 rows), the pass over the logits, the answer pairs
- * (preference loss) and a second pass where the gradient takes one.  Waits for the call's last event.  Writes min(count, cap) values to
+ * (preference loss) and a second pass where the gradient takes one; for pr_distill_loss the
+ * listing, the batch's lists (with a gradient, above 512 rows) and the pass; for
+ * pr_layernorm_backward the rows and the columns' sums.  Waits for the call's last event.
+ * Writes min(count, cap) values to
  * `ms` and the count to *n (0 if no timed call was made).
  */
 pr_status pr_ctx_kernel_times(pr_ctx* ctx, float* ms, int32_t cap, int32_t* n);
@@ -607,10 +611,11 @@ pr_status pr_preference_loss(pr_ctx* ctx, const void* logits, pr_dtype dt, int64
  *                ascending)                                                   (output)
  *   logp         device float [n_rows][k]: z_v - log sum_u exp(z_u)           (output)
  * z from 1e9 on counts as +inf, from -1e9 down (so the type's lowest value) as -inf: masked,
- * never listed.  Where fewer than k are left the list ends with id -1 and log-probability -inf.
+ * never listed.  Where fewer than k are left the list ends with ids -1 and log-probabilities -inf.
  * A row with NaN or +inf, or with nothing finite, has ids -1 and log-probabilities NaN
- * (PR_FLAG_NONFINITE in the context flag word).  Orders are exact; sums are fp32, in an order that depends on
- * the sizes alone.  n_rows < 2^31; one launch, no workspace.
+ * (PR_FLAG_NONFINITE in the context flag word).  Orders are exact; sums are fp32, in an order
+ * that depends on the sizes and on the rows' alignment alone.  n_rows < 2^31; one launch, no
+ * workspace: calls on different streams may overlap.
  */
 pr_status pr_top_logits(pr_ctx* ctx, const void* logits, pr_dtype dt, int64_t n_rows,
                         int64_t vocab, int64_t row_stride, int32_t k, float temperature,
@@ -660,11 +665,13 @@ typedef struct {
  *   t_logp     device float [n_rows][k]
  *   chosen     device int32 [n_rows], the hard labels y, or NULL
  *   kl         device float [n_rows]: each row's KL, 0 where the row does not count (output)
- * Where every token outside S is masked there is no class of the rest.  A counted row has
- * KL and gradient NaN, and so have the statistics that it enters, if it has NaN or +inf or nothing finite among its logits
- * or NaN or +inf among its t_logp, or reverse with PR_REST_NONE and no listed token unmasked (PR_FLAG_NONFINITE), or
- * an id outside the vocabulary, one listed twice or a label outside the vocabulary
- * (PR_FLAG_BAD_CHOSEN).  n_rows < 2^31.
+ * Where every token outside S is masked there is no class of the rest.  A counted row has KL
+ * and gradient NaN, and so have the statistics that it enters,
+ *   - with NaN, +inf or nothing finite among its logits, NaN or +inf among its t_logp, or, reverse
+ *     with PR_REST_NONE, no listed token that is not masked (PR_FLAG_NONFINITE);
+ *   - with an id or a label outside the vocabulary, or an id listed twice (PR_FLAG_BAD_CHOSEN).
+ * n_rows < 2^31.  With a gradient the context holds 16 k + 32 bytes per row more than the other
+ * losses' workspace.
  */
 pr_status pr_distill_loss(pr_ctx* ctx, const void* logits, pr_dtype dt, int64_t n_rows,
                           int64_t vocab, int64_t row_stride, const int32_t* ids,
@@ -682,16 +689,19 @@ pr_status pr_distill_loss(pr_ctx* ctx, const void* logits, pr_dtype dt, int64_t 
  * takes as hidden states):
  *   h = x + residual, rounded to the rows' type;  m = mean(h), or 0 with rms;
  *   rstd = 1 / sqrt(mean((h - m)^2) + eps);  y = (h - m) rstd weight + bias
- * in fp32, y rounded once; the sums are of h - m itself, not of squares less a square.
+ * in fp32, y rounded once; the sums are of h - m itself, not of squares less a square, in an
+ * order that depends on the sizes and on the rows' alignment alone.
  *   x, residual, total, y   device [n_rows][stride] of type dt, strides >= d; residual may
  *                be NULL.  total receives h, or is NULL
  *   weight, bias device [d] of type wdt; bias may be NULL
  *   eps          >= 0, finite
- *   mean, rstd   device float [n_rows] for the backward pass, or NULL (mean is not written with rms)
- * total and y may each be the buffer of x or of residual, with the same stride; else outputs overlap
- * nothing.  Any element alignment; rows whose bases and strides are multiples of 16 bytes are
- * read and written fastest.  n_rows < 2^31, 1 <= d <= PR_NORM_MAX_D.  One launch, no workspace;
- * NaN and infinities stay in their rows.
+ *   mean, rstd   device float [n_rows] for the backward pass, or NULL (mean is not written with
+ *                rms)
+ * total and y may each be the buffer of x or of residual, with the same stride; else outputs
+ * overlap nothing.  Any element alignment; rows whose bases and strides are multiples of 16 bytes
+ * are read and written fastest.  (Of rows of more than 256 bytes every 16-byte word that holds a
+ * byte of the row is read, whole.)  n_rows < 2^31, 1 <= d <= PR_NORM_MAX_D.  One launch, no
+ * workspace: calls on different streams may overlap; NaN and infinities stay in their rows.
  */
 pr_status pr_layernorm(pr_ctx* ctx, const void* x, pr_dtype dt, int64_t n_rows, int64_t d,
                        int64_t x_stride, const void* residual, int64_t residual_stride,
@@ -709,10 +719,11 @@ pr_status pr_layernorm(pr_ctx* ctx, const void* x, pr_dtype dt, int64_t n_rows, 
  *                dy, x or dtotal with the same stride
  *   mean         device float [n_rows] (not read with rms, may then be NULL); rstd [n_rows]
  *   dweight, dbias  device float [d] or NULL; with accumulate they are added to
- * One of dx, dweight, dbias must be asked for.  Sums are fp32 in an order that depends on the
- * sizes alone: results are bit-reproducible.  The context holds a workspace (up to 16 bytes
- * per column and SM), allocated or grown by the first call that needs more, as the training losses'; calls and
- * replays on different streams must not overlap (they share it).
+ * One of dx, dweight, dbias must be asked for; with n_rows 0 the sums are 0.  Sums are fp32 in an
+ * order that depends on the sizes and types (dx: and on alignment) alone: results are
+ * bit-reproducible, and the same whichever outputs are asked for.  The context holds a workspace
+ * (up to 16 bytes per column and SM), allocated or grown by the first call that needs more, as the
+ * training losses'; calls and replays on different streams must not overlap (they share it).
  */
 pr_status pr_layernorm_backward(pr_ctx* ctx, const void* dy, int64_t dy_stride, const void* x,
                                 int64_t x_stride, pr_dtype dt, int64_t n_rows, int64_t d,

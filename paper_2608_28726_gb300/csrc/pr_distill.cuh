@@ -53,9 +53,10 @@ __device__ __forceinline__ float wide(uint32_t raw) {
 }
 template <typename T>
 constexpr uint32_t DS_MASKED = sizeof(T) == 2 ? 0xff80u : 0xff800000u;  // -inf
-// A listed row's entries and scalars; then, once those are there, its logits at them.  Two steps, as
-// each waits for memory: a row's entries are fetched two rows ahead, its logits one.
-__device__ __forceinline__ ListIn fetch_list(const DistillArgs& d, const Rows& rows, const int4& ref,
+// A listed row's entries and scalars; then, once those are there, its logits at them.  Two steps,
+// as each waits for memory: a row's entries are fetched two rows ahead, its logits one.
+__device__ __forceinline__ ListIn fetch_list(const DistillArgs& d, const Rows& rows,
+    const int4& ref,
                                              int lane) {
   ListIn in;
   in.y = ref.z;
@@ -89,9 +90,9 @@ __device__ __forceinline__ void fetch_logits(const DistillArgs& d, const Share& 
   if (v >= 0) in.edge = raw_at<T>(s.x, v);
 }
 
-// A value as the sum of two fp32 numbers, for 1 - sum p.  (In fp64 the exponentials of a list and their
-// sum are 3,400 cycles of the warp that takes the rows' ends: 1,500 rows of V = 262,144 fp32 without
-// a gradient and lists of 64 784 us for 588.)
+// A value as the sum of two fp32 numbers, for 1 - sum p.  (In fp64 the exponentials of a list and
+// their sum are 3,400 cycles of the warp that takes the rows' ends: 1,500 rows of V = 262,144 fp32
+// without a gradient and lists of 64 784 us for 588.)
 struct Pair {
   float hi, lo;
 };
@@ -239,9 +240,9 @@ __device__ __forceinline__ void fetch_prepared(const DistillArgs& d, int64_t i, 
   o.labelled = f & 4u;
 }
 
-// A row's end: its sum R against 2^k, the list's and label's logits left out.  Writes the
-// result (out, and the list's entries of the gradient to g), whose barrier learns of it first, then
-// the row's KL and the statistics' terms (weight wt).  Whole warp; apart from the kernel's registers.
+// A row's end: its sum R against 2^k, the list's and label's logits left out.  Writes the result
+// (out, and the list's entries of the gradient to g), whose barrier learns of it first, then the
+// row's KL and the statistics' terms (weight wt).  Whole warp; apart from the kernel's registers.
 template <typename T>
 __device__ __forceinline__ void list_math(const DistillArgs& d, int64_t row, const ListIn& in,
                                               const ListPre& pre, float k, float R, float wt,
@@ -287,7 +288,8 @@ __device__ __forceinline__ void list_math(const DistillArgs& d, int64_t row, con
   const float f = rest ? ex2(k - K) : 0.f, Rk = R * f, eyk = ey * f;
   // the largest listed term stays out of the sum of the others: 1 - q of it is others / S
   const float m = warp_max(fmaxf(e[0], e[1]));
-  const unsigned w0 = __ballot_sync(FULL, on[0] && e[0] == m), w1 = __ballot_sync(FULL, on[1] && e[1] == m);
+  const unsigned w0 = __ballot_sync(FULL, on[0] && e[0] == m), w1 = __ballot_sync(FULL, on[1] &&
+      e[1] == m);
   const int first = w0 ? __ffs(w0) - 1 : w1 ? 32 + __ffs(w1) - 1 : -1;  // its place
   const bool any = first >= 0;
   const bool is[2] = {first == lane, first == 32 + lane};
@@ -410,7 +412,8 @@ __device__ __forceinline__ void list_math(const DistillArgs& d, int64_t row, con
   bad |= pre.bad_id;
   if (bad) kl = ce = NAN;
   if (lane < DS_TERMS) {
-    const float t = wt * (lane == 0 ? kl : lane == 1 ? ce : bad ? NAN : lane == 2 ? pre.mass : E * inv);
+    const float t = wt * (lane == 0 ? kl : lane == 1 ? ce : bad ? NAN : lane == 2 ? pre.mass
+        : E * inv);
     const float2 s = stat[lane];
     const float y = s.x + t, z = y - s.x;
     stat[lane] = make_float2(y, s.y + ((s.x - (y - z)) + (t - z)));
@@ -459,9 +462,10 @@ __device__ __forceinline__ void list_stats(const DistillArgs& d, const float2* s
 
 // ---- the lists of larger batches, ahead of the rows ---------------------------------------------
 //
-// What of a row's end does not wait for its sum, a row to a warp: the warp that takes the ends would
-// wait for the entries, then for the logits at them, and work out their probabilities, longer than
-// its row takes (64 answers of V = 151,936 bf16 with their gradient: DS_LISTS_FIGURE).
+// What of a row's end does not wait for its sum, a row to a warp: the warp that takes the ends
+// would wait for the entries, then for the logits at them, and work out their probabilities, longer
+// than its row takes (7,800 rows of V = 151,936 bf16 with lists of 64 and their gradient: 796 us
+// for 837).
 constexpr int DP_NT = 256;
 template <typename T>
 __global__ void __launch_bounds__(DP_NT) distill_lists(const __grid_constant__ DistillArgs d) {
@@ -526,13 +530,14 @@ __device__ __forceinline__ void add_rest_ends(const DistillArgs& d, const Share&
   R += warp_sum(add ? ex2(fmaf(edge, c2, -k)) : 0.f);
 }
 template <typename T>
-__device__ __forceinline__ void put_end(T* g, int32_t v, int kind, const RowOut& o, const float* list,
+__device__ __forceinline__ void put_end(T* g, int32_t v, int kind, const RowOut& o,
+    const float* list,
                                         float c2, float edge) {
   if (v >= 0) put(g + v, kind >= 0 ? list[kind] : kind == DS_LABEL ? o.gy : grad1(o, c2, edge));
 }
 
-// Element `e` of a row in shared memory is no part of its sum.  (The next copy into the place is the
-// async proxy's: a fence before the place is given back.)
+// Element `e` of a row in shared memory is no part of its sum.  (The next copy into the place is
+// the async proxy's: a fence before the place is given back.)
 template <typename T>
 __device__ __forceinline__ void leave_out(unsigned char* row, int32_t e) {
   if constexpr (sizeof(T) == 2) reinterpret_cast<uint16_t*>(row)[e] = 0xff80u;
@@ -550,9 +555,9 @@ __device__ __forceinline__ void fence_async() {
 // hold one of the row's listed tokens there write -inf over it; when it has written the words'
 // gradient, the same lanes write the list's entries over that.
 //
-// Without a gradient nothing has to be held, and `parts` of a row may go through one CTA, one after the
-// other: a row of a cluster's eight parts fills 120 of 152 SMs, as clusters of eight find no more room.
-// Sums are kept apart as a cluster's CTAs keep them, so that the loss has the same bits.
+// Without a gradient nothing has to be held, and `parts` of a row may go through one CTA, one after
+// the other: a row of a cluster's eight parts fills 120 of 152 SMs, as clusters of eight find no
+// more room. Sums are kept apart as a cluster's CTAs keep them, so that the loss has the same bits.
 
 // a lane's tokens among its warp's words of this CTA's part of a row: their elements from the
 // row's first word on, or -1
@@ -577,11 +582,13 @@ __device__ __forceinline__ Ids fetch_ids(const DistillArgs& d, const int4& ref, 
   return r;
 }
 template <int VEC>
-__device__ __forceinline__ Mine mine_of(const DistillArgs& d, const Share& s, const Ids& ids, int32_t y,
+__device__ __forceinline__ Mine mine_of(const DistillArgs& d, const Share& s, const Ids& ids,
+    int32_t y,
                                         int warp, int lane) {
   Mine m;
   m.chunks = 0u;
-  const int32_t l[2] = {ids.t[0] == -INFINITY ? -1 : ids.id[0], ids.t[1] == -INFINITY ? -1 : ids.id[1]};
+  const int32_t l[2] = {ids.t[0] == -INFINITY ? -1 : ids.id[0],
+      ids.t[1] == -INFINITY ? -1 : ids.id[1]};
   const bool listed = l[0] == y || l[1] == y;
   const bool apart = d.a.chosen && !__any_sync(FULL, listed);
 #pragma unroll
@@ -632,7 +639,8 @@ __global__ void __launch_bounds__(RG_NT, 2)
   asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
   const int64_t G = gridDim.x / C, first = blockIdx.x / C;
   const uint32_t P = HOLD ? C : C * parts;  // parts of a row; this CTA has rank, or all of them
-  const uint32_t p_first = HOLD || parts == 1 ? rank : 0, p_last = HOLD ? p_first + 1 : parts == 1 ? rank + 1 : P;
+  const uint32_t p_first = HOLD || parts == 1 ? rank : 0,
+      p_last = HOLD ? p_first + 1 : parts == 1 ? rank + 1 : P;
   uint64_t* const full = reinterpret_cast<uint64_t*>(smem_raw + DS_BARS);
   uint64_t* const empty = full + places;
   float2* const sums = reinterpret_cast<float2*>(smem_raw + distill_sums(places));
@@ -900,7 +908,8 @@ __global__ void __launch_bounds__(RG_NT, 2)
           } else {
 #pragma unroll
             for (int q = 0; q < RG_W; ++q)
-              if (w + 32 * RG_NW * q + at < sh.w1) put_word(to + 32 * RG_NW * q * Tr::VEC, v[q], vec);
+              if (w + 32 * RG_NW * q + at < sh.w1) put_word(to + 32 * RG_NW * q * Tr::VEC, v[q],
+                  vec);
           }
           if (chunks & 1u) {
             __syncwarp();  // the warp's words are written: the list's entries over them
@@ -1020,7 +1029,8 @@ __global__ void __launch_bounds__(32 * RW_MOST, 2)
     join(make_float2(k, S.x + S.y), 1.f, k, R);
     add_rest_ends(d, sh, wide<T>(in.edge), v, kind, k, R);
     const float wt = (float)(a.norm ? share / (double)in.count : share);
-    list_math<T>(d, ref.x, in, pre, k, R, wt, true, HOLD ? &sm.out[warp] : nullptr, list, nullptr, stat, lane);
+    list_math<T>(d, ref.x, in, pre, k, R, wt, true, HOLD ? &sm.out[warp] : nullptr, list, nullptr,
+        stat, lane);
     __syncwarp();
     if (HOLD) {
       const RowOut o = sm.out[warp];

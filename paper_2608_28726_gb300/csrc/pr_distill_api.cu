@@ -23,7 +23,8 @@ const void* ring_kernel(bool hold, bool own) {
                      : reinterpret_cast<const void*>(&prk::distill_ring<T, false, false>));
 }
 const void* ring_kernel(pr_dtype dt, bool hold, bool own) {
-  return dt == PR_DTYPE_BF16 ? ring_kernel<__nv_bfloat16>(hold, own) : ring_kernel<float>(hold, own);
+  return dt == PR_DTYPE_BF16 ? ring_kernel<__nv_bfloat16>(hold, own) : ring_kernel<float>(hold,
+      own);
 }
 
 const void* rows_kernel(pr_dtype dt, bool hold) {
@@ -37,7 +38,8 @@ const void* rows_kernel(pr_dtype dt, bool hold) {
 // half of an SM's shared memory
 constexpr size_t HALF = prk::distill_start(4, prk::RG_FEW, 0) + (size_t)prk::RG_FEW * prk::RG_BYTES;
 
-// shared memory opt-ins, and the clusters that the GPU has room for, as ring_setup of the other losses
+// shared memory opt-ins, and the clusters that the GPU has room for, as ring_setup of the other
+// losses
 pr_status setup(pr_ctx* c) {
   if (c->distill_ready) return PR_OK;
   for (pr_dtype dt : {PR_DTYPE_F32, PR_DTYPE_BF16})
@@ -46,7 +48,8 @@ pr_status setup(pr_ctx* c) {
         PR_CUDA(cudaFuncSetAttribute(ring_kernel(dt, hold, own),
                                      cudaFuncAttributeMaxDynamicSharedMemorySize,
                                      (int)ring_bytes(prk::RG_MOST, 8, 0, false)));
-      PR_CUDA(cudaFuncSetAttribute(rows_kernel(dt, hold), cudaFuncAttributeMaxDynamicSharedMemorySize,
+      PR_CUDA(cudaFuncSetAttribute(rows_kernel(dt, hold),
+          cudaFuncAttributeMaxDynamicSharedMemorySize,
                                    (int)HALF));
     }
   for (int i = 0; i < 4; ++i)
@@ -85,7 +88,8 @@ pr_status launch_lists(pr_ctx* c, prk::DistillArgs& d, pr_dtype dt, cudaStream_t
   return st == PR_OK ? timing_mark(c, s) : st;
 }
 
-pr_status launch_ring(pr_ctx* c, prk::DistillArgs& d, pr_dtype dt, const RingShape& shape, bool hold,
+pr_status launch_ring(pr_ctx* c, prk::DistillArgs& d, pr_dtype dt, const RingShape& shape,
+    bool hold,
                       cudaStream_t s) {
   int places = shape.places, parts = 1, cluster = 1 << shape.split;
   int64_t groups = shape.groups;

@@ -76,7 +76,8 @@ inline pr_status workspace(pr_ctx* c, prk::LossArgs& a, int64_t groups, bool pre
 }
 
 // early: set up while the kernel before it still runs
-inline pr_status launch(const void* kern, unsigned grid, unsigned threads, size_t smem, unsigned cluster,
+inline pr_status launch(const void* kern, unsigned grid, unsigned threads, size_t smem,
+    unsigned cluster,
                  void** args, cudaStream_t s, bool early = true) {
   cudaLaunchConfig_t cfg;
   memset(&cfg, 0, sizeof cfg);
@@ -136,11 +137,11 @@ struct RingShape {
   int64_t groups;   // rows in work at a time
 };
 
-// Of the launches whose CTAs hold a row, with two places left for the next row's chunks,
-// the one that takes the least time by this count (room: clusters resident, as ring_setup finds), in the time that an SM takes for a
-// chunk: each cluster's rows come one after the other, a row takes its CTA's chunks and about
-// three for its end, which two CTAs on an SM hide from one another.  The same with and
-// without a gradient, so that the losses' bits are.
+// Of the launches whose CTAs hold a row, with two places left for the next row's chunks, the one
+// that takes the least time by this count (room: clusters resident, as ring_setup finds), in the
+// time that an SM takes for a chunk: each cluster's rows come one after the other, a row takes its
+// CTA's chunks and about three for its end, which two CTAs on an SM hide from one another.  The
+// same with and without a gradient, so that the losses' bits are.
 inline RingShape choose_ring(const int (&room)[2][4], pr_dtype dt, int64_t n_rows, int64_t vocab) {
   const int64_t words = vocab * (int64_t)esize(dt) / 16;
   const int64_t chunks = (words + prk::RG_CHUNK - 1) / prk::RG_CHUNK;

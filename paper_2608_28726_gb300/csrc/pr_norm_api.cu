@@ -29,8 +29,8 @@ bool same_rows(const void* out, int64_t out_stride, const void* in, int64_t in_s
 bool on_words(const void* p, int64_t stride, pr_dtype dt) {
   return !p || (aligned16(p) && stride * (int64_t)esize(dt) % 16 == 0);
 }
-// The kernel for rows of so many words, [of whole ones on the grid], and whether it stages them; threads of a
-// row, words of each.
+// The kernel for rows of so many words, [of whole ones on the grid], and whether it stages them;
+// threads of a row, words of each.
 struct NormShape {
   const void* kernel[2];
   bool staged;
@@ -73,9 +73,10 @@ NormShape backward_of(int64_t words) {
 
 constexpr int NORM_STAGES = 4;  // at most
 constexpr size_t NORM_ROOM = 220 * 1024;
-// The shared memory of a CTA, `ctas` of which are to be on an SM: the weights (`weights` arrays), and
-// places for k rows, at least `least`.  Returns whether it fits.
-bool stage(prk::NormArgs& a, const NormShape& shape, pr_dtype dt, int ctas, int k, int weights, int least,
+// The shared memory of a CTA, `ctas` of which are to be on an SM: the weights (`weights` arrays),
+// and places for k rows, at least `least`.  Returns whether it fits.
+bool stage(prk::NormArgs& a, const NormShape& shape, pr_dtype dt, int ctas, int k, int weights,
+    int least,
            size_t& smem) {
   a.row_bytes = (int32_t)((a.d * (int64_t)esize(dt) + 30) / 16 * 16);  // wherever a row begins
   a.stages = 0;
@@ -96,12 +97,14 @@ pr_status setup(pr_ctx* c) {
     for (const NormShape& s : {forward_of<float>(words), forward_of<__nv_bfloat16>(words),
                                backward_of<float>(words), backward_of<__nv_bfloat16>(words)})
       for (const void* kernel : s.kernel)
-        if (kernel) PR_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)NORM_ROOM));
+        if (kernel) PR_CUDA(cudaFuncSetAttribute(kernel,
+            cudaFuncAttributeMaxDynamicSharedMemorySize, (int)NORM_ROOM));
   c->norm_ready = true;
   return PR_OK;
 }
 
-pr_status launch(pr_ctx* c, const void* kernel, dim3 grid, unsigned threads, size_t smem, void** args,
+pr_status launch(pr_ctx* c, const void* kernel, dim3 grid, unsigned threads, size_t smem,
+    void** args,
                  cudaStream_t s) {
   cudaLaunchConfig_t cfg;
   memset(&cfg, 0, sizeof cfg);
@@ -143,7 +146,8 @@ pr_status pr_layernorm(pr_ctx* c, const void* x, pr_dtype dt, int64_t n_rows, in
         (residual && !rows_ok(residual, d, residual_stride, dt)) ||
         (total && !rows_ok(total, d, total_stride, dt)) || y == total)
       return PR_ERR_INVALID_ARG;
-    if (!same_rows(y, y_stride, x, x_stride) || !same_rows(y, y_stride, residual, residual_stride) ||
+    if (!same_rows(y, y_stride, x, x_stride) || !same_rows(y, y_stride, residual,
+        residual_stride) ||
         (total && (!same_rows(total, total_stride, x, x_stride) ||
                    !same_rows(total, total_stride, residual, residual_stride))))
       return PR_ERR_INVALID_ARG;
@@ -178,7 +182,8 @@ pr_status pr_layernorm(pr_ctx* c, const void* x, pr_dtype dt, int64_t n_rows, in
                      on_words(residual, residual_stride, dt) && on_words(total, total_stride, dt) &&
                      on_words(y, y_stride, dt);
   const int64_t words = (d * (int64_t)esize(dt) + 15) / 16;
-  const NormShape shape = dt == PR_DTYPE_BF16 ? forward_of<__nv_bfloat16>(words) : forward_of<float>(words);
+  const NormShape shape = dt == PR_DTYPE_BF16 ? forward_of<__nv_bfloat16>(words)
+      : forward_of<float>(words);
   if (shape.threads) {
     if ((st = setup(c)) != PR_OK) return st;
     const int threads = std::max(shape.threads, prk::NR_NT), rows = threads / shape.threads;
@@ -194,7 +199,8 @@ pr_status pr_layernorm(pr_ctx* c, const void* x, pr_dtype dt, int64_t n_rows, in
     }
     if (fits) {
       if (!shape.staged) ctas = 2048 / threads;
-      const int64_t grid = std::min<int64_t>((n_rows + rows - 1) / rows, (int64_t)c->num_sms * ctas);
+      const int64_t grid = std::min<int64_t>((n_rows + rows - 1) / rows,
+          (int64_t)c->num_sms * ctas);
       void* args[] = {&a};
       return launch(c, shape.kernel[whole], dim3((unsigned)grid), (unsigned)threads, smem, args, s);
     }
@@ -216,8 +222,10 @@ pr_status pr_layernorm_backward(pr_ctx* c, const void* dy, int64_t dy_stride, co
   if (n_rows < 0 || n_rows > 0x7fffffffLL || d < 1 || d > PR_NORM_MAX_D) return PR_ERR_INVALID_ARG;
   if (!weight || !on_grid(weight, wdt) || (!dx && !dweight && !dbias)) return PR_ERR_INVALID_ARG;
   if (n_rows > 0) {
-    if (!rows_ok(dy, d, dy_stride, dt) || !rows_ok(x, d, x_stride, dt) || !rstd || (!mean && !rms) ||
-        (dtotal && !rows_ok(dtotal, d, dtotal_stride, dt)) || (dx && !rows_ok(dx, d, dx_stride, dt)))
+    if (!rows_ok(dy, d, dy_stride, dt) || !rows_ok(x, d, x_stride, dt) || !rstd || (!mean &&
+        !rms) ||
+        (dtotal && !rows_ok(dtotal, d, dtotal_stride, dt)) || (dx && !rows_ok(dx, d, dx_stride,
+            dt)))
       return PR_ERR_INVALID_ARG;
     if (dx && (!same_rows(dx, dx_stride, dy, dy_stride) || !same_rows(dx, dx_stride, x, x_stride) ||
                !same_rows(dx, dx_stride, dtotal, dtotal_stride)))
@@ -255,37 +263,44 @@ pr_status pr_layernorm_backward(pr_ctx* c, const void* dy, int64_t dy_stride, co
   a.accumulate = accumulate ? 1 : 0;
   a.vec_w = aligned16(weight);
   a.ctx_flags = c->flags;
-  const bool whole = d * (int64_t)esize(dt) % 16 == 0 && on_words(x, x_stride, dt) && on_words(dy, dy_stride, dt) &&
+  const bool whole = d * (int64_t)esize(dt) % 16 == 0 && on_words(x, x_stride, dt) && on_words(dy,
+      dy_stride, dt) &&
                      on_words(dtotal, dtotal_stride, dt) && on_words(dx, dx_stride, dt);
   const int64_t words = (d * (int64_t)esize(dt) + 15) / 16;
-  const NormShape shape = dt == PR_DTYPE_BF16 ? backward_of<__nv_bfloat16>(words) : backward_of<float>(words);
+  const NormShape shape = dt == PR_DTYPE_BF16 ? backward_of<__nv_bfloat16>(words)
+      : backward_of<float>(words);
   if (shape.threads) {
     if ((st = setup(c)) != PR_OK) return st;
     const int threads = std::max(shape.threads, prk::NR_NT), rows = threads / shape.threads;
     int ctas = threads > prk::NR_NT ? 1 : 2;
     size_t smem = 0;
-    // Places for three rows each decide how many CTAs an SM has, whether dtotal is there or not: the order
-    // of the columns' sums is to depend on the sizes alone.  Two places at least, as one is filled again a
-    // row later; where those do not fit dtotal is read by its threads, and the widest rows (eight
-    // words a thread) have one place.
+    // Places for three rows each decide how many CTAs an SM has, whether dtotal is there or not:
+    // the order of the columns' sums is to depend on the sizes alone.  Two places at least, as one
+    // is filled again a row later; where those do not fit dtotal is read by its threads, and the
+    // widest rows (eight words a thread) have one place.
     while (ctas > 1 && !stage(a, shape, dt, ctas, 3, 1, 2, smem)) --ctas;
     a.stage_res = dtotal && dx && stage(a, shape, dt, ctas, 3, 1, 2, smem);
-    const bool fits = stage(a, shape, dt, ctas, a.stage_res ? 3 : 2, 1, shape.words == 8 ? 1 : 2, smem);
+    const bool fits = stage(a, shape, dt, ctas, a.stage_res ? 3 : 2, 1, shape.words == 8 ? 1 : 2,
+        smem);
     if (fits) {
-      const int64_t grid = std::min<int64_t>((n_rows + rows - 1) / rows, (int64_t)c->num_sms * ctas);
+      const int64_t grid = std::min<int64_t>((n_rows + rows - 1) / rows,
+          (int64_t)c->num_sms * ctas);
       if (dweight || dbias) {
-        if ((st = grow(c->norm_ws, (size_t)grid * 2 * d * sizeof(float), false)) != PR_OK) return st;
+        if ((st = grow(c->norm_ws, (size_t)grid * 2 * d * sizeof(float),
+            false)) != PR_OK) return st;
         a.part = static_cast<float*>(c->norm_ws.p);
         if (rows > 1)  // the rows' columns, added up at the end
           smem = std::max(smem, (size_t)threads * shape.words * (16 / esize(dt)) * sizeof(float));
       }
       void* args[] = {&a};
-      if ((st = launch(c, shape.kernel[whole], dim3((unsigned)grid), (unsigned)threads, smem, args, s)) != PR_OK)
+      if ((st = launch(c, shape.kernel[whole], dim3((unsigned)grid), (unsigned)threads, smem,
+          args, s)) != PR_OK)
         return st;
       if (!a.part) return PR_OK;
       int parts = (int)grid;
       void* sum_args[] = {&a, &parts};
-      return launch(c, reinterpret_cast<const void*>(&prk::dnorm_sum), dim3((unsigned)((d + 31) / 32), 2),
+      return launch(c, reinterpret_cast<const void*>(&prk::dnorm_sum),
+          dim3((unsigned)((d + 31) / 32), 2),
                     prk::NS_NT, 0, sum_args, s);
     }
   }

@@ -6,7 +6,7 @@
 // groups.  (An element of another group has k elements before it, one at least in each of
 // those.)  So the stream keeps one maximum per group beside the sum of exponentials, the
 // k groups are chosen among the maxima, and the elements among theirs, whatever the row
-// holds: ties and rows in order cost what others do.
+// holds: no threshold that rises along the row, which rows in order would raise at every step.
 // l_v = (c x_v - K) ln 2 - ln sum_u 2^(c x_u - K) with c = log2(e) / T and K the largest
 // c x, rounded; the difference is one FMA, exact but for its last place as far as |c x| 2^-24 stays
 // within the exponent's range: hence the bound of 1e9 T on what counts as finite.
@@ -86,12 +86,14 @@ struct TopList {
 };
 
 // a value as a key has it: -0 is 0
-__device__ __forceinline__ uint64_t top_key(float v, uint32_t index) { return make_key(v + 0.f, index); }
+__device__ __forceinline__ uint64_t top_key(float v, uint32_t index) { return make_key(v + 0.f,
+    index); }
 
 __device__ __forceinline__ float top_max(float m) { return m; }
 __device__ __forceinline__ float top_max(uint16_t m) { return __uint_as_float((uint32_t)m << 16); }
 
-// The first k of n groups by their maxima at gm (shared memory): ranks lane and 32 + lane in hi and lo.
+// The first k of n groups by their maxima at gm (shared memory): ranks lane and 32 + lane in hi and
+// lo.
 template <typename M>
 __device__ __forceinline__ void top_groups(TopList& l, const M* gm, int n, float big, int lane) {
   // a bound that k groups reach: of 64 sets of groups the k-th largest maximum
@@ -191,15 +193,14 @@ __global__ void __launch_bounds__(TP_NT) top_rows(const TopArgs a, const int64_t
 
 // ---- rows through a ring of shared memory ------------------------------------------------------
 //
-// A row to a CTA, or its parts to the CTAs of a cluster; a warp brings 16 KB chunks in by bulk copies, eight
-// sum them and keep the groups' maxima: a group is what a thread takes of a chunk, GW
-// 16-byte words side by side.  Then the eight choose together, by counting instead of
-// sorting: of the threads' own maxima the k-th largest is a bound that k groups reach; the
-// groups that reach it (some 75 for k = 64 in a row of random values) are read again, which the chunks of the
-// next row do not wait for, and each of their elements that reaches it finds its place
-// by counting the ones before it.  Where more groups or elements reach the bound than there is
-// room for (rows of few values), a warp finds the first k groups and elements
-// in TopLists.
+// A row to a CTA, or its parts to the CTAs of a cluster; a warp brings 16 KB chunks in by bulk
+// copies, eight sum them and keep the groups' maxima: a group is what a thread takes of a chunk, GW
+// 16-byte words side by side.  Then the eight choose together, by counting instead of sorting: of
+// the threads' own maxima the k-th largest is a bound that k groups reach; the groups that reach it
+// (some 75 for k = 64 in a row of random values) are read again, which the chunks of the next row
+// do not wait for, and each of their elements that reaches it finds its place by counting the ones
+// before it.  Where more groups or elements reach the bound than there is room for (rows of few
+// values), a warp finds the first k groups and elements in TopLists.
 constexpr int TR_NW = 8;
 constexpr int TR_NT = 32 * (TR_NW + 1);
 constexpr int TR_W = 4;                       // words of a thread and chunk
@@ -243,7 +244,8 @@ struct TopMax<__nv_bfloat16> {
 // GW 4: rows of many words; GW 1: where a bound needs more groups than those have
 template <typename T, int GW>
 __global__ void __launch_bounds__(TR_NT, 3)
-    top_ring(const __grid_constant__ LossArgs a, const int k, const float big, int32_t* const out_ids,
+    top_ring(const __grid_constant__ LossArgs a, const int k, const float big,
+        int32_t* const out_ids,
              const int places, const int gm_bytes) {
   extern __shared__ __align__(16) unsigned char smem_raw[];
   TopRing& sm = *reinterpret_cast<TopRing*>(smem_raw);
@@ -331,7 +333,8 @@ __global__ void __launch_bounds__(TR_NT, 3)
       if (w + TR_CHUNK > sh.w1) {
 #pragma unroll
         for (int q = 0; q < TR_W; ++q)
-          if (w + at[q] >= sh.w1) v[q] = make_uint4(Tr::NEG_WORD, Tr::NEG_WORD, Tr::NEG_WORD, Tr::NEG_WORD);
+          if (w + at[q] >= sh.w1) v[q] = make_uint4(Tr::NEG_WORD, Tr::NEG_WORD, Tr::NEG_WORD,
+              Tr::NEG_WORD);
       }
       __syncwarp();
       if (lane == 0) bar_arrive(&sm.empty[place]);
@@ -540,13 +543,14 @@ __global__ void __launch_bounds__(TR_NT, 3)
       const float log_sum = logf(rows_sum);
       auto give = [&](int j, uint64_t q) {
         out_ids[row * k + j] = bad || q == 0 ? -1 : (int32_t)key_idx(q);
-        a.logp[row * k + j] = bad ? NAN : q ? fmaf(key_val(q), a.c2, -K) * LN2 - log_sum : -INFINITY;
+        a.logp[row * k + j] = bad ? NAN : q ? fmaf(key_val(q), a.c2,
+            -K) * LN2 - log_sum : -INFINITY;
       };
       if (C == 1) {
         if (tid < k) give(tid, mine);
       } else {
-        // an element's place is the number of those before it in each list, found by bisection (lists
-        // end with zeros, which come after everything)
+        // an element's place is the number of those before it in each list, found by bisection
+        // (lists end with zeros, which come after everything)
         for (int i = tid; i < (int)C * TP_MAX; i += 32 * TR_NW) {
           const int c = i / TP_MAX, j = i % TP_MAX;
           const uint64_t q = sm.lists[c][j];
@@ -585,9 +589,9 @@ __global__ void __launch_bounds__(TR_NT, 3)
 
 // ---- short rows: one to a warp ---------------------------------------------------------------
 //
-// A CTA's choice is a chain of some 10,000 cycles, many times what a short row's data take.  So each warp
-// has a row of its own, brought into its part of shared memory by one bulk copy: a group is a
-// word, the bound is found bit by bit among the lanes' four largest groups each, and the
+// A CTA's choice is a chain of some 10,000 cycles, many times what a short row's data take.  So
+// each warp has a row of its own, brought into its part of shared memory by one bulk copy: a group
+// is a word, the bound is found bit by bit among the lanes' four largest groups each, and the
 // elements that reach it go through a TopList.
 constexpr int TS_MOST = 10;  // warps of a CTA; two CTAs on an SM
 struct TopShort {
@@ -598,7 +602,8 @@ constexpr size_t TS_START = (sizeof(TopShort) + 15) / 16 * 16;
 
 template <typename T>
 __global__ void __launch_bounds__(32 * TS_MOST, 2)
-    top_short(const __grid_constant__ LossArgs a, const int k, const float big, int32_t* const out_ids,
+    top_short(const __grid_constant__ LossArgs a, const int k, const float big,
+        int32_t* const out_ids,
               const int bytes) {  // of a warp's part
   extern __shared__ __align__(16) unsigned char smem_raw[];
   TopShort& sm = *reinterpret_cast<TopShort*>(smem_raw);
@@ -699,7 +704,8 @@ __global__ void __launch_bounds__(32 * TS_MOST, 2)
     TopList l(sm.buf[warp], k);
     for (int32_t w = 0; w < sh.words; w += 32) {
       const bool in = w + lane < sh.words;
-      const uint4 q = in ? st[w] : make_uint4(Tr::NEG_WORD, Tr::NEG_WORD, Tr::NEG_WORD, Tr::NEG_WORD);
+      const uint4 q = in ? st[w] : make_uint4(Tr::NEG_WORD, Tr::NEG_WORD, Tr::NEG_WORD,
+          Tr::NEG_WORD);
       if (!__any_sync(FULL, reaches(Tr::gmax(q)))) continue;
       uint32_t on = 0u;  // a bit per element
 #pragma unroll
@@ -714,7 +720,8 @@ __global__ void __launch_bounds__(32 * TS_MOST, 2)
         on &= on - 1u;
       }
     }
-    if (sh.head + sh.tail > 0) l.push(v_end >= 0 && reaches(x_end), top_key(x_end, (uint32_t)v_end), lane);
+    if (sh.head + sh.tail > 0) l.push(v_end >= 0 && reaches(x_end), top_key(x_end,
+        (uint32_t)v_end), lane);
     l.finish(lane);
     const float log_sum = logf(R * rescale2(ref - K));
 #pragma unroll

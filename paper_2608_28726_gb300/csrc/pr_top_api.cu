@@ -37,12 +37,14 @@ struct TopShape {
   size_t gm, smem;
 };
 
-// Warps of a CTA of top_short, or 0 where the ring takes less time: with fewer than five rows of
-// a CTA, or no more than two for each CTA of the ring (TOP_SHORT_FIGURE).
+// Warps of a CTA of top_short, or 0 where the ring takes less time: with fewer than five rows of a
+// CTA, or no more than one for each of the ring's CTAs (k = 20, V = 4,000 bf16: 300 rows 7.9 us for
+// the ring's 6.4, 456 7.8 for 8.1, 608 7.8 for 12.3; V = 10,000: 13.2 for 9.3, 13.4 for 14.1).
 int short_warps(const pr_ctx* c, int64_t n_rows, int64_t vocab, pr_dtype dt) {
-  if (n_rows <= 6 * c->num_sms) return 0;
+  if (n_rows <= 3 * c->num_sms) return 0;
   const int64_t part = std::max<int64_t>(16, vocab * (int64_t)esize(dt) / 16 * 16);
-  const int64_t w = std::min<int64_t>(prk::TS_MOST, ((int64_t)HALF_BYTES - (int64_t)prk::TS_START) / part);
+  const int64_t w = std::min<int64_t>(prk::TS_MOST,
+      ((int64_t)HALF_BYTES - (int64_t)prk::TS_START) / part);
   return w >= 5 ? (int)w : 0;
 }
 
@@ -63,12 +65,13 @@ TopShape choose(const pr_ctx* c, pr_dtype dt, int64_t n_rows, int64_t vocab) {
     s.gm = ((size_t)groups * (dt == PR_DTYPE_BF16 ? 2 : 4) + 127) / 128 * 128;
     const size_t fixed = prk::TR_START + s.gm;
     if (fixed + 2 * prk::TR_BYTES > SM_BYTES || groups > 65536) continue;
-    // Three CTAs on an SM where their rings keep three places, two with four: while one chooses, the
-    // others stream (4,096 rows of V = 151,936 bf16, k = 20: 206 us for 234 with two).  Where
+    // Three CTAs on an SM where their rings keep three places, two with four: while one chooses,
+    // the others stream (4,096 rows of V = 151,936 bf16, k = 20: 206 us for 234 with two).  Where
     // that leaves one CTA, two with a row's parts are better (1,000 rows of V = 262,144 fp32: 190
     // for 202).  Fewer CTAs than would fit get the room of the others.
     const int64_t ctas = n_rows * s.cluster;
-    s.on_sm = fixed + 3 * prk::TR_BYTES <= THIRD_BYTES ? 3 : fixed + 4 * prk::TR_BYTES <= HALF_BYTES ? 2 : 1;
+    s.on_sm = fixed + 3 * prk::TR_BYTES <= THIRD_BYTES ? 3
+        : fixed + 4 * prk::TR_BYTES <= HALF_BYTES ? 2 : 1;
     if (s.on_sm == 1 && s.cluster < 4 && words > 2 * s.cluster * prk::TR_CHUNK) continue;
     s.on_sm = (int)std::min<int64_t>(s.on_sm, (ctas + c->num_sms - 1) / c->num_sms);
     const size_t room = s.on_sm == 3 ? THIRD_BYTES : s.on_sm == 2 ? HALF_BYTES : SM_BYTES;
@@ -104,7 +107,8 @@ pr_status pr_top_logits(pr_ctx* c, const void* logits, pr_dtype dt, int64_t n_ro
   if (!c->top_ready) {
     for (pr_dtype t : {PR_DTYPE_F32, PR_DTYPE_BF16}) {
       for (bool words : {false, true})
-        PR_CUDA(cudaFuncSetAttribute(ring_kernel(t, words), cudaFuncAttributeMaxDynamicSharedMemorySize,
+        PR_CUDA(cudaFuncSetAttribute(ring_kernel(t, words),
+            cudaFuncAttributeMaxDynamicSharedMemorySize,
                                      (int)SM_BYTES));
       PR_CUDA(cudaFuncSetAttribute(short_kernel(t), cudaFuncAttributeMaxDynamicSharedMemorySize,
                                    (int)HALF_BYTES));
@@ -112,7 +116,8 @@ pr_status pr_top_logits(pr_ctx* c, const void* logits, pr_dtype dt, int64_t n_ro
     c->top_ready = true;
   }
   prk::LossArgs l;
-  fill(l, c, logits, n_rows, vocab, row_stride, nullptr, nullptr, nullptr, 0, nullptr, temperature, 1.f,
+  fill(l, c, logits, n_rows, vocab, row_stride, nullptr, nullptr, nullptr, 0, nullptr,
+      temperature, 1.f,
        nullptr, logp, nullptr, 0);
   int kk = k;
   float limit = big;
@@ -120,7 +125,8 @@ pr_status pr_top_logits(pr_ctx* c, const void* logits, pr_dtype dt, int64_t n_ro
   if (const int warps = short_warps(c, n_rows, vocab, dt)) {
     int part = (int)std::max<int64_t>(16, vocab * (int64_t)esize(dt) / 16 * 16);
     void* args[] = {&l, &kk, &limit, &out, &part};
-    st = launch(short_kernel(dt), 2 * c->num_sms, 32u * warps, prk::TS_START + (size_t)warps * part, 1, args, s);
+    st = launch(short_kernel(dt), 2 * c->num_sms, 32u * warps,
+        prk::TS_START + (size_t)warps * part, 1, args, s);
     return st == PR_OK ? timing_mark(c, s) : st;
   }
   const TopShape shape = choose(c, dt, n_rows, vocab);
@@ -130,7 +136,8 @@ pr_status pr_top_logits(pr_ctx* c, const void* logits, pr_dtype dt, int64_t n_ro
     const int64_t groups = std::min<int64_t>(n_rows, std::max<int64_t>(1, at_once / shape.cluster));
     void* args[] = {&l, &kk, &limit, &out, &places, &gm};
     st = launch(ring_kernel(dt, shape.words),
-                (unsigned)(groups * shape.cluster), prk::TR_NT, shape.smem, (unsigned)shape.cluster, args, s,
+                (unsigned)(groups * shape.cluster), prk::TR_NT, shape.smem,
+                    (unsigned)shape.cluster, args, s,
                 n_rows < groups + 1 && groups * shape.cluster < at_once);
     return st == PR_OK ? timing_mark(c, s) : st;
   }

@@ -107,7 +107,7 @@ def both(B, ctx, x, x64, ids, sent, ch, mask, off, dtype, **kw):
 SIZES = [(1, 1, 1), (3, 2, 2), (5, 7, 3), (5, 8, 8), (4, 9, 12), (7, 31, 31), (9, 33, 40), (6, 255, 64),
          (3, 1000, 20), (37, 1001, 64), (200, 515, 33), (2, 4096, 1), (3, 8191, 32), (3, 16384, 20),
          (5, 32000, 16), (2, 32003, 50), (170, 2050, 20), (2, 70001, 64), (3, 151936, 32), (2, 262144, 64),
-         (1, 393216, 20), (700, 4001, 17), (700, 5000, 64)]
+         (1, 393216, 20), (700, 4001, 17), (700, 5000, 64), (640, 12480, 20), (620, 24577, 33)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -181,6 +181,71 @@ def test_values_that_a_row_can_hold(B, ctx, n, V, dtype):
             got, want = both(B, ctx, x, x64, ids, sent, label, some, [0, 4, 9, n], dtype, norm=1, **kw)
             assert not got[2].isnan().any() and not got[0].isnan().any()
             assert B.pr_ctx_flags(ctx, clear=True) == 0
+
+
+def vectorised(x, ids, sent, mask, reverse):
+    """The oracle's (KL, gradient, and what roundings of it are relative to) in torch, fp64, for batches of
+    whole rows: a class of the rest, no labels, mean over the counted rows."""
+    z = x.double()
+    l = z - torch.logsumexp(z, 1, keepdim=True)
+    on = (ids >= 0) & (sent > -torch.inf)
+    at = torch.where(on, ids, ids.new_tensor(0)).long()
+    p = torch.where(on, sent.double().exp(), 0.0)
+    t = torch.where(on, sent.double(), 0.0)
+    ls = torch.where(on, l.gather(1, at), 0.0)
+    out = torch.ones_like(l, dtype=torch.bool)
+    r, j = torch.nonzero(on, as_tuple=True)
+    out[r, at[r, j]] = False
+    l_sigma = torch.logsumexp(l.masked_fill(~out, -torch.inf), 1)
+    sigma, rho = l_sigma.exp(), (1 - p.sum(1)).clamp(min=2.0 ** -24)
+    if not reverse:
+        kl = (p * (t - ls)).sum(1) + rho * (rho.log() - l_sigma)
+        a, b = -p, -rho
+        size_a, size_b = p, rho
+    else:
+        q = torch.where(on, ls.exp(), 0.0)
+        kl = (q * (ls - t)).sum(1) + sigma * (l_sigma - rho.log())
+        a, b = q * (ls - t - kl[:, None]), sigma * (l_sigma - rho.log() - kl)
+        size_a = q * (1 + (ls - t).abs() + kl.abs()[:, None] + t.abs())
+        size_b = sigma * (1 + l_sigma.abs() + 2 * rho.log().abs() + kl.abs())
+    A = a.sum(1) + b
+    w = mask.double() / mask.sum()
+    g = l.exp() * torch.where(out, (b / sigma - A)[:, None], -A[:, None])
+    size = l.exp() * torch.where(out, (size_b / sigma + A.abs())[:, None], A.abs()[:, None])
+    g[r, at[r, j]] += a[r, j]
+    size[r, at[r, j]] += size_a[r, j]
+    return torch.where(mask.bool(), kl, 0.0), g * w[:, None], size * w[:, None]
+
+
+@pytest.mark.parametrize("n,V,k,dtype", [(600, 151936, 32, "bf16"), (560, 262144, 64, "f32"), (1200, 70001, 50, "bf16"),
+                                         (900, 32000, 64, "f32"), (540, 393216, 20, "f32")])
+def test_large_batches_of_long_rows(B, ctx, n, V, k, dtype):
+    """The launches that fill the GPU: rows over clusters of every size, lists prepared ahead, with
+    and without a gradient and in place of the logits.  Against fp64 on the GPU."""
+    gen = torch.Generator("cuda").manual_seed(V)
+    x = (3 * torch.randn(n, V, generator=gen, device="cuda")).to(TYPES[dtype])
+    teacher = (0.8 * x.float() + torch.randn(n, V, generator=gen, device="cuda")).to(TYPES[dtype])
+    ids, sent = B.pr_top_logits(ctx, teacher, k)
+    del teacher
+    ids[::3, -1] = -1
+    mask = (torch.rand(n, generator=gen, device="cuda") < 0.85).to(torch.uint8)
+    for reverse in (False, True):
+        kw = dict(mask=mask, loss=int(reverse))
+        s, kl, g = B.pr_distill_loss(ctx, x, ids, sent, **kw)
+        s1, kl1, _ = B.pr_distill_loss(ctx, x, ids, sent, want_grad=False, **kw)
+        assert torch.equal(s, s1) and torch.equal(kl, kl1)
+        y = x.clone()
+        B.pr_distill_loss(ctx, y, ids, sent, grad=y, **kw)
+        assert torch.equal(y, g)
+        del y
+        for a in range(0, n, 150):   # 150 rows at a time; the mean is over all counted rows
+            b = min(n, a + 150)
+            want, gw, size = vectorised(x[a:b], ids[a:b], sent[a:b], mask[a:b], reverse)
+            share = float(mask[a:b].sum()) / float(mask.sum())
+            assert ((kl[a:b].double() - want).abs() <= 4e-5 * (1 + want.abs())).all()
+            tol = 2e-4 * size * share + (2.0 ** -8 if dtype == "bf16" else 0) * gw.abs() * share + 1e-37
+            tol += 1e-14 * (size * share).amax(1, keepdim=True)
+            assert ((g[a:b].double() - gw * share).abs() <= tol).all()
 
 
 def test_small_rests_and_sure_rows_keep_their_digits(B, ctx):

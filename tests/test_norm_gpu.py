@@ -225,6 +225,9 @@ def test_values(B, ctx):
         dx, dw, db = B.pr_layernorm_backward(ctx, dy, x, w, rstd, mean=mean, want_dbias=True)
         assert dx[keep].isfinite().all() and dx[1].isnan().all() and dw.isnan().all() and db.isfinite().all()
         check_backward((dx[keep], None, None), dy[keep], x[keep], w, mean[keep], rstd[keep], None, False, "f32")
+        y, _, _, rstd = B.pr_layernorm(ctx, x, w, rms=True)
+        assert y[1].isnan().all() and rstd[1].isnan() and y[2, 7].isnan() and float(rstd[2]) == 0.0
+        check_forward((y[keep], None, rstd[keep]), x[keep], w, None, 1e-5, True, "f32")
         y = B.pr_layernorm(ctx, torch.zeros(2, d, device="cuda"), w, eps=0.0)[0]
         assert y.isnan().all()
 

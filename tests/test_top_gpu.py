@@ -147,6 +147,60 @@ def test_outputs_stay_in_their_place_and_streams_and_graphs(B, ctx):
         check(ids[1:n + 1], logp[1:n + 1], x, k)
 
 
+def test_calls_side_by_side(B, ctx):
+    """The calls that hold no workspace, of one context on two streams at once."""
+    xs = [rows(20 + i, 400, 20000, "bf16") for i in range(2)]
+    want = [B.pr_top_logits(ctx, x, 30) for x in xs]
+    w = torch.ones(20000, device="cuda", dtype=torch.bfloat16)
+    normed = [B.pr_layernorm(ctx, x, w) for x in xs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in xs]
+    for _ in range(5):
+        got = []
+        for x, s in zip(xs, streams):
+            with torch.cuda.stream(s):
+                got.append((B.pr_top_logits(ctx, x, 30), B.pr_layernorm(ctx, x, w)))
+        torch.cuda.synchronize()
+        for (top, norm), t, m in zip(got, want, normed):
+            assert torch.equal(top[0], t[0]) and torch.equal(top[1], t[1])
+            assert torch.equal(norm[0], m[0]) and torch.equal(norm[3], m[3])
+
+
+def test_the_first_call_of_a_context_captured(B):
+    for n, V in ((3, 9000), (700, 9000), (1200, 800)):
+        x = rows(n, n, V, "bf16")
+        ctx = B.pr_ctx_create(0, 1, 1)
+        try:
+            ids = torch.empty(n, 12, dtype=torch.int32, device="cuda")
+            logp = torch.empty(n, 12, device="cuda")
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g):
+                B.pr_top_logits(ctx, x, 12, ids=ids, logp=logp)
+            g.replay()
+            check(ids, logp, x, 12)
+        finally:
+            B.pr_ctx_destroy(ctx)
+
+
+def test_kernel_times(B):
+    ctx = B.pr_ctx_create(0, 1, 1)
+    try:
+        B.pr_ctx_set_option(ctx, B.PR_OPT_TIMING, 1)
+        x = rows(5, 700, 3000, "f32")
+        ids, logp = B.pr_top_logits(ctx, x, 8)
+        assert len(B.pr_ctx_kernel_times(ctx)) == 1
+        B.pr_distill_loss(ctx, x, ids, logp)
+        times = B.pr_ctx_kernel_times(ctx)
+        assert len(times) == 2 and all(t > 0 for t in times)   # the listing, the rows
+        w = torch.ones(3000, device="cuda")
+        _, _, mean, rstd = B.pr_layernorm(ctx, x, w)
+        assert len(B.pr_ctx_kernel_times(ctx)) == 1
+        B.pr_layernorm_backward(ctx, x, x, w, rstd, mean=mean)
+        assert len(B.pr_ctx_kernel_times(ctx)) == 2            # the rows, the columns
+    finally:
+        B.pr_ctx_destroy(ctx)
+
+
 def test_rows_past_32_bits(B, ctx):
     V, n, stride = 1000, 3, (1 << 31) + 24
     buf = torch.zeros(2 * stride + V, dtype=torch.bfloat16, device="cuda")
