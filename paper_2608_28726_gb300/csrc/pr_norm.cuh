@@ -431,6 +431,7 @@ __global__ void __launch_bounds__(L > NR_NT ? L : NR_NT, L > NR_NT ? 1 : 2)
     dnorm_rows(const __grid_constant__ NormArgs a) {
   using W = RowWord<T, L, WHOLE>;
   constexpr int VEC = W::VEC, H = VEC / 2, NT = L > NR_NT ? L : NR_NT, ROWS = NT / L;
+  constexpr bool KEEP = N <= 2;  // xhat and g of a row's words stay in registers
   extern __shared__ __align__(16) unsigned char nm_raw[];
   __shared__ float2 part[2][32];
   const int in_row = threadIdx.x % L, group = threadIdx.x / L;
@@ -477,6 +478,7 @@ __global__ void __launch_bounds__(L > NR_NT ? L : NR_NT, L > NR_NT ? 1 : 2)
     const float2 next = moments(row + step);
     const T *x = x_of(row), *dy = dy_of(row), *t = res_of(row);
     float2 s1 = make_float2(0.f, 0.f), s2 = make_float2(0.f, 0.f);
+    W hats[KEEP ? N : 1], gs[KEEP ? N : 1];
     if (on) {
       if (STAGED) {
         st.wait();
@@ -498,6 +500,10 @@ __global__ void __launch_bounds__(L > NR_NT ? L : NR_NT, L > NR_NT ? 1 : 2)
           s2 = __ffma2_rn(g, hat, s2);
           cw[i].f[j] = __ffma2_rn(dv.f[j], hat, cw[i].f[j]);
           cb[i].f[j] = __fadd2_rn(cb[i].f[j], dv.f[j]);
+          if (KEEP) {
+            hats[i].f[j] = hat;
+            gs[i].f[j] = g;
+          }
         }
       }
     }
@@ -515,18 +521,25 @@ __global__ void __launch_bounds__(L > NR_NT ? L : NR_NT, L > NR_NT ? 1 : 2)
 #pragma unroll
       for (int i = 0; i < N; ++i) {
         if (!W::some(in_row, i, d)) continue;
-        W xv, dv, w, tv;
-        xv.load(x, in_row, i, d);
-        dv.load(dy, in_row, i, d);
-        w.weights(nm_raw, wide, in_row, i, d);
+        W xv, tv;
+        if (!KEEP) {
+          W dv, w;
+          xv.load(x, in_row, i, d);
+          dv.load(dy, in_row, i, d);
+          w.weights(nm_raw, wide, in_row, i, d);
 #pragma unroll
-        for (int j = 0; j < H; ++j) tv.f[j] = make_float2(0.f, 0.f);
+          for (int j = 0; j < H; ++j) {
+            hats[0].f[j] = __fmul2_rn(__fadd2_rn(xv.f[j], nm_both(-mo.x)), nm_both(mo.y));
+            gs[0].f[j] = __fmul2_rn(dv.f[j], w.f[j]);
+          }
+        }
+        const W &hat = hats[KEEP ? i : 0], &gw = gs[KEEP ? i : 0];
+        tv.zero();
         if (res) tv.load(t, in_row, i, d);
 #pragma unroll
         for (int j = 0; j < H; ++j) {
-          const float2 hat = __fmul2_rn(__fadd2_rn(xv.f[j], nm_both(-mo.x)), nm_both(mo.y));
-          const float2 g = __fadd2_rn(__fmul2_rn(dv.f[j], w.f[j]), nm_both(-m1));
-          xv.f[j] = __ffma2_rn(__ffma2_rn(hat, nm_both(-m2), g), nm_both(mo.y), tv.f[j]);
+          const float2 g = __fadd2_rn(gw.f[j], nm_both(-m1));
+          xv.f[j] = __ffma2_rn(__ffma2_rn(hat.f[j], nm_both(-m2), g), nm_both(mo.y), tv.f[j]);
         }
         xv.store(dx, in_row, i, d);
       }

@@ -72,7 +72,8 @@ NormShape backward_of(int64_t words) {
 }
 
 constexpr int NORM_STAGES = 4;  // at most
-constexpr size_t NORM_ROOM = 220 * 1024;
+// of an SM's 228 KB, less what a CTA has besides (1 KB of the system's, the sums)
+constexpr size_t norm_room(int ctas) { return 228 * 1024 / ctas - 1024 - 512; }
 // The shared memory of a CTA, `ctas` of which are to be on an SM: the weights (`weights` arrays),
 // and places for k rows, at least `least`.  Returns whether it fits.
 bool stage(prk::NormArgs& a, const NormShape& shape, pr_dtype dt, int ctas, int k, int weights,
@@ -83,7 +84,7 @@ bool stage(prk::NormArgs& a, const NormShape& shape, pr_dtype dt, int ctas, int 
   smem = (size_t)weights * ((a.d + 7) / 8 * 8) * (a.wide_w ? 4 : 2);
   if (!shape.staged) return true;
   const int groups = std::max(shape.threads, prk::NR_NT) / shape.threads;
-  const size_t room = NORM_ROOM / ctas - 128, place = (size_t)groups * k * a.row_bytes;
+  const size_t room = norm_room(ctas) - 128, place = (size_t)groups * k * a.row_bytes;
   if (room < smem + least * place) return false;
   a.stages = (int)std::min<size_t>(NORM_STAGES, (room - smem) / place);
   smem += (size_t)(groups * a.stages * 8 + 127) / 128 * 128 + a.stages * place;
@@ -98,7 +99,7 @@ pr_status setup(pr_ctx* c) {
                                backward_of<float>(words), backward_of<__nv_bfloat16>(words)})
       for (const void* kernel : s.kernel)
         if (kernel) PR_CUDA(cudaFuncSetAttribute(kernel,
-            cudaFuncAttributeMaxDynamicSharedMemorySize, (int)NORM_ROOM));
+            cudaFuncAttributeMaxDynamicSharedMemorySize, (int)norm_room(1)));
   c->norm_ready = true;
   return PR_OK;
 }
