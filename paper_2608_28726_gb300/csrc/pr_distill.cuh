@@ -536,8 +536,8 @@ __device__ __forceinline__ void put_end(T* g, int32_t v, int kind, const RowOut&
   if (v >= 0) put(g + v, kind >= 0 ? list[kind] : kind == DS_LABEL ? o.gy : grad1(o, c2, edge));
 }
 
-// Element `e` of a row in shared memory is no part of its sum.  (The next copy into the place is
-// the async proxy's: a fence before the place is given back.)
+// Element `e` of a row in shared memory is no part of its sum.  The next copy into the place is the
+// async proxy's: the threads that wrote fence their writes before the place is given back.
 template <typename T>
 __device__ __forceinline__ void leave_out(unsigned char* row, int32_t e) {
   if constexpr (sizeof(T) == 2) reinterpret_cast<uint16_t*>(row)[e] = 0xff80u;
@@ -848,15 +848,16 @@ __global__ void __launch_bounds__(RG_NT, 2)
                 if (w + 32 * RG_NW * q + at >= sh.w1)
                   v[q] = make_uint4(Tr::NEG_WORD, Tr::NEG_WORD, Tr::NEG_WORD, Tr::NEG_WORD);
             }
+            add_words<T>(k, S, v, a.c2, w == sh.w0);
+            // The place is given back once every lane's words are in its sum: given back right
+            // after their loads, with a chunk's listed tokens just left out, one row in 2,000 of
+            // V = 262,144 fp32 k = 64 summed some of the next chunk.  (Not a time's difference.)
             if (!HOLD) {
-              __syncwarp();  // every lane has its words
-              if (lane == 0) {
-                if (chunks & 1u) fence_async();
-                bar_arrive(&empty[place]);
-              }
+              if (chunks & 1u) fence_async();
+              __syncwarp();
+              if (lane == 0) bar_arrive(&empty[place]);
             }
             step();
-            add_words<T>(k, S, v, a.c2, w == sh.w0);
           }
           float R;
           join(make_float2(k, S.x + S.y), 1.f, k, R);
@@ -895,11 +896,9 @@ __global__ void __launch_bounds__(RG_NT, 2)
 #pragma unroll
             for (int q = 0; q < RG_W; ++q) v[q] = make_uint4(0u, 0u, 0u, 0u);
           }
+          if (chunks & 1u) fence_async();
           __syncwarp();
-          if (lane == 0) {
-            if (chunks & 1u) fence_async();
-            bar_arrive(&empty[place0]);
-          }
+          if (lane == 0) bar_arrive(&empty[place0]);
           if (++place0 == places) place0 = 0;
           if (vec && w + RG_CHUNK <= sh.w1) {
 #pragma unroll

@@ -248,6 +248,22 @@ def test_large_batches_of_long_rows(B, ctx, n, V, k, dtype):
             assert ((g[a:b].double() - gw * share).abs() <= tol).all()
 
 
+@pytest.mark.parametrize("n,V,k,dtype", [(2100, 262144, 64, "f32"), (2500, 70001, 64, "bf16"), (3000, 9000, 64, "f32")])
+def test_the_loss_alone_repeats(B, ctx, n, V, k, dtype):
+    """Places of the ring are filled again right after their listed tokens were left out: time and
+    again the bits of the call with a gradient."""
+    gen = torch.Generator("cuda").manual_seed(V)
+    x = (3 * torch.randn(n, V, generator=gen, device="cuda")).to(TYPES[dtype])
+    ids, sent = B.pr_top_logits(ctx, 1.1 * x.float() + torch.randn(n, V, generator=gen, device="cuda"), k)
+    s, kl, g = B.pr_distill_loss(ctx, x, ids, sent)
+    for _ in range(30):
+        s1, kl1, _ = B.pr_distill_loss(ctx, x, ids, sent, want_grad=False)
+        assert torch.equal(kl, kl1) and torch.equal(s, s1)
+    for _ in range(5):
+        g1 = B.pr_distill_loss(ctx, x, ids, sent)[2]
+        assert torch.equal(g, g1)
+
+
 def test_small_rests_and_sure_rows_keep_their_digits(B, ctx):
     """A rest of 1e-9 of the mass, and a label whose probability is 1 - 1e-6: gradients and
     divergences to 2e-3 of themselves (the exponents' error of 30 x 2^-23 in sums of few terms)."""
