@@ -113,29 +113,40 @@ __device__ __forceinline__ Pair warp_sum(Pair v) {
   }
   return v;
 }
-// exp(t) within 2e-9 of itself: 2^n exp(z), t log2(e) = n + z log2(e) with z in two parts, and the
-// exponential's series, its first three terms in two parts
+// 2^(j / 16) in two parts
+__constant__ float2 DS_ROOTS[16] = {
+    {1.0f, 0.0f}, {1.0442737340927124f, 4.8334701574503924e-08f},
+    {1.0905077457427979f, -1.3077539939843064e-08f}, {1.1387885808944702f, 5.386222312608879e-08f},
+    {1.1892070770263672f, 3.797635272917432e-08f}, {1.2418577671051025f, 4.496838101886169e-08f},
+    {1.2968395948410034f, -4.018999533172973e-08f}, {1.3542555570602417f, -1.0123349269974824e-08f},
+    {1.4142135381698608f, 2.4203234971764687e-08f}, {1.4768261909484863f, -4.500898853621038e-08f},
+    {1.5422108173370361f, 8.070904833346049e-09f}, {1.610490322113037f, 9.836217174097328e-09f},
+    {1.6817928552627563f, -2.4755326677450284e-08f}, {1.7562521696090698f, -9.235770370707996e-09f},
+    {1.8340080976486206f, -1.1239277952768134e-08f}, {1.9152065515518188f, 9.845328108326612e-09f}};
+// exp(t) within 1e-12 of itself for t >= -80: t log2(e) = n / 16 + z log2(e) with z in two parts
+// and below ln 2 / 32, 2^(n / 16) from its table, exp(z) - 1 = z + z^2 / 2 + z^3 / 6 + ... whose
+// first two terms are in two parts.  (rho down to 2^-24 is to keep five digits.)
 __device__ __forceinline__ Pair exp_pair(float t) {
-  constexpr float L2E_LOW = 1.92596303e-8f;  // log2(e) - L2E
-  const float y = t * L2E, n = rintf(y), r = y - n;
+  constexpr float L2E_LOW = 1.925963033500011e-08f;  // log2(e) - L2E
+  const float y = t * L2E, n = rintf(y * 16.f), r = fmaf(n, -0.0625f, y);
   const float y_lo = fmaf(t, L2E, -y) + t * L2E_LOW;
-  const float z = r * LN2, z_lo = fmaf(r, LN2, -z) + (r * LN2_LOW + y_lo * LN2);
-  float c = fmaf(z, 1.f / 362880.f, 1.f / 40320.f);
-  c = fmaf(z, c, 1.f / 5040.f);
-  c = fmaf(z, c, 1.f / 720.f);
-  c = fmaf(z, c, 1.f / 120.f);
-  c = fmaf(z, c, 1.f / 24.f);
-  c = fmaf(z, c, 1.f / 6.f);
-  c = c * z * z * z;
+  const float z0 = r * LN2, z0_lo = fmaf(r, LN2, -z0) + (r * LN2_LOW + y_lo * LN2);
+  const float z = z0 + z0_lo, z_lo = z0_lo - (z - z0);
+  const float c = z * z * z * fmaf(z, fmaf(z, 1.f / 120.f, 1.f / 24.f), 1.f / 6.f);
   const float h = 0.5f * z, q = h * z, q_lo = fmaf(h, z, -q) + z * z_lo;
-  const float s1 = 1.f + z, e1 = z - (s1 - 1.f);
-  const float s2 = s1 + q, e2 = q - (s2 - s1);
-  const float s3 = s2 + c, e3 = c - (s3 - s2);
-  const float scale = n < -126.f ? 0.f : exp2f(n);  // (a power of two: exact)
-  Pair p;
-  p.hi = scale * s3;
-  p.lo = n < -100.f ? 0.f : scale * ((e1 + e2) + (e3 + (z_lo + q_lo)));
-  return p;
+  const float w = z + q, w_lo = ((q - (w - z)) + q_lo) + (z_lo + c);
+  const int whole = (int)fminf(fmaxf(n, -3200.f), 3200.f);
+  const float2 root = DS_ROOTS[whole & 15];
+  const float p = root.x * w, p_lo = fmaf(root.x, w, -p) + fmaf(root.x, w_lo, root.y * w);
+  const float s = root.x + p, s_lo = (p - (s - root.x)) + (p_lo + root.y);
+  const int e = whole >> 4;
+  const float scale = e < -126 ? 0.f : exp2f((float)e);  // (a power of two: exact)
+  const float all = s + s_lo;  // (its first part alone is a probability: rounded once)
+  Pair v;
+  v.hi = scale * all;
+  v.lo = e < -90 ? 0.f : scale * (s_lo - (all - s));
+  if (!(t < 1000.f)) v.hi = t;  // (what is no log-probability: NaN, infinity)
+  return v;
 }
 
 // whether an id is listed twice.  Whole warp.
@@ -240,6 +251,46 @@ __device__ __forceinline__ void fetch_prepared(const DistillArgs& d, int64_t i, 
   o.labelled = f & 4u;
 }
 
+// log2 of a sum in two parts, e + f
+struct LogSum {
+  float e, f;
+  __device__ __forceinline__ explicit LogSum(float S) {
+    int ei = (int)(__float_as_uint(S) >> 23) - 127;
+    float m = __uint_as_float((__float_as_uint(S) & 0x7fffffu) | 0x3f800000u);
+    if (m > 1.41f) {
+      m *= 0.5f;
+      ++ei;
+    }
+    e = (float)ei;
+    f = log2f(m);
+  }
+};
+// ln 2 (c x - K - log2 S) in two parts.  A divergence sums differences of logarithms that nearly
+// cancel: what the roundings of c x - K (2^-24 of it) and of the logarithm would leave, 1e-6 of
+// a KL of 0.1, has to stay.  (c is the one that the row's sum was taken with: an error of it
+// is a temperature's, which hardly shows where both models agree.)
+struct LogProb {
+  float hi, lo;
+  __device__ __forceinline__ LogProb(float x, float c2, float K, const LogSum& S) {
+    const float h = x * c2;
+    float u = h - K, u_lo = 0.f;
+    if (h > -INFINITY) {
+      const float t = u - h, left = ((h - (u - t)) + (-K - t)) + fmaf(x, c2, -h), all = u + left;
+      u_lo = (u - all) + left;
+      u = all;
+    }
+    const float w = u - S.e, t = w - u;
+    const float w_lo = ((u - (w - t)) + (-S.e - t)) + u_lo - S.f;
+    const float p = w * LN2, rest = fmaf(w, LN2, -p) + w * LN2_LOW + w_lo * LN2;
+    hi = p + rest;
+    lo = (p - hi) + rest;
+    if (!(u > -INFINITY)) {  // a masked token
+      hi = -INFINITY;
+      lo = 0.f;
+    }
+  }
+};
+
 // A row's end: its sum R against 2^k, the list's and label's logits left out.  Writes the result
 // (out, and the list's entries of the gradient to g), whose barrier learns of it first, then the
 // row's KL and the statistics' terms (weight wt).  Whole warp; apart from the kernel's registers.
@@ -279,13 +330,13 @@ __device__ __forceinline__ void list_math(const DistillArgs& d, int64_t row, con
                                        on[1] ? x[1] * a.c2 : -INFINITY)),
                         rest ? k : -INFINITY);
   if (!(K > -INFINITY)) bad = true;
-  float u[2], e[2], l[2], q[2];
+  float u[2], e[2], q[2];
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     u[h] = on[h] ? fmaf(x[h], a.c2, -K) : -INFINITY;
-    e[h] = ex2(u[h]);
+    e[h] = rescale2(u[h]);  // (as exact as a sum of few terms needs)
   }
-  const float f = rest ? ex2(k - K) : 0.f, Rk = R * f, eyk = ey * f;
+  const float f = rest ? rescale2(k - K) : 0.f, Rk = R * f, eyk = ey * f;
   // the largest listed term stays out of the sum of the others: 1 - q of it is others / S
   const float m = warp_max(fmaxf(e[0], e[1]));
   const unsigned w0 = __ballot_sync(FULL, on[0] && e[0] == m), w1 = __ballot_sync(FULL, on[1] &&
@@ -345,21 +396,18 @@ __device__ __forceinline__ void list_math(const DistillArgs& d, int64_t row, con
     if (out) result();
     if (out_bar && lane == 0) bar_arrive(out_bar);
   }
-  // log q, of what single precision holds from q itself (1.5 x 2^-24 off, whatever the exponents)
-  auto log_q = [&](float v, float exponent) {
-    return v > 1e-30f ? logf(v) : (exponent - log2f(S)) * LN2;
-  };
-  l[0] = log_q(q[0], u[0]);
-  l[1] = log_q(q[1], u[1]);
-  const float l_sigma = log_q(sigma, k - K + log2f(R));
+  const LogSum log_S(S);
+  LogProb l[2] = {LogProb(x[0], a.c2, K, log_S), LogProb(x[1], a.c2, K, log_S)};
+  const LogSum log_R(R);
+  const float l_sigma = ((k - K) + (log_R.e - log_S.e) + (log_R.f - log_S.f)) * LN2;
   // the label, from 1 - q where that is small
   float ce = 0.f;
   if (a.chosen) {
-    float v, less, exponent;
+    float v, less, log_v;
     if (apart) {
       v = eyk * inv;
       less = not_y * inv;
-      exponent = fmaf(xy, a.c2, -K);
+      log_v = LogProb(xy, a.c2, K, log_S).hi;
     } else {
       const bool y0 = on[0] && in.id[0] == in.y, y1 = on[1] && in.id[1] == in.y;
       const unsigned who = __ballot_sync(FULL, y0 || y1);
@@ -367,16 +415,16 @@ __device__ __forceinline__ void list_math(const DistillArgs& d, int64_t row, con
       const bool sure = most && (y0 ? is[0] : is[1]);
       v = __shfl_sync(FULL, y0 ? q[0] : q[1], from);
       less = __shfl_sync(FULL, sure ? others * inv : 1.f - (y0 ? q[0] : q[1]), from);
-      exponent = __shfl_sync(FULL, y0 ? u[0] : u[1], from);
+      log_v = __shfl_sync(FULL, y0 ? l[0].hi : l[1].hi, from);
     }
-    ce = v > 0.5f ? -log1pf(-less) : -log_q(v, exponent);
+    ce = v > 0.5f ? -log1pf(-less) : -log_v;
   }
   // the divergence
   float kl = 0.f;
   if (!d.reverse) {
 #pragma unroll
     for (int h = 0; h < 2; ++h)
-      if (pre.p[h] > 0.f) kl += pre.p[h] * (pre.lt[h] - l[h]);
+      if (pre.p[h] > 0.f) kl += pre.p[h] * ((pre.lt[h] - l[h].hi) - l[h].lo);
     kl = warp_sum(kl);
     if (klass && any) kl += pre.rho * (pre.l_rho - l_sigma);
   } else {
@@ -384,26 +432,31 @@ __device__ __forceinline__ void list_math(const DistillArgs& d, int64_t row, con
       av[0] = q[0];
       av[1] = q[1];
       if (d.none) {  // q over the list
-        const float um = warp_max(fmaxf(u[0], u[1]));
-        if (um == -INFINITY) bad = true;
+        const float K1 = warp_max(fmaxf(on[0] ? x[0] * a.c2 : -INFINITY,
+                                        on[1] ? x[1] * a.c2 : -INFINITY));
+        if (K1 == -INFINITY) bad = true;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) av[h] = on[h] ? ex2(u[h] - um) : 0.f;
-        const float Q = warp_sum(av[0] + av[1]), lQ = logf(Q), per_Q = __fdividef(1.f, Q);
+        for (int h = 0; h < 2; ++h) av[h] = on[h] ? rescale2(fmaf(x[h], a.c2, -K1)) : 0.f;
+        const float Q = warp_sum(av[0] + av[1]), per_Q = __fdividef(1.f, Q);
+        const LogSum log_Q(Q);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          l[h] = (u[h] - um) * LN2 - lQ;
+          l[h] = LogProb(x[h], a.c2, K1, log_Q);
           av[h] *= per_Q;
         }
       }
+      float more[2];  // log q - log p
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
-        if (av[h] > 0.f) kl += av[h] * (l[h] - pre.lt[h]);
+      for (int h = 0; h < 2; ++h) {
+        more[h] = (l[h].hi - pre.lt[h]) + l[h].lo;
+        if (av[h] > 0.f) kl += av[h] * more[h];
+      }
       kl = warp_sum(kl);
       const float far = l_sigma - pre.l_rho;
       const bool out_there = klass && sigma > 0.f;
       if (out_there) kl += sigma * far;
 #pragma unroll
-      for (int h = 0; h < 2; ++h) av[h] = av[h] > 0.f ? av[h] * (l[h] - pre.lt[h] - kl) : 0.f;
+      for (int h = 0; h < 2; ++h) av[h] = av[h] > 0.f ? av[h] * (more[h] - kl) : 0.f;
       if (out_there) b = sigma * (far - kl);
     }
     if (out) result();
