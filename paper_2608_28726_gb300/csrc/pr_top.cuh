@@ -336,9 +336,6 @@ __global__ void __launch_bounds__(TR_NT, 3)
           if (w + at[q] >= sh.w1) v[q] = make_uint4(Tr::NEG_WORD, Tr::NEG_WORD, Tr::NEG_WORD,
               Tr::NEG_WORD);
       }
-      __syncwarp();
-      if (lane == 0) bar_arrive(&sm.empty[place]);
-      step();
       const int32_t g = (w - sh.w0) / GW + tid;
       if constexpr (GW == 4) {
         const float m = Tr::tile_max(v);
@@ -362,6 +359,9 @@ __global__ void __launch_bounds__(TR_NT, 3)
         }
       }
       add_words<T>(ref, S, v, a.c2, w == sh.w0);
+      __syncwarp();  // every lane's words are summed
+      if (lane == 0) bar_arrive(&sm.empty[place]);
+      step();
     }
     float R;
     join(make_float2(ref, S.x + S.y), 1.f, ref, R);
