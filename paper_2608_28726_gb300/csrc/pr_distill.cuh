@@ -149,6 +149,20 @@ __device__ __forceinline__ Pair exp_pair(float t) {
   return v;
 }
 
+// log2 of a sum in two parts, e + f
+struct LogSum {
+  float e, f;
+  __device__ __forceinline__ explicit LogSum(float S) {
+    int ei = (int)(__float_as_uint(S) >> 23) - 127;
+    float m = __uint_as_float((__float_as_uint(S) & 0x7fffffu) | 0x3f800000u);
+    if (m > 1.41f) {
+      m *= 0.5f;
+      ++ei;
+    }
+    e = (float)ei;
+    f = log2f(m);
+  }
+};
 // whether an id is listed twice.  Whole warp.
 __device__ __forceinline__ bool listed_twice(const ListIn& in, int lane) {
   bool twice = false;
@@ -168,7 +182,8 @@ __device__ __forceinline__ bool listed_twice(const ListIn& in, int lane) {
 struct ListPre {
   float p[2], lt[2];     // probabilities and their logarithms
   float sum;             // of p
-  float rho, l_rho, mass;
+  float rho, l_rho;      // without a class of the rest: two parts of what lt has too much
+  float mass;
   bool bad, bad_id, labelled;
 };
 // Whole warp.
@@ -193,13 +208,16 @@ __device__ __forceinline__ void list_pre(const DistillArgs& d, const ListIn& in,
     const float tm = warp_max(fmaxf(on[0] ? in.t[0] : -INFINITY, on[1] ? in.t[1] : -INFINITY));
 #pragma unroll
     for (int h = 0; h < 2; ++h) o.p[h] = on[h] ? expf(in.t[h] - tm) : 0.f;
-    const float P = warp_sum(o.p[0] + o.p[1]), lP = logf(P), inv = __fdividef(1.f, P);
+    const float P = warp_sum(o.p[0] + o.p[1]), inv = __fdividef(1.f, P);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      o.lt[h] = (in.t[h] - tm) - lP;
+      o.lt[h] = in.t[h] - tm;
       o.p[h] *= inv;
     }
     if (tm > -INFINITY) {
+      const LogSum l(P);
+      o.rho = l.e * LN2;
+      o.l_rho = fmaf(l.e, LN2, -o.rho) + (l.e * LN2_LOW + l.f * LN2);
       o.sum = 1.f;
       o.mass = expf(tm) * P;
     }
@@ -251,20 +269,6 @@ __device__ __forceinline__ void fetch_prepared(const DistillArgs& d, int64_t i, 
   o.labelled = f & 4u;
 }
 
-// log2 of a sum in two parts, e + f
-struct LogSum {
-  float e, f;
-  __device__ __forceinline__ explicit LogSum(float S) {
-    int ei = (int)(__float_as_uint(S) >> 23) - 127;
-    float m = __uint_as_float((__float_as_uint(S) & 0x7fffffu) | 0x3f800000u);
-    if (m > 1.41f) {
-      m *= 0.5f;
-      ++ei;
-    }
-    e = (float)ei;
-    f = log2f(m);
-  }
-};
 // ln 2 (c x - K - log2 S) in two parts.  A divergence sums differences of logarithms that nearly
 // cancel: what the roundings of c x - K (2^-24 of it) and of the logarithm would leave, 1e-6 of
 // a KL of 0.1, has to stay.  (c is the one that the row's sum was taken with: an error of it
@@ -420,11 +424,15 @@ __device__ __forceinline__ void list_math(const DistillArgs& d, int64_t row, con
     ce = v > 0.5f ? -log1pf(-less) : -log_v;
   }
   // the divergence
+  const float to = d.none ? pre.rho : 0.f, to_lo = d.none ? pre.l_rho : 0.f;
+  auto more = [&](const LogProb& v, float t) {  // log q - log p
+    return ((v.hi - t) + to) + (v.lo + to_lo);
+  };
   float kl = 0.f;
   if (!d.reverse) {
 #pragma unroll
     for (int h = 0; h < 2; ++h)
-      if (pre.p[h] > 0.f) kl += pre.p[h] * ((pre.lt[h] - l[h].hi) - l[h].lo);
+      if (pre.p[h] > 0.f) kl -= pre.p[h] * more(l[h], pre.lt[h]);
     kl = warp_sum(kl);
     if (klass && any) kl += pre.rho * (pre.l_rho - l_sigma);
   } else {
@@ -445,18 +453,18 @@ __device__ __forceinline__ void list_math(const DistillArgs& d, int64_t row, con
           av[h] *= per_Q;
         }
       }
-      float more[2];  // log q - log p
+      float far_off[2];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        more[h] = (l[h].hi - pre.lt[h]) + l[h].lo;
-        if (av[h] > 0.f) kl += av[h] * more[h];
+        far_off[h] = more(l[h], pre.lt[h]);
+        if (av[h] > 0.f) kl += av[h] * far_off[h];
       }
       kl = warp_sum(kl);
       const float far = l_sigma - pre.l_rho;
       const bool out_there = klass && sigma > 0.f;
       if (out_there) kl += sigma * far;
 #pragma unroll
-      for (int h = 0; h < 2; ++h) av[h] = av[h] > 0.f ? av[h] * (more[h] - kl) : 0.f;
+      for (int h = 0; h < 2; ++h) av[h] = av[h] > 0.f ? av[h] * (far_off[h] - kl) : 0.f;
       if (out_there) b = sigma * (far - kl);
     }
     if (out) result();
