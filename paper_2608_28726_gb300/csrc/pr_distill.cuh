@@ -404,6 +404,54 @@ __device__ __forceinline__ void list_math(const DistillArgs& d, int64_t row, con
   LogProb l[2] = {LogProb(x[0], a.c2, K, log_S), LogProb(x[1], a.c2, K, log_S)};
   const LogSum log_R(R);
   const float l_sigma = ((k - K) + (log_R.e - log_S.e) + (log_R.f - log_S.f)) * LN2;
+  // the divergence
+  const float to = d.none ? pre.rho : 0.f, to_lo = d.none ? pre.l_rho : 0.f;
+  auto more = [&](const LogProb& v, float t) {  // log q - log p
+    return ((v.hi - t) + to) + (v.lo + to_lo);
+  };
+  float kl = 0.f;
+  if (!d.reverse) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      if (pre.p[h] > 0.f) kl -= pre.p[h] * more(l[h], pre.lt[h]);
+    kl = warp_sum(kl);
+    if (klass && any) kl += pre.rho * (pre.l_rho - l_sigma);
+  } else {
+    if (any) {  // (a and b add up to 0)
+      float off[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        av[h] = q[h];
+        off[h] = more(l[h], pre.lt[h]);
+      }
+      if (d.none) {  // q over the list
+        const float K1 = warp_max(fmaxf(on[0] ? x[0] * a.c2 : -INFINITY,
+                                        on[1] ? x[1] * a.c2 : -INFINITY));
+        if (K1 == -INFINITY) bad = true;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) av[h] = on[h] ? rescale2(fmaf(x[h], a.c2, -K1)) : 0.f;
+        const float Q = warp_sum(av[0] + av[1]), per_Q = __fdividef(1.f, Q);
+        const LogSum log_Q(Q);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          off[h] = more(LogProb(x[h], a.c2, K1, log_Q), pre.lt[h]);
+          av[h] *= per_Q;
+        }
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        if (av[h] > 0.f) kl += av[h] * off[h];
+      kl = warp_sum(kl);
+      const float far = l_sigma - pre.l_rho;
+      const bool out_there = klass && sigma > 0.f;
+      if (out_there) kl += sigma * far;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) av[h] = av[h] > 0.f ? av[h] * (off[h] - kl) : 0.f;
+      if (out_there) b = sigma * (far - kl);
+    }
+    if (out) result();
+    if (out_bar && lane == 0) bar_arrive(out_bar);
+  }
   // the label, from 1 - q where that is small
   float ce = 0.f;
   if (a.chosen) {
@@ -422,53 +470,6 @@ __device__ __forceinline__ void list_math(const DistillArgs& d, int64_t row, con
       log_v = __shfl_sync(FULL, y0 ? l[0].hi : l[1].hi, from);
     }
     ce = v > 0.5f ? -log1pf(-less) : -log_v;
-  }
-  // the divergence
-  const float to = d.none ? pre.rho : 0.f, to_lo = d.none ? pre.l_rho : 0.f;
-  auto more = [&](const LogProb& v, float t) {  // log q - log p
-    return ((v.hi - t) + to) + (v.lo + to_lo);
-  };
-  float kl = 0.f;
-  if (!d.reverse) {
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-      if (pre.p[h] > 0.f) kl -= pre.p[h] * more(l[h], pre.lt[h]);
-    kl = warp_sum(kl);
-    if (klass && any) kl += pre.rho * (pre.l_rho - l_sigma);
-  } else {
-    if (any) {  // (a and b add up to 0)
-      av[0] = q[0];
-      av[1] = q[1];
-      if (d.none) {  // q over the list
-        const float K1 = warp_max(fmaxf(on[0] ? x[0] * a.c2 : -INFINITY,
-                                        on[1] ? x[1] * a.c2 : -INFINITY));
-        if (K1 == -INFINITY) bad = true;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) av[h] = on[h] ? rescale2(fmaf(x[h], a.c2, -K1)) : 0.f;
-        const float Q = warp_sum(av[0] + av[1]), per_Q = __fdividef(1.f, Q);
-        const LogSum log_Q(Q);
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          l[h] = LogProb(x[h], a.c2, K1, log_Q);
-          av[h] *= per_Q;
-        }
-      }
-      float far_off[2];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        far_off[h] = more(l[h], pre.lt[h]);
-        if (av[h] > 0.f) kl += av[h] * far_off[h];
-      }
-      kl = warp_sum(kl);
-      const float far = l_sigma - pre.l_rho;
-      const bool out_there = klass && sigma > 0.f;
-      if (out_there) kl += sigma * far;
-#pragma unroll
-      for (int h = 0; h < 2; ++h) av[h] = av[h] > 0.f ? av[h] * (far_off[h] - kl) : 0.f;
-      if (out_there) b = sigma * (far - kl);
-    }
-    if (out) result();
-    if (out_bar && lane == 0) bar_arrive(out_bar);
   }
   bad |= pre.bad_id;
   if (bad) kl = ce = NAN;
@@ -598,7 +599,10 @@ __device__ __forceinline__ void put_end(T* g, int32_t v, int kind, const RowOut&
 }
 
 // Element `e` of a row in shared memory is no part of its sum.  The next copy into the place is the
-// async proxy's: the threads that wrote fence their writes before the place is given back.
+// async proxy's: a fence lies between, of the thread that issues the copy, which has no stores on
+// their way.  (Fences of the threads that write gradients waited for those: 1 to 2%.  In registers,
+// a loaded word's elements left out one by one: 9,000 rows of 151,936 bf16 with k = 64 1,045 us for
+// 953.)
 template <typename T>
 __device__ __forceinline__ void leave_out(unsigned char* row, int32_t e) {
   if constexpr (sizeof(T) == 2) reinterpret_cast<uint16_t*>(row)[e] = 0xff80u;
@@ -754,7 +758,10 @@ __global__ void __launch_bounds__(RG_NT, 2)
         const Share sh = share_of<T>(a, ref.x, P, p);
         const char* src = sh.x + sizeof(T) * sh.head + 16 * (int64_t)sh.w0;
         for (int32_t left = sh.w1 - sh.w0; left > 0; left -= RG_CHUNK) {
-          if (n >= places) wait(&empty[place], turn ^ 1u);
+          if (n >= places) {
+            wait(&empty[place], turn ^ 1u);
+            fence_async();
+          }
           if (ok && lane == 0) {
             const uint32_t bytes = 16u * (uint32_t)min(RG_CHUNK, left);
             bar_expect(&full[place], bytes);
@@ -910,11 +917,10 @@ __global__ void __launch_bounds__(RG_NT, 2)
                   v[q] = make_uint4(Tr::NEG_WORD, Tr::NEG_WORD, Tr::NEG_WORD, Tr::NEG_WORD);
             }
             add_words<T>(k, S, v, a.c2, w == sh.w0);
-            // The place is given back once every lane's words are in its sum: given back right
-            // after their loads, with a chunk's listed tokens just left out, one row in 2,000 of
-            // V = 262,144 fp32 k = 64 summed some of the next chunk.  (Not a time's difference.)
             if (!HOLD) {
-              if (chunks & 1u) fence_async();
+              // The place is given back once every lane's words are in its sum: given back right
+              // after their loads, with a chunk's listed tokens just left out, one row in 2,000
+              // of V = 262,144 fp32 k = 64 summed some of the next chunk.  (No time between them.)
               __syncwarp();
               if (lane == 0) bar_arrive(&empty[place]);
             }
@@ -957,7 +963,6 @@ __global__ void __launch_bounds__(RG_NT, 2)
 #pragma unroll
             for (int q = 0; q < RG_W; ++q) v[q] = make_uint4(0u, 0u, 0u, 0u);
           }
-          if (chunks & 1u) fence_async();
           __syncwarp();
           if (lane == 0) bar_arrive(&empty[place0]);
           if (++place0 == places) place0 = 0;
