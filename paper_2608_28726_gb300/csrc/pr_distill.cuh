@@ -602,7 +602,7 @@ __device__ __forceinline__ void put_end(T* g, int32_t v, int kind, const RowOut&
 // async proxy's: a fence lies between, of the thread that issues the copy, which has no stores on
 // their way.  (Fences of the threads that write gradients waited for those: 1 to 2%.  In registers,
 // a loaded word's elements left out one by one: 9,000 rows of 151,936 bf16 with k = 64 1,045 us for
-// 953.)
+// 930.)
 template <typename T>
 __device__ __forceinline__ void leave_out(unsigned char* row, int32_t e) {
   if constexpr (sizeof(T) == 2) reinterpret_cast<uint16_t*>(row)[e] = 0xff80u;
@@ -900,16 +900,21 @@ __global__ void __launch_bounds__(RG_NT, 2)
           for (int32_t w = sh.w0; w < sh.w1; w += RG_CHUNK, chunks >>= 1) {
             wait(&full[place], turn);
             unsigned char* const here = ring + (size_t)place * RG_BYTES;
-            if (chunks & 1u) {
-#pragma unroll
-              for (int h = 0; h < 3; ++h)
-                if (within(own.e[h], w)) leave_out<T>(here, own.e[h] - w * Tr::VEC);
-              __syncwarp();
-            }
             const uint4* st = reinterpret_cast<const uint4*>(here) + at;
             uint4 v[RG_W];
 #pragma unroll
             for (int q = 0; q < RG_W; ++q) v[q] = st[32 * RG_NW * q];
+            // (The loads come first: most chunks hold none of a warp's tokens.  9,000 rows of
+            // 151,936 bf16, k = 32: 907 us, with the branch ahead of them 933.)
+            if (chunks & 1u) {
+              __syncwarp();
+#pragma unroll
+              for (int h = 0; h < 3; ++h)
+                if (within(own.e[h], w)) leave_out<T>(here, own.e[h] - w * Tr::VEC);
+              __syncwarp();
+#pragma unroll
+              for (int q = 0; q < RG_W; ++q) v[q] = st[32 * RG_NW * q];
+            }
             if (w + RG_CHUNK > sh.w1) {
 #pragma unroll
               for (int q = 0; q < RG_W; ++q)
