@@ -232,7 +232,7 @@ __device__ __forceinline__ void list_pre(const DistillArgs& d, const ListIn& in,
     const Pair s = warp_sum(v[0] + v[1]);
     o.sum = o.mass = s.hi;
     o.rho = fmaxf((1.f - s.hi) - s.lo, DS_RHO);
-    o.l_rho = logf(o.rho);
+    o.l_rho = o.rho > 0.5f ? log1pf(-s.hi) : logf(o.rho);
   }
 }
 
@@ -356,8 +356,9 @@ __device__ __forceinline__ void list_math(const DistillArgs& d, int64_t row, con
   q[1] = on[1] ? e[1] * inv : 0.f;
   const float E = listed + (any ? m : 0.f), sigma = Rk * inv, not_y = R0 * f + E;
   const bool klass = !d.none && rest;
-  float av[2] = {0.f, 0.f}, b = 0.f, kA = 0.f;
-  // the gradient, from a (av) and b, whose sum is kA
+  float av[2] = {0.f, 0.f}, b = 0.f, a_all = 0.f, kA = 0.f;
+  // the gradient, from a (av), its sum a_all, b, and A = a_all + b (kA).  b - A sigma is taken as
+  // b (1 - sigma) - sigma sum a: sigma and rho near 1 differ by what the lists' masses do.
   auto result = [&]() {
     const float kc = d.kl_coef, cc = a.chosen ? d.ce_coef : 0.f;
     const float w = wt * (a.grad_scale * a.inv_t), A = (kc != 0.f ? kc * kA : 0.f) - cc;
@@ -382,10 +383,11 @@ __device__ __forceinline__ void list_math(const DistillArgs& d, int64_t row, con
       o.K = k;
       o.M = 0.f;
       const float per_R = rest ? __fdividef(1.f, R) : 0.f;
-      o.nk = nan ? NAN : w * (bc - A * sigma) * per_R;
+      const float sum_a = kc != 0.f ? kc * a_all : 0.f, ba = bc * (E * inv);
+      o.nk = nan ? NAN : w * (ba - (sum_a - cc) * sigma) * per_R;
       o.mode = o.nk == 0.f ? ROW_ZERO : ROW_FAST;
       // q_y (b / sigma - kA) - ce (1 - q_y)
-      o.gy = nan ? NAN : w * (ey * per_R * (bc - (A + cc) * sigma) - cc * (not_y * inv));
+      o.gy = nan ? NAN : w * (ey * per_R * (ba - sum_a * sigma) - cc * (not_y * inv));
       *out = o;
     }
     __syncwarp();
@@ -395,7 +397,8 @@ __device__ __forceinline__ void list_math(const DistillArgs& d, int64_t row, con
       av[0] = -pre.p[0];
       av[1] = -pre.p[1];
       b = klass ? -pre.rho : 0.f;
-      kA = b - pre.sum;
+      a_all = -pre.sum;
+      kA = b + a_all;
     }
     if (out) result();
     if (out_bar && lane == 0) bar_arrive(out_bar);
@@ -403,7 +406,8 @@ __device__ __forceinline__ void list_math(const DistillArgs& d, int64_t row, con
   const LogSum log_S(S);
   LogProb l[2] = {LogProb(x[0], a.c2, K, log_S), LogProb(x[1], a.c2, K, log_S)};
   const LogSum log_R(R);
-  const float l_sigma = ((k - K) + (log_R.e - log_S.e) + (log_R.f - log_S.f)) * LN2;
+  const float l_sigma = sigma > 0.5f ? log1pf(-E * inv)
+      : ((k - K) + (log_R.e - log_S.e) + (log_R.f - log_S.f)) * LN2;
   // the divergence
   const float to = d.none ? pre.rho : 0.f, to_lo = d.none ? pre.l_rho : 0.f;
   auto more = [&](const LogProb& v, float t) {  // log q - log p
@@ -425,16 +429,15 @@ __device__ __forceinline__ void list_math(const DistillArgs& d, int64_t row, con
         off[h] = more(l[h], pre.lt[h]);
       }
       if (d.none) {  // q over the list
-        const float K1 = warp_max(fmaxf(on[0] ? x[0] * a.c2 : -INFINITY,
-                                        on[1] ? x[1] * a.c2 : -INFINITY));
-        if (K1 == -INFINITY) bad = true;
+        const float xm = warp_max(fmaxf(on[0] ? x[0] : -INFINITY, on[1] ? x[1] : -INFINITY));
+        if (xm == -INFINITY) bad = true;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) av[h] = on[h] ? rescale2(fmaf(x[h], a.c2, -K1)) : 0.f;
+        for (int h = 0; h < 2; ++h) av[h] = on[h] ? rescale2((x[h] - xm) * a.c2) : 0.f;
         const float Q = warp_sum(av[0] + av[1]), per_Q = __fdividef(1.f, Q);
         const LogSum log_Q(Q);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          off[h] = more(LogProb(x[h], a.c2, K1, log_Q), pre.lt[h]);
+          off[h] = more(LogProb(x[h] - xm, a.c2, 0.f, log_Q), pre.lt[h]);
           av[h] *= per_Q;
         }
       }
@@ -448,6 +451,7 @@ __device__ __forceinline__ void list_math(const DistillArgs& d, int64_t row, con
 #pragma unroll
       for (int h = 0; h < 2; ++h) av[h] = av[h] > 0.f ? av[h] * (off[h] - kl) : 0.f;
       if (out_there) b = sigma * (far - kl);
+      a_all = -b;
     }
     if (out) result();
     if (out_bar && lane == 0) bar_arrive(out_bar);
