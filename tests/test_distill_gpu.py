@@ -287,6 +287,50 @@ def test_small_rests_and_sure_rows_keep_their_digits(B, ctx):
             assert np.abs(g.double().cpu().numpy()[1, :k] / go[1, :k] - 1).max() < 2e-3
 
 
+@pytest.mark.parametrize("n,V", [(40, 30000), (900, 3000)])
+@pytest.mark.parametrize("loss", [0, 1])
+def test_lists_that_hold_little_of_a_row(B, ctx, n, V, loss):
+    """Soft rows whose lists hold 1e-4 to 1e-2 of the mass.  Exponentials are within 2^-22 and their
+    exponents of up to 30 within 30 x 2^-24, so probabilities and listed masses are within 2e-6 of
+    themselves and log q within 2e-6: KL, a sum of P (log p - log q) and of logarithms of 1 - P
+    and 1 - E, within 4e-6 (P + E); the rest's factor b - A sigma, a difference of E's and P's
+    multiples (forward) or of the two logarithms, within as much, and its q within 4e-6."""
+    T, k = 8.0, 3
+    gen = torch.Generator("cuda").manual_seed(V + loss)
+    x = 3 * torch.randn(n, V, generator=gen, device="cuda")
+    ids, sent = B.pr_top_logits(ctx, 1.1 * x + torch.randn(n, V, generator=gen, device="cuda"), k, temperature=T)
+    _, kl, grad = B.pr_distill_loss(ctx, x, ids, sent, temperature=T, loss=loss, grad_scale=float(n))
+    lq = torch.log_softmax(x.double() / T, 1)
+    at, q = ids.long(), lq.exp()
+    l, t = lq.gather(1, at), sent.double()
+    P, E = t.exp().sum(1), l.exp().sum(1)
+    l_rho, l_sigma = torch.log1p(-P), torch.log1p(-E)
+    if loss == 0:
+        want = (t.exp() * (t - l)).sum(1) + (1 - P) * (l_rho - l_sigma)
+        a, b = -t.exp(), P - 1
+    else:
+        want = (l.exp() * (l - t)).sum(1) + (1 - E) * (l_sigma - l_rho)
+        a, b = l.exp() * (l - t - want[:, None]), (1 - E) * (l_sigma - l_rho - want)
+    assert ((kl.double() - want).abs() <= 4e-6 * (P + E)).all()
+    A, sigma = a.sum(1) + b, 1 - E
+    g = q * ((b - A * sigma) / sigma)[:, None]
+    tol = q * (8e-6 * (P + E) / sigma)[:, None]
+    g.scatter_(1, at, a - A[:, None] * l.exp())
+    # (reverse: a sums k terms with log q - log p, here below 4 in size)
+    tol.scatter_(1, at, 4e-6 * (5 if loss else 1) * (l.exp() + t.exp()))
+    assert ((grad.double() * T - g).abs() <= tol + 2. ** -23 * g.abs()).all()
+
+
+def test_one_listed_token_is_the_whole_distribution(B, ctx):
+    gen = torch.Generator("cuda").manual_seed(6)
+    for n, V in ((6, 50000), (700, 4001)):
+        x = 20 * torch.randn(n, V, generator=gen, device="cuda")
+        ids, sent = B.pr_top_logits(ctx, x + torch.randn(n, V, generator=gen, device="cuda"), 1, temperature=0.7)
+        _, kl, grad = B.pr_distill_loss(ctx, x, ids, sent, temperature=0.7, loss=B.PR_DISTILL_REVERSE,
+                                        rest=B.PR_REST_NONE)
+        assert (kl == 0).all() and (grad == 0).all()
+
+
 def test_coefficients_of_nothing(B, ctx):
     """A term of coefficient 0 is a statistic alone, even an infinite one."""
     n, V, k = 6, 300, 5
