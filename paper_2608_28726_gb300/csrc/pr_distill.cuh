@@ -56,8 +56,7 @@ constexpr uint32_t DS_MASKED = sizeof(T) == 2 ? 0xff80u : 0xff800000u;  // -inf
 // A listed row's entries and scalars; then, once those are there, its logits at them.  Two steps,
 // as each waits for memory: a row's entries are fetched two rows ahead, its logits one.
 __device__ __forceinline__ ListIn fetch_list(const DistillArgs& d, const Rows& rows,
-    const int4& ref,
-                                             int lane) {
+                                             const int4& ref, int lane) {
   ListIn in;
   in.y = ref.z;
   in.count = 1;
@@ -188,7 +187,7 @@ struct ListPre {
 };
 // Whole warp.
 __device__ __forceinline__ void list_pre(const DistillArgs& d, const ListIn& in, ListPre& o,
-                                             int lane) {
+                                         int lane) {
   const LossArgs& a = d.a;
   bool bad_id = a.chosen && !(in.y >= 0 && (int64_t)in.y < a.vocab), bad = false, labelled = false;
   bool on[2];
@@ -343,8 +342,8 @@ __device__ __forceinline__ void list_math(const DistillArgs& d, int64_t row, con
   const float f = rest ? rescale2(k - K) : 0.f, Rk = R * f, eyk = ey * f;
   // the largest listed term stays out of the sum of the others: 1 - q of it is others / S
   const float m = warp_max(fmaxf(e[0], e[1]));
-  const unsigned w0 = __ballot_sync(FULL, on[0] && e[0] == m), w1 = __ballot_sync(FULL, on[1] &&
-      e[1] == m);
+  const unsigned w0 = __ballot_sync(FULL, on[0] && e[0] == m);
+  const unsigned w1 = __ballot_sync(FULL, on[1] && e[1] == m);
   const int first = w0 ? __ffs(w0) - 1 : w1 ? 32 + __ffs(w1) - 1 : -1;  // its place
   const bool any = first >= 0;
   const bool is[2] = {first == lane, first == 32 + lane};
@@ -597,8 +596,7 @@ __device__ __forceinline__ void add_rest_ends(const DistillArgs& d, const Share&
 }
 template <typename T>
 __device__ __forceinline__ void put_end(T* g, int32_t v, int kind, const RowOut& o,
-    const float* list,
-                                        float c2, float edge) {
+                                        const float* list, float c2, float edge) {
   if (v >= 0) put(g + v, kind >= 0 ? list[kind] : kind == DS_LABEL ? o.gy : grad1(o, c2, edge));
 }
 
@@ -652,18 +650,17 @@ __device__ __forceinline__ Ids fetch_ids(const DistillArgs& d, const int4& ref, 
 }
 template <int VEC>
 __device__ __forceinline__ Mine mine_of(const DistillArgs& d, const Share& s, const Ids& ids,
-    int32_t y,
-                                        int warp, int lane) {
+                                        int32_t y, int warp, int lane) {
   Mine m;
   m.chunks = 0u;
   const int32_t l[2] = {ids.t[0] == -INFINITY ? -1 : ids.id[0],
-      ids.t[1] == -INFINITY ? -1 : ids.id[1]};
+                        ids.t[1] == -INFINITY ? -1 : ids.id[1]};
   const bool listed = l[0] == y || l[1] == y;
   const bool apart = d.a.chosen && !__any_sync(FULL, listed);
 #pragma unroll
   for (int h = 0; h < 3; ++h) {
     const int32_t id = h < 2 ? l[h] : apart && lane == 0 ? y : -1;
-    const int32_t e = id - s.head, w = e / VEC - s.w0;  // (a negative e divides to a word of its own check)
+    const int32_t e = id - s.head, w = e / VEC - s.w0;  // (`in` looks at a negative e)
     const bool in = id >= s.head && w >= 0 && e / VEC < s.w1;
     const bool here = in && ((w % (32 * RG_NW)) >> 5) == warp;
     m.e[h] = here ? e : -1;
@@ -682,7 +679,9 @@ struct DistillCtl {
 // then the bars of the ring's places (landed, read), the warps' (k, R) [RG_SLOTS][C][RG_NW], the
 // lists' entries of the gradient [1 + lag][DS_MAX], and the ring
 constexpr size_t DS_BARS = (sizeof(DistillCtl) + 15) / 16 * 16;
-__host__ __device__ constexpr size_t distill_sums(int places) { return DS_BARS + 16 * (size_t)places; }
+__host__ __device__ constexpr size_t distill_sums(int places) {
+  return DS_BARS + 16 * (size_t)places;
+}
 __host__ __device__ constexpr size_t distill_list(int C, int places) {
   return distill_sums(places) + (size_t)RG_SLOTS * C * RG_NW * sizeof(float2);
 }

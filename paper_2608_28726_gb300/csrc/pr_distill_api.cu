@@ -23,8 +23,8 @@ const void* ring_kernel(bool hold, bool own) {
                      : reinterpret_cast<const void*>(&prk::distill_ring<T, false, false>));
 }
 const void* ring_kernel(pr_dtype dt, bool hold, bool own) {
-  return dt == PR_DTYPE_BF16 ? ring_kernel<__nv_bfloat16>(hold, own) : ring_kernel<float>(hold,
-      own);
+  return dt == PR_DTYPE_BF16 ? ring_kernel<__nv_bfloat16>(hold, own)
+                             : ring_kernel<float>(hold, own);
 }
 
 const void* rows_kernel(pr_dtype dt, bool hold) {
@@ -49,8 +49,7 @@ pr_status setup(pr_ctx* c) {
                                      cudaFuncAttributeMaxDynamicSharedMemorySize,
                                      (int)ring_bytes(prk::RG_MOST, 8, 0, false)));
       PR_CUDA(cudaFuncSetAttribute(rows_kernel(dt, hold),
-          cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                   (int)HALF));
+                                   cudaFuncAttributeMaxDynamicSharedMemorySize, (int)HALF));
     }
   for (int i = 0; i < 4; ++i)
     for (int whole = 0; whole < 2; ++whole) {
@@ -89,8 +88,7 @@ pr_status launch_lists(pr_ctx* c, prk::DistillArgs& d, pr_dtype dt, cudaStream_t
 }
 
 pr_status launch_ring(pr_ctx* c, prk::DistillArgs& d, pr_dtype dt, const RingShape& shape,
-    bool hold,
-                      cudaStream_t s) {
+                      bool hold, cudaStream_t s) {
   int places = shape.places, parts = 1, cluster = 1 << shape.split;
   int64_t groups = shape.groups;
   bool full = shape.full;
@@ -178,7 +176,8 @@ pr_status pr_distill_loss(pr_ctx* c, const void* logits, pr_dtype dt, int64_t n_
     return PR_OK;
   }
   if ((st = setup(c)) != PR_OK) return st;
-  const RingShape ring = choose_ring(c->distill_places, dt, n_rows, vocab);  // (PR_DISTILL_MAX_VOCAB: it holds)
+  // (up to PR_DISTILL_MAX_VOCAB a cluster holds the row)
+  const RingShape ring = choose_ring(c->distill_places, dt, n_rows, vocab);
   if ((st = workspace(c, d.a, std::max(ring.groups, forward_grid(c)), false, false)) != PR_OK)
     return st;
   d.a.own = own_list(d.a);

@@ -80,8 +80,8 @@ __device__ __forceinline__ float nm_block_sum(float v, float* part) {
 // stays busy while rows are summed.  Rows of up to 16 words are read by their threads.  Rows of up
 // to 32 threads are summed by shuffles, wider ones through shared memory with a barrier of the
 // row's threads alone, so that the CTA's other rows go on meanwhile.  The weights are in shared
-// memory, too. 8,847 x 3,584 bf16: forward with a residual 48 us, 5.3 TB/s of its four passes over
-// the rows, backward 60; what bounds both is the rows' chain of two sums (one) and some 2,000
+// memory, too.  8,847 x 3,584 bf16: forward with a residual 49 us, 5.2 TB/s of its four passes over
+// the rows, backward 54; what bounds both is the rows' chain of two sums (one) and some 2,000
 // instructions a row, not memory.
 //
 // Columns of thread t's word i: VEC neighbours from (t + i L) VEC on; in rows off the 16-byte grid,
@@ -100,8 +100,9 @@ struct RowWord {
     return WHOLE ? (t + i * L) * VEC + j : t + (i * VEC + j) * L;
   }
   // whether word i has all of its columns, or any
-  static __device__ __forceinline__ bool full(int t, int i, int d) { return column(t, i,
-      VEC - 1) < d; }
+  static __device__ __forceinline__ bool full(int t, int i, int d) {
+    return column(t, i, VEC - 1) < d;
+  }
   static __device__ __forceinline__ bool some(int t, int i, int d) { return column(t, i, 0) < d; }
   __device__ __forceinline__ void zero() {
 #pragma unroll
@@ -268,7 +269,8 @@ struct RowStages {
   }
   // the words that a row touches
   __device__ __forceinline__ uint32_t size(const T* row) const {
-    return ((uint32_t)(reinterpret_cast<uintptr_t>(row) & 15u) + (uint32_t)d * (uint32_t)sizeof(T) + 15u) & ~15u;
+    const uint32_t head = (uint32_t)(reinterpret_cast<uintptr_t>(row) & 15u);
+    return (head + (uint32_t)d * (uint32_t)sizeof(T) + 15u) & ~15u;
   }
   __device__ __forceinline__ void expect(int i, uint32_t all) { bar_expect(&full[i], all); }
   __device__ __forceinline__ void copy(int i, int j, const T* row) {

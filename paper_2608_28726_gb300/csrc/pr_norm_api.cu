@@ -77,8 +77,7 @@ constexpr size_t norm_room(int ctas) { return 228 * 1024 / ctas - 1024 - 512; }
 // The shared memory of a CTA, `ctas` of which are to be on an SM: the weights (`weights` arrays),
 // and places for k rows, at least `least`.  Returns whether it fits.
 bool stage(prk::NormArgs& a, const NormShape& shape, pr_dtype dt, int ctas, int k, int weights,
-    int least,
-           size_t& smem) {
+           int least, size_t& smem) {
   a.row_bytes = (int32_t)((a.d * (int64_t)esize(dt) + 30) / 16 * 16);  // wherever a row begins
   a.stages = 0;
   smem = (size_t)weights * ((a.d + 7) / 8 * 8) * (a.wide_w ? 4 : 2);
@@ -98,15 +97,15 @@ pr_status setup(pr_ctx* c) {
     for (const NormShape& s : {forward_of<float>(words), forward_of<__nv_bfloat16>(words),
                                backward_of<float>(words), backward_of<__nv_bfloat16>(words)})
       for (const void* kernel : s.kernel)
-        if (kernel) PR_CUDA(cudaFuncSetAttribute(kernel,
-            cudaFuncAttributeMaxDynamicSharedMemorySize, (int)norm_room(1)));
+        if (kernel)
+          PR_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                       (int)norm_room(1)));
   c->norm_ready = true;
   return PR_OK;
 }
 
 pr_status launch(pr_ctx* c, const void* kernel, dim3 grid, unsigned threads, size_t smem,
-    void** args,
-                 cudaStream_t s) {
+                 void** args, cudaStream_t s) {
   cudaLaunchConfig_t cfg;
   memset(&cfg, 0, sizeof cfg);
   cfg.gridDim = grid;
@@ -223,10 +222,9 @@ pr_status pr_layernorm_backward(pr_ctx* c, const void* dy, int64_t dy_stride, co
   if (n_rows < 0 || n_rows > 0x7fffffffLL || d < 1 || d > PR_NORM_MAX_D) return PR_ERR_INVALID_ARG;
   if (!weight || !on_grid(weight, wdt) || (!dx && !dweight && !dbias)) return PR_ERR_INVALID_ARG;
   if (n_rows > 0) {
-    if (!rows_ok(dy, d, dy_stride, dt) || !rows_ok(x, d, x_stride, dt) || !rstd || (!mean &&
-        !rms) ||
-        (dtotal && !rows_ok(dtotal, d, dtotal_stride, dt)) || (dx && !rows_ok(dx, d, dx_stride,
-            dt)))
+    if (!rows_ok(dy, d, dy_stride, dt) || !rows_ok(x, d, x_stride, dt) || !rstd ||
+        (!mean && !rms) || (dtotal && !rows_ok(dtotal, d, dtotal_stride, dt)) ||
+        (dx && !rows_ok(dx, d, dx_stride, dt)))
       return PR_ERR_INVALID_ARG;
     if (dx && (!same_rows(dx, dx_stride, dy, dy_stride) || !same_rows(dx, dx_stride, x, x_stride) ||
                !same_rows(dx, dx_stride, dtotal, dtotal_stride)))
@@ -264,9 +262,9 @@ pr_status pr_layernorm_backward(pr_ctx* c, const void* dy, int64_t dy_stride, co
   a.accumulate = accumulate ? 1 : 0;
   a.vec_w = aligned16(weight);
   a.ctx_flags = c->flags;
-  const bool whole = d * (int64_t)esize(dt) % 16 == 0 && on_words(x, x_stride, dt) && on_words(dy,
-      dy_stride, dt) &&
-                     on_words(dtotal, dtotal_stride, dt) && on_words(dx, dx_stride, dt);
+  const bool whole = d * (int64_t)esize(dt) % 16 == 0 && on_words(x, x_stride, dt) &&
+                     on_words(dy, dy_stride, dt) && on_words(dtotal, dtotal_stride, dt) &&
+                     on_words(dx, dx_stride, dt);
   const int64_t words = (d * (int64_t)esize(dt) + 15) / 16;
   const NormShape shape = dt == PR_DTYPE_BF16 ? backward_of<__nv_bfloat16>(words)
       : backward_of<float>(words);

@@ -108,17 +108,15 @@ pr_status pr_top_logits(pr_ctx* c, const void* logits, pr_dtype dt, int64_t n_ro
     for (pr_dtype t : {PR_DTYPE_F32, PR_DTYPE_BF16}) {
       for (bool words : {false, true})
         PR_CUDA(cudaFuncSetAttribute(ring_kernel(t, words),
-            cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                     (int)SM_BYTES));
+                                     cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SM_BYTES));
       PR_CUDA(cudaFuncSetAttribute(short_kernel(t), cudaFuncAttributeMaxDynamicSharedMemorySize,
                                    (int)HALF_BYTES));
     }
     c->top_ready = true;
   }
   prk::LossArgs l;
-  fill(l, c, logits, n_rows, vocab, row_stride, nullptr, nullptr, nullptr, 0, nullptr,
-      temperature, 1.f,
-       nullptr, logp, nullptr, 0);
+  fill(l, c, logits, n_rows, vocab, row_stride, nullptr, nullptr, nullptr, 0, nullptr, temperature,
+       1.f, nullptr, logp, nullptr, 0);
   int kk = k;
   float limit = big;
   int32_t* out = ids;
@@ -137,7 +135,7 @@ pr_status pr_top_logits(pr_ctx* c, const void* logits, pr_dtype dt, int64_t n_ro
     void* args[] = {&l, &kk, &limit, &out, &places, &gm};
     st = launch(ring_kernel(dt, shape.words),
                 (unsigned)(groups * shape.cluster), prk::TR_NT, shape.smem,
-                    (unsigned)shape.cluster, args, s,
+                (unsigned)shape.cluster, args, s,
                 n_rows < groups + 1 && groups * shape.cluster < at_once);
     return st == PR_OK ? timing_mark(c, s) : st;
   }
