@@ -433,7 +433,7 @@ __global__ void __launch_bounds__(L > NR_NT ? L : NR_NT, L > NR_NT ? 1 : 2)
     dnorm_rows(const __grid_constant__ NormArgs a) {
   using W = RowWord<T, L, WHOLE>;
   constexpr int VEC = W::VEC, H = VEC / 2, NT = L > NR_NT ? L : NR_NT, ROWS = NT / L;
-  constexpr bool KEEP = N <= 2;  // xhat and g of a row's words stay in registers
+  constexpr bool KEEP = N <= 3;  // xhat and g of a row's words stay in registers
   extern __shared__ __align__(16) unsigned char nm_raw[];
   __shared__ float2 part[2][32];
   const int in_row = threadIdx.x % L, group = threadIdx.x / L;

@@ -93,7 +93,7 @@ def check_backward(got, dy, h, w, mean, rstd, dtotal, rms, dtype, before=(0.0, 0
 SIZES = [(1, 1), (3, 2), (5, 7), (4, 8), (33, 9), (7, 16), (70, 33), (257, 64), (5, 100), (9, 256),
          (400, 257), (17, 512), (3, 1000), (301, 1024), (30, 1025), (650, 2048), (7, 2056), (40, 3584),
          (5, 3585), (160, 4096), (3, 5000), (330, 7168), (2, 8192), (9, 8200), (3, 12288), (4, 16384), (200, 12001), (160, 16384), (170, 8192), (161, 16000),
-         (3, 16385), (2, 16392), (2, 40000), (1, 100003)]
+         (3, 16385), (2, 16392), (2, 40000), (1, 100003), (320, 4288), (330, 5003), (310, 2501), (152, 6144), (153, 6144)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
