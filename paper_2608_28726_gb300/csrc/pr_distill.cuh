@@ -379,11 +379,17 @@ __device__ __forceinline__ void list_math(const DistillArgs& d, int64_t row, con
     }
     if (lane == 0) {
       RowOut o;
-      o.K = k;
       o.M = 0.f;
       const float per_R = rest ? __fdividef(1.f, R) : 0.f;
       const float sum_a = kc != 0.f ? kc * a_all : 0.f, ba = bc * (E * inv);
-      o.nk = nan ? NAN : w * (ba - (sum_a - cc) * sigma) * per_R;
+      // n 2^(c x - k) = n R / r 2^-lost 2^(c x - K), with R = r 2^e and K = k + e less what its
+      // rounding lost: n by itself is denormal, or 0, where a small weight meets a sum of 1e30
+      const float r = __uint_as_float((__float_as_uint(R) & 0x7fffffu) | 0x3f800000u);
+      const float up = rest ? (float)((int)(__float_as_uint(R) >> 23) - 127) : 0.f;
+      o.K = k + up;
+      const float t = o.K - k, lost = (k - (o.K - t)) + (up - t);
+      const float per_r = rest ? __fdividef(exp2f(-lost), r) : 0.f;
+      o.nk = nan ? NAN : w * (ba - (sum_a - cc) * sigma) * per_r;
       o.mode = o.nk == 0.f ? ROW_ZERO : ROW_FAST;
       // q_y (b / sigma - kA) - ce (1 - q_y)
       o.gy = nan ? NAN : w * (ey * per_R * (ba - sum_a * sigma) - cc * (not_y * inv));

@@ -550,3 +550,31 @@ def test_refusals(B, ctx):
     big = torch.empty(4, B.PR_DISTILL_MAX_VOCAB + 1, device="cuda")
     refused(big, i, s)
     assert B.launch_count() == n0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,V", [(6, 20001), (6, 150000), (640, 20001), (700, 3001)])
+@pytest.mark.parametrize("rise", [40.0, 66.0])
+def test_gradients_of_rows_that_rise(B, ctx, n, V, rise, dtype):
+    """Logits that rise along the row: the sum is against a reference far below the largest, up to
+    1e30, and the gradient's factor, a weight over that sum, is to keep its digits all the same.
+    Gradients of down to 1e-27 of the ordinary, to `check`'s tolerance of each row's own size."""
+    k = 5
+    g = np.random.Generator(np.random.PCG64(V + n))
+    x = np.linspace(-rise, 0.0, V)[None] + 0.2 * g.normal(size=(n, V))
+    x = torch.from_numpy(x.astype(np.float32)).to(TYPES[dtype])
+    x64 = x.double().numpy()
+    x = x.cuda()
+    ids = np.stack([g.permutation(V // 2)[:k] for _ in range(n)]).astype(np.int32)
+    sent = np.log(g.dirichlet(np.ones(k + 1), n)[:, :k]).astype(np.float32)
+    ch = g.integers(0, V, n).astype(np.int32)
+    for scale in (1.0, 1e-7, 1e-12, 1e-20):
+        for loss in (0, 1):
+            kw = dict(loss=loss, ce_coef=0.3, grad_scale=scale * n)
+            got = B.pr_distill_loss(ctx, x, to(ids), to(sent), chosen=to(ch), **kw)
+            want = D.distill(x64, ids, sent, ch, **kw)
+            grad, go, size = got[2].double().cpu().numpy(), want[2], want[4]
+            tol = 2e-4 * size + (2.0 ** -8 if dtype == "bf16" else 0) * np.abs(go) + 1e-37
+            tol += 1e-14 * size.max(axis=1, keepdims=True)
+            bad = ~(np.abs(grad - go) <= tol)
+            assert not bad.any(), (scale, loss, bad.sum(), grad[bad][:4], go[bad][:4], tol[bad][:4])
