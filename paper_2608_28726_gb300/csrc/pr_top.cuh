@@ -119,6 +119,7 @@ __device__ __forceinline__ void top_groups(TopList& l, const M* gm, int n, float
 struct TopSmem {
   float gm[TP_GROUPS];
   float2 part[TP_NT / 32];
+  float best[TP_NT / 32];
   uint64_t buf[64];
 };
 
@@ -131,12 +132,13 @@ __global__ void __launch_bounds__(TP_NT) top_rows(const TopArgs a, const int64_t
   const int64_t row = blockIdx.x;
   const T* x = reinterpret_cast<const T*>(a.logits) + row * a.row_stride;
   const int groups = (int)((a.vocab + group - 1) / group);
-  float k = -3e38f, S = 0.f;
+  float k = -3e38f, S = 0.f, best = -INFINITY;
   for (int g = tid; g < groups; g += TP_NT) {
     const int64_t v0 = g * group, v1 = min(a.vocab, v0 + group);
     float m = -INFINITY;
     for (int64_t v = v0; v < v1; ++v) m = fmaxf(m, Traits<T>::elem(x, v));
     sm.gm[g] = m;
+    best = fmaxf(best, m);
     const float top = fmaxf(k, m * a.c2);
     float e = 0.f;
     for (int64_t v = v0; v < v1; ++v) e += ex2(fmaf(Traits<T>::elem(x, v), a.c2, -top));
@@ -147,9 +149,14 @@ __global__ void __launch_bounds__(TP_NT) top_rows(const TopArgs a, const int64_t
   S *= exp2f(k - kw);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) S += __shfl_xor_sync(FULL, S, o);
-  if (lane == 0) sm.part[warp] = make_float2(kw, S);
+  best = warp_max(best);
+  if (lane == 0) {
+    sm.part[warp] = make_float2(kw, S);
+    sm.best[warp] = best;
+  }
   __syncthreads();
   if (warp > 0) return;
+  best = warp_max(lane < TP_NT / 32 ? sm.best[lane] : -INFINITY);
   const float2 p = lane < TP_NT / 32 ? sm.part[lane] : make_float2(-3e38f, 0.f);
   const float K = unord(__reduce_max_sync(FULL, ord(p.x)));
   float R = p.y * exp2f(p.x - K);
@@ -157,7 +164,7 @@ __global__ void __launch_bounds__(TP_NT) top_rows(const TopArgs a, const int64_t
   for (int o = 16; o > 0; o >>= 1) R += __shfl_xor_sync(FULL, R, o);
   int32_t* const ids = a.ids + row * a.k;
   float* const logp = a.logp + row * a.k;
-  if (!(K < a.big * a.c2) || !(K > -a.big * a.c2) || !(R > 0.f) || !(R < INFINITY)) {
+  if (!(best < a.big) || !(best > -a.big) || !(R > 0.f) || !(R < INFINITY)) {
     for (int j = lane; j < a.k; j += 32) {
       ids[j] = -1;
       logp[j] = NAN;
@@ -539,7 +546,8 @@ __global__ void __launch_bounds__(TR_NT, 3)
       for (uint32_t c = 0; c < C; ++c) best = max(best, C > 1 ? sm.lists[c][0] : sm.top[0]);
       const float K = best ? key_val(best) * a.c2 : -INFINITY;
       const float rows_sum = all.y * rescale2(all.x - K);
-      const bool bad = !(all.x < big * a.c2) || !(all.y < INFINITY) || !(all.y >= 0.f) || !best;
+      // (the border by the element itself: times c it is one with its neighbours)
+      const bool bad = !best || !(key_val(best) < big) || !(all.y < INFINITY) || !(all.y >= 0.f);
       const float log_sum = logf(rows_sum);
       auto give = [&](int j, uint64_t q) {
         out_ids[row * k + j] = bad || q == 0 ? -1 : (int32_t)key_idx(q);
@@ -678,7 +686,7 @@ __global__ void __launch_bounds__(32 * TS_MOST, 2)
     int32_t* const ids = out_ids + row * k;
     float* const logp = a.logp + row * k;
     const float best = warp_max(t1), K = best * a.c2;
-    if (!(ref < big * a.c2) || !(best > -big) || !(R >= 0.f) || !(R < INFINITY)) {
+    if (!(best < big) || !(best > -big) || !(R >= 0.f) || !(R < INFINITY)) {
       for (int j = lane; j < k; j += 32) {
         ids[j] = -1;
         logp[j] = NAN;

@@ -236,3 +236,25 @@ def test_refusals(B, ctx):
     ids, logp = B.pr_top_logits(ctx, x[:0], 5)
     assert ids.shape == (0, 5) and logp.shape == (0, 5)
     assert B.launch_count() == n0
+
+
+@pytest.mark.parametrize("temperature", [1.0, 0.41, 0.44, 0.47, 1000.0])
+@pytest.mark.parametrize("n,V", [(6, 1003), (6, 40000), (1000, 1003), (2, 6_500_001)])
+def test_the_border_of_infinity(B, ctx, n, V, temperature):
+    """x / T from 1e9 on is infinite, the value before it is not; the same below."""
+    big = torch.tensor(1e9 * temperature, dtype=torch.float32)
+    below = torch.nextafter(big, torch.zeros(()))
+    x = torch.empty(n, V, device="cuda").normal_(generator=torch.Generator("cuda").manual_seed(V))
+    x[0] = below                           # the largest finite one alone
+    x[1, :] = below
+    x[1, V - 2] = big                      # one infinite one among those
+    if n > 2:
+        x[2, 5] = below
+        x[3, 5] = big
+        x[4] = -big                        # nothing left
+        x[5] = -big
+        x[5, 7:9] = -below                 # two left
+    B.pr_ctx_flags(ctx, clear=True)
+    ids, logp = B.pr_top_logits(ctx, x, 20, temperature=temperature)
+    check(ids, logp, x, 20, temperature)
+    assert B.pr_ctx_flags(ctx, clear=True) == B.PR_FLAG_NONFINITE
