@@ -8,6 +8,7 @@
 
 #include "pr_ctx.h"
 #include "pr_norm.cuh"
+#include "pr_norm_host.h"
 
 using namespace prh;
 
@@ -75,23 +76,15 @@ NormShape backward_of(int64_t words, bool many) {
   return {{nullptr, nullptr}, false, 0, 0};
 }
 
-constexpr int NORM_STAGES = 4;  // at most
-// of an SM's 228 KB, less what a CTA has besides (1 KB of the system's, the sums)
-constexpr size_t norm_room(int ctas) { return 228 * 1024 / ctas - 1024 - 512; }
-// The shared memory of a CTA, `ctas` of which are to be on an SM: the weights (`weights` arrays),
-// and places for k rows, at least `least`.  Returns whether it fits.
+// `ctas` CTAs on an SM (see norm_stages): whether it fits
 bool stage(prk::NormArgs& a, const NormShape& shape, pr_dtype dt, int ctas, int k, int weights,
            int least, size_t& smem) {
-  a.row_bytes = (int32_t)((a.d * (int64_t)esize(dt) + 30) / 16 * 16);  // wherever a row begins
-  a.stages = 0;
-  smem = (size_t)weights * ((a.d + 7) / 8 * 8) * (a.wide_w ? 4 : 2);
-  if (!shape.staged) return true;
-  const int groups = std::max(shape.threads, prk::NR_NT) / shape.threads;
-  const size_t room = norm_room(ctas) - 128, place = (size_t)groups * k * a.row_bytes;
-  if (room < smem + least * place) return false;
-  a.stages = (int)std::min<size_t>(NORM_STAGES, (room - smem) / place);
-  smem += (size_t)(groups * a.stages * 8 + 127) / 128 * 128 + a.stages * place;
-  return true;
+  const int groups = shape.staged ? std::max(shape.threads, prk::NR_NT) / shape.threads : 0;
+  const NormStages s = norm_stages(a.d, esize(dt), a.wide_w ? 4 : 2, groups, ctas, k, weights, least);
+  a.row_bytes = s.row_bytes;
+  a.stages = s.stages;
+  smem = s.smem;
+  return s.fits;
 }
 
 // shared memory opt-ins, once per context
