@@ -51,7 +51,9 @@ NormShape forward_of(int64_t words) {
   if (words <= 512) return forward_shape<T, 128, 4>();
   if (words <= 1024) return forward_shape<T, 256, 4>();
   if (words <= 2048) return forward_shape<T, 512, 4>();
-  if (sizeof(T) == 4 && words <= 4096) return forward_shape<T, 512, 8>();
+  if constexpr (sizeof(T) == 4) {  // (wider bf16 rows: norm_wide)
+    if (words <= 4096) return forward_shape<T, 512, 8>();
+  }
   return {{nullptr, nullptr}, false, 0, 0};
 }
 template <typename T, int L, int N>
@@ -72,7 +74,9 @@ NormShape backward_of(int64_t words, bool many) {
   if (words <= 768 && many) return backward_shape<T, 256, 3>();
   if (words <= 1024) return backward_shape<T, 512, 2>();
   if (words <= 2048) return backward_shape<T, 512, 4>();
-  if (sizeof(T) == 4 && words <= 4096) return backward_shape<T, 512, 8>();
+  if constexpr (sizeof(T) == 4) {
+    if (words <= 4096) return backward_shape<T, 512, 8>();
+  }
   return {{nullptr, nullptr}, false, 0, 0};
 }
 

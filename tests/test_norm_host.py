@@ -67,3 +67,16 @@ def test_as_many_ctas_fit_an_sm_as_the_grid_counts_on(stages, esize, wsize):
 def test_rows_that_are_not_staged_take_their_weights_alone(stages):
     for d in (1, 7, 8, 64, 128):
         assert stages(d, 2, 4, 0, 1, 2, 2, 1)[:2] == (0, 2 * 4 * ((d + 7) // 8 * 8))
+
+
+def test_no_kernel_is_compiled_that_no_width_takes():
+    """bf16 rows of more than 2,048 words are read again instead."""
+    nm = shutil.which("nm")
+    if nm is None:
+        pytest.skip("no nm")
+    from paper_2608_28726_gb300 import build as prbuild
+    names = subprocess.run([nm, "-C", "--defined-only", prbuild.build()], check=True, text=True,
+                           capture_output=True).stdout
+    rows = {w for w in names.splitlines() if "norm_rows<" in w}
+    assert any("norm_rows<float, 512, 8, true, true>" in w for w in rows)
+    assert not [w for w in rows if "norm_rows<__nv_bfloat16, 512, 8" in w]
