@@ -1245,12 +1245,13 @@ __global__ void __launch_bounds__(RG_NT, 2)
             for (int q = 0; q < RG_W; ++q)
               if (w + 32 * RG_NW * q + at == yw) v[q] = without<T>(v[q], yj);
           }
+          add_words<T>(k, S, v, a.c2, w == sh.w0);
           if (!HOLD) {
-            __syncwarp();  // every lane has its words
+            // (once every lane's words are summed, not only loaded: see distill_ring)
+            __syncwarp();
             if (lane == 0) bar_arrive(&sm.empty[place]);
           }
           step();
-          add_words<T>(k, S, v, a.c2, w == sh.w0);
         }
         float R;
         join(make_float2(k, S.x + S.y), 1.f, k, R);

@@ -963,3 +963,17 @@ def test_no_advantage_under_a_ratio_out_of_range(B, ctx, n, V, dtype):
     st, lp, gr = B.pr_policy_loss(ctx, x, to(ch), to(adv), old_logp=to(old))
     assert torch.isnan(st[0]) and torch.isnan(gr[1]).all() and torch.isfinite(gr[0]).all()
     assert B.pr_ctx_flags(ctx, clear=True) == B.PR_FLAG_NONFINITE
+
+
+@pytest.mark.parametrize("n,V,dtype", [(2100, 262144, "f32"), (2500, 70001, "bf16"), (900, 70001, "bf16")])
+def test_the_policy_loss_alone_repeats(B, ctx, n, V, dtype):
+    """Without a gradient the ring's places are filled again while rows are summed: time and again the
+    bits of the call with one."""
+    gen = torch.Generator("cuda").manual_seed(V)
+    x = (3 * torch.randn(n, V, generator=gen, device="cuda")).to(torch.bfloat16 if dtype == "bf16" else torch.float32)
+    ch = torch.randint(0, V, (n,), generator=gen, device="cuda", dtype=torch.int32)
+    adv = torch.randn(n, generator=gen, device="cuda")
+    s, logp, _ = B.pr_policy_loss(ctx, x, ch, adv)
+    for _ in range(30):
+        s1, logp1, _ = B.pr_policy_loss(ctx, x, ch, adv, want_grad=False)
+        assert torch.equal(logp, logp1) and torch.equal(s, s1)
