@@ -61,17 +61,14 @@ NormShape backward_shape() {
   return {{reinterpret_cast<const void*>(&prk::dnorm_rows<T, L, N, (L > 8), false>),
            reinterpret_cast<const void*>(&prk::dnorm_rows<T, L, N, (L > 8), true>)}, L > 8, L, N};
 }
-// many: more rows than SMs
 template <typename T>
-NormShape backward_of(int64_t words, bool many) {
+NormShape backward_of(int64_t words, bool two_rows) {
   if (words <= 16) return backward_shape<T, 8, 2>();
   if (words <= 64) return backward_shape<T, 32, 2>();
   if (words <= 128) return backward_shape<T, 64, 2>();
   if (words <= 256) return backward_shape<T, 128, 2>();
   if (words <= 512) return backward_shape<T, 256, 2>();
-  // two rows of three words a thread on an SM, or one of two on all of its threads (d = 5,120 bf16:
-  // 8,000 rows 73 us for 83, 100 rows 10.9 for 9.7; of four words, d = 7,168, 97 for 89)
-  if (words <= 768 && many) return backward_shape<T, 256, 3>();
+  if (words <= 768 && two_rows) return backward_shape<T, 256, 3>();
   if (words <= 1024) return backward_shape<T, 512, 2>();
   if (words <= 2048) return backward_shape<T, 512, 4>();
   if constexpr (sizeof(T) == 4) {
@@ -267,9 +264,9 @@ pr_status pr_layernorm_backward(pr_ctx* c, const void* dy, int64_t dy_stride, co
                      on_words(dy, dy_stride, dt) && on_words(dtotal, dtotal_stride, dt) &&
                      on_words(dx, dx_stride, dt);
   const int64_t words = (d * (int64_t)esize(dt) + 15) / 16;
-  const bool many = n_rows > c->num_sms;
-  const NormShape shape = dt == PR_DTYPE_BF16 ? backward_of<__nv_bfloat16>(words, many)
-                                              : backward_of<float>(words, many);
+  const bool two_rows = norm_two_rows(n_rows, c->num_sms, d, esize(dt), esize(wdt));
+  const NormShape shape = dt == PR_DTYPE_BF16 ? backward_of<__nv_bfloat16>(words, two_rows)
+                                              : backward_of<float>(words, two_rows);
   if (shape.threads) {
     if ((st = setup(c)) != PR_OK) return st;
     const int threads = std::max(shape.threads, prk::NR_NT), rows = threads / shape.threads;

@@ -42,4 +42,15 @@ inline NormStages norm_stages(int64_t d, size_t esize, size_t wsize, int groups,
   return s;
 }
 
+// The backward pass of rows of 513 to 768 words: two rows of three words a thread on an SM, or one of
+// two on all of its threads.  Two rows pay from eight of an SM on and with three places each, as fit
+// up to some 715 words with weights of the rows' type.  us, two rows for one:
+//   5,120 bf16       304 rows 14.2 for 11.9   1,400 22.4 for 22.6   8,000 72.1 for 83.7
+//   4,288 bf16       608      13.1 for 12.7   1,216 17.1 for 18.3   8,000 68.3 for 82.5
+//   6,144, 2 places  304      16.1 for 12.4   1,700 29.7 for 27.0   8,000 87.4 for 86.4
+//   2,960 fp32, 2    608      10.8 for 10.6   2,000 24.5 for 22.0   8,000 73.7 for 67.5
+inline bool norm_two_rows(int64_t n_rows, int num_sms, int64_t d, size_t esize, size_t wsize) {
+  return n_rows > 8 * (int64_t)num_sms && norm_stages(d, esize, wsize, 1, 2, 3, 1, 3).fits;
+}
+
 }  // namespace prh

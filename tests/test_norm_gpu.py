@@ -367,3 +367,11 @@ def test_refusals(B, ctx):
     big = torch.empty(1, (1 << 20) + 1, device="cuda")
     refused(fwd, big, big[0])
     assert B.launch_count() == n0
+
+
+@pytest.mark.parametrize("n,d,dtype", [(1217, 4104, "bf16"), (1300, 4111, "bf16"), (1400, 5720, "bf16"),
+                                       (1300, 6144, "bf16"), (1217, 2056, "f32"), (1521, 2501, "f32")])
+def test_backward_of_many_rows_of_three_words_a_thread(B, ctx, n, d, dtype):
+    """513 to 768 words a row, two rows on an SM or one."""
+    test_backward_sizes(B, ctx, n, d, dtype)
+    test_outputs_in_place_of_inputs(B, ctx, n, d, dtype)

@@ -26,6 +26,9 @@ extern "C" int stages(long long d, int esize, int wsize, int groups, int ctas, i
   *row_bytes = s.row_bytes;
   return s.fits ? s.stages : -1;
 }
+extern "C" int two_rows(long long n_rows, int num_sms, long long d, int esize, int wsize) {
+  return prh::norm_two_rows(n_rows, num_sms, d, esize, wsize);
+}
 """)
     subprocess.run([cxx, "-std=c++17", "-Wall", "-Werror", "-O1", "-shared", "-fPIC", "-I", CSRC,
                     str(tmp / "norm.cpp"), "-o", str(tmp / "norm.so")], check=True)
@@ -36,6 +39,8 @@ extern "C" int stages(long long d, int esize, int wsize, int groups, int ctas, i
     def call(*args):
         smem, row = ctypes.c_longlong(), ctypes.c_int()
         return lib.stages(*args, ctypes.byref(smem), ctypes.byref(row)), smem.value, row.value
+    lib.two_rows.argtypes = [ctypes.c_longlong, ctypes.c_int, ctypes.c_longlong, ctypes.c_int, ctypes.c_int]
+    call.two_rows = lib.two_rows
     return call
 
 
@@ -67,6 +72,16 @@ def test_as_many_ctas_fit_an_sm_as_the_grid_counts_on(stages, esize, wsize):
 def test_rows_that_are_not_staged_take_their_weights_alone(stages):
     for d in (1, 7, 8, 64, 128):
         assert stages(d, 2, 4, 0, 1, 2, 2, 1)[:2] == (0, 2 * 4 * ((d + 7) // 8 * 8))
+
+
+def test_two_rows_share_an_sm_where_there_are_rows_and_places(stages):
+    """As measured on 152 SMs: not for some hundred rows, nor for rows with fewer than three places."""
+    for n_rows, d, esize, wsize, want in (
+            (153, 5120, 2, 2, False), (304, 6144, 2, 2, False), (608, 4288, 2, 2, False),
+            (1700, 4288, 2, 2, True), (8000, 5120, 2, 2, True), (8000, 5600, 2, 2, True),
+            (8000, 2560, 4, 4, True), (1700, 6144, 2, 2, False), (8000, 6144, 2, 2, False),
+            (8000, 2960, 4, 4, False)):
+        assert bool(stages.two_rows(n_rows, 152, d, esize, wsize)) == want, (n_rows, d)
 
 
 def test_no_kernel_is_compiled_that_no_width_takes():
