@@ -294,6 +294,16 @@ struct LogProb {
   }
 };
 
+// (K, n) with n 2^(c x - K) = nR / R 2^(c x - k), for a sum of up to 1e33: nR / R by itself would
+// be denormal, or 0, for small weights.  R = r 2^up, and K is k + up less what its rounding lost.
+// (Apart, for sums above 1e9: with every row's here the batch takes 0.8 to 2% longer.)
+__device__ __noinline__ float2 far_factor(float nR, float R, float k) {
+  const float r = __uint_as_float((__float_as_uint(R) & 0x7fffffu) | 0x3f800000u);
+  const float up = (float)((int)(__float_as_uint(R) >> 23) - 127), K = k + up;
+  const float t = K - k, lost = (k - (K - t)) + (up - t);
+  return make_float2(K, nR * __fdividef(exp2f(-lost), r));
+}
+
 // A row's end: its sum R against 2^k, the list's and label's logits left out.  Writes the result
 // (out, and the list's entries of the gradient to g), whose barrier learns of it first, then the
 // row's KL and the statistics' terms (weight wt).  Whole warp; apart from the kernel's registers.
@@ -382,14 +392,14 @@ __device__ __forceinline__ void list_math(const DistillArgs& d, int64_t row, con
       o.M = 0.f;
       const float per_R = rest ? __fdividef(1.f, R) : 0.f;
       const float sum_a = kc != 0.f ? kc * a_all : 0.f, ba = bc * (E * inv);
-      // n 2^(c x - k) = n R / r 2^-lost 2^(c x - K), with R = r 2^e and K = k + e less what its
-      // rounding lost: n by itself is denormal, or 0, where a small weight meets a sum of 1e30
-      const float r = __uint_as_float((__float_as_uint(R) & 0x7fffffu) | 0x3f800000u);
-      const float up = rest ? (float)((int)(__float_as_uint(R) >> 23) - 127) : 0.f;
-      o.K = k + up;
-      const float t = o.K - k, lost = (k - (o.K - t)) + (up - t);
-      const float per_r = rest ? __fdividef(exp2f(-lost), r) : 0.f;
-      o.nk = nan ? NAN : w * (ba - (sum_a - cc) * sigma) * per_r;
+      const float nR = nan ? NAN : w * (ba - (sum_a - cc) * sigma);
+      o.K = k;
+      o.nk = nR * per_R;
+      if (R > 1e9f) {
+        const float2 f = far_factor(nR, R, k);
+        o.K = f.x;
+        o.nk = f.y;
+      }
       o.mode = o.nk == 0.f ? ROW_ZERO : ROW_FAST;
       // q_y (b / sigma - kA) - ce (1 - q_y)
       o.gy = nan ? NAN : w * (ey * per_R * (ba - sum_a * sigma) - cc * (not_y * inv));
