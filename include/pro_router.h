@@ -170,8 +170,9 @@ pr_status pr_last_error(pr_ctx* ctx, uint32_t* flags);
  * reduction; for the training losses the listing of the rows (one kernel, two for
  * large batches, none for up to 512 rows), the pass over the logits, the answer pairs
  * (preference loss) and a second pass where the gradient takes one; for pr_distill_loss the
- * listing, the batch's lists (with a gradient, above 512 rows) and the pass; for
- * pr_layernorm_backward the rows and the columns' sums.  Waits for the call's last event.
+ * listing, the batch's lists (with a gradient, above 512 rows, but not where many rows of up to
+ * 22 KB go one to a warp) and the pass; for pr_layernorm_backward the rows and the columns'
+ * sums.  Waits for the call's last event.
  * Writes min(count, cap) values to
  * `ms` and the count to *n (0 if no timed call was made).
  */
@@ -614,8 +615,10 @@ pr_status pr_preference_loss(pr_ctx* ctx, const void* logits, pr_dtype dt, int64
  * never listed.  Where fewer than k are left the list ends with ids -1 and log-probabilities -inf.
  * A row with NaN or +inf, or with nothing finite, has ids -1 and log-probabilities NaN
  * (PR_FLAG_NONFINITE in the context flag word).  Orders are exact; sums are fp32, in an order
- * that depends on the sizes and on the rows' alignment alone.  n_rows < 2^31; one launch, no
- * workspace: calls on different streams may overlap.
+ * that depends on the sizes and on the rows' alignment alone.  A log-probability is good to some
+ * 2^-23 (1 + its size), not to digits of its own: of a token that has all but 1e-6 of its row the
+ * -1e-6 may be 10% off, and so may a rest of that size that is worked out from the list.
+ * n_rows < 2^31; one launch, no workspace: calls on different streams may overlap.
  */
 pr_status pr_top_logits(pr_ctx* ctx, const void* logits, pr_dtype dt, int64_t n_rows,
                         int64_t vocab, int64_t row_stride, int32_t k, float temperature,
@@ -658,7 +661,8 @@ typedef struct {
  *   a term with coefficient 0 is a statistic alone, whatever its value.
  *   logits, mask, offsets, grad, workspace, sums: as "common to both losses" above says, but
  *              that vocab <= PR_DISTILL_MAX_VOCAB and that x / T from 1e9 on counts as +inf,
- *              from -1e9 down as -inf
+ *              from -1e9 down as -inf (of tokens that are not listed, the border itself to
+ *              within an fp32 step of 1e9)
  *   ids        device int32 [n_rows][k], 1 <= k <= PR_MAX_LISTED, in any order.  An entry
  *              with id -1, or with log-probability -inf, is absent; a row without entries
  *              has KL 0 and no gradient of it.

@@ -122,9 +122,10 @@ __constant__ float2 DS_ROOTS[16] = {
     {1.5422108173370361f, 8.070904833346049e-09f}, {1.610490322113037f, 9.836217174097328e-09f},
     {1.6817928552627563f, -2.4755326677450284e-08f}, {1.7562521696090698f, -9.235770370707996e-09f},
     {1.8340080976486206f, -1.1239277952768134e-08f}, {1.9152065515518188f, 9.845328108326612e-09f}};
-// exp(t) within 1e-12 of itself for t >= -80: t log2(e) = n / 16 + z log2(e) with z in two parts
-// and below ln 2 / 32, 2^(n / 16) from its table, exp(z) - 1 = z + z^2 / 2 + z^3 / 6 + ... whose
-// first two terms are in two parts.  (rho down to 2^-24 is to keep five digits.)
+// exp(t) within 1e-12 of itself for t >= -62 (below that rounded once, which is under 1e-34):
+// t log2(e) = n / 16 + z log2(e) with z in two parts and below ln 2 / 32, 2^(n / 16) from its table,
+// exp(z) - 1 = z + z^2 / 2 + z^3 / 6 + ... whose first two terms are in two parts.  (rho down to
+// 2^-24 is to keep five digits.)
 __device__ __forceinline__ Pair exp_pair(float t) {
   constexpr float L2E_LOW = 1.925963033500011e-08f;  // log2(e) - L2E
   const float y = t * L2E, n = rintf(y * 16.f), r = fmaf(n, -0.0625f, y);
@@ -309,9 +310,9 @@ __device__ __noinline__ float2 far_factor(float nR, float R, float k) {
 // row's KL and the statistics' terms (weight wt).  Whole warp; apart from the kernel's registers.
 template <typename T>
 __device__ __forceinline__ void list_math(const DistillArgs& d, int64_t row, const ListIn& in,
-                                              const ListPre& pre, float k, float R, float wt,
-                                              bool writes, RowOut* out, float* g, uint64_t* out_bar,
-                                              float2* stat, int lane) {
+                                          const ListPre& pre, float k, float R, float wt,
+                                          bool writes, RowOut* out, float* g, uint64_t* out_bar,
+                                          float2* stat, int lane) {
   const LossArgs& a = d.a;
   const float big = d.big * a.c2;
   bool on[2], bad = false;
@@ -421,8 +422,9 @@ __device__ __forceinline__ void list_math(const DistillArgs& d, int64_t row, con
   const LogSum log_S(S);
   LogProb l[2] = {LogProb(x[0], a.c2, K, log_S), LogProb(x[1], a.c2, K, log_S)};
   const LogSum log_R(R);
-  const float l_sigma = sigma > 0.5f ? log1pf(-E * inv)
-      : ((k - K) + (log_R.e - log_S.e) + (log_R.f - log_S.f)) * LN2;
+  const float l_sigma = sigma > 0.5f
+                            ? log1pf(-E * inv)
+                            : ((k - K) + (log_R.e - log_S.e) + (log_R.f - log_S.f)) * LN2;
   // the divergence
   const float to = d.none ? pre.rho : 0.f, to_lo = d.none ? pre.l_rho : 0.f;
   auto more = [&](const LogProb& v, float t) {  // log q - log p
@@ -493,8 +495,8 @@ __device__ __forceinline__ void list_math(const DistillArgs& d, int64_t row, con
   bad |= pre.bad_id;
   if (bad) kl = ce = NAN;
   if (lane < DS_TERMS) {
-    const float t = wt * (lane == 0 ? kl : lane == 1 ? ce : bad ? NAN : lane == 2 ? pre.mass
-        : E * inv);
+    const float t =
+        wt * (lane == 0 ? kl : lane == 1 ? ce : bad ? NAN : lane == 2 ? pre.mass : E * inv);
     const float2 s = stat[lane];
     const float y = s.x + t, z = y - s.x;
     stat[lane] = make_float2(y, s.y + ((s.x - (y - z)) + (t - z)));
@@ -640,7 +642,7 @@ __device__ __forceinline__ void fence_async() {
 //
 // Without a gradient nothing has to be held, and `parts` of a row may go through one CTA, one after
 // the other: a row of a cluster's eight parts fills 120 of 152 SMs, as clusters of eight find no
-// more room. Sums are kept apart as a cluster's CTAs keep them, so that the loss has the same bits.
+// more room.  Sums are kept apart as a cluster's CTAs keep them, so that the loss has the same bits.
 
 // a lane's tokens among its warp's words of this CTA's part of a row: their elements from the
 // row's first word on, or -1
@@ -877,7 +879,7 @@ __global__ void __launch_bounds__(RG_NT, 2)
       add_rest_ends(d, sh, wide<T>(in.edge), v, kind, k, R);
       if (C > 1) landed(next);
       list_math<T>(d, row, in, pre, k, R, wt, rank == 0, HOLD ? &sm.out[s] : nullptr, entries,
-                &sm.out_bar[s], sm.stat, lane);
+                   &sm.out_bar[s], sm.stat, lane);
       __syncwarp();
       if (HOLD && rank == 0) put_end(g, v, kind, sm.out[s], entries, a.c2, wide<T>(in.edge));
       in = next;
@@ -997,8 +999,8 @@ __global__ void __launch_bounds__(RG_NT, 2)
           } else {
 #pragma unroll
             for (int q = 0; q < RG_W; ++q)
-              if (w + 32 * RG_NW * q + at < sh.w1) put_word(to + 32 * RG_NW * q * Tr::VEC, v[q],
-                  vec);
+              if (w + 32 * RG_NW * q + at < sh.w1)
+                put_word(to + 32 * RG_NW * q * Tr::VEC, v[q], vec);
           }
           if (chunks & 1u) {
             __syncwarp();  // the warp's words are written: the list's entries over them
@@ -1119,7 +1121,7 @@ __global__ void __launch_bounds__(32 * RW_MOST, 2)
     add_rest_ends(d, sh, wide<T>(in.edge), v, kind, k, R);
     const float wt = (float)(a.norm ? share / (double)in.count : share);
     list_math<T>(d, ref.x, in, pre, k, R, wt, true, HOLD ? &sm.out[warp] : nullptr, list, nullptr,
-        stat, lane);
+                 stat, lane);
     __syncwarp();
     if (HOLD) {
       const RowOut o = sm.out[warp];

@@ -110,7 +110,11 @@ pr_status launch_ring(pr_ctx* c, prk::DistillArgs& d, pr_dtype dt, const RingSha
   return st == PR_OK ? timing_mark(c, s) : st;
 }
 
-// Warps of a CTA of distill_rows, or 0 where the ring takes less time: the other losses' rule.
+// Warps of a CTA of distill_rows, or 0 where the ring takes no more time: the other losses' rule.
+// us with a gradient, rows for the ring, k = 32 bf16:
+//   V 2,000   700 rows 17 for 24   8,000 37 for 108     V 8,192    700 21 for 25   8,000 84 for 120
+//   V 11,000  700 rows 23 for 26   8,000 106 for 137    V 17,000   700 27 for 28   8,000 174 for 170
+// (The border could lie higher without a gradient: V 14,000, 8,000 rows 79 for 99.)
 int rows_warps(const pr_ctx* c, const prk::LossArgs& a, pr_dtype dt) {
   if (a.own || a.n_rows <= 4 * c->num_sms) return 0;
   const int64_t part = std::max<int64_t>(16, a.vocab * (int64_t)esize(dt) / 16 * 16);
@@ -139,7 +143,7 @@ pr_status pr_distill_loss(pr_ctx* c, const void* logits, pr_dtype dt, int64_t n_
                           const pr_distill* p, float* stats, float* kl, void* grad,
                           int64_t grad_stride, void* stream) {
   if (!c || !p) return PR_ERR_INVALID_ARG;
-  pr_status st = check_loss(dt, logits, n_rows, vocab, row_stride, chosen, offsets, n_req,
+  pr_status st = check_loss(dt, logits, n_rows, vocab, row_stride, offsets, n_req,
                             p->temperature, p->grad_scale, stats, kl, grad, grad_stride);
   if (st != PR_OK) return st;
   if (vocab > PR_DISTILL_MAX_VOCAB || k < 1 || k > PR_MAX_LISTED) return PR_ERR_INVALID_ARG;

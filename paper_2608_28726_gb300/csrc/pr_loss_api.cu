@@ -162,7 +162,7 @@ pr_status pr_policy_loss(pr_ctx* c, const void* logits, pr_dtype dt, int64_t n_r
                          const pr_policy* p, float* stats, float* logp, void* grad,
                          int64_t grad_stride, void* stream) {
   if (!c || !p) return PR_ERR_INVALID_ARG;
-  pr_status st = check_loss(dt, logits, n_rows, vocab, row_stride, chosen, offsets, n_req,
+  pr_status st = check_loss(dt, logits, n_rows, vocab, row_stride, offsets, n_req,
                             p->temperature, p->grad_scale, stats, logp, grad, grad_stride);
   if (st != PR_OK) return st;
   if (n_rows > 0 && (!chosen || !advantage)) return PR_ERR_INVALID_ARG;
@@ -213,7 +213,7 @@ pr_status pr_preference_loss(pr_ctx* c, const void* logits, pr_dtype dt, int64_t
                              float* ratio, float* logp, void* grad, int64_t grad_stride,
                              void* stream) {
   if (!c || !p) return PR_ERR_INVALID_ARG;
-  pr_status st = check_loss(dt, logits, n_rows, vocab, row_stride, chosen, offsets, n_req,
+  pr_status st = check_loss(dt, logits, n_rows, vocab, row_stride, offsets, n_req,
                             p->temperature, p->grad_scale, stats, logp, grad, grad_stride);
   if (st != PR_OK) return st;
   if (!offsets || n_req % 2 != 0 || !ratio || (n_rows > 0 && !chosen)) return PR_ERR_INVALID_ARG;

@@ -18,9 +18,9 @@ inline size_t esize(pr_dtype dt) { return dt == PR_DTYPE_BF16 ? 2 : 4; }
 inline size_t up16(size_t n) { return (n + 15) & ~(size_t)15; }
 
 inline pr_status check_loss(pr_dtype dt, const void* logits, int64_t n_rows, int64_t vocab,
-                     int64_t row_stride, const int32_t* chosen, const int64_t* offsets,
-                     int32_t n_req, float temperature, float grad_scale, const float* stats,
-                     const float* logp, const void* grad, int64_t grad_stride) {
+                            int64_t row_stride, const int64_t* offsets, int32_t n_req,
+                            float temperature, float grad_scale, const float* stats,
+                            const float* logp, const void* grad, int64_t grad_stride) {
   if (dt != PR_DTYPE_F32 && dt != PR_DTYPE_BF16) return PR_ERR_INVALID_ARG;
   if (n_rows < 0 || n_rows > 0x7fffffffLL || vocab <= 0 || vocab > 0x7fffffffLL ||
       row_stride < vocab || n_req < 0)
@@ -77,8 +77,7 @@ inline pr_status workspace(pr_ctx* c, prk::LossArgs& a, int64_t groups, bool pre
 
 // early: set up while the kernel before it still runs
 inline pr_status launch(const void* kern, unsigned grid, unsigned threads, size_t smem,
-    unsigned cluster,
-                 void** args, cudaStream_t s, bool early = true) {
+                        unsigned cluster, void** args, cudaStream_t s, bool early = true) {
   cudaLaunchConfig_t cfg;
   memset(&cfg, 0, sizeof cfg);
   cfg.gridDim = dim3(grid);
@@ -172,9 +171,9 @@ inline RingShape choose_ring(const int (&room)[2][4], pr_dtype dt, int64_t n_row
 }
 
 inline void fill(prk::LossArgs& a, pr_ctx* c, const void* logits, int64_t n_rows, int64_t vocab,
-          int64_t row_stride, const int32_t* chosen, const uint8_t* mask, const int64_t* offsets,
-          int32_t n_req, const float* ref_logp, float temperature, float grad_scale, float* stats,
-          float* logp, void* grad, int64_t grad_stride) {
+                 int64_t row_stride, const int32_t* chosen, const uint8_t* mask,
+                 const int64_t* offsets, int32_t n_req, const float* ref_logp, float temperature,
+                 float grad_scale, float* stats, float* logp, void* grad, int64_t grad_stride) {
   memset(&a, 0, sizeof a);
   a.logits = logits;
   a.n_rows = n_rows;

@@ -148,8 +148,8 @@ struct RowWord {
       for (int j = 0; j < VEC; ++j) set(j, nm_get(row + column(t, i, j)));
     } else {
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) set(j, column(t, i, j) < d ? nm_get(row + column(t, i,
-          j)) : 0.f);
+      for (int j = 0; j < VEC; ++j)
+        set(j, column(t, i, j) < d ? nm_get(row + column(t, i, j)) : 0.f);
     }
   }
   __device__ __forceinline__ void store(T* row, int t, int i, int d) const {  // (of a word with some)
@@ -179,8 +179,8 @@ struct RowWord {
         for (int q = 0; q < VEC / 4; ++q) {
           const uint2 v = reinterpret_cast<const uint2*>(w)[c0 / 4 + q];
           f[2 * q] = make_float2(__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xffff0000u));
-          f[2 * q + 1] = make_float2(__uint_as_float(v.y << 16),
-              __uint_as_float(v.y & 0xffff0000u));
+          f[2 * q + 1] =
+              make_float2(__uint_as_float(v.y << 16), __uint_as_float(v.y & 0xffff0000u));
         }
       }
     } else if (wide) {
@@ -188,10 +188,10 @@ struct RowWord {
       for (int j = 0; j < VEC; ++j)
         set(j, column(t, i, j) < d ? reinterpret_cast<const float*>(w)[column(t, i, j)] : 0.f);
     } else {
+      const __nv_bfloat16* const narrow = reinterpret_cast<const __nv_bfloat16*>(w);
 #pragma unroll
       for (int j = 0; j < VEC; ++j)
-        set(j, column(t, i, j) < d ? nm_get(reinterpret_cast<const __nv_bfloat16*>(w) + column(t,
-            i, j)) : 0.f);
+        set(j, column(t, i, j) < d ? nm_get(narrow + column(t, i, j)) : 0.f);
     }
   }
 };
@@ -199,10 +199,11 @@ __device__ __forceinline__ float2 nm_both(float v) { return make_float2(v, v); }
 
 // the weights of d columns into shared memory, 0 up to a multiple of eight; by a CTA, then a
 // barrier
-__device__ __forceinline__ int nm_weight_bytes(int d,
-    bool wide) { return (d + 7) / 8 * 8 * (wide ? 4 : 2); }
+__device__ __forceinline__ int nm_weight_bytes(int d, bool wide) {
+  return (d + 7) / 8 * 8 * (wide ? 4 : 2);
+}
 __device__ __forceinline__ void nm_keep(unsigned char* to, const void* w, bool wide, bool vec,
-    int d) {
+                                        int d) {
   const int words = vec ? d / (wide ? 4 : 8) : 0;
 #pragma unroll 4
   for (int i = threadIdx.x; i < words; i += blockDim.x)
@@ -212,8 +213,8 @@ __device__ __forceinline__ void nm_keep(unsigned char* to, const void* w, bool w
     if (wide)
       reinterpret_cast<float*>(to)[i] = i < d ? reinterpret_cast<const float*>(w)[i] : 0.f;
     else
-      reinterpret_cast<uint16_t*>(to)[i] = i < d ? reinterpret_cast<const uint16_t*>(w)[i]
-          : (uint16_t)0;
+      reinterpret_cast<uint16_t*>(to)[i] =
+          i < d ? reinterpret_cast<const uint16_t*>(w)[i] : (uint16_t)0;
   }
 }
 
@@ -446,8 +447,8 @@ __global__ void __launch_bounds__(L > NR_NT ? L : NR_NT, L > NR_NT ? 1 : 2)
   auto res_of = [&](int64_t row) { return reinterpret_cast<const T*>(a.res) + row * a.res_stride; };
   RowStages<T, L> st(nm_raw + w_bytes, a, res_staged ? 3 : 2);
   auto fill = [&](int i, int64_t row) {
-    st.expect(i, st.size(x_of(row)) + st.size(dy_of(row)) + (res_staged ? st.size(res_of(row))
-        : 0u));
+    st.expect(i, st.size(x_of(row)) + st.size(dy_of(row)) +
+                     (res_staged ? st.size(res_of(row)) : 0u));
     st.copy(i, 0, x_of(row));
     st.copy(i, 1, dy_of(row));
     if (res_staged) st.copy(i, 2, res_of(row));
@@ -590,8 +591,8 @@ __global__ void __launch_bounds__(L > NR_NT ? L : NR_NT, L > NR_NT ? 1 : 2)
 
 // The gradients of the weights from the CTAs' sums: 32 columns a CTA, each warp every 32nd of them
 constexpr int NS_NT = 1024;
-static __global__ void __launch_bounds__(NS_NT) dnorm_sum(const __grid_constant__ NormArgs a,
-    const int ctas) {
+static __global__ void __launch_bounds__(NS_NT)
+    dnorm_sum(const __grid_constant__ NormArgs a, const int ctas) {
   __shared__ float part[NS_NT / 32][32];
   pdl_wait();
   pdl_trigger();

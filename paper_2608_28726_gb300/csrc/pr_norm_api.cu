@@ -144,8 +144,8 @@ pr_status pr_layernorm(pr_ctx* c, const void* x, pr_dtype dt, int64_t n_rows, in
         (residual && !rows_ok(residual, d, residual_stride, dt)) ||
         (total && !rows_ok(total, d, total_stride, dt)) || y == total)
       return PR_ERR_INVALID_ARG;
-    if (!same_rows(y, y_stride, x, x_stride) || !same_rows(y, y_stride, residual,
-        residual_stride) ||
+    if (!same_rows(y, y_stride, x, x_stride) ||
+        !same_rows(y, y_stride, residual, residual_stride) ||
         (total && (!same_rows(total, total_stride, x, x_stride) ||
                    !same_rows(total, total_stride, residual, residual_stride))))
       return PR_ERR_INVALID_ARG;
@@ -180,8 +180,8 @@ pr_status pr_layernorm(pr_ctx* c, const void* x, pr_dtype dt, int64_t n_rows, in
                      on_words(residual, residual_stride, dt) && on_words(total, total_stride, dt) &&
                      on_words(y, y_stride, dt);
   const int64_t words = (d * (int64_t)esize(dt) + 15) / 16;
-  const NormShape shape = dt == PR_DTYPE_BF16 ? forward_of<__nv_bfloat16>(words)
-      : forward_of<float>(words);
+  const NormShape shape =
+      dt == PR_DTYPE_BF16 ? forward_of<__nv_bfloat16>(words) : forward_of<float>(words);
   if (shape.threads) {
     if ((st = setup(c)) != PR_OK) return st;
     const int threads = std::max(shape.threads, prk::NR_NT), rows = threads / shape.threads;
@@ -197,8 +197,8 @@ pr_status pr_layernorm(pr_ctx* c, const void* x, pr_dtype dt, int64_t n_rows, in
     }
     if (fits) {
       if (!shape.staged) ctas = 2048 / threads;
-      const int64_t grid = std::min<int64_t>((n_rows + rows - 1) / rows,
-          (int64_t)c->num_sms * ctas);
+      const int64_t grid =
+          std::min<int64_t>((n_rows + rows - 1) / rows, (int64_t)c->num_sms * ctas);
       void* args[] = {&a};
       return launch(c, shape.kernel[whole], dim3((unsigned)grid), (unsigned)threads, smem, args, s);
     }
@@ -279,27 +279,25 @@ pr_status pr_layernorm_backward(pr_ctx* c, const void* dy, int64_t dy_stride, co
     while (ctas > 1 && !stage(a, shape, dt, ctas, 3, 1, 2, smem)) --ctas;
     a.stage_res = dtotal && dx && stage(a, shape, dt, ctas, 3, 1, 2, smem);
     const bool fits = stage(a, shape, dt, ctas, a.stage_res ? 3 : 2, 1, shape.words == 8 ? 1 : 2,
-        smem);
+                            smem);
     if (fits) {
-      const int64_t grid = std::min<int64_t>((n_rows + rows - 1) / rows,
-          (int64_t)c->num_sms * ctas);
+      const int64_t grid =
+          std::min<int64_t>((n_rows + rows - 1) / rows, (int64_t)c->num_sms * ctas);
       if (dweight || dbias) {
-        if ((st = grow(c->norm_ws, (size_t)grid * 2 * d * sizeof(float),
-            false)) != PR_OK) return st;
+        if ((st = grow(c->norm_ws, (size_t)grid * 2 * d * sizeof(float), false)) != PR_OK)
+          return st;
         a.part = static_cast<float*>(c->norm_ws.p);
         if (rows > 1)  // the rows' columns, added up at the end
           smem = std::max(smem, (size_t)threads * shape.words * (16 / esize(dt)) * sizeof(float));
       }
       void* args[] = {&a};
-      if ((st = launch(c, shape.kernel[whole], dim3((unsigned)grid), (unsigned)threads, smem,
-          args, s)) != PR_OK)
-        return st;
+      st = launch(c, shape.kernel[whole], dim3((unsigned)grid), (unsigned)threads, smem, args, s);
+      if (st != PR_OK) return st;
       if (!a.part) return PR_OK;
       int parts = (int)grid;
       void* sum_args[] = {&a, &parts};
       return launch(c, reinterpret_cast<const void*>(&prk::dnorm_sum),
-          dim3((unsigned)((d + 31) / 32), 2),
-                    prk::NS_NT, 0, sum_args, s);
+                    dim3((unsigned)((d + 31) / 32), 2), prk::NS_NT, 0, sum_args, s);
     }
   }
   if (dweight || dbias) {  // first: dx may be written over dy and x

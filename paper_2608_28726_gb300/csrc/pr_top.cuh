@@ -86,14 +86,15 @@ struct TopList {
 };
 
 // a value as a key has it: -0 is 0
-__device__ __forceinline__ uint64_t top_key(float v, uint32_t index) { return make_key(v + 0.f,
-    index); }
+__device__ __forceinline__ uint64_t top_key(float v, uint32_t index) {
+  return make_key(v + 0.f, index);
+}
 
 __device__ __forceinline__ float top_max(float m) { return m; }
 __device__ __forceinline__ float top_max(uint16_t m) { return __uint_as_float((uint32_t)m << 16); }
 
-// The first k of n groups by their maxima at gm (shared memory): ranks lane and 32 + lane in hi and
-// lo.
+// The first k of n groups by their maxima at gm (shared memory): ranks lane and 32 + lane in hi
+// and lo.
 template <typename M>
 __device__ __forceinline__ void top_groups(TopList& l, const M* gm, int n, float big, int lane) {
   // a bound that k groups reach: of 64 sets of groups the k-th largest maximum
@@ -252,8 +253,7 @@ struct TopMax<__nv_bfloat16> {
 template <typename T, int GW>
 __global__ void __launch_bounds__(TR_NT, 3)
     top_ring(const __grid_constant__ LossArgs a, const int k, const float big,
-        int32_t* const out_ids,
-             const int places, const int gm_bytes) {
+             int32_t* const out_ids, const int places, const int gm_bytes) {
   extern __shared__ __align__(16) unsigned char smem_raw[];
   TopRing& sm = *reinterpret_cast<TopRing*>(smem_raw);
   using Tr = Traits<T>;
@@ -340,8 +340,8 @@ __global__ void __launch_bounds__(TR_NT, 3)
       if (w + TR_CHUNK > sh.w1) {
 #pragma unroll
         for (int q = 0; q < TR_W; ++q)
-          if (w + at[q] >= sh.w1) v[q] = make_uint4(Tr::NEG_WORD, Tr::NEG_WORD, Tr::NEG_WORD,
-              Tr::NEG_WORD);
+          if (w + at[q] >= sh.w1)
+            v[q] = make_uint4(Tr::NEG_WORD, Tr::NEG_WORD, Tr::NEG_WORD, Tr::NEG_WORD);
       }
       const int32_t g = (w - sh.w0) / GW + tid;
       if constexpr (GW == 4) {
@@ -551,8 +551,8 @@ __global__ void __launch_bounds__(TR_NT, 3)
       const float log_sum = logf(rows_sum);
       auto give = [&](int j, uint64_t q) {
         out_ids[row * k + j] = bad || q == 0 ? -1 : (int32_t)key_idx(q);
-        a.logp[row * k + j] = bad ? NAN : q ? fmaf(key_val(q), a.c2,
-            -K) * LN2 - log_sum : -INFINITY;
+        a.logp[row * k + j] =
+            bad ? NAN : q ? fmaf(key_val(q), a.c2, -K) * LN2 - log_sum : -INFINITY;
       };
       if (C == 1) {
         if (tid < k) give(tid, mine);
@@ -611,8 +611,7 @@ constexpr size_t TS_START = (sizeof(TopShort) + 15) / 16 * 16;
 template <typename T>
 __global__ void __launch_bounds__(32 * TS_MOST, 2)
     top_short(const __grid_constant__ LossArgs a, const int k, const float big,
-        int32_t* const out_ids,
-              const int bytes) {  // of a warp's part
+              int32_t* const out_ids, const int bytes) {  // of a warp's part
   extern __shared__ __align__(16) unsigned char smem_raw[];
   TopShort& sm = *reinterpret_cast<TopShort*>(smem_raw);
   using Tr = Traits<T>;
@@ -712,8 +711,8 @@ __global__ void __launch_bounds__(32 * TS_MOST, 2)
     TopList l(sm.buf[warp], k);
     for (int32_t w = 0; w < sh.words; w += 32) {
       const bool in = w + lane < sh.words;
-      const uint4 q = in ? st[w] : make_uint4(Tr::NEG_WORD, Tr::NEG_WORD, Tr::NEG_WORD,
-          Tr::NEG_WORD);
+      const uint4 q =
+          in ? st[w] : make_uint4(Tr::NEG_WORD, Tr::NEG_WORD, Tr::NEG_WORD, Tr::NEG_WORD);
       if (!__any_sync(FULL, reaches(Tr::gmax(q)))) continue;
       uint32_t on = 0u;  // a bit per element
 #pragma unroll
@@ -728,8 +727,8 @@ __global__ void __launch_bounds__(32 * TS_MOST, 2)
         on &= on - 1u;
       }
     }
-    if (sh.head + sh.tail > 0) l.push(v_end >= 0 && reaches(x_end), top_key(x_end,
-        (uint32_t)v_end), lane);
+    if (sh.head + sh.tail > 0)
+      l.push(v_end >= 0 && reaches(x_end), top_key(x_end, (uint32_t)v_end), lane);
     l.finish(lane);
     const float log_sum = logf(R * rescale2(ref - K));
 #pragma unroll

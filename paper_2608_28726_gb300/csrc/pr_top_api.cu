@@ -43,8 +43,8 @@ struct TopShape {
 int short_warps(const pr_ctx* c, int64_t n_rows, int64_t vocab, pr_dtype dt) {
   if (n_rows <= 3 * c->num_sms) return 0;
   const int64_t part = std::max<int64_t>(16, vocab * (int64_t)esize(dt) / 16 * 16);
-  const int64_t w = std::min<int64_t>(prk::TS_MOST,
-      ((int64_t)HALF_BYTES - (int64_t)prk::TS_START) / part);
+  const int64_t w = std::min<int64_t>(
+      prk::TS_MOST, ((int64_t)HALF_BYTES - (int64_t)prk::TS_START) / part);
   return w >= 5 ? (int)w : 0;
 }
 
@@ -70,8 +70,9 @@ TopShape choose(const pr_ctx* c, pr_dtype dt, int64_t n_rows, int64_t vocab) {
     // that leaves one CTA, two with a row's parts are better (1,000 rows of V = 262,144 fp32: 190
     // for 202).  Fewer CTAs than would fit get the room of the others.
     const int64_t ctas = n_rows * s.cluster;
-    s.on_sm = fixed + 3 * prk::TR_BYTES <= THIRD_BYTES ? 3
-        : fixed + 4 * prk::TR_BYTES <= HALF_BYTES ? 2 : 1;
+    s.on_sm = fixed + 3 * prk::TR_BYTES <= THIRD_BYTES  ? 3
+              : fixed + 4 * prk::TR_BYTES <= HALF_BYTES ? 2
+                                                        : 1;
     if (s.on_sm == 1 && s.cluster < 4 && words > 2 * s.cluster * prk::TR_CHUNK) continue;
     s.on_sm = (int)std::min<int64_t>(s.on_sm, (ctas + c->num_sms - 1) / c->num_sms);
     const size_t room = s.on_sm == 3 ? THIRD_BYTES : s.on_sm == 2 ? HALF_BYTES : SM_BYTES;
@@ -124,7 +125,7 @@ pr_status pr_top_logits(pr_ctx* c, const void* logits, pr_dtype dt, int64_t n_ro
     int part = (int)std::max<int64_t>(16, vocab * (int64_t)esize(dt) / 16 * 16);
     void* args[] = {&l, &kk, &limit, &out, &part};
     st = launch(short_kernel(dt), 2 * c->num_sms, 32u * warps,
-        prk::TS_START + (size_t)warps * part, 1, args, s);
+                prk::TS_START + (size_t)warps * part, 1, args, s);
     return st == PR_OK ? timing_mark(c, s) : st;
   }
   const TopShape shape = choose(c, dt, n_rows, vocab);
@@ -133,9 +134,8 @@ pr_status pr_top_logits(pr_ctx* c, const void* logits, pr_dtype dt, int64_t n_ro
     const int64_t at_once = (int64_t)shape.on_sm * c->num_sms;
     const int64_t groups = std::min<int64_t>(n_rows, std::max<int64_t>(1, at_once / shape.cluster));
     void* args[] = {&l, &kk, &limit, &out, &places, &gm};
-    st = launch(ring_kernel(dt, shape.words),
-                (unsigned)(groups * shape.cluster), prk::TR_NT, shape.smem,
-                (unsigned)shape.cluster, args, s,
+    st = launch(ring_kernel(dt, shape.words), (unsigned)(groups * shape.cluster), prk::TR_NT,
+                shape.smem, (unsigned)shape.cluster, args, s,
                 n_rows < groups + 1 && groups * shape.cluster < at_once);
     return st == PR_OK ? timing_mark(c, s) : st;
   }
