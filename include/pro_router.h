@@ -615,9 +615,10 @@ pr_status pr_preference_loss(pr_ctx* ctx, const void* logits, pr_dtype dt, int64
  * never listed.  Where fewer than k are left the list ends with ids -1 and log-probabilities -inf.
  * A row with NaN or +inf, or with nothing finite, has ids -1 and log-probabilities NaN
  * (PR_FLAG_NONFINITE in the context flag word).  Orders are exact; sums are fp32, in an order
- * that depends on the sizes and on the rows' alignment alone.  A log-probability is good to some
- * 2^-23 (1 + its size), not to digits of its own: of a token that has all but 1e-6 of its row the
- * -1e-6 may be 10% off, and so may a rest of that size that is worked out from the list.
+ * that depends on the sizes and on the rows' alignment alone.  Log-probabilities are at most 0 and
+ * good to some 2^-21 (1 + their size), not to digits of their own: of a token that has all but
+ * 1e-6 of its row the -1e-6 may be half as much off, and so may a rest of that size that is worked
+ * out from the list.
  * n_rows < 2^31; one launch, no workspace: calls on different streams may overlap.
  */
 pr_status pr_top_logits(pr_ctx* ctx, const void* logits, pr_dtype dt, int64_t n_rows,

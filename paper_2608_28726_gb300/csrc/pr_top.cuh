@@ -115,6 +115,70 @@ __device__ __forceinline__ void top_groups(TopList& l, const M* gm, int n, float
   l.finish(lane);
 }
 
+// ---- a row's sum ------------------------------------------------------------------------------
+//
+// The losses leave the emitted token or the listed ones out of a row's sum, where here the largest
+// element is nearly all of it.  So references are whole numbers, which the parts of a sum are
+// brought to one another by exactly, and a term is below 2^15: its exponent is rounded by 2^-21 at
+// most.  (With a reference that only an overflow raised, exponents of 30 and factors between
+// references had a token of p = 1 - 1e-6 come out at -1e-6 +- 3e-6, now +- 4e-7; 4,096 rows of
+// V = 151,936 bf16 k = 32 take 208 us for 207, with terms below 2^6 214.)
+
+// 2^d of a whole d <= 0
+__device__ __forceinline__ float top_scale(float d) {
+  return d < -126.f ? 0.f : __uint_as_float((uint32_t)(127 + (int)d) << 23);
+}
+
+// A thread's words into its sum (k, S), as add_words' of the losses.
+template <typename T, int N>
+__device__ __forceinline__ void top_words(float& k, float2& S, const uint4 (&v)[N], float c2,
+                                          bool begin) {
+  using Tr = Traits<T>;
+  auto top = [&]() {
+    float m = Tr::gmax(v[0]);
+#pragma unroll
+    for (int q = 1; q < N; ++q) m = fmaxf(m, Tr::gmax(v[q]));
+    return rintf(fmaxf(m * c2, -3e38f));
+  };
+  if (begin) k = top();
+  float2 here = make_float2(0.f, 0.f);
+#pragma unroll
+  for (int q = 0; q < N; ++q) add_word<T>(here, v[q], c2, -k);
+  if (__any_sync(FULL, !(here.x + here.y < 32768.f))) {
+    const float up = fmaxf(top(), k), f = top_scale(k - up);
+    k = up;
+    S.x *= f;
+    S.y *= f;
+    here = make_float2(0.f, 0.f);
+#pragma unroll
+    for (int q = 0; q < N; ++q) add_word<T>(here, v[q], c2, -k);
+  }
+  S = __fadd2_rn(S, here);
+}
+
+// (k, R) of the lanes together
+__device__ __forceinline__ void top_join(float2 q, float& k, float& R) {
+  k = warp_max(q.x);
+  R = warp_sum(q.y * top_scale(q.x - k));
+}
+
+// The elements of the lanes that have one (x, else -inf), at a row's ends, into its sum
+__device__ __forceinline__ void top_ends(float x, float c2, float& k, float& R) {
+  const float t = fmaxf(warp_max(rintf(x * c2)), -3e38f);
+  if (t > k) {
+    R *= top_scale(k - t);
+    k = t;
+  }
+  R += warp_sum(x > -INFINITY || x != x ? ex2(fmaf(x, c2, -k)) : 0.f);
+}
+
+// ln of the sum R against 2^k, against 2^K; an element of exponent u against 2^K from it.  (In
+// fp32 the sum of a row that is one token may come out below its term.)
+__device__ __forceinline__ float top_log(float k, float R, float K) { return logf(R * exp2f(k - K)); }
+__device__ __forceinline__ float top_logp(float x, float c2, float K, float log_sum) {
+  return fminf(fmaf(x, c2, -K) * LN2 - log_sum, 0.f);
+}
+
 // ---- any row: one to a CTA, in up to 8,192 groups, whatever their length --------------------
 
 struct TopSmem {
@@ -194,7 +258,7 @@ __global__ void __launch_bounds__(TP_NT) top_rows(const TopArgs a, const int64_t
     const uint64_t q = h == 0 ? e.hi : e.lo;
     if (j < a.k) {
       ids[j] = q ? (int32_t)key_idx(q) : -1;
-      logp[j] = q ? fmaf(key_val(q), a.c2, -K) * LN2 - lS : -INFINITY;
+      logp[j] = q ? top_logp(key_val(q), a.c2, K, lS) : -INFINITY;
     }
   }
 }
@@ -365,13 +429,13 @@ __global__ void __launch_bounds__(TR_NT, 3)
           top = fmaxf(top, m);
         }
       }
-      add_words<T>(ref, S, v, a.c2, w == sh.w0);
+      top_words<T>(ref, S, v, a.c2, w == sh.w0);
       __syncwarp();  // every lane's words are summed
       if (lane == 0) bar_arrive(&sm.empty[place]);
       step();
     }
     float R;
-    join(make_float2(ref, S.x + S.y), 1.f, ref, R);
+    top_join(make_float2(ref, S.x + S.y), ref, R);
     // the elements before and after the words: the first CTA's
     const float first_max = top;
     int32_t v_end = -1;
@@ -379,12 +443,7 @@ __global__ void __launch_bounds__(TR_NT, 3)
     if (warp == 0) {
       v_end = rank == 0 ? end_of(a, sh, lane) : -1;
       if (v_end >= 0) x_end = Tr::elem(sh.x, v_end);
-      const float t = fmaxf(warp_max(x_end * a.c2), -3e38f);
-      if (t > ref) {
-        R *= rescale2(ref - t);
-        ref = t;
-      }
-      R += warp_sum(v_end >= 0 ? ex2(fmaf(x_end, a.c2, -ref)) : 0.f);
+      top_ends(x_end, a.c2, ref, R);
       top = fmaxf(top, x_end);
       if (lane == 0) sm.crowded[parity ^ 1u] = sm.keys[parity ^ 1u] = 0;
     }
@@ -393,7 +452,7 @@ __global__ void __launch_bounds__(TR_NT, 3)
     sm.max[tid] = sorted;
     named_bar_sync(BAR_TOP, 32 * TR_NW);
     // ---- the bound: the k-th largest of the threads' maxima
-    join(lane < TR_NW ? sm.part[lane] : make_float2(-3e38f, 0.f), 1.f, ref, R);
+    top_join(lane < TR_NW ? sm.part[lane] : make_float2(-3e38f, 0.f), ref, R);
     {
       // the values before this lane's in each warp's list, of equal ones those of earlier warps
       int before = 0;
@@ -540,19 +599,18 @@ __global__ void __launch_bounds__(TR_NT, 3)
       cluster_sync_all();
     }
     if (rank == 0) {
-      if (C > 1) join(lane < (int)C ? sm.sums[lane] : make_float2(-3e38f, 0.f), 1.f, all.x, all.y);
+      if (C > 1) top_join(lane < (int)C ? sm.sums[lane] : make_float2(-3e38f, 0.f), all.x, all.y);
       // against the row's largest element
       uint64_t best = 0ull;
       for (uint32_t c = 0; c < C; ++c) best = max(best, C > 1 ? sm.lists[c][0] : sm.top[0]);
       const float K = best ? key_val(best) * a.c2 : -INFINITY;
-      const float rows_sum = all.y * rescale2(all.x - K);
       // (the border by the element itself: times c it is one with its neighbours)
       const bool bad = !best || !(key_val(best) < big) || !(all.y < INFINITY) || !(all.y >= 0.f);
-      const float log_sum = logf(rows_sum);
+      const float log_sum = top_log(all.x, all.y, K);
       auto give = [&](int j, uint64_t q) {
         out_ids[row * k + j] = bad || q == 0 ? -1 : (int32_t)key_idx(q);
         a.logp[row * k + j] =
-            bad ? NAN : q ? fmaf(key_val(q), a.c2, -K) * LN2 - log_sum : -INFINITY;
+            bad ? NAN : q ? top_logp(key_val(q), a.c2, K, log_sum) : -INFINITY;
       };
       if (C == 1) {
         if (tid < k) give(tid, mine);
@@ -671,17 +729,10 @@ __global__ void __launch_bounds__(32 * TS_MOST, 2)
         t3 = fmaxf(t3, m);
         t4 = fmaxf(t4, u);
       }
-      add_words<T>(ref, S, v, a.c2, w == 0);
+      top_words<T>(ref, S, v, a.c2, w == 0);
     }
-    join(make_float2(ref, S.x + S.y), 1.f, ref, R);
-    if (sh.head + sh.tail > 0) {
-      const float t = fmaxf(warp_max(x_end * a.c2), -3e38f);
-      if (t > ref) {
-        R *= rescale2(ref - t);
-        ref = t;
-      }
-      R += warp_sum(v_end >= 0 ? ex2(fmaf(x_end, a.c2, -ref)) : 0.f);
-    }
+    top_join(make_float2(ref, S.x + S.y), ref, R);
+    if (sh.head + sh.tail > 0) top_ends(x_end, a.c2, ref, R);
     int32_t* const ids = out_ids + row * k;
     float* const logp = a.logp + row * k;
     const float best = warp_max(t1), K = best * a.c2;
@@ -730,14 +781,14 @@ __global__ void __launch_bounds__(32 * TS_MOST, 2)
     if (sh.head + sh.tail > 0)
       l.push(v_end >= 0 && reaches(x_end), top_key(x_end, (uint32_t)v_end), lane);
     l.finish(lane);
-    const float log_sum = logf(R * rescale2(ref - K));
+    const float log_sum = top_log(ref, R, K);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const int j = 32 * h + lane;
       const uint64_t q = h == 0 ? l.hi : l.lo;
       if (j < k) {
         ids[j] = q ? (int32_t)key_idx(q) : -1;
-        logp[j] = q ? fmaf(key_val(q), a.c2, -K) * LN2 - log_sum : -INFINITY;
+        logp[j] = q ? top_logp(key_val(q), a.c2, K, log_sum) : -INFINITY;
       }
     }
     __syncwarp();  // every lane has read what the next row is written over

@@ -258,3 +258,26 @@ def test_the_border_of_infinity(B, ctx, n, V, temperature):
     ids, logp = B.pr_top_logits(ctx, x, 20, temperature=temperature)
     check(ids, logp, x, 20, temperature)
     assert B.pr_ctx_flags(ctx, clear=True) == B.PR_FLAG_NONFINITE
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,V", [(64, 151936), (16, 32003), (64, 1001), (1000, 4001), (700, 24001), (2, 6_500_001)])
+def test_sure_tokens(B, ctx, n, V, dtype):
+    """Rows of which one token, somewhere, has nearly all: its log-probability is never above 0, and as
+    near as a sum can be that holds it.  Its term is off by 2^-22 and by its exponent's rounding, of
+    up to 16 in size, 2^-21 ln 2; the factor between references by 2^-22; the sum's other roundings
+    are of terms below 2^-14 of it, but for those on the way through lanes, warps and CTAs, 13 of
+    2^-24, and the thread's own: 2^-24 for each of up to 160 chunks, random, 8 of them (four
+    deviations of their mean); the logarithm and its difference 2^-23 (|l| + 1).  The tokens
+    after it: the product's rounding as well, 4e-7 |l|."""
+    g = torch.Generator("cuda").manual_seed(V)
+    for up in (12.0, 17.0, 20.0, 24.0, 40.0):
+        x = torch.randn(n, V, generator=g, device="cuda").to(TYPES[dtype])
+        at = torch.randint(0, V, (n,), generator=g, device="cuda")
+        x[torch.arange(n, device="cuda"), at] = (up + 3 * torch.rand(n, generator=g, device="cuda")).to(x.dtype)
+        ids, logp = B.pr_top_logits(ctx, x, 3)
+        want = torch.log_softmax(x.double(), 1).gather(1, ids.long())
+        tol = (1.4 + 1 + 1) * 2.0 ** -22 + (13 + 8) * 2.0 ** -24 + 2.0 ** -23 + 5e-7 * want.abs()
+        off = (logp.double() - want).abs()
+        assert (off <= tol).all(), (up, float(off[:, 0].max()), float(off.max()))
+        assert (logp <= 0).all() and (up < 12.5 or torch.equal(ids[:, 0].long(), at))
