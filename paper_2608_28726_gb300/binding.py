@@ -860,7 +860,9 @@ def pr_layernorm(ctx, x, weight, bias=None, residual=None, eps: float = 1e-5, rm
     if total is not None or (residual is not None and want_total):
         total, t_p, ts = _norm_out(call, dev, "total", total, x)
     mean_p = rstd_p = None
-    if mean is not None or (want_stats and not rms):
+    if rms:
+        mean = None  # (not written)
+    elif mean is not None or want_stats:
         mean, mean_p = _loss_out(call, dev, "mean", mean, n, x.device)
     if rstd is not None or want_stats:
         rstd, rstd_p = _loss_out(call, dev, "rstd", rstd, n, x.device)

@@ -375,3 +375,11 @@ def test_backward_of_many_rows_of_three_words_a_thread(B, ctx, n, d, dtype):
     """513 to 768 words a row, two rows on an SM or one."""
     test_backward_sizes(B, ctx, n, d, dtype)
     test_outputs_in_place_of_inputs(B, ctx, n, d, dtype)
+
+
+def test_rms_norm_has_no_mean(B, ctx):
+    x, r, w, b, _ = draw(3, 5, 96, "f32")
+    mean = torch.full((5,), 7.0, device="cuda")
+    got = B.pr_layernorm(ctx, x, w, bias=b, rms=True, mean=mean)
+    assert got[2] is None and (mean == 7).all()
+    check_forward((got[0], None, got[3]), x, w, b, 1e-5, True, "f32")
