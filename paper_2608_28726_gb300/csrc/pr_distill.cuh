@@ -605,7 +605,7 @@ __device__ __forceinline__ void add_rest_ends(const DistillArgs& d, const Share&
   if (s.head + s.tail == 0) return;
   const float c2 = d.a.c2;
   const bool add = v >= 0 && kind == DS_REST;
-  const float top = warp_max(add ? fmaxf(edge * c2, -3e38f) : -3e38f);
+  const float top = warp_max(add ? fmaxf(edge * c2, LOWEST_REF) : LOWEST_REF);
   if (top > k) {
     R *= rescale2(k - top);
     k = top;
@@ -942,7 +942,7 @@ __global__ void __launch_bounds__(RG_NT, 2)
                 if (w + 32 * RG_NW * q + at >= sh.w1)
                   v[q] = make_uint4(Tr::NEG_WORD, Tr::NEG_WORD, Tr::NEG_WORD, Tr::NEG_WORD);
             }
-            add_words<T>(k, S, v, a.c2, w == sh.w0);
+            add_words<T>(k, S, v, a.c2, w == sh.w0, LOWEST_REF);
             if (!HOLD) {
               // The place is given back once every lane's words are in its sum: given back right
               // after their loads, with a chunk's listed tokens just left out, one row in 2,000
@@ -1115,7 +1115,7 @@ __global__ void __launch_bounds__(32 * RW_MOST, 2)
         x[q] = w + 32 * q + lane < sh.words
                    ? st[w + 32 * q]
                    : make_uint4(Tr::NEG_WORD, Tr::NEG_WORD, Tr::NEG_WORD, Tr::NEG_WORD);
-      add_words<T>(k, S, x, a.c2, w == 0);
+      add_words<T>(k, S, x, a.c2, w == 0, LOWEST_REF);
     }
     join(make_float2(k, S.x + S.y), 1.f, k, R);
     add_rest_ends(d, sh, wide<T>(in.edge), v, kind, k, R);

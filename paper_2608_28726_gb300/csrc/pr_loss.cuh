@@ -456,6 +456,10 @@ struct RowEnd {
   }
 };
 
+// The lowest reference of sums that leave out what is masked by x / T <= -1e9 (c x about -1.44e9).  A
+// reference among masked values would not do: c x of -1e30 is rounded by 1e22, and 2^1e22 is infinite.
+constexpr float LOWEST_REF = -1.5e9f;
+
 // What a row's backward sweep needs: entries nk 2^(c x - K) (FAST), nk 2^(c (x - M) - K)
 // (ROBUST) or 0; gy at the emitted token.
 enum RowMode { ROW_ZERO = 0, ROW_FAST = 1, ROW_ROBUST = 2 };
@@ -782,15 +786,16 @@ __device__ __forceinline__ void raise_to(const LossArgs& a, float xy, float& M, 
 // A thread's words into its sum (k, S); the row's first ones give k.  They are summed by
 // themselves first: one by one, the many terms below 2^-25 of S would all be lost (rows of
 // V = 262,144 whose logits spread by 4: l 1e-7 too high on average, now 1e-8).
+// least: the lowest reference.
 template <typename T, int N>
 __device__ __forceinline__ void add_words(float& k, float2& S, const uint4 (&v)[N], float c2,
-                                          bool begin) {
+                                          bool begin, float least = -3e38f) {
   using Tr = Traits<T>;
   auto top = [&]() {
     float m = Tr::gmax(v[0]);
 #pragma unroll
     for (int q = 1; q < N; ++q) m = fmaxf(m, Tr::gmax(v[q]));
-    return fmaxf(m * c2, -3e38f);
+    return fmaxf(m * c2, least);
   };
   if (begin) k = top();
   float2 here = make_float2(0.f, 0.f);

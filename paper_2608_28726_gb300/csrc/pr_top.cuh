@@ -138,7 +138,7 @@ __device__ __forceinline__ void top_words(float& k, float2& S, const uint4 (&v)[
     float m = Tr::gmax(v[0]);
 #pragma unroll
     for (int q = 1; q < N; ++q) m = fmaxf(m, Tr::gmax(v[q]));
-    return rintf(fmaxf(m * c2, -3e38f));
+    return rintf(fmaxf(m * c2, LOWEST_REF));
   };
   if (begin) k = top();
   float2 here = make_float2(0.f, 0.f);
@@ -164,7 +164,7 @@ __device__ __forceinline__ void top_join(float2 q, float& k, float& R) {
 
 // The elements of the lanes that have one (x, else -inf), at a row's ends, into its sum
 __device__ __forceinline__ void top_ends(float x, float c2, float& k, float& R) {
-  const float t = fmaxf(warp_max(rintf(x * c2)), -3e38f);
+  const float t = fmaxf(warp_max(rintf(x * c2)), LOWEST_REF);
   if (t > k) {
     R *= top_scale(k - t);
     k = t;
@@ -197,7 +197,7 @@ __global__ void __launch_bounds__(TP_NT) top_rows(const TopArgs a, const int64_t
   const int64_t row = blockIdx.x;
   const T* x = reinterpret_cast<const T*>(a.logits) + row * a.row_stride;
   const int groups = (int)((a.vocab + group - 1) / group);
-  float k = -3e38f, S = 0.f, best = -INFINITY;
+  float k = LOWEST_REF, S = 0.f, best = -INFINITY;
   for (int g = tid; g < groups; g += TP_NT) {
     const int64_t v0 = g * group, v1 = min(a.vocab, v0 + group);
     float m = -INFINITY;

@@ -578,3 +578,33 @@ def test_gradients_of_rows_that_rise(B, ctx, n, V, rise, dtype):
             tol += 1e-14 * size.max(axis=1, keepdims=True)
             bad = ~(np.abs(grad - go) <= tol)
             assert not bad.any(), (scale, loss, bad.sum(), grad[bad][:4], go[bad][:4], tol[bad][:4])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,V", [(5, 7), (6, 1003), (6, 40000), (700, 1003), (620, 12011)])
+def test_masks_of_any_size(B, ctx, n, V, dtype):
+    """What is masked by a large negative number is no part of a row, at any temperature: also where
+    nothing else is near."""
+    k = 4
+    g, x0, _, ids, sent, ch = draw(V, n, V, k, dtype)
+    r = np.random.Generator(np.random.PCG64(V))
+    hide = r.random((n, V)) < 0.97
+    hide[0, : V - 2], hide[1, 2:] = True, True
+    hide[0, V - 2:], hide[1, :2], hide[2:, V // 2] = False, False, False
+    ch = np.where(np.arange(n) == 0, V - 1, np.where(np.arange(n) == 1, 0, V // 2)).astype(np.int32)
+    hide_t = to(hide)
+    for low in ("lowest", -1e38, -2.3e38, -1e30, -7e20, -1e12, -6e9):
+        x = x0.masked_fill(hide_t, torch.finfo(x0.dtype).min if low == "lowest" else low)
+        x64 = x.double().cpu().numpy()
+        for T, loss, rest in ((1.0, 0, 0), (1.7, 1, 0), (2.0, 0, 1), (5.0, 0, 0), (5.0, 1, 1)):
+            B.pr_ctx_flags(ctx, clear=True)
+            some = None
+            if loss and rest:  # a row whose whole list is masked is NaN by right
+                at = np.maximum(ids, 0)
+                listed = (ids >= 0) & (sent > -np.inf)
+                left = (listed & (np.take_along_axis(x64, at, 1) > -1e9 * T)).any(1) | ~listed.any(1)
+                some = left.astype(np.uint8)
+            got, want = both(B, ctx, x, x64, ids, sent, ch, some, None, dtype, loss=loss, rest=rest,
+                             temperature=T, ce_coef=0.2)
+            assert not got[1].isnan().any() and not got[2].isnan().any(), (low, T, loss, rest)
+            assert B.pr_ctx_flags(ctx, clear=True) == 0

@@ -281,3 +281,40 @@ def test_sure_tokens(B, ctx, n, V, dtype):
         off = (logp.double() - want).abs()
         assert (off <= tol).all(), (up, float(off[:, 0].max()), float(off.max()))
         assert (logp <= 0).all() and (up < 12.5 or torch.equal(ids[:, 0].long(), at))
+
+
+MASKS = ["lowest", -1e38, -2.3e38, -1e30, -7e20, -1e12, -3e9]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,V", [(5, 7), (6, 1003), (6, 40000), (1000, 1003), (700, 24001), (2, 6_500_001)])
+def test_masks_of_any_size(B, ctx, n, V, dtype):
+    """What is masked by a large negative number is no part of a row, at any temperature: also where
+    nothing else is near."""
+    g = torch.Generator("cuda").manual_seed(V)
+    for mask in MASKS:
+        x = torch.randn(n, V, generator=g, device="cuda").to(TYPES[dtype])
+        low = torch.finfo(x.dtype).min if mask == "lowest" else mask
+        x[0, : V - 2] = low
+        x[1, 2:] = low
+        hide = torch.rand(n, V, generator=g, device="cuda") < 0.97
+        hide[:2] = False
+        hide[:, V // 2] = False
+        x = x.masked_fill(hide, low)
+        if n > 3:
+            x[3] = low                      # nothing left
+        for T in (1e-3, 0.5, 1.0, 1.7, 2.0, 5.0, 100.0):
+            B.pr_ctx_flags(ctx, clear=True)
+            xt = torch.where(x > -1e3, (x.double() * T).to(x.dtype), x) if T < 1 else x
+            ids, logp = B.pr_top_logits(ctx, xt, 5, temperature=T)
+            masked = xt.double() <= -float(torch.tensor(1e9 * T, dtype=torch.float32))
+            z = (xt.double() / T).masked_fill(masked, -torch.inf)
+            top, at = torch.sort(z, dim=1, descending=True, stable=True)
+            top, at = top[:, :5], at[:, :5].masked_fill(torch.isinf(top[:, :5]), -1)
+            assert torch.equal(ids.long(), at), (mask, T)
+            want = top - torch.logsumexp(z, 1, keepdim=True)
+            off = (logp.double() - want).abs()
+            ok = (off <= 2e-5 + 4e-7 * want.abs()) | (logp == want) | (logp.isnan() & want.isnan())
+            assert ok.all(), (mask, T)
+            none = bool(masked.all(1).any())
+            assert B.pr_ctx_flags(ctx, clear=True) == (B.PR_FLAG_NONFINITE if none else 0)
