@@ -172,8 +172,8 @@ __device__ __forceinline__ void top_ends(float x, float c2, float& k, float& R) 
   R += warp_sum(x > -INFINITY || x != x ? ex2(fmaf(x, c2, -k)) : 0.f);
 }
 
-// ln of the sum R against 2^k, against 2^K; an element of exponent u against 2^K from it.  (In
-// fp32 the sum of a row that is one token may come out below its term.)
+// ln of the sum, R against 2^k, in units of 2^K; an element's log-probability from it.  (In fp32
+// the sum of a row that is one token may come out below its term.)
 __device__ __forceinline__ float top_log(float k, float R, float K) { return logf(R * exp2f(k - K)); }
 __device__ __forceinline__ float top_logp(float x, float c2, float K, float log_sum) {
   return fminf(fmaf(x, c2, -K) * LN2 - log_sum, 0.f);
